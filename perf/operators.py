@@ -203,7 +203,7 @@ def prepare(case, seed):
             n, k = case["rows"], case["top_k"]
             # what the forward pass left, and the gradients that reach it
             f = _logprobs(s["logits"], s["tokens"], k, s["row_scale"], s["allowed"])
-            s.update(lse=f["lse"], entropy=f["entropy"], top_idx=f.get("top_idx"))
+            s.update(stats=f["stats"], entropy=f["entropy"], top_idx=f.get("top_idx"))
             s["grad_logprobs"] = normal(n, case["tokens"]) / n
             s["grad_top"] = 0.1 * normal(n, k) / n if k else None
             s["grad_entropy"] = 0.1 * normal(n) / n
@@ -278,16 +278,16 @@ def _plain_scaled(logits, row_scale, allowed):
 def _logprobs(logits, tokens, k, row_scale, allowed):
     x, z = _plain_scaled(logits, row_scale, allowed)
     m = z.amax(-1, keepdim=True)
-    shift = torch.where(m == -math.inf, 0.0, m)         # a row without tokens
-    e = torch.exp(z - shift)
+    none = m == -math.inf                               # a row without tokens
+    z = z - torch.where(none, 0.0, m)
+    e = torch.exp(z)
     total = e.sum(-1, keepdim=True)
-    lse = torch.log(total) + shift
-    safe = torch.where(m == -math.inf, 0.0, lse)
-    lp = z - safe
+    log_sum = torch.log(total)
+    lp = z - torch.where(none, 0.0, log_sum)
     entropy = -torch.where(e > 0, e / total * lp, 0.0).sum(-1)
     at = tokens.long()
     given = torch.where(at >= 0, lp.gather(1, at.clamp(min=0)), 0.0)
-    out = dict(logprobs=given, lse=lse[:, 0], entropy=entropy)
+    out = dict(logprobs=given, lse=(m + log_sum)[:, 0], entropy=entropy, stats=torch.cat((m, log_sum), 1))
     if k:
         # distinct keys: the logit's bits in order, then the lower token first
         bits = (x + 0.0).view(torch.int32).long()
@@ -302,8 +302,8 @@ def _logprobs(logits, tokens, k, row_scale, allowed):
 
 def _plain_grad(s):
     _, z = _plain_scaled(s["logits"], s["row_scale"], s["allowed"])
-    lse = s["lse"][:, None]
-    lp = z - torch.where(lse == -math.inf, 0.0, lse)
+    stats = torch.where(s["stats"] == -math.inf, 0.0, s["stats"])
+    lp = (z - stats[:, :1]) - stats[:, 1:]
     p = torch.exp(lp)
     at, g = s["tokens"].long(), s["grad_logprobs"]
     if s["grad_top"] is not None:
@@ -339,7 +339,7 @@ def run(s):
         if kind == "logprobs":
             return fovea.token_logprobs(s["logits"], s["tokens"], case["top_k"], row_scale=s["row_scale"],
                                         allowed=s["allowed"])
-        return fovea.token_logprobs_grad(s["logits"], s["lse"], s["entropy"], tokens=s["tokens"],
+        return fovea.token_logprobs_grad(s["logits"], s["stats"], s["entropy"], tokens=s["tokens"],
                                          grad_logprobs=s["grad_logprobs"], top_idx=s["top_idx"],
                                          grad_top=s["grad_top"], grad_entropy=s["grad_entropy"],
                                          grad_lse=s["grad_lse"], row_scale=s["row_scale"], allowed=s["allowed"])
@@ -403,7 +403,7 @@ def _exact_linear(s, case):
 
 
 def _exact_rows(s, r0, r1):
-    """Scaled logits of some rows in 64 bits, -inf where not allowed, with their log sum and entropy."""
+    """Some rows' logits in 64 bits (-inf where not allowed), logp, p, lse, (largest, log sum) and entropy."""
     x = s["logits"][r0:r1].double()
     if s["allowed"] is not None:
         words = s["allowed"][r0:r1].long() & 0xFFFFFFFF
@@ -413,16 +413,18 @@ def _exact_rows(s, r0, r1):
     lse = torch.logsumexp(z, 1)
     lp = z - lse.nan_to_num(neginf=0.0)[:, None]
     p = lp.exp()
-    return x, lp, p, lse, -(p * lp.clamp(min=-1e300)).sum(1)
+    top = z.max(1).values
+    stats = torch.stack((top, lse - top.nan_to_num(neginf=0.0)), 1)
+    return x, lp, p, lse, stats, -(p * lp.clamp(min=-1e300)).sum(1)
 
 
 def _exact_scores(s, case):
     got = []
     step = max(1, (1 << 25) // case["vocab"])
     for r in range(0, case["rows"], step):
-        x, lp, p, lse, entropy = _exact_rows(s, r, r + step)
+        x, lp, _, lse, stats, entropy = _exact_rows(s, r, r + step)
         t = s["tokens"][r:r + step].long()
-        o = dict(logprobs=lp.gather(1, t.clamp(min=0)).masked_fill(t < 0, 0.0), lse=lse, entropy=entropy)
+        o = dict(logprobs=lp.gather(1, t.clamp(min=0)).masked_fill(t < 0, 0.0), lse=lse, stats=stats, entropy=entropy)
         if case["top_k"]:
             order = x.sort(dim=1, descending=True, stable=True).indices[:, :case["top_k"]]
             o["top_logprobs"] = lp.gather(1, order)
@@ -436,7 +438,7 @@ def _exact_grad(s, case):
     got = []
     step = max(1, (1 << 25) // case["vocab"])
     for r in range(0, case["rows"], step):
-        _, lp, p, _, entropy = _exact_rows(s, r, r + step)
+        _, lp, p, _, _, entropy = _exact_rows(s, r, r + step)
         dz = p * s["grad_lse"][r:r + step].double()[:, None]
         dz -= s["grad_entropy"][r:r + step].double()[:, None] * p * (lp.clamp(min=-1e300) + entropy[:, None])
         pairs = [(s["tokens"], s["grad_logprobs"])]
