@@ -317,6 +317,144 @@ FOVEA_API fovea_status fovea_lm_head_topk(const void* W_LM, int vocab, int d_mod
 FOVEA_API fovea_status fovea_lm_head_workspace_size(int vocab, int d_model, int N, int k_c,
                                                     size_t* bytes);
 
+/*
+ * Operators of the drafter's exit
+ * -------------------------------
+ * What stands between a drafter's last block and the tokens of its tree, for
+ * weights held in 4 bits: the residual's addition with an RMS norm and an 8-bit
+ * output, the making of 4-bit weights, their product with a few rows, the log
+ * probabilities of tokens and their gradient.  (The paper's own path ends in
+ * bf16: RMSNorm inside fovea_retrieve_fuse, then fovea_lm_head_topk.)
+ *
+ * Unlike the tensors of the entry points above, x, residual, W and logits here
+ * need only be contiguous along their rows: each has a row stride `ld` in
+ * elements (>= its row length), and pointers aligned to their element.  Outputs
+ * are dense.  None of these calls allocates, needs a workspace or synchronises;
+ * all enqueue on `stream` and can be captured.  N = 0 is valid and does nothing.
+ * Errors: INVALID_ARG, UNSUPPORTED (nothing enqueued), CUDA.
+ */
+#define FOVEA_E4M3 2                /* 8-bit float rows (x of fovea_linear_w4) */
+#define FOVEA_MAX_IN 32768          /* columns of a 4-bit matrix */
+#define FOVEA_MAX_TOKENS 1024       /* given tokens per row */
+
+/*
+ * s = x + residual, y = s / sqrt(mean(s^2) + eps) * gamma per row of d columns,
+ * and y in 8 bits: q8 = e4m3(y / scale), scale = max |y| / 448 over the row
+ * (q8_group 0) or over each q8_group consecutive columns (32, 64 or 128; the
+ * last group may be shorter); where scale is 0, q8 is 0.  The norm and q8 follow
+ * from the unrounded fp32 sum.  A row that holds a NaN or an infinity gives NaN
+ * scales and NaN in y where s is not finite.
+ *   x, residual [N, d] dtype (residual NULL: s = x); gamma [d] dtype
+ *   sum         [N, d] dtype: s, or NULL; may be x or residual when that is dense
+ *   out         [N, d] dtype: y, or NULL
+ *   q8          [N, d] e4m3 bytes, or NULL; then q8_scale [N, ceil(d / q8_group)]
+ *               ([N] for q8_group 0) fp32 is written
+ * dtype FOVEA_BF16 or FOVEA_FP32; 1 <= d <= FOVEA_MAX_D; eps > 0.
+ */
+FOVEA_API fovea_status fovea_add_rms_norm(const void* x, int64_t x_ld, const void* residual,
+                                          int64_t residual_ld, const void* gamma, int N, int d,
+                                          int dtype, float eps, void* sum, void* out, void* q8,
+                                          float* q8_scale, int q8_group, void* stream);
+
+/*
+ * W [out_features, in_features] in 4 bits, w ~ (code - zero) * scale with a
+ * scale (and a zero point) per `group` consecutive columns of a row (32, 64 or
+ * 128; the last group may be shorter):
+ *   zeros NULL (symmetric):  scale = bf16(max|w| / 7), zero = 8,
+ *                            code = clamp(round(w / scale), -8, 7) + 8
+ *   zeros given:             lo = min(0, min w), hi = max(0, max w),
+ *                            scale = bf16((hi - lo) / 15),
+ *                            zero = clamp(round(-lo / scale), 0, 15),
+ *                            code = clamp(round(w / scale) + zero, 0, 15)
+ * rounding to nearest even; where scale is 0, code and zero are 8.  A group
+ * that holds a NaN gets a NaN scale.
+ *   codes  [out_features, in_features / 2] bytes (4-byte aligned), the even
+ *          column of a pair in the low four bits
+ *   scales [out_features, groups] bf16, zeros [out_features, groups] bytes,
+ *          groups = ceil(in_features / group)
+ * in_features a multiple of 32, <= FOVEA_MAX_IN.
+ */
+FOVEA_API fovea_status fovea_quantize_w4(const void* W, int64_t ld, int out_features,
+                                         int in_features, int dtype, int group, void* codes,
+                                         void* scales, void* zeros, void* stream);
+
+/*
+ * y[n, o] = sum_k x[n, k] (code[o, k] - zero[o, k / group]) scale[o, k / group]
+ * (+ bias[o]) for a few rows of x (a draft tree's states): weights as
+ * fovea_quantize_w4 lays them out (codes 16-byte aligned; zeros NULL: 8).
+ *   x       [N, in_features] x_dtype: FOVEA_BF16, FOVEA_FP32, or FOVEA_E4M3 with
+ *   x_scale [N, groups] fp32 for x_group = group, or [N] for x_group = 0 (as
+ *           fovea_add_rms_norm writes q8 and q8_scale); NULL for the others
+ *   bias    [out_features] fp32, or NULL
+ *   y       [N, out_features] y_dtype: FOVEA_FP32 or FOVEA_BF16
+ * Products and sums of a group are exact up to fp32 accumulation (an fp32 x
+ * counts with all its bits); y is rounded once.
+ */
+FOVEA_API fovea_status fovea_linear_w4(const void* x, int64_t x_ld, int x_dtype,
+                                       const float* x_scale, int x_group, int N, const void* codes,
+                                       const void* scales, const void* zeros, const float* bias,
+                                       int out_features, int in_features, int group, void* y,
+                                       int y_dtype, void* stream);
+
+/*
+ * Scores of tokens under the softmax of each row of logits: with z = logit *
+ * row_scale over the row's allowed tokens,
+ *   lse = log sum e^z, logp = z - lse, entropy = -sum p logp,
+ * and the top_k tokens with the largest logits, ties broken by the smaller token.
+ *   logits       [N, vocab] dtype (FOVEA_BF16 or FOVEA_FP32), row stride ld
+ *   row_scale    [N] fp32 inverse temperatures, finite and > 0, or NULL (1)
+ *   allowed      [N, ceil(vocab / 32)] 32-bit words (row stride allowed_ld words;
+ *                0: one mask for every row), token i allowed when bit i % 32 of
+ *                word i / 32 is set; NULL: every token.  What stands in the place
+ *                of a token that is not allowed is not used, whatever it is.
+ *   tokens       [N, n_tokens] int32: -1 (or any negative) for none, whose logp is
+ *                0; a token >= vocab gives NaN
+ *   logprobs     [N, n_tokens] fp32
+ *   lse, entropy [N] fp32; stats [N, 2] fp32: the largest z and log sum e^(z - it)
+ *                (what the gradient needs: lse alone loses the second where |z| is
+ *                large)
+ *   top_idx      [N, top_k] int32, top_logprobs [N, top_k] fp32
+ * A token that is not allowed, or whose z is -inf, has logp -inf and is no
+ * alternative: with fewer than top_k others the last top_idx are -1, their logp
+ * -inf.  A row without any token left has lse -inf and entropy 0.  A NaN or +inf
+ * among the allowed logits makes the row's probabilities NaN (alternatives: NaN
+ * first, then +inf).
+ * 0 <= n_tokens <= FOVEA_MAX_TOKENS, 0 <= top_k <= FOVEA_MAX_KC; 1 <= vocab <= 2^24.
+ */
+FOVEA_API fovea_status fovea_token_logprobs(const void* logits, int64_t ld, int N, int vocab,
+                                            int dtype, const float* row_scale,
+                                            const int32_t* allowed, int64_t allowed_ld,
+                                            const int32_t* tokens, int n_tokens, int top_k,
+                                            float* logprobs, float* lse, float* entropy,
+                                            float* stats, int32_t* top_idx, float* top_logprobs,
+                                            void* stream);
+
+/*
+ * The gradient of fovea_token_logprobs with respect to the logits, from the
+ * gradients of its outputs (row_scale and allowed as in that call; stats,
+ * entropy and top_idx as it wrote them):
+ *   dlogit_i = row_scale * (sum over tokens and alternatives equal to i of their
+ *              gradients - p_i G - grad_entropy p_i (logp_i + entropy)
+ *              + grad_lse p_i),
+ * G the sum of the gradients of the row's counted tokens and alternatives (those
+ * that are none or have probability 0 do not count; a token >= vocab makes the
+ * row NaN).  Tokens that are not allowed get 0, and so does a row without tokens.
+ *   grad_logprobs [N, n_tokens], grad_top [N, top_k], grad_entropy [N],
+ *                 grad_lse [N], all fp32; the last two may be NULL (0)
+ *   dlogits       [N, vocab] dtype, dense; may be logits themselves when ld = vocab
+ * A token given more than once takes the sum in the order given: the result does
+ * not vary from run to run.
+ */
+FOVEA_API fovea_status fovea_token_logprobs_grad(const void* logits, int64_t ld, int N, int vocab,
+                                                 int dtype, const float* row_scale,
+                                                 const int32_t* allowed, int64_t allowed_ld,
+                                                 const float* stats, const float* entropy,
+                                                 const int32_t* tokens, const float* grad_logprobs,
+                                                 int n_tokens, const int32_t* top_idx,
+                                                 const float* grad_top, int top_k,
+                                                 const float* grad_entropy, const float* grad_lse,
+                                                 void* dlogits, void* stream);
+
 /* Synchronise `stream`, read and clear the workspace's sticky error word.
  * Returns FOVEA_OK, FOVEA_ERR_INVALID_ARG (a depth outside [0, D] was seen)
  * or FOVEA_ERR_TIMEOUT (a bounded device wait gave up), or FOVEA_ERR_CUDA.

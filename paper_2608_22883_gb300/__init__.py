@@ -6,6 +6,7 @@ include/fovea.h); ``fovea`` is its thin Python binding.
 
 from . import fovea  # noqa: F401
 from .fovea import (  # noqa: F401
-    BF16, FP32, FoveaError, Memory, Params, build_memory, new_workspace, retrieve_fuse,
-    step, sync_errors, timing_enable, timing_read, workspace_size,
+    BF16, E4M3, FP32, FoveaError, Memory, Params, add_rms_norm, build_memory, linear_w4,
+    new_workspace, quantize_w4, retrieve_fuse, step, sync_errors, timing_enable, timing_read,
+    token_logprobs, token_logprobs_grad, workspace_size,
 )

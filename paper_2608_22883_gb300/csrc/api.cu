@@ -1252,6 +1252,235 @@ FOVEA_API fovea_status fovea_lm_head_workspace_size(int vocab, int d_model, int 
   return FOVEA_OK;
 }
 
+// ---------------------------------------------------------------------------
+// Operators of the drafter's exit
+// ---------------------------------------------------------------------------
+
+// A pointer of the operators below: present and aligned to `align` bytes.
+#define NEED_ALIGNED(ptr, align, name)                                                  \
+  do {                                                                                  \
+    if ((ptr) == nullptr) return fail(FOVEA_ERR_INVALID_ARG, "%s is NULL", name);       \
+    WANT_ALIGNED(ptr, align, name);                                                     \
+  } while (0)
+#define WANT_ALIGNED(ptr, align, name)                                                  \
+  do {                                                                                  \
+    if ((reinterpret_cast<uintptr_t>(ptr) & ((align) - 1)) != 0)                        \
+      return fail(FOVEA_ERR_INVALID_ARG, "%s is not %d-byte aligned", name, (int)(align)); \
+  } while (0)
+#define NEED_ROWS(N, ld, cols, name)                                                    \
+  do {                                                                                  \
+    if ((N) < 0) return fail(FOVEA_ERR_INVALID_ARG, "N = %d < 0", N);                   \
+    if ((N) > 1 && (ld) < (cols))                                                       \
+      return fail(FOVEA_ERR_INVALID_ARG, "row stride %lld of %s is below its %d columns", \
+                  (long long)(ld), name, cols);                                         \
+  } while (0)
+
+static fovea_status check_dtype(int dtype) {
+  if (dtype != FOVEA_BF16 && dtype != FOVEA_FP32)
+    return fail(FOVEA_ERR_INVALID_ARG, "dtype %d is neither FOVEA_BF16 nor FOVEA_FP32", dtype);
+  return FOVEA_OK;
+}
+static fovea_status check_w4(int out_features, int in_features, int group) {
+  if (out_features < 1) return fail(FOVEA_ERR_INVALID_ARG, "out_features = %d < 1", out_features);
+  if (in_features < 32 || in_features % 32 != 0)
+    return fail(FOVEA_ERR_INVALID_ARG, "in_features %d must be a positive multiple of 32", in_features);
+  if (in_features > FOVEA_MAX_IN)
+    return fail(FOVEA_ERR_UNSUPPORTED, "in_features %d > %d", in_features, FOVEA_MAX_IN);
+  if (group != 32 && group != 64 && group != 128)
+    return fail(FOVEA_ERR_INVALID_ARG, "group %d is not 32, 64 or 128", group);
+  return FOVEA_OK;
+}
+
+FOVEA_API fovea_status fovea_add_rms_norm(const void* x, int64_t x_ld, const void* residual,
+                                          int64_t residual_ld, const void* gamma, int N, int d,
+                                          int dtype, float eps, void* sum, void* out, void* q8,
+                                          float* q8_scale, int q8_group, void* stream) {
+  g_last_error.clear();
+  fovea_status st = check_dtype(dtype);
+  if (st != FOVEA_OK) return st;
+  if (d < 1) return fail(FOVEA_ERR_INVALID_ARG, "d = %d < 1", d);
+  if (d > FOVEA_MAX_D) return fail(FOVEA_ERR_UNSUPPORTED, "d %d > %d", d, FOVEA_MAX_D);
+  if (!(eps > 0.0f)) return fail(FOVEA_ERR_INVALID_ARG, "eps must be > 0");
+  if (q8_group != 0 && q8_group != 32 && q8_group != 64 && q8_group != 128)
+    return fail(FOVEA_ERR_INVALID_ARG, "q8_group %d is not 0, 32, 64 or 128", q8_group);
+  NEED_ROWS(N, x_ld, d, "x");
+  if (residual != nullptr) NEED_ROWS(N, residual_ld, d, "residual");
+  const int size = dtype == FOVEA_BF16 ? 2 : 4;
+  NEED_ALIGNED(gamma, size, "gamma");
+  WANT_ALIGNED(residual, size, "residual");
+  WANT_ALIGNED(sum, size, "sum");
+  WANT_ALIGNED(out, size, "out");
+  if (N == 0) return FOVEA_OK;
+  if (sum == nullptr && out == nullptr && q8 == nullptr)
+    return fail(FOVEA_ERR_INVALID_ARG, "sum, out and q8 are all NULL");
+  if (q8 != nullptr) NEED_ALIGNED(q8_scale, 4, "q8_scale");
+  NEED_ALIGNED(x, size, "x");
+  NormArgs a{};
+  a.x = x; a.residual = residual; a.gamma = gamma;
+  a.x_ld = x_ld; a.residual_ld = residual != nullptr ? residual_ld : 0;
+  a.N = N; a.d = d; a.eps = eps;
+  a.sum = sum; a.out = out;
+  a.q8 = static_cast<uint8_t*>(q8); a.q8_scale = q8_scale; a.q8_group = q8_group;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KernelTimer t("add_rms_norm", s);
+  FOVEA_CUDA(launch_add_rms_norm(dtype, a, s), "add_rms_norm");
+  return FOVEA_OK;
+}
+
+FOVEA_API fovea_status fovea_quantize_w4(const void* W, int64_t ld, int out_features,
+                                         int in_features, int dtype, int group, void* codes,
+                                         void* scales, void* zeros, void* stream) {
+  g_last_error.clear();
+  fovea_status st = check_dtype(dtype);
+  if (st == FOVEA_OK) st = check_w4(out_features, in_features, group);
+  if (st != FOVEA_OK) return st;
+  NEED_ROWS(out_features, ld, in_features, "W");
+  NEED_ALIGNED(W, dtype == FOVEA_BF16 ? 2 : 4, "W");
+  NEED_ALIGNED(codes, 4, "codes");
+  NEED_ALIGNED(scales, 2, "scales");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KernelTimer t("quantize_w4", s);
+  FOVEA_CUDA(launch_quantize_w4(dtype, W, ld, out_features, in_features, group,
+                                static_cast<uint8_t*>(codes), static_cast<__nv_bfloat16*>(scales),
+                                static_cast<uint8_t*>(zeros), s), "quantize_w4");
+  return FOVEA_OK;
+}
+
+FOVEA_API fovea_status fovea_linear_w4(const void* x, int64_t x_ld, int x_dtype,
+                                       const float* x_scale, int x_group, int N, const void* codes,
+                                       const void* scales, const void* zeros, const float* bias,
+                                       int out_features, int in_features, int group, void* y,
+                                       int y_dtype, void* stream) {
+  g_last_error.clear();
+  if (x_dtype != FOVEA_BF16 && x_dtype != FOVEA_FP32 && x_dtype != FOVEA_E4M3)
+    return fail(FOVEA_ERR_INVALID_ARG, "x_dtype %d is not FOVEA_BF16, FOVEA_FP32 or FOVEA_E4M3", x_dtype);
+  fovea_status st = check_dtype(y_dtype);
+  if (st == FOVEA_OK) st = check_w4(out_features, in_features, group);
+  if (st != FOVEA_OK) return st;
+  NEED_ROWS(N, x_ld, in_features, "x");
+  if (x_dtype != FOVEA_E4M3 && x_scale != nullptr)
+    return fail(FOVEA_ERR_INVALID_ARG, "x_scale is for e4m3 rows only");
+  if (x_dtype == FOVEA_E4M3 && x_group != 0 && x_group != group)
+    return fail(FOVEA_ERR_INVALID_ARG, "x_group %d is neither 0 nor the weights' group %d", x_group, group);
+  NEED_ALIGNED(codes, 16, "codes");
+  NEED_ALIGNED(scales, 2, "scales");
+  WANT_ALIGNED(bias, 4, "bias");
+  if (N == 0) return FOVEA_OK;
+  NEED_ALIGNED(x, x_dtype == FOVEA_BF16 ? 2 : x_dtype == FOVEA_FP32 ? 4 : 1, "x");
+  if (x_dtype == FOVEA_E4M3) NEED_ALIGNED(x_scale, 4, "x_scale");
+  NEED_ALIGNED(y, y_dtype == FOVEA_BF16 ? 2 : 4, "y");
+  LinearW4Args a{};
+  a.w = W4{static_cast<const uint8_t*>(codes), static_cast<const __nv_bfloat16*>(scales),
+           static_cast<const uint8_t*>(zeros), out_features, in_features, group};
+  a.x = x; a.x_ld = x_ld; a.x_dtype = x_dtype;
+  a.x_scale = x_scale; a.x_group = x_dtype == FOVEA_E4M3 ? x_group : 0;
+  a.bias = bias;
+  a.y = y; a.y_dtype = y_dtype;
+  a.N = N;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KernelTimer t("linear_w4", s);
+  FOVEA_CUDA(launch_linear_w4(a, s), "linear_w4");
+  return FOVEA_OK;
+}
+
+// What both score calls ask of the logits, the mask and the tokens.
+static fovea_status check_scores(const void* logits, int64_t ld, int N, int vocab, int dtype,
+                                 const float* row_scale, const int32_t* allowed, int64_t allowed_ld,
+                                 const int32_t* tokens, int n_tokens, int top_k) {
+  const fovea_status st = check_dtype(dtype);
+  if (st != FOVEA_OK) return st;
+  if (vocab < 1) return fail(FOVEA_ERR_INVALID_ARG, "vocab = %d < 1", vocab);
+  if (vocab > 1 << 24) return fail(FOVEA_ERR_UNSUPPORTED, "vocab %d > 2^24", vocab);
+  if (n_tokens < 0 || top_k < 0)
+    return fail(FOVEA_ERR_INVALID_ARG, "n_tokens %d and top_k %d must not be negative", n_tokens, top_k);
+  if (n_tokens > FOVEA_MAX_TOKENS)
+    return fail(FOVEA_ERR_UNSUPPORTED, "n_tokens %d > %d", n_tokens, FOVEA_MAX_TOKENS);
+  if (top_k > FOVEA_MAX_KC) return fail(FOVEA_ERR_UNSUPPORTED, "top_k %d > %d", top_k, FOVEA_MAX_KC);
+  NEED_ROWS(N, ld, vocab, "logits");
+  if (allowed != nullptr && allowed_ld != 0 && N > 1 && allowed_ld < (vocab + 31) / 32)
+    return fail(FOVEA_ERR_INVALID_ARG, "row stride %lld of allowed is below its %d words",
+                (long long)allowed_ld, (vocab + 31) / 32);
+  WANT_ALIGNED(row_scale, 4, "row_scale");
+  WANT_ALIGNED(allowed, 4, "allowed");
+  if (N == 0) return FOVEA_OK;
+  NEED_ALIGNED(logits, dtype == FOVEA_BF16 ? 2 : 4, "logits");
+  if (n_tokens > 0) NEED_ALIGNED(tokens, 4, "tokens");
+  return FOVEA_OK;
+}
+
+FOVEA_API fovea_status fovea_token_logprobs(const void* logits, int64_t ld, int N, int vocab,
+                                            int dtype, const float* row_scale,
+                                            const int32_t* allowed, int64_t allowed_ld,
+                                            const int32_t* tokens, int n_tokens, int top_k,
+                                            float* logprobs, float* lse, float* entropy,
+                                            float* stats, int32_t* top_idx, float* top_logprobs,
+                                            void* stream) {
+  g_last_error.clear();
+  const fovea_status st = check_scores(logits, ld, N, vocab, dtype, row_scale, allowed, allowed_ld,
+                                       tokens, n_tokens, top_k);
+  if (st != FOVEA_OK || N == 0) return st;
+  if (n_tokens > 0) NEED_ALIGNED(logprobs, 4, "logprobs");
+  NEED_ALIGNED(lse, 4, "lse");
+  NEED_ALIGNED(entropy, 4, "entropy");
+  NEED_ALIGNED(stats, 4, "stats");
+  if (top_k > 0) {
+    NEED_ALIGNED(top_idx, 4, "top_idx");
+    NEED_ALIGNED(top_logprobs, 4, "top_logprobs");
+  }
+  ScoreArgs a{};
+  a.logits = logits; a.ld = ld; a.N = N; a.V = vocab;
+  a.row_scale = row_scale;
+  a.allowed = reinterpret_cast<const uint32_t*>(allowed); a.allowed_ld = allowed_ld;
+  a.tokens = tokens; a.T = n_tokens; a.k = top_k;
+  a.logprobs = logprobs; a.lse = lse; a.entropy = entropy; a.stats = stats;
+  a.top_idx = top_idx; a.top_logprobs = top_logprobs;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KernelTimer t("token_logprobs", s);
+  FOVEA_CUDA(launch_token_logprobs(dtype, a, s), "token_logprobs");
+  return FOVEA_OK;
+}
+
+FOVEA_API fovea_status fovea_token_logprobs_grad(const void* logits, int64_t ld, int N, int vocab,
+                                                 int dtype, const float* row_scale,
+                                                 const int32_t* allowed, int64_t allowed_ld,
+                                                 const float* stats, const float* entropy,
+                                                 const int32_t* tokens, const float* grad_logprobs,
+                                                 int n_tokens, const int32_t* top_idx,
+                                                 const float* grad_top, int top_k,
+                                                 const float* grad_entropy, const float* grad_lse,
+                                                 void* dlogits, void* stream) {
+  g_last_error.clear();
+  const fovea_status st = check_scores(logits, ld, N, vocab, dtype, row_scale, allowed, allowed_ld,
+                                       tokens, n_tokens, top_k);
+  if (st != FOVEA_OK || N == 0) return st;
+  NEED_ALIGNED(stats, 4, "stats");
+  NEED_ALIGNED(entropy, 4, "entropy");
+  if (n_tokens > 0) NEED_ALIGNED(grad_logprobs, 4, "grad_logprobs");
+  if (top_k > 0) {
+    NEED_ALIGNED(top_idx, 4, "top_idx");
+    NEED_ALIGNED(grad_top, 4, "grad_top");
+  }
+  WANT_ALIGNED(grad_entropy, 4, "grad_entropy");
+  WANT_ALIGNED(grad_lse, 4, "grad_lse");
+  NEED_ALIGNED(dlogits, dtype == FOVEA_BF16 ? 2 : 4, "dlogits");
+  if (dlogits == logits && N > 1 && ld != vocab)
+    return fail(FOVEA_ERR_INVALID_ARG, "dlogits may be logits only when these are dense (ld %lld, vocab %d)",
+                (long long)ld, vocab);
+  ScoreGradArgs a{};
+  a.logits = logits; a.ld = ld; a.N = N; a.V = vocab;
+  a.row_scale = row_scale;
+  a.allowed = reinterpret_cast<const uint32_t*>(allowed); a.allowed_ld = allowed_ld;
+  a.stats = stats; a.entropy = entropy;
+  a.tokens = tokens; a.grad_logprobs = grad_logprobs; a.T = n_tokens;
+  a.top_idx = top_idx; a.grad_top = grad_top; a.k = top_k;
+  a.grad_entropy = grad_entropy; a.grad_lse = grad_lse;
+  a.dlogits = dlogits;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KernelTimer t("token_logprobs_grad", s);
+  FOVEA_CUDA(launch_token_logprobs_grad(dtype, a, s), "token_logprobs_grad");
+  return FOVEA_OK;
+}
+
 FOVEA_API fovea_status fovea_timing_enable(int enable) {
   std::lock_guard<std::mutex> lk(g_tmu);
   for (auto& r : g_recs) {

@@ -352,6 +352,68 @@ cudaError_t launch_gemm_tc(int epi, const GemmArgs& a, const TmaOperand& A0, con
                            const TmaOperand& B0, const TmaOperand& B1, int max_m, int max_n,
                            cudaStream_t s, const TmaOperand& A2 = TmaOperand{nullptr, 0, 0, 0});
 
+// Residual addition, RMS norm and 8-bit output (norm.cu): rows of d columns, x
+// and residual (null: none) with a row stride, the outputs dense and each null
+// when not wanted; q8_group columns share a scale (0: the whole row).
+constexpr float kE4m3Max = 448.0f;   // the largest e4m3 value
+struct NormArgs {
+  const void* x; const void* residual; const void* gamma;
+  long long x_ld, residual_ld;       // elements
+  long long N;
+  int d;
+  float eps;
+  void* sum; void* out;
+  uint8_t* q8; float* q8_scale; int q8_group;
+};
+cudaError_t launch_add_rms_norm(int dtype, const NormArgs& a, cudaStream_t s);
+
+// Weights in 4 bits (w4.cu): codes [out, in / 2], two a byte with the even
+// column in the low half, scales [out, groups] bf16, zero points [out, groups]
+// (null: 8 everywhere), groups = ceil(in / group); w = (code - zero) * scale.
+struct W4 {
+  const uint8_t* codes; const __nv_bfloat16* scales; const uint8_t* zeros;
+  int out, in, group;
+};
+cudaError_t launch_quantize_w4(int dtype, const void* W, long long ld, int out, int in, int group,
+                               uint8_t* codes, __nv_bfloat16* scales, uint8_t* zeros, cudaStream_t s);
+// y[n, o] = sum_k x[n, k] w[o, k] (+ bias[o]).  x_scale: null, or of e4m3 rows
+// one per row (x_group 0) or per group of the weights.
+struct LinearW4Args {
+  W4 w;
+  const void* x; long long x_ld; int x_dtype;
+  const float* x_scale; int x_group;
+  const float* bias;
+  void* y; int y_dtype;
+  int N;
+};
+cudaError_t launch_linear_w4(const LinearW4Args& a, cudaStream_t s);
+
+// Log probabilities of tokens and their gradient (logprobs.cu).
+struct ScoreArgs {
+  const void* logits; long long ld;
+  long long N; int V;
+  const float* row_scale;                          // null: 1
+  const uint32_t* allowed; long long allowed_ld;   // words; null: every token
+  const int32_t* tokens; int T;
+  int k;
+  float* logprobs; float* lse; float* entropy;
+  float* stats;                                    // [N, 2]: largest z, log sum e^{z - largest}
+  int32_t* top_idx; float* top_logprobs;
+};
+cudaError_t launch_token_logprobs(int dtype, const ScoreArgs& a, cudaStream_t s);
+struct ScoreGradArgs {
+  const void* logits; long long ld;
+  long long N; int V;
+  const float* row_scale;
+  const uint32_t* allowed; long long allowed_ld;
+  const float* stats; const float* entropy;
+  const int32_t* tokens; const float* grad_logprobs; int T;   // null when T = 0
+  const int32_t* top_idx; const float* grad_top; int k;       // null when k = 0
+  const float* grad_entropy; const float* grad_lse;           // null: 0
+  void* dlogits;                                              // [N, V] dense
+};
+cudaError_t launch_token_logprobs_grad(int dtype, const ScoreGradArgs& a, cudaStream_t s);
+
 // The memory build's GEMMs out[i] = R . F[i]^T on CTA pairs (gemm_build.cu):
 // token rows R [rows, K] (R0 for part 0, R1 for the others) against up to
 // three feature matrices F[i] [cols, K] (bf16; a null base: no such part),

@@ -1,0 +1,528 @@
+// Log probabilities of given tokens with entropy and the best alternatives
+// (fovea_token_logprobs), and their gradient (fovea_token_logprobs_grad).
+// With z_i = logit_i * row_scale over a row's allowed tokens (z = -inf for the
+// others):
+//   lse = log sum_i e^{z_i},  logp_i = z_i - lse,  H = -sum_i p_i logp_i
+//   dz_i = [gradients of the tokens equal to i] - p_i G - g_H p_i (logp_i + H) + g_lse p_i
+// with G the sum of the counted tokens' gradients.
+#include "common.cuh"
+#include "rowmath.cuh"
+#include "tc_ptx.cuh"
+
+namespace fovea {
+
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kGroups = kThreads / 4;   // four neighbouring lanes' tokens are one group of the selection
+constexpr int kCands = 512;             // candidate keys a CTA collects
+constexpr int kMaxCluster = 8;
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+__device__ __forceinline__ float ex2(float x) {       // 2^x, subnormal results as 0
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// Order of logits as signed integers: every NaN above +inf, both zeros equal.
+__device__ __forceinline__ int32_t order_of(float x) {
+  if (x != x) return 0x7FFFFFFF;
+  const int32_t b = __float_as_int(x + 0.0f);
+  return b < 0 ? b ^ 0x7FFFFFFF : b;
+}
+__device__ __forceinline__ float value_of(int32_t o) { return __int_as_float(o < 0 ? o ^ 0x7FFFFFFF : o); }
+constexpr int32_t kOrderNegInf = (int32_t)0x807FFFFF;     // order_of(-inf)
+
+// A token's key: larger logits first, then the lower token; never 0.
+__device__ __forceinline__ unsigned long long key_of(int32_t order, int token) {
+  return (unsigned long long)((uint32_t)order ^ 0x80000000u) << 32 | (uint32_t)~token;
+}
+__device__ __forceinline__ int token_of(unsigned long long key) { return (int)~(uint32_t)key; }
+__device__ __forceinline__ int32_t order_in(unsigned long long key) {
+  return (int32_t)((uint32_t)(key >> 32) ^ 0x80000000u);
+}
+
+// One row's logits in 16-byte chunks of the address space: chunk c holds the
+// tokens c * NV - shift ... of the row, those outside [0, V) as -inf.  Only
+// chunks that lie in the row whole are read as vectors.
+template <class T>
+struct Row {
+  static constexpr int NV = VecOf<T>::N;
+  const T* p;
+  int V, shift, chunks;
+  const uint32_t* allowed;
+
+  __device__ __forceinline__ Row(const void* base, long long ld, long long row, int V_,
+                                 const uint32_t* allowed_, long long allowed_ld)
+      : p(static_cast<const T*>(base) + row * ld), V(V_) {
+    shift = (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T));
+    chunks = (int)(((long long)V + shift + NV - 1) / NV);
+    allowed = allowed_ != nullptr ? allowed_ + row * allowed_ld : nullptr;
+  }
+  __device__ __forceinline__ int first(int c) const { return c * NV - shift; }
+  __device__ __forceinline__ bool whole(int c) const { return first(c) >= 0 && first(c) + NV <= V; }
+  __device__ __forceinline__ uint32_t bits(int i0) const {       // of the tokens i0 .. i0 + NV - 1
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int k = i0 + i;
+      if (k >= 0 && k < V) m |= ((allowed[k >> 5] >> (k & 31)) & 1u) << i;
+    }
+    return m;
+  }
+  __device__ __forceinline__ void load(int c, float (&v)[NV]) const {
+    const int i0 = first(c);
+    if (whole(c)) {
+      ln_load<T>(p + i0, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) v[i] = i0 + i >= 0 && i0 + i < V ? to_f32(p[i0 + i]) : -INFINITY;
+    }
+    if (allowed != nullptr) {
+      const uint32_t m = bits(i0);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (!(m >> i & 1u)) v[i] = -INFINITY;
+    }
+  }
+  // One token's logit: -inf where it is not allowed.
+  __device__ __forceinline__ float at(int k) const {
+    if (allowed != nullptr && !((allowed[k >> 5] >> (k & 31)) & 1u)) return -INFINITY;
+    return to_f32(p[k]);
+  }
+};
+
+// Running softmax sums about a reference m (the largest z or somewhat less):
+// S = sum e^{z - m}, W = sum e^{z - m} (z - m).
+struct Sums {
+  float m, S, W;
+};
+// The same sums about m2 >= m (or about the first m, when nothing was summed).
+__device__ __forceinline__ void rebase(Sums& a, float m2) {
+  // e^{-200} is 0 in fp32; without the bound S dm can overflow (a reference near
+  // the type's lowest value) and leave 0 * inf
+  const float dm = max_nan(a.m - m2, -200.0f);
+  const float f = a.m == -INFINITY ? 0.0f : ex2(dm * kLog2e);
+  a.W = a.m == -INFINITY ? 0.0f : f * fmaf(a.S, dm, a.W);
+  a.S *= f;
+  a.m = m2;
+}
+__device__ __forceinline__ void join(Sums& a, Sums b) {
+  if (b.m == -INFINITY) return;
+  const float m = a.m == -INFINITY ? b.m : max_nan(a.m, b.m);
+  rebase(a, m);
+  rebase(b, m);
+  a.S += b.S;
+  a.W += b.W;
+}
+
+struct Shared {
+  float m[kWarps], S[kWarps], W[kWarps];
+  unsigned long long upper[kGroups];   // no key of the group is above it
+  unsigned long long lower[kGroups];   // some key of the group is at least this
+  unsigned long long threshold;
+  unsigned long long cand[kCands];
+  unsigned long long best[FOVEA_MAX_KC];
+  unsigned long long red[kWarps];
+  int count;
+  // of the whole row (leading CTA): what the others left
+  Sums total;
+  unsigned long long all[kMaxCluster * FOVEA_MAX_KC];
+};
+
+// A cluster of CTAs takes one row, each a range of its chunks.  One pass
+// over the logits keeps the softmax sums and, per group of four lanes, the
+// largest logit.  The k-th largest of the groups' bounds is a threshold that at
+// least k tokens reach, so only groups that reach it (k of them, and ties) are
+// read again, from L2, for the tokens above it: a few more than k.
+template <class T>
+__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArgs a) {
+  constexpr int NV = Row<T>::NV;
+  __shared__ Shared sh;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int ctas = gridDim.x, rank = blockIdx.x;       // the cluster spans the grid's x
+  const long long n = blockIdx.y;
+  pdl_wait();
+  pdl_trigger();
+  const Row<T> row(a.logits, a.ld, n, a.V, a.allowed, a.allowed_ld);
+  const float scale = a.row_scale != nullptr ? a.row_scale[n] : 1.0f;
+  const int per = (row.chunks + ctas - 1) / ctas;
+  const int c_lo = min(rank * per, row.chunks), c_hi = min(c_lo + per, row.chunks);
+
+  Sums s = {-INFINITY, 0.0f, 0.0f};
+  int32_t top = kOrderNegInf;
+  int top_chunk = 0;
+  for (int c = c_lo + tid; c < c_hi; c += kThreads) {
+    float v[NV];
+    row.load(c, v);
+    float cm = v[0];
+#pragma unroll
+    for (int i = 1; i < NV; ++i) cm = max_nan(cm, v[i]);
+    const float zm = cm * scale;
+    if (zm == -INFINITY) continue;
+    const int32_t o = order_of(cm);
+    if (o > top) {
+      top = o;
+      top_chunk = c;
+    }
+    if (!(zm <= s.m + 2.0f)) rebase(s, zm);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      // -inf: e^{-200} is 0 and so is its term of W
+      const float dz = max_nan(v[i] * scale - s.m, -200.0f);
+      const float e = ex2(dz * kLog2e);
+      s.S += e;
+      s.W = fmaf(e, dz, s.W);
+    }
+  }
+  if (top != kOrderNegInf) rebase(s, value_of(top) * scale);   // the largest z itself
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    Sums b;
+    b.m = __shfl_xor_sync(0xffffffffu, s.m, o);
+    b.S = __shfl_xor_sync(0xffffffffu, s.S, o);
+    b.W = __shfl_xor_sync(0xffffffffu, s.W, o);
+    join(s, b);
+  }
+  if (lane == 0) {
+    sh.m[warp] = s.m;
+    sh.S[warp] = s.S;
+    sh.W[warp] = s.W;
+  }
+  if (tid == 0) sh.count = 0;
+  if (a.k > 0) {
+    // tokens of the chunk lie in [first, first + NV): bounds of the group's best key
+    unsigned long long up = 0, low = 0;
+    if (top != kOrderNegInf) {
+      up = key_of(top, max(row.first(top_chunk), 0));
+      low = key_of(top, row.first(top_chunk) + NV - 1);
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      const unsigned long long u2 = __shfl_xor_sync(0xffffffffu, up, o), l2 = __shfl_xor_sync(0xffffffffu, low, o);
+      up = u2 > up ? u2 : up;
+      low = l2 > low ? l2 : low;
+    }
+    if ((lane & 3) == 0) {
+      sh.upper[tid >> 2] = up;
+      sh.lower[tid >> 2] = low;
+    }
+    if (tid == 0) sh.threshold = 1ull;                 // fewer than k groups with a token: every token
+  }
+  __syncthreads();
+  if (tid == 0) {
+    Sums t = {sh.m[0], sh.S[0], sh.W[0]};
+    for (int w = 1; w < kWarps; ++w) join(t, Sums{sh.m[w], sh.S[w], sh.W[w]});
+    sh.total = t;
+  }
+  if (a.k > 0) {
+    if (tid < kGroups && sh.lower[tid] != 0ull) {
+      const unsigned long long mine = sh.lower[tid];
+      int above = 0;
+#pragma unroll 8
+      for (int i = 0; i < kGroups; ++i) above += sh.lower[i] > mine;
+      if (above == a.k - 1) sh.threshold = mine;       // keys are distinct
+    }
+    if (tid < a.k) sh.best[tid] = 0ull;
+    __syncthreads();
+    const unsigned long long threshold = sh.threshold;
+    const int turns = (c_hi - c_lo + kThreads - 1) / kThreads;
+    for (int gr = warp; gr < kGroups; gr += kWarps) {
+      if (sh.upper[gr] < threshold) continue;
+      for (int it = lane >> 2; it < turns; it += 8) {
+        const int c = c_lo + it * kThreads + gr * 4 + (lane & 3);
+        if (c >= c_hi) break;
+        float v[NV];
+        row.load(c, v);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          if (v[i] * scale == -INFINITY) continue;
+          const unsigned long long key = key_of(order_of(v[i]), row.first(c) + i);
+          if (key >= threshold) {
+            const int at = atomicAdd(&sh.count, 1);
+            if (at < kCands) sh.cand[at] = key;
+          }
+        }
+      }
+    }
+    __syncthreads();
+    const int count = sh.count;
+    if (count <= kCands) {
+      for (int i = tid; i < count; i += kThreads) {
+        const unsigned long long mine = sh.cand[i];
+        int above = 0;
+        for (int j = 0; j < count; ++j) above += sh.cand[j] > mine;
+        if (above < a.k) sh.best[above] = mine;
+      }
+    } else {
+      // more candidates than fit (many large logits in a few groups): the
+      // largest key below the last one, k times
+      unsigned long long last = ~0ull;
+      for (int r = 0; r < a.k; ++r) {
+        unsigned long long mine = 0ull;
+        for (int gr = warp; gr < kGroups; gr += kWarps) {
+          if (sh.upper[gr] < threshold) continue;
+          for (int it = lane >> 2; it < turns; it += 8) {
+            const int c = c_lo + it * kThreads + gr * 4 + (lane & 3);
+            if (c >= c_hi) break;
+            float v[NV];
+            row.load(c, v);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+              if (v[i] * scale == -INFINITY) continue;
+              const unsigned long long key = key_of(order_of(v[i]), row.first(c) + i);
+              if (key < last && key > mine) mine = key;
+            }
+          }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+          const unsigned long long t = __shfl_xor_sync(0xffffffffu, mine, o);
+          mine = t > mine ? t : mine;
+        }
+        if (lane == 0) sh.red[warp] = mine;
+        __syncthreads();
+        mine = 0ull;
+        for (int w = 0; w < kWarps; ++w) mine = sh.red[w] > mine ? sh.red[w] : mine;
+        if (tid == 0) sh.best[r] = mine;
+        last = mine;
+        __syncthreads();
+      }
+    }
+  }
+  __syncthreads();
+
+  // the CTAs' sums and keys meet in the first one, in the CTAs' order
+  Sums total = sh.total;
+  const unsigned long long* best = sh.best;
+  if (ctas > 1) {
+    tc::cluster_sync();
+    if (rank == 0) {
+      for (int i = tid; i < ctas * a.k; i += kThreads) {
+        const uint32_t at = tc::map_dsmem(tc::smem_u32(&sh.best[i % a.k]), i / a.k);
+        unsigned long long v;
+        asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(at) : "memory");
+        sh.all[i] = v;
+      }
+      for (int r = 1; r < ctas; ++r) {
+        const uint32_t at = tc::map_dsmem(tc::smem_u32(&sh.total), r);
+        Sums b;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(b.m) : "r"(at) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(b.S) : "r"(at + 4) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(b.W) : "r"(at + 8) : "memory");
+        join(total, b);
+      }
+    }
+    tc::cluster_sync();
+    if (rank != 0) return;
+    for (int i = tid; i < a.k; i += kThreads) sh.cand[i] = 0ull;
+    __syncthreads();
+    for (int i = tid; i < ctas * a.k; i += kThreads) {
+      const unsigned long long mine = sh.all[i];
+      int above = 0;
+      for (int j = 0; j < ctas * a.k; ++j) above += sh.all[j] > mine;
+      if (mine != 0ull && above < a.k) sh.cand[above] = mine;
+    }
+    __syncthreads();
+    best = sh.cand;
+  }
+  const float log_S = logf(total.S);
+  const bool empty = total.m == -INFINITY;
+  // logp = (z - max) - log S: the difference is exact for the large ones, and stays so
+  // where |max| is so large that max + log S would lose log S
+  const float m = empty ? 0.0f : total.m, log_sum = empty ? 0.0f : log_S;
+  if (tid == 0) {
+    a.lse[n] = total.m + log_S;
+    a.stats[2 * n] = total.m;
+    a.stats[2 * n + 1] = log_S;
+    a.entropy[n] = empty ? 0.0f : log_S - total.W / total.S;
+  }
+  for (int j = tid; j < a.T; j += kThreads) {
+    const int tok = a.tokens[n * a.T + j];
+    float lp = 0.0f;
+    if (tok >= 0) lp = tok < a.V ? (row.at(tok) * scale - m) - log_sum : __int_as_float(0x7FC00000);
+    a.logprobs[n * a.T + j] = lp;
+  }
+  for (int j = tid; j < a.k; j += kThreads) {
+    const unsigned long long key = best[j];
+    a.top_idx[n * a.k + j] = key != 0ull ? token_of(key) : -1;
+    a.top_logprobs[n * a.k + j] = key != 0ull ? (value_of(order_in(key)) * scale - m) - log_sum : -INFINITY;
+  }
+}
+
+// The gradient of one row's range of chunks.  Every token's term is p (A - g_H
+// logp) with A of the row; the few tokens with a gradient of their own are
+// written again after it, by the CTA whose range they lie in.
+template <class T>
+__global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const ScoreGradArgs a) {
+  constexpr int NV = Row<T>::NV;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int tid = threadIdx.x;
+  const int E = a.T + a.k;                     // entries: tokens, then alternatives
+  int* tok = reinterpret_cast<int*>(smem);
+  float* grad = reinterpret_cast<float*>(tok + E);
+  float* logit = grad + E;
+  const long long n = blockIdx.y;
+  pdl_wait();
+  pdl_trigger();
+  const Row<T> row(a.logits, a.ld, n, a.V, a.allowed, a.allowed_ld);
+  T* out = static_cast<T*>(a.dlogits) + n * a.V;
+  const bool out_vec = ((reinterpret_cast<uintptr_t>(out) & 15u) / sizeof(T)) == (unsigned)row.shift;
+  const float scale = a.row_scale != nullptr ? a.row_scale[n] : 1.0f;
+  const bool empty = a.stats[2 * n] == -INFINITY;
+  const float m = empty ? 0.0f : a.stats[2 * n], log_sum = empty ? 0.0f : a.stats[2 * n + 1];
+  for (int j = tid; j < E; j += kThreads) {
+    int k = j < a.T ? a.tokens[n * a.T + j] : a.top_idx[n * a.k + j - a.T];
+    float g = j < a.T ? a.grad_logprobs[n * a.T + j] : a.grad_top[n * a.k + j - a.T];
+    float x = 0.0f;
+    if (k >= a.V) {                            // no such token: the row's gradient shows it
+      g = __int_as_float(0x7FC00000);
+      k = -1;
+    } else if (k < 0) {
+      g = 0.0f;
+    } else {
+      x = row.at(k);
+      if (x * scale == -INFINITY) {                    // no probability, no gradient
+        k = -1;
+        g = 0.0f;
+      }
+    }
+    tok[j] = k;
+    grad[j] = g;
+    logit[j] = x;
+  }
+  __syncthreads();
+  float G = 0.0f;
+  for (int j = 0; j < E; ++j) G += grad[j];
+  const float gH = a.grad_entropy != nullptr ? a.grad_entropy[n] : 0.0f;
+  const float gl = a.grad_lse != nullptr ? a.grad_lse[n] : 0.0f;
+  const float A = gl - G - gH * a.entropy[n];
+
+  const int per = (row.chunks + gridDim.x - 1) / gridDim.x;
+  const int c_lo = min((int)blockIdx.x * per, row.chunks), c_hi = min(c_lo + per, row.chunks);
+  for (int c = c_lo + tid; c < c_hi; c += kThreads) {
+    float v[NV];
+    row.load(c, v);
+    const int i0 = row.first(c);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const float lp = max_nan((v[i] * scale - m) - log_sum, -1e4f);      // -inf: p is 0, and so is p logp
+      v[i] = ex2(lp * kLog2e) * fmaf(-gH, lp, A) * scale;
+    }
+    if (out_vec && row.whole(c)) {
+      __align__(16) T e[NV];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) e[i] = from_f32<T>(v[i]);
+      *reinterpret_cast<uint4*>(out + i0) = *reinterpret_cast<const uint4*>(e);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (i0 + i >= 0 && i0 + i < a.V) out[i0 + i] = from_f32<T>(v[i]);
+    }
+  }
+  __syncthreads();
+  for (int j = tid; j < E; j += kThreads) {
+    const int k = tok[j];
+    if (k < max(row.first(c_lo), 0) || k >= min(row.first(c_hi), a.V)) continue;
+    // a token given more than once: its first entry takes the sum, in order
+    bool again = false;
+    float g = 0.0f;
+    for (int i = 0; i < E; ++i)
+      if (tok[i] == k) {
+        again |= i < j;
+        g += grad[i];
+      }
+    if (again) continue;
+    const float lp = max_nan((logit[j] * scale - m) - log_sum, -1e4f);
+    out[k] = from_f32<T>(fmaf(ex2(lp * kLog2e), fmaf(-gH, lp, A), g) * scale);
+  }
+}
+
+template <class... KArgs, class... Args>
+cudaError_t launch_cluster(void (*kern)(KArgs...), dim3 grid, int cluster, cudaStream_t s, Args&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+}
+
+// CTAs per row: enough that the rows fill the device four times over, as long
+// as each has at least two chunks a thread.
+int row_split(long long N, int V, int size) {
+  int c = 1;
+  while (c < kMaxCluster && N * c < 4 * 152 && (long long)V * size / (16 * kThreads) >= 4 * c) c *= 2;
+  return c;
+}
+
+constexpr long long kRowsPerLaunch = 65535;        // the grid's y
+
+}  // namespace
+
+cudaError_t launch_token_logprobs(int dtype, const ScoreArgs& all, cudaStream_t s) {
+  const int size = dtype == FOVEA_BF16 ? 2 : 4;
+  for (long long n0 = 0; n0 < all.N; n0 += kRowsPerLaunch) {
+    ScoreArgs a = all;
+    a.N = std::min(kRowsPerLaunch, all.N - n0);
+    a.logits = static_cast<const uint8_t*>(all.logits) + n0 * all.ld * size;
+    if (a.row_scale != nullptr) a.row_scale += n0;
+    if (a.allowed != nullptr) a.allowed += n0 * all.allowed_ld;
+    if (a.T > 0) { a.tokens += n0 * all.T; a.logprobs += n0 * all.T; }
+    if (a.k > 0) { a.top_idx += n0 * all.k; a.top_logprobs += n0 * all.k; }
+    a.lse += n0;
+    a.stats += 2 * n0;
+    a.entropy += n0;
+    const int split = row_split(a.N, a.V, size);
+    const dim3 grid(split, (unsigned)a.N);
+    const cudaError_t e = dtype == FOVEA_BF16
+                              ? launch_cluster(token_logprobs_kernel<__nv_bfloat16>, grid, split, s, a)
+                              : launch_cluster(token_logprobs_kernel<float>, grid, split, s, a);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_token_logprobs_grad(int dtype, const ScoreGradArgs& all, cudaStream_t s) {
+  const int size = dtype == FOVEA_BF16 ? 2 : 4;
+  for (long long n0 = 0; n0 < all.N; n0 += kRowsPerLaunch) {
+    ScoreGradArgs a = all;
+    a.N = std::min(kRowsPerLaunch, all.N - n0);
+    a.logits = static_cast<const uint8_t*>(all.logits) + n0 * all.ld * size;
+    a.dlogits = static_cast<uint8_t*>(all.dlogits) + n0 * all.V * size;
+    if (a.row_scale != nullptr) a.row_scale += n0;
+    if (a.allowed != nullptr) a.allowed += n0 * all.allowed_ld;
+    if (a.T > 0) { a.tokens += n0 * all.T; a.grad_logprobs += n0 * all.T; }
+    if (a.k > 0) { a.top_idx += n0 * all.k; a.grad_top += n0 * all.k; }
+    if (a.grad_entropy != nullptr) a.grad_entropy += n0;
+    if (a.grad_lse != nullptr) a.grad_lse += n0;
+    a.stats += 2 * n0;
+    a.entropy += n0;
+    // in place, a CTA may not overwrite logits that another CTA of the row still
+    // has to read for its tokens' entries
+    const int split = a.dlogits == a.logits ? 1 : row_split(a.N, a.V, size);
+    const dim3 grid(split, (unsigned)a.N);
+    const size_t smem = (size_t)(a.T + a.k) * 12;
+    const cudaError_t e = dtype == FOVEA_BF16
+                              ? launch_pdl(token_logprobs_grad_kernel<__nv_bfloat16>, grid, dim3(kThreads), smem, s, a)
+                              : launch_pdl(token_logprobs_grad_kernel<float>, grid, dim3(kThreads), smem, s, a);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+}  // namespace fovea

@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_HERE, "_lib", "libfovea.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CUDA, ERR_OOM, ERR_TIMEOUT = range(6)
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "UNSUPPORTED", 3: "CUDA", 4: "OOM", 5: "TIMEOUT"}
-BF16, FP32 = 0, 1
+BF16, FP32, E4M3 = 0, 1, 2
 MAX_D, MAX_H, MAX_K, MAX_ENTRIES, MAX_SEQ = 8192, 4096, 1024, 32768, 512
 
 # Field order of fovea_params after the scalar header (C struct order).
@@ -37,6 +37,8 @@ EXPORTS = (
     "fovea_last_error", "fovea_timing_enable", "fovea_timing_read", "fovea_version",
     "fovea_retrieve_fuse_noalloc", "fovea_noalloc_sync_errors", "fovea_memory_folded_keys",
     "fovea_lm_head_topk", "fovea_debug_wait_limit", "fovea_lm_head_workspace_size",
+    "fovea_add_rms_norm", "fovea_quantize_w4", "fovea_linear_w4", "fovea_token_logprobs",
+    "fovea_token_logprobs_grad",
 )
 NOALLOC_WORKSPACE_BYTES = 32 << 20
 
@@ -102,10 +104,20 @@ def lib() -> ctypes.CDLL:
                                         ctypes.POINTER(ctypes.c_int), ctypes.c_int]
         L.fovea_timing_read.restype = ctypes.c_int
         L.fovea_version.restype = ctypes.c_int
+        i, i64, f32 = ctypes.c_int, ctypes.c_int64, ctypes.c_float
+        L.fovea_add_rms_norm.argtypes = [vp, i64, vp, i64, vp, i, i, i, f32, vp, vp, vp, vp, i, vp]
+        L.fovea_quantize_w4.argtypes = [vp, i64, i, i, i, i, vp, vp, vp, vp]
+        L.fovea_linear_w4.argtypes = [vp, i64, i, vp, i, i, vp, vp, vp, vp, i, i, i, vp, i, vp]
+        L.fovea_token_logprobs.argtypes = [vp, i64, i, i, i, vp, vp, i64, vp, i, i, vp, vp, vp, vp,
+                                           vp, vp, vp]
+        L.fovea_token_logprobs_grad.argtypes = [vp, i64, i, i, i, vp, vp, i64, vp, vp, vp, vp, i,
+                                                vp, vp, i, vp, vp, vp, vp]
         for name in ("fovea_build_memory", "fovea_memory_info", "fovea_memory_tensors",
                      "fovea_memory_folded_keys", "fovea_lm_head_topk",
                      "fovea_workspace_size", "fovea_workspace_init", "fovea_retrieve_fuse",
-                     "fovea_sync_errors", "fovea_timing_enable"):
+                     "fovea_sync_errors", "fovea_timing_enable", "fovea_add_rms_norm",
+                     "fovea_quantize_w4", "fovea_linear_w4", "fovea_token_logprobs",
+                     "fovea_token_logprobs_grad"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -360,6 +372,257 @@ def lm_head_topk(W_LM: torch.Tensor, h_hat: torch.Tensor, k_c: int, workspace: t
                                     _ptr(idx), _ptr(val), _ptr(workspace), workspace.numel(),
                                     _stream(stream)))
     return idx, val, logits
+
+
+# ---------------------------------------------------------------------------
+# Operators of the drafter's exit
+# ---------------------------------------------------------------------------
+
+_DTYPES = {torch.bfloat16: BF16, torch.float32: FP32, torch.float8_e4m3fn: E4M3}
+_ROW_TYPES = (torch.bfloat16, torch.float32)
+
+
+def _need(name: str, t, shape, dtypes) -> None:
+    """t is a CUDA tensor of one of these types and this shape (None: any
+    size), contiguous along its last dimension."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} has type {t.dtype}; expected {' or '.join(map(str, dtypes))}")
+    s = t.shape
+    if len(s) != len(shape) or any(want is not None and have != want for have, want in zip(s, shape)):
+        raise ValueError(f"{name} has shape {list(s)}; expected {list(shape)} (None: any)")
+    if len(s) == 2 and s[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must be contiguous along its rows")
+
+
+def _need_dense(name: str, t, shape, dtypes) -> None:
+    _need(name, t, shape, dtypes)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+class _On:
+    """The stream of a call that allocates its outputs.  None: the current one.
+    On another stream the outputs come from that stream's pool and the inputs are
+    recorded as used there, so that neither memory is reused too early; ordering
+    the streams themselves stays with the caller."""
+
+    def __init__(self, stream, device, *inputs):
+        self.device = device
+        self.other = None
+        if stream is None:
+            self.raw = torch._C._cuda_getCurrentRawStream(device.index)
+            return
+        raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+        self.raw = raw
+        if raw != torch._C._cuda_getCurrentRawStream(device.index):
+            self.other = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(raw, device)
+            for t in inputs:
+                if t is not None:
+                    t.record_stream(self.other)
+
+    def empty(self, shape, dtype) -> torch.Tensor:
+        if self.other is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.other):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+
+def _at(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def add_rms_norm(x: torch.Tensor, gamma: torch.Tensor, residual: Optional[torch.Tensor] = None, *,
+                 eps: float = 1e-6, want_out: bool = True, q8_group: Optional[int] = None,
+                 stream=None) -> Dict[str, Optional[torch.Tensor]]:
+    """fovea_add_rms_norm: s = x + residual and y = RMSNorm(s) * gamma for rows
+    x [N, d] (bf16 or fp32; rows may be strided).  Returns a dict of
+      sum       s in x's type (None without a residual)
+      out       y in x's type (None with want_out=False)
+      q8        y in 8 bits, float8_e4m3fn, and
+      q8_scale  its scales, fp32: [N] for q8_group = 0 (a scale per row), else
+                [N, ceil(d / q8_group)] for q8_group of 32, 64 or 128 columns
+                (both only when q8_group is given)."""
+    _need("x", x, (None, None), _ROW_TYPES)
+    N, d = x.shape
+    dt = (x.dtype,)
+    _need_dense("gamma", gamma, (d,), dt)
+    if residual is not None:
+        _need("residual", residual, (N, d), dt)
+    if residual is None and not want_out and q8_group is None:
+        raise ValueError("nothing to compute: no residual, want_out=False and no q8_group")
+    if q8_group is not None and q8_group not in (0, 32, 64, 128):
+        raise ValueError(f"q8_group {q8_group} is not None, 0, 32, 64 or 128")
+    on = _On(stream, x.device, x, gamma, residual)
+    s = on.empty((N, d), x.dtype) if residual is not None else None
+    out = on.empty((N, d), x.dtype) if want_out else None
+    r = dict(sum=s, out=out)
+    q8 = scale = None
+    if q8_group is not None:
+        r["q8"] = q8 = on.empty((N, d), torch.float8_e4m3fn)
+        r["q8_scale"] = scale = on.empty((N, -(-d // q8_group)) if q8_group else (N,), torch.float32)
+    _check(lib().fovea_add_rms_norm(x.data_ptr(), _ld(x), _at(residual),
+                                    _ld(residual) if residual is not None else 0, gamma.data_ptr(),
+                                    N, d, _DTYPES[x.dtype], eps, _at(s), _at(out), _at(q8),
+                                    _at(scale), q8_group or 0, on.raw))
+    return r
+
+
+def quantize_w4(W: torch.Tensor, group: int = 128, *, symmetric: bool = True,
+                stream=None) -> Dict[str, Optional[torch.Tensor]]:
+    """fovea_quantize_w4: W [out, in] (bf16 or fp32; in a multiple of 32) in 4
+    bits with a scale per `group` (32, 64 or 128) columns.  Returns a dict of
+    codes [out, in / 2] uint8 (the even column in the low four bits), scales
+    [out, ceil(in / group)] bf16 and zeros (uint8, like scales; None: symmetric,
+    8 everywhere), as linear_w4 takes them."""
+    _need("W", W, (None, None), _ROW_TYPES)
+    out_f, in_f = W.shape
+    if group not in (32, 64, 128):
+        raise ValueError(f"group {group} is not 32, 64 or 128")
+    on = _On(stream, W.device, W)
+    groups = -(-in_f // group)
+    codes = on.empty((out_f, in_f // 2), torch.uint8)
+    scales = on.empty((out_f, groups), torch.bfloat16)
+    zeros = None if symmetric else on.empty((out_f, groups), torch.uint8)
+    _check(lib().fovea_quantize_w4(W.data_ptr(), _ld(W), out_f, in_f, _DTYPES[W.dtype], group,
+                                   codes.data_ptr(), scales.data_ptr(), _at(zeros), on.raw))
+    return dict(codes=codes, scales=scales, zeros=zeros)
+
+
+def linear_w4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
+              zeros: Optional[torch.Tensor] = None, *, group: int = 128,
+              x_scale: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+              out_dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
+    """fovea_linear_w4: y [N, out] = x W^T (+ bias) with W in 4 bits (codes,
+    scales, zeros and group as quantize_w4 gives them).  x [N, in] is bf16, fp32,
+    or float8_e4m3fn with x_scale [N] or [N, ceil(in / group)] fp32 (add_rms_norm's
+    q8 and q8_scale); bias [out] fp32; y is fp32 or bf16 (out_dtype)."""
+    _need("x", x, (None, None), tuple(_DTYPES))
+    N, in_f = x.shape
+    _need_dense("codes", codes, (None, in_f // 2), (torch.uint8,))
+    out_f = codes.shape[0]
+    if group not in (32, 64, 128):
+        raise ValueError(f"group {group} is not 32, 64 or 128")
+    groups = -(-in_f // group)
+    _need_dense("scales", scales, (out_f, groups), (torch.bfloat16,))
+    if zeros is not None:
+        _need_dense("zeros", zeros, (out_f, groups), (torch.uint8,))
+    if (x.dtype == torch.float8_e4m3fn) != (x_scale is not None):
+        raise ValueError("x_scale goes with float8_e4m3fn rows, and only with them")
+    x_group = 0
+    if x_scale is not None:
+        x_group = group if x_scale.dim() == 2 else 0
+        _need_dense("x_scale", x_scale, (N, groups) if x_group else (N,), (torch.float32,))
+    if bias is not None:
+        _need_dense("bias", bias, (out_f,), (torch.float32,))
+    if out_dtype not in _ROW_TYPES:
+        raise ValueError(f"out_dtype {out_dtype} is neither bf16 nor fp32")
+    on = _On(stream, x.device, x, codes, scales, zeros, x_scale, bias)
+    y = on.empty((N, out_f), out_dtype)
+    _check(lib().fovea_linear_w4(x.data_ptr(), _ld(x), _DTYPES[x.dtype], _at(x_scale), x_group, N,
+                                 codes.data_ptr(), scales.data_ptr(), _at(zeros), _at(bias), out_f,
+                                 in_f, group, y.data_ptr(), _DTYPES[out_dtype], on.raw))
+    return y
+
+
+def _need_scores(logits, tokens, row_scale, allowed):
+    """Checks what both score calls take; returns (N, vocab, allowed's row stride)."""
+    _need("logits", logits, (None, None), _ROW_TYPES)
+    N, V = logits.shape
+    if tokens is not None:
+        _need_dense("tokens", tokens, (N, None), (torch.int32,))
+    if row_scale is not None:
+        _need_dense("row_scale", row_scale, (N,), (torch.float32,))
+    if allowed is None:
+        return N, V, 0
+    words = (V + 31) // 32
+    _need("allowed", allowed, (None, words), (torch.int32,))
+    if allowed.shape[0] not in (1, N):
+        raise ValueError(f"allowed has {allowed.shape[0]} rows; expected {N}, or 1 for all")
+    return N, V, _ld(allowed) if allowed.shape[0] == N and N > 1 else 0
+
+
+def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top_k: int = 0, *,
+                   row_scale: Optional[torch.Tensor] = None, allowed: Optional[torch.Tensor] = None,
+                   stream=None) -> Dict[str, torch.Tensor]:
+    """fovea_token_logprobs: under the softmax of z = logits * row_scale over each
+    row's allowed tokens (logits [N, vocab] bf16 or fp32, rows may be strided;
+    row_scale [N] fp32 inverse temperatures; allowed [N or 1, ceil(vocab / 32)]
+    int32 words, bit i % 32 of word i / 32 for token i), a dict of
+      logprobs      [N, T] of tokens [N, T] int32 (-1: none, 0; when given)
+      lse, entropy  [N]; stats [N, 2]: the largest z and log sum e^(z - it)
+      top_idx       [N, top_k] int32, the largest logits' tokens, descending, the
+                    smaller token first on ties, -1 past the tokens that have any
+                    probability; top_logprobs [N, top_k] (when top_k > 0)."""
+    N, V, allowed_ld = _need_scores(logits, tokens, row_scale, allowed)
+    on = _On(stream, logits.device, logits, tokens, row_scale, allowed)
+    T = tokens.shape[1] if tokens is not None else 0
+    # one allocation for the fp32 results: [lse | entropy | stats | logprobs | top_logprobs]
+    f = on.empty((N * (4 + T + max(top_k, 0)),), torch.float32)
+    lse, entropy, stats = f[:N], f[N:2 * N], f[2 * N:4 * N].view(N, 2)
+    r = dict(lse=lse, entropy=entropy, stats=stats)
+    lp = top = idx = None
+    if tokens is not None:
+        r["logprobs"] = lp = f[4 * N:(4 + T) * N].view(N, T)
+    if top_k > 0:
+        r["top_logprobs"] = top = f[(4 + T) * N:].view(N, top_k)
+        r["top_idx"] = idx = on.empty((N, top_k), torch.int32)
+    _check(lib().fovea_token_logprobs(logits.data_ptr(), _ld(logits), N, V, _DTYPES[logits.dtype],
+                                      _at(row_scale), _at(allowed), allowed_ld, _at(tokens), T,
+                                      top_k, _at(lp), lse.data_ptr(), entropy.data_ptr(),
+                                      stats.data_ptr(), _at(idx), _at(top), on.raw))
+    return r
+
+
+def token_logprobs_grad(logits: torch.Tensor, stats: torch.Tensor, entropy: torch.Tensor, *,
+                        tokens: Optional[torch.Tensor] = None,
+                        grad_logprobs: Optional[torch.Tensor] = None,
+                        top_idx: Optional[torch.Tensor] = None,
+                        grad_top: Optional[torch.Tensor] = None,
+                        grad_entropy: Optional[torch.Tensor] = None,
+                        grad_lse: Optional[torch.Tensor] = None,
+                        row_scale: Optional[torch.Tensor] = None,
+                        allowed: Optional[torch.Tensor] = None,
+                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """fovea_token_logprobs_grad: the gradient [N, vocab] (logits' type) with
+    respect to logits of token_logprobs(logits, tokens, top_k, row_scale=...,
+    allowed=...), from the stats, entropy and top_idx that call returned and the
+    fp32 gradients of its outputs (each may be left out: 0).  `out` takes the
+    result when given; it may be logits itself, when dense."""
+    if (tokens is None) != (grad_logprobs is None) or (top_idx is None) != (grad_top is None):
+        raise ValueError("tokens and grad_logprobs, top_idx and grad_top, go together")
+    N, V, allowed_ld = _need_scores(logits, tokens, row_scale, allowed)
+    f32 = (torch.float32,)
+    _need_dense("stats", stats, (N, 2), f32)
+    _need_dense("entropy", entropy, (N,), f32)
+    T = k = 0
+    if tokens is not None:
+        T = tokens.shape[1]
+        _need_dense("grad_logprobs", grad_logprobs, (N, T), f32)
+    if top_idx is not None:
+        k = top_idx.shape[1]
+        _need_dense("top_idx", top_idx, (N, None), (torch.int32,))
+        _need_dense("grad_top", grad_top, (N, k), f32)
+    if grad_entropy is not None:
+        _need_dense("grad_entropy", grad_entropy, (N,), f32)
+    if grad_lse is not None:
+        _need_dense("grad_lse", grad_lse, (N,), f32)
+    if out is not None:
+        _need_dense("out", out, (N, V), (logits.dtype,))
+    on = _On(stream, logits.device, logits, tokens, row_scale, allowed, stats, entropy, grad_logprobs,
+             top_idx, grad_top, grad_entropy, grad_lse, out)
+    if out is None:
+        out = on.empty((N, V), logits.dtype)
+    _check(lib().fovea_token_logprobs_grad(
+        logits.data_ptr(), _ld(logits), N, V, _DTYPES[logits.dtype], _at(row_scale), _at(allowed),
+        allowed_ld, stats.data_ptr(), entropy.data_ptr(), _at(tokens), _at(grad_logprobs), T,
+        _at(top_idx), _at(grad_top), k, _at(grad_entropy), _at(grad_lse), out.data_ptr(), on.raw))
+    return out
 
 
 def timing_enable(on: bool = True) -> None:
