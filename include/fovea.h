@@ -329,8 +329,9 @@ FOVEA_API fovea_status fovea_lm_head_workspace_size(int vocab, int d_model, int 
  * Unlike the tensors of the entry points above, x, residual, W and logits here
  * need only be contiguous along their rows: each has a row stride `ld` in
  * elements (>= its row length), and pointers aligned to their element.  Outputs
- * are dense.  None of these calls allocates, needs a workspace or synchronises;
- * all enqueue on `stream` and can be captured.  N = 0 is valid and does nothing.
+ * are dense.  None of these calls allocates or synchronises, and only
+ * fovea_linear_w4 needs a workspace; all enqueue on `stream` and can be captured.
+ * N = 0 is valid and does nothing.
  * Errors: INVALID_ARG, UNSUPPORTED (nothing enqueued), CUDA.
  */
 #define FOVEA_E4M3 2                /* 8-bit float rows (x of fovea_linear_w4) */
@@ -387,6 +388,11 @@ FOVEA_API fovea_status fovea_quantize_w4(const void* W, int64_t ld, int out_feat
  *           fovea_add_rms_norm writes q8 and q8_scale); NULL for the others
  *   bias    [out_features] fp32, or NULL
  *   y       [N, out_features] y_dtype: FOVEA_FP32 or FOVEA_BF16
+ *   workspace  fovea_linear_w4_workspace_size bytes (256-byte aligned; NULL when
+ *           that is 0, as for up to 16 rows, 5 of fp32).  It needs no
+ *           initialisation and may serve the next call on the stream.  A bounded
+ *           device wait that gives up leaves NaN in the y it did not reach and
+ *           FOVEA_ERR_TIMEOUT for fovea_sync_errors(workspace).
  * Products and sums of a group are exact up to fp32 accumulation (an fp32 x
  * counts with all its bits); y is rounded once.
  */
@@ -394,7 +400,12 @@ FOVEA_API fovea_status fovea_linear_w4(const void* x, int64_t x_ld, int x_dtype,
                                        const float* x_scale, int x_group, int N, const void* codes,
                                        const void* scales, const void* zeros, const float* bias,
                                        int out_features, int in_features, int group, void* y,
-                                       int y_dtype, void* stream);
+                                       int y_dtype, void* workspace, size_t workspace_bytes,
+                                       void* stream);
+/* Workspace bytes of fovea_linear_w4 for N rows of x_dtype (x_group as there; 0
+ * is possible).  Errors: INVALID_ARG, UNSUPPORTED. */
+FOVEA_API fovea_status fovea_linear_w4_workspace_size(int N, int in_features, int group,
+                                                      int x_dtype, int x_group, size_t* bytes);
 
 /*
  * Scores of tokens under the softmax of each row of logits: with z = logit *

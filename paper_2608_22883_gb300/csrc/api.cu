@@ -1350,7 +1350,8 @@ FOVEA_API fovea_status fovea_linear_w4(const void* x, int64_t x_ld, int x_dtype,
                                        const float* x_scale, int x_group, int N, const void* codes,
                                        const void* scales, const void* zeros, const float* bias,
                                        int out_features, int in_features, int group, void* y,
-                                       int y_dtype, void* stream) {
+                                       int y_dtype, void* workspace, size_t workspace_bytes,
+                                       void* stream) {
   g_last_error.clear();
   if (x_dtype != FOVEA_BF16 && x_dtype != FOVEA_FP32 && x_dtype != FOVEA_E4M3)
     return fail(FOVEA_ERR_INVALID_ARG, "x_dtype %d is not FOVEA_BF16, FOVEA_FP32 or FOVEA_E4M3", x_dtype);
@@ -1369,6 +1370,11 @@ FOVEA_API fovea_status fovea_linear_w4(const void* x, int64_t x_ld, int x_dtype,
   NEED_ALIGNED(x, x_dtype == FOVEA_BF16 ? 2 : x_dtype == FOVEA_FP32 ? 4 : 1, "x");
   if (x_dtype == FOVEA_E4M3) NEED_ALIGNED(x_scale, 4, "x_scale");
   NEED_ALIGNED(y, y_dtype == FOVEA_BF16 ? 2 : 4, "y");
+  const size_t need = linear_w4_workspace(N, in_features, group, x_dtype, x_dtype == FOVEA_E4M3 && x_group != 0);
+  if (need > 0) NEED_ALIGNED(workspace, 256, "workspace");
+  if (workspace_bytes < need)
+    return fail(FOVEA_ERR_INVALID_ARG, "workspace has %zu bytes, needs %zu (fovea_linear_w4_workspace_size)",
+                workspace_bytes, need);
   LinearW4Args a{};
   a.w = W4{static_cast<const uint8_t*>(codes), static_cast<const __nv_bfloat16*>(scales),
            static_cast<const uint8_t*>(zeros), out_features, in_features, group};
@@ -1377,9 +1383,23 @@ FOVEA_API fovea_status fovea_linear_w4(const void* x, int64_t x_ld, int x_dtype,
   a.bias = bias;
   a.y = y; a.y_dtype = y_dtype;
   a.N = N;
+  a.workspace = workspace;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   KernelTimer t("linear_w4", s);
   FOVEA_CUDA(launch_linear_w4(a, s), "linear_w4");
+  return FOVEA_OK;
+}
+
+FOVEA_API fovea_status fovea_linear_w4_workspace_size(int N, int in_features, int group,
+                                                      int x_dtype, int x_group, size_t* bytes) {
+  g_last_error.clear();
+  if (bytes == nullptr) return fail(FOVEA_ERR_INVALID_ARG, "bytes is NULL");
+  if (N < 0) return fail(FOVEA_ERR_INVALID_ARG, "N = %d < 0", N);
+  if (x_dtype != FOVEA_BF16 && x_dtype != FOVEA_FP32 && x_dtype != FOVEA_E4M3)
+    return fail(FOVEA_ERR_INVALID_ARG, "x_dtype %d is not FOVEA_BF16, FOVEA_FP32 or FOVEA_E4M3", x_dtype);
+  const fovea_status st = check_w4(1, in_features, group);
+  if (st != FOVEA_OK) return st;
+  *bytes = linear_w4_workspace(N, in_features, group, x_dtype, x_dtype == FOVEA_E4M3 && x_group != 0);
   return FOVEA_OK;
 }
 

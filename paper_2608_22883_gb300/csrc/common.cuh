@@ -347,6 +347,10 @@ GemmPlan plan_gemm_tc(int epi, const GemmArgs& a, int max_m, int max_n);
 // a multiple of 64, as (64 k, rows, cols / 64 k-blocks) with 128-byte swizzle;
 // box = 64 x box_rows x kps.
 bool encode_kblock_map(CUtensorMap* m, const TmaOperand& op, int box_rows, int kps);
+// Tensor map of a dense [rows, row_bytes] byte matrix (row_bytes a multiple of
+// 16) in boxes of 128 bytes x box_rows with 128-byte swizzle; bytes outside the
+// matrix read as 0.
+bool encode_byte_map(CUtensorMap* m, const void* base, long long rows, long long row_bytes, int box_rows);
 // A2 (optional): the feature operand of output columns >= a_split2.
 cudaError_t launch_gemm_tc(int epi, const GemmArgs& a, const TmaOperand& A0, const TmaOperand& A1,
                            const TmaOperand& B0, const TmaOperand& B1, int max_m, int max_n,
@@ -385,8 +389,14 @@ struct LinearW4Args {
   const float* bias;
   void* y; int y_dtype;
   int N;
+  void* workspace;                   // linear_w4_workspace bytes
 };
+// Bytes of workspace the product needs (0: none).
+size_t linear_w4_workspace(int N, int in, int group, int x_dtype, bool by_group);
 cudaError_t launch_linear_w4(const LinearW4Args& a, cudaStream_t s);
+// The same for more rows than a warp's tensor-core tile takes (w4_tc.cu).
+size_t linear_w4_tc_workspace(int N, int in, int group, int x_dtype, bool by_group);
+cudaError_t launch_linear_w4_tc(const LinearW4Args& a, cudaStream_t s);
 
 // Log probabilities of tokens and their gradient (logprobs.cu).
 struct ScoreArgs {

@@ -918,6 +918,18 @@ bool encode_kblock_map(CUtensorMap* m, const TmaOperand& op, int box_rows, int k
   return cached_map3(m, op, box_rows, kps);
 }
 
+bool encode_byte_map(CUtensorMap* m, const void* base, long long rows, long long row_bytes, int box_rows) {
+  EncodeTiledFn enc = encoder();
+  if (enc == nullptr) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
+  cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+  cuuint32_t es[2] = {1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, es,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 static std::atomic<unsigned long long> g_wait_limit_ns{kDefaultWaitLimitNs};
 void set_wait_limit_ns(unsigned long long ns) { g_wait_limit_ns.store(ns); }
 unsigned long long wait_limit_ns() { return g_wait_limit_ns.load(); }

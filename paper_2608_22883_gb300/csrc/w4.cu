@@ -352,7 +352,17 @@ cudaError_t launch_quantize_w4(int dtype, const void* W, long long ld, int out, 
   return vec ? go(quantize_w4_kernel<float, true>, w) : go(quantize_w4_kernel<float, false>, w);
 }
 
+// Rows (an fp32 row counts three times) from which the codes go through tensor
+// memory instead of each warp's registers.
+constexpr int kFewCols = 16;
+static bool few_rows(int N, int x_dtype) { return (long long)N * (x_dtype == FOVEA_FP32 ? 3 : 1) <= kFewCols; }
+
+size_t linear_w4_workspace(int N, int in, int group, int x_dtype, bool by_group) {
+  return few_rows(N, x_dtype) ? 0 : linear_w4_tc_workspace(N, in, group, x_dtype, by_group);
+}
+
 cudaError_t launch_linear_w4(const LinearW4Args& a, cudaStream_t s) {
+  if (!few_rows(a.N, a.x_dtype)) return launch_linear_w4_tc(a, s);
   const int parts = a.x_dtype == FOVEA_FP32 ? 3 : 1;
   const long long spans = (a.w.in + kSpan - 1) / kSpan;
   const int groups = (a.w.in + a.w.group - 1) / a.w.group;

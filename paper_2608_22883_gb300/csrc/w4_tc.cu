@@ -1,0 +1,604 @@
+// fovea_linear_w4 for more rows than fit one warp's tensor-core tile: the
+// weights' codes become bf16 integers in tensor memory, where tcgen05 takes them
+// as its 128-row operand.
+//
+//   y[n, o] = sum over groups g of scale[o, g] sum_{k in g} x[n, k] (code[o, k] - zero[o, g])
+//
+// A first kernel lays x out as the other operand: bf16 columns (an fp32 row as
+// three that add up to it), each run of eight k in the order in which a 32-bit word
+// of codes yields them, zero-padded.  The product's CTAs then stream 128 weight
+// rows x 256 k of codes a stage (16 KB, TMA) with the stage's x; eight warps turn
+// codes into integers, one weight row a thread, and write them to tensor memory;
+// one thread issues the MMAs, each group's sum into an accumulator of its own;
+// four warps read the accumulators, one weight row a thread, and add them times
+// their scales in fp32.
+#include <cuda_fp8.h>
+
+#include <algorithm>
+
+#include "common.cuh"
+#include "tc_ptx.cuh"
+
+namespace fovea {
+namespace w4tc {
+
+using namespace tc;
+
+constexpr int kRows = 128;                 // weight rows of a tile
+constexpr int kStageK = 256;               // columns of a stage: 128 bytes of codes a row
+constexpr int kCodeBytes = kRows * 128;
+constexpr int kUnitK = 128;                // columns of an operand buffer in tensor memory
+constexpr int kMaxCols = 64;               // columns of x a launch takes
+constexpr int kBufs = 4;                   // operand buffers, and accumulators
+constexpr int kMaxStages = 6;
+constexpr int kSumWarps = 4, kIntWarps = 8;
+constexpr int kThreads = 32 * (kSumWarps + kIntWarps + 2);
+constexpr int kBarBytes = 1024;
+constexpr int kSmemBudget = 224 * 1024;
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kAccCol = 256;          // accumulators follow the operand buffers (64 columns each)
+
+struct Args {
+  W4 w;
+  int groups;
+  int cols, cols_pad;                // columns of x (rows times parts); padded to 16
+  int parts;                         // columns a row of x is the sum of
+  int n0, rows;                      // rows of y
+  const float* x_scale;              // by_group: [groups, kMaxCols]; else [kMaxCols] or null
+  bool by_group;
+  const float* bias;
+  void* y; int y_dtype;
+  long long ldy;
+  int stages, ksteps, tiles, split;  // ring depth; stages of the contraction; tiles; CTAs a tile
+  unsigned long long wait_ns;
+  int* err;
+};
+
+__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc,
+                                        uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]),
+      "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+      "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, uint64_t* bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ float ld_dsmem_f32(uint32_t caddr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(caddr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t bf16_sub2(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// y of row n of the block and weight row o.
+__device__ __forceinline__ void store_y(const Args& a, long long o, int n, float v) {
+  if (!a.by_group && a.x_scale != nullptr) v *= __ldg(a.x_scale + n * a.parts);
+  if (a.bias != nullptr) v += __ldg(a.bias + o);
+  const long long at = (long long)(a.n0 + n) * a.ldy + o;
+  if (a.y_dtype == FOVEA_BF16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
+  else static_cast<float*>(a.y)[at] = v;
+}
+
+// NC: accumulator columns (a multiple of 16, cols_pad).  A tile's contraction may
+// be split over the CTAs of a cluster, which then has one tile.
+template <int NC>
+__global__ void __launch_bounds__(kThreads, 1)
+linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
+                    const __grid_constant__ Args a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  constexpr int kXBlock = NC * 128;                        // 64 k of every column
+  constexpr int kStageBytes = kCodeBytes + 4 * kXBlock;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + a.stages * kStageBytes);
+  uint64_t* empty = full + kMaxStages;
+  uint64_t* afull = empty + kMaxStages;
+  uint64_t* aempty = afull + kBufs;
+  uint64_t* dfull = aempty + kBufs;
+  uint64_t* dempty = dfull + kBufs;
+  uint64_t* drain = dempty + kBufs;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int split = a.split;
+  const int rank = split > 1 ? (int)cluster_rank() : 0;
+  const int first = (int)blockIdx.x / split, step = (int)gridDim.x / split;
+  const int k_lo = a.ksteps * rank / split, k_hi = a.ksteps * (rank + 1) / split;
+  const int per_unit = kUnitK / a.w.group;                 // groups in a unit: 1, 2 or 4
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kMaxStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    for (int i = 0; i < kBufs; ++i) {
+      mbar_init(&afull[i], kIntWarps);
+      mbar_init(&aempty[i], 1);
+      mbar_init(&dfull[i], 1);
+      mbar_init(&dempty[i], kSumWarps);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    prefetch_tmap(&tmW);
+    prefetch_tmap(&tmX);
+  }
+  if (warp == 0) {
+    tmem_alloc(tmem_slot, kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_trigger();
+
+  if (warp == kSumWarps + kIntWarps) {
+    // ---- copies.  The codes may be read before the wait: the kernel in front
+    // (the one that lays x out) had waited for whatever came before it when it let
+    // this one start.
+    if (lane == 0) {
+      bool waited = false, go = true;
+      int i = 0;
+      for (int t = first; go && t < a.tiles; t += step) {
+        for (int k = k_lo; k < k_hi; ++k, ++i) {
+          const int st = i % a.stages;
+          if (i >= a.stages &&
+              !mbar_wait(&empty[st], ((uint32_t)(i / a.stages) & 1u) ^ 1u, abort_flag, a.wait_ns)) {
+            *abort_flag = 1;
+            go = false;
+            break;
+          }
+          uint8_t* dst = smem + st * kStageBytes;
+          mbar_expect_tx(&full[st], (uint32_t)kStageBytes);
+          tma_load_2d(dst, &tmW, &full[st], k * (kStageK / 2), t * kRows);
+          if (waited) {
+            tma_load_3d(dst + kCodeBytes, &tmX, &full[st], 0, 0, k * 4);
+          } else if (i + 1 == a.stages || (t + step >= a.tiles && k + 1 == k_hi)) {
+            // the ring is full of codes: now x of the same stages
+            pdl_wait();
+            waited = true;
+            for (int j = 0; j <= i; ++j)
+              tma_load_3d(smem + j * kStageBytes + kCodeBytes, &tmX, &full[j], 0, 0,
+                          (k_lo + j % (k_hi - k_lo)) * 4);
+          }
+        }
+      }
+      if (!waited) pdl_wait();
+    }
+  } else if (warp == kSumWarps + kIntWarps + 1) {
+    // ---- MMAs
+    const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NC >> 3) << 17) |
+                           ((uint32_t)(kRows >> 4) << 24);
+    const uint64_t desc0 = sw128_desc(smem_u32(smem) + kCodeBytes);
+    int i = 0, u = 0, d = 0;                               // stages, units, accumulators so far
+    bool go = true;
+    for (int t = first; go && t < a.tiles; t += step) {
+      for (int k = k_lo; go && k < k_hi; ++k, ++i) {
+        const int st = i % a.stages;
+        if (!__all_sync(0xffffffffu, mbar_wait(&full[st], (uint32_t)(i / a.stages) & 1u, abort_flag, a.wait_ns)))
+          go = false;
+        for (int h = 0; go && h < 2; ++h, ++u) {
+          const int ab = u % kBufs;
+          if (!__all_sync(0xffffffffu, mbar_wait(&afull[ab], (uint32_t)(u / kBufs) & 1u, abort_flag, a.wait_ns))) {
+            go = false;
+            break;
+          }
+          for (int s = 0; s < per_unit; ++s, ++d) {
+            const int db = d % kBufs;
+            if (d >= kBufs && !__all_sync(0xffffffffu, mbar_wait(&dempty[db], ((uint32_t)(d / kBufs) & 1u) ^ 1u,
+                                                                 abort_flag, a.wait_ns))) {
+              go = false;
+              break;
+            }
+            tc_fence_after();
+            if (elect_one()) {
+              const int steps = 8 / per_unit;
+              for (int q = 0; q < steps; ++q) {
+                const int k16 = s * steps + q;             // of the unit's eight
+                const uint64_t b = desc0 + (uint64_t)((st * kStageBytes + (2 * h + (k16 >> 2)) * kXBlock) >> 4) +
+                                   (uint64_t)(2 * (k16 & 3));
+                umma_ts(tmem_base + kAccCol + (uint32_t)(db * 64), tmem_base + (uint32_t)(ab * 64 + k16 * 8), b, idesc,
+                        q > 0 ? 1u : 0u);
+              }
+              umma_commit(&dfull[db]);
+            }
+            __syncwarp();
+          }
+          if (go && elect_one()) {
+            umma_commit(&aempty[ab]);
+            if (h == 1) umma_commit(&empty[st]);
+          }
+          __syncwarp();
+        }
+      }
+    }
+    if (!go) *abort_flag = 1;
+  } else if (warp >= kSumWarps) {
+    // ---- codes to integers: thread = weight row, half a unit's columns
+    const int quarter = warp & 3, half = (warp - kSumWarps) >> 2;
+    const int r = quarter * 32 + lane;
+    int i = 0, u = 0;
+    bool go = true;
+    for (int t = first; go && t < a.tiles; t += step) {
+      const long long row = min((long long)t * kRows + r, (long long)a.w.out - 1);
+      const uint8_t* zeros = a.w.zeros != nullptr ? a.w.zeros + row * a.groups : nullptr;
+      for (int k = k_lo; go && k < k_hi; ++k, ++i) {
+        const int st = i % a.stages;
+        uint32_t z[4];                                     // of this half: two 32-column runs in each unit
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int g = (k * kStageK + (q >> 1) * kUnitK + half * 64 + (q & 1) * 32) / a.w.group;
+          z[q] = zeros != nullptr && g < a.groups ? __ldg(zeros + g) : 8u;
+          z[q] = 0x43004300u | z[q] * 0x10001u;
+        }
+        if (!__all_sync(0xffffffffu, mbar_wait(&full[st], (uint32_t)(i / a.stages) & 1u, abort_flag, a.wait_ns))) {
+          go = false;
+          break;
+        }
+        const uint8_t* src = smem + st * kStageBytes + r * 128;
+#pragma unroll
+        for (int h = 0; h < 2; ++h, ++u) {
+          const int ab = u % kBufs;
+          uint32_t v[32];
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const uint4 w = *reinterpret_cast<const uint4*>(src + (((h * 4 + half * 2 + q) ^ (r & 7)) << 4));
+            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+            const uint32_t zq = z[2 * h + q];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int p = 0; p < 4; ++p)
+                // 0x4300 | c is the bf16 number 128 + c
+                v[16 * q + 4 * j + p] = bf16_sub2(((ww[j] >> (4 * p)) & 0x000F000Fu) | 0x43004300u, zq);
+          }
+          if (u >= kBufs && !__all_sync(0xffffffffu, mbar_wait(&aempty[ab], ((uint32_t)(u / kBufs) & 1u) ^ 1u,
+                                                               abort_flag, a.wait_ns))) {
+            go = false;
+            break;
+          }
+          tc_fence_after();
+          tmem_st32(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(ab * 64 + half * 32), v);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&afull[ab]);
+        }
+      }
+    }
+    if (!go) *abort_flag = 1;
+  } else {
+    // ---- sums: thread = weight row
+    const int r = warp * 32 + lane;
+    const uint32_t lanes = tmem_base + ((uint32_t)(warp * 32) << 16) + kAccCol;
+    const int slots = (k_hi - k_lo) * 2 * per_unit, g0 = k_lo * 2 * per_unit;
+    int d = 0;
+    bool go = true;
+    for (int t = first; t < a.tiles; t += step) {
+      const long long o = (long long)t * kRows + r;
+      const __nv_bfloat16* scales = a.w.scales + min(o, (long long)a.w.out - 1) * a.groups;
+      float acc[NC];
+#pragma unroll
+      for (int j = 0; j < NC; ++j) acc[j] = 0.0f;
+      constexpr int kAhead = 4;                            // scales on their way
+      float s[kAhead];
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q)
+        s[q] = q < slots && g0 + q < a.groups ? __bfloat162float(scales[g0 + q]) : 0.0f;
+      for (int i0 = 0; go && i0 < slots; i0 += kAhead) {
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+          const int i = i0 + q;
+          if (i >= slots || !go) break;
+          const int db = d % kBufs;
+          if (!__all_sync(0xffffffffu, mbar_wait(&dfull[db], (uint32_t)(d / kBufs) & 1u, abort_flag, a.wait_ns))) {
+            go = false;
+            break;
+          }
+          ++d;
+          tc_fence_after();
+          const float sc = s[q];
+          const int next = g0 + i + kAhead;
+          s[q] = i + kAhead < slots && next < a.groups ? __bfloat162float(scales[next]) : 0.0f;
+          const float4* xs = a.by_group ? reinterpret_cast<const float4*>(a.x_scale + (long long)min(g0 + i, a.groups - 1) * kMaxCols) : nullptr;
+          if (i == 0 && t == first) pdl_wait();            // x's scales come from the kernel in front
+#pragma unroll
+          for (int c = 0; c < NC / 16; ++c) {
+            float v[16];
+            tmem_ld16(lanes + (uint32_t)(db * 64 + 16 * c), v);
+            if (c == NC / 16 - 1) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&dempty[db]);
+            }
+            if (xs != nullptr) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float4 f = xs[4 * c + j];
+                acc[16 * c + 4 * j] = fmaf(v[4 * j], sc * f.x, acc[16 * c + 4 * j]);
+                acc[16 * c + 4 * j + 1] = fmaf(v[4 * j + 1], sc * f.y, acc[16 * c + 4 * j + 1]);
+                acc[16 * c + 4 * j + 2] = fmaf(v[4 * j + 2], sc * f.z, acc[16 * c + 4 * j + 2]);
+                acc[16 * c + 4 * j + 3] = fmaf(v[4 * j + 3], sc * f.w, acc[16 * c + 4 * j + 3]);
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) acc[16 * c + j] = fmaf(v[j], sc, acc[16 * c + j]);
+            }
+          }
+        }
+      }
+      if (!go) {                                           // a result that shows it
+        *abort_flag = 1;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) acc[j] = __int_as_float(0x7FC00000);
+      }
+      pdl_wait();
+      if (split > 1) {
+        // every stage has been consumed: the ring takes the partial tile, [column][row]
+        float* part = reinterpret_cast<float*>(smem);
+#pragma unroll
+        for (int j = 0; j < NC; ++j) part[j * kRows + r] = acc[j];
+      } else if (o < a.w.out) {
+        if (a.parts == 1) {
+#pragma unroll
+          for (int j = 0; j < NC; ++j)
+            if (j < a.cols) store_y(a, o, j, acc[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j + 2 < NC; j += 3)
+            if (j < a.cols) store_y(a, o, j / 3, acc[j] + acc[j + 1] + acc[j + 2]);
+        }
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (*abort_flag != 0) {
+    if (threadIdx.x == 0) atomicOr(a.err, kErrTimeout);
+    if (warp == kSumWarps + kIntWarps + 1 && elect_one()) umma_commit(drain);    // the issuing warp's MMAs
+    if (lane == 0) {
+      mbar_wait(drain, 0, nullptr, kDefaultWaitLimitNs);
+      const uint64_t t0 = globaltimer_ns();                // copies in flight land
+      while (globaltimer_ns() - t0 < 2000000ull) {}
+    }
+    __syncwarp();
+    __syncthreads();
+  }
+  if (split > 1) {
+    // the CTAs' partial tiles meet: CTA `rank` sums every split-th row of y over
+    // them in rank order
+    cluster_sync();
+    const int r = threadIdx.x & (kRows - 1);
+    const long long o = (long long)first * kRows + r;
+    const uint32_t part = smem_u32(smem);
+    constexpr int kLanes = kThreads / kRows;
+    if (threadIdx.x < kLanes * kRows && o < a.w.out) {
+      for (int n = rank + split * (int)(threadIdx.x / kRows); n < a.rows; n += split * kLanes) {
+        float v = 0.0f;
+        for (int p = 0; p < a.parts; ++p)
+          for (int q = 0; q < split; ++q)
+            v += ld_dsmem_f32(map_dsmem(part + (uint32_t)(((n * a.parts + p) * kRows + r) * 4), (uint32_t)q));
+        store_y(a, o, n, v);
+      }
+    }
+    cluster_sync();
+  }
+  if (warp == 0) tmem_dealloc(tmem_base, kTmemCols);
+}
+
+// x as the product's second operand: out[c, k] bf16, c = block * kMaxCols + the
+// block's column, k padded to whole stages; every eight k in the order 0 4 1 5 2
+// 6 3 7; and its scales as [groups or 1, kMaxCols] per block.
+struct LayoutArgs {
+  const void* x; long long ld; int dtype;
+  const float* x_scale; int x_groups;      // 0: none; 1: one a row; else per group
+  int N, in, k_pad;
+  int rows_block, blocks, parts;
+  __nv_bfloat16* out;
+  float* scale_out;
+  int* err;
+};
+constexpr int kLayoutThreads = 256;
+
+__device__ __forceinline__ void split3(float v, uint32_t& b0, uint32_t& b1, uint32_t& b2) {
+  const uint32_t bits = __float_as_uint(v);
+  if ((bits & 0x7F800000u) == 0x7F800000u) {               // infinity, NaN
+    b0 = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+    b1 = b2 = 0u;
+  } else {                                                 // v is the sum of its three truncations
+    b0 = bits >> 16;
+    const float r1 = v - __uint_as_float(b0 << 16);
+    b1 = __float_as_uint(r1) >> 16;
+    b2 = __float_as_uint(r1 - __uint_as_float(b1 << 16)) >> 16;
+  }
+}
+
+__global__ void __launch_bounds__(kLayoutThreads) layout_x_kernel(const LayoutArgs a) {
+  pdl_wait();
+  pdl_trigger();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.err = 0;
+  const int units = a.k_pad / 8;
+  const int slots = kMaxCols / a.parts;                    // rows of a block, padding among them
+  const long long row_items = (long long)a.blocks * slots * units;
+  const long long total = row_items + (long long)a.x_groups * a.blocks * kMaxCols;
+  for (long long it = blockIdx.x * kLayoutThreads + threadIdx.x; it < total; it += gridDim.x * kLayoutThreads) {
+    if (it >= row_items) {                                 // [block][group][column]
+      const long long j = it - row_items;
+      const int c = (int)(j % kMaxCols), g = (int)(j / kMaxCols % a.x_groups), b = (int)(j / (kMaxCols * a.x_groups));
+      const int n = b * a.rows_block + c;
+      a.scale_out[j] = c < a.rows_block && n < a.N ? a.x_scale[(long long)n * a.x_groups + g] : 0.0f;
+      continue;
+    }
+    const int unit = (int)(it % units), slot = (int)(it / units % slots), b = (int)(it / ((long long)units * slots));
+    const int n = b * a.rows_block + slot, k0 = unit * 8;
+    uint32_t pk[3][4] = {};
+    if (slot < a.rows_block && n < a.N && k0 < a.in) {
+      constexpr int order[8] = {0, 4, 1, 5, 2, 6, 3, 7};
+      const long long at = (long long)n * a.ld + k0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t b0 = 0, b1 = 0, b2 = 0;
+        if (a.dtype == FOVEA_BF16) {
+          b0 = static_cast<const uint16_t*>(a.x)[at + order[i]];
+        } else if (a.dtype == FOVEA_FP32) {
+          split3(static_cast<const float*>(a.x)[at + order[i]], b0, b1, b2);
+        } else {
+          const __half h = __half(__nv_cvt_fp8_to_halfraw(static_cast<const uint8_t*>(a.x)[at + order[i]], __NV_E4M3));
+          b0 = __bfloat16_as_ushort(__float2bfloat16_rn(__half2float(h)));
+        }
+        pk[0][i / 2] |= b0 << (16 * (i & 1));
+        pk[1][i / 2] |= b1 << (16 * (i & 1));
+        pk[2][i / 2] |= b2 << (16 * (i & 1));
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+      if (p < a.parts)
+        *reinterpret_cast<uint4*>(a.out + ((long long)b * kMaxCols + slot * a.parts + p) * a.k_pad + k0) =
+            make_uint4(pk[p][0], pk[p][1], pk[p][2], pk[p][3]);
+  }
+}
+
+struct Plan {
+  int parts, rows_block, blocks, k_pad;
+  size_t scale_at, bytes;
+};
+static Plan plan(int N, int in, int group, int x_dtype, bool by_group) {
+  Plan p;
+  p.parts = x_dtype == FOVEA_FP32 ? 3 : 1;
+  p.rows_block = kMaxCols / p.parts;
+  p.blocks = (N + p.rows_block - 1) / p.rows_block;
+  p.k_pad = (in + kStageK - 1) / kStageK * kStageK;
+  p.scale_at = kWsHeaderBytes + (size_t)p.blocks * kMaxCols * p.k_pad * 2;
+  const int groups = x_dtype != FOVEA_E4M3 ? 0 : by_group ? (in + group - 1) / group : 1;
+  p.bytes = p.scale_at + (size_t)p.blocks * kMaxCols * groups * 4;
+  return p;
+}
+
+template <int NC>
+static cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmX, Args& a, cudaStream_t s) {
+  auto kern = linear_w4_tc_kernel<NC>;
+  constexpr int stage = kCodeBytes + 4 * NC * 128;
+  a.stages = std::min(kMaxStages, (kSmemBudget - kBarBytes - 1024) / stage);
+  const size_t smem = 1024 + (size_t)a.stages * stage + kBarBytes;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  const int groups = a.split > 1 ? a.tiles : std::min(a.tiles, 152);
+  cfg.gridDim = dim3(groups * a.split);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = a.split;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, tmW, tmX, a);
+}
+
+}  // namespace w4tc
+
+size_t linear_w4_tc_workspace(int N, int in, int group, int x_dtype, bool by_group) {
+  return w4tc::plan(N, in, group, x_dtype, by_group).bytes;
+}
+
+cudaError_t launch_linear_w4_tc(const LinearW4Args& l, cudaStream_t s) {
+  using namespace w4tc;
+  const bool by_group = l.x_group != 0;
+  const Plan p = plan(l.N, l.w.in, l.w.group, l.x_dtype, by_group);
+  uint8_t* ws = static_cast<uint8_t*>(l.workspace);
+  const int groups = (l.w.in + l.w.group - 1) / l.w.group;
+  LayoutArgs x{};
+  x.x = l.x; x.ld = l.x_ld; x.dtype = l.x_dtype;
+  x.x_scale = l.x_scale; x.x_groups = l.x_scale == nullptr ? 0 : by_group ? groups : 1;
+  x.N = l.N; x.in = l.w.in; x.k_pad = p.k_pad;
+  x.rows_block = p.rows_block; x.blocks = p.blocks; x.parts = p.parts;
+  x.out = reinterpret_cast<__nv_bfloat16*>(ws + kWsHeaderBytes);
+  x.scale_out = reinterpret_cast<float*>(ws + p.scale_at);
+  x.err = reinterpret_cast<int*>(ws);
+  const long long items = (long long)p.blocks * kMaxCols * (p.k_pad / 8 + x.x_groups);
+  const int grid = (int)std::min<long long>((items + kLayoutThreads - 1) / kLayoutThreads, 152 * 8);
+  cudaError_t e = launch_pdl(layout_x_kernel, dim3(grid), dim3(kLayoutThreads), 0, s, x);
+  if (e != cudaSuccess) return e;
+
+  CUtensorMap tmW, tmX;
+  if (!encode_byte_map(&tmW, l.w.codes, l.w.out, l.w.in / 2, kRows)) return cudaErrorInvalidValue;
+  for (int b = 0; b < p.blocks; ++b) {
+    Args a{};
+    a.w = l.w;
+    a.groups = groups;
+    a.n0 = b * p.rows_block;
+    a.rows = std::min(p.rows_block, l.N - a.n0);
+    a.parts = p.parts;
+    a.cols = a.rows * p.parts;
+    a.cols_pad = (a.cols + 15) / 16 * 16;
+    a.by_group = by_group;
+    a.x_scale = x.x_groups == 0 ? nullptr : x.scale_out + (size_t)b * kMaxCols * x.x_groups;
+    a.bias = l.bias;
+    a.y = l.y; a.y_dtype = l.y_dtype; a.ldy = l.w.out;
+    a.ksteps = p.k_pad / kStageK;
+    a.tiles = (l.w.out + kRows - 1) / kRows;
+    // one tile's contraction over a cluster while the tiles leave SMs idle
+    a.split = 1;
+    while (a.split < 8 && a.tiles * a.split * 2 <= 152 && a.split * 2 <= a.ksteps) a.split *= 2;
+    a.wait_ns = wait_limit_ns();
+    a.err = x.err;
+    const TmaOperand xop{x.out + (size_t)b * kMaxCols * p.k_pad, a.cols_pad, p.k_pad, p.k_pad};
+    if (!encode_kblock_map(&tmX, xop, a.cols_pad, kStageK / 64)) return cudaErrorInvalidValue;
+    e = a.cols_pad == 16 ? launch<16>(tmW, tmX, a, s)
+        : a.cols_pad == 32 ? launch<32>(tmW, tmX, a, s)
+        : a.cols_pad == 48 ? launch<48>(tmW, tmX, a, s) : launch<64>(tmW, tmX, a, s);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+}  // namespace fovea

@@ -38,7 +38,7 @@ EXPORTS = (
     "fovea_retrieve_fuse_noalloc", "fovea_noalloc_sync_errors", "fovea_memory_folded_keys",
     "fovea_lm_head_topk", "fovea_debug_wait_limit", "fovea_lm_head_workspace_size",
     "fovea_add_rms_norm", "fovea_quantize_w4", "fovea_linear_w4", "fovea_token_logprobs",
-    "fovea_token_logprobs_grad",
+    "fovea_token_logprobs_grad", "fovea_linear_w4_workspace_size",
 )
 NOALLOC_WORKSPACE_BYTES = 32 << 20
 
@@ -107,7 +107,9 @@ def lib() -> ctypes.CDLL:
         i, i64, f32 = ctypes.c_int, ctypes.c_int64, ctypes.c_float
         L.fovea_add_rms_norm.argtypes = [vp, i64, vp, i64, vp, i, i, i, f32, vp, vp, vp, vp, i, vp]
         L.fovea_quantize_w4.argtypes = [vp, i64, i, i, i, i, vp, vp, vp, vp]
-        L.fovea_linear_w4.argtypes = [vp, i64, i, vp, i, i, vp, vp, vp, vp, i, i, i, vp, i, vp]
+        L.fovea_linear_w4.argtypes = [vp, i64, i, vp, i, i, vp, vp, vp, vp, i, i, i, vp, i, vp,
+                                      ctypes.c_size_t, vp]
+        L.fovea_linear_w4_workspace_size.argtypes = [i, i, i, i, i, ctypes.POINTER(ctypes.c_size_t)]
         L.fovea_token_logprobs.argtypes = [vp, i64, i, i, i, vp, vp, i64, vp, i, i, vp, vp, vp, vp,
                                            vp, vp, vp]
         L.fovea_token_logprobs_grad.argtypes = [vp, i64, i, i, i, vp, vp, i64, vp, vp, vp, vp, i,
@@ -117,7 +119,7 @@ def lib() -> ctypes.CDLL:
                      "fovea_workspace_size", "fovea_workspace_init", "fovea_retrieve_fuse",
                      "fovea_sync_errors", "fovea_timing_enable", "fovea_add_rms_norm",
                      "fovea_quantize_w4", "fovea_linear_w4", "fovea_token_logprobs",
-                     "fovea_token_logprobs_grad"):
+                     "fovea_token_logprobs_grad", "fovea_linear_w4_workspace_size"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -380,61 +382,70 @@ def lm_head_topk(W_LM: torch.Tensor, h_hat: torch.Tensor, k_c: int, workspace: t
 
 _DTYPES = {torch.bfloat16: BF16, torch.float32: FP32, torch.float8_e4m3fn: E4M3}
 _ROW_TYPES = (torch.bfloat16, torch.float32)
+_X_TYPES = (torch.bfloat16, torch.float32, torch.float8_e4m3fn)
 
 
-def _need(name: str, t, shape, dtypes) -> None:
-    """t is a CUDA tensor of one of these types and this shape (None: any
-    size), contiguous along its last dimension."""
+def _refuse(name: str, t, shape, dtypes, dense: bool) -> None:
+    """The error of a tensor that is not on the GPU, not of one of these types,
+    not of this shape (None: any size), or not contiguous (along its rows)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
     if t.dtype not in dtypes:
         raise ValueError(f"{name} has type {t.dtype}; expected {' or '.join(map(str, dtypes))}")
-    s = t.shape
-    if len(s) != len(shape) or any(want is not None and have != want for have, want in zip(s, shape)):
-        raise ValueError(f"{name} has shape {list(s)}; expected {list(shape)} (None: any)")
-    if len(s) == 2 and s[1] > 1 and t.stride(1) != 1:
+    have = tuple(t.shape)
+    if len(have) != len(shape) or any(w is not None and h != w for h, w in zip(have, shape)):
+        raise ValueError(f"{name} has shape {list(have)}; expected {list(shape)} (None: any)")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if len(have) == 2 and have[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must be contiguous along its rows")
 
 
-def _need_dense(name: str, t, shape, dtypes) -> None:
-    _need(name, t, shape, dtypes)
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+# The checks below cost a call about a third of a microsecond each; _refuse
+# finds the words when one fails.
+
+def _need_rows(name: str, t, dtypes):
+    """t is a CUDA matrix of one of these types with contiguous rows: its (rows,
+    columns, row stride)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.dim() != 2:
+        _refuse(name, t, (None, None), dtypes, False)
+    n, m = t.shape
+    ld, inner = t.stride()
+    if inner != 1 and m > 1:
+        _refuse(name, t, (None, None), dtypes, False)
+    return n, m, ld if n > 1 else m
 
 
-def _ld(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _need(name: str, t, shape, dtype) -> int:
+    """t is a contiguous CUDA tensor of this type and shape: its address."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not dtype or t.shape != shape \
+            or not t.is_contiguous():
+        _refuse(name, t, shape, (dtype,), True)
+    return t.data_ptr()
 
 
-class _On:
-    """The stream of a call that allocates its outputs.  None: the current one.
-    On another stream the outputs come from that stream's pool and the inputs are
-    recorded as used there, so that neither memory is reused too early; ordering
-    the streams themselves stays with the caller."""
+def _side_stream(stream, device, raw, inputs):
+    """A call on another stream than the current one: (its handle, an allocator
+    from its pool).  The inputs are recorded as used there, so that neither memory
+    is reused too early; ordering the streams themselves stays with the caller."""
+    side = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if side == raw:
+        return raw, torch.empty
+    s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(side, device)
+    for t in inputs:
+        if t is not None:
+            t.record_stream(s)
 
-    def __init__(self, stream, device, *inputs):
-        self.device = device
-        self.other = None
-        if stream is None:
-            self.raw = torch._C._cuda_getCurrentRawStream(device.index)
-            return
-        raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
-        self.raw = raw
-        if raw != torch._C._cuda_getCurrentRawStream(device.index):
-            self.other = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(raw, device)
-            for t in inputs:
-                if t is not None:
-                    t.record_stream(self.other)
-
-    def empty(self, shape, dtype) -> torch.Tensor:
-        if self.other is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        with torch.cuda.stream(self.other):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+    def empty(shape, **kw):
+        with torch.cuda.stream(s):
+            return torch.empty(shape, **kw)
+    return side, empty
 
 
-def _at(t: Optional[torch.Tensor]) -> Optional[int]:
-    return None if t is None else t.data_ptr()
+def _on(stream, device, *inputs):
+    """(stream handle, allocator of outputs) of a call; stream None: the current one."""
+    raw = torch._C._cuda_getCurrentRawStream(device.index)
+    return (raw, torch.empty) if stream is None else _side_stream(stream, device, raw, inputs)
 
 
 def add_rms_norm(x: torch.Tensor, gamma: torch.Tensor, residual: Optional[torch.Tensor] = None, *,
@@ -448,28 +459,38 @@ def add_rms_norm(x: torch.Tensor, gamma: torch.Tensor, residual: Optional[torch.
       q8_scale  its scales, fp32: [N] for q8_group = 0 (a scale per row), else
                 [N, ceil(d / q8_group)] for q8_group of 32, 64 or 128 columns
                 (both only when q8_group is given)."""
-    _need("x", x, (None, None), _ROW_TYPES)
-    N, d = x.shape
-    dt = (x.dtype,)
-    _need_dense("gamma", gamma, (d,), dt)
+    N, d, ld = _need_rows("x", x, _ROW_TYPES)
+    dt, dev = x.dtype, x.device
+    gamma_at = _need("gamma", gamma, (d,), dt)
+    residual_at, residual_ld = None, 0
     if residual is not None:
-        _need("residual", residual, (N, d), dt)
-    if residual is None and not want_out and q8_group is None:
+        n, m, residual_ld = _need_rows("residual", residual, (dt,))
+        if n != N or m != d:
+            _refuse("residual", residual, (N, d), (dt,), False)
+        residual_at = residual.data_ptr()
+    elif not want_out and q8_group is None:
         raise ValueError("nothing to compute: no residual, want_out=False and no q8_group")
-    if q8_group is not None and q8_group not in (0, 32, 64, 128):
+    if q8_group not in (None, 0, 32, 64, 128):
         raise ValueError(f"q8_group {q8_group} is not None, 0, 32, 64 or 128")
-    on = _On(stream, x.device, x, gamma, residual)
-    s = on.empty((N, d), x.dtype) if residual is not None else None
-    out = on.empty((N, d), x.dtype) if want_out else None
-    r = dict(sum=s, out=out)
-    q8 = scale = None
+    raw, empty = _on(stream, dev, x, gamma, residual)
+    s = out = q8 = scale = None
+    s_at = out_at = q8_at = scale_at = None
+    if residual is not None:
+        s = empty((N, d), dtype=dt, device=dev)
+        s_at = s.data_ptr()
+    if want_out:
+        out = empty((N, d), dtype=dt, device=dev)
+        out_at = out.data_ptr()
+    r = {"sum": s, "out": out}
     if q8_group is not None:
-        r["q8"] = q8 = on.empty((N, d), torch.float8_e4m3fn)
-        r["q8_scale"] = scale = on.empty((N, -(-d // q8_group)) if q8_group else (N,), torch.float32)
-    _check(lib().fovea_add_rms_norm(x.data_ptr(), _ld(x), _at(residual),
-                                    _ld(residual) if residual is not None else 0, gamma.data_ptr(),
-                                    N, d, _DTYPES[x.dtype], eps, _at(s), _at(out), _at(q8),
-                                    _at(scale), q8_group or 0, on.raw))
+        r["q8"] = q8 = empty((N, d), dtype=torch.float8_e4m3fn, device=dev)
+        r["q8_scale"] = scale = empty((N, -(-d // q8_group)) if q8_group else (N,),
+                                      dtype=torch.float32, device=dev)
+        q8_at, scale_at = q8.data_ptr(), scale.data_ptr()
+    st = lib().fovea_add_rms_norm(x.data_ptr(), ld, residual_at, residual_ld, gamma_at, N, d,
+                                  _DTYPES[dt], eps, s_at, out_at, q8_at, scale_at, q8_group or 0, raw)
+    if st:
+        _check(st)
     return r
 
 
@@ -480,71 +501,108 @@ def quantize_w4(W: torch.Tensor, group: int = 128, *, symmetric: bool = True,
     codes [out, in / 2] uint8 (the even column in the low four bits), scales
     [out, ceil(in / group)] bf16 and zeros (uint8, like scales; None: symmetric,
     8 everywhere), as linear_w4 takes them."""
-    _need("W", W, (None, None), _ROW_TYPES)
-    out_f, in_f = W.shape
+    out_f, in_f, ld = _need_rows("W", W, _ROW_TYPES)
     if group not in (32, 64, 128):
         raise ValueError(f"group {group} is not 32, 64 or 128")
-    on = _On(stream, W.device, W)
+    dev = W.device
+    raw, empty = _on(stream, dev, W)
     groups = -(-in_f // group)
-    codes = on.empty((out_f, in_f // 2), torch.uint8)
-    scales = on.empty((out_f, groups), torch.bfloat16)
-    zeros = None if symmetric else on.empty((out_f, groups), torch.uint8)
-    _check(lib().fovea_quantize_w4(W.data_ptr(), _ld(W), out_f, in_f, _DTYPES[W.dtype], group,
-                                   codes.data_ptr(), scales.data_ptr(), _at(zeros), on.raw))
-    return dict(codes=codes, scales=scales, zeros=zeros)
+    codes = empty((out_f, in_f // 2), dtype=torch.uint8, device=dev)
+    scales = empty((out_f, groups), dtype=torch.bfloat16, device=dev)
+    zeros = None if symmetric else empty((out_f, groups), dtype=torch.uint8, device=dev)
+    st = lib().fovea_quantize_w4(W.data_ptr(), ld, out_f, in_f, _DTYPES[W.dtype], group,
+                                 codes.data_ptr(), scales.data_ptr(),
+                                 None if symmetric else zeros.data_ptr(), raw)
+    if st:
+        _check(st)
+    return {"codes": codes, "scales": scales, "zeros": zeros}
+
+
+W4_FEW_ROWS = 5         # up to here linear_w4 needs no workspace, whatever x's type
+
+
+def linear_w4_workspace_size(N: int, in_features: int, group: int = 128,
+                             dtype: torch.dtype = torch.bfloat16, x_group: int = 0) -> int:
+    """fovea_linear_w4_workspace_size: bytes linear_w4 needs for N rows of x (0:
+    none; x_group: group when x_scale has a scale per group)."""
+    n = ctypes.c_size_t()
+    _check(lib().fovea_linear_w4_workspace_size(N, in_features, group, _DTYPES[dtype], x_group,
+                                                ctypes.byref(n)))
+    return n.value
 
 
 def linear_w4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
               zeros: Optional[torch.Tensor] = None, *, group: int = 128,
               x_scale: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
-              out_dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
+              out_dtype: torch.dtype = torch.float32, workspace: Optional[torch.Tensor] = None,
+              stream=None) -> torch.Tensor:
     """fovea_linear_w4: y [N, out] = x W^T (+ bias) with W in 4 bits (codes,
     scales, zeros and group as quantize_w4 gives them).  x [N, in] is bf16, fp32,
     or float8_e4m3fn with x_scale [N] or [N, ceil(in / group)] fp32 (add_rms_norm's
-    q8 and q8_scale); bias [out] fp32; y is fp32 or bf16 (out_dtype)."""
-    _need("x", x, (None, None), tuple(_DTYPES))
-    N, in_f = x.shape
-    _need_dense("codes", codes, (None, in_f // 2), (torch.uint8,))
-    out_f = codes.shape[0]
+    q8 and q8_scale); bias [out] fp32; y is fp32 or bf16 (out_dtype).
+    workspace: a uint8 tensor of linear_w4_workspace_size bytes (None: allocated
+    for the call when one is needed); sync_errors(workspace) tells whether a
+    bounded device wait gave up, which also leaves NaN in y."""
+    N, in_f, ld = _need_rows("x", x, _X_TYPES)
+    dt, dev = x.dtype, x.device
     if group not in (32, 64, 128):
         raise ValueError(f"group {group} is not 32, 64 or 128")
+    out_f = codes.shape[0] if isinstance(codes, torch.Tensor) and codes.dim() == 2 else 0
+    codes_at = _need("codes", codes, (out_f, in_f // 2), torch.uint8)
     groups = -(-in_f // group)
-    _need_dense("scales", scales, (out_f, groups), (torch.bfloat16,))
+    scales_at = _need("scales", scales, (out_f, groups), torch.bfloat16)
+    zeros_at = x_scale_at = bias_at = None
     if zeros is not None:
-        _need_dense("zeros", zeros, (out_f, groups), (torch.uint8,))
-    if (x.dtype == torch.float8_e4m3fn) != (x_scale is not None):
-        raise ValueError("x_scale goes with float8_e4m3fn rows, and only with them")
+        zeros_at = _need("zeros", zeros, (out_f, groups), torch.uint8)
     x_group = 0
+    if (dt is torch.float8_e4m3fn) != (x_scale is not None):
+        raise ValueError("x_scale goes with float8_e4m3fn rows, and only with them")
     if x_scale is not None:
         x_group = group if x_scale.dim() == 2 else 0
-        _need_dense("x_scale", x_scale, (N, groups) if x_group else (N,), (torch.float32,))
+        x_scale_at = _need("x_scale", x_scale, (N, groups) if x_group else (N,), torch.float32)
     if bias is not None:
-        _need_dense("bias", bias, (out_f,), (torch.float32,))
+        bias_at = _need("bias", bias, (out_f,), torch.float32)
     if out_dtype not in _ROW_TYPES:
         raise ValueError(f"out_dtype {out_dtype} is neither bf16 nor fp32")
-    on = _On(stream, x.device, x, codes, scales, zeros, x_scale, bias)
-    y = on.empty((N, out_f), out_dtype)
-    _check(lib().fovea_linear_w4(x.data_ptr(), _ld(x), _DTYPES[x.dtype], _at(x_scale), x_group, N,
-                                 codes.data_ptr(), scales.data_ptr(), _at(zeros), _at(bias), out_f,
-                                 in_f, group, y.data_ptr(), _DTYPES[out_dtype], on.raw))
+    raw, empty = _on(stream, dev, x, codes, scales, zeros, x_scale, bias, workspace)
+    ws_at, ws_bytes = None, 0
+    if workspace is not None:
+        ws_bytes = workspace.numel()
+        ws_at = _need("workspace", workspace, (ws_bytes,), torch.uint8)
+    elif N > W4_FEW_ROWS:
+        ws_bytes = linear_w4_workspace_size(N, in_f, group, dt, x_group)
+        if ws_bytes:
+            workspace = empty((ws_bytes,), dtype=torch.uint8, device=dev)
+            ws_at = workspace.data_ptr()
+    y = empty((N, out_f), dtype=out_dtype, device=dev)
+    st = lib().fovea_linear_w4(x.data_ptr(), ld, _DTYPES[dt], x_scale_at, x_group, N, codes_at,
+                               scales_at, zeros_at, bias_at, out_f, in_f, group, y.data_ptr(),
+                               _DTYPES[out_dtype], ws_at, ws_bytes, raw)
+    if st:
+        _check(st)
     return y
 
 
 def _need_scores(logits, tokens, row_scale, allowed):
-    """Checks what both score calls take; returns (N, vocab, allowed's row stride)."""
-    _need("logits", logits, (None, None), _ROW_TYPES)
-    N, V = logits.shape
+    """Checks what both score calls take; returns (N, vocab, logits' row stride,
+    n_tokens, and the addresses of tokens, row_scale and allowed, allowed's row
+    stride)."""
+    N, V, ld = _need_rows("logits", logits, _ROW_TYPES)
+    T, tokens_at, scale_at, allowed_at, allowed_ld = 0, None, None, None, 0
     if tokens is not None:
-        _need_dense("tokens", tokens, (N, None), (torch.int32,))
+        T = tokens.shape[1] if isinstance(tokens, torch.Tensor) and tokens.dim() == 2 else 0
+        tokens_at = _need("tokens", tokens, (N, T), torch.int32)
     if row_scale is not None:
-        _need_dense("row_scale", row_scale, (N,), (torch.float32,))
-    if allowed is None:
-        return N, V, 0
-    words = (V + 31) // 32
-    _need("allowed", allowed, (None, words), (torch.int32,))
-    if allowed.shape[0] not in (1, N):
-        raise ValueError(f"allowed has {allowed.shape[0]} rows; expected {N}, or 1 for all")
-    return N, V, _ld(allowed) if allowed.shape[0] == N and N > 1 else 0
+        scale_at = _need("row_scale", row_scale, (N,), torch.float32)
+    if allowed is not None:
+        rows, words, allowed_ld = _need_rows("allowed", allowed, (torch.int32,))
+        if words != (V + 31) // 32 or rows not in (1, N):
+            raise ValueError(f"allowed has shape {list(allowed.shape)}; expected "
+                             f"[{N} or 1, {(V + 31) // 32}]")
+        allowed_at = allowed.data_ptr()
+        if rows == 1:
+            allowed_ld = 0
+    return N, V, ld, T, tokens_at, scale_at, allowed_at, allowed_ld
 
 
 def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top_k: int = 0, *,
@@ -559,23 +617,28 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
       top_idx       [N, top_k] int32, the largest logits' tokens, descending, the
                     smaller token first on ties, -1 past the tokens that have any
                     probability; top_logprobs [N, top_k] (when top_k > 0)."""
-    N, V, allowed_ld = _need_scores(logits, tokens, row_scale, allowed)
-    on = _On(stream, logits.device, logits, tokens, row_scale, allowed)
-    T = tokens.shape[1] if tokens is not None else 0
-    # one allocation for the fp32 results: [lse | entropy | stats | logprobs | top_logprobs]
-    f = on.empty((N * (4 + T + max(top_k, 0)),), torch.float32)
-    lse, entropy, stats = f[:N], f[N:2 * N], f[2 * N:4 * N].view(N, 2)
-    r = dict(lse=lse, entropy=entropy, stats=stats)
-    lp = top = idx = None
+    N, V, ld, T, tokens_at, scale_at, allowed_at, allowed_ld = _need_scores(logits, tokens, row_scale,
+                                                                            allowed)
+    dev = logits.device
+    raw, empty = _on(stream, dev, logits, tokens, row_scale, allowed)
+    f32 = torch.float32
+    lse, entropy = empty((N,), dtype=f32, device=dev), empty((N,), dtype=f32, device=dev)
+    stats = empty((N, 2), dtype=f32, device=dev)
+    r = {"lse": lse, "entropy": entropy, "stats": stats}
+    lp_at = idx_at = top_at = None
     if tokens is not None:
-        r["logprobs"] = lp = f[4 * N:(4 + T) * N].view(N, T)
+        r["logprobs"] = lp = empty((N, T), dtype=f32, device=dev)
+        lp_at = lp.data_ptr()
     if top_k > 0:
-        r["top_logprobs"] = top = f[(4 + T) * N:].view(N, top_k)
-        r["top_idx"] = idx = on.empty((N, top_k), torch.int32)
-    _check(lib().fovea_token_logprobs(logits.data_ptr(), _ld(logits), N, V, _DTYPES[logits.dtype],
-                                      _at(row_scale), _at(allowed), allowed_ld, _at(tokens), T,
-                                      top_k, _at(lp), lse.data_ptr(), entropy.data_ptr(),
-                                      stats.data_ptr(), _at(idx), _at(top), on.raw))
+        r["top_idx"] = idx = empty((N, top_k), dtype=torch.int32, device=dev)
+        r["top_logprobs"] = top = empty((N, top_k), dtype=f32, device=dev)
+        idx_at, top_at = idx.data_ptr(), top.data_ptr()
+    st = lib().fovea_token_logprobs(logits.data_ptr(), ld, N, V, _DTYPES[logits.dtype], scale_at,
+                                    allowed_at, allowed_ld, tokens_at, T, top_k, lp_at,
+                                    lse.data_ptr(), entropy.data_ptr(), stats.data_ptr(), idx_at,
+                                    top_at, raw)
+    if st:
+        _check(st)
     return r
 
 
@@ -596,32 +659,34 @@ def token_logprobs_grad(logits: torch.Tensor, stats: torch.Tensor, entropy: torc
     result when given; it may be logits itself, when dense."""
     if (tokens is None) != (grad_logprobs is None) or (top_idx is None) != (grad_top is None):
         raise ValueError("tokens and grad_logprobs, top_idx and grad_top, go together")
-    N, V, allowed_ld = _need_scores(logits, tokens, row_scale, allowed)
-    f32 = (torch.float32,)
-    _need_dense("stats", stats, (N, 2), f32)
-    _need_dense("entropy", entropy, (N,), f32)
-    T = k = 0
+    N, V, ld, T, tokens_at, scale_at, allowed_at, allowed_ld = _need_scores(logits, tokens, row_scale,
+                                                                            allowed)
+    f32 = torch.float32
+    stats_at = _need("stats", stats, (N, 2), f32)
+    entropy_at = _need("entropy", entropy, (N,), f32)
+    k, glp_at, idx_at, gtop_at, gH_at, glse_at = 0, None, None, None, None, None
     if tokens is not None:
-        T = tokens.shape[1]
-        _need_dense("grad_logprobs", grad_logprobs, (N, T), f32)
+        glp_at = _need("grad_logprobs", grad_logprobs, (N, T), f32)
     if top_idx is not None:
-        k = top_idx.shape[1]
-        _need_dense("top_idx", top_idx, (N, None), (torch.int32,))
-        _need_dense("grad_top", grad_top, (N, k), f32)
+        k = top_idx.shape[1] if isinstance(top_idx, torch.Tensor) and top_idx.dim() == 2 else 0
+        idx_at = _need("top_idx", top_idx, (N, k), torch.int32)
+        gtop_at = _need("grad_top", grad_top, (N, k), f32)
     if grad_entropy is not None:
-        _need_dense("grad_entropy", grad_entropy, (N,), f32)
+        gH_at = _need("grad_entropy", grad_entropy, (N,), f32)
     if grad_lse is not None:
-        _need_dense("grad_lse", grad_lse, (N,), f32)
-    if out is not None:
-        _need_dense("out", out, (N, V), (logits.dtype,))
-    on = _On(stream, logits.device, logits, tokens, row_scale, allowed, stats, entropy, grad_logprobs,
-             top_idx, grad_top, grad_entropy, grad_lse, out)
+        glse_at = _need("grad_lse", grad_lse, (N,), f32)
+    dt, dev = logits.dtype, logits.device
+    raw, empty = _on(stream, dev, logits, stats, entropy, tokens, grad_logprobs, top_idx, grad_top,
+                     grad_entropy, grad_lse, row_scale, allowed, out)
     if out is None:
-        out = on.empty((N, V), logits.dtype)
-    _check(lib().fovea_token_logprobs_grad(
-        logits.data_ptr(), _ld(logits), N, V, _DTYPES[logits.dtype], _at(row_scale), _at(allowed),
-        allowed_ld, stats.data_ptr(), entropy.data_ptr(), _at(tokens), _at(grad_logprobs), T,
-        _at(top_idx), _at(grad_top), k, _at(grad_entropy), _at(grad_lse), out.data_ptr(), on.raw))
+        out = empty((N, V), dtype=dt, device=dev)
+    else:
+        _need("out", out, (N, V), dt)
+    st = lib().fovea_token_logprobs_grad(logits.data_ptr(), ld, N, V, _DTYPES[dt], scale_at, allowed_at,
+                                         allowed_ld, stats_at, entropy_at, tokens_at, glp_at, T, idx_at,
+                                         gtop_at, k, gH_at, glse_at, out.data_ptr(), raw)
+    if st:
+        _check(st)
     return out
 
 

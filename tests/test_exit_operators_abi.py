@@ -28,9 +28,9 @@ def quantize(L, *, W=P, ld=128, o=4, k=128, dtype=fovea.BF16, group=128, codes=P
 
 
 def linear(L, *, x=P, ld=128, x_dtype=fovea.BF16, x_scale=None, x_group=0, N=4, codes=P, scales=P, zeros=None,
-           bias=None, o=4, k=128, group=128, y=P, y_dtype=fovea.FP32):
+           bias=None, o=4, k=128, group=128, y=P, y_dtype=fovea.FP32, ws=P, ws_bytes=1 << 30):
     return L.fovea_linear_w4(x, ld, x_dtype, x_scale, x_group, N, codes, scales, zeros, bias, o, k, group, y, y_dtype,
-                             None)
+                             ws, ws_bytes, None)
 
 
 def scores(L, *, x=P, ld=100, N=4, V=100, dtype=fovea.BF16, scale=None, allowed=None, a_ld=0, tokens=P, T=1, k=6,
@@ -60,6 +60,8 @@ BAD, NO = fovea.ERR_INVALID_ARG, fovea.ERR_UNSUPPORTED
     (linear, dict(x_scale=P), BAD), (linear, dict(x_dtype=2), BAD), (linear, dict(x_dtype=2, x_scale=P, x_group=64), BAD),
     (linear, dict(codes=P + 8), BAD), (linear, dict(scales=None), BAD), (linear, dict(bias=P + 2), BAD),
     (linear, dict(x=None), BAD), (linear, dict(y=None), BAD), (linear, dict(ld=100), BAD),
+    (linear, dict(N=17, ws=None), BAD), (linear, dict(N=17, ws=P + 16), BAD), (linear, dict(N=17, ws_bytes=5000), BAD),
+    (linear, dict(N=6, x_dtype=fovea.FP32, ws=None), BAD),
     (scores, dict(dtype=2), BAD), (scores, dict(V=0), BAD), (scores, dict(V=(1 << 24) + 1, ld=1 << 25), NO),
     (scores, dict(T=-1), BAD), (scores, dict(T=1025), NO), (scores, dict(k=33), NO), (scores, dict(k=-1), BAD),
     (scores, dict(N=-1), BAD), (scores, dict(ld=99), BAD), (scores, dict(allowed=P, a_ld=3), BAD),
@@ -78,6 +80,18 @@ def test_refusals(L, call, kw, status):
 @pytest.mark.parametrize("call", [norm, linear, scores, grad])
 def test_no_rows_is_no_work(L, call):
     assert call(L, N=0) == fovea.OK
+
+
+def test_linear_workspace_sizes():
+    import torch
+    size = fovea.linear_w4_workspace_size
+    assert size(5, 4096, dtype=torch.float32) == 0 and size(16, 4096) == 0 and size(0, 4096) == 0
+    assert size(17, 4096) >= 4096 + 17 * 4096 * 2
+    assert size(6, 4096, dtype=torch.float32) >= 4096 + 18 * 4096 * 2
+    assert size(17, 4096, dtype=torch.float8_e4m3fn, x_group=128) >= size(17, 4096) + 17 * 32 * 4
+    for bad in (dict(N=-1, in_features=64), dict(N=1, in_features=65), dict(N=1, in_features=64, group=16)):
+        with pytest.raises(fovea.FoveaError):
+            size(**bad)
 
 
 def test_binding_refuses_host_tensors():
