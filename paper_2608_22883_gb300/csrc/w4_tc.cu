@@ -31,9 +31,10 @@ constexpr int kUnitK = 128;                // columns of an operand buffer in te
 constexpr int kMaxCols = 64;               // columns of x a launch takes
 constexpr int kBufs = 4;                   // operand buffers, and accumulators
 constexpr int kMaxStages = 6;
-constexpr int kSumWarps = 4, kIntWarps = 8;
+constexpr int kSumWarps = 4, kIntWarps = 8;   // integers: two teams of four, taking turns by unit
 constexpr int kThreads = 32 * (kSumWarps + kIntWarps + 2);
 constexpr int kBarBytes = 1024;
+constexpr int kScaleBytes = kSumWarps * 2 * kMaxCols * 4;   // x's scales of two groups, a copy per warp
 constexpr int kSmemBudget = 224 * 1024;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kAccCol = 256;          // accumulators follow the operand buffers (64 columns each)
@@ -73,8 +74,8 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
       "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
-  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
   uint32_t r[16];
   asm volatile(
@@ -94,6 +95,23 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, u
       " [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y)
       : "memory");
+}
+// mbar_wait in line: a call would first wait for the caller's loads in flight,
+// and reading the clock takes longer than most of the waits here last.
+__device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
+                                           uint64_t limit_ns) {
+  const bool poll = limit_ns < kSuspendNs;                 // shorter than a suspended try may take
+  uint64_t t0 = 0;
+#pragma unroll 1
+  for (uint32_t n = 0;; ++n) {
+    if (poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
+    if (*abort_flag) return false;
+    if ((n & 3u) == 3u || poll) {
+      const uint64_t now = globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > limit_ns) return false;
+    }
+  }
 }
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
@@ -115,16 +133,49 @@ __device__ __forceinline__ uint32_t bf16_sub2(uint32_t a, uint32_t b) {
 
 // y of row n of the block and weight row o.
 __device__ __forceinline__ void store_y(const Args& a, long long o, int n, float v) {
-  if (!a.by_group && a.x_scale != nullptr) v *= __ldg(a.x_scale + n * a.parts);
+  if (!a.by_group && a.x_scale != nullptr) v *= a.x_scale[n * a.parts];
   if (a.bias != nullptr) v += __ldg(a.bias + o);
   const long long at = (long long)(a.n0 + n) * a.ldy + o;
   if (a.y_dtype == FOVEA_BF16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
   else static_cast<float*>(a.y)[at] = v;
 }
+// y of weight row o from its columns' sums.
+template <class T, int NC>
+__device__ __forceinline__ void store_rows(const Args& a, long long o, const float (&acc)[NC]) {
+  const float b = a.bias != nullptr ? __ldg(a.bias + o) : 0.0f;
+  T* y = static_cast<T*>(a.y) + (long long)a.n0 * a.ldy + o;
+  const bool scaled = !a.by_group && a.x_scale != nullptr;
+  if (a.parts == 1) {
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      if (j < a.cols) *y = from_f32<T>(fmaf(acc[j], scaled ? a.x_scale[j] : 1.0f, b));
+      y += a.ldy;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j + 2 < NC; j += 3) {
+      if (j < a.cols) *y = from_f32<T>(acc[j] + acc[j + 1] + acc[j + 2] + b);
+      y += a.ldy;
+    }
+  }
+}
 
-// NC: accumulator columns (a multiple of 16, cols_pad).  A tile's contraction may
+// A place in a ring of barriers and the parity of its round (no division in the
+// loops: one costs as much as the wait it serves).
+struct Turn {
+  int i = 0;
+  uint32_t parity = 0;
+  __device__ __forceinline__ void next(int size) {
+    if (++i == size) {
+      i = 0;
+      parity ^= 1u;
+    }
+  }
+};
+
+// NC: accumulator columns (a multiple of 16, cols_pad); G: the group.  A tile's contraction may
 // be split over the CTAs of a cluster, which then has one tile.
-template <int NC>
+template <int NC, int G>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
                     const __grid_constant__ Args a) {
@@ -132,7 +183,8 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   constexpr int kXBlock = NC * 128;                        // 64 k of every column
   constexpr int kStageBytes = kCodeBytes + 4 * kXBlock;
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + a.stages * kStageBytes);
+  float* xs_ring = reinterpret_cast<float*>(smem + a.stages * kStageBytes);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + a.stages * kStageBytes + kScaleBytes);
   uint64_t* empty = full + kMaxStages;
   uint64_t* afull = empty + kMaxStages;
   uint64_t* aempty = afull + kBufs;
@@ -147,14 +199,14 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   const int rank = split > 1 ? (int)cluster_rank() : 0;
   const int first = (int)blockIdx.x / split, step = (int)gridDim.x / split;
   const int k_lo = a.ksteps * rank / split, k_hi = a.ksteps * (rank + 1) / split;
-  const int per_unit = kUnitK / a.w.group;                 // groups in a unit: 1, 2 or 4
+  constexpr int kPerUnit = kUnitK / G;                     // groups in a unit: 1, 2 or 4
   if (threadIdx.x == 0) {
     for (int i = 0; i < kMaxStages; ++i) {
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
     }
     for (int i = 0; i < kBufs; ++i) {
-      mbar_init(&afull[i], kIntWarps);
+      mbar_init(&afull[i], kIntWarps / 2);
       mbar_init(&aempty[i], 1);
       mbar_init(&dfull[i], 1);
       mbar_init(&dempty[i], kSumWarps);
@@ -182,20 +234,19 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     if (lane == 0) {
       bool waited = false, go = true;
       int i = 0;
+      Turn st;
       for (int t = first; go && t < a.tiles; t += step) {
-        for (int k = k_lo; k < k_hi; ++k, ++i) {
-          const int st = i % a.stages;
-          if (i >= a.stages &&
-              !mbar_wait(&empty[st], ((uint32_t)(i / a.stages) & 1u) ^ 1u, abort_flag, a.wait_ns)) {
+        for (int k = k_lo; k < k_hi; ++k, ++i, st.next(a.stages)) {
+          if (i >= a.stages && !wait_phase(&empty[st.i], st.parity ^ 1u, abort_flag, a.wait_ns)) {
             *abort_flag = 1;
             go = false;
             break;
           }
-          uint8_t* dst = smem + st * kStageBytes;
-          mbar_expect_tx(&full[st], (uint32_t)kStageBytes);
-          tma_load_2d(dst, &tmW, &full[st], k * (kStageK / 2), t * kRows);
+          uint8_t* dst = smem + st.i * kStageBytes;
+          mbar_expect_tx(&full[st.i], (uint32_t)kStageBytes);
+          tma_load_2d(dst, &tmW, &full[st.i], k * (kStageK / 2), t * kRows);
           if (waited) {
-            tma_load_3d(dst + kCodeBytes, &tmX, &full[st], 0, 0, k * 4);
+            tma_load_3d(dst + kCodeBytes, &tmX, &full[st.i], 0, 0, k * 4);
           } else if (i + 1 == a.stages || (t + step >= a.tiles && k + 1 == k_hi)) {
             // the ring is full of codes: now x of the same stages
             pdl_wait();
@@ -209,85 +260,91 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
       if (!waited) pdl_wait();
     }
   } else if (warp == kSumWarps + kIntWarps + 1) {
-    // ---- MMAs
-    const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NC >> 3) << 17) |
-                           ((uint32_t)(kRows >> 4) << 24);
+    // ---- MMAs: the warp runs the loop converged, with addresses and descriptors
+    // in uniform registers; one elected lane issues
+    constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NC >> 3) << 17) |
+                                ((uint32_t)(kRows >> 4) << 24);
     const uint64_t desc0 = sw128_desc(smem_u32(smem) + kCodeBytes);
-    int i = 0, u = 0, d = 0;                               // stages, units, accumulators so far
-    bool go = true;
+    Turn st, ab, db;
+    bool go = true, reused = false;                        // an accumulator for the second time
     for (int t = first; go && t < a.tiles; t += step) {
-      for (int k = k_lo; go && k < k_hi; ++k, ++i) {
-        const int st = i % a.stages;
-        if (!__all_sync(0xffffffffu, mbar_wait(&full[st], (uint32_t)(i / a.stages) & 1u, abort_flag, a.wait_ns)))
-          go = false;
-        for (int h = 0; go && h < 2; ++h, ++u) {
-          const int ab = u % kBufs;
-          if (!__all_sync(0xffffffffu, mbar_wait(&afull[ab], (uint32_t)(u / kBufs) & 1u, abort_flag, a.wait_ns))) {
-            go = false;
-            break;
-          }
-          for (int s = 0; s < per_unit; ++s, ++d) {
-            const int db = d % kBufs;
-            if (d >= kBufs && !__all_sync(0xffffffffu, mbar_wait(&dempty[db], ((uint32_t)(d / kBufs) & 1u) ^ 1u,
-                                                                 abort_flag, a.wait_ns))) {
-              go = false;
-              break;
-            }
-            tc_fence_after();
-            if (elect_one()) {
-              const int steps = 8 / per_unit;
-              for (int q = 0; q < steps; ++q) {
-                const int k16 = s * steps + q;             // of the unit's eight
-                const uint64_t b = desc0 + (uint64_t)((st * kStageBytes + (2 * h + (k16 >> 2)) * kXBlock) >> 4) +
-                                   (uint64_t)(2 * (k16 & 3));
-                umma_ts(tmem_base + kAccCol + (uint32_t)(db * 64), tmem_base + (uint32_t)(ab * 64 + k16 * 8), b, idesc,
-                        q > 0 ? 1u : 0u);
+      for (int k = k_lo; go && k < k_hi; ++k, st.next(a.stages)) {
+        go = __all_sync(0xffffffffu, wait_phase(&full[st.i], st.parity, abort_flag, a.wait_ns));
+        const uint64_t bdesc = desc0 + (uint64_t)((st.i * kStageBytes) >> 4);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          go = go && __all_sync(0xffffffffu, wait_phase(&afull[ab.i], ab.parity, abort_flag, a.wait_ns));
+          const uint32_t ta = tmem_base + (uint32_t)(ab.i * 64);
+#pragma unroll
+          for (int s = 0; s < kPerUnit; ++s) {
+            if (reused)
+              go = go && __all_sync(0xffffffffu, wait_phase(&dempty[db.i], db.parity ^ 1u, abort_flag, a.wait_ns));
+            if (go) {
+              tc_fence_after();
+              const uint32_t td = tmem_base + kAccCol + (uint32_t)(db.i * 64);
+              if (elect_one()) {
+#pragma unroll
+                for (int q = 0; q < 8 / kPerUnit; ++q) {
+                  constexpr int kSteps = 8 / kPerUnit;
+                  const int k16 = s * kSteps + q;          // of the unit's eight
+                  umma_ts(td, ta + (uint32_t)(k16 * 8),
+                          bdesc + (uint64_t)(((2 * h + (k16 >> 2)) * kXBlock >> 4) + 2 * (k16 & 3)), kIdesc,
+                          q > 0 ? 1u : 0u);
+                }
+                umma_commit(&dfull[db.i]);
+                if (s == kPerUnit - 1) umma_commit(&aempty[ab.i]);
+                if (s == kPerUnit - 1 && h == 1) umma_commit(&empty[st.i]);
               }
-              umma_commit(&dfull[db]);
+              __syncwarp();
             }
-            __syncwarp();
+            db.next(kBufs);
+            reused = reused || db.i == 0;
           }
-          if (go && elect_one()) {
-            umma_commit(&aempty[ab]);
-            if (h == 1) umma_commit(&empty[st]);
-          }
-          __syncwarp();
+          ab.next(kBufs);
         }
       }
     }
     if (!go) *abort_flag = 1;
   } else if (warp >= kSumWarps) {
-    // ---- codes to integers: thread = weight row, half a unit's columns
-    const int quarter = warp & 3, half = (warp - kSumWarps) >> 2;
+    // ---- codes to integers: thread = weight row, a team's warps every other unit
+    const int quarter = warp & 3, team = (warp - kSumWarps) >> 2;
     const int r = quarter * 32 + lane;
-    int i = 0, u = 0;
-    bool go = true;
+    const uint32_t dst = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    Turn st, ab;
+    ab.i = team;                                           // units 2 i + team
+    bool go = true, reused = false;
     for (int t = first; go && t < a.tiles; t += step) {
       const long long row = min((long long)t * kRows + r, (long long)a.w.out - 1);
       const uint8_t* zeros = a.w.zeros != nullptr ? a.w.zeros + row * a.groups : nullptr;
-      for (int k = k_lo; go && k < k_hi; ++k, ++i) {
-        const int st = i % a.stages;
-        uint32_t z[4];                                     // of this half: two 32-column runs in each unit
+      for (int k = k_lo; k < k_hi; ++k) {
+        uint32_t z[4];                                     // of the unit's runs of 32 columns
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int g = (k * kStageK + (q >> 1) * kUnitK + half * 64 + (q & 1) * 32) / a.w.group;
+          const int g = (k * kStageK + team * kUnitK + q * 32) / G;
           z[q] = zeros != nullptr && g < a.groups ? __ldg(zeros + g) : 8u;
-          z[q] = 0x43004300u | z[q] * 0x10001u;
         }
-        if (!__all_sync(0xffffffffu, mbar_wait(&full[st], (uint32_t)(i / a.stages) & 1u, abort_flag, a.wait_ns))) {
+        if (!__all_sync(0xffffffffu, wait_phase(&full[st.i], st.parity, abort_flag, a.wait_ns))) {
           go = false;
           break;
         }
-        const uint8_t* src = smem + st * kStageBytes + r * 128;
+        const uint8_t* src = smem + st.i * kStageBytes + r * 128;
+        uint4 w[4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h, ++u) {
-          const int ab = u % kBufs;
+        for (int q = 0; q < 4; ++q)
+          w[q] = *reinterpret_cast<const uint4*>(src + (((team * 4 + q) ^ (r & 7)) << 4));
+        if (reused && !__all_sync(0xffffffffu, wait_phase(&aempty[ab.i], ab.parity ^ 1u, abort_flag, a.wait_ns))) {
+          go = false;
+          break;
+        }
+        tc_fence_after();
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
           uint32_t v[32];
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
-            const uint4 w = *reinterpret_cast<const uint4*>(src + (((h * 4 + half * 2 + q) ^ (r & 7)) << 4));
-            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-            const uint32_t zq = z[2 * h + q];
+            const uint4 c = w[2 * half + q];
+            const uint32_t ww[4] = {c.x, c.y, c.z, c.w};
+            const uint32_t zq = 0x43004300u | z[2 * half + q] * 0x10001u;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -295,16 +352,18 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
                 // 0x4300 | c is the bf16 number 128 + c
                 v[16 * q + 4 * j + p] = bf16_sub2(((ww[j] >> (4 * p)) & 0x000F000Fu) | 0x43004300u, zq);
           }
-          if (u >= kBufs && !__all_sync(0xffffffffu, mbar_wait(&aempty[ab], ((uint32_t)(u / kBufs) & 1u) ^ 1u,
-                                                               abort_flag, a.wait_ns))) {
-            go = false;
-            break;
-          }
-          tc_fence_after();
-          tmem_st32(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(ab * 64 + half * 32), v);
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&afull[ab]);
+          tmem_st32(dst + (uint32_t)(ab.i * 64 + half * 32), v);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&afull[ab.i]);
+        st.next(a.stages);
+        ab.i += 2;
+        if (ab.i >= kBufs) {
+          ab.i -= kBufs;
+          ab.parity ^= 1u;
+          reused = true;
         }
       }
     }
@@ -313,50 +372,63 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     // ---- sums: thread = weight row
     const int r = warp * 32 + lane;
     const uint32_t lanes = tmem_base + ((uint32_t)(warp * 32) << 16) + kAccCol;
-    const int slots = (k_hi - k_lo) * 2 * per_unit, g0 = k_lo * 2 * per_unit;
-    int d = 0;
+    const int slots = (k_hi - k_lo) * 2 * kPerUnit, g0 = k_lo * 2 * kPerUnit;
+    float* xs = xs_ring + warp * 2 * kMaxCols;
+    Turn db;
     bool go = true;
+    pdl_wait();                                            // x's scales come from the kernel in front
     for (int t = first; t < a.tiles; t += step) {
       const long long o = (long long)t * kRows + r;
       const __nv_bfloat16* scales = a.w.scales + min(o, (long long)a.w.out - 1) * a.groups;
       float acc[NC];
 #pragma unroll
       for (int j = 0; j < NC; ++j) acc[j] = 0.0f;
-      constexpr int kAhead = 4;                            // scales on their way
+      // scales are loaded four groups before their sums arrive: the weight row's
+      // own, and with x's in groups two columns a lane, which the warp then shares
+      constexpr int kAhead = 4;
       float s[kAhead];
+      float2 xq[kAhead];
+      auto fetch = [&](int q, int i) {
+        const bool in = i < slots && g0 + i < a.groups;
+        s[q] = in ? __bfloat162float(scales[g0 + i]) : 0.0f;
+        xq[q] = in && a.by_group ? *reinterpret_cast<const float2*>(a.x_scale + (long long)(g0 + i) * kMaxCols + 2 * lane)
+                                 : make_float2(0.0f, 0.0f);
+      };
 #pragma unroll
-      for (int q = 0; q < kAhead; ++q)
-        s[q] = q < slots && g0 + q < a.groups ? __bfloat162float(scales[g0 + q]) : 0.0f;
+      for (int q = 0; q < kAhead; ++q) fetch(q, q);
       for (int i0 = 0; go && i0 < slots; i0 += kAhead) {
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
           const int i = i0 + q;
           if (i >= slots || !go) break;
-          const int db = d % kBufs;
-          if (!__all_sync(0xffffffffu, mbar_wait(&dfull[db], (uint32_t)(d / kBufs) & 1u, abort_flag, a.wait_ns))) {
+          const float sc = s[q];
+          float* xb = xs + (q & 1) * kMaxCols;             // the warp's barrier of the next group frees it
+          if (a.by_group) {
+            *reinterpret_cast<float2*>(xb + 2 * lane) = xq[q];
+            __syncwarp();
+          }
+          fetch(q, i + kAhead);
+          if (!__all_sync(0xffffffffu, wait_phase(&dfull[db.i], db.parity, abort_flag, a.wait_ns))) {
             go = false;
             break;
           }
-          ++d;
           tc_fence_after();
-          const float sc = s[q];
-          const int next = g0 + i + kAhead;
-          s[q] = i + kAhead < slots && next < a.groups ? __bfloat162float(scales[next]) : 0.0f;
-          const float4* xs = a.by_group ? reinterpret_cast<const float4*>(a.x_scale + (long long)min(g0 + i, a.groups - 1) * kMaxCols) : nullptr;
-          if (i == 0 && t == first) pdl_wait();            // x's scales come from the kernel in front
+          const uint32_t src = lanes + (uint32_t)(db.i * 64);
+          uint64_t* freed = &dempty[db.i];
+          db.next(kBufs);
 #pragma unroll
           for (int c = 0; c < NC / 16; ++c) {
             float v[16];
-            tmem_ld16(lanes + (uint32_t)(db * 64 + 16 * c), v);
+            tmem_ld16(src + (uint32_t)(16 * c), v);
             if (c == NC / 16 - 1) {
               tc_fence_before();
               __syncwarp();
-              if (lane == 0) mbar_arrive(&dempty[db]);
+              if (lane == 0) mbar_arrive(freed);
             }
-            if (xs != nullptr) {
+            if (a.by_group) {
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                const float4 f = xs[4 * c + j];
+                const float4 f = *reinterpret_cast<const float4*>(xb + 16 * c + 4 * j);
                 acc[16 * c + 4 * j] = fmaf(v[4 * j], sc * f.x, acc[16 * c + 4 * j]);
                 acc[16 * c + 4 * j + 1] = fmaf(v[4 * j + 1], sc * f.y, acc[16 * c + 4 * j + 1]);
                 acc[16 * c + 4 * j + 2] = fmaf(v[4 * j + 2], sc * f.z, acc[16 * c + 4 * j + 2]);
@@ -374,22 +446,14 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
 #pragma unroll
         for (int j = 0; j < NC; ++j) acc[j] = __int_as_float(0x7FC00000);
       }
-      pdl_wait();
       if (split > 1) {
         // every stage has been consumed: the ring takes the partial tile, [column][row]
         float* part = reinterpret_cast<float*>(smem);
 #pragma unroll
         for (int j = 0; j < NC; ++j) part[j * kRows + r] = acc[j];
       } else if (o < a.w.out) {
-        if (a.parts == 1) {
-#pragma unroll
-          for (int j = 0; j < NC; ++j)
-            if (j < a.cols) store_y(a, o, j, acc[j]);
-        } else {
-#pragma unroll
-          for (int j = 0; j + 2 < NC; j += 3)
-            if (j < a.cols) store_y(a, o, j / 3, acc[j] + acc[j + 1] + acc[j + 2]);
-        }
+        if (a.y_dtype == FOVEA_BF16) store_rows<__nv_bfloat16, NC>(a, o, acc);
+        else store_rows<float, NC>(a, o, acc);
       }
     }
   }
@@ -519,12 +583,12 @@ static Plan plan(int N, int in, int group, int x_dtype, bool by_group) {
   return p;
 }
 
-template <int NC>
+template <int NC, int G>
 static cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmX, Args& a, cudaStream_t s) {
-  auto kern = linear_w4_tc_kernel<NC>;
+  auto kern = linear_w4_tc_kernel<NC, G>;
   constexpr int stage = kCodeBytes + 4 * NC * 128;
-  a.stages = std::min(kMaxStages, (kSmemBudget - kBarBytes - 1024) / stage);
-  const size_t smem = 1024 + (size_t)a.stages * stage + kBarBytes;
+  a.stages = std::min(kMaxStages, (kSmemBudget - kBarBytes - kScaleBytes - 1024) / stage);
+  const size_t smem = 1024 + (size_t)a.stages * stage + kScaleBytes + kBarBytes;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -542,6 +606,13 @@ static cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmX, Args& 
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kern, tmW, tmX, a);
+}
+
+template <int G>
+static cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmX, Args& a, cudaStream_t s) {
+  return a.cols_pad == 16 ? launch<16, G>(tmW, tmX, a, s)
+         : a.cols_pad == 32 ? launch<32, G>(tmW, tmX, a, s)
+         : a.cols_pad == 48 ? launch<48, G>(tmW, tmX, a, s) : launch<64, G>(tmW, tmX, a, s);
 }
 
 }  // namespace w4tc
@@ -593,9 +664,8 @@ cudaError_t launch_linear_w4_tc(const LinearW4Args& l, cudaStream_t s) {
     a.err = x.err;
     const TmaOperand xop{x.out + (size_t)b * kMaxCols * p.k_pad, a.cols_pad, p.k_pad, p.k_pad};
     if (!encode_kblock_map(&tmX, xop, a.cols_pad, kStageK / 64)) return cudaErrorInvalidValue;
-    e = a.cols_pad == 16 ? launch<16>(tmW, tmX, a, s)
-        : a.cols_pad == 32 ? launch<32>(tmW, tmX, a, s)
-        : a.cols_pad == 48 ? launch<48>(tmW, tmX, a, s) : launch<64>(tmW, tmX, a, s);
+    e = l.w.group == 128 ? launch<128>(tmW, tmX, a, s)
+        : l.w.group == 64 ? launch<64>(tmW, tmX, a, s) : launch<32>(tmW, tmX, a, s);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
