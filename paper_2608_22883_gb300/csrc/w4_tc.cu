@@ -9,9 +9,9 @@
 // of codes yields them, zero-padded.  The product's CTAs then stream 128 weight
 // rows x 256 k of codes a stage (16 KB, TMA) with the stage's x; eight warps turn
 // codes into integers, one weight row a thread, and write them to tensor memory;
-// one thread issues the MMAs, each group's sum into an accumulator of its own;
-// four warps read the accumulators, one weight row a thread, and add them times
-// their scales in fp32.
+// one lane of each of two warps issues the MMAs, each group's sum into an accumulator of its own;
+// eight warps read the accumulators, one weight row and half of the columns a
+// thread, and add them times their scales in fp32.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -31,10 +31,12 @@ constexpr int kUnitK = 128;                // columns of an operand buffer in te
 constexpr int kMaxCols = 64;               // columns of x a launch takes
 constexpr int kBufs = 4;                   // operand buffers, and accumulators
 constexpr int kMaxStages = 6;
-constexpr int kSumWarps = 4, kIntWarps = 8;   // integers: two teams of four, taking turns by unit
-constexpr int kThreads = 32 * (kSumWarps + kIntWarps + 2);
+constexpr int kSumWarps = 8;               // two teams of four, each half of the columns
+constexpr int kIntWarps = 8;               // two teams of four, taking turns by unit
+constexpr int kMmaWarps = 2;               // taking turns by unit
+constexpr int kThreads = 32 * (kSumWarps + kIntWarps + kMmaWarps + 1);
 constexpr int kBarBytes = 1024;
-constexpr int kScaleBytes = kSumWarps * 2 * kMaxCols * 4;   // x's scales of two groups, a copy per warp
+constexpr int kScaleBytes = kSumWarps * 2 * (kMaxCols / 2) * 4;   // x's scales of two groups, a copy per warp
 constexpr int kSmemBudget = 224 * 1024;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kAccCol = 256;          // accumulators follow the operand buffers (64 columns each)
@@ -42,7 +44,7 @@ constexpr uint32_t kAccCol = 256;          // accumulators follow the operand bu
 struct Args {
   W4 w;
   int groups;
-  int cols, cols_pad;                // columns of x (rows times parts); padded to 16
+  int cols, cols_pad;                // columns of x (rows times parts); padded to 32 or 64
   int parts;                         // columns a row of x is the sum of
   int n0, rows;                      // rows of y
   const float* x_scale;              // by_group: [groups, kMaxCols]; else [kMaxCols] or null
@@ -76,7 +78,9 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
+// C consecutive fp32 accumulator columns of this thread's lane.
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, float (&v)[32]) { tmem_ld32(taddr, v); }
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, float (&v)[16]) {
   uint32_t r[16];
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -139,25 +143,21 @@ __device__ __forceinline__ void store_y(const Args& a, long long o, int n, float
   if (a.y_dtype == FOVEA_BF16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
   else static_cast<float*>(a.y)[at] = v;
 }
-// y of weight row o from its columns' sums.
-template <class T, int NC>
-__device__ __forceinline__ void store_rows(const Args& a, long long o, const float (&acc)[NC]) {
+// y of weight row o from the sums of the columns col0, col0 + 1, ...
+template <class T, int C>
+__device__ __forceinline__ void store_rows(const Args& a, long long o, int col0, const float (&acc)[C]) {
   const float b = a.bias != nullptr ? __ldg(a.bias + o) : 0.0f;
-  T* y = static_cast<T*>(a.y) + (long long)a.n0 * a.ldy + o;
-  const bool scaled = !a.by_group && a.x_scale != nullptr;
-  if (a.parts == 1) {
+  T* y = static_cast<T*>(a.y) + (long long)(a.n0 + col0) * a.ldy + o;
+  const float* scale = a.by_group ? nullptr : a.x_scale;
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      if (j < a.cols) *y = from_f32<T>(fmaf(acc[j], scaled ? a.x_scale[j] : 1.0f, b));
-      y += a.ldy;
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j + 2 < NC; j += 3) {
-      if (j < a.cols) *y = from_f32<T>(acc[j] + acc[j + 1] + acc[j + 2] + b);
-      y += a.ldy;
-    }
+  for (int j = 0; j < C; ++j) {
+    if (col0 + j < a.cols) *y = from_f32<T>(fmaf(acc[j], scale != nullptr ? scale[col0 + j] : 1.0f, b));
+    y += a.ldy;
   }
+}
+// A barrier of the summing warps alone.
+__device__ __forceinline__ void sum_teams_sync() {
+  asm volatile("bar.sync 1, %0;" ::"n"(32 * kSumWarps) : "memory");
 }
 
 // A place in a ring of barriers and the parity of its round (no division in the
@@ -171,9 +171,17 @@ struct Turn {
       parity ^= 1u;
     }
   }
+  // `by` places on; true when the ring's end was passed
+  __device__ __forceinline__ bool skip(int by, int size) {
+    i += by;
+    if (i < size) return false;
+    i -= size;
+    parity ^= 1u;
+    return true;
+  }
 };
 
-// NC: accumulator columns (a multiple of 16, cols_pad); G: the group.  A tile's contraction may
+// NC: accumulator columns (cols_pad); G: the group.  A tile's contraction may
 // be split over the CTAs of a cluster, which then has one tile.
 template <int NC, int G>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -185,6 +193,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   constexpr int kStageBytes = kCodeBytes + 4 * kXBlock;
   float* xs_ring = reinterpret_cast<float*>(smem + a.stages * kStageBytes);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + a.stages * kStageBytes + kScaleBytes);
+  float* parts_tile = reinterpret_cast<float*>(smem + a.stages * kStageBytes + kScaleBytes + kBarBytes);
   uint64_t* empty = full + kMaxStages;
   uint64_t* afull = empty + kMaxStages;
   uint64_t* aempty = afull + kBufs;
@@ -200,10 +209,14 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   const int first = (int)blockIdx.x / split, step = (int)gridDim.x / split;
   const int k_lo = a.ksteps * rank / split, k_hi = a.ksteps * (rank + 1) / split;
   constexpr int kPerUnit = kUnitK / G;                     // groups in a unit: 1, 2 or 4
+  // issuing warps: as many as leave each accumulator to one of them (a barrier's
+  // parity tells a warp only of the round before its own)
+  constexpr int kMmas = kPerUnit == 4 ? 1 : kMmaWarps;
+  constexpr int kHalf = NC / 2;                            // columns of a summing team
   if (threadIdx.x == 0) {
     for (int i = 0; i < kMaxStages; ++i) {
       mbar_init(&full[i], 1);
-      mbar_init(&empty[i], 1);
+      mbar_init(&empty[i], kMmas);
     }
     for (int i = 0; i < kBufs; ++i) {
       mbar_init(&afull[i], kIntWarps / 2);
@@ -211,7 +224,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
       mbar_init(&dfull[i], 1);
       mbar_init(&dempty[i], kSumWarps);
     }
-    mbar_init(drain, 1);
+    mbar_init(drain, kMmaWarps);
     *abort_flag = 0;
     fence_mbar_init();
     prefetch_tmap(&tmW);
@@ -227,7 +240,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   const uint32_t tmem_base = *tmem_slot;
   pdl_trigger();
 
-  if (warp == kSumWarps + kIntWarps) {
+  if (warp == kSumWarps + kIntWarps + kMmaWarps) {
     // ---- copies.  The codes may be read before the wait: the kernel in front
     // (the one that lays x out) had waited for whatever came before it when it let
     // this one start.
@@ -259,52 +272,56 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
       }
       if (!waited) pdl_wait();
     }
-  } else if (warp == kSumWarps + kIntWarps + 1) {
-    // ---- MMAs: the warp runs the loop converged, with addresses and descriptors
-    // in uniform registers; one elected lane issues
+  } else if (warp >= kSumWarps + kIntWarps) {
+    // ---- MMAs: a warp runs its units converged, with addresses and descriptors
+    // in uniform registers; one elected lane issues.  That a unit's integers are
+    // there also says that its stage has landed.
     constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NC >> 3) << 17) |
                                 ((uint32_t)(kRows >> 4) << 24);
     const uint64_t desc0 = sw128_desc(smem_u32(smem) + kCodeBytes);
+    const int w = warp - kSumWarps - kIntWarps;
     Turn st, ab, db;
-    bool go = true, reused = false;                        // an accumulator for the second time
+    ab.i = w;
+    db.i = w * kPerUnit;                                   // of the unit's first group
+    bool go = w < kMmas, reused = false;                   // its accumulators for the second time
     for (int t = first; go && t < a.tiles; t += step) {
       for (int k = k_lo; go && k < k_hi; ++k, st.next(a.stages)) {
-        go = __all_sync(0xffffffffu, wait_phase(&full[st.i], st.parity, abort_flag, a.wait_ns));
         const uint64_t bdesc = desc0 + (uint64_t)((st.i * kStageBytes) >> 4);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int hh = 0; hh < 2; hh += kMmas) {
+          const int h = kMmas == 1 ? hh : w;
           go = go && __all_sync(0xffffffffu, wait_phase(&afull[ab.i], ab.parity, abort_flag, a.wait_ns));
           const uint32_t ta = tmem_base + (uint32_t)(ab.i * 64);
 #pragma unroll
           for (int s = 0; s < kPerUnit; ++s) {
             if (reused)
-              go = go && __all_sync(0xffffffffu, wait_phase(&dempty[db.i], db.parity ^ 1u, abort_flag, a.wait_ns));
+              go = go && __all_sync(0xffffffffu, wait_phase(&dempty[db.i + s], db.parity ^ 1u, abort_flag, a.wait_ns));
             if (go) {
               tc_fence_after();
-              const uint32_t td = tmem_base + kAccCol + (uint32_t)(db.i * 64);
+              const uint32_t td = tmem_base + kAccCol + (uint32_t)((db.i + s) * 64);
+              const uint64_t bh = bdesc + (uint64_t)(h * (2 * kXBlock >> 4));
               if (elect_one()) {
 #pragma unroll
                 for (int q = 0; q < 8 / kPerUnit; ++q) {
-                  constexpr int kSteps = 8 / kPerUnit;
-                  const int k16 = s * kSteps + q;          // of the unit's eight
-                  umma_ts(td, ta + (uint32_t)(k16 * 8),
-                          bdesc + (uint64_t)(((2 * h + (k16 >> 2)) * kXBlock >> 4) + 2 * (k16 & 3)), kIdesc,
-                          q > 0 ? 1u : 0u);
+                  const int k16 = s * (8 / kPerUnit) + q;  // of the unit's eight
+                  umma_ts(td, ta + (uint32_t)(k16 * 8), bh + (uint64_t)(((k16 >> 2) * kXBlock >> 4) + 2 * (k16 & 3)),
+                          kIdesc, q > 0 ? 1u : 0u);
                 }
-                umma_commit(&dfull[db.i]);
-                if (s == kPerUnit - 1) umma_commit(&aempty[ab.i]);
-                if (s == kPerUnit - 1 && h == 1) umma_commit(&empty[st.i]);
+                umma_commit(&dfull[db.i + s]);
+                if (s == kPerUnit - 1) {
+                  umma_commit(&aempty[ab.i]);
+                  if (kMmas == 2 || h == 1) umma_commit(&empty[st.i]);
+                }
               }
               __syncwarp();
             }
-            db.next(kBufs);
-            reused = reused || db.i == 0;
           }
-          ab.next(kBufs);
+          ab.skip(kMmas, kBufs);
+          reused |= db.skip(kMmas * kPerUnit, kBufs);
         }
       }
     }
-    if (!go) *abort_flag = 1;
+    if (!go && w < kMmas) *abort_flag = 1;
   } else if (warp >= kSumWarps) {
     // ---- codes to integers: thread = weight row, a team's warps every other unit
     const int quarter = warp & 3, team = (warp - kSumWarps) >> 2;
@@ -359,40 +376,34 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
         __syncwarp();
         if (lane == 0) mbar_arrive(&afull[ab.i]);
         st.next(a.stages);
-        ab.i += 2;
-        if (ab.i >= kBufs) {
-          ab.i -= kBufs;
-          ab.parity ^= 1u;
-          reused = true;
-        }
+        reused |= ab.skip(2, kBufs);
       }
     }
     if (!go) *abort_flag = 1;
   } else {
-    // ---- sums: thread = weight row
-    const int r = warp * 32 + lane;
-    const uint32_t lanes = tmem_base + ((uint32_t)(warp * 32) << 16) + kAccCol;
+    // ---- sums: thread = weight row, a team's warps half of the columns
+    const int quarter = warp & 3, col0 = (warp >> 2) * kHalf;
+    const int r = quarter * 32 + lane;
+    const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16) + kAccCol + (uint32_t)col0;
     const int slots = (k_hi - k_lo) * 2 * kPerUnit, g0 = k_lo * 2 * kPerUnit;
-    float* xs = xs_ring + warp * 2 * kMaxCols;
+    float* xs = xs_ring + warp * 2 * kHalf;
     Turn db;
     bool go = true;
     pdl_wait();                                            // x's scales come from the kernel in front
     for (int t = first; t < a.tiles; t += step) {
       const long long o = (long long)t * kRows + r;
       const __nv_bfloat16* scales = a.w.scales + min(o, (long long)a.w.out - 1) * a.groups;
-      float acc[NC];
+      float acc[kHalf];
 #pragma unroll
-      for (int j = 0; j < NC; ++j) acc[j] = 0.0f;
+      for (int j = 0; j < kHalf; ++j) acc[j] = 0.0f;
       // scales are loaded four groups before their sums arrive: the weight row's
-      // own, and with x's in groups two columns a lane, which the warp then shares
+      // own, and with x's in groups a column a lane, which the warp then shares
       constexpr int kAhead = 4;
-      float s[kAhead];
-      float2 xq[kAhead];
+      float s[kAhead], xq[kAhead];
       auto fetch = [&](int q, int i) {
         const bool in = i < slots && g0 + i < a.groups;
         s[q] = in ? __bfloat162float(scales[g0 + i]) : 0.0f;
-        xq[q] = in && a.by_group ? *reinterpret_cast<const float2*>(a.x_scale + (long long)(g0 + i) * kMaxCols + 2 * lane)
-                                 : make_float2(0.0f, 0.0f);
+        xq[q] = in && a.by_group && lane < kHalf ? a.x_scale[(long long)(g0 + i) * kMaxCols + col0 + lane] : 0.0f;
       };
 #pragma unroll
       for (int q = 0; q < kAhead; ++q) fetch(q, q);
@@ -402,9 +413,9 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
           const int i = i0 + q;
           if (i >= slots || !go) break;
           const float sc = s[q];
-          float* xb = xs + (q & 1) * kMaxCols;             // the warp's barrier of the next group frees it
+          float* xb = xs + (q & 1) * kHalf;                // the warp's barrier of the next group frees it
           if (a.by_group) {
-            *reinterpret_cast<float2*>(xb + 2 * lane) = xq[q];
+            if (lane < kHalf) xb[lane] = xq[q];
             __syncwarp();
           }
           fetch(q, i + kAhead);
@@ -413,47 +424,48 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
             break;
           }
           tc_fence_after();
-          const uint32_t src = lanes + (uint32_t)(db.i * 64);
-          uint64_t* freed = &dempty[db.i];
+          float v[kHalf];
+          tmem_ld_cols(lanes + (uint32_t)(db.i * 64), v);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&dempty[db.i]);
           db.next(kBufs);
+          if (a.by_group) {
 #pragma unroll
-          for (int c = 0; c < NC / 16; ++c) {
-            float v[16];
-            tmem_ld16(src + (uint32_t)(16 * c), v);
-            if (c == NC / 16 - 1) {
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(freed);
+            for (int j = 0; j < kHalf; j += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(xb + j);
+              acc[j] = fmaf(v[j], sc * f.x, acc[j]);
+              acc[j + 1] = fmaf(v[j + 1], sc * f.y, acc[j + 1]);
+              acc[j + 2] = fmaf(v[j + 2], sc * f.z, acc[j + 2]);
+              acc[j + 3] = fmaf(v[j + 3], sc * f.w, acc[j + 3]);
             }
-            if (a.by_group) {
+          } else {
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const float4 f = *reinterpret_cast<const float4*>(xb + 16 * c + 4 * j);
-                acc[16 * c + 4 * j] = fmaf(v[4 * j], sc * f.x, acc[16 * c + 4 * j]);
-                acc[16 * c + 4 * j + 1] = fmaf(v[4 * j + 1], sc * f.y, acc[16 * c + 4 * j + 1]);
-                acc[16 * c + 4 * j + 2] = fmaf(v[4 * j + 2], sc * f.z, acc[16 * c + 4 * j + 2]);
-                acc[16 * c + 4 * j + 3] = fmaf(v[4 * j + 3], sc * f.w, acc[16 * c + 4 * j + 3]);
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < 16; ++j) acc[16 * c + j] = fmaf(v[j], sc, acc[16 * c + j]);
-            }
+            for (int j = 0; j < kHalf; ++j) acc[j] = fmaf(v[j], sc, acc[j]);
           }
         }
       }
       if (!go) {                                           // a result that shows it
         *abort_flag = 1;
 #pragma unroll
-        for (int j = 0; j < NC; ++j) acc[j] = __int_as_float(0x7FC00000);
+        for (int j = 0; j < kHalf; ++j) acc[j] = __int_as_float(0x7FC00000);
       }
-      if (split > 1) {
-        // every stage has been consumed: the ring takes the partial tile, [column][row]
-        float* part = reinterpret_cast<float*>(smem);
+      if (split > 1 || a.parts > 1) {
+        // the partial tile, [column][row]: over the ring when its tile is the CTA's
+        // only one (every stage has been consumed), else behind it
+        float* part = split > 1 ? reinterpret_cast<float*>(smem) : parts_tile;
+        if (split == 1) sum_teams_sync();                  // the last tile's readers are done
 #pragma unroll
-        for (int j = 0; j < NC; ++j) part[j * kRows + r] = acc[j];
+        for (int j = 0; j < kHalf; ++j) part[(col0 + j) * kRows + r] = acc[j];
+        if (split == 1) {
+          sum_teams_sync();
+          if (o < a.w.out)
+            for (int n = warp >> 2; n < a.rows; n += 2)
+              store_y(a, o, n, part[3 * n * kRows + r] + part[(3 * n + 1) * kRows + r] + part[(3 * n + 2) * kRows + r]);
+        }
       } else if (o < a.w.out) {
-        if (a.y_dtype == FOVEA_BF16) store_rows<__nv_bfloat16, NC>(a, o, acc);
-        else store_rows<float, NC>(a, o, acc);
+        if (a.y_dtype == FOVEA_BF16) store_rows<__nv_bfloat16, kHalf>(a, o, col0, acc);
+        else store_rows<float, kHalf>(a, o, col0, acc);
       }
     }
   }
@@ -463,7 +475,8 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   tc_fence_after();
   if (*abort_flag != 0) {
     if (threadIdx.x == 0) atomicOr(a.err, kErrTimeout);
-    if (warp == kSumWarps + kIntWarps + 1 && elect_one()) umma_commit(drain);    // the issuing warp's MMAs
+    if (warp >= kSumWarps + kIntWarps && warp < kSumWarps + kIntWarps + kMmaWarps && elect_one())
+      umma_commit(drain);                                  // each issuing warp's MMAs
     if (lane == 0) {
       mbar_wait(drain, 0, nullptr, kDefaultWaitLimitNs);
       const uint64_t t0 = globaltimer_ns();                // copies in flight land
@@ -587,8 +600,10 @@ template <int NC, int G>
 static cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmX, Args& a, cudaStream_t s) {
   auto kern = linear_w4_tc_kernel<NC, G>;
   constexpr int stage = kCodeBytes + 4 * NC * 128;
-  a.stages = std::min(kMaxStages, (kSmemBudget - kBarBytes - kScaleBytes - 1024) / stage);
-  const size_t smem = 1024 + (size_t)a.stages * stage + kScaleBytes + kBarBytes;
+  const int tile = a.parts > 1 && a.split == 1 ? NC * kRows * 4 : 0;
+  const int rest = 1024 + kScaleBytes + kBarBytes + tile;
+  a.stages = std::min(kMaxStages, (kSmemBudget - rest) / stage);
+  const size_t smem = (size_t)a.stages * stage + rest;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -610,9 +625,7 @@ static cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmX, Args& 
 
 template <int G>
 static cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmX, Args& a, cudaStream_t s) {
-  return a.cols_pad == 16 ? launch<16, G>(tmW, tmX, a, s)
-         : a.cols_pad == 32 ? launch<32, G>(tmW, tmX, a, s)
-         : a.cols_pad == 48 ? launch<48, G>(tmW, tmX, a, s) : launch<64, G>(tmW, tmX, a, s);
+  return a.cols_pad == 32 ? launch<32, G>(tmW, tmX, a, s) : launch<64, G>(tmW, tmX, a, s);
 }
 
 }  // namespace w4tc
@@ -650,7 +663,7 @@ cudaError_t launch_linear_w4_tc(const LinearW4Args& l, cudaStream_t s) {
     a.rows = std::min(p.rows_block, l.N - a.n0);
     a.parts = p.parts;
     a.cols = a.rows * p.parts;
-    a.cols_pad = (a.cols + 15) / 16 * 16;
+    a.cols_pad = a.cols <= 32 ? 32 : 64;
     a.by_group = by_group;
     a.x_scale = x.x_groups == 0 ? nullptr : x.scale_out + (size_t)b * kMaxCols * x.x_groups;
     a.bias = l.bias;
