@@ -100,22 +100,14 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, u
       "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y)
       : "memory");
 }
-// mbar_wait in line: a call would first wait for the caller's loads in flight,
-// and reading the clock takes longer than most of the waits here last.
-__device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
-                                           uint64_t limit_ns) {
-  const bool poll = limit_ns < kSuspendNs;                 // shorter than a suspended try may take
-  uint64_t t0 = 0;
-#pragma unroll 1
-  for (uint32_t n = 0;; ++n) {
-    if (poll ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
-    if (*abort_flag) return false;
-    if ((n & 3u) == 3u || poll) {
-      const uint64_t now = globaltimer_ns();
-      if (t0 == 0) t0 = now;
-      else if (now - t0 > limit_ns) return false;
-    }
-  }
+// mbar_wait of a converged warp (the same answer in every lane).  The first try
+// is in line: a call makes the caller's loads in flight arrive first, and the
+// clock behind the limit costs more than most of the waits here last (a satisfied
+// wait: 25 clocks so, 119 with the limit's loop in line).
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
+                                          uint64_t limit_ns) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit_ns));
 }
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
@@ -250,7 +242,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
       Turn st;
       for (int t = first; go && t < a.tiles; t += step) {
         for (int k = k_lo; k < k_hi; ++k, ++i, st.next(a.stages)) {
-          if (i >= a.stages && !wait_phase(&empty[st.i], st.parity ^ 1u, abort_flag, a.wait_ns)) {
+          if (i >= a.stages && !mbar_wait(&empty[st.i], st.parity ^ 1u, abort_flag, a.wait_ns)) {
             *abort_flag = 1;
             go = false;
             break;
@@ -290,12 +282,12 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
 #pragma unroll
         for (int hh = 0; hh < 2; hh += kMmas) {
           const int h = kMmas == 1 ? hh : w;
-          go = go && __all_sync(0xffffffffu, wait_phase(&afull[ab.i], ab.parity, abort_flag, a.wait_ns));
+          go = go && warp_wait(&afull[ab.i], ab.parity, abort_flag, a.wait_ns);
           const uint32_t ta = tmem_base + (uint32_t)(ab.i * 64);
 #pragma unroll
           for (int s = 0; s < kPerUnit; ++s) {
             if (reused)
-              go = go && __all_sync(0xffffffffu, wait_phase(&dempty[db.i + s], db.parity ^ 1u, abort_flag, a.wait_ns));
+              go = go && warp_wait(&dempty[db.i + s], db.parity ^ 1u, abort_flag, a.wait_ns);
             if (go) {
               tc_fence_after();
               const uint32_t td = tmem_base + kAccCol + (uint32_t)((db.i + s) * 64);
@@ -340,7 +332,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
           const int g = (k * kStageK + team * kUnitK + q * 32) / G;
           z[q] = zeros != nullptr && g < a.groups ? __ldg(zeros + g) : 8u;
         }
-        if (!__all_sync(0xffffffffu, wait_phase(&full[st.i], st.parity, abort_flag, a.wait_ns))) {
+        if (!warp_wait(&full[st.i], st.parity, abort_flag, a.wait_ns)) {
           go = false;
           break;
         }
@@ -349,7 +341,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           w[q] = *reinterpret_cast<const uint4*>(src + (((team * 4 + q) ^ (r & 7)) << 4));
-        if (reused && !__all_sync(0xffffffffu, wait_phase(&aempty[ab.i], ab.parity ^ 1u, abort_flag, a.wait_ns))) {
+        if (reused && !warp_wait(&aempty[ab.i], ab.parity ^ 1u, abort_flag, a.wait_ns)) {
           go = false;
           break;
         }
@@ -419,7 +411,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
             __syncwarp();
           }
           fetch(q, i + kAhead);
-          if (!__all_sync(0xffffffffu, wait_phase(&dfull[db.i], db.parity, abort_flag, a.wait_ns))) {
+          if (!warp_wait(&dfull[db.i], db.parity, abort_flag, a.wait_ns)) {
             go = false;
             break;
           }
