@@ -36,7 +36,7 @@ constexpr int kIntWarps = 8;               // two teams of four, taking turns by
 constexpr int kMmaWarps = 2;               // taking turns by unit
 constexpr int kThreads = 32 * (kSumWarps + kIntWarps + kMmaWarps + 1);
 constexpr int kBarBytes = 1024;
-constexpr int kScaleBytes = kSumWarps * 2 * (kMaxCols / 2) * 4;   // x's scales of two groups, a copy per warp
+constexpr int kScaleBytes = kSumWarps * 4 * (kMaxCols / 2) * 4;   // x's scales of four groups, a copy per warp
 constexpr int kSmemBudget = 224 * 1024;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kAccCol = 256;          // accumulators follow the operand buffers (64 columns each)
@@ -78,10 +78,8 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// C consecutive fp32 accumulator columns of this thread's lane.
-__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, float (&v)[32]) { tmem_ld32(taddr, v); }
-__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, float (&v)[16]) {
-  uint32_t r[16];
+// C consecutive accumulator columns of this thread's lane.
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
       "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -90,8 +88,31 @@ __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, float (&v)[16]) {
         "=r"(r[14]), "=r"(r[15])
       : "r"(taddr));
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
+        "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
 }
 __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, uint64_t* bar, int x, int y) {
   asm volatile(
@@ -326,11 +347,13 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
       const long long row = min((long long)t * kRows + r, (long long)a.w.out - 1);
       const uint8_t* zeros = a.w.zeros != nullptr ? a.w.zeros + row * a.groups : nullptr;
       for (int k = k_lo; k < k_hi; ++k) {
-        uint32_t z[4];                                     // of the unit's runs of 32 columns
+        uint32_t z[4] = {0x43084308u, 0x43084308u, 0x43084308u, 0x43084308u};   // of the unit's runs of 32 columns
+        if (zeros != nullptr) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int g = (k * kStageK + team * kUnitK + q * 32) / G;
-          z[q] = zeros != nullptr && g < a.groups ? __ldg(zeros + g) : 8u;
+          for (int q = 0; q < 4; ++q) {
+            const int g = (k * kStageK + team * kUnitK + q * 32) / G;
+            if (g < a.groups) z[q] = 0x43004300u | __ldg(zeros + g) * 0x10001u;
+          }
         }
         if (!warp_wait(&full[st.i], st.parity, abort_flag, a.wait_ns)) {
           go = false;
@@ -353,7 +376,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
           for (int q = 0; q < 2; ++q) {
             const uint4 c = w[2 * half + q];
             const uint32_t ww[4] = {c.x, c.y, c.z, c.w};
-            const uint32_t zq = 0x43004300u | z[2 * half + q] * 0x10001u;
+            const uint32_t zq = z[2 * half + q];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -378,77 +401,98 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     const int r = quarter * 32 + lane;
     const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16) + kAccCol + (uint32_t)col0;
     const int slots = (k_hi - k_lo) * 2 * kPerUnit, g0 = k_lo * 2 * kPerUnit;
-    float* xs = xs_ring + warp * 2 * kHalf;
+    float* xs = xs_ring + warp * 4 * kHalf;
     Turn db;
     bool go = true;
     pdl_wait();                                            // x's scales come from the kernel in front
     for (int t = first; t < a.tiles; t += step) {
       const long long o = (long long)t * kRows + r;
       const __nv_bfloat16* scales = a.w.scales + min(o, (long long)a.w.out - 1) * a.groups;
-      float acc[kHalf];
+      uint64_t acc[kHalf / 2];                             // pairs of columns
 #pragma unroll
-      for (int j = 0; j < kHalf; ++j) acc[j] = 0.0f;
-      // scales are loaded four groups before their sums arrive: the weight row's
-      // own, and with x's in groups a column a lane, which the warp then shares
+      for (int j = 0; j < kHalf / 2; ++j) acc[j] = 0;
+      // scales are loaded a round of four groups before their sums arrive: the
+      // weight row's own, and with x's in groups a column a lane, which the warp
+      // then shares
       constexpr int kAhead = 4;
       float s[kAhead], xq[kAhead];
-      auto fetch = [&](int q, int i) {
-        const bool in = i < slots && g0 + i < a.groups;
-        s[q] = in ? __bfloat162float(scales[g0 + i]) : 0.0f;
-        xq[q] = in && a.by_group && lane < kHalf ? a.x_scale[(long long)(g0 + i) * kMaxCols + col0 + lane] : 0.0f;
-      };
+      const bool quads = a.groups % kAhead == 0 && g0 % kAhead == 0 && slots % kAhead == 0 &&
+                         (reinterpret_cast<uintptr_t>(a.w.scales) & 7u) == 0;
+      auto fetch = [&](int i0) {
+        const int left = min(slots - i0, a.groups - g0 - i0);
+        if (quads) {
+          uint2 raw = make_uint2(0u, 0u);
+          if (left > 0) raw = __ldg(reinterpret_cast<const uint2*>(scales + g0 + i0));
+          s[0] = __uint_as_float(raw.x << 16);
+          s[1] = __uint_as_float(raw.x & 0xFFFF0000u);
+          s[2] = __uint_as_float(raw.y << 16);
+          s[3] = __uint_as_float(raw.y & 0xFFFF0000u);
+        } else {
 #pragma unroll
-      for (int q = 0; q < kAhead; ++q) fetch(q, q);
+          for (int q = 0; q < kAhead; ++q) s[q] = q < left ? __bfloat162float(scales[g0 + i0 + q]) : 0.0f;
+        }
+        if (a.by_group) {
+          const float* x = a.x_scale + (long long)(g0 + i0) * kMaxCols + col0 + (lane & (kHalf - 1));
+#pragma unroll
+          for (int q = 0; q < kAhead; ++q) xq[q] = q < left ? x[q * kMaxCols] : 0.0f;
+        }
+      };
+      fetch(0);
       for (int i0 = 0; go && i0 < slots; i0 += kAhead) {
+        float sc[kAhead];
+        if (a.by_group) {
+          __syncwarp();                                    // the last round's have been read
+#pragma unroll
+          for (int q = 0; q < kAhead; ++q)
+            if (lane < kHalf) xs[q * kHalf + lane] = xq[q];
+          __syncwarp();
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) sc[q] = s[q];
+        if (i0 + kAhead < slots) fetch(i0 + kAhead);
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
-          const int i = i0 + q;
-          if (i >= slots || !go) break;
-          const float sc = s[q];
-          float* xb = xs + (q & 1) * kHalf;                // the warp's barrier of the next group frees it
-          if (a.by_group) {
-            if (lane < kHalf) xb[lane] = xq[q];
-            __syncwarp();
-          }
-          fetch(q, i + kAhead);
+          if (i0 + q >= slots) break;
           if (!warp_wait(&dfull[db.i], db.parity, abort_flag, a.wait_ns)) {
             go = false;
             break;
           }
           tc_fence_after();
-          float v[kHalf];
+          uint32_t v[kHalf];
           tmem_ld_cols(lanes + (uint32_t)(db.i * 64), v);
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&dempty[db.i]);
           db.next(kBufs);
+          const uint64_t s2 = pack2(__float_as_uint(sc[q]), __float_as_uint(sc[q]));
           if (a.by_group) {
 #pragma unroll
             for (int j = 0; j < kHalf; j += 4) {
-              const float4 f = *reinterpret_cast<const float4*>(xb + j);
-              acc[j] = fmaf(v[j], sc * f.x, acc[j]);
-              acc[j + 1] = fmaf(v[j + 1], sc * f.y, acc[j + 1]);
-              acc[j + 2] = fmaf(v[j + 2], sc * f.z, acc[j + 2]);
-              acc[j + 3] = fmaf(v[j + 3], sc * f.w, acc[j + 3]);
+              const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(xs + q * kHalf + j);
+              acc[j / 2] = fma2(pack2(v[j], v[j + 1]), mul2(s2, f.x), acc[j / 2]);
+              acc[j / 2 + 1] = fma2(pack2(v[j + 2], v[j + 3]), mul2(s2, f.y), acc[j / 2 + 1]);
             }
           } else {
 #pragma unroll
-            for (int j = 0; j < kHalf; ++j) acc[j] = fmaf(v[j], sc, acc[j]);
+            for (int j = 0; j < kHalf; j += 2) acc[j / 2] = fma2(pack2(v[j], v[j + 1]), s2, acc[j / 2]);
           }
         }
       }
       if (!go) {                                           // a result that shows it
         *abort_flag = 1;
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) acc[j] = __int_as_float(0x7FC00000);
+        for (int j = 0; j < kHalf / 2; ++j) acc[j] = 0x7FC000007FC00000ull;
       }
+      float sum[kHalf];
+#pragma unroll
+      for (int j = 0; j < kHalf; ++j) sum[j] = __uint_as_float((uint32_t)(acc[j / 2] >> (32 * (j & 1))));
       if (split > 1 || a.parts > 1) {
         // the partial tile, [column][row]: over the ring when its tile is the CTA's
         // only one (every stage has been consumed), else behind it
         float* part = split > 1 ? reinterpret_cast<float*>(smem) : parts_tile;
         if (split == 1) sum_teams_sync();                  // the last tile's readers are done
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) part[(col0 + j) * kRows + r] = acc[j];
+        for (int j = 0; j < kHalf; ++j) part[(col0 + j) * kRows + r] = sum[j];
         if (split == 1) {
           sum_teams_sync();
           if (o < a.w.out)
@@ -456,8 +500,8 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
               store_y(a, o, n, part[3 * n * kRows + r] + part[(3 * n + 1) * kRows + r] + part[(3 * n + 2) * kRows + r]);
         }
       } else if (o < a.w.out) {
-        if (a.y_dtype == FOVEA_BF16) store_rows<__nv_bfloat16, kHalf>(a, o, col0, acc);
-        else store_rows<float, kHalf>(a, o, col0, acc);
+        if (a.y_dtype == FOVEA_BF16) store_rows<__nv_bfloat16, kHalf>(a, o, col0, sum);
+        else store_rows<float, kHalf>(a, o, col0, sum);
       }
     }
   }
