@@ -518,7 +518,7 @@ def quantize_w4(W: torch.Tensor, group: int = 128, *, symmetric: bool = True,
     return {"codes": codes, "scales": scales, "zeros": zeros}
 
 
-W4_FEW_ROWS = 5         # up to here linear_w4 needs no workspace, whatever x's type
+W4_FEW = 5, 16384       # rows and columns up to which linear_w4 needs no workspace, whatever x's type
 
 
 def linear_w4_workspace_size(N: int, in_features: int, group: int = 128,
@@ -569,7 +569,7 @@ def linear_w4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
     if workspace is not None:
         ws_bytes = workspace.numel()
         ws_at = _need("workspace", workspace, (ws_bytes,), torch.uint8)
-    elif N > W4_FEW_ROWS:
+    elif N > W4_FEW[0] or in_f > W4_FEW[1]:
         ws_bytes = linear_w4_workspace_size(N, in_f, group, dt, x_group)
         if ws_bytes:
             workspace = empty((ws_bytes,), dtype=torch.uint8, device=dev)
