@@ -104,11 +104,11 @@ quantize_w4_kernel(const T* __restrict__ W, long long ld, int in, int slots, lon
 // Product with a few rows
 // ---------------------------------------------------------------------------
 
-constexpr int kWarps = 16, kThreads = kWarps * 32;
+constexpr int kMaxSmem = 227 * 1024;
+constexpr int kWarps = 16, kThreads = 32 * kWarps;
 constexpr int kSpan = 128;             // columns a warp handles together
 constexpr int kTileRows = 16;          // weight rows of a tile
-constexpr int kDepth = 4;              // spans of codes a warp has on their way
-constexpr int kRegScales = 4;          // scales of the next tile a thread has on their way
+constexpr int kQuad = 4;               // spans of codes a warp has on their way
 
 // Offset within a span of the eight columns of word j of lane quarter t: the
 // four quarters of a warp's lanes share the sum of one tensor-core product, so
@@ -145,6 +145,10 @@ __device__ __forceinline__ void load_words(uint32_t* r, const uint8_t* p, bool l
         "{\n .reg .pred q;\n setp.ne.u32 q, %2, 0;\n @q ld.global.nc.u32 %0, [%1];\n}"
         : "+r"(r[0]) : "l"(p), "r"((uint32_t)live));
 }
+// A barrier of the `split` warps of a team (barriers 1 to 8).
+__device__ __forceinline__ void team_sync(int team, int split) {
+  asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(split * 32) : "memory");
+}
 // v as the sum of three bf16 numbers: its truncations (an infinity or a NaN is the first alone).
 __device__ __forceinline__ void split3(float v, uint32_t& b0, uint32_t& b1, uint32_t& b2) {
   const uint32_t bits = __float_as_uint(v);
@@ -171,25 +175,6 @@ __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t
 struct Span {
   uint32_t w[2][4];
 };
-
-template <int G>
-__device__ __forceinline__ void load_span(Span& r, const W4& w, long long row0, int span, int lane, bool live) {
-  const int g = lane >> 2, t = lane & 3;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    // rows past the end repeat the last one (their results are not stored)
-    const long long row = min(row0 + g + 8 * h, (long long)w.out - 1);
-    const uint8_t* p = w.codes + row * (w.in / 2) + span * (kSpan / 2);
-    constexpr int kWords = G / 32;               // words in a row of bytes
-#pragma unroll
-    for (int j = 0; j < 4; j += kWords) {
-      const int k = word_column<G>(j, t);
-      // past the row's end (whole runs: both are multiples of theirs) the words keep
-      // what they held, and x is 0
-      load_words<kWords>(&r.w[h][j], p + k / 2, live && span * kSpan + k < w.in);
-    }
-  }
-}
 
 // Eight columns of a row of x, as the bf16 columns that add up to them, in the order
 // in which the codes of a word come out of it: 0 4 1 5 2 6 3 7.
@@ -222,61 +207,137 @@ __device__ __forceinline__ void layout_x8(const void* x, long long at, int dtype
   for (int p = 0; p < 3; ++p) out[p] = make_uint4(pk[p][0], pk[p][1], pk[p][2], pk[p][3]);
 }
 
+// The scales (bf16 pairs) and zero points (bytes) of four spans of a weight row.
+template <int G>
+struct Quad {
+  static constexpr int kGroups = kQuad * kSpan / G;      // 4, 8 or 16
+  uint32_t s[kGroups / 2], z[kGroups / 4];
+  // `vec`: every row's scales and zeros start at a multiple of kGroups, aligned
+  template <bool ZEROS>
+  __device__ __forceinline__ void load(const W4& w, long long row_at, int g0, int groups, bool vec) {
+    if (vec) {
+      const __nv_bfloat16* p = w.scales + row_at + g0;
+      if (kGroups == 4) {
+        const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+        s[0] = v.x; s[1] = v.y;
+      } else {
+#pragma unroll
+        for (int i = 0; i < kGroups / 8; ++i) {
+          const uint4 v = __ldg(reinterpret_cast<const uint4*>(p) + i);
+          s[4 * i] = v.x; s[4 * i + 1] = v.y; s[4 * i + 2] = v.z; s[4 * i + 3] = v.w;
+        }
+      }
+      if (ZEROS) {
+#pragma unroll
+        for (int i = 0; i < kGroups / 4; ++i)
+          z[i] = __ldg(reinterpret_cast<const uint32_t*>(w.zeros + row_at + g0) + i);
+      }
+    } else {                                             // past the last group x is 0
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) {
+        const uint32_t v = g0 + i < groups ? __bfloat16_as_ushort(w.scales[row_at + g0 + i]) : 0u;
+        s[i / 2] = i & 1 ? s[i / 2] | v << 16 : v;
+        if (ZEROS) {
+          const uint32_t b = g0 + i < groups ? w.zeros[row_at + g0 + i] : 8u;
+          z[i / 4] = i & 3 ? z[i / 4] | b << (8 * (i & 3)) : b;
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ float scale(int i) const {
+    return __uint_as_float(i & 1 ? s[i / 2] & 0xFFFF0000u : s[i / 2] << 16);
+  }
+  __device__ __forceinline__ uint32_t zero2(int i) const {     // 128 + z, twice
+    return 0x43004300u | ((z[i / 4] >> (8 * (i & 3))) & 15u) * 0x10001u;
+  }
+};
+
 // y of up to 8 NT columns (rows of x, an fp32 row as three) in one launch.
 //
-// A persistent CTA takes every gridDim.x-th tile of 16 weight rows.  Its warps
-// split the tile's spans; each turns its codes into bf16 integers c - z (exact)
-// and multiplies them on the tensor cores, weights as the 16-row operand, with
-// x from shared memory; a group's fp32 sum is then taken times its scale.  The
-// warps' partial tiles meet in shared memory in a fixed order.  The codes of the next
-// kDepth spans, across tiles, are on their way in registers meanwhile, and so are
-// the scales of the next tile.
+// `split` warps take a tile of 16 weight rows, each a range of its quads (four spans of
+// 128 columns); a warp goes from tile to tile by itself, x in shared memory.  It
+// turns the codes into bf16 integers c - z (exact) and multiplies them on the tensor
+// cores, weights as the 16-row operand; a group's fp32 sum is then taken times its
+// scale.  The codes of the next four spans are on their way in registers
+// meanwhile, across tiles, and so are the next quad's scales.  Only the warps of a
+// split tile meet, in shared memory, in a fixed order.
 //
 // fp32 rows enter as three bf16 rows that add up to them exactly; e4m3 rows are
 // exact in bf16 and their scales join the group's or the result.
 template <int G, int NT, bool ZEROS>
-__global__ void __launch_bounds__(kThreads, 1) linear_w4_kernel(const LinearW4Args a, int n0, int n1, bool x_vec) {
+__global__ void __launch_bounds__(kThreads, 1)
+linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bool scale_vec) {
   extern __shared__ __align__(16) uint8_t smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int parts = a.x_dtype == FOVEA_FP32 ? 3 : 1;
   const int rows = n1 - n0, cols = rows * parts;
   const int spans = (a.w.in + kSpan - 1) / kSpan;
   const int groups = (a.w.in + G - 1) / G;
-  // [span][word][quarter][column] units of eight x values; two partial tiles
-  // [warp][row][column]; scales of x [group][column]; scales and zeros of two
-  // tiles [row][group]
-  uint4* xs = reinterpret_cast<uint4*>(smem);
+  // sixteen zero bytes; [span][word][quarter][column] units of eight x values; each
+  // warp's partial tile [row][column]; scales of x [group][column]
+  uint4* xs = reinterpret_cast<uint4*>(smem) + 1;
   float* part = reinterpret_cast<float*>(xs + (long long)spans * 16 * cols);
-  float* xscale = part + 2 * kWarps * kTileRows * 8 * NT;
+  float* xscale = part + kWarps * kTileRows * 8 * NT;
   const bool by_group = a.x_scale != nullptr && a.x_group != 0;
-  __nv_bfloat16* ws = reinterpret_cast<__nv_bfloat16*>(xscale + (by_group ? groups * cols : 0));
-  const int tile_scales = kTileRows * groups;
-  uint8_t* wz = reinterpret_cast<uint8_t*>(ws + 2 * tile_scales);
   const int tiles = (a.w.out + kTileRows - 1) / kTileRows;
-  const int per = (spans + kWarps - 1) / kWarps;         // spans a warp has of a tile
-  const long long all_scales = (long long)a.w.out * groups;
-
-  // scales of a tile: kRegScales a thread through registers, others at once
-  auto scale_at = [&](int tile, int e) { return min((long long)tile * tile_scales + e, all_scales - 1); };
+  const int quads = (spans + kQuad - 1) / kQuad;
+  // tiles go round the CTAs first, so that every SM has work of a short list
+  const int team = warp / split, rank = warp - team * split;
+  const int first = team * (int)gridDim.x + (int)blockIdx.x, step = (int)gridDim.x * (kWarps / split);
+  const int q_lo = quads * rank / split, q_hi = quads * (rank + 1) / split;
 
   pdl_wait();
   pdl_trigger();
-  Span ring[kDepth] = {};
-  int next_tile = blockIdx.x, next_i = 0;
+  // The next codes: this lane's first word of row g of the tile, and how far it is
+  // into the row.  A word past its row's end, or of a row past the last, keeps what
+  // the register held: x is 0 there, or the result is not stored.
+  const int row_bytes = a.w.in / 2;
+  const int byte0 = q_lo * kQuad * (kSpan / 2) + word_column<G>(0, t) / 2;
+  const int byte1 = q_hi * kQuad * (kSpan / 2) + word_column<G>(0, t) / 2;
+  const uint8_t* next = a.w.codes + ((long long)first * kTileRows + g) * row_bytes + byte0;
+  const long long tile_step = (long long)step * kTileRows * row_bytes - (byte1 - byte0);
+  int next_tile = first, next_byte = byte0;
+  bool live0 = false, live1 = false;
+  auto enter = [&]() {                                     // a tile's rows
+    live0 = next_tile < tiles && next_tile * kTileRows + g < a.w.out;
+    live1 = next_tile < tiles && next_tile * kTileRows + g + 8 < a.w.out;
+  };
+  enter();
   auto refill = [&](Span& r) {
-    const int span = next_i * kWarps + warp;
-    load_span<G>(r, a.w, (long long)next_tile * kTileRows, span, lane, next_tile < tiles && span < spans);
-    if (++next_i == per) {
-      next_i = 0;
-      next_tile += gridDim.x;
+    constexpr int kWords = G / 32;               // words in a row of bytes
+#pragma unroll
+    for (int j = 0; j < 4; j += kWords) {
+      const int off = word_column<G>(j, 0) / 2;
+      const bool in = next_byte + off < row_bytes;
+      load_words<kWords>(&r.w[0][j], next + off, in && live0);
+      load_words<kWords>(&r.w[1][j], next + 8ll * row_bytes + off, in && live1);
+    }
+    next += kSpan / 2;
+    next_byte += kSpan / 2;
+  };
+  auto turn = [&]() {                                      // after a quad: to the next tile?
+    if (next_byte == byte1) {
+      next_byte = byte0;
+      next += tile_step;
+      next_tile += step;
+      enter();
     }
   };
+  Span ring[kQuad] = {};
+  if (first < tiles) {
 #pragma unroll
-  for (int q = 0; q < kDepth; ++q) refill(ring[q]);
-  for (int e = tid; e < tile_scales; e += kThreads) {
-    ws[e] = a.w.scales[scale_at(blockIdx.x, e)];
-    if (ZEROS) wz[e] = a.w.zeros[scale_at(blockIdx.x, e)];
+    for (int d = 0; d < kQuad; ++d) refill(ring[d]);
+    turn();
   }
+  auto row_at = [&](int tile, int h) {                     // scales of row g + 8 h, the last row's past the end
+    return min((long long)tile * kTileRows + g + 8 * h, (long long)a.w.out - 1) * groups;
+  };
+  Quad<G> n_0 = {}, n_1 = {};
+  if (first < tiles) {
+    n_0.template load<ZEROS>(a.w, row_at(first, 0), q_lo * Quad<G>::kGroups, groups, scale_vec);
+    n_1.template load<ZEROS>(a.w, row_at(first, 1), q_lo * Quad<G>::kGroups, groups, scale_vec);
+  }
+  if (tid == 0) xs[-1] = make_uint4(0u, 0u, 0u, 0u);
   for (int u = tid; u < spans * 16 * rows; u += kThreads) {
     const int n = u / (spans * 16), unit = u - n * (spans * 16);
     const int span = unit >> 4, k8 = unit & 15;
@@ -298,141 +359,136 @@ __global__ void __launch_bounds__(kThreads, 1) linear_w4_kernel(const LinearW4Ar
       xscale[u] = a.x_scale[(long long)(n0 + u % cols) * groups + u / cols];
   __syncthreads();
 
-  float acc[NT][4] = {};
-  int tile = blockIdx.x, i = 0, buf = 0;
-  __nv_bfloat16 sreg[kRegScales];
-  uint8_t zreg[kRegScales];
-  while (tile < tiles) {
+  // this lane's column of x in each eight: a column past the last reads the zeros
+  int x_step[NT];                                        // units from one word to the next
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d) {
-      if (tile >= tiles) break;
-      const int span = i * kWarps + warp;
-      if (i == 0 && tile + (int)gridDim.x < tiles) {       // the next tile's scales set out
+  for (int nt = 0; nt < NT; ++nt) x_step[nt] = nt * 8 + g < cols ? 4 * cols : 0;
+  float* mine = part + warp * kTileRows * 8 * NT;
+  const float* tile_part = part + team * split * kTileRows * 8 * NT;
+  for (int tile = first; tile < tiles; tile += step) {
+    float acc[NT][4] = {};
+    const uint4* x_at[NT];
 #pragma unroll
-        for (int q = 0; q < kRegScales; ++q) {
-          const int e = tid + q * kThreads;
-          if (e < tile_scales) {
-            sreg[q] = a.w.scales[scale_at(tile + gridDim.x, e)];
-            if (ZEROS) zreg[q] = a.w.zeros[scale_at(tile + gridDim.x, e)];
-          }
+    for (int nt = 0; nt < NT; ++nt)
+      x_at[nt] = nt * 8 + g < cols ? xs + (q_lo * kQuad * 16 + t) * cols + nt * 8 + g : xs - 1;
+    for (int quad = q_lo; quad < q_hi; ++quad) {
+      const Quad<G> c_0 = n_0, c_1 = n_1;
+      {
+        const bool same = quad + 1 < q_hi;
+        const int tt = same ? tile : tile + step, qq = same ? quad + 1 : q_lo;
+        if (tt < tiles) {
+          n_0.template load<ZEROS>(a.w, row_at(tt, 0), qq * Quad<G>::kGroups, groups, scale_vec);
+          n_1.template load<ZEROS>(a.w, row_at(tt, 1), qq * Quad<G>::kGroups, groups, scale_vec);
         }
       }
-      if (span < spans) {
-        const Span& r = ring[d];
-        const __nv_bfloat16* sp = ws + buf * tile_scales + g * groups;
-        const uint8_t* zp = wz + buf * tile_scales + g * groups;
 #pragma unroll
-        for (int ii = 0; ii < kSpan / G; ++ii) {
-          const int gi = span * (kSpan / G) + ii;
-          const int gs = kSpan / G == 1 ? gi : min(gi, groups - 1);   // past the last group x is 0
-          float sum[NT][4] = {};
-          uint32_t z0 = 0x43084308u, z1 = 0x43084308u;
-          if (ZEROS) {
-            z0 = 0x43004300u | zp[gs] * 0x10001u;
-            z1 = 0x43004300u | zp[8 * groups + gs] * 0x10001u;
-          }
+      for (int d = 0; d < kQuad; ++d) {
+        const int span = quad * kQuad + d;
+        if (span < spans) {
+          const Span& r = ring[d];
 #pragma unroll
-          for (int jj = 0; jj < G / 32; ++jj) {
-            const int j = ii * (G / 32) + jj;
-            uint32_t w0[4], w1[4];               // column pairs 0 4, 1 5, 2 6, 3 7
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-              // 0x4300 | c is the bf16 number 128 + c
-              w0[p] = bf16_sub2(((r.w[0][j] >> (4 * p)) & 0x000F000Fu) | 0x43004300u, z0);
-              w1[p] = bf16_sub2(((r.w[1][j] >> (4 * p)) & 0x000F000Fu) | 0x43004300u, z1);
+          for (int ii = 0; ii < kSpan / G; ++ii) {
+            const int gq = d * (kSpan / G) + ii;           // of the quad's groups
+            float sum[NT][4] = {};
+            uint32_t z0 = 0x43084308u, z1 = 0x43084308u;
+            if (ZEROS) {
+              z0 = c_0.zero2(gq);
+              z1 = c_1.zero2(gq);
             }
+#pragma unroll
+            for (int jj = 0; jj < G / 32; ++jj) {
+              const int j = ii * (G / 32) + jj;
+              uint32_t w0[4], w1[4];               // column pairs 0 4, 1 5, 2 6, 3 7
+#pragma unroll
+              for (int p = 0; p < 4; ++p) {
+                // 0x4300 | c is the bf16 number 128 + c
+                w0[p] = bf16_sub2(((r.w[0][j] >> (4 * p)) & 0x000F000Fu) | 0x43004300u, z0);
+                w1[p] = bf16_sub2(((r.w[1][j] >> (4 * p)) & 0x000F000Fu) | 0x43004300u, z1);
+              }
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                const uint4 b = *x_at[nt];
+                x_at[nt] += x_step[nt];
+                mma_16x8x16(sum[nt], w0[0], w1[0], w0[1], w1[1], b.x, b.y);
+                mma_16x8x16(sum[nt], w0[2], w1[2], w0[3], w1[3], b.z, b.w);
+              }
+            }
+            const float s0 = c_0.scale(gq), s1 = c_1.scale(gq);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              uint4 b = make_uint4(0u, 0u, 0u, 0u);
-              if (nt * 8 + g < cols) b = xs[((span * 4 + j) * 4 + t) * cols + nt * 8 + g];
-              mma_16x8x16(sum[nt], w0[0], w1[0], w0[1], w1[1], b.x, b.y);
-              mma_16x8x16(sum[nt], w0[2], w1[2], w0[3], w1[3], b.z, b.w);
+              if (by_group) {
+                const int n = nt * 8 + 2 * t, gs = min(quad * Quad<G>::kGroups + gq, groups - 1);
+                const float x0 = n < cols ? xscale[gs * cols + n] : 0.0f;
+                const float x1 = n + 1 < cols ? xscale[gs * cols + n + 1] : 0.0f;
+                acc[nt][0] = fmaf(sum[nt][0], s0 * x0, acc[nt][0]);
+                acc[nt][1] = fmaf(sum[nt][1], s0 * x1, acc[nt][1]);
+                acc[nt][2] = fmaf(sum[nt][2], s1 * x0, acc[nt][2]);
+                acc[nt][3] = fmaf(sum[nt][3], s1 * x1, acc[nt][3]);
+              } else {
+                acc[nt][0] = fmaf(sum[nt][0], s0, acc[nt][0]);
+                acc[nt][1] = fmaf(sum[nt][1], s0, acc[nt][1]);
+                acc[nt][2] = fmaf(sum[nt][2], s1, acc[nt][2]);
+                acc[nt][3] = fmaf(sum[nt][3], s1, acc[nt][3]);
+              }
             }
           }
-          const float s0 = __bfloat162float(sp[gs]), s1 = __bfloat162float(sp[8 * groups + gs]);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float x0 = 1.0f, x1 = 1.0f;
-            if (by_group) {
-              const int n = nt * 8 + 2 * t;
-              x0 = n < cols ? xscale[gs * cols + n] : 0.0f;
-              x1 = n + 1 < cols ? xscale[gs * cols + n + 1] : 0.0f;
-            }
-            acc[nt][0] = fmaf(sum[nt][0], s0 * x0, acc[nt][0]);
-            acc[nt][1] = fmaf(sum[nt][1], s0 * x1, acc[nt][1]);
-            acc[nt][2] = fmaf(sum[nt][2], s1 * x0, acc[nt][2]);
-            acc[nt][3] = fmaf(sum[nt][3], s1 * x1, acc[nt][3]);
-          }
         }
+        refill(ring[d]);
       }
-      refill(ring[d]);
-      if (++i < per) continue;
-      // the tile's end
-      float* mine = part + buf * (kWarps * kTileRows * 8 * NT);
+      turn();
+    }
+    // the tile's end
+    if (split > 1) team_sync(team, split);                 // the last tile has been read
+    else __syncwarp();
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          *reinterpret_cast<float2*>(mine + (warp * kTileRows + g + 8 * h) * 8 * NT + nt * 8 + 2 * t) =
-              make_float2(acc[nt][2 * h], acc[nt][2 * h + 1]);
-          acc[nt][2 * h] = acc[nt][2 * h + 1] = 0.0f;
-        }
-      if (tile + (int)gridDim.x < tiles) {
-        const int other = (buf ^ 1) * tile_scales;
-#pragma unroll
-        for (int q = 0; q < kRegScales; ++q) {
-          const int e = tid + q * kThreads;
-          if (e < tile_scales) {
-            ws[other + e] = sreg[q];
-            if (ZEROS) wz[other + e] = zreg[q];
-          }
-        }
-        for (int e = tid + kRegScales * kThreads; e < tile_scales; e += kThreads) {
-          ws[other + e] = a.w.scales[scale_at(tile + gridDim.x, e)];
-          if (ZEROS) wz[other + e] = a.w.zeros[scale_at(tile + gridDim.x, e)];
-        }
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<float2*>(mine + (g + 8 * h) * 8 * NT + nt * 8 + 2 * t) =
+            make_float2(acc[nt][2 * h], acc[nt][2 * h + 1]);
+    if (split > 1) team_sync(team, split);
+    else __syncwarp();
+    for (int u = rank * 32 + lane; u < kTileRows * rows; u += 32 * split) {
+      const int r = u & (kTileRows - 1), n = u / kTileRows;
+      const long long o = (long long)tile * kTileRows + r;
+      float v = 0.0f;
+      const float* from = tile_part + r * 8 * NT + n * parts;
+      for (int p = 0; p < parts; ++p)
+        for (int w = 0; w < split; ++w) v += from[w * kTileRows * 8 * NT + p];
+      if (o < a.w.out) {
+        if (a.x_scale != nullptr && !by_group) v *= a.x_scale[n0 + n];
+        if (a.bias != nullptr) v += a.bias[o];
+        const long long at = (long long)(n0 + n) * a.w.out + o;
+        if (a.y_dtype == FOVEA_BF16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
+        else static_cast<float*>(a.y)[at] = v;
       }
-      // one barrier a tile: the buffers written here were last read before the
-      // previous tile's barrier
-      __syncthreads();
-      for (int u = tid; u < kTileRows * rows; u += kThreads) {
-        const int r = u & (kTileRows - 1), n = u / kTileRows;
-        const long long o = (long long)tile * kTileRows + r;
-        float v = 0.0f;
-        const float* from = mine + r * 8 * NT + n * parts;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) v += from[w * kTileRows * 8 * NT];
-        for (int p = 1; p < parts; ++p)
-#pragma unroll
-          for (int w = 0; w < kWarps; ++w) v += from[w * kTileRows * 8 * NT + p];
-        if (o < a.w.out) {
-          if (a.x_scale != nullptr && !by_group) v *= a.x_scale[n0 + n];
-          if (a.bias != nullptr) v += a.bias[o];
-          const long long at = (long long)(n0 + n) * a.w.out + o;
-          if (a.y_dtype == FOVEA_BF16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
-          else static_cast<float*>(a.y)[at] = v;
-        }
-      }
-      i = 0;
-      buf ^= 1;
-      tile += gridDim.x;
     }
   }
 }
 
 template <int G, int NT, bool ZEROS>
-cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, size_t smem, int grid, cudaStream_t s) {
-  cudaError_t e = cudaFuncSetAttribute(linear_w4_kernel<G, NT, ZEROS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       227 * 1024);
+cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, size_t smem, cudaStream_t s) {
+  auto kern = linear_w4_kernel<G, NT, ZEROS>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
   if (e != cudaSuccess) return e;
   const bool x_vec = a.x_dtype == FOVEA_BF16 && (reinterpret_cast<uintptr_t>(a.x) & 15u) == 0 && a.x_ld % 8 == 0;
-  return launch_pdl(linear_w4_kernel<G, NT, ZEROS>, dim3(grid), dim3(kThreads), smem, s, a, n0, n1, x_vec);
+  const int groups = (a.w.in + G - 1) / G;
+  const bool scale_vec = groups % Quad<G>::kGroups == 0 && (reinterpret_cast<uintptr_t>(a.w.scales) & 15u) == 0 &&
+                         (reinterpret_cast<uintptr_t>(a.w.zeros) & 3u) == 0;
+  const int tiles = (a.w.out + kTileRows - 1) / kTileRows;
+  const int quads = (a.w.in + kQuad * kSpan - 1) / (kQuad * kSpan);
+  // warps a tile: few tiles are split until each warp of the device has work
+  int split = 1;
+  while (split < 8 && split * 2 <= quads && (long long)tiles * split * 2 <= 152 * kWarps) split *= 2;
+  const long long work = (long long)tiles * split;
+  const int grid = (int)std::min<long long>(152, std::max<long long>(1, split == 1 ? work : (work + split - 1) / split));
+  return launch_pdl(kern, dim3(grid), dim3(kThreads), smem, s, a, n0, n1, split, x_vec, scale_vec);
 }
 template <int G>
-cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, int nt, size_t smem, int grid, cudaStream_t s) {
+cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, int nt, size_t smem, cudaStream_t s) {
   if (a.w.zeros != nullptr)
-    return nt == 1 ? launch_few<G, 1, true>(a, n0, n1, smem, grid, s) : launch_few<G, 2, true>(a, n0, n1, smem, grid, s);
-  return nt == 1 ? launch_few<G, 1, false>(a, n0, n1, smem, grid, s) : launch_few<G, 2, false>(a, n0, n1, smem, grid, s);
+    return nt == 1 ? launch_few<G, 1, true>(a, n0, n1, smem, s) : launch_few<G, 2, true>(a, n0, n1, smem, s);
+  return nt == 1 ? launch_few<G, 1, false>(a, n0, n1, smem, s) : launch_few<G, 2, false>(a, n0, n1, smem, s);
 }
 
 }  // namespace
@@ -461,18 +517,15 @@ cudaError_t launch_quantize_w4(int dtype, const void* W, long long ld, int out, 
 // Columns of x (an fp32 row counts three times) that the warps' registers take;
 // beyond them the codes go through tensor memory.
 constexpr int kFewCols = 16;
-// Shared memory of the few-column product: of a column, and whatever their number
-// (with zero points, so that the choice of path does not depend on them).
+// Shared memory of the few-column product: of a column, and whatever their number.
 static long long col_bytes(int in, int group, bool by_group) {
   return (in + kSpan - 1) / kSpan * 256ll + (by_group ? 4ll * ((in + group - 1) / group) : 0);
 }
-static long long fixed_bytes(int in, int group) {
-  return 2 * kWarps * kTileRows * 16 * 4 + 2ll * kTileRows * ((in + group - 1) / group) * 3;
-}
+constexpr long long kFixedBytes = 16 + kWarps * kTileRows * kFewCols * 4;
 static long long few_rows(int in, int group, int x_dtype, bool by_group) {    // of a launch
   const int parts = x_dtype == FOVEA_FP32 ? 3 : 1;
   return std::min<long long>(kFewCols / parts,
-                             (227 * 1024 - fixed_bytes(in, group)) / (col_bytes(in, group, by_group) * parts));
+                             (kMaxSmem - kFixedBytes) / (col_bytes(in, group, by_group) * parts));
 }
 static bool is_few(int N, int in, int group, int x_dtype, bool by_group) {
   return (long long)N * (x_dtype == FOVEA_FP32 ? 3 : 1) <= kFewCols && few_rows(in, group, x_dtype, by_group) > 0;
@@ -488,15 +541,13 @@ cudaError_t launch_linear_w4(const LinearW4Args& a, cudaStream_t s) {
   if (!is_few(a.N, a.w.in, a.w.group, a.x_dtype, by_group)) return launch_linear_w4_tc(a, s);
   const int parts = a.x_dtype == FOVEA_FP32 ? 3 : 1;
   const int rows = (int)few_rows(a.w.in, a.w.group, a.x_dtype, by_group);
-  const int tiles = (a.w.out + kTileRows - 1) / kTileRows;
-  const int grid = std::min(tiles, 152);
   for (int n0 = 0; n0 < a.N; n0 += rows) {
     const int n1 = std::min(a.N, n0 + rows);
     const int cols = (n1 - n0) * parts, nt = cols <= 8 ? 1 : 2;
-    const size_t smem = cols * col_bytes(a.w.in, a.w.group, by_group) + fixed_bytes(a.w.in, a.w.group);
-    const cudaError_t e = a.w.group == 128 ? launch_few<128>(a, n0, n1, nt, smem, grid, s)
-                          : a.w.group == 64 ? launch_few<64>(a, n0, n1, nt, smem, grid, s)
-                                            : launch_few<32>(a, n0, n1, nt, smem, grid, s);
+    const size_t smem = (size_t)(cols * col_bytes(a.w.in, a.w.group, by_group) + kFixedBytes);
+    const cudaError_t e = a.w.group == 128 ? launch_few<128>(a, n0, n1, nt, smem, s)
+                          : a.w.group == 64 ? launch_few<64>(a, n0, n1, nt, smem, s)
+                                            : launch_few<32>(a, n0, n1, nt, smem, s);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
