@@ -389,7 +389,7 @@ FOVEA_API fovea_status fovea_quantize_w4(const void* W, int64_t ld, int out_feat
  *   bias    [out_features] fp32, or NULL
  *   y       [N, out_features] y_dtype: FOVEA_FP32 or FOVEA_BF16
  *   workspace  fovea_linear_w4_workspace_size bytes (256-byte aligned; NULL when
- *           that is 0, as for up to 16 rows, 5 of fp32, of 16384 columns).  It needs no
+ *           that is 0, as for up to 8 rows, 2 of fp32, of 16384 columns).  It needs no
  *           initialisation and may serve the next call on the stream.  A bounded
  *           device wait that gives up leaves NaN in the y it did not reach and
  *           FOVEA_ERR_TIMEOUT for fovea_sync_errors(workspace).

@@ -378,6 +378,16 @@ struct W4 {
   const uint8_t* codes; const __nv_bfloat16* scales; const uint8_t* zeros;
   int out, in, group;
 };
+// 128 + c as bf16 in both halves, from two codes c in the lowest four bits of the
+// halves of w: bits 0x4300 | c.  One instruction takes both constants only when one of
+// them is in a register; the compiler would rather fold them and spend two, so the
+// kernels get `k128` (kW4One28) as an argument.
+constexpr uint32_t kW4One28 = 0x43004300u;
+__device__ __forceinline__ uint32_t w4_pair(uint32_t w, uint32_t k128) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(r) : "r"(w), "r"(k128));   // (w & mask) | k128
+  return r;
+}
 cudaError_t launch_quantize_w4(int dtype, const void* W, long long ld, int out, int in, int group,
                                uint8_t* codes, __nv_bfloat16* scales, uint8_t* zeros, cudaStream_t s);
 // y[n, o] = sum_k x[n, k] w[o, k] (+ bias[o]).  x_scale: null, or of e4m3 rows

@@ -109,6 +109,12 @@ constexpr int kWarps = 16, kThreads = 32 * kWarps;
 constexpr int kSpan = 128;             // columns a warp handles together
 constexpr int kTileRows = 16;          // weight rows of a tile
 constexpr int kQuad = 4;               // spans of codes a warp has on their way
+// Columns of x (an fp32 row counts three times) that a tile takes: the tensor-core
+// instruction's eight.  More go through tensor memory (w4_tc.cu): with two such
+// instructions a word 16 rows by 4096 x 32000 took 44.8 us here against 27.3 there, 8
+// rows 26.4.
+constexpr int kFewCols = 8;
+constexpr int kTilePart = kTileRows * kFewCols;
 
 // Offset within a span of the eight columns of word j of lane quarter t: the
 // four quarters of a warp's lanes share the sum of one tensor-core product, so
@@ -130,20 +136,20 @@ __device__ __forceinline__ uint32_t bf16_sub2(uint32_t a, uint32_t b) {
 // so waited for, at once).  Codes are read once: they need not displace x and the
 // scales in L1; runs shorter than a sector share it with the next.
 template <int N>
-__device__ __forceinline__ void load_words(uint32_t* r, const uint8_t* p, bool live) {
+__device__ __forceinline__ void load_words(uint32_t* r, const uint8_t* p, uint32_t live) {
   if (N == 4)
     asm volatile(
         "{\n .reg .pred q;\n setp.ne.u32 q, %5, 0;\n"
         " @q ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n}"
-        : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]) : "l"(p), "r"((uint32_t)live));
+        : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]) : "l"(p), "r"(live));
   else if (N == 2)
     asm volatile(
         "{\n .reg .pred q;\n setp.ne.u32 q, %3, 0;\n @q ld.global.nc.v2.u32 {%0, %1}, [%2];\n}"
-        : "+r"(r[0]), "+r"(r[1]) : "l"(p), "r"((uint32_t)live));
+        : "+r"(r[0]), "+r"(r[1]) : "l"(p), "r"(live));
   else
     asm volatile(
         "{\n .reg .pred q;\n setp.ne.u32 q, %2, 0;\n @q ld.global.nc.u32 %0, [%1];\n}"
-        : "+r"(r[0]) : "l"(p), "r"((uint32_t)live));
+        : "+r"(r[0]) : "l"(p), "r"(live));
 }
 // A barrier of the `split` warps of a team (barriers 1 to 8).
 __device__ __forceinline__ void team_sync(int team, int split) {
@@ -164,11 +170,24 @@ __device__ __forceinline__ void split3(float v, uint32_t& b0, uint32_t& b1, uint
 }
 __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                             uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
       "{%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The first product of a sum.
+__device__ __forceinline__ void mma_16x8x16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                                  uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+      "{%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
+// x from shared memory, which nothing writes once it is laid out (so: not volatile).
+__device__ __forceinline__ uint4 lds_x(uint32_t at) {
+  uint4 v;
+  asm("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+  return v;
 }
 
 // The codes of one span of weight rows g and g + 8 that this lane holds.
@@ -252,7 +271,7 @@ struct Quad {
   }
 };
 
-// y of up to 8 NT columns (rows of x, an fp32 row as three) in one launch.
+// y of up to kFewCols columns (rows of x, an fp32 row as three) in one launch.
 //
 // `split` warps take a tile of 16 weight rows, each a range of its quads (four spans of
 // 128 columns); a warp goes from tile to tile by itself, x in shared memory.  It
@@ -264,9 +283,10 @@ struct Quad {
 //
 // fp32 rows enter as three bf16 rows that add up to them exactly; e4m3 rows are
 // exact in bf16 and their scales join the group's or the result.
-template <int G, int NT, bool ZEROS>
+template <int G, bool ZEROS>
 __global__ void __launch_bounds__(kThreads, 1)
-linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bool scale_vec) {
+linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bool scale_vec,
+                 uint32_t k128) {
   extern __shared__ __align__(16) uint8_t smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int parts = a.x_dtype == FOVEA_FP32 ? 3 : 1;
@@ -277,7 +297,7 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
   // warp's partial tile [row][column]; scales of x [group][column]
   uint4* xs = reinterpret_cast<uint4*>(smem) + 1;
   float* part = reinterpret_cast<float*>(xs + (long long)spans * 16 * cols);
-  float* xscale = part + kWarps * kTileRows * 8 * NT;
+  float* xscale = part + kWarps * kTilePart;
   const bool by_group = a.x_scale != nullptr && a.x_group != 0;
   const int tiles = (a.w.out + kTileRows - 1) / kTileRows;
   const int quads = (spans + kQuad - 1) / kQuad;
@@ -288,45 +308,45 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
 
   pdl_wait();
   pdl_trigger();
-  // The next codes: this lane's first word of row g of the tile, and how far it is
-  // into the row.  A word past its row's end, or of a row past the last, keeps what
-  // the register held: x is 0 there, or the result is not stored.
+  // The next quad's codes: this lane's first words of rows g and g + 8 (past the last
+  // row, of that one again: the results are not stored), and how far they are into the
+  // row.  A word past its row's end keeps what the register held: x is 0 there.
   const int row_bytes = a.w.in / 2;
-  const int byte0 = q_lo * kQuad * (kSpan / 2) + word_column<G>(0, t) / 2;
-  const int byte1 = q_hi * kQuad * (kSpan / 2) + word_column<G>(0, t) / 2;
-  const uint8_t* next = a.w.codes + ((long long)first * kTileRows + g) * row_bytes + byte0;
-  const long long tile_step = (long long)step * kTileRows * row_bytes - (byte1 - byte0);
-  int next_tile = first, next_byte = byte0;
-  bool live0 = false, live1 = false;
-  auto enter = [&]() {                                     // a tile's rows
-    live0 = next_tile < tiles && next_tile * kTileRows + g < a.w.out;
-    live1 = next_tile < tiles && next_tile * kTileRows + g + 8 < a.w.out;
+  constexpr int kQuadBytes = kQuad * kSpan / 2;
+  const int lane_byte = word_column<G>(0, t) / 2;
+  const uint8_t *next0, *next1;
+  int next_tile = first, next_quad = q_lo;
+  auto enter = [&]() {                                     // a tile
+    const long long row = (long long)next_tile * kTileRows + g, last = a.w.out - 1;
+    next0 = a.w.codes + min(row, last) * row_bytes + q_lo * kQuadBytes + lane_byte;
+    next1 = a.w.codes + min(row + 8, last) * row_bytes + q_lo * kQuadBytes + lane_byte;
   };
-  enter();
-  auto refill = [&](Span& r) {
+  auto refill = [&](Span& r, int d) {
     constexpr int kWords = G / 32;               // words in a row of bytes
 #pragma unroll
     for (int j = 0; j < 4; j += kWords) {
-      const int off = word_column<G>(j, 0) / 2;
-      const bool in = next_byte + off < row_bytes;
-      load_words<kWords>(&r.w[0][j], next + off, in && live0);
-      load_words<kWords>(&r.w[1][j], next + 8ll * row_bytes + off, in && live1);
+      const int off = d * (kSpan / 2) + word_column<G>(j, 0) / 2;
+      uint32_t in = next_tile < tiles;
+      if (in && (next_quad + 1) * kQuadBytes > row_bytes)  // the row's last quad, cut short
+        in = next_quad * kQuadBytes + lane_byte + off < row_bytes;
+      load_words<kWords>(&r.w[0][j], next0 + off, in);
+      load_words<kWords>(&r.w[1][j], next1 + off, in);
     }
-    next += kSpan / 2;
-    next_byte += kSpan / 2;
   };
-  auto turn = [&]() {                                      // after a quad: to the next tile?
-    if (next_byte == byte1) {
-      next_byte = byte0;
-      next += tile_step;
+  auto turn = [&]() {                                      // after a quad
+    next0 += kQuadBytes;
+    next1 += kQuadBytes;
+    if (++next_quad == q_hi) {
+      next_quad = q_lo;
       next_tile += step;
-      enter();
+      if (next_tile < tiles) enter();
     }
   };
   Span ring[kQuad] = {};
   if (first < tiles) {
+    enter();
 #pragma unroll
-    for (int d = 0; d < kQuad; ++d) refill(ring[d]);
+    for (int d = 0; d < kQuad; ++d) refill(ring[d], d);
     turn();
   }
   auto row_at = [&](int tile, int h) {                     // scales of row g + 8 h, the last row's past the end
@@ -339,7 +359,8 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
   }
   if (tid == 0) xs[-1] = make_uint4(0u, 0u, 0u, 0u);
   for (int u = tid; u < spans * 16 * rows; u += kThreads) {
-    const int n = u / (spans * 16), unit = u - n * (spans * 16);
+    // neighbouring lanes take neighbouring rows, whose units lie side by side
+    const int unit = u / rows, n = u - unit * rows;
     const int span = unit >> 4, k8 = unit & 15;
     int j, q;                                  // word and quarter of these columns
     if (G == 128) { q = k8 >> 2; j = k8 & 3; }
@@ -359,18 +380,15 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
       xscale[u] = a.x_scale[(long long)(n0 + u % cols) * groups + u / cols];
   __syncthreads();
 
-  // this lane's column of x in each eight: a column past the last reads the zeros
-  int x_step[NT];                                        // units from one word to the next
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) x_step[nt] = nt * 8 + g < cols ? 4 * cols : 0;
-  float* mine = part + warp * kTileRows * 8 * NT;
-  const float* tile_part = part + team * split * kTileRows * 8 * NT;
+  // this lane's column of x: a column past the last reads the zeros
+  const uint32_t x_step = g < cols ? 64u * cols : 0u;    // bytes from one word to the next
+  const uint32_t x_first =
+      (uint32_t)__cvta_generic_to_shared(g < cols ? xs + (q_lo * kQuad * 16 + t) * cols + g : xs - 1);
+  float* mine = part + warp * kTilePart;
+  const float* tile_part = part + team * split * kTilePart;
   for (int tile = first; tile < tiles; tile += step) {
-    float acc[NT][4] = {};
-    const uint4* x_at[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-      x_at[nt] = nt * 8 + g < cols ? xs + (q_lo * kQuad * 16 + t) * cols + nt * 8 + g : xs - 1;
+    float acc[4] = {};
+    uint32_t x_at = x_first;
     for (int quad = q_lo; quad < q_hi; ++quad) {
       const Quad<G> c_0 = n_0, c_1 = n_1;
       {
@@ -389,7 +407,7 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
 #pragma unroll
           for (int ii = 0; ii < kSpan / G; ++ii) {
             const int gq = d * (kSpan / G) + ii;           // of the quad's groups
-            float sum[NT][4] = {};
+            float sum[4];
             uint32_t z0 = 0x43084308u, z1 = 0x43084308u;
             if (ZEROS) {
               z0 = c_0.zero2(gq);
@@ -401,39 +419,33 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
               uint32_t w0[4], w1[4];               // column pairs 0 4, 1 5, 2 6, 3 7
 #pragma unroll
               for (int p = 0; p < 4; ++p) {
-                // 0x4300 | c is the bf16 number 128 + c
-                w0[p] = bf16_sub2(((r.w[0][j] >> (4 * p)) & 0x000F000Fu) | 0x43004300u, z0);
-                w1[p] = bf16_sub2(((r.w[1][j] >> (4 * p)) & 0x000F000Fu) | 0x43004300u, z1);
+                w0[p] = bf16_sub2(w4_pair(r.w[0][j] >> (4 * p), k128), z0);
+                w1[p] = bf16_sub2(w4_pair(r.w[1][j] >> (4 * p), k128), z1);
               }
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                const uint4 b = *x_at[nt];
-                x_at[nt] += x_step[nt];
-                mma_16x8x16(sum[nt], w0[0], w1[0], w0[1], w1[1], b.x, b.y);
-                mma_16x8x16(sum[nt], w0[2], w1[2], w0[3], w1[3], b.z, b.w);
-              }
+              const uint4 b = lds_x(x_at);
+              x_at += x_step;
+              if (jj == 0) mma_16x8x16_first(sum, w0[0], w1[0], w0[1], w1[1], b.x, b.y);
+              else mma_16x8x16(sum, w0[0], w1[0], w0[1], w1[1], b.x, b.y);
+              mma_16x8x16(sum, w0[2], w1[2], w0[3], w1[3], b.z, b.w);
             }
             const float s0 = c_0.scale(gq), s1 = c_1.scale(gq);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              if (by_group) {
-                const int n = nt * 8 + 2 * t, gs = min(quad * Quad<G>::kGroups + gq, groups - 1);
-                const float x0 = n < cols ? xscale[gs * cols + n] : 0.0f;
-                const float x1 = n + 1 < cols ? xscale[gs * cols + n + 1] : 0.0f;
-                acc[nt][0] = fmaf(sum[nt][0], s0 * x0, acc[nt][0]);
-                acc[nt][1] = fmaf(sum[nt][1], s0 * x1, acc[nt][1]);
-                acc[nt][2] = fmaf(sum[nt][2], s1 * x0, acc[nt][2]);
-                acc[nt][3] = fmaf(sum[nt][3], s1 * x1, acc[nt][3]);
-              } else {
-                acc[nt][0] = fmaf(sum[nt][0], s0, acc[nt][0]);
-                acc[nt][1] = fmaf(sum[nt][1], s0, acc[nt][1]);
-                acc[nt][2] = fmaf(sum[nt][2], s1, acc[nt][2]);
-                acc[nt][3] = fmaf(sum[nt][3], s1, acc[nt][3]);
-              }
+            if (by_group) {
+              const int n = 2 * t, gs = min(quad * Quad<G>::kGroups + gq, groups - 1);
+              const float x0 = n < cols ? xscale[gs * cols + n] : 0.0f;
+              const float x1 = n + 1 < cols ? xscale[gs * cols + n + 1] : 0.0f;
+              acc[0] = fmaf(sum[0], s0 * x0, acc[0]);
+              acc[1] = fmaf(sum[1], s0 * x1, acc[1]);
+              acc[2] = fmaf(sum[2], s1 * x0, acc[2]);
+              acc[3] = fmaf(sum[3], s1 * x1, acc[3]);
+            } else {
+              acc[0] = fmaf(sum[0], s0, acc[0]);
+              acc[1] = fmaf(sum[1], s0, acc[1]);
+              acc[2] = fmaf(sum[2], s1, acc[2]);
+              acc[3] = fmaf(sum[3], s1, acc[3]);
             }
           }
         }
-        refill(ring[d]);
+        refill(ring[d], d);
       }
       turn();
     }
@@ -441,20 +453,17 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
     if (split > 1) team_sync(team, split);                 // the last tile has been read
     else __syncwarp();
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        *reinterpret_cast<float2*>(mine + (g + 8 * h) * 8 * NT + nt * 8 + 2 * t) =
-            make_float2(acc[nt][2 * h], acc[nt][2 * h + 1]);
+    for (int h = 0; h < 2; ++h)
+      *reinterpret_cast<float2*>(mine + (g + 8 * h) * kFewCols + 2 * t) = make_float2(acc[2 * h], acc[2 * h + 1]);
     if (split > 1) team_sync(team, split);
     else __syncwarp();
     for (int u = rank * 32 + lane; u < kTileRows * rows; u += 32 * split) {
       const int r = u & (kTileRows - 1), n = u / kTileRows;
       const long long o = (long long)tile * kTileRows + r;
       float v = 0.0f;
-      const float* from = tile_part + r * 8 * NT + n * parts;
+      const float* from = tile_part + r * kFewCols + n * parts;
       for (int p = 0; p < parts; ++p)
-        for (int w = 0; w < split; ++w) v += from[w * kTileRows * 8 * NT + p];
+        for (int w = 0; w < split; ++w) v += from[w * kTilePart + p];
       if (o < a.w.out) {
         if (a.x_scale != nullptr && !by_group) v *= a.x_scale[n0 + n];
         if (a.bias != nullptr) v += a.bias[o];
@@ -466,9 +475,9 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
   }
 }
 
-template <int G, int NT, bool ZEROS>
+template <int G, bool ZEROS>
 cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, size_t smem, cudaStream_t s) {
-  auto kern = linear_w4_kernel<G, NT, ZEROS>;
+  auto kern = linear_w4_kernel<G, ZEROS>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
   if (e != cudaSuccess) return e;
   const bool x_vec = a.x_dtype == FOVEA_BF16 && (reinterpret_cast<uintptr_t>(a.x) & 15u) == 0 && a.x_ld % 8 == 0;
@@ -482,13 +491,12 @@ cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, size_t smem, cudaS
   while (split < 8 && split * 2 <= quads && (long long)tiles * split * 2 <= 152 * kWarps) split *= 2;
   const long long work = (long long)tiles * split;
   const int grid = (int)std::min<long long>(152, std::max<long long>(1, split == 1 ? work : (work + split - 1) / split));
-  return launch_pdl(kern, dim3(grid), dim3(kThreads), smem, s, a, n0, n1, split, x_vec, scale_vec);
+  return launch_pdl(kern, dim3(grid), dim3(kThreads), smem, s, a, n0, n1, split, x_vec, scale_vec,
+                    kW4One28);
 }
 template <int G>
-cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, int nt, size_t smem, cudaStream_t s) {
-  if (a.w.zeros != nullptr)
-    return nt == 1 ? launch_few<G, 1, true>(a, n0, n1, smem, s) : launch_few<G, 2, true>(a, n0, n1, smem, s);
-  return nt == 1 ? launch_few<G, 1, false>(a, n0, n1, smem, s) : launch_few<G, 2, false>(a, n0, n1, smem, s);
+cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, size_t smem, cudaStream_t s) {
+  return a.w.zeros != nullptr ? launch_few<G, true>(a, n0, n1, smem, s) : launch_few<G, false>(a, n0, n1, smem, s);
 }
 
 }  // namespace
@@ -514,14 +522,11 @@ cudaError_t launch_quantize_w4(int dtype, const void* W, long long ld, int out, 
   return vec ? go(quantize_w4_kernel<float, true>, w) : go(quantize_w4_kernel<float, false>, w);
 }
 
-// Columns of x (an fp32 row counts three times) that the warps' registers take;
-// beyond them the codes go through tensor memory.
-constexpr int kFewCols = 16;
 // Shared memory of the few-column product: of a column, and whatever their number.
 static long long col_bytes(int in, int group, bool by_group) {
   return (in + kSpan - 1) / kSpan * 256ll + (by_group ? 4ll * ((in + group - 1) / group) : 0);
 }
-constexpr long long kFixedBytes = 16 + kWarps * kTileRows * kFewCols * 4;
+constexpr long long kFixedBytes = 16 + kWarps * kTilePart * 4;
 static long long few_rows(int in, int group, int x_dtype, bool by_group) {    // of a launch
   const int parts = x_dtype == FOVEA_FP32 ? 3 : 1;
   return std::min<long long>(kFewCols / parts,
@@ -543,11 +548,11 @@ cudaError_t launch_linear_w4(const LinearW4Args& a, cudaStream_t s) {
   const int rows = (int)few_rows(a.w.in, a.w.group, a.x_dtype, by_group);
   for (int n0 = 0; n0 < a.N; n0 += rows) {
     const int n1 = std::min(a.N, n0 + rows);
-    const int cols = (n1 - n0) * parts, nt = cols <= 8 ? 1 : 2;
+    const int cols = (n1 - n0) * parts;
     const size_t smem = (size_t)(cols * col_bytes(a.w.in, a.w.group, by_group) + kFixedBytes);
-    const cudaError_t e = a.w.group == 128 ? launch_few<128>(a, n0, n1, nt, smem, s)
-                          : a.w.group == 64 ? launch_few<64>(a, n0, n1, nt, smem, s)
-                                            : launch_few<32>(a, n0, n1, nt, smem, s);
+    const cudaError_t e = a.w.group == 128 ? launch_few<128>(a, n0, n1, smem, s)
+                          : a.w.group == 64 ? launch_few<64>(a, n0, n1, smem, s)
+                                            : launch_few<32>(a, n0, n1, smem, s);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;

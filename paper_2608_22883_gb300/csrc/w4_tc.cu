@@ -53,6 +53,7 @@ struct Args {
   void* y; int y_dtype;
   long long ldy;
   int stages, ksteps, tiles, split;  // ring depth; stages of the contraction; tiles; CTAs a tile
+  uint32_t k128;                     // kW4One28
   unsigned long long wait_ns;
   int* err;
 };
@@ -343,6 +344,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     Turn st, ab;
     ab.i = team;                                           // units 2 i + team
     bool go = true, reused = false;
+    const uint32_t k128 = a.k128;
     for (int t = first; go && t < a.tiles; t += step) {
       const long long row = min((long long)t * kRows + r, (long long)a.w.out - 1);
       const uint8_t* zeros = a.w.zeros != nullptr ? a.w.zeros + row * a.groups : nullptr;
@@ -381,8 +383,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
             for (int j = 0; j < 4; ++j)
 #pragma unroll
               for (int p = 0; p < 4; ++p)
-                // 0x4300 | c is the bf16 number 128 + c
-                v[16 * q + 4 * j + p] = bf16_sub2(((ww[j] >> (4 * p)) & 0x000F000Fu) | 0x43004300u, zq);
+                v[16 * q + 4 * j + p] = bf16_sub2(w4_pair(ww[j] >> (4 * p), k128), zq);
           }
           tmem_st32(dst + (uint32_t)(ab.i * 64 + half * 32), v);
         }
@@ -709,6 +710,7 @@ cudaError_t launch_linear_w4_tc(const LinearW4Args& l, cudaStream_t s) {
     // one tile's contraction over a cluster while the tiles leave SMs idle
     a.split = 1;
     while (a.split < 8 && a.tiles * a.split * 2 <= 152 && a.split * 2 <= a.ksteps) a.split *= 2;
+    a.k128 = kW4One28;
     a.wait_ns = wait_limit_ns();
     a.err = x.err;
     const TmaOperand xop{x.out + (size_t)b * kMaxCols * p.k_pad, a.cols_pad, p.k_pad, p.k_pad};

@@ -518,7 +518,7 @@ def quantize_w4(W: torch.Tensor, group: int = 128, *, symmetric: bool = True,
     return {"codes": codes, "scales": scales, "zeros": zeros}
 
 
-W4_FEW = 5, 16384       # rows and columns up to which linear_w4 needs no workspace, whatever x's type
+W4_FEW = 2, 16384       # rows and columns up to which linear_w4 needs no workspace, whatever x's type
 
 
 def linear_w4_workspace_size(N: int, in_features: int, group: int = 128,

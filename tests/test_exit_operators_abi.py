@@ -85,7 +85,7 @@ def test_no_rows_is_no_work(L, call):
 def test_linear_workspace_sizes():
     import torch
     size = fovea.linear_w4_workspace_size
-    assert size(5, 4096, dtype=torch.float32) == 0 and size(16, 4096) == 0 and size(0, 4096) == 0
+    assert size(2, 16384, dtype=torch.float32) == 0 and size(8, 16384) == 0 and size(0, 4096) == 0
     assert size(17, 4096) >= 4096 + 17 * 4096 * 2
     assert size(6, 4096, dtype=torch.float32) >= 4096 + 18 * 4096 * 2
     assert size(17, 4096, dtype=torch.float8_e4m3fn, x_group=128) >= size(17, 4096) + 17 * 32 * 4
