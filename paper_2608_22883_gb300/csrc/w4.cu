@@ -2,11 +2,10 @@
 // their making (fovea_quantize_w4) and the product with a few rows
 // (fovea_linear_w4).
 //   w[o, k] = (code[o, k] - zero[o, k / group]) * scale[o, k / group]
-#include <cuda_fp8.h>
-
 #include <algorithm>
 
 #include "common.cuh"
+#include "w4_x.cuh"
 
 namespace fovea {
 
@@ -155,19 +154,6 @@ __device__ __forceinline__ void load_words(uint32_t* r, const uint8_t* p, uint32
 __device__ __forceinline__ void team_sync(int team, int split) {
   asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(split * 32) : "memory");
 }
-// v as the sum of three bf16 numbers: its truncations (an infinity or a NaN is the first alone).
-__device__ __forceinline__ void split3(float v, uint32_t& b0, uint32_t& b1, uint32_t& b2) {
-  const uint32_t bits = __float_as_uint(v);
-  if ((bits & 0x7F800000u) == 0x7F800000u) {
-    b0 = __bfloat16_as_ushort(__float2bfloat16_rn(v));
-    b1 = b2 = 0u;
-  } else {
-    b0 = bits >> 16;
-    const float r1 = v - __uint_as_float(b0 << 16);
-    b1 = __float_as_uint(r1) >> 16;
-    b2 = __float_as_uint(r1 - __uint_as_float(b1 << 16)) >> 16;
-  }
-}
 __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                             uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
@@ -194,37 +180,6 @@ __device__ __forceinline__ uint4 lds_x(uint32_t at) {
 struct Span {
   uint32_t w[2][4];
 };
-
-// Eight columns of a row of x, as the bf16 columns that add up to them, in the order
-// in which the codes of a word come out of it: 0 4 1 5 2 6 3 7.
-__device__ __forceinline__ void layout_x8(const void* x, long long at, int dtype, bool vec, uint4 (&out)[3]) {
-  out[1] = out[2] = make_uint4(0u, 0u, 0u, 0u);
-  if (dtype == FOVEA_BF16 && vec) {
-    const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + at);
-    out[0] = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632),
-                        __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-    return;
-  }
-  uint32_t pk[3][4] = {};
-  constexpr int order[8] = {0, 4, 1, 5, 2, 6, 3, 7};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    uint32_t b0 = 0, b1 = 0, b2 = 0;
-    if (dtype == FOVEA_BF16) {
-      b0 = static_cast<const uint16_t*>(x)[at + order[i]];
-    } else if (dtype == FOVEA_FP32) {
-      split3(static_cast<const float*>(x)[at + order[i]], b0, b1, b2);
-    } else {
-      const __half h = __half(__nv_cvt_fp8_to_halfraw(static_cast<const uint8_t*>(x)[at + order[i]], __NV_E4M3));
-      b0 = __bfloat16_as_ushort(__float2bfloat16_rn(__half2float(h)));
-    }
-    pk[0][i / 2] |= b0 << (16 * (i & 1));
-    pk[1][i / 2] |= b1 << (16 * (i & 1));
-    pk[2][i / 2] |= b2 << (16 * (i & 1));
-  }
-#pragma unroll
-  for (int p = 0; p < 3; ++p) out[p] = make_uint4(pk[p][0], pk[p][1], pk[p][2], pk[p][3]);
-}
 
 // The scales (bf16 pairs) and zero points (bytes) of four spans of a weight row.
 template <int G>
@@ -289,7 +244,7 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
                  uint32_t k128) {
   extern __shared__ __align__(16) uint8_t smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  const int parts = a.x_dtype == FOVEA_FP32 ? 3 : 1;
+  const int parts = x_parts(a.x_dtype);
   const int rows = n1 - n0, cols = rows * parts;
   const int spans = (a.w.in + kSpan - 1) / kSpan;
   const int groups = (a.w.in + G - 1) / G;
@@ -358,21 +313,32 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
     n_1.template load<ZEROS>(a.w, row_at(first, 1), q_lo * Quad<G>::kGroups, groups, scale_vec);
   }
   if (tid == 0) xs[-1] = make_uint4(0u, 0u, 0u, 0u);
-  for (int u = tid; u < spans * 16 * rows; u += kThreads) {
-    // neighbouring lanes take neighbouring rows, whose units lie side by side
-    const int unit = u / rows, n = u - unit * rows;
-    const int span = unit >> 4, k8 = unit & 15;
-    int j, q;                                  // word and quarter of these columns
-    if (G == 128) { q = k8 >> 2; j = k8 & 3; }
-    else if (G == 64) { j = 2 * (k8 >> 3) + (k8 & 1); q = (k8 & 7) >> 1; }
-    else { j = k8 >> 2; q = k8 & 3; }
-    uint4 v[3] = {};
-    if (unit * 8 < a.w.in) layout_x8(a.x, (long long)(n0 + n) * a.x_ld + unit * 8, a.x_dtype, x_vec, v);
-    uint4* dst = xs + ((span * 4 + j) * 4 + q) * cols + n * parts;
-    dst[0] = v[0];
-    if (parts == 3) {
-      dst[1] = v[1];
-      dst[2] = v[2];
+  // x, a few units a thread on their way together
+  constexpr int kBatch = 4;
+  for (int u0 = tid; u0 < spans * 16 * rows; u0 += kBatch * kThreads) {
+    X8 raw[kBatch] = {};
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int u = u0 + i * kThreads, n = u / (spans * 16), k0 = (u - n * (spans * 16)) * 8;
+      if (n < rows && k0 < a.w.in) raw[i].load(a.x, (long long)(n0 + n) * a.x_ld + k0, a.x_dtype, x_vec);
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int u = u0 + i * kThreads, n = u / (spans * 16), unit = u - n * (spans * 16);
+      if (n >= rows) continue;
+      const int span = unit >> 4, k8 = unit & 15;
+      int j, q;                                // word and quarter of these columns
+      if (G == 128) { q = k8 >> 2; j = k8 & 3; }
+      else if (G == 64) { j = 2 * (k8 >> 3) + (k8 & 1); q = (k8 & 7) >> 1; }
+      else { j = k8 >> 2; q = k8 & 3; }
+      uint4 v[3];
+      raw[i].columns(a.x_dtype, v);
+      uint4* dst = xs + ((span * 4 + j) * 4 + q) * cols + n * parts;
+      dst[0] = v[0];
+      if (parts == 3) {
+        dst[1] = v[1];
+        dst[2] = v[2];
+      }
     }
   }
   if (by_group)
@@ -480,7 +446,7 @@ cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, size_t smem, cudaS
   auto kern = linear_w4_kernel<G, ZEROS>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
   if (e != cudaSuccess) return e;
-  const bool x_vec = a.x_dtype == FOVEA_BF16 && (reinterpret_cast<uintptr_t>(a.x) & 15u) == 0 && a.x_ld % 8 == 0;
+  const bool x_vec = x_vectors(a.x, a.x_ld, a.x_dtype);
   const int groups = (a.w.in + G - 1) / G;
   const bool scale_vec = groups % Quad<G>::kGroups == 0 && (reinterpret_cast<uintptr_t>(a.w.scales) & 15u) == 0 &&
                          (reinterpret_cast<uintptr_t>(a.w.zeros) & 3u) == 0;
@@ -528,12 +494,12 @@ static long long col_bytes(int in, int group, bool by_group) {
 }
 constexpr long long kFixedBytes = 16 + kWarps * kTilePart * 4;
 static long long few_rows(int in, int group, int x_dtype, bool by_group) {    // of a launch
-  const int parts = x_dtype == FOVEA_FP32 ? 3 : 1;
+  const int parts = x_parts(x_dtype);
   return std::min<long long>(kFewCols / parts,
                              (kMaxSmem - kFixedBytes) / (col_bytes(in, group, by_group) * parts));
 }
 static bool is_few(int N, int in, int group, int x_dtype, bool by_group) {
-  return (long long)N * (x_dtype == FOVEA_FP32 ? 3 : 1) <= kFewCols && few_rows(in, group, x_dtype, by_group) > 0;
+  return (long long)N * x_parts(x_dtype) <= kFewCols && few_rows(in, group, x_dtype, by_group) > 0;
 }
 
 size_t linear_w4_workspace(int N, int in, int group, int x_dtype, bool by_group) {
@@ -544,7 +510,7 @@ size_t linear_w4_workspace(int N, int in, int group, int x_dtype, bool by_group)
 cudaError_t launch_linear_w4(const LinearW4Args& a, cudaStream_t s) {
   const bool by_group = a.x_group != 0;
   if (!is_few(a.N, a.w.in, a.w.group, a.x_dtype, by_group)) return launch_linear_w4_tc(a, s);
-  const int parts = a.x_dtype == FOVEA_FP32 ? 3 : 1;
+  const int parts = x_parts(a.x_dtype);
   const int rows = (int)few_rows(a.w.in, a.w.group, a.x_dtype, by_group);
   for (int n0 = 0; n0 < a.N; n0 += rows) {
     const int n1 = std::min(a.N, n0 + rows);

@@ -12,12 +12,11 @@
 // one lane of each of two warps issues the MMAs, each group's sum into an accumulator of its own;
 // eight warps read the accumulators, one weight row and half of the columns a
 // thread, and add them times their scales in fp32.
-#include <cuda_fp8.h>
-
 #include <algorithm>
 
 #include "common.cuh"
 #include "tc_ptx.cuh"
+#include "w4_x.cuh"
 
 namespace fovea {
 namespace w4tc {
@@ -548,7 +547,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
 // block's column, k padded to whole stages; every eight k in the order 0 4 1 5 2
 // 6 3 7; and its scales as [groups or 1, kMaxCols] per block.
 struct LayoutArgs {
-  const void* x; long long ld; int dtype;
+  const void* x; long long ld; int dtype; bool vec;
   const float* x_scale; int x_groups;      // 0: none; 1: one a row; else per group
   int N, in, k_pad;
   int rows_block, blocks, parts;
@@ -557,19 +556,6 @@ struct LayoutArgs {
   int* err;
 };
 constexpr int kLayoutThreads = 256;
-
-__device__ __forceinline__ void split3(float v, uint32_t& b0, uint32_t& b1, uint32_t& b2) {
-  const uint32_t bits = __float_as_uint(v);
-  if ((bits & 0x7F800000u) == 0x7F800000u) {               // infinity, NaN
-    b0 = __bfloat16_as_ushort(__float2bfloat16_rn(v));
-    b1 = b2 = 0u;
-  } else {                                                 // v is the sum of its three truncations
-    b0 = bits >> 16;
-    const float r1 = v - __uint_as_float(b0 << 16);
-    b1 = __float_as_uint(r1) >> 16;
-    b2 = __float_as_uint(r1 - __uint_as_float(b1 << 16)) >> 16;
-  }
-}
 
 __global__ void __launch_bounds__(kLayoutThreads) layout_x_kernel(const LayoutArgs a) {
   pdl_wait();
@@ -589,31 +575,14 @@ __global__ void __launch_bounds__(kLayoutThreads) layout_x_kernel(const LayoutAr
     }
     const int unit = (int)(it % units), slot = (int)(it / units % slots), b = (int)(it / ((long long)units * slots));
     const int n = b * a.rows_block + slot, k0 = unit * 8;
-    uint32_t pk[3][4] = {};
-    if (slot < a.rows_block && n < a.N && k0 < a.in) {
-      constexpr int order[8] = {0, 4, 1, 5, 2, 6, 3, 7};
-      const long long at = (long long)n * a.ld + k0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        uint32_t b0 = 0, b1 = 0, b2 = 0;
-        if (a.dtype == FOVEA_BF16) {
-          b0 = static_cast<const uint16_t*>(a.x)[at + order[i]];
-        } else if (a.dtype == FOVEA_FP32) {
-          split3(static_cast<const float*>(a.x)[at + order[i]], b0, b1, b2);
-        } else {
-          const __half h = __half(__nv_cvt_fp8_to_halfraw(static_cast<const uint8_t*>(a.x)[at + order[i]], __NV_E4M3));
-          b0 = __bfloat16_as_ushort(__float2bfloat16_rn(__half2float(h)));
-        }
-        pk[0][i / 2] |= b0 << (16 * (i & 1));
-        pk[1][i / 2] |= b1 << (16 * (i & 1));
-        pk[2][i / 2] |= b2 << (16 * (i & 1));
-      }
-    }
+    X8 raw = {};
+    if (slot < a.rows_block && n < a.N && k0 < a.in) raw.load(a.x, (long long)n * a.ld + k0, a.dtype, a.vec);
+    uint4 v[3];
+    raw.columns(a.dtype, v);
 #pragma unroll
     for (int p = 0; p < 3; ++p)
       if (p < a.parts)
-        *reinterpret_cast<uint4*>(a.out + ((long long)b * kMaxCols + slot * a.parts + p) * a.k_pad + k0) =
-            make_uint4(pk[p][0], pk[p][1], pk[p][2], pk[p][3]);
+        *reinterpret_cast<uint4*>(a.out + ((long long)b * kMaxCols + slot * a.parts + p) * a.k_pad + k0) = v[p];
   }
 }
 
@@ -623,7 +592,7 @@ struct Plan {
 };
 static Plan plan(int N, int in, int group, int x_dtype, bool by_group) {
   Plan p;
-  p.parts = x_dtype == FOVEA_FP32 ? 3 : 1;
+  p.parts = x_parts(x_dtype);
   p.rows_block = kMaxCols / p.parts;
   p.blocks = (N + p.rows_block - 1) / p.rows_block;
   p.k_pad = (in + kStageK - 1) / kStageK * kStageK;
@@ -678,7 +647,7 @@ cudaError_t launch_linear_w4_tc(const LinearW4Args& l, cudaStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(l.workspace);
   const int groups = (l.w.in + l.w.group - 1) / l.w.group;
   LayoutArgs x{};
-  x.x = l.x; x.ld = l.x_ld; x.dtype = l.x_dtype;
+  x.x = l.x; x.ld = l.x_ld; x.dtype = l.x_dtype; x.vec = x_vectors(l.x, l.x_ld, l.x_dtype);
   x.x_scale = l.x_scale; x.x_groups = l.x_scale == nullptr ? 0 : by_group ? groups : 1;
   x.N = l.N; x.in = l.w.in; x.k_pad = p.k_pad;
   x.rows_block = p.rows_block; x.blocks = p.blocks; x.parts = p.parts;
