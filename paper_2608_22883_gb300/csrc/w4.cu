@@ -16,9 +16,9 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-__device__ __forceinline__ float min_nan(float a, float b) {
-  float r;
-  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 
@@ -28,72 +28,161 @@ __device__ __forceinline__ float min_nan(float a, float b) {
 
 constexpr int kQuantThreads = 256;
 
-// Eight columns a thread, so that a group of 32, 64 or 128 columns is 4, 8 or
-// 16 neighbouring lanes; each row is laid out over a multiple of 16 lanes
-// (`slots`), so that no group crosses a warp.  Scale and code use IEEE
-// divisions: the codes are those of the definition, bit for bit.
+// bf16 of the IEEE quotient a / n (a >= 0, n a small integer).  a times the reciprocal is
+// off by less than four units of fp32's last place, which matters only that near a
+// midpoint of two bf16 numbers.
+static __device__ __noinline__ float quotient(float a, float b) { return __fdiv_rn(a, b); }
+__device__ __forceinline__ __nv_bfloat16 bf16_quotient(float a, float n) {
+  float v = a * (1.0f / n);
+  const uint32_t below = __float_as_uint(v) & 0xFFFFu;
+  if ((below > 0x7FF0u && below < 0x8010u) || !(v > 1e-30f)) v = quotient(a, n);
+  return __float2bfloat16_rn(v);
+}
+
+// rint(w / scale) of the quotient rounded to fp32; twice_rcp is 2 / scale to 2^-21.
+//
+// The nearest half-integer h / 2 is wrong by one place at most, and the remainder w - h
+// scale / 2 is exact (scale has 8 bits, h at most 6).  On a midpoint of two integers,
+// where bf16 weights often lie, the remainder is 0 and the sum below the midpoint
+// itself, which rounds to even; elsewhere the remainder's own quotient is so small that
+// its error of 2^-21 stays far below the rounding of the sum.
+__device__ __forceinline__ float rint_quotient(float w, float half_scale, float twice_rcp) {
+  constexpr float kMagic = 12582912.0f;                  // 1.5 * 2^23: a sum with it is an integer
+  const float h = fmaf(w, twice_rcp, kMagic) - kMagic;
+  const float r = fmaf(-h, half_scale, w);
+  return fmaf(fmaf(r, twice_rcp, h), 0.5f, kMagic) - kMagic;
+}
+
+// A warp takes strips of 256 columns of a row, eight columns a lane, so that a group
+// of G columns is G / 8 neighbouring lanes; U strips are on their way together.  Scale
+// and code are those of IEEE divisions, bit for bit.
 template <class T, bool VEC>
-__global__ void __launch_bounds__(kQuantThreads)
-quantize_w4_kernel(const T* __restrict__ W, long long ld, int in, int slots, long long total, int group,
-                   bool symmetric, uint8_t* __restrict__ codes, __nv_bfloat16* __restrict__ scales,
-                   uint8_t* __restrict__ zeros) {
+struct QuantShape {                                      // strips on their way; CTAs an SM
+  static constexpr int U = VEC && sizeof(T) == 4 ? 2 : 1, kCtas = U == 2 ? 4 : 6;
+};
+template <class T, int G, bool VEC, bool SYMMETRIC>
+__global__ void __launch_bounds__(kQuantThreads, (QuantShape<T, VEC>::kCtas))
+quantize_w4_kernel(const T* __restrict__ W, long long ld, int out, int in, uint8_t* __restrict__ codes,
+                   __nv_bfloat16* __restrict__ scales, uint8_t* __restrict__ zeros) {
+  constexpr int U = QuantShape<T, VEC>::U;
+  constexpr int kVecs = sizeof(T) / 2;                   // 16-byte vectors of eight columns
+  constexpr int kStrip = 256;
+  const int lane = threadIdx.x & 31;
+  const int groups = (in + G - 1) / G, strips = (in + kStrip - 1) / kStrip;
+  const int warps = (int)gridDim.x * (kQuantThreads / 32);
+  const int first = (int)blockIdx.x * (kQuantThreads / 32) + (int)(threadIdx.x >> 5);
+  // the warp's next strip: row, first column, where this lane's weights, codes and
+  // scale lie; and the steps to the one after it, without and with a carry to the next row
+  const int row0 = first / strips, row_step = warps / strips;
+  const int col_step = (warps - row_step * strips) * kStrip;
+  int row = row0, col = (first - row0 * strips) * kStrip + lane * 8;
+  const T* src = W + (long long)row * ld + col;
+  long long code_at = (long long)row * in + col, scale_at = (long long)row * groups + col / G;
+  const long long src_step = (long long)row_step * ld + col_step, src_carry = ld - strips * kStrip;
+  const long long code_step = (long long)row_step * in + col_step, code_carry = in - strips * kStrip;
+  const long long scale_step = (long long)row_step * groups + col_step / G, scale_carry = groups - strips * (kStrip / G);
   pdl_wait();
   pdl_trigger();
-  const int groups = (in + group - 1) / group;
-  const long long step = (long long)gridDim.x * kQuantThreads;
-  // every lane of a warp takes the same number of turns: total is a multiple of 16
-  // and the tail's lanes run with nothing in hand
-  for (long long base = (long long)blockIdx.x * kQuantThreads; base < total; base += step) {
-    const long long i = base + threadIdx.x;
-    const long long row = i / slots;
-    const int c0 = (int)(i - row * slots) * 8;
-    const bool live = i < total && c0 < in;
-    float w[8];
-    if (live) {
-      const T* p = W + row * ld + c0;
-      if (VEC) {
-        uint4 raw[sizeof(T) / 2];
+  while (row < out) {
+    uint4 raw[U][kVecs];
+    long long code_of[U], scale_of[U];
+    bool live[U];
 #pragma unroll
-        for (int h = 0; h < (int)(sizeof(T) / 2); ++h) raw[h] = reinterpret_cast<const uint4*>(p)[h];
-        const T* e = reinterpret_cast<const T*>(raw);
+    for (int u = 0; u < U; ++u) {
+      live[u] = row < out && col < in;
+      code_of[u] = code_at;
+      scale_of[u] = scale_at;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = to_f32(e[j]);
-      } else {
+      for (int h = 0; h < kVecs; ++h) raw[u][h] = make_uint4(0u, 0u, 0u, 0u);
+      if (live[u]) {
+        if (VEC) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = to_f32(p[j]);
+          for (int h = 0; h < kVecs; ++h) raw[u][h] = __ldg(reinterpret_cast<const uint4*>(src) + h);
+        } else {
+          T* e = reinterpret_cast<T*>(raw[u]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) e[j] = src[j];
+        }
       }
-    } else {
+      row += row_step;
+      col += col_step;
+      src += src_step;
+      code_at += code_step;
+      scale_at += scale_step;
+      if (col >= strips * kStrip) {
+        ++row;
+        col -= strips * kStrip;
+        src += src_carry;
+        code_at += code_carry;
+        scale_at += scale_carry;
+      }
+    }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = 0.0f;
-    }
-    float hi = 0.0f, lo = 0.0f;
+    for (int u = 0; u < U; ++u) {
+      float w[8];
+      const T* e = reinterpret_cast<const T*>(raw[u]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      hi = max_nan(hi, symmetric ? fabsf(w[j]) : w[j]);
-      lo = symmetric ? 0.0f : min_nan(lo, w[j]);
-    }
-    for (int o = group / 16; o > 0; o >>= 1) {
-      hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-      lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    }
-    const __nv_bfloat16 stored = __float2bfloat16_rn(symmetric ? __fdiv_rn(hi, 7.0f) : __fdiv_rn(hi - lo, 15.0f));
-    const float scale = __bfloat162float(stored);
-    const bool some = scale > 0.0f;
-    float zero = 8.0f;
-    if (!symmetric && some) zero = fminf(fmaxf(rintf(__fdiv_rn(-lo, scale)), 0.0f), 15.0f);
-    uint32_t word = 0;
+      for (int j = 0; j < 8; ++j) w[j] = to_f32(e[j]);
+      float hi = 0.0f, lo = 0.0f;
+      if (SYMMETRIC && sizeof(T) == 2) {
+        // two at a time, a NaN the largest
+        const uint32_t v[4] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w};
+        uint32_t m = v[0] & 0x7FFF7FFFu;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float q = some ? rintf(__fdiv_rn(w[j], scale)) : 0.0f;
-      const float code = fminf(fmaxf(q, -zero), 15.0f - zero) + zero;
-      word |= (uint32_t)code << (4 * j);
-    }
-    if (live) {
-      *reinterpret_cast<uint32_t*>(codes + (row * in + c0) / 2) = word;
-      if (c0 % group == 0) {
-        const long long at = row * groups + c0 / group;
-        scales[at] = stored;
-        if (zeros != nullptr) zeros[at] = (uint8_t)zero;
+        for (int j = 1; j < 4; ++j) m = max_nan_bf16x2(m, v[j] & 0x7FFF7FFFu);
+        hi = max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+      } else {
+        float odd = 0.0f;                                // w 0: NaN for a NaN, which fmaxf drops (and for an infinity)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          hi = fmaxf(hi, SYMMETRIC ? fabsf(w[j]) : w[j]);
+          if (!SYMMETRIC) lo = fminf(lo, w[j]);
+          odd = fmaf(w[j], 0.0f, odd);
+        }
+        if (odd != 0.0f) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (w[j] != w[j]) hi = w[j];
+        }
+      }
+#pragma unroll
+      for (int o = G / 16; o > 0; o >>= 1) {
+        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        if (!SYMMETRIC) lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      }
+      const __nv_bfloat16 stored = SYMMETRIC ? bf16_quotient(hi, 7.0f) : bf16_quotient(hi - lo, 15.0f);
+      const float scale = __bfloat162float(stored);
+      const bool some = scale > 0.0f;                    // not 0, not NaN
+      float zero = 8.0f;
+      float q[8];
+      if (scale > 1e-30f && scale < 1e30f) {
+        const float half_scale = 0.5f * scale, twice_rcp = __fdividef(2.0f, scale);
+        if (!SYMMETRIC) zero = fminf(fmaxf(rint_quotient(-lo, half_scale, twice_rcp), 0.0f), 15.0f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          q[j] = rint_quotient(w[j], half_scale, twice_rcp);
+          // symmetric: max |w| / scale < 7.03, so no code leaves [-7, 7]
+          if (!SYMMETRIC) q[j] = fminf(fmaxf(q[j], -zero), 15.0f - zero);
+        }
+      } else {                                           // 0, NaN, or no remainder to rely on
+        if (!SYMMETRIC && some) zero = fminf(fmaxf(rintf(quotient(-lo, scale)), 0.0f), 15.0f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          q[j] = fminf(fmaxf(some ? rintf(quotient(w[j], scale)) : 0.0f, -zero), 15.0f - zero);
+      }
+      // four codes are one integer below 2^16, which the low bits of its sum with 2^23 hold
+      const float base = fmaf(zero, 4369.0f, 8388608.0f);
+      uint32_t half[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        half[h] = __float_as_uint(fmaf(fmaf(fmaf(q[4 * h + 3], 16.0f, q[4 * h + 2]), 16.0f, q[4 * h + 1]), 16.0f,
+                                       q[4 * h]) + base);
+      if (live[u]) {
+        *reinterpret_cast<uint32_t*>(codes + code_of[u] / 2) = __byte_perm(half[0], half[1], 0x5410);
+        if ((lane & (G / 8 - 1)) == 0) {
+          scales[scale_of[u]] = stored;
+          if (!SYMMETRIC) zeros[scale_of[u]] = (uint8_t)zero;
+        }
       }
     }
   }
@@ -107,7 +196,7 @@ constexpr int kMaxSmem = 227 * 1024;
 constexpr int kWarps = 16, kThreads = 32 * kWarps;
 constexpr int kSpan = 128;             // columns a warp handles together
 constexpr int kTileRows = 16;          // weight rows of a tile
-constexpr int kQuad = 4;               // spans of codes a warp has on their way
+constexpr int kQuad = 2;               // spans of codes a warp has on their way
 // Columns of x (an fp32 row counts three times) that a tile takes: the tensor-core
 // instruction's eight.  More go through tensor memory (w4_tc.cu): with two such
 // instructions a word 16 rows by 4096 x 32000 took 44.8 us here against 27.3 there, 8
@@ -181,17 +270,19 @@ struct Span {
   uint32_t w[2][4];
 };
 
-// The scales (bf16 pairs) and zero points (bytes) of four spans of a weight row.
+// The scales (bf16 pairs) and zero points (bytes) of kQuad spans of a weight row.
 template <int G>
 struct Quad {
-  static constexpr int kGroups = kQuad * kSpan / G;      // 4, 8 or 16
-  uint32_t s[kGroups / 2], z[kGroups / 4];
+  static constexpr int kGroups = kQuad * kSpan / G;
+  uint32_t s[kGroups / 2], z[(kGroups + 3) / 4];
   // `vec`: every row's scales and zeros start at a multiple of kGroups, aligned
   template <bool ZEROS>
   __device__ __forceinline__ void load(const W4& w, long long row_at, int g0, int groups, bool vec) {
     if (vec) {
       const __nv_bfloat16* p = w.scales + row_at + g0;
-      if (kGroups == 4) {
+      if (kGroups == 2) {
+        s[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
+      } else if (kGroups == 4) {
         const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
         s[0] = v.x; s[1] = v.y;
       } else {
@@ -201,7 +292,9 @@ struct Quad {
           s[4 * i] = v.x; s[4 * i + 1] = v.y; s[4 * i + 2] = v.z; s[4 * i + 3] = v.w;
         }
       }
-      if (ZEROS) {
+      if (ZEROS && kGroups == 2) {
+        z[0] = __ldg(reinterpret_cast<const uint16_t*>(w.zeros + row_at + g0));
+      } else if (ZEROS) {
 #pragma unroll
         for (int i = 0; i < kGroups / 4; ++i)
           z[i] = __ldg(reinterpret_cast<const uint32_t*>(w.zeros + row_at + g0) + i);
@@ -228,11 +321,11 @@ struct Quad {
 
 // y of up to kFewCols columns (rows of x, an fp32 row as three) in one launch.
 //
-// `split` warps take a tile of 16 weight rows, each a range of its quads (four spans of
+// `split` warps take a tile of 16 weight rows, each a range of its quads (kQuad spans of
 // 128 columns); a warp goes from tile to tile by itself, x in shared memory.  It
 // turns the codes into bf16 integers c - z (exact) and multiplies them on the tensor
 // cores, weights as the 16-row operand; a group's fp32 sum is then taken times its
-// scale.  The codes of the next four spans are on their way in registers
+// scale.  The codes of the next kQuad spans are on their way in registers
 // meanwhile, across tiles, and so are the next quad's scales.  Only the warps of a
 // split tile meet, in shared memory, in a fixed order.
 //
@@ -467,25 +560,32 @@ cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, size_t smem, cudaS
 
 }  // namespace
 
+template <class T, int G, bool VEC>
+static cudaError_t quantize(const T* W, long long ld, int out, int in, uint8_t* codes, __nv_bfloat16* scales,
+                            uint8_t* zeros, cudaStream_t s) {
+  const long long strips = (long long)out * ((in + 255) / 256);
+  const long long ctas = (strips + kQuantThreads / 32 - 1) / (kQuantThreads / 32);
+  const int grid = (int)std::min<long long>(ctas, 152 * QuantShape<T, VEC>::kCtas);
+  return launch_pdl(zeros == nullptr ? quantize_w4_kernel<T, G, VEC, true> : quantize_w4_kernel<T, G, VEC, false>,
+                    dim3(grid), dim3(kQuantThreads), 0, s, W, ld, out, in, codes, scales, zeros);
+}
+template <class T>
+static cudaError_t quantize(const void* W, long long ld, int out, int in, int group, uint8_t* codes,
+                            __nv_bfloat16* scales, uint8_t* zeros, cudaStream_t s) {
+  const T* w = static_cast<const T*>(W);
+  if ((reinterpret_cast<uintptr_t>(W) & 15u) == 0 && ld * sizeof(T) % 16 == 0)
+    return group == 128 ? quantize<T, 128, true>(w, ld, out, in, codes, scales, zeros, s)
+           : group == 64 ? quantize<T, 64, true>(w, ld, out, in, codes, scales, zeros, s)
+                         : quantize<T, 32, true>(w, ld, out, in, codes, scales, zeros, s);
+  return group == 128 ? quantize<T, 128, false>(w, ld, out, in, codes, scales, zeros, s)
+         : group == 64 ? quantize<T, 64, false>(w, ld, out, in, codes, scales, zeros, s)
+                       : quantize<T, 32, false>(w, ld, out, in, codes, scales, zeros, s);
+}
+
 cudaError_t launch_quantize_w4(int dtype, const void* W, long long ld, int out, int in, int group,
                                uint8_t* codes, __nv_bfloat16* scales, uint8_t* zeros, cudaStream_t s) {
-  const int slots = (in / 8 + 15) / 16 * 16;
-  const long long total = (long long)slots * out;
-  const long long blocks = (total + kQuantThreads - 1) / kQuantThreads;
-  const int grid = (int)(blocks < 152 * 8 ? blocks : 152 * 8);
-  const bool symmetric = zeros == nullptr;
-  const size_t size = dtype == FOVEA_BF16 ? 2 : 4;
-  const bool vec = (reinterpret_cast<uintptr_t>(W) & 15u) == 0 && ld * size % 16 == 0;
-  auto go = [&](auto kern, auto* w) {
-    return launch_pdl(kern, dim3(grid), dim3(kQuantThreads), 0, s, w, ld, in, slots, total, group, symmetric,
-                      codes, scales, zeros);
-  };
-  if (dtype == FOVEA_BF16) {
-    const __nv_bfloat16* w = static_cast<const __nv_bfloat16*>(W);
-    return vec ? go(quantize_w4_kernel<__nv_bfloat16, true>, w) : go(quantize_w4_kernel<__nv_bfloat16, false>, w);
-  }
-  const float* w = static_cast<const float*>(W);
-  return vec ? go(quantize_w4_kernel<float, true>, w) : go(quantize_w4_kernel<float, false>, w);
+  return dtype == FOVEA_BF16 ? quantize<__nv_bfloat16>(W, ld, out, in, group, codes, scales, zeros, s)
+                             : quantize<float>(W, ld, out, in, group, codes, scales, zeros, s);
 }
 
 // Shared memory of the few-column product: of a column, and whatever their number.
