@@ -68,29 +68,32 @@ struct Row {
   }
   __device__ __forceinline__ int first(int c) const { return c * NV - shift; }
   __device__ __forceinline__ bool whole(int c) const { return first(c) >= 0 && first(c) + NV <= V; }
-  __device__ __forceinline__ uint32_t bits(int i0) const {       // of the tokens i0 .. i0 + NV - 1
-    uint32_t m = 0;
+  // The first and last chunk of the row that are whole.
+  __device__ __forceinline__ int whole_lo() const { return shift != 0 ? 1 : 0; }
+  __device__ __forceinline__ int whole_hi() const { return (V + shift) / NV; }
+  // Bits of the tokens of a chunk (those outside the row: any).
+  __device__ __forceinline__ uint32_t bits(int c) const {
+    const int i0 = first(c), last = (V - 1) >> 5;
+    const uint32_t lo = allowed[max(i0, 0) >> 5], hi = allowed[min((i0 + NV - 1) >> 5, last)];
+    return i0 < 0 ? lo << -i0 : __funnelshift_r(lo, hi, i0 & 31);
+  }
+  __device__ __forceinline__ uint4 raw(int c) const {            // of a whole chunk
+    return *reinterpret_cast<const uint4*>(p + first(c));        // (which the gradient may overwrite)
+  }
+  __device__ __forceinline__ void mask(uint32_t m, float (&v)[NV]) const {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int k = i0 + i;
-      if (k >= 0 && k < V) m |= ((allowed[k >> 5] >> (k & 31)) & 1u) << i;
-    }
-    return m;
+    for (int i = 0; i < NV; ++i)
+      if (!(m >> i & 1u)) v[i] = -INFINITY;
   }
   __device__ __forceinline__ void load(int c, float (&v)[NV]) const {
     const int i0 = first(c);
     if (whole(c)) {
-      ln_load<T>(p + i0, v);
+      ln_unpack<T>(raw(c), v);
     } else {
 #pragma unroll
       for (int i = 0; i < NV; ++i) v[i] = i0 + i >= 0 && i0 + i < V ? to_f32(p[i0 + i]) : -INFINITY;
     }
-    if (allowed != nullptr) {
-      const uint32_t m = bits(i0);
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (!(m >> i & 1u)) v[i] = -INFINITY;
-    }
+    if (allowed != nullptr) mask(bits(c), v);
   }
   // One token's logit: -inf where it is not allowed.
   __device__ __forceinline__ float at(int k) const {
@@ -123,6 +126,72 @@ __device__ __forceinline__ void join(Sums& a, Sums b) {
   a.W += b.W;
 }
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  return (uint64_t)__float_as_uint(hi) << 32 | __float_as_uint(lo);
+}
+__device__ __forceinline__ float lo2(uint64_t v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float hi2(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// A thread's sums over the tokens it has seen (even and odd ones apart), and the
+// largest logit with its chunk.
+struct Seen {
+  float m = -INFINITY;
+  uint64_t S = 0, W = 0;
+  float top = -INFINITY;
+  int chunk = 0;
+
+  __device__ __forceinline__ Sums sums() const { return Sums{m, lo2(S) + hi2(S), lo2(W) + hi2(W)}; }
+  // One chunk's logits; a NaN among them makes the sums NaN.
+  template <int NV>
+  __device__ __forceinline__ void take(const float (&v)[NV], int c, float scale) {
+    float cm = v[0];
+#pragma unroll
+    for (int i = 1; i < NV; ++i) cm = max_nan(cm, v[i]);
+    const float zm = cm * scale;
+    if (zm == -INFINITY) return;
+    if (cm > top) {
+      top = cm;
+      chunk = c;
+    }
+    if (!(zm <= m + 2.0f)) {
+      Sums a = {m, lo2(S), lo2(W)}, b = {m, hi2(S), hi2(W)};
+      rebase(a, zm);
+      rebase(b, zm);
+      m = zm;
+      S = pack2(a.S, b.S);
+      W = pack2(a.W, b.W);
+    }
+    const uint64_t scale2 = pack2(scale, scale), m2 = pack2(-m, -m), log2e2 = pack2(kLog2e, kLog2e);
+#pragma unroll
+    for (int i = 0; i < NV; i += 2) {
+      // (rounded product) - m, not one fused operation: the largest z gives 0 exactly
+      const uint64_t d = add2(mul2(pack2(v[i], v[i + 1]), scale2), m2);
+      // -inf: e^{-200} is 0 and so is its term of W
+      const uint64_t dz = pack2(max_nan(lo2(d), -200.0f), max_nan(hi2(d), -200.0f));
+      const uint64_t x = mul2(dz, log2e2);
+      const uint64_t e = pack2(ex2(lo2(x)), ex2(hi2(x)));
+      S = add2(S, e);
+      W = fma2(e, dz, W);
+    }
+  }
+};
+
 struct Shared {
   float m[kWarps], S[kWarps], W[kWarps];
   unsigned long long upper[kGroups];   // no key of the group is above it
@@ -142,7 +211,7 @@ struct Shared {
 // largest logit.  The k-th largest of the groups' bounds is a threshold that at
 // least k tokens reach, so only groups that reach it (k of them, and ties) are
 // read again, from L2, for the tokens above it: a few more than k.
-template <class T>
+template <class T, bool MASKED>
 __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArgs a) {
   constexpr int NV = Row<T>::NV;
   __shared__ Shared sh;
@@ -156,33 +225,48 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArg
   const int per = (row.chunks + ctas - 1) / ctas;
   const int c_lo = min(rank * per, row.chunks), c_hi = min(c_lo + per, row.chunks);
 
-  Sums s = {-INFINITY, 0.0f, 0.0f};
-  int32_t top = kOrderNegInf;
-  int top_chunk = 0;
-  for (int c = c_lo + tid; c < c_hi; c += kThreads) {
-    float v[NV];
-    row.load(c, v);
-    float cm = v[0];
+  // whole chunks lo + tid, + kThreads, ... of this CTA; and the row's ragged ends, the
+  // first one thread 0's, the last one thread 1's
+  const int lo = max(c_lo, row.whole_lo()), hi = min(c_hi, row.whole_hi());
+  auto ragged = [&](int i) {                               // chunk of end i, or -1
+    const int e = i == 0 ? 0 : row.chunks - 1;
+    return e >= c_lo && e < c_hi && !row.whole(e) && (i == 0 || e != 0) ? e : -1;
+  };
+  Seen seen;
+  {
+    constexpr int U = 4;                                   // chunks on their way together
+    int c = lo + tid;
+    for (; c + (U - 1) * kThreads < hi; c += U * kThreads) {
+      uint4 raw[U];
+      uint32_t keep[U];
 #pragma unroll
-    for (int i = 1; i < NV; ++i) cm = max_nan(cm, v[i]);
-    const float zm = cm * scale;
-    if (zm == -INFINITY) continue;
-    const int32_t o = order_of(cm);
-    if (o > top) {
-      top = o;
-      top_chunk = c;
+      for (int u = 0; u < U; ++u) {
+        raw[u] = row.raw(c + u * kThreads);
+        if (MASKED) keep[u] = row.bits(c + u * kThreads);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float v[NV];
+        ln_unpack<T>(raw[u], v);
+        if (MASKED) row.mask(keep[u], v);
+        seen.take(v, c + u * kThreads, scale);
+      }
     }
-    if (!(zm <= s.m + 2.0f)) rebase(s, zm);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      // -inf: e^{-200} is 0 and so is its term of W
-      const float dz = max_nan(v[i] * scale - s.m, -200.0f);
-      const float e = ex2(dz * kLog2e);
-      s.S += e;
-      s.W = fmaf(e, dz, s.W);
+    for (; c < hi; c += kThreads) {
+      float v[NV];
+      row.load(c, v);
+      seen.take(v, c, scale);
+    }
+    if (tid < 2 && ragged(tid) >= 0) {
+      float v[NV];
+      row.load(ragged(tid), v);
+      seen.take(v, ragged(tid), scale);
     }
   }
-  if (top != kOrderNegInf) rebase(s, value_of(top) * scale);   // the largest z itself
+  Sums s = seen.sums();
+  int32_t top = order_of(seen.top);
+  const int top_chunk = seen.chunk;
+  if (top != kOrderNegInf) rebase(s, seen.top * scale);   // the largest z itself
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     Sums b;
@@ -232,29 +316,36 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArg
     }
     if (tid < a.k) sh.best[tid] = 0ull;
     __syncthreads();
-    const unsigned long long threshold = sh.threshold;
-    const int turns = (c_hi - c_lo + kThreads - 1) / kThreads;
-    for (int gr = warp; gr < kGroups; gr += kWarps) {
-      if (sh.upper[gr] < threshold) continue;
-      for (int it = lane >> 2; it < turns; it += 8) {
-        const int c = c_lo + it * kThreads + gr * 4 + (lane & 3);
-        if (c >= c_hi) break;
+    // a NaN (or +inf) is in no bound: then every token is looked at
+    const bool odd = sh.total.S != sh.total.S;
+    const unsigned long long threshold = odd ? 1ull : sh.threshold;
+    auto each_key = [&](int gr, auto&& f) {                // of a group's tokens, by a warp
+      for (int c = lo + gr * 4 + (lane >> 2) * kThreads + (lane & 3); c < hi; c += 8 * kThreads) {
         float v[NV];
         row.load(c, v);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          if (v[i] * scale == -INFINITY) continue;
-          const unsigned long long key = key_of(order_of(v[i]), row.first(c) + i);
-          if (key >= threshold) {
-            const int at = atomicAdd(&sh.count, 1);
-            if (at < kCands) sh.cand[at] = key;
-          }
-        }
+        for (int i = 0; i < NV; ++i)
+          if (v[i] * scale != -INFINITY) f(key_of(order_of(v[i]), row.first(c) + i));
       }
-    }
+      if (gr == 0 && lane < 2 && ragged(lane) >= 0) {
+        float v[NV];
+        row.load(ragged(lane), v);
+        for (int i = 0; i < NV; ++i)
+          if (v[i] * scale != -INFINITY) f(key_of(order_of(v[i]), row.first(ragged(lane)) + i));
+      }
+    };
+    if (!odd)
+      for (int gr = warp; gr < kGroups; gr += kWarps) {
+        if (sh.upper[gr] < threshold) continue;
+        each_key(gr, [&](unsigned long long key) {
+          if (key < threshold) return;
+          const int at = atomicAdd(&sh.count, 1);
+          if (at < kCands) sh.cand[at] = key;
+        });
+      }
     __syncthreads();
     const int count = sh.count;
-    if (count <= kCands) {
+    if (!odd && count <= kCands) {
       for (int i = tid; i < count; i += kThreads) {
         const unsigned long long mine = sh.cand[i];
         int above = 0;
@@ -268,19 +359,10 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArg
       for (int r = 0; r < a.k; ++r) {
         unsigned long long mine = 0ull;
         for (int gr = warp; gr < kGroups; gr += kWarps) {
-          if (sh.upper[gr] < threshold) continue;
-          for (int it = lane >> 2; it < turns; it += 8) {
-            const int c = c_lo + it * kThreads + gr * 4 + (lane & 3);
-            if (c >= c_hi) break;
-            float v[NV];
-            row.load(c, v);
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-              if (v[i] * scale == -INFINITY) continue;
-              const unsigned long long key = key_of(order_of(v[i]), row.first(c) + i);
-              if (key < last && key > mine) mine = key;
-            }
-          }
+          if (!odd && sh.upper[gr] < threshold) continue;
+          each_key(gr, [&](unsigned long long key) {
+            if (key < last && key > mine) mine = key;
+          });
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
@@ -360,7 +442,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArg
 // The gradient of one row's range of chunks.  Every token's term is p (A - g_H
 // logp) with A of the row; the few tokens with a gradient of their own are
 // written again after it, by the CTA whose range they lie in.
-template <class T>
+template <class T, bool MASKED>
 __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const ScoreGradArgs a) {
   constexpr int NV = Row<T>::NV;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -407,24 +489,69 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
 
   const int per = (row.chunks + gridDim.x - 1) / gridDim.x;
   const int c_lo = min((int)blockIdx.x * per, row.chunks), c_hi = min(c_lo + per, row.chunks);
-  for (int c = c_lo + tid; c < c_hi; c += kThreads) {
-    float v[NV];
-    row.load(c, v);
+  auto gradient = [&](float (&v)[NV]) {
+    const uint64_t scale2 = pack2(scale, scale), m2 = pack2(-m, -m), s2 = pack2(-log_sum, -log_sum),
+                   log2e2 = pack2(kLog2e, kLog2e), gH2 = pack2(-gH, -gH), A2 = pack2(A, A);
+#pragma unroll
+    for (int i = 0; i < NV; i += 2) {
+      const uint64_t d = add2(add2(mul2(pack2(v[i], v[i + 1]), scale2), m2), s2);
+      // -inf: p is 0, and so is p logp
+      const uint64_t lp = pack2(max_nan(lo2(d), -1e4f), max_nan(hi2(d), -1e4f));
+      const uint64_t x = mul2(lp, log2e2);
+      const uint64_t g = mul2(mul2(pack2(ex2(lo2(x)), ex2(hi2(x))), fma2(gH2, lp, A2)), scale2);
+      v[i] = lo2(g);
+      v[i + 1] = hi2(g);
+    }
+  };
+  auto store = [&](int c, const float (&v)[NV]) {          // one value at a time
     const int i0 = row.first(c);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const float lp = max_nan((v[i] * scale - m) - log_sum, -1e4f);      // -inf: p is 0, and so is p logp
-      v[i] = ex2(lp * kLog2e) * fmaf(-gH, lp, A) * scale;
-    }
-    if (out_vec && row.whole(c)) {
+    for (int i = 0; i < NV; ++i)
+      if (i0 + i >= 0 && i0 + i < a.V) out[i0 + i] = from_f32<T>(v[i]);
+  };
+  auto store_whole = [&](int c, const float (&v)[NV]) {
+    if (out_vec) {
       __align__(16) T e[NV];
 #pragma unroll
       for (int i = 0; i < NV; ++i) e[i] = from_f32<T>(v[i]);
-      *reinterpret_cast<uint4*>(out + i0) = *reinterpret_cast<const uint4*>(e);
+      *reinterpret_cast<uint4*>(out + row.first(c)) = *reinterpret_cast<const uint4*>(e);
     } else {
+      store(c, v);
+    }
+  };
+  {
+    constexpr int U = 4;                                   // chunks on their way together
+    const int lo = max(c_lo, row.whole_lo()), hi = min(c_hi, row.whole_hi());
+    int c = lo + tid;
+    for (; c + (U - 1) * kThreads < hi; c += U * kThreads) {
+      uint4 raw[U];
+      uint32_t keep[U];
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (i0 + i >= 0 && i0 + i < a.V) out[i0 + i] = from_f32<T>(v[i]);
+      for (int u = 0; u < U; ++u) {
+        raw[u] = row.raw(c + u * kThreads);
+        if (MASKED) keep[u] = row.bits(c + u * kThreads);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float v[NV];
+        ln_unpack<T>(raw[u], v);
+        if (MASKED) row.mask(keep[u], v);
+        gradient(v);
+        store_whole(c + u * kThreads, v);
+      }
+    }
+    for (; c < hi; c += kThreads) {
+      float v[NV];
+      row.load(c, v);
+      gradient(v);
+      store_whole(c, v);
+    }
+    const int e = tid == 0 ? 0 : row.chunks - 1;           // the ragged ends
+    if (tid < 2 && e >= c_lo && e < c_hi && !row.whole(e) && (tid == 0 || e != 0)) {
+      float v[NV];
+      row.load(e, v);
+      gradient(v);
+      store(e, v);
     }
   }
   __syncthreads();
@@ -489,9 +616,13 @@ cudaError_t launch_token_logprobs(int dtype, const ScoreArgs& all, cudaStream_t 
     a.entropy += n0;
     const int split = row_split(a.N, a.V, size);
     const dim3 grid(split, (unsigned)a.N);
-    const cudaError_t e = dtype == FOVEA_BF16
-                              ? launch_cluster(token_logprobs_kernel<__nv_bfloat16>, grid, split, s, a)
-                              : launch_cluster(token_logprobs_kernel<float>, grid, split, s, a);
+    const bool masked = a.allowed != nullptr;
+    const cudaError_t e =
+        dtype == FOVEA_BF16
+            ? launch_cluster(masked ? token_logprobs_kernel<__nv_bfloat16, true> : token_logprobs_kernel<__nv_bfloat16, false>,
+                             grid, split, s, a)
+            : launch_cluster(masked ? token_logprobs_kernel<float, true> : token_logprobs_kernel<float, false>, grid,
+                             split, s, a);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -517,9 +648,13 @@ cudaError_t launch_token_logprobs_grad(int dtype, const ScoreGradArgs& all, cuda
     const int split = a.dlogits == a.logits ? 1 : row_split(a.N, a.V, size);
     const dim3 grid(split, (unsigned)a.N);
     const size_t smem = (size_t)(a.T + a.k) * 12;
-    const cudaError_t e = dtype == FOVEA_BF16
-                              ? launch_pdl(token_logprobs_grad_kernel<__nv_bfloat16>, grid, dim3(kThreads), smem, s, a)
-                              : launch_pdl(token_logprobs_grad_kernel<float>, grid, dim3(kThreads), smem, s, a);
+    const bool masked = a.allowed != nullptr;
+    const cudaError_t e =
+        dtype == FOVEA_BF16
+            ? launch_pdl(masked ? token_logprobs_grad_kernel<__nv_bfloat16, true> : token_logprobs_grad_kernel<__nv_bfloat16, false>,
+                         grid, dim3(kThreads), smem, s, a)
+            : launch_pdl(masked ? token_logprobs_grad_kernel<float, true> : token_logprobs_grad_kernel<float, false>,
+                         grid, dim3(kThreads), smem, s, a);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
