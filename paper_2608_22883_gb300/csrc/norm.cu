@@ -22,27 +22,29 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
-// Columns [c0, c0 + 8) of a row; columns from d on read as 0.
-template <class T, bool VEC>
-__device__ __forceinline__ void load_chunk(const T* p, int c0, int d, float (&v)[kChunk]) {
-  if (VEC) {
-    if (c0 < d) {
+// Columns [c0, c0 + 8) of a row as they lie in memory; columns from d on are 0.
+template <class T>
+struct Chunk {
+  uint4 raw[sizeof(T) / 2];
+  template <bool VEC>
+  __device__ __forceinline__ void load(const T* p, int c0, int d) {
+    constexpr int kVecs = sizeof(T) / 2;
 #pragma unroll
-      for (int h = 0; h < (int)(kChunk * sizeof(T) / 16); ++h) {
-        const uint4 raw = *reinterpret_cast<const uint4*>(p + c0 + h * (16 / sizeof(T)));
-        const T* e = reinterpret_cast<const T*>(&raw);
+    for (int h = 0; h < kVecs; ++h) raw[h] = make_uint4(0u, 0u, 0u, 0u);
+    if (VEC) {
+      if (c0 < d) {
 #pragma unroll
-        for (int i = 0; i < (int)(16 / sizeof(T)); ++i) v[h * (16 / sizeof(T)) + i] = to_f32(e[i]);
+        for (int h = 0; h < kVecs; ++h) raw[h] = reinterpret_cast<const uint4*>(p + c0)[h];
       }
     } else {
+      T* e = reinterpret_cast<T*>(raw);
 #pragma unroll
-      for (int i = 0; i < kChunk; ++i) v[i] = 0.0f;
+      for (int i = 0; i < kChunk; ++i)
+        if (c0 + i < d) e[i] = p[c0 + i];
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < kChunk; ++i) v[i] = c0 + i < d ? to_f32(p[c0 + i]) : 0.0f;
   }
-}
+  __device__ __forceinline__ float at(int i) const { return to_f32(reinterpret_cast<const T*>(raw)[i]); }
+};
 template <class T, bool VEC>
 __device__ __forceinline__ void store_chunk(T* p, int c0, int d, const float (&v)[kChunk]) {
   if (VEC) {
@@ -88,40 +90,44 @@ __device__ __forceinline__ void store_q8(uint8_t* p, int c0, int d, const float 
 }
 
 // One row at a time by all threads of the CTA; thread t holds the chunks t,
-// t + blockDim, ... (C of them) in registers from the load to the last store.
-// blockDim is a multiple of 32, so a group of 32, 64 or 128 columns lies in 4,
-// 8 or 16 neighbouring lanes.
-template <class T, int C, bool VEC>
+// t + blockDim, ... (C of them) in registers from the load to the last store, and
+// the next row's are on their way meanwhile.  blockDim is a multiple of 32, so a group
+// of 32, 64 or 128 columns lies in 4, 8 or 16 neighbouring lanes.
+template <class T, int C, bool VEC, bool RESIDUAL>
 __global__ void __launch_bounds__(512) add_rms_norm_kernel(const NormArgs a) {
-  __shared__ float red[2][2][32];
+  __shared__ float red[2][2][16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   const int d = a.d;
+  Chunk<T> x[C], r[C], g[C];
+  auto fetch = [&](long long row) {
+    if (row >= a.N) return;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int c0 = (c * blockDim.x + tid) * kChunk;
+      x[c].template load<VEC>(static_cast<const T*>(a.x) + row * a.x_ld, c0, d);
+      if (RESIDUAL) r[c].template load<VEC>(static_cast<const T*>(a.residual) + row * a.residual_ld, c0, d);
+    }
+  };
   pdl_wait();
   pdl_trigger();
-  float g[C][kChunk];
+  fetch(blockIdx.x);
 #pragma unroll
   for (int c = 0; c < C; ++c)
-    load_chunk<T, VEC>(static_cast<const T*>(a.gamma), (c * blockDim.x + tid) * kChunk, d, g[c]);
+    g[c].template load<VEC>(static_cast<const T*>(a.gamma), (c * blockDim.x + tid) * kChunk, d);
+  const int groups = a.q8_group != 0 ? (d + a.q8_group - 1) / a.q8_group : 1;
   int buf = 0;
   for (long long row = blockIdx.x; row < a.N; row += gridDim.x, buf ^= 1) {
     float s[C][kChunk];
     float ss = 0.0f, top = 0.0f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int c0 = (c * blockDim.x + tid) * kChunk;
-      load_chunk<T, VEC>(static_cast<const T*>(a.x) + row * a.x_ld, c0, d, s[c]);
-      if (a.residual != nullptr) {
-        float r[kChunk];
-        load_chunk<T, VEC>(static_cast<const T*>(a.residual) + row * a.residual_ld, c0, d, r);
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i) s[c][i] += r[i];
-      }
+    for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int i = 0; i < kChunk; ++i) {
+        s[c][i] = RESIDUAL ? x[c].at(i) + r[c].at(i) : x[c].at(i);
         ss = fmaf(s[c][i], s[c][i], ss);
-        top = max_nan(top, fabsf(s[c][i] * g[c][i]));
+        top = max_nan(top, fabsf(s[c][i] * g[c].at(i)));
       }
-    }
+    fetch(row + gridDim.x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       ss += __shfl_xor_sync(0xffffffffu, ss, o);
@@ -132,11 +138,17 @@ __global__ void __launch_bounds__(512) add_rms_norm_kernel(const NormArgs a) {
       red[buf][0][warp] = ss;
       red[buf][1][warp] = top;
     }
-    __syncthreads();
-    ss = lane < warps ? red[buf][0][lane] : 0.0f;
-    top = lane < warps ? red[buf][1][lane] : 0.0f;
+    if (RESIDUAL && a.sum != nullptr) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
+      for (int c = 0; c < C; ++c)
+        store_chunk<T, VEC>(static_cast<T*>(a.sum) + row * d, (c * blockDim.x + tid) * kChunk, d, s[c]);
+    }
+    __syncthreads();
+    const int w = lane & 15;                               // of at most 16 warps, in both halves
+    ss = w < warps ? red[buf][0][w] : 0.0f;
+    top = w < warps ? red[buf][1][w] : 0.0f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) {
       ss += __shfl_xor_sync(0xffffffffu, ss, o);
       top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
     }
@@ -148,10 +160,10 @@ __global__ void __launch_bounds__(512) add_rms_norm_kernel(const NormArgs a) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int c0 = (c * blockDim.x + tid) * kChunk;
-      if (a.sum != nullptr) store_chunk<T, VEC>(static_cast<T*>(a.sum) + row * d, c0, d, s[c]);
+      if (!RESIDUAL && a.sum != nullptr) store_chunk<T, VEC>(static_cast<T*>(a.sum) + row * d, c0, d, s[c]);
       float y[kChunk];
 #pragma unroll
-      for (int i = 0; i < kChunk; ++i) y[i] = s[c][i] * rstd * g[c][i];
+      for (int i = 0; i < kChunk; ++i) y[i] = s[c][i] * rstd * g[c].at(i);
       if (a.out != nullptr) store_chunk<T, VEC>(static_cast<T*>(a.out) + row * d, c0, d, y);
       if (a.q8 == nullptr) continue;
       float scale = row_scale;
@@ -162,18 +174,30 @@ __global__ void __launch_bounds__(512) add_rms_norm_kernel(const NormArgs a) {
         for (int o = a.q8_group / kChunk / 2; o > 0; o >>= 1)
           m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
         scale = m / kE4m3Max;
-        const int groups = (d + a.q8_group - 1) / a.q8_group;
-        if (c0 < d && c0 % a.q8_group == 0) a.q8_scale[row * groups + c0 / a.q8_group] = scale;
+        if (c0 < d && (c0 & (a.q8_group - 1)) == 0) a.q8_scale[row * groups + c0 / a.q8_group] = scale;
       }
       store_q8<VEC>(a.q8 + row * d, c0, d, y, scale);
     }
   }
 }
 
-template <class T, int C>
-cudaError_t launch(const NormArgs& a, int threads, bool vec, int grid, cudaStream_t s) {
-  return vec ? launch_pdl(add_rms_norm_kernel<T, C, true>, dim3(grid), dim3(threads), 0, s, a)
-             : launch_pdl(add_rms_norm_kernel<T, C, false>, dim3(grid), dim3(threads), 0, s, a);
+template <class T, int C, bool VEC, bool RESIDUAL>
+cudaError_t launch(const NormArgs& a, int threads, cudaStream_t s) {
+  auto kern = add_rms_norm_kernel<T, C, VEC, RESIDUAL>;
+  int resident = 0;
+  const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kern, threads, 0);
+  if (e != cudaSuccess) return e;
+  const long long most = 152ll * resident;
+  return launch_pdl(kern, dim3((unsigned)(a.N < most ? a.N : most)), dim3(threads), 0, s, a);
+}
+template <class T>
+cudaError_t launch(const NormArgs& a, int threads, int per, bool vec, cudaStream_t s) {
+  if (a.residual != nullptr) {
+    if (per == 1) return vec ? launch<T, 1, true, true>(a, threads, s) : launch<T, 1, false, true>(a, threads, s);
+    return vec ? launch<T, 2, true, true>(a, threads, s) : launch<T, 2, false, true>(a, threads, s);
+  }
+  if (per == 1) return vec ? launch<T, 1, true, false>(a, threads, s) : launch<T, 1, false, false>(a, threads, s);
+  return vec ? launch<T, 2, true, false>(a, threads, s) : launch<T, 2, false, false>(a, threads, s);
 }
 
 }  // namespace
@@ -187,13 +211,7 @@ cudaError_t launch_add_rms_norm(int dtype, const NormArgs& a, cudaStream_t s) {
   const int chunks = (a.d + kChunk - 1) / kChunk;
   const int per = chunks <= 128 ? 1 : 2;
   const int threads = (chunks + per * 32 - 1) / (per * 32) * 32;
-  const int resident = 2048 / threads > 16 ? 16 : 2048 / threads;
-  const long long most = 152ll * resident;
-  const int grid = (int)(a.N < most ? a.N : most);
-  if (dtype == FOVEA_BF16)
-    return per == 1 ? launch<__nv_bfloat16, 1>(a, threads, vec, grid, s)
-                    : launch<__nv_bfloat16, 2>(a, threads, vec, grid, s);
-  return per == 1 ? launch<float, 1>(a, threads, vec, grid, s) : launch<float, 2>(a, threads, vec, grid, s);
+  return dtype == FOVEA_BF16 ? launch<__nv_bfloat16>(a, threads, per, vec, s) : launch<float>(a, threads, per, vec, s);
 }
 
 }  // namespace fovea
