@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "fovea.h"
 
 namespace fovea {
@@ -236,6 +238,20 @@ cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t sme
   return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
 }
 
+// Raises a kernel's limit of dynamic shared memory, once per device (`done`, of the
+// kernel: bit i for device i; devices past the 64th each time).
+template <class K>
+cudaError_t raise_smem_limit(K kern, int bytes, std::atomic<unsigned long long>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+  if ((done.load(std::memory_order_relaxed) & bit) != 0) return cudaSuccess;
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
 // Sets the message fovea_last_error() returns on this thread (api.cu).
 fovea_status report_error(fovea_status st, const char* msg);
 
@@ -368,8 +384,9 @@ struct NormArgs {
   float eps;
   void* sum; void* out;
   uint8_t* q8; float* q8_scale; int q8_group;
+  bool out_vec;                      // the outputs' rows are aligned (set by the launch)
 };
-cudaError_t launch_add_rms_norm(int dtype, const NormArgs& a, cudaStream_t s);
+cudaError_t launch_add_rms_norm(int dtype, NormArgs a, cudaStream_t s);
 
 // Weights in 4 bits (w4.cu): codes [out, in / 2], two a byte with the even
 // column in the low half, scales [out, groups] bf16, zero points [out, groups]

@@ -3,6 +3,7 @@
 // (fovea_linear_w4).
 //   w[o, k] = (code[o, k] - zero[o, k / group]) * scale[o, k / group]
 #include <algorithm>
+#include <atomic>
 
 #include "common.cuh"
 #include "w4_x.cuh"
@@ -537,7 +538,8 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
 template <int G, bool ZEROS>
 cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, size_t smem, cudaStream_t s) {
   auto kern = linear_w4_kernel<G, ZEROS>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+  static std::atomic<unsigned long long> done{0};          // devices whose limit is raised
+  const cudaError_t e = raise_smem_limit(kern, kMaxSmem, done);
   if (e != cudaSuccess) return e;
   const bool x_vec = x_vectors(a.x, a.x_ld, a.x_dtype);
   const int groups = (a.w.in + G - 1) / G;

@@ -13,6 +13,7 @@
 // eight warps read the accumulators, one weight row and half of the columns a
 // thread, and add them times their scales in fp32.
 #include <algorithm>
+#include <atomic>
 
 #include "common.cuh"
 #include "tc_ptx.cuh"
@@ -610,7 +611,8 @@ static cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmX, Args& 
   const int rest = 1024 + kScaleBytes + kBarBytes + tile;
   a.stages = std::min(kMaxStages, (kSmemBudget - rest) / stage);
   const size_t smem = (size_t)a.stages * stage + rest;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  static std::atomic<unsigned long long> done{0};          // devices whose limit is raised
+  const cudaError_t e = raise_smem_limit(kern, 227 * 1024, done);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   const int groups = a.split > 1 ? a.tiles : std::min(a.tiles, 152);
