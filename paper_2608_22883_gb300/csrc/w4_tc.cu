@@ -36,7 +36,7 @@ constexpr int kIntWarps = 8;               // two teams of four, taking turns by
 constexpr int kMmaWarps = 2;               // taking turns by unit
 constexpr int kThreads = 32 * (kSumWarps + kIntWarps + kMmaWarps + 1);
 constexpr int kBarBytes = 1024;
-constexpr int kScaleBytes = kSumWarps * 4 * (kMaxCols / 2) * 4;   // x's scales of four groups, a copy per warp
+constexpr int kScaleBytes = kSumWarps * 4 * (kMaxCols / (kSumWarps / 4)) * 4;   // x's scales of four groups, a copy per warp
 constexpr int kSmemBudget = 224 * 1024;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kAccCol = 256;          // accumulators follow the operand buffers (64 columns each)
@@ -226,7 +226,8 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   // issuing warps: as many as leave each accumulator to one of them (a barrier's
   // parity tells a warp only of the round before its own)
   constexpr int kMmas = kPerUnit == 4 ? 1 : kMmaWarps;
-  constexpr int kHalf = NC / 2;                            // columns of a summing team
+  constexpr int kPart = NC / (kSumWarps / 4);              // columns of a summing team
+  constexpr int kRead = kPart < 32 ? kPart : 32;           // and of one read of theirs
   if (threadIdx.x == 0) {
     for (int i = 0; i < kMaxStages; ++i) {
       mbar_init(&full[i], 1);
@@ -398,25 +399,25 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     if (!go) *abort_flag = 1;
   } else {
     // ---- sums: thread = weight row, a team's warps half of the columns
-    const int quarter = warp & 3, col0 = (warp >> 2) * kHalf;
+    const int quarter = warp & 3, col0 = (warp >> 2) * kPart;
     const int r = quarter * 32 + lane;
     const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16) + kAccCol + (uint32_t)col0;
     const int slots = (k_hi - k_lo) * 2 * kPerUnit, g0 = k_lo * 2 * kPerUnit;
-    float* xs = xs_ring + warp * 4 * kHalf;
+    float* xs = xs_ring + warp * 4 * kPart;
     Turn db;
     bool go = true;
     pdl_wait();                                            // x's scales come from the kernel in front
     for (int t = first; t < a.tiles; t += step) {
       const long long o = (long long)t * kRows + r;
       const __nv_bfloat16* scales = a.w.scales + min(o, (long long)a.w.out - 1) * a.groups;
-      uint64_t acc[kHalf / 2];                             // pairs of columns
+      uint64_t acc[kPart / 2];                             // pairs of columns
 #pragma unroll
-      for (int j = 0; j < kHalf / 2; ++j) acc[j] = 0;
+      for (int j = 0; j < kPart / 2; ++j) acc[j] = 0;
       // scales are loaded a round of four groups before their sums arrive: the
       // weight row's own, and with x's in groups a column a lane, which the warp
       // then shares
       constexpr int kAhead = 4;
-      float s[kAhead], xq[kAhead];
+      float s[kAhead], xq[kAhead][(kPart + 31) / 32];
       const bool quads = a.groups % kAhead == 0 && g0 % kAhead == 0 && slots % kAhead == 0 &&
                          (reinterpret_cast<uintptr_t>(a.w.scales) & 7u) == 0;
       auto fetch = [&](int i0) {
@@ -433,9 +434,11 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
           for (int q = 0; q < kAhead; ++q) s[q] = q < left ? __bfloat162float(scales[g0 + i0 + q]) : 0.0f;
         }
         if (a.by_group) {
-          const float* x = a.x_scale + (long long)(g0 + i0) * kMaxCols + col0 + (lane & (kHalf - 1));
+          const float* x = a.x_scale + (long long)(g0 + i0) * kMaxCols + col0 + (lane & (kRead - 1));
 #pragma unroll
-          for (int q = 0; q < kAhead; ++q) xq[q] = q < left ? x[q * kMaxCols] : 0.0f;
+          for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+            for (int c = 0; c < kPart; c += kRead) xq[q][c / kRead] = q < left ? x[q * kMaxCols + c] : 0.0f;
         }
       };
       fetch(0);
@@ -445,7 +448,9 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
           __syncwarp();                                    // the last round's have been read
 #pragma unroll
           for (int q = 0; q < kAhead; ++q)
-            if (lane < kHalf) xs[q * kHalf + lane] = xq[q];
+#pragma unroll
+            for (int c = 0; c < kPart; c += kRead)
+              if (lane < kRead) xs[q * kPart + c + lane] = xq[q][c / kRead];
           __syncwarp();
         }
 #pragma unroll
@@ -459,50 +464,56 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
             break;
           }
           tc_fence_after();
-          uint32_t v[kHalf];
-          tmem_ld_cols(lanes + (uint32_t)(db.i * 64), v);
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&dempty[db.i]);
-          db.next(kBufs);
           const uint64_t s2 = pack2(__float_as_uint(sc[q]), __float_as_uint(sc[q]));
-          if (a.by_group) {
 #pragma unroll
-            for (int j = 0; j < kHalf; j += 4) {
-              const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(xs + q * kHalf + j);
-              acc[j / 2] = fma2(pack2(v[j], v[j + 1]), mul2(s2, f.x), acc[j / 2]);
-              acc[j / 2 + 1] = fma2(pack2(v[j + 2], v[j + 3]), mul2(s2, f.y), acc[j / 2 + 1]);
+          for (int c = 0; c < kPart; c += kRead) {
+            uint32_t v[kRead];
+            tmem_ld_cols(lanes + (uint32_t)(db.i * 64 + c), v);
+            if (c == kPart - kRead) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&dempty[db.i]);
             }
-          } else {
+            if (a.by_group) {
 #pragma unroll
-            for (int j = 0; j < kHalf; j += 2) acc[j / 2] = fma2(pack2(v[j], v[j + 1]), s2, acc[j / 2]);
+              for (int j = 0; j < kRead; j += 4) {
+                const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(xs + q * kPart + c + j);
+                uint64_t* to = acc + (c + j) / 2;
+                to[0] = fma2(pack2(v[j], v[j + 1]), mul2(s2, f.x), to[0]);
+                to[1] = fma2(pack2(v[j + 2], v[j + 3]), mul2(s2, f.y), to[1]);
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < kRead; j += 2) acc[(c + j) / 2] = fma2(pack2(v[j], v[j + 1]), s2, acc[(c + j) / 2]);
+            }
           }
+          db.next(kBufs);
         }
       }
       if (!go) {                                           // a result that shows it
         *abort_flag = 1;
 #pragma unroll
-        for (int j = 0; j < kHalf / 2; ++j) acc[j] = 0x7FC000007FC00000ull;
+        for (int j = 0; j < kPart / 2; ++j) acc[j] = 0x7FC000007FC00000ull;
       }
-      float sum[kHalf];
+      float sum[kPart];
 #pragma unroll
-      for (int j = 0; j < kHalf; ++j) sum[j] = __uint_as_float((uint32_t)(acc[j / 2] >> (32 * (j & 1))));
+      for (int j = 0; j < kPart; ++j) sum[j] = __uint_as_float((uint32_t)(acc[j / 2] >> (32 * (j & 1))));
       if (split > 1 || a.parts > 1) {
         // the partial tile, [column][row]: over the ring when its tile is the CTA's
         // only one (every stage has been consumed), else behind it
         float* part = split > 1 ? reinterpret_cast<float*>(smem) : parts_tile;
         if (split == 1) sum_teams_sync();                  // the last tile's readers are done
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) part[(col0 + j) * kRows + r] = sum[j];
+        for (int j = 0; j < kPart; ++j) part[(col0 + j) * kRows + r] = sum[j];
         if (split == 1) {
           sum_teams_sync();
           if (o < a.w.out)
-            for (int n = warp >> 2; n < a.rows; n += 2)
+            for (int n = warp >> 2; n < a.rows; n += kSumWarps / 4)
               store_y(a, o, n, part[3 * n * kRows + r] + part[(3 * n + 1) * kRows + r] + part[(3 * n + 2) * kRows + r]);
         }
       } else if (o < a.w.out) {
-        if (a.y_dtype == FOVEA_BF16) store_rows<__nv_bfloat16, kHalf>(a, o, col0, sum);
-        else store_rows<float, kHalf>(a, o, col0, sum);
+        if (a.y_dtype == FOVEA_BF16) store_rows<__nv_bfloat16, kPart>(a, o, col0, sum);
+        else store_rows<float, kPart>(a, o, col0, sum);
       }
     }
   }

@@ -9,6 +9,7 @@ no CPU fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Dict, Optional
 
@@ -518,9 +519,7 @@ def quantize_w4(W: torch.Tensor, group: int = 128, *, symmetric: bool = True,
     return {"codes": codes, "scales": scales, "zeros": zeros}
 
 
-W4_FEW = 2, 16384       # rows and columns up to which linear_w4 needs no workspace, whatever x's type
-
-
+@functools.lru_cache(maxsize=512)       # a function of its arguments alone
 def linear_w4_workspace_size(N: int, in_features: int, group: int = 128,
                              dtype: torch.dtype = torch.bfloat16, x_group: int = 0) -> int:
     """fovea_linear_w4_workspace_size: bytes linear_w4 needs for N rows of x (0:
@@ -569,7 +568,7 @@ def linear_w4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
     if workspace is not None:
         ws_bytes = workspace.numel()
         ws_at = _need("workspace", workspace, (ws_bytes,), torch.uint8)
-    elif N > W4_FEW[0] or in_f > W4_FEW[1]:
+    else:
         ws_bytes = linear_w4_workspace_size(N, in_f, group, dt, x_group)
         if ws_bytes:
             workspace = empty((ws_bytes,), dtype=torch.uint8, device=dev)
