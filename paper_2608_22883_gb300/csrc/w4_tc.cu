@@ -139,6 +139,11 @@ __device__ __forceinline__ float ld_dsmem_f32(uint32_t caddr) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(caddr) : "memory");
   return v;
 }
+__device__ __forceinline__ uint32_t ld_dsmem_u32(uint32_t caddr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(caddr) : "memory");
+  return v;
+}
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -539,15 +544,17 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     cluster_sync();
     const int r = threadIdx.x & (kRows - 1);
     const long long o = (long long)first * kRows + r;
-    const uint32_t part = smem_u32(smem);
+    const uint32_t part = smem_u32(smem), aborted = smem_u32(const_cast<int*>(abort_flag));
     constexpr int kLanes = kThreads / kRows;
     if (threadIdx.x < kLanes * kRows && o < a.w.out) {
+      bool whole = true;                                   // no CTA of the tile gave up
+      for (int q = 0; q < split; ++q) whole &= ld_dsmem_u32(map_dsmem(aborted, (uint32_t)q)) == 0u;
       for (int n = rank + split * (int)(threadIdx.x / kRows); n < a.rows; n += split * kLanes) {
         float v = 0.0f;
         for (int p = 0; p < a.parts; ++p)
           for (int q = 0; q < split; ++q)
             v += ld_dsmem_f32(map_dsmem(part + (uint32_t)(((n * a.parts + p) * kRows + r) * 4), (uint32_t)q));
-        store_y(a, o, n, v);
+        store_y(a, o, n, whole ? v : __int_as_float(0x7FC00000));
       }
     }
     cluster_sync();

@@ -265,6 +265,45 @@ def test_linear(fovea, x_type, group, n, o, k, pad):
         check_product(y, x, x_scale, codes, scales, zeros, group, bias)
 
 
+@pytest.mark.parametrize("n,o,k,group", [
+    (1, 40001, 512, 128), (3, 39000, 320, 32),           # more tiles than the device has warps
+    (33, 20100, 768, 64), (64, 39100, 256, 128),         # more tiles than it has SMs
+    (20, 20000, 512, 32),
+])
+def test_linear_many_tiles(fovea, n, o, k, group):
+    g = gen(o)
+    codes, scales, zeros = make_w4(g, o, k, group, n % 2 == 1)
+    for dtype in (BF16, FP32):
+        x = torch.randn((n, k), generator=g, device="cuda").to(dtype)
+        y = fovea.linear_w4(x, codes, scales, zeros, group=group)
+        torch.cuda.synchronize()
+        check_product(y, x, None, codes, scales, zeros, group, None)
+
+
+@pytest.mark.parametrize("o", [300, 6000])               # tiles split over clusters, and not
+def test_linear_wait_that_gives_up(fovea, o):
+    """A bounded wait that runs out is told by the workspace and by NaN, and the
+    workspace serves the next call."""
+    g = gen(o)
+    n, k = 64, 16384
+    codes, scales, _ = make_w4(g, o, k, 128, False)
+    x = torch.randn((n, k), generator=g, device="cuda").to(BF16)
+    ws = torch.empty(fovea.linear_w4_workspace_size(n, k), device="cuda", dtype=torch.uint8)
+    want = fovea.linear_w4(x, codes, scales, workspace=ws)
+    fovea.sync_errors(ws)
+    fovea.debug_wait_limit(1)
+    try:
+        y = fovea.linear_w4(x, codes, scales, workspace=ws)
+        with pytest.raises(fovea.FoveaError) as e:
+            fovea.sync_errors(ws)
+    finally:
+        fovea.debug_wait_limit(0)
+    assert e.value.status == fovea.ERR_TIMEOUT
+    assert torch.isnan(y).any()
+    assert torch.equal(fovea.linear_w4(x, codes, scales, workspace=ws), want)
+    fovea.sync_errors(ws)
+
+
 def test_linear_fp32_rows_keep_all_their_bits(fovea):
     # codes and scales of 1: y is the row's sum; values that bf16 cannot hold
     k = 64
