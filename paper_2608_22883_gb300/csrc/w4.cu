@@ -196,7 +196,8 @@ quantize_w4_kernel(const T* __restrict__ W, long long ld, int out, int in, uint8
 constexpr int kMaxSmem = 227 * 1024;
 constexpr int kWarps = 16, kThreads = 32 * kWarps;
 constexpr int kSpan = 128;             // columns a warp handles together
-constexpr int kTileRows = 16;          // weight rows of a tile
+constexpr int kLaneRows = 2;           // weight rows a lane holds words of: two per 16-row operand
+constexpr int kTileRows = 8 * kLaneRows;   // weight rows of a tile
 constexpr int kQuad = 2;               // spans of codes a warp has on their way
 // Columns of x (an fp32 row counts three times) that a tile takes: the tensor-core
 // instruction's eight.  More go through tensor memory (w4_tc.cu): with two such
@@ -266,9 +267,9 @@ __device__ __forceinline__ uint4 lds_x(uint32_t at) {
   return v;
 }
 
-// The codes of one span of weight rows g and g + 8 that this lane holds.
+// The codes of one span of weight rows g, g + 8, ... that this lane holds.
 struct Span {
-  uint32_t w[2][4];
+  uint32_t w[kLaneRows][4];
 };
 
 // The scales (bf16 pairs) and zero points (bytes) of kQuad spans of a weight row.
@@ -277,10 +278,10 @@ struct Quad {
   static constexpr int kGroups = kQuad * kSpan / G;
   uint32_t s[kGroups / 2], z[(kGroups + 3) / 4];
   // `vec`: every row's scales and zeros start at a multiple of kGroups, aligned
+  // p, pz: of the row's group g0
   template <bool ZEROS>
-  __device__ __forceinline__ void load(const W4& w, long long row_at, int g0, int groups, bool vec) {
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, const uint8_t* pz, int g0, int groups, bool vec) {
     if (vec) {
-      const __nv_bfloat16* p = w.scales + row_at + g0;
       if (kGroups == 2) {
         s[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
       } else if (kGroups == 4) {
@@ -294,19 +295,19 @@ struct Quad {
         }
       }
       if (ZEROS && kGroups == 2) {
-        z[0] = __ldg(reinterpret_cast<const uint16_t*>(w.zeros + row_at + g0));
+        z[0] = __ldg(reinterpret_cast<const uint16_t*>(pz));
       } else if (ZEROS) {
 #pragma unroll
         for (int i = 0; i < kGroups / 4; ++i)
-          z[i] = __ldg(reinterpret_cast<const uint32_t*>(w.zeros + row_at + g0) + i);
+          z[i] = __ldg(reinterpret_cast<const uint32_t*>(pz) + i);
       }
     } else {                                             // past the last group x is 0
 #pragma unroll
       for (int i = 0; i < kGroups; ++i) {
-        const uint32_t v = g0 + i < groups ? __bfloat16_as_ushort(w.scales[row_at + g0 + i]) : 0u;
+        const uint32_t v = g0 + i < groups ? __bfloat16_as_ushort(p[i]) : 0u;
         s[i / 2] = i & 1 ? s[i / 2] | v << 16 : v;
         if (ZEROS) {
-          const uint32_t b = g0 + i < groups ? w.zeros[row_at + g0 + i] : 8u;
+          const uint32_t b = g0 + i < groups ? pz[i] : 8u;
           z[i / 4] = i & 3 ? z[i / 4] | b << (8 * (i & 3)) : b;
         }
       }
@@ -357,18 +358,24 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
 
   pdl_wait();
   pdl_trigger();
-  // The next quad's codes: this lane's first words of rows g and g + 8 (past the last
-  // row, of that one again: the results are not stored), and how far they are into the
-  // row.  A word past its row's end keeps what the register held: x is 0 there.
+  // The next quad: this lane's first words of its rows (past the last row, of that one
+  // again: the results are not stored) and their scales.  A word past its row's end keeps
+  // what the register held: x is 0 there.
   const int row_bytes = a.w.in / 2;
   constexpr int kQuadBytes = kQuad * kSpan / 2;
   const int lane_byte = word_column<G>(0, t) / 2;
-  const uint8_t *next0, *next1;
+  const uint8_t* next[kLaneRows];
+  const __nv_bfloat16* next_scale[kLaneRows];
+  const uint8_t* next_zero[kLaneRows];
   int next_tile = first, next_quad = q_lo;
   auto enter = [&]() {                                     // a tile
-    const long long row = (long long)next_tile * kTileRows + g, last = a.w.out - 1;
-    next0 = a.w.codes + min(row, last) * row_bytes + q_lo * kQuadBytes + lane_byte;
-    next1 = a.w.codes + min(row + 8, last) * row_bytes + q_lo * kQuadBytes + lane_byte;
+#pragma unroll
+    for (int h = 0; h < kLaneRows; ++h) {
+      const long long row = min((long long)next_tile * kTileRows + g + 8 * h, (long long)a.w.out - 1);
+      next[h] = a.w.codes + row * row_bytes + q_lo * kQuadBytes + lane_byte;
+      next_scale[h] = a.w.scales + row * groups + q_lo * Quad<G>::kGroups;
+      if (ZEROS) next_zero[h] = a.w.zeros + row * groups + q_lo * Quad<G>::kGroups;
+    }
   };
   auto refill = [&](Span& r, int d) {
     constexpr int kWords = G / 32;               // words in a row of bytes
@@ -378,13 +385,24 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
       uint32_t in = next_tile < tiles;
       if (in && (next_quad + 1) * kQuadBytes > row_bytes)  // the row's last quad, cut short
         in = next_quad * kQuadBytes + lane_byte + off < row_bytes;
-      load_words<kWords>(&r.w[0][j], next0 + off, in);
-      load_words<kWords>(&r.w[1][j], next1 + off, in);
+#pragma unroll
+      for (int h = 0; h < kLaneRows; ++h) load_words<kWords>(&r.w[h][j], next[h] + off, in);
     }
   };
+  Quad<G> n[kLaneRows] = {};
+  auto refill_scales = [&]() {
+    if (next_tile < tiles)
+#pragma unroll
+      for (int h = 0; h < kLaneRows; ++h)
+        n[h].template load<ZEROS>(next_scale[h], next_zero[h], next_quad * Quad<G>::kGroups, groups, scale_vec);
+  };
   auto turn = [&]() {                                      // after a quad
-    next0 += kQuadBytes;
-    next1 += kQuadBytes;
+#pragma unroll
+    for (int h = 0; h < kLaneRows; ++h) {
+      next[h] += kQuadBytes;
+      next_scale[h] += Quad<G>::kGroups;
+      if (ZEROS) next_zero[h] += Quad<G>::kGroups;
+    }
     if (++next_quad == q_hi) {
       next_quad = q_lo;
       next_tile += step;
@@ -396,15 +414,8 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
     enter();
 #pragma unroll
     for (int d = 0; d < kQuad; ++d) refill(ring[d], d);
+    refill_scales();
     turn();
-  }
-  auto row_at = [&](int tile, int h) {                     // scales of row g + 8 h, the last row's past the end
-    return min((long long)tile * kTileRows + g + 8 * h, (long long)a.w.out - 1) * groups;
-  };
-  Quad<G> n_0 = {}, n_1 = {};
-  if (first < tiles) {
-    n_0.template load<ZEROS>(a.w, row_at(first, 0), q_lo * Quad<G>::kGroups, groups, scale_vec);
-    n_1.template load<ZEROS>(a.w, row_at(first, 1), q_lo * Quad<G>::kGroups, groups, scale_vec);
   }
   if (tid == 0) xs[-1] = make_uint4(0u, 0u, 0u, 0u);
   // x, a few units a thread on their way together
@@ -447,18 +458,13 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
   float* mine = part + warp * kTilePart;
   const float* tile_part = part + team * split * kTilePart;
   for (int tile = first; tile < tiles; tile += step) {
-    float acc[4] = {};
+    float acc[kLaneRows / 2][4] = {};
     uint32_t x_at = x_first;
     for (int quad = q_lo; quad < q_hi; ++quad) {
-      const Quad<G> c_0 = n_0, c_1 = n_1;
-      {
-        const bool same = quad + 1 < q_hi;
-        const int tt = same ? tile : tile + step, qq = same ? quad + 1 : q_lo;
-        if (tt < tiles) {
-          n_0.template load<ZEROS>(a.w, row_at(tt, 0), qq * Quad<G>::kGroups, groups, scale_vec);
-          n_1.template load<ZEROS>(a.w, row_at(tt, 1), qq * Quad<G>::kGroups, groups, scale_vec);
-        }
-      }
+      Quad<G> c[kLaneRows];
+#pragma unroll
+      for (int h = 0; h < kLaneRows; ++h) c[h] = n[h];
+      refill_scales();
 #pragma unroll
       for (int d = 0; d < kQuad; ++d) {
         const int span = quad * kQuad + d;
@@ -467,41 +473,41 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
 #pragma unroll
           for (int ii = 0; ii < kSpan / G; ++ii) {
             const int gq = d * (kSpan / G) + ii;           // of the quad's groups
-            float sum[4];
-            uint32_t z0 = 0x43084308u, z1 = 0x43084308u;
-            if (ZEROS) {
-              z0 = c_0.zero2(gq);
-              z1 = c_1.zero2(gq);
-            }
+            float sum[kLaneRows / 2][4];
+            uint32_t z[kLaneRows];
+#pragma unroll
+            for (int h = 0; h < kLaneRows; ++h) z[h] = ZEROS ? c[h].zero2(gq) : 0x43084308u;
 #pragma unroll
             for (int jj = 0; jj < G / 32; ++jj) {
               const int j = ii * (G / 32) + jj;
-              uint32_t w0[4], w1[4];               // column pairs 0 4, 1 5, 2 6, 3 7
-#pragma unroll
-              for (int p = 0; p < 4; ++p) {
-                w0[p] = bf16_sub2(w4_pair(r.w[0][j] >> (4 * p), k128), z0);
-                w1[p] = bf16_sub2(w4_pair(r.w[1][j] >> (4 * p), k128), z1);
-              }
               const uint4 b = lds_x(x_at);
               x_at += x_step;
-              if (jj == 0) mma_16x8x16_first(sum, w0[0], w1[0], w0[1], w1[1], b.x, b.y);
-              else mma_16x8x16(sum, w0[0], w1[0], w0[1], w1[1], b.x, b.y);
-              mma_16x8x16(sum, w0[2], w1[2], w0[3], w1[3], b.z, b.w);
+#pragma unroll
+              for (int m = 0; m < kLaneRows / 2; ++m) {
+                uint32_t w0[4], w1[4];             // column pairs 0 4, 1 5, 2 6, 3 7
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                  w0[p] = bf16_sub2(w4_pair(r.w[2 * m][j] >> (4 * p), k128), z[2 * m]);
+                  w1[p] = bf16_sub2(w4_pair(r.w[2 * m + 1][j] >> (4 * p), k128), z[2 * m + 1]);
+                }
+                if (jj == 0) mma_16x8x16_first(sum[m], w0[0], w1[0], w0[1], w1[1], b.x, b.y);
+                else mma_16x8x16(sum[m], w0[0], w1[0], w0[1], w1[1], b.x, b.y);
+                mma_16x8x16(sum[m], w0[2], w1[2], w0[3], w1[3], b.z, b.w);
+              }
             }
-            const float s0 = c_0.scale(gq), s1 = c_1.scale(gq);
+            float x0 = 1.0f, x1 = 1.0f;
             if (by_group) {
-              const int n = 2 * t, gs = min(quad * Quad<G>::kGroups + gq, groups - 1);
-              const float x0 = n < cols ? xscale[gs * cols + n] : 0.0f;
-              const float x1 = n + 1 < cols ? xscale[gs * cols + n + 1] : 0.0f;
-              acc[0] = fmaf(sum[0], s0 * x0, acc[0]);
-              acc[1] = fmaf(sum[1], s0 * x1, acc[1]);
-              acc[2] = fmaf(sum[2], s1 * x0, acc[2]);
-              acc[3] = fmaf(sum[3], s1 * x1, acc[3]);
-            } else {
-              acc[0] = fmaf(sum[0], s0, acc[0]);
-              acc[1] = fmaf(sum[1], s0, acc[1]);
-              acc[2] = fmaf(sum[2], s1, acc[2]);
-              acc[3] = fmaf(sum[3], s1, acc[3]);
+              const int col = 2 * t, gs = min(quad * Quad<G>::kGroups + gq, groups - 1);
+              x0 = col < cols ? xscale[gs * cols + col] : 0.0f;
+              x1 = col + 1 < cols ? xscale[gs * cols + col + 1] : 0.0f;
+            }
+#pragma unroll
+            for (int m = 0; m < kLaneRows / 2; ++m) {
+              const float s0 = c[2 * m].scale(gq), s1 = c[2 * m + 1].scale(gq);
+              acc[m][0] = fmaf(sum[m][0], s0 * x0, acc[m][0]);
+              acc[m][1] = fmaf(sum[m][1], s0 * x1, acc[m][1]);
+              acc[m][2] = fmaf(sum[m][2], s1 * x0, acc[m][2]);
+              acc[m][3] = fmaf(sum[m][3], s1 * x1, acc[m][3]);
             }
           }
         }
@@ -513,8 +519,9 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
     if (split > 1) team_sync(team, split);                 // the last tile has been read
     else __syncwarp();
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      *reinterpret_cast<float2*>(mine + (g + 8 * h) * kFewCols + 2 * t) = make_float2(acc[2 * h], acc[2 * h + 1]);
+    for (int h = 0; h < kLaneRows; ++h)
+      *reinterpret_cast<float2*>(mine + (g + 8 * h) * kFewCols + 2 * t) =
+          make_float2(acc[h / 2][2 * (h & 1)], acc[h / 2][2 * (h & 1) + 1]);
     if (split > 1) team_sync(team, split);
     else __syncwarp();
     for (int u = rank * 32 + lane; u < kTileRows * rows; u += 32 * split) {
