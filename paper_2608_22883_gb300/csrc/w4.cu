@@ -196,15 +196,22 @@ quantize_w4_kernel(const T* __restrict__ W, long long ld, int out, int in, uint8
 constexpr int kMaxSmem = 227 * 1024;
 constexpr int kWarps = 16, kThreads = 32 * kWarps;
 constexpr int kSpan = 128;             // columns a warp handles together
-constexpr int kLaneRows = 2;           // weight rows a lane holds words of: two per 16-row operand
-constexpr int kTileRows = 8 * kLaneRows;   // weight rows of a tile
 constexpr int kQuad = 2;               // spans of codes a warp has on their way
 // Columns of x (an fp32 row counts three times) that a tile takes: the tensor-core
 // instruction's eight.  More go through tensor memory (w4_tc.cu): with two such
 // instructions a word 16 rows by 4096 x 32000 took 44.8 us here against 27.3 there, 8
-// rows 26.4.
+// rows 22.4.
 constexpr int kFewCols = 8;
-constexpr int kTilePart = kTileRows * kFewCols;
+// A tile is 8 * R weight rows, of which a lane holds the words of R: 16 rows are one
+// operand, 32 two that share each read of x.  The registers for 32 are there with
+// symmetric groups of 128 alone (64: spills, 23.2 against 22.1 us).  There 32 rows are
+// faster once every SM has more than four tiles of 16 and rows are long enough to pay
+// for fewer warps at work; one row of x, us with 16 and with 32 weight rows a tile:
+// 128000 x 4096 67.1 and 57.2, 48000 33.3 and 27.8, 32000 20.2 and 19.1, 11000 10.9 and
+// 10.2, 8192 7.6 and 8.4; 32000 x 1024 7.4 and 7.9.  Eight rows of x, 32000 x 4096: 26.2
+// and 22.4.
+template <int R> constexpr int kTileFloats = 8 * R * kFewCols;     // a warp's partial tile
+template <int R> constexpr long long kFixedBytes = 16 + kWarps * kTileFloats<R> * 4;
 
 // Offset within a span of the eight columns of word j of lane quarter t: the
 // four quarters of a warp's lanes share the sum of one tensor-core product, so
@@ -268,8 +275,9 @@ __device__ __forceinline__ uint4 lds_x(uint32_t at) {
 }
 
 // The codes of one span of weight rows g, g + 8, ... that this lane holds.
+template <int R>
 struct Span {
-  uint32_t w[kLaneRows][4];
+  uint32_t w[R][4];
 };
 
 // The scales (bf16 pairs) and zero points (bytes) of kQuad spans of a weight row.
@@ -323,20 +331,21 @@ struct Quad {
 
 // y of up to kFewCols columns (rows of x, an fp32 row as three) in one launch.
 //
-// `split` warps take a tile of 16 weight rows, each a range of its quads (kQuad spans of
-// 128 columns); a warp goes from tile to tile by itself, x in shared memory.  It
+// `split` warps take a tile of 8 * R weight rows, each a range of its quads (kQuad spans
+// of 128 columns); a warp goes from tile to tile by itself, x in shared memory.  It
 // turns the codes into bf16 integers c - z (exact) and multiplies them on the tensor
-// cores, weights as the 16-row operand; a group's fp32 sum is then taken times its
+// cores, weights as the operands of 16 rows; a group's fp32 sum is then taken times its
 // scale.  The codes of the next kQuad spans are on their way in registers
 // meanwhile, across tiles, and so are the next quad's scales.  Only the warps of a
 // split tile meet, in shared memory, in a fixed order.
 //
 // fp32 rows enter as three bf16 rows that add up to them exactly; e4m3 rows are
 // exact in bf16 and their scales join the group's or the result.
-template <int G, bool ZEROS>
+template <int G, bool ZEROS, int R>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bool scale_vec,
                  uint32_t k128) {
+  constexpr int kRows = 8 * R, kTilePart = kTileFloats<R>;
   extern __shared__ __align__(16) uint8_t smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int parts = x_parts(a.x_dtype);
@@ -349,7 +358,7 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
   float* part = reinterpret_cast<float*>(xs + (long long)spans * 16 * cols);
   float* xscale = part + kWarps * kTilePart;
   const bool by_group = a.x_scale != nullptr && a.x_group != 0;
-  const int tiles = (a.w.out + kTileRows - 1) / kTileRows;
+  const int tiles = (a.w.out + kRows - 1) / kRows;
   const int quads = (spans + kQuad - 1) / kQuad;
   // tiles go round the CTAs first, so that every SM has work of a short list
   const int team = warp / split, rank = warp - team * split;
@@ -364,20 +373,20 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
   const int row_bytes = a.w.in / 2;
   constexpr int kQuadBytes = kQuad * kSpan / 2;
   const int lane_byte = word_column<G>(0, t) / 2;
-  const uint8_t* next[kLaneRows];
-  const __nv_bfloat16* next_scale[kLaneRows];
-  const uint8_t* next_zero[kLaneRows];
+  const uint8_t* next[R];
+  const __nv_bfloat16* next_scale[R];
+  const uint8_t* next_zero[R];
   int next_tile = first, next_quad = q_lo;
   auto enter = [&]() {                                     // a tile
 #pragma unroll
-    for (int h = 0; h < kLaneRows; ++h) {
-      const long long row = min((long long)next_tile * kTileRows + g + 8 * h, (long long)a.w.out - 1);
+    for (int h = 0; h < R; ++h) {
+      const long long row = min((long long)next_tile * kRows + g + 8 * h, (long long)a.w.out - 1);
       next[h] = a.w.codes + row * row_bytes + q_lo * kQuadBytes + lane_byte;
       next_scale[h] = a.w.scales + row * groups + q_lo * Quad<G>::kGroups;
       if (ZEROS) next_zero[h] = a.w.zeros + row * groups + q_lo * Quad<G>::kGroups;
     }
   };
-  auto refill = [&](Span& r, int d) {
+  auto refill = [&](Span<R>& r, int d) {
     constexpr int kWords = G / 32;               // words in a row of bytes
 #pragma unroll
     for (int j = 0; j < 4; j += kWords) {
@@ -386,19 +395,19 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
       if (in && (next_quad + 1) * kQuadBytes > row_bytes)  // the row's last quad, cut short
         in = next_quad * kQuadBytes + lane_byte + off < row_bytes;
 #pragma unroll
-      for (int h = 0; h < kLaneRows; ++h) load_words<kWords>(&r.w[h][j], next[h] + off, in);
+      for (int h = 0; h < R; ++h) load_words<kWords>(&r.w[h][j], next[h] + off, in);
     }
   };
-  Quad<G> n[kLaneRows] = {};
+  Quad<G> n[R] = {};
   auto refill_scales = [&]() {
     if (next_tile < tiles)
 #pragma unroll
-      for (int h = 0; h < kLaneRows; ++h)
+      for (int h = 0; h < R; ++h)
         n[h].template load<ZEROS>(next_scale[h], next_zero[h], next_quad * Quad<G>::kGroups, groups, scale_vec);
   };
   auto turn = [&]() {                                      // after a quad
 #pragma unroll
-    for (int h = 0; h < kLaneRows; ++h) {
+    for (int h = 0; h < R; ++h) {
       next[h] += kQuadBytes;
       next_scale[h] += Quad<G>::kGroups;
       if (ZEROS) next_zero[h] += Quad<G>::kGroups;
@@ -409,7 +418,7 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
       if (next_tile < tiles) enter();
     }
   };
-  Span ring[kQuad] = {};
+  Span<R> ring[kQuad] = {};
   if (first < tiles) {
     enter();
 #pragma unroll
@@ -458,32 +467,32 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
   float* mine = part + warp * kTilePart;
   const float* tile_part = part + team * split * kTilePart;
   for (int tile = first; tile < tiles; tile += step) {
-    float acc[kLaneRows / 2][4] = {};
+    float acc[R / 2][4] = {};
     uint32_t x_at = x_first;
     for (int quad = q_lo; quad < q_hi; ++quad) {
-      Quad<G> c[kLaneRows];
+      Quad<G> c[R];
 #pragma unroll
-      for (int h = 0; h < kLaneRows; ++h) c[h] = n[h];
+      for (int h = 0; h < R; ++h) c[h] = n[h];
       refill_scales();
 #pragma unroll
       for (int d = 0; d < kQuad; ++d) {
         const int span = quad * kQuad + d;
         if (span < spans) {
-          const Span& r = ring[d];
+          const Span<R>& r = ring[d];
 #pragma unroll
           for (int ii = 0; ii < kSpan / G; ++ii) {
             const int gq = d * (kSpan / G) + ii;           // of the quad's groups
-            float sum[kLaneRows / 2][4];
-            uint32_t z[kLaneRows];
+            float sum[R / 2][4];
+            uint32_t z[R];
 #pragma unroll
-            for (int h = 0; h < kLaneRows; ++h) z[h] = ZEROS ? c[h].zero2(gq) : 0x43084308u;
+            for (int h = 0; h < R; ++h) z[h] = ZEROS ? c[h].zero2(gq) : 0x43084308u;
 #pragma unroll
             for (int jj = 0; jj < G / 32; ++jj) {
               const int j = ii * (G / 32) + jj;
               const uint4 b = lds_x(x_at);
               x_at += x_step;
 #pragma unroll
-              for (int m = 0; m < kLaneRows / 2; ++m) {
+              for (int m = 0; m < R / 2; ++m) {
                 uint32_t w0[4], w1[4];             // column pairs 0 4, 1 5, 2 6, 3 7
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
@@ -502,7 +511,7 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
               x1 = col + 1 < cols ? xscale[gs * cols + col + 1] : 0.0f;
             }
 #pragma unroll
-            for (int m = 0; m < kLaneRows / 2; ++m) {
+            for (int m = 0; m < R / 2; ++m) {
               const float s0 = c[2 * m].scale(gq), s1 = c[2 * m + 1].scale(gq);
               acc[m][0] = fmaf(sum[m][0], s0 * x0, acc[m][0]);
               acc[m][1] = fmaf(sum[m][1], s0 * x1, acc[m][1]);
@@ -519,14 +528,14 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
     if (split > 1) team_sync(team, split);                 // the last tile has been read
     else __syncwarp();
 #pragma unroll
-    for (int h = 0; h < kLaneRows; ++h)
+    for (int h = 0; h < R; ++h)
       *reinterpret_cast<float2*>(mine + (g + 8 * h) * kFewCols + 2 * t) =
           make_float2(acc[h / 2][2 * (h & 1)], acc[h / 2][2 * (h & 1) + 1]);
     if (split > 1) team_sync(team, split);
     else __syncwarp();
-    for (int u = rank * 32 + lane; u < kTileRows * rows; u += 32 * split) {
-      const int r = u & (kTileRows - 1), n = u / kTileRows;
-      const long long o = (long long)tile * kTileRows + r;
+    for (int u = rank * 32 + lane; u < kRows * rows; u += 32 * split) {
+      const int r = u & (kRows - 1), n = u / kRows;
+      const long long o = (long long)tile * kRows + r;
       float v = 0.0f;
       const float* from = tile_part + r * kFewCols + n * parts;
       for (int p = 0; p < parts; ++p)
@@ -542,9 +551,9 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
   }
 }
 
-template <int G, bool ZEROS>
-cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, size_t smem, cudaStream_t s) {
-  auto kern = linear_w4_kernel<G, ZEROS>;
+template <int G, bool ZEROS, int R>
+cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, long long x_bytes, cudaStream_t s) {
+  auto kern = linear_w4_kernel<G, ZEROS, R>;
   static std::atomic<unsigned long long> done{0};          // devices whose limit is raised
   const cudaError_t e = raise_smem_limit(kern, kMaxSmem, done);
   if (e != cudaSuccess) return e;
@@ -552,19 +561,23 @@ cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, size_t smem, cudaS
   const int groups = (a.w.in + G - 1) / G;
   const bool scale_vec = groups % Quad<G>::kGroups == 0 && (reinterpret_cast<uintptr_t>(a.w.scales) & 15u) == 0 &&
                          (reinterpret_cast<uintptr_t>(a.w.zeros) & 3u) == 0;
-  const int tiles = (a.w.out + kTileRows - 1) / kTileRows;
+  const int tiles = (a.w.out + 8 * R - 1) / (8 * R);
   const int quads = (a.w.in + kQuad * kSpan - 1) / (kQuad * kSpan);
   // warps a tile: few tiles are split until each warp of the device has work
   int split = 1;
   while (split < 8 && split * 2 <= quads && (long long)tiles * split * 2 <= 152 * kWarps) split *= 2;
   const long long work = (long long)tiles * split;
   const int grid = (int)std::min<long long>(152, std::max<long long>(1, split == 1 ? work : (work + split - 1) / split));
-  return launch_pdl(kern, dim3(grid), dim3(kThreads), smem, s, a, n0, n1, split, x_vec, scale_vec,
+  return launch_pdl(kern, dim3(grid), dim3(kThreads), (size_t)(x_bytes + kFixedBytes<R>), s, a, n0, n1, split, x_vec, scale_vec,
                     kW4One28);
 }
 template <int G>
-cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, size_t smem, cudaStream_t s) {
-  return a.w.zeros != nullptr ? launch_few<G, true>(a, n0, n1, smem, s) : launch_few<G, false>(a, n0, n1, smem, s);
+cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, long long x_bytes, cudaStream_t s) {
+  if (a.w.zeros != nullptr) return launch_few<G, true, 2>(a, n0, n1, x_bytes, s);
+  if constexpr (G == 128)
+    if (a.w.out > 4 * 152 * 16 && a.w.in >= 2048 && x_bytes + kFixedBytes<4> <= kMaxSmem)
+      return launch_few<G, false, 4>(a, n0, n1, x_bytes, s);
+  return launch_few<G, false, 2>(a, n0, n1, x_bytes, s);
 }
 
 }  // namespace
@@ -601,11 +614,10 @@ cudaError_t launch_quantize_w4(int dtype, const void* W, long long ld, int out, 
 static long long col_bytes(int in, int group, bool by_group) {
   return (in + kSpan - 1) / kSpan * 256ll + (by_group ? 4ll * ((in + group - 1) / group) : 0);
 }
-constexpr long long kFixedBytes = 16 + kWarps * kTilePart * 4;
 static long long few_rows(int in, int group, int x_dtype, bool by_group) {    // of a launch
   const int parts = x_parts(x_dtype);
   return std::min<long long>(kFewCols / parts,
-                             (kMaxSmem - kFixedBytes) / (col_bytes(in, group, by_group) * parts));
+                             (kMaxSmem - kFixedBytes<2>) / (col_bytes(in, group, by_group) * parts));
 }
 static bool is_few(int N, int in, int group, int x_dtype, bool by_group) {
   return (long long)N * x_parts(x_dtype) <= kFewCols && few_rows(in, group, x_dtype, by_group) > 0;
@@ -624,10 +636,10 @@ cudaError_t launch_linear_w4(const LinearW4Args& a, cudaStream_t s) {
   for (int n0 = 0; n0 < a.N; n0 += rows) {
     const int n1 = std::min(a.N, n0 + rows);
     const int cols = (n1 - n0) * parts;
-    const size_t smem = (size_t)(cols * col_bytes(a.w.in, a.w.group, by_group) + kFixedBytes);
-    const cudaError_t e = a.w.group == 128 ? launch_few<128>(a, n0, n1, smem, s)
-                          : a.w.group == 64 ? launch_few<64>(a, n0, n1, smem, s)
-                                            : launch_few<32>(a, n0, n1, smem, s);
+    const long long x_bytes = cols * col_bytes(a.w.in, a.w.group, by_group);
+    const cudaError_t e = a.w.group == 128 ? launch_few<128>(a, n0, n1, x_bytes, s)
+                          : a.w.group == 64 ? launch_few<64>(a, n0, n1, x_bytes, s)
+                                            : launch_few<32>(a, n0, n1, x_bytes, s);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
