@@ -280,6 +280,26 @@ def test_linear_many_tiles(fovea, n, o, k, group):
         check_product(y, x, None, codes, scales, zeros, group, None)
 
 
+@pytest.mark.parametrize("x_type", ["bf16", "fp32", "e4m3-row", "e4m3-group"])
+@pytest.mark.parametrize("n,o,k,pad", [
+    (1, 9729, 2048, 0), (2, 9759, 2080, 0), (5, 9985, 2176, 3), (8, 10016, 4096, 8), (8, 9745, 13824, 0),
+    (1, 39111, 2048, 0),
+])
+def test_linear_wide_tiles(fovea, x_type, n, o, k, pad):
+    # many weight rows in symmetric groups of 128, a few rows of x: the last tile is ragged
+    g = gen(n + o + k)
+    codes, scales, _ = make_w4(g, o, k, 128, False)
+    x_scale = None
+    if x_type.startswith("e4m3"):
+        x_scale = 0.01 + torch.rand((n, -(-k // 128)) if x_type == "e4m3-group" else (n,), generator=g, device="cuda")
+    x = torch.empty((n, k + pad), device="cuda", dtype=dict(bf16=BF16, fp32=FP32).get(x_type, E4M3))[:, :k]
+    x.copy_(torch.randn((n, k), generator=g, device="cuda"))
+    bias = torch.randn(o, generator=g, device="cuda") if n > 1 else None
+    y = fovea.linear_w4(x, codes, scales, x_scale=x_scale, bias=bias)
+    torch.cuda.synchronize()
+    check_product(y, x, x_scale, codes, scales, None, 128, bias)
+
+
 @pytest.mark.parametrize("o", [300, 6000])               # tiles split over clusters, and not
 def test_linear_wait_that_gives_up(fovea, o):
     """A bounded wait that runs out is told by the workspace and by NaN, and the
