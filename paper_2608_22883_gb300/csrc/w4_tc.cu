@@ -44,7 +44,7 @@ constexpr uint32_t kAccCol = 256;          // accumulators follow the operand bu
 struct Args {
   W4 w;
   int groups;
-  int cols, cols_pad;                // columns of x (rows times parts); padded to 32 or 64
+  int cols, cols_pad;                // columns of x (rows times parts); padded to 16, 32, 48 or 64
   int parts;                         // columns a row of x is the sum of
   int n0, rows;                      // rows of y
   const float* x_scale;              // by_group: [groups, kMaxCols]; else [kMaxCols] or null
@@ -79,29 +79,56 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// C consecutive accumulator columns of this thread's lane.
+// Consecutive accumulator columns of this thread's lane.
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7"
+      "}, [%8];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+      : "r"(taddr)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-        "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15"
+      "}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+// (early outputs: the first read's may not take the place of the next one's address)
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[24]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%24];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%8, %9, %10, %11, %12, %13, %14, %15}, [%25];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%16, %17, %18, %19, %20, %21, %22, %23}, [%26];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=&r"(r[0]), "=&r"(r[1]), "=&r"(r[2]), "=&r"(r[3]), "=&r"(r[4]), "=&r"(r[5]), "=&r"(r[6]),
+        "=&r"(r[7]), "=&r"(r[8]), "=&r"(r[9]), "=&r"(r[10]), "=&r"(r[11]), "=&r"(r[12]), "=&r"(r[13]),
+        "=&r"(r[14]), "=&r"(r[15]), "=&r"(r[16]), "=&r"(r[17]), "=&r"(r[18]), "=&r"(r[19]), "=&r"(r[20]),
+        "=&r"(r[21]), "=&r"(r[22]), "=&r"(r[23])
+      : "r"(taddr), "r"(taddr + 8u), "r"(taddr + 16u)
+      : "memory");
 }
 __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[32]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-        "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
-        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
-        "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+      "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31"
+      "}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
+        "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]),
+        "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]),
+        "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
 }
 // Two fp32 operations in one instruction.
 __device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
@@ -200,7 +227,9 @@ struct Turn {
   }
 };
 
-// NC: accumulator columns (cols_pad); G: the group.  A tile's contraction may
+// NC: accumulator columns (cols_pad), in the instruction's steps of 16: the summing
+// warps' work goes with them (40 rows by 4096 x 32000, 48 columns against 64: 27.3 and
+// 28.8 us, in groups of 64 40.1 and 44.0).  G: the group.  A tile's contraction may
 // be split over the CTAs of a cluster, which then has one tile.
 template <int NC, int G>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -232,7 +261,6 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   // parity tells a warp only of the round before its own)
   constexpr int kMmas = kPerUnit == 4 ? 1 : kMmaWarps;
   constexpr int kPart = NC / (kSumWarps / 4);              // columns of a summing team
-  constexpr int kRead = kPart < 32 ? kPart : 32;           // and of one read of theirs
   if (threadIdx.x == 0) {
     for (int i = 0; i < kMaxStages; ++i) {
       mbar_init(&full[i], 1);
@@ -422,7 +450,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
       // weight row's own, and with x's in groups a column a lane, which the warp
       // then shares
       constexpr int kAhead = 4;
-      float s[kAhead], xq[kAhead][(kPart + 31) / 32];
+      float s[kAhead], xq[kAhead];
       const bool quads = a.groups % kAhead == 0 && g0 % kAhead == 0 && slots % kAhead == 0 &&
                          (reinterpret_cast<uintptr_t>(a.w.scales) & 7u) == 0;
       auto fetch = [&](int i0) {
@@ -439,11 +467,9 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
           for (int q = 0; q < kAhead; ++q) s[q] = q < left ? __bfloat162float(scales[g0 + i0 + q]) : 0.0f;
         }
         if (a.by_group) {
-          const float* x = a.x_scale + (long long)(g0 + i0) * kMaxCols + col0 + (lane & (kRead - 1));
+          const float* x = a.x_scale + (long long)(g0 + i0) * kMaxCols + col0 + min(lane, kPart - 1);
 #pragma unroll
-          for (int q = 0; q < kAhead; ++q)
-#pragma unroll
-            for (int c = 0; c < kPart; c += kRead) xq[q][c / kRead] = q < left ? x[q * kMaxCols + c] : 0.0f;
+          for (int q = 0; q < kAhead; ++q) xq[q] = q < left ? x[q * kMaxCols] : 0.0f;
         }
       };
       fetch(0);
@@ -453,9 +479,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
           __syncwarp();                                    // the last round's have been read
 #pragma unroll
           for (int q = 0; q < kAhead; ++q)
-#pragma unroll
-            for (int c = 0; c < kPart; c += kRead)
-              if (lane < kRead) xs[q * kPart + c + lane] = xq[q][c / kRead];
+            if (lane < kPart) xs[q * kPart + lane] = xq[q];
           __syncwarp();
         }
 #pragma unroll
@@ -470,27 +494,21 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
           }
           tc_fence_after();
           const uint64_t s2 = pack2(__float_as_uint(sc[q]), __float_as_uint(sc[q]));
+          uint32_t v[kPart];
+          tmem_ld_cols(lanes + (uint32_t)(db.i * 64), v);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&dempty[db.i]);
+          if (a.by_group) {
 #pragma unroll
-          for (int c = 0; c < kPart; c += kRead) {
-            uint32_t v[kRead];
-            tmem_ld_cols(lanes + (uint32_t)(db.i * 64 + c), v);
-            if (c == kPart - kRead) {
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(&dempty[db.i]);
+            for (int j = 0; j < kPart; j += 4) {
+              const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(xs + q * kPart + j);
+              acc[j / 2] = fma2(pack2(v[j], v[j + 1]), mul2(s2, f.x), acc[j / 2]);
+              acc[j / 2 + 1] = fma2(pack2(v[j + 2], v[j + 3]), mul2(s2, f.y), acc[j / 2 + 1]);
             }
-            if (a.by_group) {
+          } else {
 #pragma unroll
-              for (int j = 0; j < kRead; j += 4) {
-                const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(xs + q * kPart + c + j);
-                uint64_t* to = acc + (c + j) / 2;
-                to[0] = fma2(pack2(v[j], v[j + 1]), mul2(s2, f.x), to[0]);
-                to[1] = fma2(pack2(v[j + 2], v[j + 3]), mul2(s2, f.y), to[1]);
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < kRead; j += 2) acc[(c + j) / 2] = fma2(pack2(v[j], v[j + 1]), s2, acc[(c + j) / 2]);
-            }
+            for (int j = 0; j < kPart; j += 2) acc[j / 2] = fma2(pack2(v[j], v[j + 1]), s2, acc[j / 2]);
           }
           db.next(kBufs);
         }
@@ -651,7 +669,10 @@ static cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmX, Args& 
 
 template <int G>
 static cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmX, Args& a, cudaStream_t s) {
-  return a.cols_pad == 32 ? launch<32, G>(tmW, tmX, a, s) : launch<64, G>(tmW, tmX, a, s);
+  return a.cols_pad == 16   ? launch<16, G>(tmW, tmX, a, s)
+         : a.cols_pad == 32 ? launch<32, G>(tmW, tmX, a, s)
+         : a.cols_pad == 48 ? launch<48, G>(tmW, tmX, a, s)
+                            : launch<64, G>(tmW, tmX, a, s);
 }
 
 }  // namespace w4tc
@@ -689,7 +710,7 @@ cudaError_t launch_linear_w4_tc(const LinearW4Args& l, cudaStream_t s) {
     a.rows = std::min(p.rows_block, l.N - a.n0);
     a.parts = p.parts;
     a.cols = a.rows * p.parts;
-    a.cols_pad = a.cols <= 32 ? 32 : 64;
+    a.cols_pad = (a.cols + 15) / 16 * 16;                  // the instruction's step
     a.by_group = by_group;
     a.x_scale = x.x_groups == 0 ? nullptr : x.scale_out + (size_t)b * kMaxCols * x.x_groups;
     a.bias = l.bias;
