@@ -31,12 +31,17 @@ constexpr int kUnitK = 128;                // columns of an operand buffer in te
 constexpr int kMaxCols = 64;               // columns of x a launch takes
 constexpr int kBufs = 4;                   // operand buffers, and accumulators
 constexpr int kMaxStages = 6;
-constexpr int kSumWarps = 8;               // two teams of four, each half of the columns
+constexpr int kMaxSumWarps = 8;
 constexpr int kIntWarps = 8;               // two teams of four, taking turns by unit
 constexpr int kMmaWarps = 2;               // taking turns by unit
-constexpr int kThreads = 32 * (kSumWarps + kIntWarps + kMmaWarps + 1);
+// Summing warps for NC columns: one team of four, or two that take half of the
+// columns each.
+// us with one and with two, 4096 x 32000 in groups of 128: 16 rows 24.4 and 26.3, 32
+// 25.6 and 26.5; in two teams 64 took less than in one.
+template <int NC> constexpr int kSums = NC <= 32 ? 4 : kMaxSumWarps;
+template <int NC> constexpr int kThreads = 32 * (kSums<NC> + kIntWarps + kMmaWarps + 1);
 constexpr int kBarBytes = 1024;
-constexpr int kScaleBytes = kSumWarps * 4 * (kMaxCols / (kSumWarps / 4)) * 4;   // x's scales of four groups, a copy per warp
+constexpr int kScaleBytes = 4 * 4 * kMaxCols * 4;   // x's scales of four groups, a copy per warp
 constexpr int kSmemBudget = 224 * 1024;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kAccCol = 256;          // accumulators follow the operand buffers (64 columns each)
@@ -202,8 +207,9 @@ __device__ __forceinline__ void store_rows(const Args& a, long long o, int col0,
   }
 }
 // A barrier of the summing warps alone.
+template <int WARPS>
 __device__ __forceinline__ void sum_teams_sync() {
-  asm volatile("bar.sync 1, %0;" ::"n"(32 * kSumWarps) : "memory");
+  asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");
 }
 
 // A place in a ring of barriers and the parity of its round (no division in the
@@ -232,11 +238,12 @@ struct Turn {
 // 28.8 us, in groups of 64 40.1 and 44.0).  G: the group.  A tile's contraction may
 // be split over the CTAs of a cluster, which then has one tile.
 template <int NC, int G>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads<NC>, 1)
 linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
                     const __grid_constant__ Args a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  constexpr int kSumWarps = kSums<NC>;
   constexpr int kXBlock = NC * 128;                        // 64 k of every column
   constexpr int kStageBytes = kCodeBytes + 4 * kXBlock;
   float* xs_ring = reinterpret_cast<float*>(smem + a.stages * kStageBytes);
@@ -525,11 +532,11 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
         // the partial tile, [column][row]: over the ring when its tile is the CTA's
         // only one (every stage has been consumed), else behind it
         float* part = split > 1 ? reinterpret_cast<float*>(smem) : parts_tile;
-        if (split == 1) sum_teams_sync();                  // the last tile's readers are done
+        if (split == 1) sum_teams_sync<kSumWarps>();                  // the last tile's readers are done
 #pragma unroll
         for (int j = 0; j < kPart; ++j) part[(col0 + j) * kRows + r] = sum[j];
         if (split == 1) {
-          sum_teams_sync();
+          sum_teams_sync<kSumWarps>();
           if (o < a.w.out)
             for (int n = warp >> 2; n < a.rows; n += kSumWarps / 4)
               store_y(a, o, n, part[3 * n * kRows + r] + part[(3 * n + 1) * kRows + r] + part[(3 * n + 2) * kRows + r]);
@@ -563,7 +570,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     const int r = threadIdx.x & (kRows - 1);
     const long long o = (long long)first * kRows + r;
     const uint32_t part = smem_u32(smem), aborted = smem_u32(const_cast<int*>(abort_flag));
-    constexpr int kLanes = kThreads / kRows;
+    constexpr int kLanes = kThreads<NC> / kRows;
     if (threadIdx.x < kLanes * kRows && o < a.w.out) {
       bool whole = true;                                   // no CTA of the tile gave up
       for (int q = 0; q < split; ++q) whole &= ld_dsmem_u32(map_dsmem(aborted, (uint32_t)q)) == 0u;
@@ -653,7 +660,7 @@ static cudaError_t launch(const CUtensorMap& tmW, const CUtensorMap& tmX, Args& 
   cudaLaunchConfig_t cfg = {};
   const int groups = a.split > 1 ? a.tiles : std::min(a.tiles, 152);
   cfg.gridDim = dim3(groups * a.split);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(kThreads<NC>);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
