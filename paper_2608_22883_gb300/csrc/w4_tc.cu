@@ -29,7 +29,7 @@ constexpr int kStageK = 256;               // columns of a stage: 128 bytes of c
 constexpr int kCodeBytes = kRows * 128;
 constexpr int kUnitK = 128;                // columns of an operand buffer in tensor memory
 constexpr int kMaxCols = 64;               // columns of x a launch takes
-constexpr int kBufs = 4;                   // operand buffers, and accumulators
+constexpr int kBufs = 4;                   // operand buffers
 constexpr int kMaxStages = 6;
 constexpr int kMaxSumWarps = 8;
 constexpr int kIntWarps = 8;               // two teams of four, taking turns by unit
@@ -44,7 +44,8 @@ constexpr int kBarBytes = 1024;
 constexpr int kScaleBytes = 4 * 4 * kMaxCols * 4;   // x's scales of four groups, a copy per warp
 constexpr int kSmemBudget = 224 * 1024;
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kAccCol = 256;          // accumulators follow the operand buffers (64 columns each)
+constexpr int kSlots = 4;                  // accumulator slots
+constexpr uint32_t kAccCol = 256;          // they follow the operand buffers (64 columns each)
 
 struct Args {
   W4 w;
@@ -84,55 +85,91 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// Consecutive accumulator columns of this thread's lane.
-__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[8]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {"
-      "%0, %1, %2, %3, %4, %5, %6, %7"
-      "}, [%8];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-      : "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[16]) {
+// Consecutive accumulator columns of this thread's lane, of one group or of two that
+// lie kPair columns apart, with their wait (several reads: early outputs, that none
+// takes the place of a later read's address).
+constexpr uint32_t kPair = 32;
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[1][16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
-      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15"
-      "}, [%16];\n\t"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "=r"(r[0][0]), "=r"(r[0][1]), "=r"(r[0][2]), "=r"(r[0][3]), "=r"(r[0][4]), "=r"(r[0][5]),
+        "=r"(r[0][6]), "=r"(r[0][7]), "=r"(r[0][8]), "=r"(r[0][9]), "=r"(r[0][10]), "=r"(r[0][11]),
+        "=r"(r[0][12]), "=r"(r[0][13]), "=r"(r[0][14]), "=r"(r[0][15])
       : "r"(taddr)
       : "memory");
 }
-// (early outputs: the first read's may not take the place of the next one's address)
-__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[24]) {
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[1][24]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%24];\n\t"
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%8, %9, %10, %11, %12, %13, %14, %15}, [%25];\n\t"
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%16, %17, %18, %19, %20, %21, %22, %23}, [%26];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7}, [%24];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {"
+      "%8, %9, %10, %11, %12, %13, %14, %15}, [%25];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {"
+      "%16, %17, %18, %19, %20, %21, %22, %23}, [%26];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
-      : "=&r"(r[0]), "=&r"(r[1]), "=&r"(r[2]), "=&r"(r[3]), "=&r"(r[4]), "=&r"(r[5]), "=&r"(r[6]),
-        "=&r"(r[7]), "=&r"(r[8]), "=&r"(r[9]), "=&r"(r[10]), "=&r"(r[11]), "=&r"(r[12]), "=&r"(r[13]),
-        "=&r"(r[14]), "=&r"(r[15]), "=&r"(r[16]), "=&r"(r[17]), "=&r"(r[18]), "=&r"(r[19]), "=&r"(r[20]),
-        "=&r"(r[21]), "=&r"(r[22]), "=&r"(r[23])
+      : "=&r"(r[0][0]), "=&r"(r[0][1]), "=&r"(r[0][2]), "=&r"(r[0][3]), "=&r"(r[0][4]), "=&r"(r[0][5]),
+        "=&r"(r[0][6]), "=&r"(r[0][7]), "=&r"(r[0][8]), "=&r"(r[0][9]), "=&r"(r[0][10]), "=&r"(r[0][11]),
+        "=&r"(r[0][12]), "=&r"(r[0][13]), "=&r"(r[0][14]), "=&r"(r[0][15]), "=&r"(r[0][16]),
+        "=&r"(r[0][17]), "=&r"(r[0][18]), "=&r"(r[0][19]), "=&r"(r[0][20]), "=&r"(r[0][21]),
+        "=&r"(r[0][22]), "=&r"(r[0][23])
       : "r"(taddr), "r"(taddr + 8u), "r"(taddr + 16u)
       : "memory");
 }
-__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[1][32]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
-      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
-      "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31"
-      "}, [%32];\n\t"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, "
+      "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
-        "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]),
-        "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]),
-        "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "=r"(r[0][0]), "=r"(r[0][1]), "=r"(r[0][2]), "=r"(r[0][3]), "=r"(r[0][4]), "=r"(r[0][5]),
+        "=r"(r[0][6]), "=r"(r[0][7]), "=r"(r[0][8]), "=r"(r[0][9]), "=r"(r[0][10]), "=r"(r[0][11]),
+        "=r"(r[0][12]), "=r"(r[0][13]), "=r"(r[0][14]), "=r"(r[0][15]), "=r"(r[0][16]), "=r"(r[0][17]),
+        "=r"(r[0][18]), "=r"(r[0][19]), "=r"(r[0][20]), "=r"(r[0][21]), "=r"(r[0][22]), "=r"(r[0][23]),
+        "=r"(r[0][24]), "=r"(r[0][25]), "=r"(r[0][26]), "=r"(r[0][27]), "=r"(r[0][28]), "=r"(r[0][29]),
+        "=r"(r[0][30]), "=r"(r[0][31])
       : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[2][16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=&r"(r[0][0]), "=&r"(r[0][1]), "=&r"(r[0][2]), "=&r"(r[0][3]), "=&r"(r[0][4]), "=&r"(r[0][5]),
+        "=&r"(r[0][6]), "=&r"(r[0][7]), "=&r"(r[0][8]), "=&r"(r[0][9]), "=&r"(r[0][10]), "=&r"(r[0][11]),
+        "=&r"(r[0][12]), "=&r"(r[0][13]), "=&r"(r[0][14]), "=&r"(r[0][15]), "=&r"(r[1][0]), "=&r"(r[1][1]),
+        "=&r"(r[1][2]), "=&r"(r[1][3]), "=&r"(r[1][4]), "=&r"(r[1][5]), "=&r"(r[1][6]), "=&r"(r[1][7]),
+        "=&r"(r[1][8]), "=&r"(r[1][9]), "=&r"(r[1][10]), "=&r"(r[1][11]), "=&r"(r[1][12]), "=&r"(r[1][13]),
+        "=&r"(r[1][14]), "=&r"(r[1][15])
+      : "r"(taddr), "r"(taddr + kPair)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[2][32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, "
+      "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%64];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, "
+      "%49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%65];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=&r"(r[0][0]), "=&r"(r[0][1]), "=&r"(r[0][2]), "=&r"(r[0][3]), "=&r"(r[0][4]), "=&r"(r[0][5]),
+        "=&r"(r[0][6]), "=&r"(r[0][7]), "=&r"(r[0][8]), "=&r"(r[0][9]), "=&r"(r[0][10]), "=&r"(r[0][11]),
+        "=&r"(r[0][12]), "=&r"(r[0][13]), "=&r"(r[0][14]), "=&r"(r[0][15]), "=&r"(r[0][16]),
+        "=&r"(r[0][17]), "=&r"(r[0][18]), "=&r"(r[0][19]), "=&r"(r[0][20]), "=&r"(r[0][21]),
+        "=&r"(r[0][22]), "=&r"(r[0][23]), "=&r"(r[0][24]), "=&r"(r[0][25]), "=&r"(r[0][26]),
+        "=&r"(r[0][27]), "=&r"(r[0][28]), "=&r"(r[0][29]), "=&r"(r[0][30]), "=&r"(r[0][31]), "=&r"(r[1][0]),
+        "=&r"(r[1][1]), "=&r"(r[1][2]), "=&r"(r[1][3]), "=&r"(r[1][4]), "=&r"(r[1][5]), "=&r"(r[1][6]),
+        "=&r"(r[1][7]), "=&r"(r[1][8]), "=&r"(r[1][9]), "=&r"(r[1][10]), "=&r"(r[1][11]), "=&r"(r[1][12]),
+        "=&r"(r[1][13]), "=&r"(r[1][14]), "=&r"(r[1][15]), "=&r"(r[1][16]), "=&r"(r[1][17]),
+        "=&r"(r[1][18]), "=&r"(r[1][19]), "=&r"(r[1][20]), "=&r"(r[1][21]), "=&r"(r[1][22]),
+        "=&r"(r[1][23]), "=&r"(r[1][24]), "=&r"(r[1][25]), "=&r"(r[1][26]), "=&r"(r[1][27]),
+        "=&r"(r[1][28]), "=&r"(r[1][29]), "=&r"(r[1][30]), "=&r"(r[1][31])
+      : "r"(taddr), "r"(taddr + kPair)
       : "memory");
 }
 // Two fp32 operations in one instruction.
@@ -253,8 +290,8 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   uint64_t* afull = empty + kMaxStages;
   uint64_t* aempty = afull + kBufs;
   uint64_t* dfull = aempty + kBufs;
-  uint64_t* dempty = dfull + kBufs;
-  uint64_t* drain = dempty + kBufs;
+  uint64_t* dempty = dfull + kSlots;
+  uint64_t* drain = dempty + kSlots;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -264,9 +301,13 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   const int first = (int)blockIdx.x / split, step = (int)gridDim.x / split;
   const int k_lo = a.ksteps * rank / split, k_hi = a.ksteps * (rank + 1) / split;
   constexpr int kPerUnit = kUnitK / G;                     // groups in a unit: 1, 2 or 4
-  // issuing warps: as many as leave each accumulator to one of them (a barrier's
-  // parity tells a warp only of the round before its own)
-  constexpr int kMmas = kPerUnit == 4 ? 1 : kMmaWarps;
+  // accumulators, 64 columns a slot: of one group, or of two of up to 32 columns, which
+  // then share its waits (16 rows by 4096 x 32000 in groups of 32: 48.3 us, one by one
+  // 60.0; with more columns there were only two slots, 40 rows: 68.5 us and 67.3)
+  constexpr int kSlotGroups = NC <= 32 && kPerUnit > 1 ? 2 : 1, kSlotsUnit = kPerUnit / kSlotGroups;
+  // issuing warps: as many as leave each slot to one of them (a barrier's parity tells
+  // a warp only of the round before its own)
+  constexpr int kMmas = kSlots >= kMmaWarps * kSlotsUnit ? kMmaWarps : 1;
   constexpr int kPart = NC / (kSumWarps / 4);              // columns of a summing team
   if (threadIdx.x == 0) {
     for (int i = 0; i < kMaxStages; ++i) {
@@ -276,6 +317,8 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     for (int i = 0; i < kBufs; ++i) {
       mbar_init(&afull[i], kIntWarps / 2);
       mbar_init(&aempty[i], 1);
+    }
+    for (int i = 0; i < kSlots; ++i) {
       mbar_init(&dfull[i], 1);
       mbar_init(&dempty[i], kSumWarps);
     }
@@ -337,8 +380,8 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     const int w = warp - kSumWarps - kIntWarps;
     Turn st, ab, db;
     ab.i = w;
-    db.i = w * kPerUnit;                                   // of the unit's first group
-    bool go = w < kMmas, reused = false;                   // its accumulators for the second time
+    db.i = w * kSlotsUnit;                                 // the unit's first slot
+    bool go = w < kMmas, reused = false;                   // its slots for the second time
     for (int t = first; go && t < a.tiles; t += step) {
       for (int k = k_lo; go && k < k_hi; ++k, st.next(a.stages)) {
         const uint64_t bdesc = desc0 + (uint64_t)((st.i * kStageBytes) >> 4);
@@ -348,7 +391,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
           go = go && warp_wait(&afull[ab.i], ab.parity, abort_flag, a.wait_ns);
           const uint32_t ta = tmem_base + (uint32_t)(ab.i * 64);
 #pragma unroll
-          for (int s = 0; s < kPerUnit; ++s) {
+          for (int s = 0; s < kSlotsUnit; ++s) {
             if (reused)
               go = go && warp_wait(&dempty[db.i + s], db.parity ^ 1u, abort_flag, a.wait_ns);
             if (go) {
@@ -356,14 +399,16 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
               const uint32_t td = tmem_base + kAccCol + (uint32_t)((db.i + s) * 64);
               const uint64_t bh = bdesc + (uint64_t)(h * (2 * kXBlock >> 4));
               if (elect_one()) {
+                constexpr int kSteps = 8 / kPerUnit;       // of 16 columns, a group
 #pragma unroll
-                for (int q = 0; q < 8 / kPerUnit; ++q) {
-                  const int k16 = s * (8 / kPerUnit) + q;  // of the unit's eight
-                  umma_ts(td, ta + (uint32_t)(k16 * 8), bh + (uint64_t)(((k16 >> 2) * kXBlock >> 4) + 2 * (k16 & 3)),
-                          kIdesc, q > 0 ? 1u : 0u);
+                for (int q = 0; q < kSlotGroups * kSteps; ++q) {
+                  const int k16 = s * kSlotGroups * kSteps + q;      // of the unit's eight
+                  umma_ts(td + (uint32_t)(q / kSteps) * kPair, ta + (uint32_t)(k16 * 8),
+                          bh + (uint64_t)(((k16 >> 2) * kXBlock >> 4) + 2 * (k16 & 3)), kIdesc,
+                          q % kSteps > 0 ? 1u : 0u);
                 }
                 umma_commit(&dfull[db.i + s]);
-                if (s == kPerUnit - 1) {
+                if (s == kSlotsUnit - 1) {
                   umma_commit(&aempty[ab.i]);
                   if (kMmas == 2 || h == 1) umma_commit(&empty[st.i]);
                 }
@@ -372,7 +417,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
             }
           }
           ab.skip(kMmas, kBufs);
-          reused |= db.skip(kMmas * kPerUnit, kBufs);
+          reused |= db.skip(kMmas * kSlotsUnit, kSlots);
         }
       }
     }
@@ -493,31 +538,35 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
         for (int q = 0; q < kAhead; ++q) sc[q] = s[q];
         if (i0 + kAhead < slots) fetch(i0 + kAhead);
 #pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
+        for (int q = 0; q < kAhead; q += kSlotGroups) {
           if (i0 + q >= slots) break;
           if (!warp_wait(&dfull[db.i], db.parity, abort_flag, a.wait_ns)) {
             go = false;
             break;
           }
           tc_fence_after();
-          const uint64_t s2 = pack2(__float_as_uint(sc[q]), __float_as_uint(sc[q]));
-          uint32_t v[kPart];
+          uint32_t v[kSlotGroups][kPart];
           tmem_ld_cols(lanes + (uint32_t)(db.i * 64), v);
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&dempty[db.i]);
-          if (a.by_group) {
 #pragma unroll
-            for (int j = 0; j < kPart; j += 4) {
-              const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(xs + q * kPart + j);
-              acc[j / 2] = fma2(pack2(v[j], v[j + 1]), mul2(s2, f.x), acc[j / 2]);
-              acc[j / 2 + 1] = fma2(pack2(v[j + 2], v[j + 3]), mul2(s2, f.y), acc[j / 2 + 1]);
+          for (int u = 0; u < kSlotGroups; ++u) {
+            const uint32_t sq = __float_as_uint(sc[q + u]);
+            const uint64_t s2 = pack2(sq, sq);
+            if (a.by_group) {
+#pragma unroll
+              for (int j = 0; j < kPart; j += 4) {
+                const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(xs + (q + u) * kPart + j);
+                acc[j / 2] = fma2(pack2(v[u][j], v[u][j + 1]), mul2(s2, f.x), acc[j / 2]);
+                acc[j / 2 + 1] = fma2(pack2(v[u][j + 2], v[u][j + 3]), mul2(s2, f.y), acc[j / 2 + 1]);
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < kPart; j += 2) acc[j / 2] = fma2(pack2(v[u][j], v[u][j + 1]), s2, acc[j / 2]);
             }
-          } else {
-#pragma unroll
-            for (int j = 0; j < kPart; j += 2) acc[j / 2] = fma2(pack2(v[j], v[j + 1]), s2, acc[j / 2]);
           }
-          db.next(kBufs);
+          db.next(kSlots);
         }
       }
       if (!go) {                                           // a result that shows it
