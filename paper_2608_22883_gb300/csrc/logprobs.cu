@@ -589,9 +589,22 @@ cudaError_t launch_cluster(void (*kern)(KArgs...), dim3 grid, int cluster, cudaS
   return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
 }
 
-// CTAs per row: enough that the rows fill the device four times over, as long
-// as each has at least two chunks a thread.
-int row_split(long long N, int V, int size) {
+// CTAs of a row's log probabilities.  Each CTA has a search for the largest logits of
+// its own, so the row is cut in two while that leaves a thread six chunks or more,
+// and as many more as there are CTAs for an SM already.  us, one CTA and this: 1 x 151000
+// bf16 29.0 and 13.0, 150 x 151000 51 and 28.7, 40 x 32000 fp32 22.4 and 13.7 (eight
+// CTAs a row 14.6), 250 x 32000 bf16 15.7, not cut (four CTAs a row 25.8).
+int score_split(long long N, int V, int size) {
+  const long long chunks = (long long)V * size / (16 * kThreads);          // a thread's of a whole row
+  int c = 1;
+  while (c < kMaxCluster && chunks * 152 >= 12 * c * std::max(152ll, N * c)) c *= 2;
+  return c;
+}
+
+// CTAs of a row's gradient: enough that the rows fill the device four times over, as
+// long as each has at least two chunks a thread (us, one CTA a row and this: 1 x 151000
+// bf16 13.0 and 4.0, 40 x 32000 fp32 13.8 and 7.8, 200 x 151000 bf16 30.3 and 24.7).
+int grad_split(long long N, int V, int size) {
   int c = 1;
   while (c < kMaxCluster && N * c < 4 * 152 && (long long)V * size / (16 * kThreads) >= 4 * c) c *= 2;
   return c;
@@ -614,7 +627,7 @@ cudaError_t launch_token_logprobs(int dtype, const ScoreArgs& all, cudaStream_t 
     a.lse += n0;
     a.stats += 2 * n0;
     a.entropy += n0;
-    const int split = row_split(a.N, a.V, size);
+    const int split = score_split(a.N, a.V, size);
     const dim3 grid(split, (unsigned)a.N);
     const bool masked = a.allowed != nullptr;
     const cudaError_t e =
@@ -645,7 +658,7 @@ cudaError_t launch_token_logprobs_grad(int dtype, const ScoreGradArgs& all, cuda
     a.entropy += n0;
     // in place, a CTA may not overwrite logits that another CTA of the row still
     // has to read for its tokens' entries
-    const int split = a.dlogits == a.logits ? 1 : row_split(a.N, a.V, size);
+    const int split = a.dlogits == a.logits ? 1 : grad_split(a.N, a.V, size);
     const dim3 grid(split, (unsigned)a.N);
     const size_t smem = (size_t)(a.T + a.k) * 12;
     const bool masked = a.allowed != nullptr;
