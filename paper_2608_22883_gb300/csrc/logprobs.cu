@@ -211,6 +211,13 @@ struct Shared {
 // largest logit.  The k-th largest of the groups' bounds is a threshold that at
 // least k tokens reach, so only groups that reach it (k of them, and ties) are
 // read again, from L2, for the tokens above it: a few more than k.
+//
+// Instructions bound the pass (eighteen a logit, the row's ends and the search among
+// them; two fp32 operations in one where there is such a form) and latency the search.
+// 4096 rows of 32000 bf16: 61 us without alternatives (64 % of the measured copy's
+// bandwidth), 96 us with six (40 %), 144 with 32; one fp32 row of 32000 9.3 us, where the
+// cluster's two meetings and the search's steps follow one another.  256 threads: 128
+// and 512 measured no better.
 template <class T, bool MASKED>
 __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArgs a) {
   constexpr int NV = Row<T>::NV;
@@ -441,7 +448,9 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArg
 
 // The gradient of one row's range of chunks.  Every token's term is p (A - g_H
 // logp) with A of the row; the few tokens with a gradient of their own are
-// written again after it, by the CTA whose range they lie in.
+// written again after it, by the CTA whose range they lie in.  Bound by memory: 4096
+// rows of 32000 bf16 85 us, 6.2 TB/s (91 % of the measured copy); 40 masked fp32 rows
+// 7.8 us.
 template <class T, bool MASKED>
 __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const ScoreGradArgs a) {
   constexpr int NV = Row<T>::NV;

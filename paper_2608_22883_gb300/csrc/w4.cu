@@ -348,6 +348,14 @@ struct Quad {
 //
 // fp32 rows enter as three bf16 rows that add up to them exactly; e4m3 rows are
 // exact in bf16 and their scales join the group's or the result.
+//
+// The weights' bytes are the floor; what it spends is instructions on the codes: a
+// shift, a LOP3 and a subtraction for two of them, at most 4.75 cycles of a scheduler,
+// besides the products.  A warp a tile without barriers and the operands' layout
+// chosen so that a word needs no exchange between lanes keep the rest small.  One bf16
+// row by [32000, 4096] in groups of 128: 19.1 us, 3.5 TB/s (52 % of the measured copy;
+// tensor pipe 20 %); by [128000, 4096] 57 us (70 %); 7 rows by [3584, 3584] in groups of
+// 64 with zero points 7.7 us, a tile's latency.
 template <int G, bool ZEROS, int R>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bool scale_vec,
@@ -570,7 +578,9 @@ cudaError_t launch_few(const LinearW4Args& a, int n0, int n1, long long x_bytes,
                          (reinterpret_cast<uintptr_t>(a.w.zeros) & 3u) == 0;
   const int tiles = (a.w.out + 8 * R - 1) / (8 * R);
   const int quads = (a.w.in + kQuad * kSpan - 1) / (kQuad * kSpan);
-  // warps a tile: few tiles are split until each warp of the device has work
+  // warps a tile: few tiles are split until each warp of the device has work (one row by
+  // [4096, 4096]: one warp a tile 15.4 us, up to four 6.3, up to eight 5.5; [1024, 8192]:
+  // 29.4, 9.0, 6.3)
   int split = 1;
   while (split < 8 && split * 2 <= quads && (long long)tiles * split * 2 <= 152 * kWarps) split *= 2;
   const long long work = (long long)tiles * split;
