@@ -24,10 +24,7 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
-// Columns [c0, c0 + 8) of a row as they lie in memory; columns from d on are 0.  Where
-// the row is off the vectors' boundary, whole chunks are cut out of the aligned vectors
-// around them, which lie within the row but for its first and last chunk; those go by
-// element.
+// Columns [c0, c0 + 8) of a row as they lie in memory; columns from d on are 0.
 template <class T>
 struct Chunk {
   static constexpr int kVecs = sizeof(T) / 2;
@@ -40,56 +37,126 @@ struct Chunk {
       for (int h = 0; h < kVecs; ++h) raw[h] = reinterpret_cast<const uint4*>(p + c0)[h];
     }
   }
-  __device__ __forceinline__ void load_any(const T* p, int c0, int d) {
+  __device__ __forceinline__ float at(int i) const { return to_f32(reinterpret_cast<const T*>(raw)[i]); }
+};
+
+// The same of a row anywhere, in three steps, so that the loads of several rows are on
+// their way together (a wait within a branch for each took 7500 clocks a row): the
+// aligned vectors around the chunk that lie in the row whole; the chunk cut out of them;
+// and the few chunks around which a vector sticks out of the row by element.
+template <class T>
+struct Around {
+  static constexpr int kVecs = sizeof(T) / 2, kUnit = 16 / sizeof(T);
+  uint4 v[kVecs + 1];
+  __device__ __forceinline__ static int off(const T* p) {                  // one for the whole row
+    return (int)(reinterpret_cast<uintptr_t>(p) & 15u) / (int)sizeof(T);
+  }
+  __device__ __forceinline__ void load(const T* p, int c0, int d) {
+    const int at = c0 - off(p);
 #pragma unroll
-    for (int h = 0; h < kVecs; ++h) raw[h] = make_uint4(0u, 0u, 0u, 0u);
-    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u);     // one for the whole row
-    const T* from = p + c0 - off / sizeof(T);
-    if (from >= p && c0 + kChunk + 16 / (int)sizeof(T) <= d) {
-      uint32_t w[4 * (kVecs + 1)], v[4 * kVecs];
-#pragma unroll
-      for (int h = 0; h <= kVecs; ++h) {
-        const uint4 u = reinterpret_cast<const uint4*>(from)[h];
-        w[4 * h] = u.x; w[4 * h + 1] = u.y; w[4 * h + 2] = u.z; w[4 * h + 3] = u.w;
-      }
-      const uint32_t bits = 8 * (off & 3);
-      switch (off >> 2) {                                  // the same in the whole CTA
-        case 0: cut<0>(w, bits, v); break;
-        case 1: cut<1>(w, bits, v); break;
-        case 2: cut<2>(w, bits, v); break;
-        default: cut<3>(w, bits, v);
-      }
-#pragma unroll
-      for (int h = 0; h < kVecs; ++h) raw[h] = make_uint4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
-    } else {
-      T* e = reinterpret_cast<T*>(raw);
-#pragma unroll
-      for (int i = 0; i < kChunk; ++i)
-        if (c0 + i < d) e[i] = p[c0 + i];
+    for (int h = 0; h <= kVecs; ++h) {
+      v[h] = make_uint4(0u, 0u, 0u, 0u);
+      if (at + h * kUnit >= 0 && at + (h + 1) * kUnit <= d && (h < kVecs || at != c0))
+        v[h] = *reinterpret_cast<const uint4*>(p + at + h * kUnit);
     }
   }
   template <int Q>
-  __device__ __forceinline__ static void cut(const uint32_t (&w)[4 * (kVecs + 1)], uint32_t bits, uint32_t (&v)[4 * kVecs]) {
+  __device__ __forceinline__ void cut(uint32_t bits, Chunk<T>& to) const {
+    uint32_t w[4 * (kVecs + 1)];
 #pragma unroll
-    for (int i = 0; i < 4 * kVecs; ++i) v[i] = __funnelshift_r(w[i + Q], w[i + Q + 1 < 4 * (kVecs + 1) ? i + Q + 1 : i + Q], bits);
+    for (int h = 0; h <= kVecs; ++h) {
+      w[4 * h] = v[h].x; w[4 * h + 1] = v[h].y; w[4 * h + 2] = v[h].z; w[4 * h + 3] = v[h].w;
+    }
+    uint32_t r[4 * kVecs];
+#pragma unroll
+    for (int i = 0; i < 4 * kVecs; ++i)
+      r[i] = __funnelshift_r(w[i + Q], w[i + Q + 1 < 4 * (kVecs + 1) ? i + Q + 1 : i + Q], bits);
+#pragma unroll
+    for (int h = 0; h < kVecs; ++h) to.raw[h] = make_uint4(r[4 * h], r[4 * h + 1], r[4 * h + 2], r[4 * h + 3]);
   }
-  __device__ __forceinline__ float at(int i) const { return to_f32(reinterpret_cast<const T*>(raw)[i]); }
+  __device__ __forceinline__ void chunk(const T* p, Chunk<T>& to) const {
+    const uint32_t bytes = off(p) * sizeof(T);
+    switch (bytes >> 2) {                                  // the same in the whole CTA
+      case 0: cut<0>(8 * (bytes & 3), to); break;
+      case 1: cut<1>(8 * (bytes & 3), to); break;
+      case 2: cut<2>(8 * (bytes & 3), to); break;
+      default: cut<3>(8 * (bytes & 3), to);
+    }
+  }
+  __device__ __forceinline__ static bool ragged(const T* p, int c0, int d) {
+    const int at = c0 - off(p);
+    return c0 < d && (at < 0 || at + (kVecs + (at != c0)) * kUnit > d);
+  }
+  __device__ __forceinline__ static void elements(const T* p, int c0, int d, Chunk<T>& to) {
+    T e[kChunk];
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) e[i] = c0 + i < d ? p[c0 + i] : from_f32<T>(0.0f);
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) reinterpret_cast<T*>(to.raw)[i] = e[i];
+  }
 };
+// The W words of each lane's chunk to rows off the vectors' boundary: aligned vectors of
+// V words, cut out of a lane's chunk and the next lane's; what no vector covers (the
+// warp's first and last bytes, the row's end) goes by element.  p: the chunk's place, its
+// first `left` elements in the row.  All lanes of the warp.
+template <class E, int Q, int W, int V>
+__device__ __forceinline__ void store_cut(const uint32_t (&both)[W + V], uint32_t bits, E* p, int head, int left,
+                                          bool last) {
+#pragma unroll
+  for (int h = 0; h < W / V; ++h) {
+    if (head + (h + 1) * (4 * V / (int)sizeof(E)) > left || (last && h == W / V - 1)) continue;
+    uint32_t v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      v[i] = __funnelshift_r(both[h * V + i + Q], both[h * V + i + Q + 1 < W + V ? h * V + i + Q + 1 : W + V - 1], bits);
+    E* to = p + head + h * (4 * V / (int)sizeof(E));
+    if (V == 4) *reinterpret_cast<uint4*>(to) = make_uint4(v[0], v[1], v[V - 2], v[V - 1]);
+    else *reinterpret_cast<uint2*>(to) = make_uint2(v[0], v[1]);
+  }
+}
+template <class E, int W, int V>
+__device__ __forceinline__ void store_shifted(E* p, int left, const uint32_t (&w)[W]) {
+  constexpr int kUnit = 4 * V / (int)sizeof(E);            // elements of a vector
+  const int lane = threadIdx.x & 31;
+  const int off = (int)(reinterpret_cast<uintptr_t>(p) & (4 * V - 1)) / (int)sizeof(E);    // the same in the whole row
+  uint32_t both[W + V];
+#pragma unroll
+  for (int i = 0; i < W; ++i) both[i] = w[i];
+#pragma unroll
+  for (int i = 0; i < V; ++i) both[W + i] = __shfl_down_sync(0xffffffffu, w[i], 1);
+  const int head = off == 0 ? 0 : kUnit - off;             // elements before the first vector's
+  const int bytes = head * (int)sizeof(E);
+  const uint32_t bits = 8 * (bytes & 3);
+  const bool last = lane == 31 && head != 0;               // the next lane's words are not here
+  switch (bytes >> 2) {
+    case 0: store_cut<E, 0, W, V>(both, bits, p, head, left, last); break;
+    case 1: store_cut<E, 1, W, V>(both, bits, p, head, left, last); break;
+    case 2: store_cut<E, V == 4 ? 2 : 0, W, V>(both, bits, p, head, left, last); break;
+    default: store_cut<E, V == 4 ? 3 : 0, W, V>(both, bits, p, head, left, last);
+  }
+  if (lane == 0 || last || left < 2 * kChunk) {
+    const bool before = lane > 0 && head <= left;          // the lane before has stored this one's head
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) {
+      const int h = (i - head) / kUnit;                    // of i >= head: its vector
+      const bool stored = i < head ? before : head + (h + 1) * kUnit <= left && !(last && h == W / V - 1);
+      if (i < left && !stored)
+        p[i] = reinterpret_cast<const E*>(w)[i];
+    }
+  }
+}
 template <class T>
 __device__ __forceinline__ void store_chunk(T* p, int c0, int d, const float (&v)[kChunk], bool vec) {
-  if (vec) {
-    if (c0 < d) {
-      __align__(16) T e[kChunk];
+  constexpr int kWords = kChunk * sizeof(T) / 4;
+  uint32_t w[kWords];
 #pragma unroll
-      for (int i = 0; i < kChunk; ++i) e[i] = from_f32<T>(v[i]);
+  for (int i = 0; i < kChunk; ++i) reinterpret_cast<T*>(w)[i] = from_f32<T>(v[i]);
+  if (!vec) {
+    store_shifted<T, kWords, 4>(p + c0, d - c0, w);
+  } else if (c0 < d) {
 #pragma unroll
-      for (int h = 0; h < (int)(kChunk * sizeof(T) / 16); ++h)
-        reinterpret_cast<uint4*>(p + c0)[h] = reinterpret_cast<const uint4*>(e)[h];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < kChunk; ++i)
-      if (c0 + i < d) p[c0 + i] = from_f32<T>(v[i]);
+    for (int h = 0; h < kWords / 4; ++h)
+      reinterpret_cast<uint4*>(p + c0)[h] = make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]);
   }
 }
 // The chunk of y in e4m3 at the given scale.  y / scale is y times the scale's
@@ -113,21 +180,18 @@ __device__ __forceinline__ void store_q8(uint8_t* p, int c0, int d, const float 
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * h + 2], v[4 * h + 3]), __NV_SATFINITE, __NV_E4M3);
     w[h] = lo | hi << 16;
   }
-  if (vec) {
-    if (c0 < d) *reinterpret_cast<uint2*>(p + c0) = make_uint2(w[0], w[1]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < kChunk; ++i)
-      if (c0 + i < d) p[c0 + i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
-  }
+  if (!vec) store_shifted<uint8_t, 2, 2>(p + c0, d - c0, w);
+  else if (c0 < d) *reinterpret_cast<uint2*>(p + c0) = make_uint2(w[0], w[1]);
 }
 
 // One row at a time by all threads of the CTA; thread t holds the chunks t,
 // t + blockDim, ... (C of them) in registers from the load to the last store.
 // blockDim is a multiple of 32, so a group of 32, 64 or 128 columns lies in 4, 8 or 16
 // neighbouring lanes.  VEC: every row of every tensor is aligned, and the next row is on
-// its way meanwhile; otherwise (fewer registers, more CTAs an SM) rows that are not
-// aligned are read through shifted vectors, and written by element.
+// its way meanwhile; otherwise rows that are not aligned are read and written through
+// shifted vectors, in 64 registers, which leaves an SM more CTAs to wait with (4096 bf16
+// rows of 5111 with 8 bits by 128: 97 us against 113 in 122 registers; 139 with element
+// stores and a wait for each load; aligned rows of 5120 take 33).
 //
 // One pass: a row is read once, normalised and written from registers, so memory bounds
 // a long run of rows.  8192 rows of 5120 bf16 with a residual, three outputs and 8 bits
@@ -135,22 +199,40 @@ __device__ __forceinline__ void store_q8(uint8_t* p, int c0, int d, const float 
 // row on its way 78 us.  One row of 4096: 1.8 us on the device, the call's own cost on
 // the host is several times that.
 template <class T, int C, bool VEC, bool RESIDUAL>
-__global__ void __launch_bounds__(512) add_rms_norm_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(512, (VEC ? 0 : 2)) add_rms_norm_kernel(const NormArgs a) {
   __shared__ float red[2][2][16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   const int d = a.d;
   Chunk<T> x[C], r[C], g[C];
   auto fetch = [&](long long row) {
     if (row >= a.N) return;
+    const T* xp = static_cast<const T*>(a.x) + row * a.x_ld;
+    const T* rp = static_cast<const T*>(a.residual) + row * a.residual_ld;
+    if constexpr (VEC) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int c0 = (c * blockDim.x + tid) * kChunk;
-      const T* xp = static_cast<const T*>(a.x) + row * a.x_ld;
-      const T* rp = static_cast<const T*>(a.residual) + row * a.residual_ld;
-      if (VEC) x[c].load(xp, c0, d);
-      else x[c].load_any(xp, c0, d);
-      if (RESIDUAL && VEC) r[c].load(rp, c0, d);
-      else if (RESIDUAL) r[c].load_any(rp, c0, d);
+      for (int c = 0; c < C; ++c) {
+        const int c0 = (c * blockDim.x + tid) * kChunk;
+        x[c].load(xp, c0, d);
+        if (RESIDUAL) r[c].load(rp, c0, d);
+      }
+    } else {
+      Around<T> ax[C], ar[C];
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int c0 = (c * blockDim.x + tid) * kChunk;
+        ax[c].load(xp, c0, d);
+        if (RESIDUAL) ar[c].load(rp, c0, d);
+      }
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int c0 = (c * blockDim.x + tid) * kChunk;
+        ax[c].chunk(xp, x[c]);
+        if (RESIDUAL) ar[c].chunk(rp, r[c]);
+        if (Around<T>::ragged(xp, c0, d) || (RESIDUAL && Around<T>::ragged(rp, c0, d))) {
+          Around<T>::elements(xp, c0, d, x[c]);
+          if (RESIDUAL) Around<T>::elements(rp, c0, d, r[c]);
+        }
+      }
     }
   };
   pdl_wait();
@@ -158,8 +240,16 @@ __global__ void __launch_bounds__(512) add_rms_norm_kernel(const NormArgs a) {
   if (VEC) fetch(blockIdx.x);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    if (VEC) g[c].load(static_cast<const T*>(a.gamma), (c * blockDim.x + tid) * kChunk, d);
-    else g[c].load_any(static_cast<const T*>(a.gamma), (c * blockDim.x + tid) * kChunk, d);
+    const int c0 = (c * blockDim.x + tid) * kChunk;
+    const T* gp = static_cast<const T*>(a.gamma);
+    if (VEC) {
+      g[c].load(gp, c0, d);
+    } else {
+      Around<T> ag;
+      ag.load(gp, c0, d);
+      ag.chunk(gp, g[c]);
+      if (Around<T>::ragged(gp, c0, d)) Around<T>::elements(gp, c0, d, g[c]);
+    }
   }
   const bool vec = VEC || a.out_vec;
   const int groups = a.q8_group != 0 ? (d + a.q8_group - 1) / a.q8_group : 1;
@@ -265,8 +355,9 @@ cudaError_t launch_add_rms_norm(int dtype, NormArgs a, cudaStream_t s) {
                    aligned(a.residual, 16) && a.residual_ld * size % 16 == 0;
   const int chunks = (a.d + kChunk - 1) / kChunk;
   // two chunks a thread halve the reductions' share of a long run of rows; a few rows are
-  // done sooner with one (64 rows of 4096: 2.75 us against 3.22; 8192 rows 41.1 against 37.4)
-  const int per = chunks <= 128 || (a.N <= 2 * 152 && chunks <= 512) ? 1 : 2;
+  // done sooner with one (64 rows of 4096: 2.75 us against 3.22; 8192 rows 41.1 against
+  // 37.4), and so are rows that need shifting (4096 fp32 rows of 3001: 51 against 55)
+  const int per = chunks <= 128 || ((a.N <= 2 * 152 || !vec) && chunks <= 512) ? 1 : 2;
   const int threads = (chunks + per * 32 - 1) / (per * 32) * 32;
   return dtype == FOVEA_BF16 ? launch<__nv_bfloat16>(a, threads, per, vec, s) : launch<float>(a, threads, per, vec, s);
 }

@@ -95,6 +95,47 @@ def test_norm(fovea, dtype, n, d, pad, q8):
     check_norm(fovea, x, None, gamma, q8, want_out=q8 is None)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("d", [1, 5, 9, 255, 1003, 2050, 4103, 8189])
+def test_norm_rows_anywhere(fovea, dtype, d):
+    """Every offset from the vectors' boundary, of the inputs (residual and gamma at
+    other offsets) and of the outputs; the sum in x's place; nothing outside written."""
+    n, size = 5, 2 if dtype is BF16 else 4
+    g = gen(d)
+    eight = d % 2 == 1
+    for off in range(16 // size):
+        def rows(at, v=None):
+            b = torch.full((n * d + 64,), 7.0, device="cuda", dtype=dtype)
+            if v is not None:
+                b[at:at + n * d] = v.flatten()
+            return b, b[at:at + n * d].view(n, d)
+        v = torch.randn((n, d), generator=g, device="cuda").to(dtype)
+        w = torch.randn((n, d), generator=g, device="cuda").to(dtype)
+        xb, x = rows(16 + off, v)
+        rb, r = rows(16 + 3 * off % 8, w)
+        ob, out = rows(16 + 5 * off % 8)
+        gamma = torch.ones(d + 8, device="cuda", dtype=dtype)[off % 8:off % 8 + d]
+        gamma.copy_(1 + 0.1 * torch.randn(d, generator=g, device="cuda"))
+        q8b = torch.full((n * d + 64,), 99, device="cuda", dtype=torch.uint8)
+        scale = torch.empty((n,), device="cuda")
+        s, y = norm_reference(v, w, gamma, 1e-6)
+        st = fovea.lib().fovea_add_rms_norm(
+            x.data_ptr(), d, r.data_ptr(), d, gamma.data_ptr(), n, d, fovea._DTYPES[dtype], 1e-6, x.data_ptr(),
+            out.data_ptr(), q8b.data_ptr() + 16 + off if eight else None, scale.data_ptr() if eight else None, 0,
+            torch.cuda.current_stream().cuda_stream)
+        assert st == 0
+        torch.cuda.synchronize()
+        assert torch.equal(x, s.to(dtype)) and torch.equal(r, w)
+        within(out, y, y.abs() * (HALF_ULP[dtype] + 40 * U) + 1e-38, "out")
+        for b, at in ((xb, 16 + off), (rb, 16 + 3 * off % 8), (ob, 16 + 5 * off % 8)):
+            assert bool((b[:at] == 7).all()) and bool((b[at + n * d:] == 7).all())
+        if eight:
+            at = 16 + off
+            assert bool((q8b[:at] == 99).all()) and bool((q8b[at + n * d:] == 99).all())
+            q = q8b[at:at + n * d].view(E4M3).view(n, d).double() * scale.double()[:, None]
+            within(q, y, y.abs() * (2.0 ** -4 + 80 * U) + scale.double()[:, None] * 2.0 ** -10 * (1 + 40 * U), "q8")
+
+
 def test_norm_rows_without_size(fovea):
     # zeros, a group of zeros, the smallest and the largest values
     x = torch.zeros((4, 256), device="cuda")
