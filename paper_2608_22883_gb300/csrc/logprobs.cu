@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArg
     if (tid == 0) sh.threshold = 1ull;                 // fewer than k groups with a token: every token
   }
   __syncthreads();
-  if (tid == 0) {
+  if (tid == kThreads - 32) {                              // not of a warp that ranks below
     Sums t = {sh.m[0], sh.S[0], sh.W[0]};
     for (int w = 1; w < kWarps; ++w) join(t, Sums{sh.m[w], sh.S[w], sh.W[w]});
     sh.total = t;
@@ -326,13 +326,15 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArg
     // a NaN (or +inf) is in no bound: then every token is looked at
     const bool odd = sh.total.S != sh.total.S;
     const unsigned long long threshold = odd ? 1ull : sh.threshold;
+    // no key at or above the threshold has a logit below this (a NaN lets all pass)
+    const float least = value_of(order_in(threshold));
     auto each_key = [&](int gr, auto&& f) {                // of a group's tokens, by a warp
       for (int c = lo + gr * 4 + (lane >> 2) * kThreads + (lane & 3); c < hi; c += 8 * kThreads) {
         float v[NV];
         row.load(c, v);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-          if (v[i] * scale != -INFINITY) f(key_of(order_of(v[i]), row.first(c) + i));
+          if (!(v[i] < least) && v[i] * scale != -INFINITY) f(key_of(order_of(v[i]), row.first(c) + i));
       }
       if (gr == 0 && lane < 2 && ragged(lane) >= 0) {
         float v[NV];
