@@ -329,12 +329,27 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArg
     // no key at or above the threshold has a logit below this (a NaN lets all pass)
     const float least = value_of(order_in(threshold));
     auto each_key = [&](int gr, auto&& f) {                // of a group's tokens, by a warp
-      for (int c = lo + gr * 4 + (lane >> 2) * kThreads + (lane & 3); c < hi; c += 8 * kThreads) {
-        float v[NV];
-        row.load(c, v);
+      constexpr int U = 2;                                 // chunks on their way together
+      for (int c = lo + gr * 4 + (lane >> 2) * kThreads + (lane & 3); c < hi; c += U * 8 * kThreads) {
+        uint4 raw[U];
+        uint32_t keep[U];
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-          if (!(v[i] < least) && v[i] * scale != -INFINITY) f(key_of(order_of(v[i]), row.first(c) + i));
+        for (int u = 0; u < U; ++u) {
+          const int at = min(c + u * 8 * kThreads, hi - 1);
+          raw[u] = row.raw(at);
+          if (MASKED) keep[u] = row.bits(at);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (u > 0 && c + u * 8 * kThreads >= hi) break;
+          float v[NV];
+          ln_unpack<T>(raw[u], v);
+          if (MASKED) row.mask(keep[u], v);
+          const int first = row.first(c + u * 8 * kThreads);
+#pragma unroll
+          for (int i = 0; i < NV; ++i)
+            if (!(v[i] < least) && v[i] * scale != -INFINITY) f(key_of(order_of(v[i]), first + i));
+        }
       }
       if (gr == 0 && lane < 2 && ragged(lane) >= 0) {
         float v[NV];
