@@ -117,13 +117,16 @@ __device__ __forceinline__ void rebase(Sums& a, float m2) {
   a.S *= f;
   a.m = m2;
 }
+// The sums of both about the larger reference; the smaller one's are rescaled.
 __device__ __forceinline__ void join(Sums& a, Sums b) {
-  if (b.m == -INFINITY) return;
-  const float m = a.m == -INFINITY ? b.m : max_nan(a.m, b.m);
-  rebase(a, m);
-  rebase(b, m);
-  a.S += b.S;
-  a.W += b.W;
+  const bool up = !(b.m <= a.m);                           // (a NaN goes through d)
+  const Sums hi = up ? b : a, lo = up ? a : b;
+  const float m = max_nan(a.m, b.m);
+  const float d = lo.m == -INFINITY ? 0.0f : max_nan(lo.m - m, -200.0f);   // nothing summed: S, W are 0
+  const float f = ex2(d * kLog2e);
+  a.S = fmaf(f, lo.S, hi.S);
+  a.W = fmaf(f, fmaf(lo.S, d, lo.W), hi.W);
+  a.m = m;
 }
 
 // Two fp32 operations in one instruction.
