@@ -221,8 +221,12 @@ struct Shared {
 // bandwidth), 96 us with six (40 %), 144 with 32; one fp32 row of 32000 9.3 us, where the
 // cluster's two meetings and the search's steps follow one another.  256 threads: 128
 // and 512 measured no better.
+//
+// Six CTAs an SM are worth 40 registers to unmasked bf16 rows (81.2 to 77.6 us) and not to
+// the others (masked bf16 59 to 72, fp32 59.4 to 60.8).
 template <class T, bool MASKED>
-__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArgs a) {
+__global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && !MASKED ? 6 : 0))
+token_logprobs_kernel(const ScoreArgs a) {
   constexpr int NV = Row<T>::NV;
   __shared__ Shared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -244,7 +248,9 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArg
   };
   Seen seen;
   {
-    constexpr int U = 4;                                   // chunks on their way together
+    // chunks on their way together (measured one by one; bf16 4, 3 and 5: 73.9, 74.8 and
+    // 76.1 us; masked bf16 3 and 4: 57.1 and 59.9)
+    constexpr int U = MASKED ? 3 : sizeof(T) == 4 ? 6 : 4;
     int c = lo + tid;
     for (; c + (U - 1) * kThreads < hi; c += U * kThreads) {
       uint4 raw[U];
@@ -262,10 +268,23 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const ScoreArg
         seen.take(v, c + u * kThreads, scale);
       }
     }
-    for (; c < hi; c += kThreads) {
-      float v[NV];
-      row.load(c, v);
-      seen.take(v, c, scale);
+    if (c < hi) {                                          // the last round, cut short
+      uint4 raw[U - 1];
+      uint32_t keep[U - 1];
+#pragma unroll
+      for (int u = 0; u < U - 1; ++u) {
+        const int at = min(c + u * kThreads, hi - 1);
+        raw[u] = row.raw(at);
+        if (MASKED) keep[u] = row.bits(at);
+      }
+#pragma unroll
+      for (int u = 0; u < U - 1; ++u) {
+        if (c + u * kThreads >= hi) break;
+        float v[NV];
+        ln_unpack<T>(raw[u], v);
+        if (MASKED) row.mask(keep[u], v);
+        seen.take(v, c + u * kThreads, scale);
+      }
     }
     if (tid < 2 && ragged(tid) >= 0) {
       float v[NV];
