@@ -588,11 +588,24 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
         store_whole(c + u * kThreads, v);
       }
     }
-    for (; c < hi; c += kThreads) {
-      float v[NV];
-      row.load(c, v);
-      gradient(v);
-      store_whole(c, v);
+    if (c < hi) {                                          // the last round, cut short
+      uint4 raw[U - 1];
+      uint32_t keep[U - 1];
+#pragma unroll
+      for (int u = 0; u < U - 1; ++u)
+        if (c + u * kThreads < hi) {
+          raw[u] = row.raw(c + u * kThreads);
+          if (MASKED) keep[u] = row.bits(c + u * kThreads);
+        }
+#pragma unroll
+      for (int u = 0; u < U - 1; ++u) {
+        if (c + u * kThreads >= hi) break;
+        float v[NV];
+        ln_unpack<T>(raw[u], v);
+        if (MASKED) row.mask(keep[u], v);
+        gradient(v);
+        store_whole(c + u * kThreads, v);
+      }
     }
     const int e = tid == 0 ? 0 : row.chunks - 1;           // the ragged ends
     if (tid < 2 && e >= c_lo && e < c_hi && !row.whole(e) && (tid == 0 || e != 0)) {
