@@ -380,10 +380,12 @@ token_logprobs_kernel(const ScoreArgs a) {
           if (v[i] * scale != -INFINITY) f(key_of(order_of(v[i]), row.first(ragged(lane)) + i));
       }
     };
+    uint32_t mine = 0;                                     // of this warp's groups, those to search
+#pragma unroll
+    for (int q = 0; q < kGroups / kWarps; ++q) mine |= (uint32_t)(sh.upper[q * kWarps + warp] >= threshold) << q;
     if (!odd)
-      for (int gr = warp; gr < kGroups; gr += kWarps) {
-        if (sh.upper[gr] < threshold) continue;
-        each_key(gr, [&](unsigned long long key) {
+      for (; mine != 0; mine &= mine - 1) {
+        each_key((__ffs(mine) - 1) * kWarps + warp, [&](unsigned long long key) {
           if (key < threshold) return;
           const int at = atomicAdd(&sh.count, 1);
           if (at < kCands) sh.cand[at] = key;
