@@ -102,7 +102,8 @@ struct Row {
   }
 };
 
-// Running softmax sums about a reference m (the largest z or somewhat less):
+// Running softmax sums about a reference m (one of the row's z, which the largest seen
+// passes by 2 at most):
 // S = sum e^{z - m}, W = sum e^{z - m} (z - m).
 struct Sums {
   float m, S, W;
@@ -160,6 +161,16 @@ struct Seen {
   int chunk = 0;
 
   __device__ __forceinline__ Sums sums() const { return Sums{m, lo2(S) + hi2(S), lo2(W) + hi2(W)}; }
+  // Before the first chunk, by a whole warp: the largest logit of its lanes' chunks as the
+  // reference, which few later ones pass by 2.
+  template <int NV>
+  __device__ __forceinline__ void seed(const float (&v)[NV], float scale) {
+    float cm = v[0];
+#pragma unroll
+    for (int i = 1; i < NV; ++i) cm = max_nan(cm, v[i]);
+    const float z = value_of(__reduce_max_sync(0xffffffffu, order_of(cm))) * scale;
+    if (fabsf(z) < INFINITY) m = z;
+  }
   // One chunk's logits; a NaN among them makes the sums NaN.
   template <int NV>
   __device__ __forceinline__ void take(const float (&v)[NV], int c, float scale) {
@@ -252,6 +263,7 @@ token_logprobs_kernel(const ScoreArgs a) {
     // 76.1 us; masked bf16 3 and 4: 57.1 and 59.9)
     constexpr int U = MASKED ? 3 : sizeof(T) == 4 ? 6 : 4;
     int c = lo + tid;
+    bool seeded = lo + (tid | 31) + (U - 1) * kThreads >= hi;      // no round of a whole warp
     for (; c + (U - 1) * kThreads < hi; c += U * kThreads) {
       uint4 raw[U];
       uint32_t keep[U];
@@ -265,6 +277,10 @@ token_logprobs_kernel(const ScoreArgs a) {
         float v[NV];
         ln_unpack<T>(raw[u], v);
         if (MASKED) row.mask(keep[u], v);
+        if (u == 0 && !seeded) {
+          seen.seed(v, scale);
+          seeded = true;
+        }
         seen.take(v, c + u * kThreads, scale);
       }
     }
@@ -295,7 +311,8 @@ token_logprobs_kernel(const ScoreArgs a) {
   Sums s = seen.sums();
   int32_t top = order_of(seen.top);
   const int top_chunk = seen.chunk;
-  if (top != kOrderNegInf) rebase(s, seen.top * scale);   // the largest z itself
+  // the largest z itself (the reference is one of the row's)
+  if (top != kOrderNegInf && seen.top * scale > s.m) rebase(s, seen.top * scale);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     Sums b;
