@@ -226,15 +226,14 @@ struct Shared {
 // least k tokens reach, so only groups that reach it (k of them, and ties) are
 // read again, from L2, for the tokens above it: a few more than k.
 //
-// Instructions bound the pass (eighteen a logit, the row's ends and the search among
-// them; two fp32 operations in one where there is such a form) and latency the search.
-// 4096 rows of 32000 bf16: 61 us without alternatives (64 % of the measured copy's
-// bandwidth), 96 us with six (40 %), 144 with 32; one fp32 row of 32000 9.3 us, where the
-// cluster's two meetings and the search's steps follow one another.  256 threads: 128
-// and 512 measured no better.
+// Instructions bound the pass (two fp32 operations in one where there is such a form)
+// and latency the search.  4096 rows of 32000 bf16: 49 us without alternatives (78 % of
+// the measured copy's bandwidth), 70 us with six (56 %), 98 with 32; one fp32 row of 32000
+// 6.9 us, where the cluster's two meetings and the search's steps follow one another.
+// 256 threads: 128 and 512 measured no better.
 //
-// Six CTAs an SM are worth 40 registers to unmasked bf16 rows (81.2 to 77.6 us) and not to
-// the others (masked bf16 59 to 72, fp32 59.4 to 60.8).
+// Six CTAs an SM are worth 40 registers to unmasked bf16 rows (72.6 to 69.6 us) and not to
+// the others (masked bf16 a fifth slower, fp32 2 %).
 template <class T, bool MASKED>
 __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && !MASKED ? 6 : 0))
 token_logprobs_kernel(const ScoreArgs a) {
@@ -259,8 +258,8 @@ token_logprobs_kernel(const ScoreArgs a) {
   };
   Seen seen;
   {
-    // chunks on their way together (measured one by one; bf16 4, 3 and 5: 73.9, 74.8 and
-    // 76.1 us; masked bf16 3 and 4: 57.1 and 59.9)
+    // chunks on their way together (4096 rows of 32000 bf16, 4, 3 and 5: 69.6, 70.5 and 71.5
+    // us; 64 masked fp32 rows 3 and 4: 10.5 and 10.9; 64 unmasked 6 and 4: 9.2 and 9.7)
     constexpr int U = MASKED ? 3 : sizeof(T) == 4 ? 6 : 4;
     int c = lo + tid;
     bool seeded = lo + (tid | 31) + (U - 1) * kThreads >= hi;      // no round of a whole warp
@@ -507,8 +506,8 @@ token_logprobs_kernel(const ScoreArgs a) {
 // The gradient of one row's range of chunks.  Every token's term is p (A - g_H
 // logp) with A of the row; the few tokens with a gradient of their own are
 // written again after it, by the CTA whose range they lie in.  Bound by memory: 4096
-// rows of 32000 bf16 85 us, 6.2 TB/s (91 % of the measured copy); 40 masked fp32 rows
-// 7.8 us.
+// rows of 32000 bf16 82 us, 6.4 TB/s (94 % of the measured copy); 40 masked fp32 rows
+// 7.0 us.
 template <class T, bool MASKED>
 __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const ScoreGradArgs a) {
   constexpr int NV = Row<T>::NV;
@@ -672,8 +671,8 @@ cudaError_t launch_cluster(void (*kern)(KArgs...), dim3 grid, int cluster, cudaS
 // CTAs of a row's log probabilities.  Each CTA has a search for the largest logits of
 // its own, so the row is cut in two while that leaves a thread six chunks or more,
 // and as many more as there are CTAs for an SM already.  us, one CTA and this: 1 x 151000
-// bf16 29.0 and 13.0, 150 x 151000 51 and 28.7, 40 x 32000 fp32 22.4 and 13.7 (eight
-// CTAs a row 14.6), 250 x 32000 bf16 15.7, not cut (four CTAs a row 25.8).
+// bf16 21.6 and 9.4, 40 x 32000 fp32 11.6 and 8.8, 64 masked 16.2 and 10.5 (eight CTAs a
+// row 12.5), 250 x 32000 bf16 11.6, not cut (four CTAs a row 19.1).
 int score_split(long long N, int V, int size) {
   const long long chunks = (long long)V * size / (16 * kThreads);          // a thread's of a whole row
   int c = 1;
@@ -683,7 +682,7 @@ int score_split(long long N, int V, int size) {
 
 // CTAs of a row's gradient: enough that the rows fill the device four times over, as
 // long as each has at least two chunks a thread (us, one CTA a row and this: 1 x 151000
-// bf16 13.0 and 4.0, 40 x 32000 fp32 13.8 and 7.8, 200 x 151000 bf16 30.3 and 24.7).
+// bf16 12.9 and 3.8, 40 x 32000 fp32 11.2 and 6.7, 200 x 151000 bf16 30.1 and 24.3).
 int grad_split(long long N, int V, int size) {
   int c = 1;
   while (c < kMaxCluster && N * c < 4 * 152 && (long long)V * size / (16 * kThreads) >= 4 * c) c *= 2;
