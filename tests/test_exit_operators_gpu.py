@@ -549,6 +549,23 @@ def test_scores_sorted_and_crowded_rows(fovea, dtype):
         check_scores(fovea, x[2:], None, k)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("height", [3.0, 40.0, 300.0, 3e4])
+def test_scores_spikes(fovea, dtype, height):
+    # one token far above, or far below, all others, in the first chunks and in later ones
+    v = 40003
+    at = [0, 7, 2047, 2048, 9000, 30000, v - 1]
+    x = torch.randn((2 * len(at), v), generator=gen(v), device="cuda")
+    for i, a in enumerate(at):
+        x[2 * i, a] = height
+        x[2 * i + 1] += height
+        x[2 * i + 1, a] = -height
+    tokens = torch.tensor([[a, 1] for a in at for _ in range(2)], device="cuda", dtype=torch.int32)
+    check_scores(fovea, x.to(dtype), tokens, 3)
+    keep = torch.rand(x.shape, generator=gen(1), device="cuda") < 0.5
+    check_scores(fovea, x.to(dtype), tokens, 3, keep=keep)
+
+
 def test_scores_not_finite_rows(fovea):
     x = make_logits(gen(11), 4, 3000, FP32)
     x[0, 17] = math.nan
