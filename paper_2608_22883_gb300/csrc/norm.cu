@@ -195,7 +195,7 @@ __device__ __forceinline__ void store_q8(uint8_t* p, int c0, int d, const float 
 //
 // One pass: a row is read once, normalised and written from registers, so memory bounds
 // a long run of rows.  8192 rows of 5120 bf16 with a residual, three outputs and 8 bits
-// in groups of 128: 63.4 us, 5.97 TB/s (88 % of the measured copy); without the next
+// in groups of 128: 63.8 us, 5.94 TB/s (88 % of the measured copy); without the next
 // row on its way 78 us.  One row of 4096: 1.8 us on the device, the call's own cost on
 // the host is several times that.
 template <class T, int C, bool VEC, bool RESIDUAL>
