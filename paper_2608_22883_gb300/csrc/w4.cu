@@ -54,25 +54,48 @@ __device__ __forceinline__ float rint_quotient(float w, float half_scale, float 
   return fmaf(fmaf(r, twice_rcp, h), 0.5f, kMagic) - kMagic;
 }
 
+// Two of them in packed instructions, the same operations.
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  return (uint64_t)__float_as_uint(hi) << 32 | __float_as_uint(lo);
+}
+__device__ __forceinline__ float lo2(uint64_t v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float hi2(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t rint_quotient2(uint64_t w, uint64_t minus_half_scale, uint64_t twice_rcp) {
+  constexpr float kMagic = 12582912.0f;
+  const uint64_t up = pack2(kMagic, kMagic), down = pack2(-kMagic, -kMagic), half = pack2(0.5f, 0.5f);
+  const uint64_t h = add2(fma2(w, twice_rcp, up), down);
+  const uint64_t r = fma2(h, minus_half_scale, w);
+  return add2(fma2(fma2(r, twice_rcp, h), half, up), down);
+}
+
 // A warp takes strips of 256 columns of a row, eight columns a lane, so that a group
 // of G columns is G / 8 neighbouring lanes; U strips are on their way together.  Scale
 // and code are those of IEEE divisions, bit for bit.
 //
 // Reads W once and writes a seventh (fp32) or a quarter (bf16) of its bytes: bound by
-// memory and by instruction issue about evenly.  W [32000, 4096]: fp32 in groups of
-// 32 with zero points 108 us (5.6 TB/s, 82 % of the measured copy), bf16 symmetric in
-// groups of 128 85 us; W [4096, 4096] takes 13 us.  Strips and CTAs an SM, us with two
-// and four, one and six: fp32 108.3 and 114.7, bf16 with zero points 114 and 122, bf16
-// symmetric 89.0 and 84.9.
-template <class T, bool VEC, bool SYMMETRIC>
+// memory and by instruction issue about evenly, hence the packed arithmetic (fp32 108 us
+// without).  W [32000, 4096]: fp32 in groups of 32 with zero points 101 us (6.0 TB/s, 88 %
+// of the measured copy), bf16 the same 103, symmetric in groups of 128 81; W [4096, 4096]
+// bf16 takes 13 us.  One strip and six CTAs an SM: 115, 122 and 86 us.
+template <bool VEC>
 struct QuantShape {                                      // strips on their way; CTAs an SM
-  static constexpr int U = VEC && (sizeof(T) == 4 || !SYMMETRIC) ? 2 : 1, kCtas = U == 2 ? 4 : 6;
+  static constexpr int U = VEC ? 2 : 1, kCtas = VEC ? 4 : 6;
 };
 template <class T, int G, bool VEC, bool SYMMETRIC>
-__global__ void __launch_bounds__(kQuantThreads, (QuantShape<T, VEC, SYMMETRIC>::kCtas))
+__global__ void __launch_bounds__(kQuantThreads, (QuantShape<VEC>::kCtas))
 quantize_w4_kernel(const T* __restrict__ W, long long ld, int out, int in, uint8_t* __restrict__ codes,
                    __nv_bfloat16* __restrict__ scales, uint8_t* __restrict__ zeros) {
-  constexpr int U = QuantShape<T, VEC, SYMMETRIC>::U;
+  constexpr int U = QuantShape<VEC>::U;
   constexpr int kVecs = sizeof(T) / 2;                   // 16-byte vectors of eight columns
   constexpr int kStrip = 256;
   const int lane = threadIdx.x & 31;
@@ -166,9 +189,15 @@ quantize_w4_kernel(const T* __restrict__ W, long long ld, int out, int in, uint8
       if (scale > 1e-30f && scale < 1e30f) {
         const float half_scale = 0.5f * scale, twice_rcp = __fdividef(2.0f, scale);
         if (!SYMMETRIC) zero = fminf(fmaxf(rint_quotient(-lo, half_scale, twice_rcp), 0.0f), 15.0f);
+        const uint64_t mh2 = pack2(-half_scale, -half_scale), tr2 = pack2(twice_rcp, twice_rcp);
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const uint64_t v = rint_quotient2(pack2(w[j], w[j + 1]), mh2, tr2);
+          q[j] = lo2(v);
+          q[j + 1] = hi2(v);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          q[j] = rint_quotient(w[j], half_scale, twice_rcp);
           // symmetric: max |w| / scale < 7.03, so no code leaves [-7, 7]
           if (!SYMMETRIC) q[j] = fminf(fmaxf(q[j], -zero), 15.0f - zero);
         }
@@ -182,9 +211,10 @@ quantize_w4_kernel(const T* __restrict__ W, long long ld, int out, int in, uint8
       const float base = fmaf(zero, 4369.0f, 8388608.0f);
       uint32_t half[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        half[h] = __float_as_uint(fmaf(fmaf(fmaf(q[4 * h + 3], 16.0f, q[4 * h + 2]), 16.0f, q[4 * h + 1]), 16.0f,
-                                       q[4 * h]) + base);
+      for (int h = 0; h < 2; ++h) {
+        const uint64_t two = fma2(pack2(q[4 * h + 2], q[4 * h + 3]), pack2(256.0f, 256.0f), pack2(q[4 * h], q[4 * h + 1]));
+        half[h] = __float_as_uint(fmaf(hi2(two), 16.0f, lo2(two)) + base);
+      }
       if (live[u]) {
         *reinterpret_cast<uint32_t*>(codes + code_of[u] / 2) = __byte_perm(half[0], half[1], 0x5410);
         if ((lane & (G / 8 - 1)) == 0) {
@@ -605,10 +635,9 @@ static cudaError_t quantize(const T* W, long long ld, int out, int in, uint8_t* 
   const long long strips = (long long)out * ((in + 255) / 256);
   const long long ctas = (strips + kQuantThreads / 32 - 1) / (kQuantThreads / 32);
   const bool symmetric = zeros == nullptr;
-  const int most = 152 * (symmetric ? QuantShape<T, VEC, true>::kCtas : QuantShape<T, VEC, false>::kCtas);
   return launch_pdl(symmetric ? quantize_w4_kernel<T, G, VEC, true> : quantize_w4_kernel<T, G, VEC, false>,
-                    dim3((int)std::min<long long>(ctas, most)), dim3(kQuantThreads), 0, s, W, ld, out, in, codes,
-                    scales, zeros);
+                    dim3((int)std::min<long long>(ctas, 152 * QuantShape<VEC>::kCtas)), dim3(kQuantThreads), 0, s, W,
+                    ld, out, in, codes, scales, zeros);
 }
 template <class T>
 static cudaError_t quantize(const void* W, long long ld, int out, int in, int group, uint8_t* codes,
