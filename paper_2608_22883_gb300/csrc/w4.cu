@@ -23,6 +23,12 @@ __device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
   return r;
 }
 
+__device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b) {        // a NaN is dropped
+  uint32_t r;
+  asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
 // ---------------------------------------------------------------------------
 // Codes, scales and zero points of a matrix
 // ---------------------------------------------------------------------------
@@ -85,7 +91,7 @@ __device__ __forceinline__ uint64_t rint_quotient2(uint64_t w, uint64_t minus_ha
 // Reads W once and writes a seventh (fp32) or a quarter (bf16) of its bytes: bound by
 // memory and by instruction issue about evenly, hence the packed arithmetic (fp32 108 us
 // without).  W [32000, 4096]: fp32 in groups of 32 with zero points 101 us (6.0 TB/s, 88 %
-// of the measured copy), bf16 the same 103, symmetric in groups of 128 81; W [4096, 4096]
+// of the measured copy), bf16 the same 96, symmetric in groups of 128 81; W [4096, 4096]
 // bf16 takes 13 us.  One strip and six CTAs an SM: 115, 122 and 86 us.
 template <bool VEC>
 struct QuantShape {                                      // strips on their way; CTAs an SM
@@ -155,13 +161,19 @@ quantize_w4_kernel(const T* __restrict__ W, long long ld, int out, int in, uint8
 #pragma unroll
       for (int j = 0; j < 8; ++j) w[j] = to_f32(e[j]);
       float hi = 0.0f, lo = 0.0f;
-      if (SYMMETRIC && sizeof(T) == 2) {
+      if (sizeof(T) == 2) {
         // two at a time, a NaN the largest
         const uint32_t v[4] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w};
-        uint32_t m = v[0] & 0x7FFF7FFFu;
+        constexpr uint32_t kKeep = SYMMETRIC ? 0x7FFF7FFFu : ~0u;
+        uint32_t m = v[0] & kKeep, least = v[0];
 #pragma unroll
-        for (int j = 1; j < 4; ++j) m = max_nan_bf16x2(m, v[j] & 0x7FFF7FFFu);
-        hi = max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+        for (int j = 1; j < 4; ++j) {
+          m = max_nan_bf16x2(m, v[j] & kKeep);
+          if (!SYMMETRIC) least = min_bf16x2(least, v[j]);
+        }
+        hi = max_nan(max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u)), 0.0f);
+        if (!SYMMETRIC)
+          lo = fminf(fminf(__uint_as_float(least << 16), __uint_as_float(least & 0xFFFF0000u)), 0.0f);
       } else {
         float odd = 0.0f;                                // w 0: NaN for a NaN, which fmaxf drops (and for an infinity)
 #pragma unroll
