@@ -6,6 +6,7 @@
 //   dz_i = [gradients of the tokens equal to i] - p_i G - g_H p_i (logp_i + H) + g_lse p_i
 // with G the sum of the counted tokens' gradients.
 #include "common.cuh"
+#include "packed.cuh"
 #include "rowmath.cuh"
 #include "tc_ptx.cuh"
 
@@ -128,28 +129,6 @@ __device__ __forceinline__ void join(Sums& a, Sums b) {
   a.S = fmaf(f, lo.S, hi.S);
   a.W = fmaf(f, fmaf(lo.S, d, lo.W), hi.W);
   a.m = m;
-}
-
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-  return (uint64_t)__float_as_uint(hi) << 32 | __float_as_uint(lo);
-}
-__device__ __forceinline__ float lo2(uint64_t v) { return __uint_as_float((uint32_t)v); }
-__device__ __forceinline__ float hi2(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
 }
 
 // A thread's sums over the tokens it has seen (even and odd ones apart), and the

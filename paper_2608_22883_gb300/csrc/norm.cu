@@ -9,6 +9,7 @@
 #include <atomic>
 
 #include "common.cuh"
+#include "packed.cuh"
 
 namespace fovea {
 
@@ -37,7 +38,10 @@ struct Chunk {
       for (int h = 0; h < kVecs; ++h) raw[h] = reinterpret_cast<const uint4*>(p + c0)[h];
     }
   }
-  __device__ __forceinline__ float at(int i) const { return to_f32(reinterpret_cast<const T*>(raw)[i]); }
+  __device__ __forceinline__ uint64_t two(int i) const {                   // columns i and i + 1
+    const T* e = reinterpret_cast<const T*>(raw);
+    return pack2(to_f32(e[i]), to_f32(e[i + 1]));
+  }
 };
 
 // The same of a row anywhere, in three steps, so that the loads of several rows are on
@@ -168,7 +172,11 @@ __device__ __forceinline__ void store_q8(uint8_t* p, int c0, int d, const float 
   if (scale > 1e-30f && scale < 1e30f) {
     const float inv = __fdividef(1.0f, scale);
 #pragma unroll
-    for (int i = 0; i < kChunk; ++i) v[i] = y[i] * inv;
+    for (int i = 0; i < kChunk; i += 2) {
+      const uint64_t two = mul2(pack2(y[i], y[i + 1]), pack2(inv, inv));
+      v[i] = lo2(two);
+      v[i + 1] = hi2(two);
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < kChunk; ++i) v[i] = scale == 0.0f ? 0.0f : y[i] / scale;
@@ -191,13 +199,14 @@ __device__ __forceinline__ void store_q8(uint8_t* p, int c0, int d, const float 
 // its way meanwhile; otherwise rows that are not aligned are read and written through
 // shifted vectors, in 64 registers, which leaves an SM more CTAs to wait with (4096 bf16
 // rows of 5111 with 8 bits by 128: 97 us against 113 in 122 registers; 139 with element
-// stores and a wait for each load; aligned rows of 5120 take 33).
+// stores and a wait for each load).
 //
 // One pass: a row is read once, normalised and written from registers, so memory bounds
-// a long run of rows.  8192 rows of 5120 bf16 with a residual, three outputs and 8 bits
-// in groups of 128: 63.8 us, 5.94 TB/s (88 % of the measured copy); without the next
-// row on its way 78 us.  One row of 4096: 1.8 us on the device, the call's own cost on
-// the host is several times that.
+// a long run of rows, if instructions are few (pairs of columns in packed arithmetic).
+// 8192 rows of 5120 bf16 with a residual, three outputs and 8 bits in groups of 128: 61.6
+// us, 6.15 TB/s (91 % of the measured copy); 63.7 without the packed arithmetic, 78
+// without the next row on its way either.  One row of 4096: 1.8 us on the device, the
+// call's own cost on the host is several times that.
 template <class T, int C, bool VEC, bool RESIDUAL>
 __global__ void __launch_bounds__(512, (VEC ? 0 : 2)) add_rms_norm_kernel(const NormArgs a) {
   __shared__ float red[2][2][16];
@@ -257,15 +266,21 @@ __global__ void __launch_bounds__(512, (VEC ? 0 : 2)) add_rms_norm_kernel(const 
   for (long long row = blockIdx.x; row < a.N; row += gridDim.x, buf ^= 1) {
     if (!VEC) fetch(row);
     float s[C][kChunk];
-    float ss = 0.0f, top = 0.0f;
+    uint64_t squares = 0;
+    float top = 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int i = 0; i < kChunk; ++i) {
-        s[c][i] = RESIDUAL ? x[c].at(i) + r[c].at(i) : x[c].at(i);
-        ss = fmaf(s[c][i], s[c][i], ss);
-        top = max_nan(top, fabsf(s[c][i] * g[c].at(i)));
+      for (int i = 0; i < kChunk; i += 2) {
+        uint64_t v = x[c].two(i);
+        if (RESIDUAL) v = add2(v, r[c].two(i));
+        squares = fma2(v, v, squares);
+        const uint64_t y = mul2(v, g[c].two(i));
+        top = max_nan(max_nan(top, fabsf(lo2(y))), fabsf(hi2(y)));
+        s[c][i] = lo2(v);
+        s[c][i + 1] = hi2(v);
       }
+    float ss = lo2(squares) + hi2(squares);
     if (VEC) fetch(row + gridDim.x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -302,7 +317,11 @@ __global__ void __launch_bounds__(512, (VEC ? 0 : 2)) add_rms_norm_kernel(const 
       if (!RESIDUAL && a.sum != nullptr) store_chunk(static_cast<T*>(a.sum) + row * d, c0, d, s[c], vec);
       float y[kChunk];
 #pragma unroll
-      for (int i = 0; i < kChunk; ++i) y[i] = s[c][i] * rstd * g[c].at(i);
+      for (int i = 0; i < kChunk; i += 2) {
+        const uint64_t v = mul2(mul2(pack2(s[c][i], s[c][i + 1]), pack2(rstd, rstd)), g[c].two(i));
+        y[i] = lo2(v);
+        y[i + 1] = hi2(v);
+      }
       if (a.out != nullptr) store_chunk(static_cast<T*>(a.out) + row * d, c0, d, y, vec);
       if (a.q8 == nullptr) continue;
       float scale = row_scale;

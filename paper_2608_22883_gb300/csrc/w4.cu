@@ -6,6 +6,7 @@
 #include <atomic>
 
 #include "common.cuh"
+#include "packed.cuh"
 #include "w4_x.cuh"
 
 namespace fovea {
@@ -61,21 +62,6 @@ __device__ __forceinline__ float rint_quotient(float w, float half_scale, float 
 }
 
 // Two of them in packed instructions, the same operations.
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-  return (uint64_t)__float_as_uint(hi) << 32 | __float_as_uint(lo);
-}
-__device__ __forceinline__ float lo2(uint64_t v) { return __uint_as_float((uint32_t)v); }
-__device__ __forceinline__ float hi2(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 __device__ __forceinline__ uint64_t rint_quotient2(uint64_t w, uint64_t minus_half_scale, uint64_t twice_rcp) {
   constexpr float kMagic = 12582912.0f;
   const uint64_t up = pack2(kMagic, kMagic), down = pack2(-kMagic, -kMagic), half = pack2(0.5f, 0.5f);
