@@ -150,15 +150,16 @@ struct Seen {
     const float z = value_of(__reduce_max_sync(0xffffffffu, order_of(cm))) * scale;
     if (fabsf(z) < INFINITY) m = z;
   }
-  // One chunk's logits; a NaN among them makes the sums NaN.
-  template <int NV>
+  // One chunk's logits; a NaN among them makes the sums NaN.  ASCENDING: no later chunk
+  // was taken before this one (of equal logits the lowest chunk's is kept).
+  template <bool ASCENDING = true, int NV>
   __device__ __forceinline__ void take(const float (&v)[NV], int c, float scale) {
     float cm = v[0];
 #pragma unroll
     for (int i = 1; i < NV; ++i) cm = max_nan(cm, v[i]);
     const float zm = cm * scale;
     if (zm == -INFINITY) return;
-    if (cm > top) {
+    if (cm > top || (!ASCENDING && cm == top && c < chunk)) {
       top = cm;
       chunk = c;
     }
@@ -283,7 +284,7 @@ token_logprobs_kernel(const ScoreArgs a) {
     if (tid < 2 && ragged(tid) >= 0) {
       float v[NV];
       row.load(ragged(tid), v);
-      seen.take(v, ragged(tid), scale);
+      seen.take<false>(v, ragged(tid), scale);             // thread 0's comes before its whole ones
     }
   }
   Sums s = seen.sums();

@@ -1,0 +1,67 @@
+"""Edges of the drafter-exit operators that a plain comparison on random rows
+does not reach: ties and non-numbers in the selection, rows and tokens without
+probability in the gradient, exponents, zero points, the error word and devices."""
+
+import math
+
+import pytest
+import torch
+
+from test_exit_operators_gpu import BF16, FP32, U, check_product, fovea, gen, make_w4, pack_bits, within  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def at_offset(x, offset):
+    """x with its first element `offset` elements behind a 16-byte boundary."""
+    buf = torch.empty(offset + x.numel(), device="cuda", dtype=x.dtype)
+    assert buf.data_ptr() % 16 == 0
+    out = buf[offset:].view(x.shape)
+    out.copy_(x)
+    return out
+
+
+def expected_top(x, k):
+    # NaN above +inf, the smaller token first on ties (x: no zeros of both signs)
+    return torch.sort(x.float(), dim=1, descending=True, stable=True).indices[:, :k]
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("offset", range(8))
+def test_ties_with_the_first_chunk_of_a_row_off_the_boundary(fovea, dtype, offset):
+    """The largest logit stands in a row's first, ragged chunk, again in a later chunk of
+    the thread that takes it (the first whole one, or 256 or 512 further on), and in
+    another group of lanes."""
+    per = 16 // dtype.itemsize
+    v = 20000 if dtype == BF16 else 10000
+    rows = []
+    for first in (0, 1, per - 1, per):
+        for later in (per, per * 257, per * 513 - 1):
+            for other in (per * 5, per * 40 + 3):
+                rows.append({first, later, other})
+                rows.append({first, later})
+    x = torch.randn((len(rows), v), generator=gen(offset), device="cuda").clamp(-3, 3)
+    for r, at in enumerate(rows):
+        x[r, list(at)] = 4.0
+    x = at_offset(x.to(dtype), offset)
+    keep = torch.ones(x.shape, device="cuda", dtype=torch.bool)
+    for k in (1, 2, 6):
+        for allowed in (None, pack_bits(keep)):
+            got = fovea.token_logprobs(x, None, k, allowed=allowed)
+            assert torch.equal(got["top_idx"].long(), expected_top(x, k)), k
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("v", [5000, 4999, 32001, 70001])
+def test_ties_of_many_tokens_in_odd_vocabularies(fovea, dtype, v):
+    # dense rows of an odd width start at every offset; few rows are cut over a cluster
+    g = gen(v)
+    for n in (2, 300):
+        x = torch.zeros((n, v), device="cuda")
+        at = torch.randint(0, v, (n, 40), generator=g, device="cuda")
+        at[:, 0] = torch.arange(n, device="cuda") % 3
+        x.scatter_(1, at, 1.0)
+        x = x.to(dtype)
+        for k in (1, 6, 32):
+            got = fovea.token_logprobs(x, None, k)
+            assert torch.equal(got["top_idx"].long(), expected_top(x, k)), (n, k)
