@@ -405,7 +405,7 @@ token_logprobs_kernel(const ScoreArgs a) {
         for (int gr = warp; gr < kGroups; gr += kWarps) {
           if (!odd && sh.upper[gr] < threshold) continue;
           each_key(gr, [&](unsigned long long key) {
-            if (key < last && key > mine) mine = key;
+            if ((r == 0 || key < last) && key > mine) mine = key;      // (a NaN at token 0 has the largest key)
           });
         }
 #pragma unroll

@@ -65,3 +65,22 @@ def test_ties_of_many_tokens_in_odd_vocabularies(fovea, dtype, v):
         for k in (1, 6, 32):
             got = fovea.token_logprobs(x, None, k)
             assert torch.equal(got["top_idx"].long(), expected_top(x, k)), (n, k)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("v,offset", [(1, 0), (3000, 0), (3000, 1), (100001, 3)])
+def test_a_nan_at_the_first_token_is_an_alternative(fovea, dtype, v, offset):
+    places = [{0: math.nan}, {0: math.nan, v // 2: math.nan}, {0: math.nan, v - 1: math.nan, v // 3: math.inf},
+              {0: math.inf}, {v - 1: math.nan}]
+    x = torch.randn((len(places), v), generator=gen(v), device="cuda")
+    x += torch.arange(v, device="cuda") * 1e-4
+    for r, place in enumerate(places):
+        for at, value in place.items():
+            x[r, at] = value
+    x = at_offset(x.to(dtype), offset)
+    for k in (1, 2, 6):
+        got = fovea.token_logprobs(x, None, k)
+        want = expected_top(x, k)
+        assert torch.equal(got["top_idx"][:, :want.shape[1]].long(), want), k
+        assert torch.isnan(got["top_logprobs"][:, :want.shape[1]]).all()
+        assert (got["top_idx"][:, want.shape[1]:] == -1).all()
