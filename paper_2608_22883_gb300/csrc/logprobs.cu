@@ -32,16 +32,17 @@ __device__ __forceinline__ float ex2(float x) {       // 2^x, subnormal results 
   return r;
 }
 
-// Order of logits as signed integers: every NaN above +inf, both zeros equal.
+// Order of logits as signed integers: every NaN above +inf (and not the largest integer:
+// no key below is ~0), both zeros equal.
 __device__ __forceinline__ int32_t order_of(float x) {
-  if (x != x) return 0x7FFFFFFF;
+  if (x != x) return 0x7FFFFFFE;
   const int32_t b = __float_as_int(x + 0.0f);
   return b < 0 ? b ^ 0x7FFFFFFF : b;
 }
 __device__ __forceinline__ float value_of(int32_t o) { return __int_as_float(o < 0 ? o ^ 0x7FFFFFFF : o); }
 constexpr int32_t kOrderNegInf = (int32_t)0x807FFFFF;     // order_of(-inf)
 
-// A token's key: larger logits first, then the lower token; never 0.
+// A token's key: larger logits first, then the lower token; neither 0 nor ~0.
 __device__ __forceinline__ unsigned long long key_of(int32_t order, int token) {
   return (unsigned long long)((uint32_t)order ^ 0x80000000u) << 32 | (uint32_t)~token;
 }
@@ -405,7 +406,7 @@ token_logprobs_kernel(const ScoreArgs a) {
         for (int gr = warp; gr < kGroups; gr += kWarps) {
           if (!odd && sh.upper[gr] < threshold) continue;
           each_key(gr, [&](unsigned long long key) {
-            if ((r == 0 || key < last) && key > mine) mine = key;      // (a NaN at token 0 has the largest key)
+            if (key < last && key > mine) mine = key;
           });
         }
 #pragma unroll
