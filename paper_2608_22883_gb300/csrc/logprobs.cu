@@ -530,8 +530,9 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
   __syncthreads();
   float G = 0.0f;
   for (int j = 0; j < E; ++j) G += grad[j];
-  const float gH = a.grad_entropy != nullptr ? a.grad_entropy[n] : 0.0f;
-  const float gl = a.grad_lse != nullptr ? a.grad_lse[n] : 0.0f;
+  // a row without tokens has lse -inf: an infinity may come back, and counts for nothing
+  const float gH = a.grad_entropy != nullptr && !empty ? a.grad_entropy[n] : 0.0f;
+  const float gl = a.grad_lse != nullptr && !empty ? a.grad_lse[n] : 0.0f;
   const float A = gl - G - gH * a.entropy[n];
 
   const int per = (row.chunks + gridDim.x - 1) / gridDim.x;

@@ -84,3 +84,28 @@ def test_a_nan_at_the_first_token_is_an_alternative(fovea, dtype, v, offset):
         assert torch.equal(got["top_idx"][:, :want.shape[1]].long(), want), k
         assert torch.isnan(got["top_logprobs"][:, :want.shape[1]]).all()
         assert (got["top_idx"][:, want.shape[1]:] == -1).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("v", [1, 40, 3001])
+def test_gradient_of_a_row_without_tokens_is_zero_whatever_comes_back(fovea, dtype, v):
+    """lse is -inf there, so that a loss of it, squared for instance, sends an infinity
+    back; rows with tokens beside it keep theirs."""
+    x = torch.randn((4, v), generator=gen(v), device="cuda").to(dtype)
+    x[0] = -math.inf
+    keep = torch.ones((4, v), device="cuda", dtype=torch.bool)
+    keep[1] = False
+    tokens = torch.zeros((4, 1), device="cuda", dtype=torch.int32)
+    allowed = pack_bits(keep)
+    f = fovea.token_logprobs(x, tokens, 1, allowed=allowed)
+    assert (f["lse"][:2] == -math.inf).all() and torch.isfinite(f["lse"][2:]).all()
+    one = torch.ones(4, device="cuda")
+    for value in (-math.inf, math.inf, math.nan, 1.0):
+        back = one.clone()
+        back[:2] = value
+        for gH, gz in ((back, None), (None, back), (back, back), (one, 2 * f["lse"])):
+            d = fovea.token_logprobs_grad(x, f["stats"], f["entropy"], tokens=tokens, grad_logprobs=back[:, None],
+                                          top_idx=f["top_idx"], grad_top=back[:, None], grad_entropy=gH, grad_lse=gz,
+                                          allowed=allowed)
+            assert (d[:2] == 0).all()
+            assert torch.isfinite(d[2:]).all()
