@@ -534,6 +534,9 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
   const float gH = a.grad_entropy != nullptr && !empty ? a.grad_entropy[n] : 0.0f;
   const float gl = a.grad_lse != nullptr && !empty ? a.grad_lse[n] : 0.0f;
   const float A = gl - G - gH * a.entropy[n];
+  // where any of these is not finite, 0 times it is no 0 for the tokens that are not allowed
+  const bool odd = MASKED && !(fabsf(A) < INFINITY && fabsf(gH) < INFINITY && fabsf(m) < INFINITY &&
+                               fabsf(log_sum) < INFINITY);
 
   const int per = (row.chunks + gridDim.x - 1) / gridDim.x;
   const int c_lo = min((int)blockIdx.x * per, row.chunks), c_hi = min(c_lo + per, row.chunks);
@@ -550,6 +553,11 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
       v[i] = lo2(g);
       v[i + 1] = hi2(g);
     }
+  };
+  auto clear = [&](uint32_t keep, float (&v)[NV]) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (!(keep >> i & 1u)) v[i] = 0.0f;
   };
   auto store = [&](int c, const float (&v)[NV]) {          // one value at a time
     const int i0 = row.first(c);
@@ -585,6 +593,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
         ln_unpack<T>(raw[u], v);
         if (MASKED) row.mask(keep[u], v);
         gradient(v);
+        if (odd) clear(keep[u], v);
         store_whole(c + u * kThreads, v);
       }
     }
@@ -604,6 +613,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
         ln_unpack<T>(raw[u], v);
         if (MASKED) row.mask(keep[u], v);
         gradient(v);
+        if (odd) clear(keep[u], v);
         store_whole(c + u * kThreads, v);
       }
     }
@@ -612,6 +622,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
       float v[NV];
       row.load(e, v);
       gradient(v);
+      if (odd) clear(row.bits(e), v);
       store(e, v);
     }
   }

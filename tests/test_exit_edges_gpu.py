@@ -109,3 +109,26 @@ def test_gradient_of_a_row_without_tokens_is_zero_whatever_comes_back(fovea, dty
                                           allowed=allowed)
             assert (d[:2] == 0).all()
             assert torch.isfinite(d[2:]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("n,v", [(6, 40), (6, 3001), (3, 50000)])
+def test_gradient_of_tokens_that_are_not_allowed_is_zero_in_any_row(fovea, dtype, n, v):
+    g = gen(v)
+    keep = torch.rand((n, v), generator=g, device="cuda") < 0.5
+    keep[:, 1] = True
+    x = torch.randn((n, v), generator=g, device="cuda").to(dtype)
+    x[0, 1] = math.nan                                     # every probability of the row is NaN
+    x[1, 1] = math.inf
+    tokens = torch.ones((n, 1), device="cuda", dtype=torch.int32)
+    tokens[2] = v                                          # no such token
+    allowed = pack_bits(keep)
+    f = fovea.token_logprobs(x, tokens, 2, allowed=allowed)
+    d = fovea.token_logprobs_grad(x, f["stats"], f["entropy"], tokens=tokens, top_idx=f["top_idx"],
+                                  grad_logprobs=torch.ones((n, 1), device="cuda"),
+                                  grad_top=torch.ones((n, 2), device="cuda"),
+                                  grad_entropy=torch.ones(n, device="cuda"), allowed=allowed)
+    assert (d[~keep] == 0).all()
+    for r in range(3):
+        assert torch.isnan(d[r][keep[r]]).all()
+    assert torch.isfinite(d[3:]).all()
