@@ -534,9 +534,6 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
   const float gH = a.grad_entropy != nullptr && !empty ? a.grad_entropy[n] : 0.0f;
   const float gl = a.grad_lse != nullptr && !empty ? a.grad_lse[n] : 0.0f;
   const float A = gl - G - gH * a.entropy[n];
-  // where any of these is not finite, 0 times it is no 0 for the tokens that are not allowed
-  const bool odd = MASKED && !(fabsf(A) < INFINITY && fabsf(gH) < INFINITY && fabsf(m) < INFINITY &&
-                               fabsf(log_sum) < INFINITY);
 
   const int per = (row.chunks + gridDim.x - 1) / gridDim.x;
   const int c_lo = min((int)blockIdx.x * per, row.chunks), c_hi = min(c_lo + per, row.chunks);
@@ -553,11 +550,6 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
       v[i] = lo2(g);
       v[i + 1] = hi2(g);
     }
-  };
-  auto clear = [&](uint32_t keep, float (&v)[NV]) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (!(keep >> i & 1u)) v[i] = 0.0f;
   };
   auto store = [&](int c, const float (&v)[NV]) {          // one value at a time
     const int i0 = row.first(c);
@@ -593,7 +585,6 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
         ln_unpack<T>(raw[u], v);
         if (MASKED) row.mask(keep[u], v);
         gradient(v);
-        if (odd) clear(keep[u], v);
         store_whole(c + u * kThreads, v);
       }
     }
@@ -613,7 +604,6 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
         ln_unpack<T>(raw[u], v);
         if (MASKED) row.mask(keep[u], v);
         gradient(v);
-        if (odd) clear(keep[u], v);
         store_whole(c + u * kThreads, v);
       }
     }
@@ -622,11 +612,19 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
       float v[NV];
       row.load(e, v);
       gradient(v);
-      if (odd) clear(row.bits(e), v);
       store(e, v);
     }
   }
   __syncthreads();
+  // where any of these is not finite, p = 0 times it was no 0 for the tokens that are not
+  // allowed (a select for each in the loops above: 58.5 us for 51.7, 2048 masked bf16 rows)
+  if (MASKED && !(fabsf(A) < INFINITY && fabsf(gH) < INFINITY && fabsf(m) < INFINITY && fabsf(log_sum) < INFINITY))
+    for (int c = c_lo + tid; c < c_hi; c += kThreads) {
+      const int i0 = row.first(c);
+      const uint32_t keep = row.bits(c);
+      for (int i = 0; i < NV; ++i)
+        if (i0 + i >= 0 && i0 + i < a.V && !(keep >> i & 1u)) out[i0 + i] = from_f32<T>(0.0f);
+    }
   for (int j = tid; j < E; j += kThreads) {
     const int k = tok[j];
     if (k < max(row.first(c_lo), 0) || k >= min(row.first(c_hi), a.V)) continue;

@@ -1,4 +1,5 @@
-// Two fp32 operations in one instruction, each rounded as the single one is.
+// Two fp32 operations in one instruction, each rounded as the single one is, but for a
+// product that goes into a sum (mul2).
 #pragma once
 #include <cstdint>
 
@@ -15,6 +16,9 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
   return d;
 }
+// Where an add2 takes the product the assembler makes one operation of both, and the
+// product is not rounded; product2 is (-0 comes out as +0).
+__device__ __forceinline__ uint64_t product2(uint64_t a, uint64_t b) { return fma2(a, b, 0); }
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
