@@ -32,6 +32,15 @@ __device__ __forceinline__ float ex2(float x) {       // 2^x, subnormal results 
   return r;
 }
 
+// z of a logit: the product rounded once, also where a difference follows that the compiler
+// would fuse with it (z - max of the largest is 0 then, and no log probability above 0).
+__device__ __forceinline__ float z_of(float x, float scale) { return __fmul_rn(x, scale); }
+template <bool SCALED>
+__device__ __forceinline__ uint64_t z_of2(float x0, float x1, float scale) {
+  const uint64_t x = pack2(x0, x1);
+  return SCALED ? product2(x, pack2(scale, scale)) : x;
+}
+
 // Order of logits as signed integers: every NaN above +inf (and not the largest integer:
 // no key below is ~0), both zeros equal.
 __device__ __forceinline__ int32_t order_of(float x) {
@@ -148,17 +157,17 @@ struct Seen {
     float cm = v[0];
 #pragma unroll
     for (int i = 1; i < NV; ++i) cm = max_nan(cm, v[i]);
-    const float z = value_of(__reduce_max_sync(0xffffffffu, order_of(cm))) * scale;
+    const float z = z_of(value_of(__reduce_max_sync(0xffffffffu, order_of(cm))), scale);
     if (fabsf(z) < INFINITY) m = z;
   }
   // One chunk's logits; a NaN among them makes the sums NaN.  ASCENDING: no later chunk
   // was taken before this one (of equal logits the lowest chunk's is kept).
-  template <bool ASCENDING = true, int NV>
+  template <bool SCALED, bool ASCENDING = true, int NV>
   __device__ __forceinline__ void take(const float (&v)[NV], int c, float scale) {
     float cm = v[0];
 #pragma unroll
     for (int i = 1; i < NV; ++i) cm = max_nan(cm, v[i]);
-    const float zm = cm * scale;
+    const float zm = z_of(cm, scale);
     if (zm == -INFINITY) return;
     if (cm > top || (!ASCENDING && cm == top && c < chunk)) {
       top = cm;
@@ -172,11 +181,10 @@ struct Seen {
       S = pack2(a.S, b.S);
       W = pack2(a.W, b.W);
     }
-    const uint64_t scale2 = pack2(scale, scale), m2 = pack2(-m, -m), log2e2 = pack2(kLog2e, kLog2e);
+    const uint64_t m2 = pack2(-m, -m), log2e2 = pack2(kLog2e, kLog2e);
 #pragma unroll
     for (int i = 0; i < NV; i += 2) {
-      // (rounded product) - m, not one fused operation: the largest z gives 0 exactly
-      const uint64_t d = add2(mul2(pack2(v[i], v[i + 1]), scale2), m2);
+      const uint64_t d = add2(z_of2<SCALED>(v[i], v[i + 1], scale), m2);
       // -inf: e^{-200} is 0 and so is its term of W
       const uint64_t dz = pack2(max_nan(lo2(d), -200.0f), max_nan(hi2(d), -200.0f));
       const uint64_t x = mul2(dz, log2e2);
@@ -215,7 +223,7 @@ struct Shared {
 //
 // Six CTAs an SM are worth 40 registers to unmasked bf16 rows (72.6 to 69.6 us) and not to
 // the others (masked bf16 a fifth slower, fp32 2 %).
-template <class T, bool MASKED>
+template <class T, bool MASKED, bool SCALED>
 __global__ void __launch_bounds__(kThreads, (sizeof(T) == 2 && !MASKED ? 6 : 0))
 token_logprobs_kernel(const ScoreArgs a) {
   constexpr int NV = Row<T>::NV;
@@ -226,7 +234,7 @@ token_logprobs_kernel(const ScoreArgs a) {
   pdl_wait();
   pdl_trigger();
   const Row<T> row(a.logits, a.ld, n, a.V, a.allowed, a.allowed_ld);
-  const float scale = a.row_scale != nullptr ? a.row_scale[n] : 1.0f;
+  const float scale = SCALED ? a.row_scale[n] : 1.0f;
   const int per = (row.chunks + ctas - 1) / ctas;
   const int c_lo = min(rank * per, row.chunks), c_hi = min(c_lo + per, row.chunks);
 
@@ -261,7 +269,7 @@ token_logprobs_kernel(const ScoreArgs a) {
           seen.seed(v, scale);
           seeded = true;
         }
-        seen.take(v, c + u * kThreads, scale);
+        seen.take<SCALED>(v, c + u * kThreads, scale);
       }
     }
     if (c < hi) {                                          // the last round, cut short
@@ -279,20 +287,20 @@ token_logprobs_kernel(const ScoreArgs a) {
         float v[NV];
         ln_unpack<T>(raw[u], v);
         if (MASKED) row.mask(keep[u], v);
-        seen.take(v, c + u * kThreads, scale);
+        seen.take<SCALED>(v, c + u * kThreads, scale);
       }
     }
     if (tid < 2 && ragged(tid) >= 0) {
       float v[NV];
       row.load(ragged(tid), v);
-      seen.take<false>(v, ragged(tid), scale);             // thread 0's comes before its whole ones
+      seen.take<SCALED, false>(v, ragged(tid), scale);             // thread 0's comes before its whole ones
     }
   }
   Sums s = seen.sums();
   int32_t top = order_of(seen.top);
   const int top_chunk = seen.chunk;
   // the largest z itself (the reference is one of the row's)
-  if (top != kOrderNegInf && seen.top * scale > s.m) rebase(s, seen.top * scale);
+  if (top != kOrderNegInf && z_of(seen.top, scale) > s.m) rebase(s, z_of(seen.top, scale));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     Sums b;
@@ -367,14 +375,14 @@ token_logprobs_kernel(const ScoreArgs a) {
           const int first = row.first(c + u * 8 * kThreads);
 #pragma unroll
           for (int i = 0; i < NV; ++i)
-            if (!(v[i] < least) && v[i] * scale != -INFINITY) f(key_of(order_of(v[i]), first + i));
+            if (!(v[i] < least) && z_of(v[i], scale) != -INFINITY) f(key_of(order_of(v[i]), first + i));
         }
       }
       if (gr == 0 && lane < 2 && ragged(lane) >= 0) {
         float v[NV];
         row.load(ragged(lane), v);
         for (int i = 0; i < NV; ++i)
-          if (v[i] * scale != -INFINITY) f(key_of(order_of(v[i]), row.first(ragged(lane)) + i));
+          if (z_of(v[i], scale) != -INFINITY) f(key_of(order_of(v[i]), row.first(ragged(lane)) + i));
       }
     };
     uint32_t mine = 0;                                     // of this warp's groups, those to search
@@ -474,13 +482,13 @@ token_logprobs_kernel(const ScoreArgs a) {
   for (int j = tid; j < a.T; j += kThreads) {
     const int tok = a.tokens[n * a.T + j];
     float lp = 0.0f;
-    if (tok >= 0) lp = tok < a.V ? (row.at(tok) * scale - m) - log_sum : __int_as_float(0x7FC00000);
+    if (tok >= 0) lp = tok < a.V ? (z_of(row.at(tok), scale) - m) - log_sum : __int_as_float(0x7FC00000);
     a.logprobs[n * a.T + j] = lp;
   }
   for (int j = tid; j < a.k; j += kThreads) {
     const unsigned long long key = best[j];
     a.top_idx[n * a.k + j] = key != 0ull ? token_of(key) : -1;
-    a.top_logprobs[n * a.k + j] = key != 0ull ? (value_of(order_in(key)) * scale - m) - log_sum : -INFINITY;
+    a.top_logprobs[n * a.k + j] = key != 0ull ? (z_of(value_of(order_in(key)), scale) - m) - log_sum : -INFINITY;
   }
 }
 
@@ -489,7 +497,7 @@ token_logprobs_kernel(const ScoreArgs a) {
 // written again after it, by the CTA whose range they lie in.  Bound by memory: 4096
 // rows of 32000 bf16 82 us, 6.4 TB/s (94 % of the measured copy); 40 masked fp32 rows
 // 7.0 us.
-template <class T, bool MASKED>
+template <class T, bool MASKED, bool SCALED>
 __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const ScoreGradArgs a) {
   constexpr int NV = Row<T>::NV;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -504,7 +512,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
   const Row<T> row(a.logits, a.ld, n, a.V, a.allowed, a.allowed_ld);
   T* out = static_cast<T*>(a.dlogits) + n * a.V;
   const bool out_vec = ((reinterpret_cast<uintptr_t>(out) & 15u) / sizeof(T)) == (unsigned)row.shift;
-  const float scale = a.row_scale != nullptr ? a.row_scale[n] : 1.0f;
+  const float scale = SCALED ? a.row_scale[n] : 1.0f;
   const bool empty = a.stats[2 * n] == -INFINITY;
   const float m = empty ? 0.0f : a.stats[2 * n], log_sum = empty ? 0.0f : a.stats[2 * n + 1];
   for (int j = tid; j < E; j += kThreads) {
@@ -518,7 +526,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
       g = 0.0f;
     } else {
       x = row.at(k);
-      if (x * scale == -INFINITY) {                    // no probability, no gradient
+      if (z_of(x, scale) == -INFINITY) {                // no probability, no gradient
         k = -1;
         g = 0.0f;
       }
@@ -542,11 +550,12 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
                    log2e2 = pack2(kLog2e, kLog2e), gH2 = pack2(-gH, -gH), A2 = pack2(A, A);
 #pragma unroll
     for (int i = 0; i < NV; i += 2) {
-      const uint64_t d = add2(add2(mul2(pack2(v[i], v[i + 1]), scale2), m2), s2);
+      const uint64_t d = add2(add2(z_of2<SCALED>(v[i], v[i + 1], scale), m2), s2);
       // -inf: p is 0, and so is p logp
       const uint64_t lp = pack2(max_nan(lo2(d), -1e4f), max_nan(hi2(d), -1e4f));
       const uint64_t x = mul2(lp, log2e2);
-      const uint64_t g = mul2(mul2(pack2(ex2(lo2(x)), ex2(hi2(x))), fma2(gH2, lp, A2)), scale2);
+      uint64_t g = mul2(pack2(ex2(lo2(x)), ex2(hi2(x))), fma2(gH2, lp, A2));
+      if (SCALED) g = mul2(g, scale2);
       v[i] = lo2(g);
       v[i + 1] = hi2(g);
     }
@@ -637,7 +646,7 @@ __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const Sco
         g += grad[i];
       }
     if (again) continue;
-    const float lp = max_nan((logit[j] * scale - m) - log_sum, -1e4f);
+    const float lp = max_nan((z_of(logit[j], scale) - m) - log_sum, -1e4f);
     out[k] = from_f32<T>(fmaf(ex2(lp * kLog2e), fmaf(-gH, lp, A), g) * scale);
   }
 }
@@ -680,6 +689,21 @@ int grad_split(long long N, int V, int size) {
   return c;
 }
 
+// The kernels of a call: a mask and temperatures each have code of their own (a
+// multiplication by 1 of every logit: 72.6 us for 69.4 in training).
+template <class T>
+auto scores_of(const ScoreArgs& a) {
+  if (a.allowed != nullptr)
+    return a.row_scale != nullptr ? token_logprobs_kernel<T, true, true> : token_logprobs_kernel<T, true, false>;
+  return a.row_scale != nullptr ? token_logprobs_kernel<T, false, true> : token_logprobs_kernel<T, false, false>;
+}
+template <class T>
+auto grad_of(const ScoreGradArgs& a) {
+  if (a.allowed != nullptr)
+    return a.row_scale != nullptr ? token_logprobs_grad_kernel<T, true, true> : token_logprobs_grad_kernel<T, true, false>;
+  return a.row_scale != nullptr ? token_logprobs_grad_kernel<T, false, true> : token_logprobs_grad_kernel<T, false, false>;
+}
+
 constexpr long long kRowsPerLaunch = 65535;        // the grid's y
 
 }  // namespace
@@ -699,13 +723,8 @@ cudaError_t launch_token_logprobs(int dtype, const ScoreArgs& all, cudaStream_t 
     a.entropy += n0;
     const int split = score_split(a.N, a.V, size);
     const dim3 grid(split, (unsigned)a.N);
-    const bool masked = a.allowed != nullptr;
-    const cudaError_t e =
-        dtype == FOVEA_BF16
-            ? launch_cluster(masked ? token_logprobs_kernel<__nv_bfloat16, true> : token_logprobs_kernel<__nv_bfloat16, false>,
-                             grid, split, s, a)
-            : launch_cluster(masked ? token_logprobs_kernel<float, true> : token_logprobs_kernel<float, false>, grid,
-                             split, s, a);
+    const cudaError_t e = launch_cluster(dtype == FOVEA_BF16 ? scores_of<__nv_bfloat16>(a) : scores_of<float>(a),
+                                         grid, split, s, a);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -731,13 +750,8 @@ cudaError_t launch_token_logprobs_grad(int dtype, const ScoreGradArgs& all, cuda
     const int split = a.dlogits == a.logits ? 1 : grad_split(a.N, a.V, size);
     const dim3 grid(split, (unsigned)a.N);
     const size_t smem = (size_t)(a.T + a.k) * 12;
-    const bool masked = a.allowed != nullptr;
-    const cudaError_t e =
-        dtype == FOVEA_BF16
-            ? launch_pdl(masked ? token_logprobs_grad_kernel<__nv_bfloat16, true> : token_logprobs_grad_kernel<__nv_bfloat16, false>,
-                         grid, dim3(kThreads), smem, s, a)
-            : launch_pdl(masked ? token_logprobs_grad_kernel<float, true> : token_logprobs_grad_kernel<float, false>,
-                         grid, dim3(kThreads), smem, s, a);
+    const cudaError_t e = launch_pdl(dtype == FOVEA_BF16 ? grad_of<__nv_bfloat16>(a) : grad_of<float>(a), grid,
+                                     dim3(kThreads), smem, s, a);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;

@@ -132,3 +132,42 @@ def test_gradient_of_tokens_that_are_not_allowed_is_zero_in_any_row(fovea, dtype
     for r in range(3):
         assert torch.isnan(d[r][keep[r]]).all()
     assert torch.isfinite(d[3:]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("v", [40, 3001, 100003])
+def test_no_log_probability_is_above_zero_under_a_temperature(fovea, dtype, v):
+    """z is the product of logit and temperature rounded once, wherever it stands: the
+    largest one's log probability is minus the log sum exactly, which is 0 or more."""
+    g = gen(v)
+    n = 200
+    x = torch.randn((n, v), generator=g, device="cuda")
+    x[:, v // 3] = 10 + 20 * torch.rand(n, generator=g, device="cuda")
+    x = x.to(dtype)
+    t = torch.empty(n, device="cuda").uniform_(0.3, 3.0, generator=g)
+    tokens = torch.full((n, 1), v // 3, device="cuda", dtype=torch.int32)
+    got = fovea.token_logprobs(x, tokens, 2, row_scale=t)
+    assert (got["top_idx"][:, 0] == v // 3).all()
+    assert torch.equal(got["stats"][:, 0], x[:, v // 3].float() * t)
+    assert (got["stats"][:, 1] >= 0).all()
+    assert torch.equal(got["top_logprobs"][:, 0], 0 - got["stats"][:, 1])
+    assert torch.equal(got["logprobs"][:, 0], 0 - got["stats"][:, 1])
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_a_token_with_a_gradient_of_zero_changes_no_bit(fovea, dtype):
+    # its gradient is written again by another piece of code, with the same operations
+    g = gen(17)
+    n, v = 40, 3001
+    x = (5 * torch.randn((n, v), generator=g, device="cuda")).to(dtype)
+    t = torch.empty(n, device="cuda").uniform_(0.3, 3.0, generator=g)
+    tokens = torch.randint(0, v, (n, 500), generator=g, device="cuda", dtype=torch.int32)
+    f = fovea.token_logprobs(x, tokens, 6, row_scale=t)
+    assert (f["logprobs"] <= 0).all()
+    back = dict(grad_entropy=torch.randn(n, generator=g, device="cuda"),
+                grad_lse=torch.randn(n, generator=g, device="cuda"), row_scale=t)
+    want = fovea.token_logprobs_grad(x, f["stats"], f["entropy"], **back)
+    got = fovea.token_logprobs_grad(x, f["stats"], f["entropy"], tokens=tokens, top_idx=f["top_idx"],
+                                    grad_logprobs=torch.zeros((n, 500), device="cuda"),
+                                    grad_top=torch.zeros((n, 6), device="cuda"), **back)
+    assert torch.equal(got, want)
