@@ -171,3 +171,23 @@ def test_a_token_with_a_gradient_of_zero_changes_no_bit(fovea, dtype):
                                     grad_logprobs=torch.zeros((n, 500), device="cuda"),
                                     grad_top=torch.zeros((n, 6), device="cuda"), **back)
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("lowest", [-4.0, -20.0, -80.0])
+def test_gradient_keeps_the_bits_of_small_probabilities(fovea, lowest):
+    """With a largest z and a log sum of 0 the logits are the log probabilities, exactly:
+    grad_lse gives p = e^logit.  Its exponential is good to 2^-22, and three roundings
+    follow: 7 u, and one for what the exponent's own remainder loses."""
+    g = gen(7)
+    n, v = 4, 50000
+    x = lowest * torch.rand((n, v), generator=g, device="cuda")
+    tokens = torch.randint(0, v, (n, 500), generator=g, device="cuda", dtype=torch.int32)
+    stats, zero = torch.zeros((n, 2), device="cuda"), torch.zeros(n, device="cuda")
+    one = torch.ones(n, device="cuda")
+    want = x.double().exp()
+    got = fovea.token_logprobs_grad(x, stats, zero, grad_lse=one)
+    within(got, want, 8 * U * want)
+    # tokens with an entry of their own are computed again
+    got = fovea.token_logprobs_grad(x, stats, zero, tokens=tokens, grad_logprobs=torch.zeros((n, 500), device="cuda"),
+                                    grad_lse=one)
+    within(got, want, 8 * U * want)
