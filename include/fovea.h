@@ -382,7 +382,8 @@ FOVEA_API fovea_status fovea_quantize_w4(const void* W, int64_t ld, int out_feat
 /*
  * y[n, o] = sum_k x[n, k] (code[o, k] - zero[o, k / group]) scale[o, k / group]
  * (+ bias[o]) for a few rows of x (a draft tree's states): weights as
- * fovea_quantize_w4 lays them out (codes 16-byte aligned; zeros NULL: 8).
+ * fovea_quantize_w4 lays them out (codes 16-byte aligned; zeros NULL: 8; a zero
+ * point is 0 to 127, the low seven bits of its byte).
  *   x       [N, in_features] x_dtype: FOVEA_BF16, FOVEA_FP32, or FOVEA_E4M3 with
  *   x_scale [N, groups] fp32 for x_group = group, or [N] for x_group = 0 (as
  *           fovea_add_rms_norm writes q8 and q8_scale); NULL for the others

@@ -390,7 +390,8 @@ cudaError_t launch_add_rms_norm(int dtype, NormArgs a, cudaStream_t s);
 
 // Weights in 4 bits (w4.cu): codes [out, in / 2], two a byte with the even
 // column in the low half, scales [out, groups] bf16, zero points [out, groups]
-// (null: 8 everywhere), groups = ceil(in / group); w = (code - zero) * scale.
+// (null: 8 everywhere; 0 to 127, the low seven bits of the byte: 128 + zero is exact in
+// bf16), groups = ceil(in / group); w = (code - zero) * scale.
 struct W4 {
   const uint8_t* codes; const __nv_bfloat16* scales; const uint8_t* zeros;
   int out, in, group;

@@ -360,7 +360,7 @@ struct Quad {
     return __uint_as_float(i & 1 ? s[i / 2] & 0xFFFF0000u : s[i / 2] << 16);
   }
   __device__ __forceinline__ uint32_t zero2(int i) const {     // 128 + z, twice
-    return 0x43004300u | ((z[i / 4] >> (8 * (i & 3))) & 15u) * 0x10001u;
+    return 0x43004300u | ((z[i / 4] >> (8 * (i & 3))) & 127u) * 0x10001u;
   }
 };
 

@@ -437,7 +437,7 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const int g = (k * kStageK + team * kUnitK + q * 32) / G;
-            if (g < a.groups) z[q] = 0x43004300u | __ldg(zeros + g) * 0x10001u;
+            if (g < a.groups) z[q] = 0x43004300u | (__ldg(zeros + g) & 127u) * 0x10001u;
           }
         }
         if (!warp_wait(&full[st.i], st.parity, abort_flag, a.wait_ns)) {

@@ -536,7 +536,8 @@ def linear_w4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
               out_dtype: torch.dtype = torch.float32, workspace: Optional[torch.Tensor] = None,
               stream=None) -> torch.Tensor:
     """fovea_linear_w4: y [N, out] = x W^T (+ bias) with W in 4 bits (codes,
-    scales, zeros and group as quantize_w4 gives them).  x [N, in] is bf16, fp32,
+    scales, zeros and group as quantize_w4 gives them; a zero point may be up to
+    127, the low seven bits of its byte).  x [N, in] is bf16, fp32,
     or float8_e4m3fn with x_scale [N] or [N, ceil(in / group)] fp32 (add_rms_norm's
     q8 and q8_scale); bias [out] fp32; y is fp32 or bf16 (out_dtype).
     workspace: a uint8 tensor of linear_w4_workspace_size bytes (None: allocated

@@ -191,3 +191,21 @@ def test_gradient_keeps_the_bits_of_small_probabilities(fovea, lowest):
     got = fovea.token_logprobs_grad(x, stats, zero, tokens=tokens, grad_logprobs=torch.zeros((n, 500), device="cuda"),
                                     grad_lse=one)
     within(got, want, 8 * U * want)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("n", [1, 3, 8, 9, 40])            # few rows, and through tensor memory
+def test_zero_points_above_15(fovea, n, group):
+    """A zero point is what its low seven bits say, in every path (formats that store it
+    less one reach 16)."""
+    g = gen(n + group)
+    o, k = 200, 544
+    codes, scales, _ = make_w4(g, o, k, group, False)
+    zeros = torch.randint(0, 128, scales.shape, generator=g, device="cuda", dtype=torch.uint8)
+    zeros[:, 0] = 16
+    zeros[0] = 127
+    for dtype in (BF16, FP32):
+        x = torch.randn((n, k), generator=g, device="cuda").to(dtype)
+        y = fovea.linear_w4(x, codes, scales, zeros, group=group)
+        check_product(y, x, None, codes, scales, zeros, group, None)
+        assert torch.equal(y, fovea.linear_w4(x, codes, scales, zeros + 128, group=group))
