@@ -191,8 +191,8 @@ FOVEA_API fovea_status fovea_workspace_size(const fovea_params* p, const fovea_m
                                             const int32_t* row_offsets, int k_max,
                                             size_t* bytes);
 
-/* Zero the workspace's header (the sticky error word and reserved words;
- * enqueued on `stream`).  One initialisation serves every later call;
+/* Write the workspace's header (the sticky error word and reserved words at
+ * zero, and a mark; enqueued on `stream`).  One initialisation serves every later call;
  * fovea_sync_errors clears the header again after it reports an error. */
 FOVEA_API fovea_status fovea_workspace_init(void* workspace, size_t bytes, void* stream);
 
@@ -390,10 +390,13 @@ FOVEA_API fovea_status fovea_quantize_w4(const void* W, int64_t ld, int out_feat
  *   bias    [out_features] fp32, or NULL
  *   y       [N, out_features] y_dtype: FOVEA_FP32 or FOVEA_BF16
  *   workspace  fovea_linear_w4_workspace_size bytes (256-byte aligned; NULL when
- *           that is 0, as for up to 8 rows, 2 of fp32, of 16384 columns).  It needs no
- *           initialisation and may serve the next call on the stream.  A bounded
- *           device wait that gives up leaves NaN in the y it did not reach and
- *           FOVEA_ERR_TIMEOUT for fovea_sync_errors(workspace).
+ *           that is 0, as for up to 8 rows, 2 of fp32, of 16384 columns).  Any call
+ *           on the stream may use it next.  A bounded device wait that gives up
+ *           leaves NaN in the y it did not reach and FOVEA_ERR_TIMEOUT for
+ *           fovea_sync_errors(workspace), however many calls follow before that.
+ *           fovea_workspace_init is not needed: a call with rows writes a header
+ *           where there is none (needing no workspace, too, in one of 4096 bytes
+ *           or more that is 256-byte aligned).
  * Products and sums of a group are exact up to fp32 accumulation (an fp32 x
  * counts with all its bits); y is rounded once.
  */

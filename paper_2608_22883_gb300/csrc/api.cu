@@ -754,13 +754,17 @@ FOVEA_API fovea_status fovea_workspace_size(const fovea_params* p, const fovea_m
   return FOVEA_OK;
 }
 
+static cudaError_t init_header(void* ws, cudaStream_t s) {
+  const cudaError_t e = cudaMemsetAsync(ws, 0, kWsHeaderBytes, s);
+  return e != cudaSuccess ? e : cudaMemsetAsync(static_cast<uint8_t*>(ws) + kWsMarkAt, kWsMarkByte, kWsMarkBytes, s);
+}
+
 FOVEA_API fovea_status fovea_workspace_init(void* workspace, size_t bytes, void* stream) {
   g_last_error.clear();
   if (workspace == nullptr) return fail(FOVEA_ERR_INVALID_ARG, "workspace is NULL");
   if (bytes < kWsHeaderBytes)
     return fail(FOVEA_ERR_INVALID_ARG, "workspace of %zu bytes is too small", bytes);
-  FOVEA_CUDA(cudaMemsetAsync(workspace, 0, kWsHeaderBytes, static_cast<cudaStream_t>(stream)),
-             "cudaMemsetAsync");
+  FOVEA_CUDA(init_header(workspace, static_cast<cudaStream_t>(stream)), "cudaMemsetAsync");
   return FOVEA_OK;
 }
 
@@ -773,7 +777,7 @@ FOVEA_API fovea_status fovea_sync_errors(void* workspace, void* stream) {
              "cudaMemcpyAsync");
   FOVEA_CUDA(cudaStreamSynchronize(s), "cudaStreamSynchronize");
   // clear the whole header: a kernel that gave up may have left other words set
-  FOVEA_CUDA(cudaMemsetAsync(workspace, 0, herr ? kWsHeaderBytes : sizeof(int), s),
+  FOVEA_CUDA(herr ? init_header(workspace, s) : cudaMemsetAsync(workspace, 0, sizeof(int), s),
              "cudaMemsetAsync");
   FOVEA_CUDA(cudaStreamSynchronize(s), "cudaStreamSynchronize");
   if (herr & kErrTimeout)
@@ -1384,6 +1388,8 @@ FOVEA_API fovea_status fovea_linear_w4(const void* x, int64_t x_ld, int x_dtype,
   a.y = y; a.y_dtype = y_dtype;
   a.N = N;
   a.workspace = workspace;
+  if (need == 0 && workspace_bytes >= kWsHeaderBytes && (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0)
+    a.header = static_cast<int*>(workspace);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   KernelTimer t("linear_w4", s);
   FOVEA_CUDA(launch_linear_w4(a, s), "linear_w4");

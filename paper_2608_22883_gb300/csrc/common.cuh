@@ -15,9 +15,23 @@ namespace fovea {
 // Sticky device error bits (workspace / memory error word).
 enum : int { kErrDepth = 1, kErrTimeout = 2 };
 
-// Bytes at the start of a step workspace: the sticky error word and reserved
-// words (fovea_workspace_init zeroes them).
-constexpr size_t kWsHeaderBytes = 4096;
+// Bytes at the start of a workspace: the sticky error word, reserved words, and a
+// mark that tells an initialised header from whatever else the memory held
+// (fovea_workspace_init writes it and zeroes the rest).
+constexpr size_t kWsHeaderBytes = 4096, kWsMarkAt = 64, kWsMarkBytes = 32;
+constexpr int kWsMarkByte = 0xA5;
+// By one thread of a kernel that takes workspaces without a header: writes one where there
+// is none; the error word of an initialised header is left as it is.
+__device__ __forceinline__ void ensure_header(int* err) {
+  constexpr unsigned kMark = 0x01010101u * kWsMarkByte;
+  uint4* mark = reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(err) + kWsMarkAt);
+  bool there = (*err & ~(kErrDepth | kErrTimeout)) == 0;
+  for (int i = 0; i < (int)kWsMarkBytes / 16; ++i)
+    there = there && mark[i].x == kMark && mark[i].y == kMark && mark[i].z == kMark && mark[i].w == kMark;
+  if (there) return;
+  *err = 0;
+  for (int i = 0; i < (int)kWsMarkBytes / 16; ++i) mark[i] = make_uint4(kMark, kMark, kMark, kMark);
+}
 
 // Limit of a bounded mbarrier wait inside the tensor-core kernels (ns).  A
 // wait that gives up sets kErrTimeout; the kernel then waits for the work it
@@ -418,6 +432,7 @@ struct LinearW4Args {
   void* y; int y_dtype;
   int N;
   void* workspace;                   // linear_w4_workspace bytes
+  int* header;                       // a workspace given to a call that needs none: its header, or null
 };
 // Bytes of workspace the product needs (0: none).
 size_t linear_w4_workspace(int N, int in, int group, int x_dtype, bool by_group);

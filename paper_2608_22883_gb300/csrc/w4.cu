@@ -469,7 +469,10 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
     refill_scales();
     turn();
   }
-  if (tid == 0) xs[-1] = make_uint4(0u, 0u, 0u, 0u);
+  if (tid == 0) {
+    xs[-1] = make_uint4(0u, 0u, 0u, 0u);
+    if (a.header != nullptr && blockIdx.x == 0) ensure_header(a.header);
+  }
   // x, a few units a thread on their way together
   constexpr int kBatch = 4;
   for (int u0 = tid; u0 < spans * 16 * rows; u0 += kBatch * kThreads) {

@@ -650,7 +650,7 @@ constexpr int kLayoutThreads = 256;
 __global__ void __launch_bounds__(kLayoutThreads) layout_x_kernel(const LayoutArgs a) {
   pdl_wait();
   pdl_trigger();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.err = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) ensure_header(a.err);
   const int units = a.k_pad / 8;
   const int slots = kMaxCols / a.parts;                    // rows of a block, padding among them
   const long long row_items = (long long)a.blocks * slots * units;

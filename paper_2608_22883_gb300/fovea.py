@@ -335,6 +335,11 @@ def noalloc_sync_errors(stream=None) -> None:
     _check(lib().fovea_noalloc_sync_errors(_stream(stream)))
 
 
+def workspace_init(workspace: torch.Tensor, stream=None) -> None:
+    """fovea_workspace_init: write the header of a workspace."""
+    _check(lib().fovea_workspace_init(_ptr(workspace), workspace.numel(), _stream(stream)))
+
+
 def sync_errors(workspace: torch.Tensor, stream=None) -> None:
     _check(lib().fovea_sync_errors(_ptr(workspace), _stream(stream)))
 
@@ -541,8 +546,9 @@ def linear_w4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
     or float8_e4m3fn with x_scale [N] or [N, ceil(in / group)] fp32 (add_rms_norm's
     q8 and q8_scale); bias [out] fp32; y is fp32 or bf16 (out_dtype).
     workspace: a uint8 tensor of linear_w4_workspace_size bytes (None: allocated
-    for the call when one is needed); sync_errors(workspace) tells whether a
-    bounded device wait gave up, which also leaves NaN in y."""
+    for the call when one is needed; it needs no workspace_init); sync_errors(workspace)
+    tells whether a bounded device wait gave up in a call since the last one, which
+    also leaves NaN in y."""
     N, in_f, ld = _need_rows("x", x, _X_TYPES)
     dt, dev = x.dtype, x.device
     if group not in (32, 64, 128):

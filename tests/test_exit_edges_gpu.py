@@ -209,3 +209,67 @@ def test_zero_points_above_15(fovea, n, group):
         y = fovea.linear_w4(x, codes, scales, zeros, group=group)
         check_product(y, x, None, codes, scales, zeros, group, None)
         assert torch.equal(y, fovea.linear_w4(x, codes, scales, zeros + 128, group=group))
+
+
+def exhausted(fovea, call):
+    """call() with bounded waits that give up."""
+    fovea.debug_wait_limit(1)
+    try:
+        return call()
+    finally:
+        fovea.debug_wait_limit(0)
+
+
+def big_product(fovea, o):
+    g = gen(o)
+    n, k = 64, 16384
+    codes, scales, _ = make_w4(g, o, k, 128, False)
+    x = torch.randn((n, k), generator=g, device="cuda").to(BF16)
+    ws = torch.empty(fovea.linear_w4_workspace_size(n, k), device="cuda", dtype=torch.uint8)
+    return x, codes, scales, ws
+
+
+def test_a_wait_that_gave_up_is_told_after_later_calls(fovea):
+    x, codes, scales, ws = big_product(fovea, 6000)
+    want = fovea.linear_w4(x, codes, scales, workspace=ws)
+    fovea.sync_errors(ws)
+    y = exhausted(fovea, lambda: fovea.linear_w4(x, codes, scales, workspace=ws))
+    assert torch.equal(fovea.linear_w4(x, codes, scales, workspace=ws), want)      # through tensor memory
+    fovea.linear_w4(x[:2], codes, scales, workspace=ws)                            # few rows
+    with pytest.raises(fovea.FoveaError) as e:
+        fovea.sync_errors(ws)
+    assert e.value.status == fovea.ERR_TIMEOUT and torch.isnan(y).any()
+    assert torch.equal(fovea.linear_w4(x, codes, scales, workspace=ws), want)
+    fovea.sync_errors(ws)
+
+
+@pytest.mark.parametrize("n", [2, 64])
+@pytest.mark.parametrize("byte", [0, 1, 2, 3, 0xA5, 0xFF])
+def test_an_uninitialised_workspace_reports_nothing(fovea, n, byte):
+    x, codes, scales, ws = big_product(fovea, 300)
+    ws.fill_(byte)
+    fovea.linear_w4(x[:n], codes, scales, workspace=ws)
+    fovea.sync_errors(ws)
+
+
+@pytest.mark.parametrize("n", [2, 64])
+def test_a_pending_error_of_another_call_is_kept(fovea, n):
+    # a workspace of the step, with a depth out of range seen and not yet told
+    x, codes, scales, ws = big_product(fovea, 300)
+    fovea.workspace_init(ws)
+    ws[0] = 1
+    fovea.linear_w4(x[:n], codes, scales, workspace=ws)
+    with pytest.raises(fovea.FoveaError) as e:
+        fovea.sync_errors(ws)
+    assert e.value.status == fovea.ERR_INVALID_ARG
+    fovea.linear_w4(x[:n], codes, scales, workspace=ws)
+    fovea.sync_errors(ws)
+
+
+def test_a_small_workspace_that_few_rows_do_not_need(fovea):
+    x, codes, scales, _ = big_product(fovea, 300)
+    want = fovea.linear_w4(x[:2], codes, scales)
+    for size in (0, 1, 100, 4097):
+        ws = torch.full((size + 1,), 7, device="cuda", dtype=torch.uint8)[1:]
+        assert torch.equal(fovea.linear_w4(x[:2], codes, scales, workspace=ws), want)
+        assert (ws == 7).all()
