@@ -383,7 +383,7 @@ def lm_head_topk(W_LM: torch.Tensor, h_hat: torch.Tensor, k_c: int, workspace: t
 
 
 # ---------------------------------------------------------------------------
-# Operators of the drafter's exit
+# Operators of the drafter's exit.  All tensors of a call are on the current device.
 # ---------------------------------------------------------------------------
 
 _DTYPES = {torch.bfloat16: BF16, torch.float32: FP32, torch.float8_e4m3fn: E4M3}
@@ -391,11 +391,13 @@ _ROW_TYPES = (torch.bfloat16, torch.float32)
 _X_TYPES = (torch.bfloat16, torch.float32, torch.float8_e4m3fn)
 
 
-def _refuse(name: str, t, shape, dtypes, dense: bool) -> None:
-    """The error of a tensor that is not on the GPU, not of one of these types,
-    not of this shape (None: any size), or not contiguous (along its rows)."""
+def _refuse(name: str, t, shape, dtypes, dense: bool, device: Optional[int] = None) -> None:
+    """The error of a tensor that is not on the GPU (on this one), not of one of these
+    types, not of this shape (None: any size), or not contiguous (along its rows)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
+    if device is not None and t.get_device() != device:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}; the others are on cuda:{device}")
     if t.dtype not in dtypes:
         raise ValueError(f"{name} has type {t.dtype}; expected {' or '.join(map(str, dtypes))}")
     have = tuple(t.shape)
@@ -410,11 +412,12 @@ def _refuse(name: str, t, shape, dtypes, dense: bool) -> None:
 # The checks below cost a call about a third of a microsecond each; _refuse
 # finds the words when one fails.
 
-def _need_rows(name: str, t, dtypes):
-    """t is a CUDA matrix of one of these types with contiguous rows: its (rows,
-    columns, row stride)."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.dim() != 2:
-        _refuse(name, t, (None, None), dtypes, False)
+def _need_rows(name: str, t, dtypes, device: Optional[int] = None):
+    """t is a CUDA matrix of one of these types with contiguous rows, on this device
+    (None: any): its (rows, columns, row stride)."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.dim() != 2 \
+            or (not t.is_cuda if device is None else t.get_device() != device):
+        _refuse(name, t, (None, None), dtypes, False, device)
     n, m = t.shape
     ld, inner = t.stride()
     if inner != 1 and m > 1:
@@ -422,12 +425,21 @@ def _need_rows(name: str, t, dtypes):
     return n, m, ld if n > 1 else m
 
 
-def _need(name: str, t, shape, dtype) -> int:
-    """t is a contiguous CUDA tensor of this type and shape: its address."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not dtype or t.shape != shape \
-            or not t.is_contiguous():
-        _refuse(name, t, shape, (dtype,), True)
+def _need(name: str, t, shape, dtype, device: int) -> int:
+    """t is a contiguous tensor of this type and shape on this device: its address."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != device or t.dtype is not dtype \
+            or t.shape != shape or not t.is_contiguous():
+        _refuse(name, t, shape, (dtype,), True, device)
     return t.data_ptr()
+
+
+def _device_of(name: str, t: torch.Tensor) -> int:
+    """The device of a call's first tensor: the current one, where the kernels launch."""
+    device = t.get_device()
+    if device != torch.cuda.current_device():
+        raise ValueError(f"{name} is on cuda:{device}, which is not the current device "
+                         f"(cuda:{torch.cuda.current_device()})")
+    return device
 
 
 def _side_stream(stream, device, raw, inputs):
@@ -466,11 +478,11 @@ def add_rms_norm(x: torch.Tensor, gamma: torch.Tensor, residual: Optional[torch.
                 [N, ceil(d / q8_group)] for q8_group of 32, 64 or 128 columns
                 (both only when q8_group is given)."""
     N, d, ld = _need_rows("x", x, _ROW_TYPES)
-    dt, dev = x.dtype, x.device
-    gamma_at = _need("gamma", gamma, (d,), dt)
+    dt, dev, at = x.dtype, x.device, _device_of("x", x)
+    gamma_at = _need("gamma", gamma, (d,), dt, at)
     residual_at, residual_ld = None, 0
     if residual is not None:
-        n, m, residual_ld = _need_rows("residual", residual, (dt,))
+        n, m, residual_ld = _need_rows("residual", residual, (dt,), at)
         if n != N or m != d:
             _refuse("residual", residual, (N, d), (dt,), False)
         residual_at = residual.data_ptr()
@@ -511,6 +523,7 @@ def quantize_w4(W: torch.Tensor, group: int = 128, *, symmetric: bool = True,
     if group not in (32, 64, 128):
         raise ValueError(f"group {group} is not 32, 64 or 128")
     dev = W.device
+    _device_of("W", W)
     raw, empty = _on(stream, dev, W)
     groups = -(-in_f // group)
     codes = empty((out_f, in_f // 2), dtype=torch.uint8, device=dev)
@@ -550,31 +563,31 @@ def linear_w4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
     tells whether a bounded device wait gave up in a call since the last one, which
     also leaves NaN in y."""
     N, in_f, ld = _need_rows("x", x, _X_TYPES)
-    dt, dev = x.dtype, x.device
+    dt, dev, at = x.dtype, x.device, _device_of("x", x)
     if group not in (32, 64, 128):
         raise ValueError(f"group {group} is not 32, 64 or 128")
     out_f = codes.shape[0] if isinstance(codes, torch.Tensor) and codes.dim() == 2 else 0
-    codes_at = _need("codes", codes, (out_f, in_f // 2), torch.uint8)
+    codes_at = _need("codes", codes, (out_f, in_f // 2), torch.uint8, at)
     groups = -(-in_f // group)
-    scales_at = _need("scales", scales, (out_f, groups), torch.bfloat16)
+    scales_at = _need("scales", scales, (out_f, groups), torch.bfloat16, at)
     zeros_at = x_scale_at = bias_at = None
     if zeros is not None:
-        zeros_at = _need("zeros", zeros, (out_f, groups), torch.uint8)
+        zeros_at = _need("zeros", zeros, (out_f, groups), torch.uint8, at)
     x_group = 0
     if (dt is torch.float8_e4m3fn) != (x_scale is not None):
         raise ValueError("x_scale goes with float8_e4m3fn rows, and only with them")
     if x_scale is not None:
         x_group = group if x_scale.dim() == 2 else 0
-        x_scale_at = _need("x_scale", x_scale, (N, groups) if x_group else (N,), torch.float32)
+        x_scale_at = _need("x_scale", x_scale, (N, groups) if x_group else (N,), torch.float32, at)
     if bias is not None:
-        bias_at = _need("bias", bias, (out_f,), torch.float32)
+        bias_at = _need("bias", bias, (out_f,), torch.float32, at)
     if out_dtype not in _ROW_TYPES:
         raise ValueError(f"out_dtype {out_dtype} is neither bf16 nor fp32")
     raw, empty = _on(stream, dev, x, codes, scales, zeros, x_scale, bias, workspace)
     ws_at, ws_bytes = None, 0
     if workspace is not None:
         ws_bytes = workspace.numel()
-        ws_at = _need("workspace", workspace, (ws_bytes,), torch.uint8)
+        ws_at = _need("workspace", workspace, (ws_bytes,), torch.uint8, at)
     else:
         ws_bytes = linear_w4_workspace_size(N, in_f, group, dt, x_group)
         if ws_bytes:
@@ -590,25 +603,26 @@ def linear_w4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
 
 
 def _need_scores(logits, tokens, row_scale, allowed):
-    """Checks what both score calls take; returns (N, vocab, logits' row stride,
-    n_tokens, and the addresses of tokens, row_scale and allowed, allowed's row
-    stride)."""
+    """Checks what both score calls take; returns (device, N, vocab, logits' row
+    stride, n_tokens, and the addresses of tokens, row_scale and allowed, allowed's
+    row stride)."""
     N, V, ld = _need_rows("logits", logits, _ROW_TYPES)
+    at = _device_of("logits", logits)
     T, tokens_at, scale_at, allowed_at, allowed_ld = 0, None, None, None, 0
     if tokens is not None:
         T = tokens.shape[1] if isinstance(tokens, torch.Tensor) and tokens.dim() == 2 else 0
-        tokens_at = _need("tokens", tokens, (N, T), torch.int32)
+        tokens_at = _need("tokens", tokens, (N, T), torch.int32, at)
     if row_scale is not None:
-        scale_at = _need("row_scale", row_scale, (N,), torch.float32)
+        scale_at = _need("row_scale", row_scale, (N,), torch.float32, at)
     if allowed is not None:
-        rows, words, allowed_ld = _need_rows("allowed", allowed, (torch.int32,))
+        rows, words, allowed_ld = _need_rows("allowed", allowed, (torch.int32,), at)
         if words != (V + 31) // 32 or rows not in (1, N):
             raise ValueError(f"allowed has shape {list(allowed.shape)}; expected "
                              f"[{N} or 1, {(V + 31) // 32}]")
         allowed_at = allowed.data_ptr()
         if rows == 1:
             allowed_ld = 0
-    return N, V, ld, T, tokens_at, scale_at, allowed_at, allowed_ld
+    return at, N, V, ld, T, tokens_at, scale_at, allowed_at, allowed_ld
 
 
 def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top_k: int = 0, *,
@@ -623,8 +637,8 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
       top_idx       [N, top_k] int32, the largest logits' tokens, descending, the
                     smaller token first on ties, -1 past the tokens that have any
                     probability; top_logprobs [N, top_k] (when top_k > 0)."""
-    N, V, ld, T, tokens_at, scale_at, allowed_at, allowed_ld = _need_scores(logits, tokens, row_scale,
-                                                                            allowed)
+    at, N, V, ld, T, tokens_at, scale_at, allowed_at, allowed_ld = _need_scores(logits, tokens, row_scale,
+                                                                                allowed)
     dev = logits.device
     raw, empty = _on(stream, dev, logits, tokens, row_scale, allowed)
     f32 = torch.float32
@@ -665,29 +679,29 @@ def token_logprobs_grad(logits: torch.Tensor, stats: torch.Tensor, entropy: torc
     result when given; it may be logits itself, when dense."""
     if (tokens is None) != (grad_logprobs is None) or (top_idx is None) != (grad_top is None):
         raise ValueError("tokens and grad_logprobs, top_idx and grad_top, go together")
-    N, V, ld, T, tokens_at, scale_at, allowed_at, allowed_ld = _need_scores(logits, tokens, row_scale,
-                                                                            allowed)
+    at, N, V, ld, T, tokens_at, scale_at, allowed_at, allowed_ld = _need_scores(logits, tokens, row_scale,
+                                                                                allowed)
     f32 = torch.float32
-    stats_at = _need("stats", stats, (N, 2), f32)
-    entropy_at = _need("entropy", entropy, (N,), f32)
+    stats_at = _need("stats", stats, (N, 2), f32, at)
+    entropy_at = _need("entropy", entropy, (N,), f32, at)
     k, glp_at, idx_at, gtop_at, gH_at, glse_at = 0, None, None, None, None, None
     if tokens is not None:
-        glp_at = _need("grad_logprobs", grad_logprobs, (N, T), f32)
+        glp_at = _need("grad_logprobs", grad_logprobs, (N, T), f32, at)
     if top_idx is not None:
         k = top_idx.shape[1] if isinstance(top_idx, torch.Tensor) and top_idx.dim() == 2 else 0
-        idx_at = _need("top_idx", top_idx, (N, k), torch.int32)
-        gtop_at = _need("grad_top", grad_top, (N, k), f32)
+        idx_at = _need("top_idx", top_idx, (N, k), torch.int32, at)
+        gtop_at = _need("grad_top", grad_top, (N, k), f32, at)
     if grad_entropy is not None:
-        gH_at = _need("grad_entropy", grad_entropy, (N,), f32)
+        gH_at = _need("grad_entropy", grad_entropy, (N,), f32, at)
     if grad_lse is not None:
-        glse_at = _need("grad_lse", grad_lse, (N,), f32)
+        glse_at = _need("grad_lse", grad_lse, (N,), f32, at)
     dt, dev = logits.dtype, logits.device
     raw, empty = _on(stream, dev, logits, stats, entropy, tokens, grad_logprobs, top_idx, grad_top,
                      grad_entropy, grad_lse, row_scale, allowed, out)
     if out is None:
         out = empty((N, V), dtype=dt, device=dev)
     else:
-        _need("out", out, (N, V), dt)
+        _need("out", out, (N, V), dt, at)
     st = lib().fovea_token_logprobs_grad(logits.data_ptr(), ld, N, V, _DTYPES[dt], scale_at, allowed_at,
                                          allowed_ld, stats_at, entropy_at, tokens_at, glp_at, T, idx_at,
                                          gtop_at, k, gH_at, glse_at, out.data_ptr(), raw)

@@ -273,3 +273,51 @@ def test_a_small_workspace_that_few_rows_do_not_need(fovea):
         ws = torch.full((size + 1,), 7, device="cuda", dtype=torch.uint8)[1:]
         assert torch.equal(fovea.linear_w4(x[:2], codes, scales, workspace=ws), want)
         assert (ws == 7).all()
+
+
+class Elsewhere(torch.Tensor):
+    """A tensor of this GPU that says it is another one's."""
+
+    def get_device(self):
+        return 1
+
+
+def operator_calls(fovea):
+    x = torch.randn((4, 128), device="cuda")
+    w = fovea.quantize_w4(x)
+    gamma, bias = torch.ones(128, device="cuda"), torch.zeros(4, device="cuda")
+    x8, x_scale = x.to(torch.float8_e4m3fn), torch.ones(4, device="cuda")
+    ws = torch.zeros(1 << 20, device="cuda", dtype=torch.uint8)
+    tokens = torch.zeros((4, 1), device="cuda", dtype=torch.int32)
+    allowed = torch.full((4, 4), -1, device="cuda", dtype=torch.int32)
+    f = fovea.token_logprobs(x, tokens, 2)
+    g1, g2 = torch.ones((4, 1), device="cuda"), torch.ones((4, 2), device="cuda")
+    return [
+        (fovea.add_rms_norm, dict(x=x, gamma=gamma, residual=x.clone())),
+        (fovea.quantize_w4, dict(W=x)),
+        (fovea.linear_w4, dict(x=x8, codes=w["codes"], scales=w["scales"], zeros=torch.zeros_like(w["scales"]).byte(),
+                               x_scale=x_scale, bias=bias, workspace=ws)),
+        (fovea.token_logprobs, dict(logits=x, tokens=tokens, row_scale=bias + 1, allowed=allowed)),
+        (fovea.token_logprobs_grad, dict(logits=x, stats=f["stats"], entropy=f["entropy"], tokens=tokens,
+                                         grad_logprobs=g1, top_idx=f["top_idx"], grad_top=g2, grad_entropy=bias,
+                                         grad_lse=bias.clone(), row_scale=bias + 1, allowed=allowed,
+                                         out=torch.empty_like(x))),
+    ]
+
+
+def test_tensors_of_several_devices_are_refused(fovea):
+    for call, kw in operator_calls(fovea):
+        call(**kw)
+        for name, t in kw.items():
+            with pytest.raises(ValueError, match="cuda:1"):
+                call(**dict(kw, **{name: t.as_subclass(Elsewhere)}))
+                pytest.fail(f"{call.__name__}: {name} was not refused")
+
+
+def test_tensors_of_a_device_that_is_not_the_current_one_are_refused(fovea, monkeypatch):
+    calls = operator_calls(fovea)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call, kw in calls:
+        with pytest.raises(ValueError, match="current device"):
+            call(**kw)
+            pytest.fail(f"{call.__name__} was not refused")
