@@ -302,7 +302,9 @@ __device__ __forceinline__ void mma_16x8x16_first(float (&c)[4], uint32_t a0, ui
       : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
-// x from shared memory, which nothing writes once it is laid out (so: not volatile).
+// x from shared memory, which nothing writes once it is laid out: not volatile, so that
+// the compiler may move it.  What keeps it behind the barrier is its address, which comes
+// out of a volatile statement there.
 __device__ __forceinline__ uint4 lds_x(uint32_t at) {
   uint4 v;
   asm("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
@@ -508,8 +510,9 @@ linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bo
 
   // this lane's column of x: a column past the last reads the zeros
   const uint32_t x_step = g < cols ? 64u * cols : 0u;    // bytes from one word to the next
-  const uint32_t x_first =
+  uint32_t x_first =
       (uint32_t)__cvta_generic_to_shared(g < cols ? xs + (q_lo * kQuad * 16 + t) * cols + g : xs - 1);
+  asm volatile("" : "+r"(x_first) : : "memory");           // no read of x (lds_x) passes the barrier
   float* mine = part + warp * kTilePart;
   const float* tile_part = part + team * split * kTilePart;
   for (int tile = first; tile < tiles; tile += step) {
