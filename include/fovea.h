@@ -343,8 +343,9 @@ FOVEA_API fovea_status fovea_lm_head_workspace_size(int vocab, int d_model, int 
  * and y in 8 bits: q8 = e4m3(y / scale), scale = max |y| / 448 over the row
  * (q8_group 0) or over each q8_group consecutive columns (32, 64 or 128; the
  * last group may be shorter); where scale is 0, q8 is 0.  The norm and q8 follow
- * from the unrounded fp32 sum.  A row that holds a NaN or an infinity gives NaN
- * scales and NaN in y where s is not finite.
+ * from the unrounded fp32 sum; its squares and s gamma are fp32 (|s| beyond 1e17
+ * can overflow there).  A row that holds a NaN or an infinity gives NaN scales and
+ * NaN in y where s is not finite.
  *   x, residual [N, d] dtype (residual NULL: s = x); gamma [d] dtype
  *   sum         [N, d] dtype: s, or NULL; may be x or residual when that is dense
  *   out         [N, d] dtype: y, or NULL
@@ -368,7 +369,8 @@ FOVEA_API fovea_status fovea_add_rms_norm(const void* x, int64_t x_ld, const voi
  *                            zero = clamp(round(-lo / scale), 0, 15),
  *                            code = clamp(round(w / scale) + zero, 0, 15)
  * rounding to nearest even; where scale is 0, code and zero are 8.  A group
- * that holds a NaN gets a NaN scale.
+ * that holds a NaN gets a NaN scale.  hi - lo is fp32 (|w| beyond 1.7e38 can
+ * overflow there).
  *   codes  [out_features, in_features / 2] bytes (4-byte aligned), the even
  *          column of a pair in the low four bits
  *   scales [out_features, groups] bf16, zeros [out_features, groups] bytes,
@@ -398,7 +400,12 @@ FOVEA_API fovea_status fovea_quantize_w4(const void* W, int64_t ld, int out_feat
  *           where there is none (needing no workspace, too, in one of 4096 bytes
  *           or more that is 256-byte aligned).
  * Products and sums of a group are exact up to fp32 accumulation (an fp32 x
- * counts with all its bits); y is rounded once.
+ * counts with all its bits); y is rounded once.  A group's sum of x (code - zero)
+ * is formed before its scale: with |x| beyond 1e34 it can overflow fp32 where y
+ * would not.
+ * Up to 8 rows (2 of fp32) pass over the weights once for as many rows as fit
+ * shared memory (8 up to about 13800 columns, 6 of 16384, 3 of 32768; fp32 2 up
+ * to 18500, then 1); more rows once for 64 (21 of fp32).
  */
 FOVEA_API fovea_status fovea_linear_w4(const void* x, int64_t x_ld, int x_dtype,
                                        const float* x_scale, int x_group, int N, const void* codes,
@@ -413,7 +420,7 @@ FOVEA_API fovea_status fovea_linear_w4_workspace_size(int N, int in_features, in
 
 /*
  * Scores of tokens under the softmax of each row of logits: with z = logit *
- * row_scale over the row's allowed tokens,
+ * row_scale (rounded to fp32) over the row's allowed tokens,
  *   lse = log sum e^z, logp = z - lse, entropy = -sum p logp,
  * and the top_k tokens with the largest logits, ties broken by the smaller token.
  *   logits       [N, vocab] dtype (FOVEA_BF16 or FOVEA_FP32), row stride ld
@@ -453,7 +460,8 @@ FOVEA_API fovea_status fovea_token_logprobs(const void* logits, int64_t ld, int 
  *              + grad_lse p_i),
  * G the sum of the gradients of the row's counted tokens and alternatives (those
  * that are none or have probability 0 do not count; a token >= vocab makes the
- * row NaN).  Tokens that are not allowed get 0, and so does a row without tokens.
+ * row's allowed tokens NaN).  Tokens that are not allowed get 0 in every row, and
+ * so does a row without tokens whatever the gradients of its entropy and lse.
  *   grad_logprobs [N, n_tokens], grad_top [N, top_k], grad_entropy [N],
  *                 grad_lse [N], all fp32; the last two may be NULL (0)
  *   dlogits       [N, vocab] dtype, dense; may be logits themselves when ld = vocab

@@ -232,8 +232,9 @@ struct Shared {
 //
 // Instructions bound the pass (two fp32 operations in one where there is such a form)
 // and latency the search.  4096 rows of 32000 bf16: 49 us without alternatives (78 % of
-// the measured copy's bandwidth), 70 us with six (56 %), 98 with 32; one fp32 row of 32000
-// 6.9 us, where the cluster's two meetings and the search's steps follow one another.
+// the measured copy's bandwidth), 69.5 us with six (56 %), 98 with 32, 72.4 with six under
+// temperatures; 2048 masked 49.2 (42 %); 2048 fp32 rows 55 (70 %); one fp32 row of 32000
+// 7.1 us, where the cluster's two meetings and the search's steps follow one another.
 // 256 threads: 128 and 512 measured no better.
 //
 // Six CTAs an SM are worth 40 registers to unmasked bf16 rows (72.6 to 69.6 us) and not to
@@ -510,8 +511,8 @@ token_logprobs_kernel(const ScoreArgs a) {
 // The gradient of one row's range of chunks.  Every token's term is p (A - g_H
 // logp) with A of the row; the few tokens with a gradient of their own are
 // written again after it, by the CTA whose range they lie in.  Bound by memory: 4096
-// rows of 32000 bf16 82 us, 6.4 TB/s (94 % of the measured copy); 40 masked fp32 rows
-// 7.0 us.
+// rows of 32000 bf16 82 us, 6.4 TB/s (94 % of the measured copy); 2048 masked 51.3 (78 %);
+// 40 masked fp32 rows 7.1 us.
 template <class T, bool MASKED, bool SCALED>
 __global__ void __launch_bounds__(kThreads) token_logprobs_grad_kernel(const ScoreGradArgs a) {
   constexpr int NV = Row<T>::NV;

@@ -235,7 +235,9 @@ constexpr int kQuad = 2;               // spans of codes a warp has on their way
 // Columns of x (an fp32 row counts three times) that a tile takes: the tensor-core
 // instruction's eight.  More go through tensor memory (w4_tc.cu): with two such
 // instructions a word 16 rows by 4096 x 32000 took 44.8 us here against 27.3 there, 8
-// rows 22.4.
+// rows 22.4.  (Rows that do not fit shared memory together take a launch each few, which
+// that path would do sooner: 8 rows by [4096, 14336] 32.4 us, 9 there 15.9; by [4096,
+// 32768] 86.5 and 26.5.)
 constexpr int kFewCols = 8;
 // A tile is 8 * R weight rows, of which a lane holds the words of R: 16 rows are one
 // operand, 32 two that share each read of x.  The registers for 32 are there with
@@ -383,9 +385,9 @@ struct Quad {
 // shift, a LOP3 and a subtraction for two of them, at most 4.75 cycles of a scheduler,
 // besides the products.  A warp a tile without barriers and the operands' layout
 // chosen so that a word needs no exchange between lanes keep the rest small.  One bf16
-// row by [32000, 4096] in groups of 128: 19.1 us, 3.5 TB/s (52 % of the measured copy;
-// tensor pipe 20 %); by [128000, 4096] 57 us (70 %); 7 rows by [3584, 3584] in groups of
-// 64 with zero points 7.7 us, a tile's latency.
+// row by [32000, 4096] in groups of 128: 19.3 us, 3.5 TB/s (52 % of the measured copy;
+// tensor pipe 20 %); by [128000, 4096] 58.0 us (69 %); 7 rows by [3584, 3584] in groups of
+// 64 with zero points 7.8 us, a tile's latency.
 template <int G, bool ZEROS, int R>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_w4_kernel(const LinearW4Args a, int n0, int n1, int split, bool x_vec, bool scale_vec,

@@ -17,9 +17,11 @@
 // What bounds it are the instructions that make integers of the codes (a shift, a LOP3
 // and a subtraction for two), the trips of each group's sum through tensor memory, and
 // the last round of tiles: 250 tiles of [32000, 4096] give 98 SMs two and 54 one.  By
-// that matrix in groups of 128: 16 bf16 rows 24.4 us, 40 27.3, 64 29.2 (2.6 TB/s, 39 % of
-// the measured copy); 64 e4m3 rows with scales by group 36.5, whose every sum takes
-// a product of two scales; 40 rows in groups of 64 40, of 32 67.
+// that matrix in symmetric groups of 128: 16 bf16 rows 24.3 us, 40 27.6, 64 29.5 (2.6
+// TB/s, 38 % of the measured copy); 64 e4m3 rows with scales by row 32.0, by group 36.6,
+// whose every sum takes a product of two scales; 40 bf16 rows in groups of 64 37.0, of 32
+// 62.0 (with zero points 40.0 and 66.8).  Each 64 columns of x are a launch that makes the
+// integers again: 128 bf16 rows 55.2, 1024 418; 64 fp32 rows 108.
 #include <algorithm>
 #include <atomic>
 
@@ -269,7 +271,7 @@ struct Turn {
 
 // NC: accumulator columns (cols_pad), in the instruction's steps of 16: the summing
 // warps' work goes with them (40 rows by 4096 x 32000, 48 columns against 64: 27.3 and
-// 28.8 us, in groups of 64 40.1 and 44.0).  G: the group.  A tile's contraction may
+// 28.8 us, in groups of 64 with zero points 40.1 and 44.0).  G: the group.  A tile's contraction may
 // be split over the CTAs of a cluster, which then has one tile.
 template <int NC, int G>
 __global__ void __launch_bounds__(kThreads<NC>, 1)
@@ -299,8 +301,8 @@ linear_w4_tc_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
   const int k_lo = a.ksteps * rank / split, k_hi = a.ksteps * (rank + 1) / split;
   constexpr int kPerUnit = kUnitK / G;                     // groups in a unit: 1, 2 or 4
   // accumulators, 64 columns a slot: of one group, or of two of up to 32 columns, which
-  // then share its waits (16 rows by 4096 x 32000 in groups of 32: 48.3 us, one by one
-  // 60.0; with more columns there were only two slots, 40 rows: 68.5 us and 67.3)
+  // then share its waits (with zero points, 16 rows by 4096 x 32000 in groups of 32: 48.3 us,
+  // one by one 60.0; with more columns there were only two slots, 40 rows: 68.5 us and 67.3)
   constexpr int kSlotGroups = NC <= 32 && kPerUnit > 1 ? 2 : 1, kSlotsUnit = kPerUnit / kSlotGroups;
   // issuing warps: as many as leave each slot to one of them (a barrier's parity tells
   // a warp only of the round before its own)
