@@ -478,6 +478,157 @@ FOVEA_API fovea_status fovea_token_logprobs_grad(const void* logits, int64_t ld,
                                                  const float* grad_entropy, const float* grad_lse,
                                                  void* dlogits, void* stream);
 
+/*
+ * Operators of the drafter's cache
+ * --------------------------------
+ * What a draft model's block does between its projections: rotary positions, new
+ * entries of a paged key-value cache, the attention of a new token or of a draft
+ * tree over it, and the cache's upkeep when a tree has been verified or sequences
+ * are forked and dropped.
+ *
+ * A cache is two pools of pages, k_pages and v_pages [n_pages, kv_heads, page, dim]
+ * dense and 16-byte aligned, of cache_dtype: FOVEA_BF16, FOVEA_E4M3 (beside bf16
+ * rows) or FOVEA_FP32 (beside fp32 rows); dim is 64, 128 or 256, page a multiple
+ * of 16 up to 1024.  k_scale and v_scale [kv_heads] fp32 (e4m3 only, or NULL: 1):
+ * an entry stands for its 8 bits times the head's scale.  Entry e of sequence b
+ * lies in page table[b, e / page] at e % page; table [B, width] int32 is dense,
+ * and what stands behind a sequence's pages is not used.  A page number outside
+ * [0, n_pages) is never followed: each call states what it does instead.
+ * Rows of q, k and v are [N, heads, dim] with a stride of tokens `ld` and of heads
+ * `hs` in elements (a row itself is contiguous), aligned to their element.
+ * None of these calls allocates or synchronises; all enqueue on `stream` and can
+ * be captured.  N = 0 or B = 0 is valid and does nothing (fovea_cache_fork counts its
+ * free pages all the same).
+ * Errors: INVALID_ARG, UNSUPPORTED (nothing enqueued), CUDA.
+ */
+#define FOVEA_MAX_AXES 8           /* axes of a position */
+#define FOVEA_MAX_HEAD 512         /* dims of a rotated head */
+#define FOVEA_MAX_HEADS 1024       /* heads of q, k and v together */
+#define FOVEA_MAX_TREE 256         /* newest entries of a sequence that attend together */
+#define FOVEA_MAX_PAGE 1024        /* entries of a page */
+#define FOVEA_MAX_PAGES (1 << 20)  /* pages of a pool, for fovea_cache_fork */
+#define FOVEA_MAX_CACHE_SEQ 2048   /* sequences of a call */
+
+/*
+ * Rotary positions with several axes (time, height, width, ...): pair j < rot / 2 of
+ * a head's first rot dims is turned by phi = positions[axis[j], n] * frequencies[j],
+ *   a' = a cos phi - b sin phi,  b' = a sin phi + b cos phi,
+ * (a, b) the dims (j, j + rot / 2), or (2j, 2j + 1) with adjacent != 0; the dims from
+ * rot on are copied.  inverse != 0 turns by -phi: the gradient with respect to q and k
+ * from that of the outputs.
+ *   q [N, heads, dim], k [N, kv_heads, dim] dtype (FOVEA_BF16 or FOVEA_FP32; k NULL
+ *               and kv_heads 0: q alone)
+ *   positions   [axes, N] int32 (row stride pos_ld), any value
+ *   frequencies [rot / 2] fp64, radians per position; axis [rot / 2] int32, or NULL
+ *               (axis 0).  A frequency that is not finite, or an axis outside
+ *               [0, axes), gives NaN.
+ *   q_out, k_out dense, dtype; may be q and k where these are dense
+ * The angle is right to 1e-7 at every position (whole turns are taken off in 64-bit
+ * fixed point); sums are fp32, rounded once.  rot even, 2 <= rot <= dim <= FOVEA_MAX_HEAD.
+ */
+FOVEA_API fovea_status fovea_rotary_axes(const void* q, int64_t q_ld, int64_t q_hs, int heads,
+                                         const void* k, int64_t k_ld, int64_t k_hs, int kv_heads,
+                                         int N, int dim, int dtype, const int32_t* positions,
+                                         int64_t pos_ld, int axes, const double* frequencies,
+                                         const int32_t* axis, int rot, int adjacent, int inverse,
+                                         void* q_out, void* k_out, void* stream);
+
+/*
+ * New entries of a cache: keys k and values v [N, kv_heads, dim] dtype of token n go
+ * to entry[n] of sequence[n] ([N] int32), in 8 bits as e4m3(x / scale) with the ends
+ * at +-448.  With rot > 0 keys are rotated first, as fovea_rotary_axes does (rounded
+ * once, to the cache's type), and so is q [N, heads, dim] to q_out (q NULL: none);
+ * rot = 0: keys are stored as they are, and q must be NULL.
+ * A token whose sequence or entry is outside the table (sequence -1: a padded batch),
+ * or whose page is outside the pool, is not stored; its q is rotated all the same.
+ * No two tokens of a call may name one entry (either may be stored, or a mixture).
+ */
+FOVEA_API fovea_status fovea_cache_append(const void* q, int64_t q_ld, int64_t q_hs, int heads,
+                                          const void* k, int64_t k_ld, int64_t k_hs,
+                                          const void* v, int64_t v_ld, int64_t v_hs, int N,
+                                          int dtype, const int32_t* positions, int64_t pos_ld,
+                                          int axes, const double* frequencies,
+                                          const int32_t* axis, int rot, int adjacent, void* q_out,
+                                          void* k_pages, void* v_pages, int cache_dtype,
+                                          const float* k_scale, const float* v_scale, int n_pages,
+                                          int page, int kv_heads, int dim, const int32_t* table,
+                                          int B, int width, const int32_t* sequence,
+                                          const int32_t* entry, void* stream);
+
+/*
+ * Attention of the `nodes` newest entries of each of B sequences (one new token, or the
+ * nodes of a draft tree) over its lens[b] entries, themselves included:
+ *   s_e = scale q.k_e,  lse = log sum e^s,  out = sum e^(s - lse) v_e
+ * over the entries that a row sees: all before the newest `nodes`, and of those entry
+ * lens[b] - nodes + j where bit j % 32 of word j / 32 of its row of `tree` is set (NULL:
+ * j up to the row's own node).  What stands in the place of an entry that a row does not
+ * see is not used, whatever it is.
+ *   q     [B * nodes, heads, dim] bf16 (cache_dtype BF16, E4M3) or fp32 (FP32); query
+ *         head i reads key head i / (heads / kv_heads)
+ *   lens  [B] int32; below 1: a sequence without entries
+ *   tree  [tree_rows, nodes, ceil(nodes / 32)] 32-bit words, tree_rows B or 1, or NULL
+ *   out   [B * nodes, heads, dim] q's type, dense; lse [B * nodes, heads] fp32, or NULL
+ *   workspace  fovea_paged_attention_workspace_size bytes (256-byte aligned).  Any call on
+ *         the stream may use it next; it needs no fovea_workspace_init.
+ * A row that sees nothing (or only scores of -inf) has out 0 and lse -inf.  Where a page
+ * that a row needs is outside the pool, or lens[b] beyond the table, the row is NaN.
+ * Softmax and sums are fp32: p is held to 16 bits beside bf16 values, to 11 beside e4m3,
+ * fp32 in full; out is rounded once.  The order of the sums depends on the sizes alone.
+ * 1 <= nodes <= FOVEA_MAX_TREE; kv_heads divides heads; scale finite.
+ */
+FOVEA_API fovea_status fovea_paged_attention(const void* q, int64_t q_ld, int64_t q_hs, int heads,
+                                             const void* k_pages, const void* v_pages,
+                                             int cache_dtype, const float* k_scale,
+                                             const float* v_scale, int n_pages, int page,
+                                             int kv_heads, int dim, const int32_t* table, int B,
+                                             int width, const int32_t* lens, int nodes,
+                                             const int32_t* tree, int tree_rows, float scale,
+                                             void* out, float* lse, void* workspace,
+                                             size_t workspace_bytes, void* stream);
+/* Workspace bytes of fovea_paged_attention for these sizes.  Errors: INVALID_ARG, UNSUPPORTED. */
+FOVEA_API fovea_status fovea_paged_attention_workspace_size(int B, int nodes, int heads,
+                                                            int kv_heads, int dim, int cache_dtype,
+                                                            size_t* bytes);
+
+/*
+ * The accepted nodes of a verified tree kept: of each sequence's newest `size` entries,
+ * nodes[b, 0], nodes[b, 1], ... (nodes [B, path] int32, up to the first that is not in
+ * [0, size)) move to the first places, in this order, and
+ *   new_lens[b] = lens[b] - size + their number.
+ * All are read before any is written.  A sequence of fewer than `size` entries is left as
+ * it is, its length too; entries whose page is outside the pool are not moved.  Places
+ * that no entry moves to are left as they were.  1 <= path <= size <= FOVEA_MAX_TREE.
+ * new_lens is not lens' own memory.
+ */
+FOVEA_API fovea_status fovea_cache_keep(void* k_pages, void* v_pages, int cache_dtype, int n_pages,
+                                        int page, int kv_heads, int dim, const int32_t* table,
+                                        int B, int width, const int32_t* lens,
+                                        const int32_t* nodes, int path, int size,
+                                        int32_t* new_lens, void* stream);
+
+/*
+ * B sequences replaced by C continuations of them, by their pages: continuation c has the
+ * first new_lens[c] = min(keep[c], lens[parents[c]]) entries (at least 0; keep NULL: all)
+ * of sequence parents[c] (outside [0, B): of none), and pages for room[c] more (NULL: 0).
+ * Full pages are shared.  A partly filled last page stays with the first continuation
+ * that holds it, unless another holds it in full; the others get a copy of the entries
+ * they keep in a fresh page.  Pages that no continuation holds are free (those of
+ * dropped sequences too): fresh pages are taken from them, the lowest first, in the order
+ * of the continuations and their entries.
+ *   new_table [C, new_width] int32: -1 behind the pages; new_lens [C] int32
+ *   free      [1] int32: free pages left; negative: as many were missing, the last fresh
+ *             pages in the table are -1 and nothing has been copied
+ * A page number outside the pool is handed on as it is.  new_width bounds the pages (and
+ * new_lens) of a continuation.  n_pages <= FOVEA_MAX_PAGES.
+ */
+FOVEA_API fovea_status fovea_cache_fork(void* k_pages, void* v_pages, int cache_dtype, int n_pages,
+                                        int page, int kv_heads, int dim, const int32_t* table,
+                                        int B, int width, const int32_t* lens,
+                                        const int32_t* parents, const int32_t* keep,
+                                        const int32_t* room, int C, int32_t* new_table,
+                                        int new_width, int32_t* new_lens, int32_t* free_pages,
+                                        void* stream);
+
 /* Synchronise `stream`, read and clear the workspace's sticky error word.
  * Returns FOVEA_OK, FOVEA_ERR_INVALID_ARG (a depth outside [0, D] was seen)
  * or FOVEA_ERR_TIMEOUT (a bounded device wait gave up), or FOVEA_ERR_CUDA.

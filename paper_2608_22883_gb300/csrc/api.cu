@@ -1507,6 +1507,292 @@ FOVEA_API fovea_status fovea_token_logprobs_grad(const void* logits, int64_t ld,
   return FOVEA_OK;
 }
 
+// ---------------------------------------------------------------------------
+// Operators of the drafter's cache
+// ---------------------------------------------------------------------------
+
+// Rows [N, heads, dim] of a call: strides that keep heads and tokens apart are the
+// caller's; here only that they are not negative.
+static fovea_status check_heads(const void* x, long long ld, long long hs, int heads, int size, const char* name) {
+  if (ld < 0 || hs < 0)
+    return fail(FOVEA_ERR_INVALID_ARG, "strides %lld and %lld of %s must not be negative", ld, hs, name);
+  if (heads > 0) NEED_ALIGNED(x, size, name);
+  return FOVEA_OK;
+}
+static fovea_status check_rotary(int N, int dim, const int32_t* positions, long long pos_ld, int axes,
+                                 const double* frequencies, const int32_t* axis, int rot) {
+  if (rot < 2 || rot % 2 != 0 || rot > dim)
+    return fail(FOVEA_ERR_INVALID_ARG, "rot %d must be even and in [2, dim = %d]", rot, dim);
+  if (axes < 1) return fail(FOVEA_ERR_INVALID_ARG, "axes = %d < 1", axes);
+  if (axes > FOVEA_MAX_AXES) return fail(FOVEA_ERR_UNSUPPORTED, "axes %d > %d", axes, FOVEA_MAX_AXES);
+  if (axes > 1 && pos_ld < N)
+    return fail(FOVEA_ERR_INVALID_ARG, "row stride %lld of positions is below N = %d", pos_ld, N);
+  if (N > 0) {
+    NEED_ALIGNED(positions, 4, "positions");
+    NEED_ALIGNED(frequencies, 8, "frequencies");
+    WANT_ALIGNED(axis, 4, "axis");
+  }
+  return FOVEA_OK;
+}
+// The pools and tables of a call; rows: the type of the rows beside them, -1: none.
+static fovea_status check_cache(const CachePages& c, int rows) {
+  if (c.dtype != FOVEA_BF16 && c.dtype != FOVEA_FP32 && c.dtype != FOVEA_E4M3)
+    return fail(FOVEA_ERR_INVALID_ARG, "cache_dtype %d is not FOVEA_BF16, FOVEA_FP32 or FOVEA_E4M3", c.dtype);
+  if (rows >= 0 && (rows == FOVEA_FP32) != (c.dtype == FOVEA_FP32))
+    return fail(FOVEA_ERR_UNSUPPORTED, "fp32 rows go with an fp32 cache, bf16 rows with bf16 or e4m3");
+  if (c.dtype != FOVEA_E4M3 && (c.k_scale != nullptr || c.v_scale != nullptr))
+    return fail(FOVEA_ERR_INVALID_ARG, "k_scale and v_scale are for an e4m3 cache only");
+  if (c.dim != 64 && c.dim != 128 && c.dim != 256)
+    return fail(FOVEA_ERR_UNSUPPORTED, "dim %d is not 64, 128 or 256", c.dim);
+  if (c.page < 16 || c.page % 16 != 0)
+    return fail(FOVEA_ERR_INVALID_ARG, "page %d must be a positive multiple of 16", c.page);
+  if (c.page > FOVEA_MAX_PAGE) return fail(FOVEA_ERR_UNSUPPORTED, "page %d > %d", c.page, FOVEA_MAX_PAGE);
+  if (c.kv_heads < 1) return fail(FOVEA_ERR_INVALID_ARG, "kv_heads = %d < 1", c.kv_heads);
+  if (c.kv_heads > FOVEA_MAX_HEADS)
+    return fail(FOVEA_ERR_UNSUPPORTED, "kv_heads %d > %d", c.kv_heads, FOVEA_MAX_HEADS);
+  if (c.n_pages < 1) return fail(FOVEA_ERR_INVALID_ARG, "n_pages = %d < 1", c.n_pages);
+  if (c.B < 0 || c.width < 1)
+    return fail(FOVEA_ERR_INVALID_ARG, "the table's sizes %d and %d must be at least 0 and 1", c.B, c.width);
+  if (c.B > FOVEA_MAX_CACHE_SEQ)
+    return fail(FOVEA_ERR_UNSUPPORTED, "%d sequences > %d", c.B, FOVEA_MAX_CACHE_SEQ);
+  if ((long long)c.width * c.page > (1ll << 30) || (long long)c.B * c.width * c.page > (1ll << 34))
+    return fail(FOVEA_ERR_UNSUPPORTED, "tables of %d by %d pages of %d entries", c.B, c.width, c.page);
+  WANT_ALIGNED(c.k_scale, 4, "k_scale");
+  WANT_ALIGNED(c.v_scale, 4, "v_scale");
+  if (c.B == 0) return FOVEA_OK;
+  NEED_ALIGNED(c.k, 16, "k_pages");
+  NEED_ALIGNED(c.v, 16, "v_pages");
+  NEED_ALIGNED(c.table, 4, "table");
+  return FOVEA_OK;
+}
+static RotaryArgs rotary_args(const int32_t* positions, int64_t pos_ld, int axes, const double* frequencies,
+                              const int32_t* axis, int rot, int adjacent, int inverse) {
+  RotaryArgs r{};
+  r.positions = positions; r.pos_ld = pos_ld;
+  r.frequencies = frequencies; r.axis = axis;
+  r.axes = axes; r.rot = rot; r.adjacent = adjacent != 0; r.inverse = inverse != 0;
+  return r;
+}
+
+FOVEA_API fovea_status fovea_rotary_axes(const void* q, int64_t q_ld, int64_t q_hs, int heads,
+                                         const void* k, int64_t k_ld, int64_t k_hs, int kv_heads,
+                                         int N, int dim, int dtype, const int32_t* positions,
+                                         int64_t pos_ld, int axes, const double* frequencies,
+                                         const int32_t* axis, int rot, int adjacent, int inverse,
+                                         void* q_out, void* k_out, void* stream) {
+  g_last_error.clear();
+  fovea_status st = check_dtype(dtype);
+  if (st != FOVEA_OK) return st;
+  if (N < 0) return fail(FOVEA_ERR_INVALID_ARG, "N = %d < 0", N);
+  if (dim < 2) return fail(FOVEA_ERR_INVALID_ARG, "dim = %d < 2", dim);
+  if (dim > FOVEA_MAX_HEAD) return fail(FOVEA_ERR_UNSUPPORTED, "dim %d > %d", dim, FOVEA_MAX_HEAD);
+  if (heads < 1 || kv_heads < 0)
+    return fail(FOVEA_ERR_INVALID_ARG, "heads %d and kv_heads %d must be at least 1 and 0", heads, kv_heads);
+  if (heads > FOVEA_MAX_HEADS || kv_heads > FOVEA_MAX_HEADS - heads)
+    return fail(FOVEA_ERR_UNSUPPORTED, "heads %d and kv_heads %d > %d", heads, kv_heads, FOVEA_MAX_HEADS);
+  if ((st = check_rotary(N, dim, positions, pos_ld, axes, frequencies, axis, rot)) != FOVEA_OK) return st;
+  if (N == 0) return FOVEA_OK;
+  const int size = dtype == FOVEA_BF16 ? 2 : 4;
+  if ((st = check_heads(q, q_ld, q_hs, heads, size, "q")) != FOVEA_OK) return st;
+  if ((st = check_heads(k, k_ld, k_hs, kv_heads, size, "k")) != FOVEA_OK) return st;
+  NEED_ALIGNED(q_out, size, "q_out");
+  if (kv_heads > 0) NEED_ALIGNED(k_out, size, "k_out");
+  auto dense = [&](long long ld, long long hs, int h) {
+    return (h == 1 || hs == dim) && (N == 1 || ld == (long long)h * dim);
+  };
+  if ((q_out == q && !dense(q_ld, q_hs, heads)) || (kv_heads > 0 && k_out == k && !dense(k_ld, k_hs, kv_heads)))
+    return fail(FOVEA_ERR_INVALID_ARG, "outputs may be the inputs' own memory only where these are dense");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KernelTimer t("rotary_axes", s);
+  FOVEA_CUDA(launch_rotary(dtype, HeadRows{q, q_ld, q_hs, heads}, HeadRows{k, k_ld, k_hs, kv_heads}, N, dim,
+                           rotary_args(positions, pos_ld, axes, frequencies, axis, rot, adjacent, inverse), q_out,
+                           k_out, s), "rotary_axes");
+  return FOVEA_OK;
+}
+
+FOVEA_API fovea_status fovea_cache_append(const void* q, int64_t q_ld, int64_t q_hs, int heads,
+                                          const void* k, int64_t k_ld, int64_t k_hs,
+                                          const void* v, int64_t v_ld, int64_t v_hs, int N,
+                                          int dtype, const int32_t* positions, int64_t pos_ld,
+                                          int axes, const double* frequencies,
+                                          const int32_t* axis, int rot, int adjacent, void* q_out,
+                                          void* k_pages, void* v_pages, int cache_dtype,
+                                          const float* k_scale, const float* v_scale, int n_pages,
+                                          int page, int kv_heads, int dim, const int32_t* table,
+                                          int B, int width, const int32_t* sequence,
+                                          const int32_t* entry, void* stream) {
+  g_last_error.clear();
+  fovea_status st = check_dtype(dtype);
+  if (st != FOVEA_OK) return st;
+  if (N < 0) return fail(FOVEA_ERR_INVALID_ARG, "N = %d < 0", N);
+  const CachePages c{k_pages, v_pages, cache_dtype, n_pages, page, kv_heads, dim, k_scale, v_scale, table, B, width};
+  if ((st = check_cache(c, dtype)) != FOVEA_OK) return st;
+  if (q == nullptr) heads = 0;
+  else if (heads < 1) return fail(FOVEA_ERR_INVALID_ARG, "heads = %d < 1", heads);
+  if (heads > FOVEA_MAX_HEADS || 2 * kv_heads > FOVEA_MAX_HEADS - heads)
+    return fail(FOVEA_ERR_UNSUPPORTED, "heads %d and twice kv_heads %d > %d", heads, kv_heads, FOVEA_MAX_HEADS);
+  if (rot != 0) {
+    st = check_rotary(N, dim, positions, pos_ld, axes, frequencies, axis, rot);
+    if (st != FOVEA_OK) return st;
+  } else if (q != nullptr) {
+    return fail(FOVEA_ERR_INVALID_ARG, "q is rotated or NULL: rot is 0");
+  }
+  if (N == 0) return FOVEA_OK;
+  const int size = dtype == FOVEA_BF16 ? 2 : 4;
+  if ((st = check_heads(q, q_ld, q_hs, heads, size, "q")) != FOVEA_OK) return st;
+  if ((st = check_heads(k, k_ld, k_hs, kv_heads, size, "k")) != FOVEA_OK) return st;
+  if ((st = check_heads(v, v_ld, v_hs, kv_heads, size, "v")) != FOVEA_OK) return st;
+  if (heads > 0) {
+    NEED_ALIGNED(q_out, size, "q_out");
+    if (q_out == q && !((heads == 1 || q_hs == dim) && (N == 1 || q_ld == (long long)heads * dim)))
+      return fail(FOVEA_ERR_INVALID_ARG, "q_out may be q's own memory only where q is dense");
+  }
+  NEED_ALIGNED(sequence, 4, "sequence");
+  NEED_ALIGNED(entry, 4, "entry");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KernelTimer t("cache_append", s);
+  FOVEA_CUDA(launch_cache_append(dtype, HeadRows{q, q_ld, q_hs, heads}, HeadRows{k, k_ld, k_hs, kv_heads},
+                                 HeadRows{v, v_ld, v_hs, kv_heads}, N,
+                                 rotary_args(positions, pos_ld, axes, frequencies, axis, rot, adjacent, 0), c,
+                                 sequence, entry, q_out, s), "cache_append");
+  return FOVEA_OK;
+}
+
+static fovea_status check_attention(int B, int nodes, int heads, int kv_heads, int dim, int cache_dtype) {
+  if (cache_dtype != FOVEA_BF16 && cache_dtype != FOVEA_FP32 && cache_dtype != FOVEA_E4M3)
+    return fail(FOVEA_ERR_INVALID_ARG, "cache_dtype %d is not FOVEA_BF16, FOVEA_FP32 or FOVEA_E4M3", cache_dtype);
+  if (B < 0) return fail(FOVEA_ERR_INVALID_ARG, "B = %d < 0", B);
+  if (dim != 64 && dim != 128 && dim != 256)
+    return fail(FOVEA_ERR_UNSUPPORTED, "dim %d is not 64, 128 or 256", dim);
+  if (nodes < 1) return fail(FOVEA_ERR_INVALID_ARG, "nodes = %d < 1", nodes);
+  if (nodes > FOVEA_MAX_TREE) return fail(FOVEA_ERR_UNSUPPORTED, "nodes %d > %d", nodes, FOVEA_MAX_TREE);
+  if (kv_heads < 1 || heads < 1 || heads % kv_heads != 0)
+    return fail(FOVEA_ERR_INVALID_ARG, "heads %d must be a positive multiple of kv_heads %d", heads, kv_heads);
+  if (heads > FOVEA_MAX_HEADS) return fail(FOVEA_ERR_UNSUPPORTED, "heads %d > %d", heads, FOVEA_MAX_HEADS);
+  return FOVEA_OK;
+}
+
+FOVEA_API fovea_status fovea_paged_attention(const void* q, int64_t q_ld, int64_t q_hs, int heads,
+                                             const void* k_pages, const void* v_pages,
+                                             int cache_dtype, const float* k_scale,
+                                             const float* v_scale, int n_pages, int page,
+                                             int kv_heads, int dim, const int32_t* table, int B,
+                                             int width, const int32_t* lens, int nodes,
+                                             const int32_t* tree, int tree_rows, float scale,
+                                             void* out, float* lse, void* workspace,
+                                             size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  const CachePages c{const_cast<void*>(k_pages), const_cast<void*>(v_pages), cache_dtype, n_pages, page, kv_heads,
+                     dim, k_scale, v_scale, table, B, width};
+  fovea_status st = check_cache(c, -1);
+  if (st == FOVEA_OK) st = check_attention(B, nodes, heads, kv_heads, dim, cache_dtype);
+  if (st != FOVEA_OK) return st;
+  if (tree != nullptr && tree_rows != 1 && tree_rows != B)
+    return fail(FOVEA_ERR_INVALID_ARG, "tree_rows %d is neither 1 nor B = %d", tree_rows, B);
+  if (!(fabsf(scale) <= 3.4028235e38f)) return fail(FOVEA_ERR_INVALID_ARG, "scale must be finite");
+  if (B == 0) return FOVEA_OK;
+  const int size = cache_dtype == FOVEA_FP32 ? 4 : 2;
+  if ((st = check_heads(q, q_ld, q_hs, heads, size, "q")) != FOVEA_OK) return st;
+  NEED_ALIGNED(lens, 4, "lens");
+  WANT_ALIGNED(tree, 4, "tree");
+  NEED_ALIGNED(out, 16, "out");
+  WANT_ALIGNED(lse, 4, "lse");
+  PagedArgs a{};
+  a.q = q; a.q_ld = q_ld; a.q_hs = q_hs;
+  a.k_pages = k_pages; a.v_pages = v_pages;
+  a.cache_dtype = cache_dtype; a.n_pages = n_pages; a.page = page; a.kv_heads = kv_heads; a.dim = dim;
+  a.k_scale = k_scale; a.v_scale = v_scale;
+  a.table = table; a.width = width; a.lens = lens; a.B = B;
+  a.nodes = nodes; a.heads = heads; a.group = heads / kv_heads;
+  a.tree = reinterpret_cast<const uint32_t*>(tree); a.tree_rows = tree_rows; a.words = (nodes + 31) / 32;
+  a.scale = scale;
+  a.out = out; a.lse = lse;
+  a.workspace = workspace;
+  const size_t need = paged_attention_workspace(a);
+  NEED_ALIGNED(workspace, 256, "workspace");
+  if (workspace_bytes < need)
+    return fail(FOVEA_ERR_INVALID_ARG, "workspace has %zu bytes, needs %zu (fovea_paged_attention_workspace_size)",
+                workspace_bytes, need);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KernelTimer t("paged_attention", s);
+  FOVEA_CUDA(launch_paged_attention(a, s), "paged_attention");
+  return FOVEA_OK;
+}
+
+FOVEA_API fovea_status fovea_paged_attention_workspace_size(int B, int nodes, int heads,
+                                                            int kv_heads, int dim, int cache_dtype,
+                                                            size_t* bytes) {
+  g_last_error.clear();
+  if (bytes == nullptr) return fail(FOVEA_ERR_INVALID_ARG, "bytes is NULL");
+  const fovea_status st = check_attention(B, nodes, heads, kv_heads, dim, cache_dtype);
+  if (st != FOVEA_OK) return st;
+  PagedArgs a{};
+  a.cache_dtype = cache_dtype; a.dim = dim; a.B = B; a.nodes = nodes;
+  a.heads = heads; a.kv_heads = kv_heads; a.group = heads / kv_heads;
+  *bytes = paged_attention_workspace(a);
+  return FOVEA_OK;
+}
+
+FOVEA_API fovea_status fovea_cache_keep(void* k_pages, void* v_pages, int cache_dtype, int n_pages,
+                                        int page, int kv_heads, int dim, const int32_t* table,
+                                        int B, int width, const int32_t* lens,
+                                        const int32_t* nodes, int path, int size,
+                                        int32_t* new_lens, void* stream) {
+  g_last_error.clear();
+  const CachePages c{k_pages, v_pages, cache_dtype, n_pages, page, kv_heads, dim, nullptr, nullptr, table, B, width};
+  const fovea_status st = check_cache(c, -1);
+  if (st != FOVEA_OK) return st;
+  if (path < 1 || path > size)
+    return fail(FOVEA_ERR_INVALID_ARG, "path %d must lie in [1, size = %d]", path, size);
+  if (size > FOVEA_MAX_TREE) return fail(FOVEA_ERR_UNSUPPORTED, "size %d > %d", size, FOVEA_MAX_TREE);
+  if (B == 0) return FOVEA_OK;
+  NEED_ALIGNED(lens, 4, "lens");
+  NEED_ALIGNED(nodes, 4, "nodes");
+  NEED_ALIGNED(new_lens, 4, "new_lens");
+  if (new_lens == lens) return fail(FOVEA_ERR_INVALID_ARG, "new_lens must not be lens' own memory");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KernelTimer t("cache_keep", s);
+  FOVEA_CUDA(launch_cache_keep(c, lens, nodes, path, size, new_lens, s), "cache_keep");
+  return FOVEA_OK;
+}
+
+FOVEA_API fovea_status fovea_cache_fork(void* k_pages, void* v_pages, int cache_dtype, int n_pages,
+                                        int page, int kv_heads, int dim, const int32_t* table,
+                                        int B, int width, const int32_t* lens,
+                                        const int32_t* parents, const int32_t* keep,
+                                        const int32_t* room, int C, int32_t* new_table,
+                                        int new_width, int32_t* new_lens, int32_t* free_pages,
+                                        void* stream) {
+  g_last_error.clear();
+  const CachePages c{k_pages, v_pages, cache_dtype, n_pages, page, kv_heads, dim, nullptr, nullptr, table, B, width};
+  const fovea_status st = check_cache(c, -1);
+  if (st != FOVEA_OK) return st;
+  if (C < 0 || new_width < 1)
+    return fail(FOVEA_ERR_INVALID_ARG, "the new table's sizes %d and %d must be at least 0 and 1", C, new_width);
+  if (C > FOVEA_MAX_CACHE_SEQ) return fail(FOVEA_ERR_UNSUPPORTED, "%d continuations > %d", C, FOVEA_MAX_CACHE_SEQ);
+  if (n_pages > FOVEA_MAX_PAGES) return fail(FOVEA_ERR_UNSUPPORTED, "n_pages %d > %d", n_pages, FOVEA_MAX_PAGES);
+  if ((long long)new_width * page > (1ll << 30))
+    return fail(FOVEA_ERR_UNSUPPORTED, "tables of %d pages of %d entries", new_width, page);
+  NEED_ALIGNED(free_pages, 4, "free_pages");
+  if (C > 0) {
+    if (B > 0) NEED_ALIGNED(lens, 4, "lens");
+    NEED_ALIGNED(parents, 4, "parents");
+    NEED_ALIGNED(new_table, 4, "new_table");
+    NEED_ALIGNED(new_lens, 4, "new_lens");
+  }
+  WANT_ALIGNED(keep, 4, "keep");
+  WANT_ALIGNED(room, 4, "room");
+  if (C > 0 && B > 0 && (new_table == table || new_lens == lens))
+    return fail(FOVEA_ERR_INVALID_ARG, "new_table and new_lens must not be the old ones' memory");
+  ForkArgs f{};
+  f.lens = lens; f.parents = parents; f.keep = keep; f.room = room; f.C = C;
+  f.new_table = new_table; f.new_width = new_width; f.new_lens = new_lens; f.free = free_pages;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KernelTimer t("cache_fork", s);
+  FOVEA_CUDA(launch_cache_fork(c, f, s), "cache_fork");
+  return FOVEA_OK;
+}
+
 FOVEA_API fovea_status fovea_timing_enable(int enable) {
   std::lock_guard<std::mutex> lk(g_tmu);
   for (auto& r : g_recs) {

@@ -467,6 +467,60 @@ struct ScoreGradArgs {
 };
 cudaError_t launch_token_logprobs_grad(int dtype, const ScoreGradArgs& a, cudaStream_t s);
 
+// Rotary positions (rotary.cu) of rows [N, heads, dim] with strides, and new entries of a
+// paged cache.  `phi` of pair j of token n is positions[axis[j] * pos_ld + n] * frequencies[j].
+struct RotaryArgs {
+  const int32_t* positions; long long pos_ld;
+  const double* frequencies; const int32_t* axis;
+  int axes, rot;                                   // rot: rotated dims, 0: none
+  int adjacent, inverse;
+};
+struct HeadRows { const void* x; long long ld, hs; int heads; };   // strides of tokens and heads, elements
+constexpr int kRotaryPairs = 256;                  // pairs of a head, at most
+// q and k rotated to dense q_out and k_out (null: none of them).
+cudaError_t launch_rotary(int dtype, const HeadRows& q, const HeadRows& k, int N, int dim, const RotaryArgs& r,
+                          void* q_out, void* k_out, cudaStream_t s);
+// A cache's pages [n_pages, kv_heads, page, dim] and the sequences' tables [B, width] of them.
+struct CachePages {
+  void* k; void* v;
+  int dtype, n_pages, page, kv_heads, dim;
+  const float* k_scale; const float* v_scale;      // e4m3: of each head (null: 1)
+  const int32_t* table; int B, width;
+};
+// k (rotated when r.rot > 0) and v of N tokens to entry[n] of sequence[n], q rotated to q_out (q.heads 0: none).
+cudaError_t launch_cache_append(int dtype, const HeadRows& q, const HeadRows& k, const HeadRows& v, int N,
+                                const RotaryArgs& r, const CachePages& c, const int32_t* sequence,
+                                const int32_t* entry, void* q_out, cudaStream_t s);
+// Accepted nodes of the last `size` entries moved to the front of them (pages.cu).
+cudaError_t launch_cache_keep(const CachePages& c, const int32_t* lens, const int32_t* nodes, int path, int size,
+                              int32_t* new_lens, cudaStream_t s);
+// Sequences continued, forked and dropped by their pages (pages.cu).
+struct ForkArgs {
+  const int32_t* lens; const int32_t* parents; const int32_t* keep; const int32_t* room;
+  int C;
+  int32_t* new_table; int new_width;
+  int32_t* new_lens; int32_t* free;
+};
+cudaError_t launch_cache_fork(const CachePages& c, const ForkArgs& f, cudaStream_t s);
+
+// Attention of the newest entries over a paged cache (paged.cu).
+struct PagedArgs {
+  const void* q; long long q_ld, q_hs;             // [B * nodes, heads, dim]
+  const void* k_pages; const void* v_pages;
+  int cache_dtype, n_pages, page, kv_heads, dim;
+  const float* k_scale; const float* v_scale;
+  const int32_t* table; int width;
+  const int32_t* lens; int B;
+  int nodes, heads, group;
+  const uint32_t* tree; int tree_rows, words;      // null: a node sees itself and the ones before it
+  float scale;
+  void* out; float* lse;
+  void* workspace;
+  int row_blocks;                                  // of a key head (set by the launch)
+};
+size_t paged_attention_workspace(const PagedArgs& a);
+cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s);
+
 // The memory build's GEMMs out[i] = R . F[i]^T on CTA pairs (gemm_build.cu):
 // token rows R [rows, K] (R0 for part 0, R1 for the others) against up to
 // three feature matrices F[i] [cols, K] (bf16; a null base: no such part),
