@@ -516,7 +516,9 @@ struct PagedArgs {
   float scale;
   void* out; float* lse;
   void* workspace;
-  int row_blocks;                                  // of a key head (set by the launch)
+  // set by the launch
+  int row_blocks;                                  // of a key head
+  uint32_t page_magic;                             // block / (page / 16) = the high word of block * this; 0: block
 };
 size_t paged_attention_workspace(const PagedArgs& a);
 cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s);

@@ -32,7 +32,7 @@ namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kBlock = 16;           // entries of a block
-constexpr int kLeast = kWarps;       // blocks of a run, at least (a block a warp)
+constexpr int kLeast = kWarps;       // blocks of a run, at least
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_(float x) {
@@ -92,8 +92,14 @@ template <class C, int D> struct Cut {
   static constexpr int kSteps = kSize == 4 ? D / 8 : D / 16;      // of the contraction over dims
 };
 
-// The blocks of all segments as one list: sequence by sequence, key head by key head,
-// rows by rows.
+// A segment's rows are staged and its sums put together, which takes a CTA as long as some
+// blocks: the runs are cut as if each segment had so many empty ones in front.  (The batch
+// of 64 sequences of 0 to 8192 entries, us, with 0 / 4 / 8 / 16 / 24: 85 / 49 / 38 / 36 / 37;
+// eight trees of 32 nodes 204 / 85 / 63 / 46 / 44.)
+template <int RT> constexpr uint32_t kFront = RT == 1 ? 16 : 24;
+
+// The blocks of all segments as one list: sequence by sequence, key head by key head, rows
+// by rows.
 struct Plan {
   uint64_t total;      // blocks
   uint32_t runs;       // that have any
@@ -109,15 +115,17 @@ __device__ __forceinline__ int length_of(const PagedArgs& a, int b) {
   return n < 0 ? 0 : n > most ? (int)most : n;
 }
 __device__ __forceinline__ bool too_long(const PagedArgs& a, int b) { return a.lens[b] > (long long)a.width * a.page; }
-__device__ __forceinline__ uint32_t blocks_of(int len) { return (uint32_t)(len + kBlock - 1) / kBlock; }
+__device__ __forceinline__ uint32_t blocks_of(int len, uint32_t front) {
+  return len > 0 ? (uint32_t)(len + kBlock - 1) / kBlock + front : 0;
+}
 
 // Sums of the sequences' blocks before each (before[0 .. B], in shared memory) and the
 // cut into runs.  All threads of the CTA.
-__device__ Plan make_plan(const PagedArgs& a, uint32_t* before, uint32_t* scratch, int max_runs) {
+__device__ Plan make_plan(const PagedArgs& a, uint32_t* before, uint32_t* scratch, int max_runs, uint32_t front) {
   const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5;
   const int per = (a.B + nt - 1) / nt, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
   uint32_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += blocks_of(length_of(a, b));
+  for (int b = b0; b < b1; ++b) mine += blocks_of(length_of(a, b), front);
   uint32_t sum = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -130,7 +138,7 @@ __device__ Plan make_plan(const PagedArgs& a, uint32_t* before, uint32_t* scratc
   for (int w = 0; w < warp; ++w) base += scratch[w];
   for (int b = b0; b < b1; ++b) {
     before[b] = base;
-    base += blocks_of(length_of(a, b));
+    base += blocks_of(length_of(a, b), front);
   }
   if (b1 == a.B && b0 < b1) before[a.B] = base;
   __syncthreads();
@@ -156,11 +164,15 @@ __device__ __forceinline__ bool sees(const PagedArgs& a, const uint32_t* tree, i
   return (tree[(size_t)node * a.words + (j >> 5)] >> (j & 31)) & 1u;
 }
 
+// Blocks that a warp takes together.
+template <class C, int D, int RT> constexpr int kTogether = sizeof(C) * D * RT <= 128 ? 2 : 1;
+
 template <class C, class Q, int D, int RT>
 struct Attention {
   using G = Cut<C, D>;
   static constexpr bool kF32 = sizeof(C) == 4, kE4 = sizeof(C) == 1;
   static constexpr int kRows = 8 * RT;
+  static constexpr uint32_t kBytes = kBlock * D * sizeof(C);     // of a block
   // p of 8-bit values is held in fp16, times 2^15: its smallest step is then 2^-39
   static constexpr float kLift = kE4 ? 15.0f : 0.0f;
 
@@ -172,9 +184,10 @@ struct Attention {
     alignas(16) float o[kWarps][kRows][D + 4];
   };
 
-  // One block's keys and values as a lane holds them.
-  uint4 k[2][G::kKeyChunks];
-  uint32_t v[4][G::kParts][G::kSpanWords];
+  static constexpr int kSub = kTogether<C, D, RT>;
+  // The keys and values of kSub blocks as a lane holds them.
+  uint4 k[kSub][2][G::kKeyChunks];
+  uint32_t v[kSub][4][G::kParts][G::kSpanWords];
   float o[RT][G::kTiles][4];
   float m[RT][2], l[RT][2];
 
@@ -190,27 +203,34 @@ struct Attention {
   __device__ __forceinline__ static int value_entry(int t, int e) {      // the lane's e-th entry of values
     return kF32 ? t + 4 * e : 2 * t + (e & 1) + 8 * (e >> 1);
   }
-  __device__ __forceinline__ void load_keys(const C* base) {             // base: the block's first entry
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  // `at`: the lane's first byte of the block (keys_from and values_from behind its start).
+  __device__ __forceinline__ static uint32_t keys_from() {
+    const int lane = threadIdx.x & 31;
+    return ((lane >> 2) * D + (lane & 3) * G::kUnit) * G::kSize;
+  }
+  __device__ __forceinline__ static uint32_t values_from() {
+    const int lane = threadIdx.x & 31;
+    return (value_entry(lane & 3, 0) * D + (lane >> 2) * G::kSpan) * G::kSize;
+  }
+  __device__ __forceinline__ void load_keys(int u, const uint8_t* at) {
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int j = 0; j < G::kKeyChunks; ++j)
-        k[e][j] = __ldg(reinterpret_cast<const uint4*>(base + (size_t)(g + 8 * e) * D + (4 * j + t) * G::kUnit));
+        k[u][e][j] = __ldg(reinterpret_cast<const uint4*>(at + 8 * e * D * G::kSize + 64 * j));
   }
-  __device__ __forceinline__ void load_values(const C* base) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  __device__ __forceinline__ void load_values(int u, const uint8_t* at) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int p = 0; p < G::kParts; ++p) {
-        const C* at = base + (size_t)value_entry(t, e) * D + p * 8 * G::kSpan + g * G::kSpan;
+        const uint8_t* q = at + (value_entry(0, e) * D + p * 8 * G::kSpan) * G::kSize;
         if constexpr (G::kSpanWords == 4) {
-          const uint4 x = __ldg(reinterpret_cast<const uint4*>(at));
-          v[e][p][0] = x.x; v[e][p][1] = x.y; v[e][p][2] = x.z; v[e][p][3] = x.w;
+          const uint4 x = __ldg(reinterpret_cast<const uint4*>(q));
+          v[u][e][p][0] = x.x; v[u][e][p][1] = x.y; v[u][e][p][2] = x.z; v[u][e][p][3] = x.w;
         } else {
-          const uint2 x = __ldg(reinterpret_cast<const uint2*>(at));
-          v[e][p][0] = x.x; v[e][p][1] = x.y;
+          const uint2 x = __ldg(reinterpret_cast<const uint2*>(q));
+          v[u][e][p][0] = x.x; v[u][e][p][1] = x.y;
         }
       }
   }
@@ -219,7 +239,7 @@ struct Attention {
   }
 
   // S^T of the block: s[r][0..3] = entries g, g, g + 8, g + 8 by rows 2t, 2t + 1, 2t, 2t + 1.
-  __device__ __forceinline__ void scores(const Shared& sh, float (&s)[RT][4]) const {
+  __device__ __forceinline__ void scores(int u, const Shared& sh, float (&s)[RT][4]) const {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int r = 0; r < RT; ++r) s[r][0] = s[r][1] = s[r][2] = s[r][3] = 0.0f;
@@ -237,7 +257,7 @@ struct Attention {
 #pragma unroll
         for (int i = c; i < c + 4; ++i) {
           const int j = i >> 1, h = 2 * (i & 1);
-          const uint32_t x[4] = {word(k[0][j], h), word(k[1][j], h), word(k[0][j], h + 1), word(k[1][j], h + 1)};
+          const uint32_t x[4] = {word(k[u][0][j], h), word(k[u][1][j], h), word(k[u][0][j], h + 1), word(k[u][1][j], h + 1)};
           uint32_t hi[4], lo[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) split_tf32(x[e], hi[e], lo[e]);
@@ -266,13 +286,13 @@ struct Attention {
       for (int i = 0; i < G::kSteps; ++i) {
         uint32_t a[4];
         if constexpr (kE4) {
-          const uint32_t x = word(k[0][i >> 2], i & 3), y = word(k[1][i >> 2], i & 3);
+          const uint32_t x = word(k[u][0][i >> 2], i & 3), y = word(k[u][1][i >> 2], i & 3);
           a[0] = halves_of_e4m3(x & 0xFFFFu); a[1] = halves_of_e4m3(y & 0xFFFFu);
           a[2] = halves_of_e4m3(x >> 16);     a[3] = halves_of_e4m3(y >> 16);
         } else {
           const int j = i >> 1, h = 2 * (i & 1);
-          a[0] = word(k[0][j], h); a[1] = word(k[1][j], h);
-          a[2] = word(k[0][j], h + 1); a[3] = word(k[1][j], h + 1);
+          a[0] = word(k[u][0][j], h); a[1] = word(k[u][1][j], h);
+          a[2] = word(k[u][0][j], h + 1); a[3] = word(k[u][1][j], h + 1);
         }
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
@@ -284,24 +304,25 @@ struct Attention {
   }
 
   // The values' fragment of a tile of 16 dims (dims 2i and 2i + 1 of the spans, i = tile
-  // within the part): a[0..3] of the entries 2t, 2t + 1 and 2t + 8, 2t + 9.
-  __device__ __forceinline__ void value_tile(int tile, uint32_t (&f)[4]) const {
+  // within the part): f[0..3] of the entries 2t, 2t + 1 and 2t + 8, 2t + 9.
+  __device__ __forceinline__ void value_tile(int u, int tile, uint32_t (&f)[4]) const {
     constexpr int kPer = G::kSpan / 2;                     // tiles of a part
     const int p = tile / kPer, i = tile % kPer;
-    uint32_t x[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if constexpr (kE4) x[e] = halves_of_e4m3(i & 1 ? v[e][p][i >> 1] >> 16 : v[e][p][i >> 1] & 0xFFFFu);
-      else x[e] = v[e][p][i];
+    for (int e = 0; e < 4; e += 2) {
+      if constexpr (kE4) {                                 // bytes of two entries side by side, then to fp16
+        const uint32_t x = __byte_perm(v[u][e][p][i >> 1], v[u][e + 1][p][i >> 1], i & 1 ? 0x7362 : 0x5140);
+        f[e] = halves_of_e4m3(x & 0xFFFFu);
+        f[e + 1] = halves_of_e4m3(x >> 16);
+      } else {
+        f[e] = low_halves(v[u][e][p][i], v[u][e + 1][p][i]);
+        f[e + 1] = high_halves(v[u][e][p][i], v[u][e + 1][p][i]);
+      }
     }
-    f[0] = low_halves(x[0], x[1]);
-    f[1] = high_halves(x[0], x[1]);
-    f[2] = low_halves(x[2], x[3]);
-    f[3] = high_halves(x[2], x[3]);
   }
 
   // O^T += V^T P^T; p in S^T's layout.
-  __device__ __forceinline__ void add_values(const float (&p)[RT][4]) {
+  __device__ __forceinline__ void add_values(int u, const float (&p)[RT][4]) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     if constexpr (kF32) {
       uint32_t bh[RT][4], bl[RT][4];                       // entries t, t + 4, t + 8, t + 12 of row g
@@ -323,10 +344,10 @@ struct Attention {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           uint32_t hi[4], lo[4];
-          split_tf32(v[2 * c][part][w], hi[0], lo[0]);
-          split_tf32(v[2 * c][part][w + 1], hi[1], lo[1]);
-          split_tf32(v[2 * c + 1][part][w], hi[2], lo[2]);
-          split_tf32(v[2 * c + 1][part][w + 1], hi[3], lo[3]);
+          split_tf32(v[u][2 * c][part][w], hi[0], lo[0]);
+          split_tf32(v[u][2 * c][part][w + 1], hi[1], lo[1]);
+          split_tf32(v[u][2 * c + 1][part][w], hi[2], lo[2]);
+          split_tf32(v[u][2 * c + 1][part][w + 1], hi[3], lo[3]);
 #pragma unroll
           for (int r = 0; r < RT; ++r) {
             mma_tf32(sum[r], lo, bh[r][2 * c], bh[r][2 * c + 1]);
@@ -363,7 +384,7 @@ struct Attention {
 #pragma unroll
       for (int i = 0; i < G::kTiles; ++i) {
         uint32_t f[4];
-        value_tile(i, f);
+        value_tile(u, i, f);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
           mma16<kE4>(o[r][i], f, bh[r][0], bh[r][1]);
@@ -374,7 +395,7 @@ struct Attention {
   }
 
   // Values of entries from `left` on are cleared: what stands there is not used.
-  __device__ __forceinline__ void clear_values(int left) {
+  __device__ __forceinline__ void clear_values(int u, int left) {
     const int t = threadIdx.x & 3;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -382,13 +403,13 @@ struct Attention {
 #pragma unroll
         for (int p = 0; p < G::kParts; ++p)
 #pragma unroll
-          for (int w = 0; w < G::kSpanWords; ++w) v[e][p][w] = 0;
+          for (int w = 0; w < G::kSpanWords; ++w) v[u][e][p][w] = 0;
   }
 
   // Values that are infinite or NaN, where only some rows see an entry: a product with a
   // p of 0 would give NaN to the others.  They are cleared here, and the rows that see one
   // take it when the segment is finished.  True where there was one.
-  __device__ __forceinline__ bool clear_odd_values() {
+  __device__ __forceinline__ bool clear_odd_values(int u) {
     uint32_t any = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -396,7 +417,7 @@ struct Attention {
       for (int p = 0; p < G::kParts; ++p)
 #pragma unroll
         for (int w = 0; w < G::kSpanWords; ++w) {
-          uint32_t& x = v[e][p][w];
+          uint32_t& x = v[u][e][p][w];
           uint32_t odd;
           if constexpr (kF32) odd = (x & 0x7F800000u) == 0x7F800000u ? 0xFFFFFFFFu : 0u;
           else if constexpr (kE4) odd = __vcmpeq4(x & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
@@ -474,13 +495,15 @@ struct Attention {
     }
   }
 
-  // Blocks [lo, hi) of one segment, by all warps in turn.
+  // Blocks [lo, hi) of one segment, kSub by each warp in turn.
   __device__ __forceinline__ void blocks(const PagedArgs& a, Shared& sh, int b, int h, int row0, int n,
                                          uint32_t lo, uint32_t hi) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const uint32_t* tree = tree_of(a, b);
     const int32_t* table = a.table + (size_t)b * a.width;
-    const uint32_t per_page = a.page / kBlock;
+    const uint32_t per_page = a.page / kBlock, stride = a.kv_heads * per_page;
+    const uint8_t* keys = static_cast<const uint8_t*>(a.k_pages) + (size_t)h * per_page * kBytes + keys_from();
+    const uint8_t* values = static_cast<const uint8_t*>(a.v_pages) + (size_t)h * per_page * kBytes + values_from();
     const float factor = a.scale * kLog2e * (kE4 && a.k_scale != nullptr ? a.k_scale[h] : 1.0f);
     float f[RT][2];
 #pragma unroll
@@ -488,41 +511,78 @@ struct Attention {
 #pragma unroll
       for (int e = 0; e < 2; ++e) f[r][e] = kE4 ? factor * sh.row_scale[8 * r + 2 * t + e] : factor;
     clear();
-    uint32_t at = lo + warp;
+    uint32_t at = lo + warp * kSub;
     if (at >= hi) return;
-    int page = table[at / per_page];
-    bool bad = (unsigned)page >= (unsigned)a.n_pages;
-    size_t off = (((size_t)(bad ? 0 : page) * a.kv_heads + h) * a.page + (at % per_page) * kBlock) * D;
-    load_keys(static_cast<const C*>(a.k_pages) + off);
+    // Where a block's page stands in the table and where the block in its page: a page has
+    // 1 to 64 blocks and a sequence fewer than 2^26, for which the product is exact.
+    auto page_of = [&](uint32_t block) { return a.page_magic == 0 ? block : __umulhi(block, a.page_magic); };
+    int id[kSub];
+    uint32_t in_page[kSub];
+    auto look_up = [&](uint32_t first) {
+#pragma unroll
+      for (int u = 0; u < kSub; ++u) {
+        const uint32_t block = u == 0 ? first : min(first + u, hi - 1), p = page_of(block);
+        id[u] = table[p];
+        in_page[u] = block - p * per_page;
+      }
+    };
+    unsigned long long off[kSub];                          // bytes from the pools' lane pointers
+    bool bad = false;                                      // a page is not in the pool
+    auto place = [&]() {
+      bad = false;
+#pragma unroll
+      for (int u = 0; u < kSub; ++u) {
+        const bool out = (unsigned)id[u] >= (unsigned)a.n_pages;
+        bad |= out;
+        off[u] = ((unsigned long long)(out ? 0u : (uint32_t)id[u]) * stride + in_page[u]) * kBytes;
+      }
+    };
+    look_up(at);
+    place();
+#pragma unroll
+    for (int u = 0; u < kSub; ++u) load_keys(u, keys + off[u]);
+    const int end = min(n, (int)(hi * kBlock));            // the run's last entry
+    const int plain = min(end, n - a.nodes + (a.nodes == 1 && tree == nullptr));   // up to here all rows see all
     while (true) {
-      load_values(static_cast<const C*>(a.v_pages) + off);
-      const uint32_t next = at + kWarps;
-      int next_page = 0;
-      if (next < hi) next_page = table[next / per_page];
-      float s[RT][4];
-      scores(sh, s);
-      const bool next_bad = (unsigned)next_page >= (unsigned)a.n_pages;
-      if (next < hi) {
-        off = (((size_t)(next_bad ? 0 : next_page) * a.kv_heads + h) * a.page + (next % per_page) * kBlock) * D;
-        load_keys(static_cast<const C*>(a.k_pages) + off);
+#pragma unroll
+      for (int u = 0; u < kSub; ++u) load_values(u, values + off[u]);
+      const uint32_t next = at + kWarps * kSub;
+      const bool more = next < hi;
+      if (more) look_up(next);
+      float s[kSub][RT][4];
+#pragma unroll
+      for (int u = 0; u < kSub; ++u) scores(u, sh, s[u]);
+      const bool was_bad = bad;
+      if (more) {
+        place();
+#pragma unroll
+        for (int u = 0; u < kSub; ++u) load_keys(u, keys + off[u]);
       }
       const int first = (int)at * kBlock;
-      const bool whole = !bad && first + kBlock <= n - a.nodes + (a.nodes == 1 && tree == nullptr);
 #pragma unroll
-      for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[r][e] *= f[r][e & 1];
-      if (!whole) {
+      for (int u = 0; u < kSub; ++u)
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int node = min((row0 + 8 * r + 2 * t + (e & 1)) / a.group, a.nodes - 1);
-            const bool yes = sees(a, tree, n, node, first + g + 8 * (e >> 1));
-            s[r][e] = yes ? (bad ? NAN : s[r][e]) : -INFINITY;
-          }
-        clear_values(bad ? 0 : n - first);
-        if ((a.nodes > 1 || tree != nullptr) && clear_odd_values()) sh.odd = 1;
+          for (int e = 0; e < 4; ++e) s[u][r][e] *= f[r][e & 1];
+      if (was_bad || first + kSub * kBlock > plain) {
+#pragma unroll
+        for (int u = 0; u < kSub; ++u) {
+          const int start = first + u * kBlock;
+          // which of the block's pages: looked up again, this is rare
+          const bool out = was_bad && start < end && (unsigned)table[page_of(at + u)] >= (unsigned)a.n_pages;
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int node = min((row0 + 8 * r + 2 * t + (e & 1)) / a.group, a.nodes - 1);
+              const int entry = start + g + 8 * (e >> 1);
+              const bool yes = entry < end && sees(a, tree, n, node, entry);
+              s[u][r][e] = yes ? (out ? NAN : s[u][r][e]) : -INFINITY;
+            }
+          clear_values(u, out ? 0 : end - start);
+          if ((a.nodes > 1 || tree != nullptr) && clear_odd_values(u)) sh.odd = 1;
+        }
       }
       // running maxima and sums
       bool moved = false;
@@ -531,7 +591,9 @@ struct Attention {
       for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float x = fmaxf(s[r][e], s[r][e + 2]);
+          float x = fmaxf(s[0][r][e], s[0][r][e + 2]);
+#pragma unroll
+          for (int u = 1; u < kSub; ++u) x = fmaxf(x, fmaxf(s[u][r][e], s[u][r][e + 2]));
 #pragma unroll
           for (int w = 4; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
           top[r][e] = fmaxf(m[r][e], x);
@@ -553,19 +615,21 @@ struct Attention {
             for (int e = 0; e < 4; ++e) o[r][i][e] *= c[e & 1];
         }
       }
-      float p[RT][4];
 #pragma unroll
-      for (int r = 0; r < RT; ++r)
+      for (int u = 0; u < kSub; ++u) {
+        float p[RT][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float base = m[r][e & 1] == -INFINITY ? 0.0f : m[r][e & 1] - kLift;
-          p[r][e] = exp2_(s[r][e] - base);
-          l[r][e & 1] += p[r][e];
-        }
-      add_values(p);
-      if (next >= hi) break;
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float base = m[r][e & 1] == -INFINITY ? 0.0f : m[r][e & 1] - kLift;
+            p[r][e] = exp2_(s[u][r][e] - base);
+            l[r][e & 1] += p[r][e];
+          }
+        add_values(u, p);
+      }
+      if (!more) break;
       at = next;
-      bad = next_bad;
     }
   }
 
@@ -660,9 +724,10 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_attention_
   uint32_t* before = reinterpret_cast<uint32_t*>(raw + sizeof(typename A::Shared));
   static_assert(offsetof(typename A::Shared, o) % 16 == 0 && sizeof(typename A::Shared) % 16 == 0, "16-byte loads");
   __shared__ uint32_t scratch[kWarps];
+  constexpr uint32_t front = kFront<RT>;
   pdl_wait();
   pdl_trigger();                     // the joining kernel makes the same plan meanwhile
-  const Plan plan = make_plan(a, before, scratch, (int)gridDim.x);
+  const Plan plan = make_plan(a, before, scratch, (int)gridDim.x, front);
   if (blockIdx.x >= plan.runs) return;
   const uint64_t from = plan.start(blockIdx.x), to = plan.start(blockIdx.x + 1);
   const uint32_t segments = a.kv_heads * a.row_blocks;    // of a sequence
@@ -680,18 +745,20 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_attention_
     while ((uint64_t)before[b + 1] * segments <= u) ++b;
     const uint32_t count = before[b + 1] - before[b];
     const uint64_t within = u - (uint64_t)before[b] * segments;
-    const uint32_t seg = (uint32_t)(within / count), lo = (uint32_t)(within % count);
-    const uint32_t hi = (uint32_t)min((uint64_t)count, lo + (to - u));
+    const uint32_t seg = (uint32_t)(within / count), first = (uint32_t)(within % count);
+    const uint32_t end = (uint32_t)min((uint64_t)count, first + (to - u));
+    // a segment that begins before or with this run goes to its first slot, a later one to its second
+    const bool begun = u - first <= from;
+    u += end - first;
+    if (end <= front) continue;
+    const uint32_t lo = max(first, front) - front, hi = end - front;
     const int h = seg / a.row_blocks, row0 = (seg % a.row_blocks) * A::kRows;
     A::stage_rows(a, sh, b, h, row0);
     __syncthreads();
     const int n = length_of(a, b);
     at.blocks(a, sh, b, h, row0, n, lo, hi);
-    // a segment that begins before or with this run goes to its first slot, a later one to its second
-    const bool begun = u - lo <= from;
-    at.finish(a, sh, b, h, row0, n, lo, hi, lo == 0 && hi == count, slots + (begun ? 0 : A::kRows * (D + 2)));
+    at.finish(a, sh, b, h, row0, n, lo, hi, lo == 0 && hi == count - front, slots + (begun ? 0 : A::kRows * (D + 2)));
     __syncthreads();
-    u += hi - lo;
   }
 }
 
@@ -703,8 +770,9 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
   extern __shared__ __align__(16) uint8_t raw[];
   uint32_t* before = reinterpret_cast<uint32_t*>(raw);
   __shared__ uint32_t scratch[kWarps];
+  constexpr uint32_t front = kFront<RT>;
   const int lane = threadIdx.x & 31;
-  const Plan plan = make_plan(a, before, scratch, runs);
+  const Plan plan = make_plan(a, before, scratch, runs, front);
   pdl_wait();
   const long long rows = (long long)a.B * a.nodes * a.heads;
   for (long long i = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * kWarps) {
@@ -719,7 +787,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
       continue;
     }
     const uint64_t s0 = (uint64_t)before[b] * segments + (uint64_t)(h * a.row_blocks + row / A::kRows) * count;
-    const uint32_t first = plan.run_of(s0), last = plan.run_of(s0 + count - 1);
+    const uint32_t first = plan.run_of(s0 + front), last = plan.run_of(s0 + count - 1);
     if (first == last) continue;     // written already
     const float* base = static_cast<const float*>(a.workspace);
     const int r = row % A::kRows;
@@ -766,6 +834,8 @@ template <class C, int D> constexpr int most_tiles() {
 template <class C, class Q, int D, int RT>
 cudaError_t launch_as(PagedArgs a, cudaStream_t s, size_t* workspace) {
   using A = Attention<C, Q, D, RT>;
+  const uint32_t per_page = a.page / kBlock;
+  a.page_magic = per_page <= 1 ? 0 : (uint32_t)((1ull << 32) / per_page + 1);
   a.row_blocks = (a.nodes * a.group + A::kRows - 1) / A::kRows;
   const size_t plan_bytes = ((size_t)a.B + 1) * 4;
   const size_t smem = sizeof(typename A::Shared) + plan_bytes;
