@@ -1,8 +1,11 @@
-"""Build libfovea.so (the C-ABI library) in-tree for sm_103a with nvcc.
+"""Build libfovea.so (the C-ABI library) in-tree for sm_103a with nvcc, and beside
+it fovea_binding.so, the Python module of the drafter's cache.
 
-Each CUDA translation unit under csrc/ is compiled in parallel, then linked
-into ``paper_2608_22883_gb300/_lib/libfovea.so``.  Objects go to ``_build/``
-at the repository root.  Both outputs are git-ignored.
+Each translation unit under csrc/ is compiled in parallel, then linked into
+``paper_2608_22883_gb300/_lib/libfovea.so`` (the CUDA ones) and
+``_lib/fovea_binding.so`` (binding.cpp, with torch's headers and the host
+compiler).  Objects go to ``_build/`` at the repository root.  All of it is
+git-ignored.
 """
 
 from __future__ import annotations
@@ -12,6 +15,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -20,6 +24,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libfovea.so")
+BINDING = os.path.join(LIBDIR, "fovea_binding.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CFLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC,-fvisibility=hidden",
@@ -35,6 +40,20 @@ def nvcc() -> str:
 
 def sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
+
+
+def binding_flags():
+    """(flags to compile binding.cpp, flags to link it) against the torch that is installed."""
+    import torch
+    home = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(nvcc()))
+    compile_flags = ["-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                     "-I", INCLUDE, "-isystem", os.path.join(home, "include"),
+                     "-isystem", os.path.join(home, "include", "torch", "csrc", "api", "include"),
+                     "-isystem", os.path.join(cuda, "include"), "-isystem", sysconfig.get_paths()["include"]]
+    link_flags = ["-L", LIBDIR, "-lfovea", "-Wl,-rpath,$ORIGIN", "-L", os.path.join(home, "lib"), "-ltorch_python",
+                  "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    return compile_flags, link_flags
 
 
 def _newer(out: str, deps) -> bool:
@@ -61,6 +80,13 @@ def build(verbose: bool = False, force: bool = False, extra_flags=()) -> str:
         if force or not _newer(obj, [src] + headers):
             jobs.append([cc, *ARCH, *CFLAGS, *extra_flags, "-c", src, "-o", obj])
 
+    compile_flags, link_flags = binding_flags()
+    cxx = os.environ.get("CXX") or shutil.which("g++")
+    source, binding = os.path.join(CSRC, "binding.cpp"), os.path.join(BUILD, "binding.o")
+    if force or not _newer(binding, [source] + headers):
+        # first: it takes as long as the longest of the others
+        jobs.insert(0, [cxx, *compile_flags, "-c", source, "-o", binding])
+
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
         return cmd, r
@@ -71,14 +97,16 @@ def build(verbose: bool = False, force: bool = False, extra_flags=()) -> str:
                 if verbose or r.returncode != 0:
                     sys.stderr.write(" ".join(cmd) + "\n" + r.stdout + r.stderr)
                 if r.returncode != 0:
-                    raise RuntimeError(f"nvcc failed on {cmd[-3]}")
-    if force or jobs or not _newer(LIB, objs):
-        cmd = [cc, *ARCH, "-shared", "-o", LIB, *objs, "-lpthread", "-ldl", "-lrt"]
-        r = subprocess.run(cmd, capture_output=True, text=True)
+                    raise RuntimeError(f"{os.path.basename(cmd[0])} failed on {cmd[-3]}")
+    for out, parts, cmd in ((LIB, objs, [cc, *ARCH, "-shared", "-o", LIB, *objs, "-lpthread", "-ldl", "-lrt"]),
+                            (BINDING, [binding, LIB], [cxx, "-shared", "-o", BINDING, binding, *link_flags])):
+        if not force and not jobs and _newer(out, parts):
+            continue
+        _, r = run(cmd)
         if verbose or r.returncode != 0:
             sys.stderr.write(" ".join(cmd) + "\n" + r.stdout + r.stderr)
         if r.returncode != 0:
-            raise RuntimeError("linking libfovea.so failed")
+            raise RuntimeError(f"linking {os.path.basename(out)} failed")
     return LIB
 
 

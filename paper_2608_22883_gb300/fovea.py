@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import importlib.util
 import os
 from typing import Dict, Optional
 
@@ -729,56 +730,44 @@ def token_logprobs_grad(logits: torch.Tensor, stats: torch.Tensor, entropy: torc
 # Operators of the drafter's cache.  All tensors of a call are on the current device.
 # ---------------------------------------------------------------------------
 
-def _need_heads(name: str, t, dtypes, device: Optional[int] = None):
-    """t is a CUDA tensor [N, heads, dim] of one of these types whose heads are contiguous:
-    its shape, its strides of tokens and heads."""
-    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.dim() != 3 \
-            or (not t.is_cuda if device is None else t.get_device() != device):
-        _refuse(name, t, (None, None, None), dtypes, False, device)
-    n, h, d = t.shape
-    ld, hs, inner = t.stride()
-    if inner != 1 and d > 1:
-        raise ValueError(f"{name} must be contiguous along its heads")
-    return n, h, d, ld, hs
+_native = None
 
 
-def _need_pages(k_pages, v_pages, table, k_scale, v_scale, device: int):
-    """What the calls on a cache check of it; returns its part of the C arguments with the
-    scales (k_pages .. width)."""
-    if not isinstance(k_pages, torch.Tensor) or k_pages.dim() != 4 or k_pages.dtype not in _X_TYPES \
-            or k_pages.get_device() != device or not k_pages.is_contiguous():
-        _refuse("k_pages", k_pages, (None, None, None, None), _X_TYPES, True, device)
-    shape, dt = k_pages.shape, k_pages.dtype
-    v_at = _need("v_pages", v_pages, shape, dt, device)
-    if not isinstance(table, torch.Tensor) or table.dtype is not torch.int32 or table.dim() != 2 \
-            or table.get_device() != device or not table.is_contiguous():
-        _refuse("table", table, (None, None), (torch.int32,), True, device)
-    B, width = table.shape
-    n_pages, heads, page, dim = shape
-    ks_at = vs_at = None
-    if k_scale is not None or v_scale is not None:
-        if dt is not torch.float8_e4m3fn:
-            raise ValueError("k_scale and v_scale go with a float8_e4m3fn cache, and only with it")
-        if k_scale is not None:
-            ks_at = _need("k_scale", k_scale, (heads,), torch.float32, device)
-        if v_scale is not None:
-            vs_at = _need("v_scale", v_scale, (heads,), torch.float32, device)
-    return (k_pages.data_ptr(), v_at, _DTYPES[dt], ks_at, vs_at, n_pages, page, heads, dim, table.data_ptr(), B, width)
+def native():
+    """The module of the calls below (csrc/binding.cpp: their checks, allocations and
+    launches); raises if it has not been built."""
+    global _native
+    if _native is None:
+        lib()
+        path = os.path.join(os.path.dirname(LIB_PATH), "fovea_binding.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with __graft_entry__.build()")
+        spec = importlib.util.spec_from_file_location("fovea_binding", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _native = module
+    return _native
 
 
-def _need_rotary(positions, frequencies, axis, N: int, device: int):
-    """The checks of rotary positions; returns their part of the C arguments (positions .. rot)."""
-    if not isinstance(positions, torch.Tensor) or positions.dtype is not torch.int32 or positions.dim() != 2 \
-            or positions.get_device() != device or positions.shape[1] != N:
-        _refuse("positions", positions, (None, N), (torch.int32,), False, device)
-    axes = positions.shape[0]
-    ld, inner = positions.stride()
-    if inner != 1 and N > 1:
-        raise ValueError("positions must be contiguous along its rows")
-    pairs = frequencies.shape[0] if isinstance(frequencies, torch.Tensor) and frequencies.dim() == 1 else 0
-    f_at = _need("frequencies", frequencies, (pairs,), torch.float64, device)
-    a_at = None if axis is None else _need("axis", axis, (pairs,), torch.int32, device)
-    return positions.data_ptr(), ld if axes > 1 else N, axes, f_at, a_at, 2 * pairs
+def _run(call, stream, *args):
+    """call(*args) on a stream (None: the current one).  On another than the current one the
+    outputs come from its pool and the inputs are recorded as used there; ordering the
+    streams themselves stays with the caller."""
+    if stream is not None:
+        side = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+        if side.cuda_stream != torch.cuda.current_stream().cuda_stream:
+            with torch.cuda.stream(side):
+                r = call(*args)
+            for t in args:
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(side)
+            if type(r) is int:
+                _check(r)
+            return r
+    r = call(*args)
+    if type(r) is int:
+        _check(r)
+    return r
 
 
 def rotary_frequencies(rot: int, sections=None, *, base: float = 10000.0, interleaved: bool = False,
@@ -818,23 +807,7 @@ def rotary_axes(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Ten
     axis [rot / 2] int32 (rotary_frequencies makes both; None: axis 0).  Pairs are dims
     (j, j + rot / 2), or (2j, 2j + 1) with adjacent=True.  With inverse=True it is the gradient:
     of the outputs' gradients the inputs'."""
-    N, heads, dim, ld, hs = _need_heads("q", q, _ROW_TYPES)
-    dt, dev, at = q.dtype, q.device, _device_of("q", q)
-    kv, k_at, k_ld, k_hs = 0, None, 0, 0
-    if k is not None:
-        n, kv, d, k_ld, k_hs = _need_heads("k", k, (dt,), at)
-        if n != N or d != dim:
-            _refuse("k", k, (N, None, dim), (dt,), False)
-        k_at = k.data_ptr()
-    rotary = _need_rotary(positions, frequencies, axis, N, at)
-    raw, empty = _on(stream, dev, q, k, positions, frequencies, axis)
-    q_out = empty((N, heads, dim), dtype=dt, device=dev)
-    k_out = None if k is None else empty((N, kv, dim), dtype=dt, device=dev)
-    st = lib().fovea_rotary_axes(q.data_ptr(), ld, hs, heads, k_at, k_ld, k_hs, kv, N, dim, _DTYPES[dt], *rotary,
-                                 adjacent, inverse, q_out.data_ptr(), None if k is None else k_out.data_ptr(), raw)
-    if st:
-        _check(st)
-    return q_out, k_out
+    return _run((_native or native()).rotary_axes, stream, q, k, positions, frequencies, axis, adjacent, inverse)
 
 
 def cache_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
@@ -849,37 +822,8 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_page
     with table [B, width] int32.  With positions and frequencies (as rotary_axes takes them)
     keys are rotated on the way, and so is q [N, heads, dim] when given: its rotated form is
     returned (else None)."""
-    N, kv, dim, k_ld, k_hs = _need_heads("k", k, _ROW_TYPES)
-    dt, dev, at = k.dtype, k.device, _device_of("k", k)
-    n, h, d, v_ld, v_hs = _need_heads("v", v, (dt,), at)
-    pages = _need_pages(k_pages, v_pages, table, k_scale, v_scale, at)
-    if (n, h, d) != (N, kv, dim) or (pages[7], pages[8]) != (kv, dim):
-        raise ValueError(f"k {list(k.shape)}, v {list(v.shape)} and pages {list(k_pages.shape)} differ in size")
-    sequence_at = _need("sequence", sequence, (N,), torch.int32, at)
-    entry_at = _need("entry", entry, (N,), torch.int32, at)
-    rotary = (None, 0, 1, None, None, 0)
-    if (positions is None) != (frequencies is None):
-        raise ValueError("positions and frequencies go together")
-    if positions is not None:
-        rotary = _need_rotary(positions, frequencies, axis, N, at)
-    elif q is not None or axis is not None:
-        raise ValueError("q and axis go with positions and frequencies")
-    heads, q_at, q_ld, q_hs, out, out_at = 0, None, 0, 0, None, None
-    if q is not None:
-        n, heads, d, q_ld, q_hs = _need_heads("q", q, (dt,), at)
-        if n != N or d != dim:
-            _refuse("q", q, (N, None, dim), (dt,), False)
-        q_at = q.data_ptr()
-    raw, empty = _on(stream, dev, q, k, v, k_pages, v_pages, table, sequence, entry, k_scale, v_scale, positions,
-                     frequencies, axis)
-    if q is not None:
-        out = empty((N, heads, dim), dtype=dt, device=dev)
-        out_at = out.data_ptr()
-    st = lib().fovea_cache_append(q_at, q_ld, q_hs, heads, k.data_ptr(), k_ld, k_hs, v.data_ptr(), v_ld, v_hs, N,
-                                  _DTYPES[dt], *rotary, adjacent, out_at, *pages, sequence_at, entry_at, raw)
-    if st:
-        _check(st)
-    return out
+    return _run((_native or native()).cache_append, stream, k, v, k_pages, v_pages, table, sequence, entry, k_scale,
+                v_scale, q, positions, frequencies, axis, adjacent)
 
 
 @functools.lru_cache(maxsize=512)       # a function of its arguments alone
@@ -903,46 +847,8 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
     itself).  scale: of the products (None: dim^-1/2).  Returns a dict of out, like q, and lse
     [B * nodes, heads] fp32 (with want_lse).  workspace: a uint8 tensor of
     paged_attention_workspace_size bytes (None: allocated for the call; it needs no workspace_init)."""
-    N, heads, dim, ld, hs = _need_heads("q", q, _ROW_TYPES)
-    dt, dev, at = q.dtype, q.device, _device_of("q", q)
-    pages = _need_pages(k_pages, v_pages, table, k_scale, v_scale, at)
-    if (dt is torch.float32) != (pages[2] == FP32):
-        raise ValueError(f"q of {dt} does not go with pages of {k_pages.dtype}")
-    kv, B = pages[7], pages[10]
-    if pages[8] != dim or kv == 0 or heads % kv:
-        raise ValueError(f"q {list(q.shape)} does not go with pages {list(k_pages.shape)}")
-    if (B == 0 and N) or (B and N % B):
-        raise ValueError(f"q has {N} rows, which are not the same number for each of {B} sequences")
-    nodes = N // B if B else 1
-    lens_at = _need("lens", lens, (B,), torch.int32, at)
-    tree_at, tree_rows = None, 0
-    if tree is not None:
-        tree_rows = tree.shape[0] if isinstance(tree, torch.Tensor) and tree.dim() == 3 else 0
-        if tree_rows not in (1, B):
-            raise ValueError(f"tree has {tree_rows} trees; expected {B} or 1")
-        tree_at = _need("tree", tree, (tree_rows, nodes, (nodes + 31) // 32), torch.int32, at)
-    raw, empty = _on(stream, dev, q, k_pages, v_pages, table, lens, tree, k_scale, v_scale, workspace)
-    if workspace is not None:
-        ws_bytes = workspace.numel()
-        ws_at = _need("workspace", workspace, (ws_bytes,), torch.uint8, at)
-    else:
-        ws_bytes = paged_attention_workspace_size(B, max(nodes, 1), heads, kv, dim, k_pages.dtype)
-        workspace = empty((ws_bytes,), dtype=torch.uint8, device=dev)
-        ws_at = workspace.data_ptr()
-    out = empty((N, heads, dim), dtype=dt, device=dev)
-    r = {"out": out}
-    lse_at = None
-    if want_lse:
-        r["lse"] = lse = empty((N, heads), dtype=torch.float32, device=dev)
-        lse_at = lse.data_ptr()
-    if N == 0:
-        return r
-    st = lib().fovea_paged_attention(q.data_ptr(), ld, hs, heads, *pages, lens_at, nodes, tree_at, tree_rows,
-                                     dim ** -0.5 if scale is None else scale, out.data_ptr(), lse_at, ws_at, ws_bytes,
-                                     raw)
-    if st:
-        _check(st)
-    return r
+    return _run((_native or native()).paged_attention, stream, q, k_pages, v_pages, table, lens, tree, scale, k_scale,
+                v_scale, want_lse, workspace)
 
 
 def cache_keep(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
@@ -950,20 +856,7 @@ def cache_keep(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor
     """fovea_cache_keep: of each sequence's newest `size` entries, nodes[b] ([B, path] int32, up to
     the first that is negative) move to the first places, in order.  Returns the new lengths
     [B] int32 (lens - size + the nodes' number)."""
-    if not isinstance(k_pages, torch.Tensor) or not k_pages.is_cuda:
-        raise ValueError("k_pages must be a CUDA tensor")
-    at = _device_of("k_pages", k_pages)
-    pages = _need_pages(k_pages, v_pages, table, None, None, at)
-    B, dev = pages[10], table.device
-    lens_at = _need("lens", lens, (B,), torch.int32, at)
-    path = nodes.shape[1] if isinstance(nodes, torch.Tensor) and nodes.dim() == 2 else 0
-    nodes_at = _need("nodes", nodes, (B, path), torch.int32, at)
-    raw, empty = _on(stream, dev, k_pages, v_pages, table, lens, nodes)
-    out = empty((B,), dtype=torch.int32, device=dev)
-    st = lib().fovea_cache_keep(*pages[:3], *pages[5:], lens_at, nodes_at, path, size, out.data_ptr(), raw)
-    if st:
-        _check(st)
-    return out
+    return _run((_native or native()).cache_keep, stream, k_pages, v_pages, table, lens, nodes, size)
 
 
 def cache_fork(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
@@ -974,28 +867,7 @@ def cache_fork(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor
     entries (None: all), room [C] int32 for how many more it gets pages (None: 0).  Returns a
     dict of table [C, width] (width: None: as before), lens [C] and free [1], the free pages
     left (negative: so many were missing, and nothing has been copied)."""
-    if not isinstance(k_pages, torch.Tensor) or not k_pages.is_cuda:
-        raise ValueError("k_pages must be a CUDA tensor")
-    at = _device_of("k_pages", k_pages)
-    pages = _need_pages(k_pages, v_pages, table, None, None, at)
-    B, dev = pages[10], table.device
-    lens_at = _need("lens", lens, (B,), torch.int32, at)
-    C = parents.shape[0] if isinstance(parents, torch.Tensor) and parents.dim() == 1 else 0
-    parents_at = _need("parents", parents, (C,), torch.int32, at)
-    keep_at = None if keep is None else _need("keep", keep, (C,), torch.int32, at)
-    room_at = None if room is None else _need("room", room, (C,), torch.int32, at)
-    width = pages[11] if width is None else int(width)
-    if width < 1:
-        raise ValueError(f"width {width} is below 1")
-    raw, empty = _on(stream, dev, k_pages, v_pages, table, lens, parents, keep, room)
-    i32 = torch.int32
-    r = {"table": empty((C, width), dtype=i32, device=dev), "lens": empty((C,), dtype=i32, device=dev),
-         "free": empty((1,), dtype=i32, device=dev)}
-    st = lib().fovea_cache_fork(*pages[:3], *pages[5:], lens_at, parents_at, keep_at, room_at, C, r["table"].data_ptr(),
-                                width, r["lens"].data_ptr(), r["free"].data_ptr(), raw)
-    if st:
-        _check(st)
-    return r
+    return _run((_native or native()).cache_fork, stream, k_pages, v_pages, table, lens, parents, keep, room, width)
 
 
 def timing_enable(on: bool = True) -> None:
