@@ -9,8 +9,11 @@
 // 2^64 is exact in integers; the upper 32 bits are the angle to 1.5e-9.
 //
 // Bound by memory: each element is read and written once.  A thread keeps the sines of
-// eight pairs of a token and applies them to up to eight heads, so that their cost is
-// shared; its two 16-byte chunks of a head are the pairs' two halves.
+// eight pairs of a token and applies them to up to sixteen heads, so that their cost is
+// shared; its two chunks of eight elements of a head are the pairs' two halves.  Measured:
+// image prompts (23040 bf16 tokens, 28 + 4 heads of 128, three axes) 62 us, 6.1 TB/s; the
+// gradient of 9216 fp32 tokens of 80 heads 120 us, 6.3 TB/s; prompts into an 8-bit cache
+// (32768 rows, 20480 of them stored, 32 + 8 heads) 115 us, 5.8 TB/s.
 #include <cuda_fp8.h>
 
 #include <atomic>
@@ -21,7 +24,16 @@ namespace fovea {
 
 namespace {
 
-constexpr int kMaxThreads = 512;
+constexpr int kMaxThreads = 256;
+
+// CTAs an SM and heads on their way together in a thread: of 16-bit rows many threads with
+// one, of 32-bit rows (whose angles and values take twice the registers) fewer with two.
+// 23040 bf16 tokens of 32 heads with 1 head and 4 / 3 / 5 CTAs: 62 / 72 / 68 us, 2 heads
+// and 3 CTAs 67, 4 and 2 68; 9216 fp32 tokens of 80 heads with 2 heads and 2 CTAs 120, 1
+// and 4 128.
+template <class T> constexpr int kResident = sizeof(T) == 2 ? 4 : 2;
+template <class T> constexpr int kAhead = sizeof(T) == 2 ? 1 : 2;
+constexpr int kChunk = 8;            // elements of a thread's chunk
 
 struct Work {
   HeadRows q, k, v;                  // v: entries alone
@@ -47,17 +59,26 @@ struct Chunk {
       for (int i = 0; i < (int)(E * sizeof(T) / 16); ++i) raw[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
     }
   }
+  template <class C> __device__ __forceinline__ void copy(C* p) const {
+    if constexpr (E == 1) {
+      *p = *reinterpret_cast<const C*>(raw);
+    } else {
+#pragma unroll
+      for (int i = 0; i < (int)(E * sizeof(T) / 16); ++i) reinterpret_cast<uint4*>(p)[i] = raw[i];
+    }
+  }
   __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T*>(raw)[i]); }
 };
 
-// E values in the cache's type; `scale` is of 8-bit entries.
+// E values in the cache's type; those of 8-bit entries times `inverse`, the reciprocal of
+// their scale.
 template <class C, int E>
-__device__ __forceinline__ void store(C* p, const float (&x)[E], float scale) {
+__device__ __forceinline__ void store(C* p, const float (&x)[E], float inverse) {
   if constexpr (sizeof(C) == 1) {
     uint32_t w[(E + 3) / 4] = {};
 #pragma unroll
     for (int i = 0; i < E; i += 2) {
-      const float2 two = make_float2(__fdiv_rn(x[i], scale), i + 1 < E ? __fdiv_rn(x[i + 1 < E ? i + 1 : i], scale) : 0.0f);
+      const float2 two = make_float2(x[i] * inverse, i + 1 < E ? x[i + 1 < E ? i + 1 : i] * inverse : 0.0f);
       w[i / 4] |= (uint32_t)__nv_cvt_float2_to_fp8x2(two, __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
     }
     if constexpr (E == 1) *reinterpret_cast<uint8_t*>(p) = (uint8_t)w[0];
@@ -73,13 +94,85 @@ __device__ __forceinline__ void store(C* p, const float (&x)[E], float scale) {
     }
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
   } else {
-    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+    for (int i = 0; i < E; i += 4) reinterpret_cast<float4*>(p)[i / 4] = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
   }
 }
 
-template <class T, class C, int E, bool PAGED>
-__global__ void __launch_bounds__(kMaxThreads) rotary_kernel(const __grid_constant__ Work w) {
+// cos and sin of an angle in 2^-32 turns.  It is taken to the nearest quarter turn, the
+// rest (at most pi / 4) goes through the Taylor series: up to x^9 and x^8, whose next terms
+// are below 2e-9 and 2.5e-8.
+__device__ __forceinline__ void cos_sin(uint32_t turn, float& c, float& s) {
+  const uint32_t quarter = (turn + 0x20000000u) >> 30;
+  const float x = (float)(int)(turn - (quarter << 30)) * 1.4629180792671596e-9f;   // 2 pi / 2^32
+  const float y = x * x;
+  const float sine = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f), x);
+  const float cosine = fmaf(y, fmaf(y, fmaf(y, fmaf(y, 2.4801587e-5f, -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.0f);
+  c = quarter & 1 ? sine : cosine;
+  s = quarter & 1 ? cosine : sine;
+  if ((quarter + 1) & 2) c = -c;
+  if (quarter & 2) s = -s;
+}
+
+// Where a thread's chunks lie in a head, and its angles.
+template <int E> struct Turn {
+  int at, apart;                     // the first chunk's first element, the second's behind it
+  bool turns, second;                // rotated dims; there is a second chunk
+  float c[E], s[E];
+};
+
+// The heads block, block + blocks, ... of a token: from `in`, `step` elements from one to the
+// next, to `out`.  TURN: they are rotated where the thread's dims are; ADJ: in adjacent pairs.
+template <class T, class C, int E, bool ADJ, bool TURN>
+__device__ __forceinline__ void run_heads(const Turn<E>& w, const T* in, long long step, C* out, long long out_step,
+                                          int block, int blocks, int heads, const float* scales) {
+  constexpr int kHeads = kAhead<T>;
+  for (int h = block; h < heads; h += kHeads * blocks) {
+    Chunk<T, E> x[kHeads][2];
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+      if (h + i * blocks < heads) {
+        x[i][0].load(in);
+        if (w.second) x[i][1].load(in + w.apart);
+      }
+      in += step;
+    }
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+      if (h + i * blocks >= heads) break;
+      C* p = out;
+      out += out_step;
+      if (sizeof(T) == sizeof(C) && !(TURN && w.turns)) {            // as they are
+        x[i][0].copy(p);
+        if (w.second) x[i][1].copy(p + w.apart);
+      } else {
+        float y[2][E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          y[0][e] = x[i][0].get(e);
+          y[1][e] = w.second ? x[i][1].get(e) : 0.0f;
+        }
+        if (TURN && w.turns) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            // pair e: elements 2e, 2e + 1 of both chunks together, or e of each
+            float& a = ADJ ? y[2 * e / E][2 * e % E] : y[0][e];
+            float& b = ADJ ? y[(2 * e + 1) / E][(2 * e + 1) % E] : y[1][e];
+            const float a0 = a, b0 = b;
+            a = a0 * w.c[e] - b0 * w.s[e];
+            b = a0 * w.s[e] + b0 * w.c[e];
+          }
+        }
+        const float inverse = sizeof(C) == 1 && scales != nullptr ? 1.0f / scales[h + i * blocks] : 1.0f;
+        store<C, E>(p, y[0], inverse);
+        if (w.second) store<C, E>(p + w.apart, y[1], inverse);
+      }
+    }
+  }
+}
+
+template <class T, class C, int E, bool ADJ, bool PAGED>
+__global__ void __launch_bounds__(kMaxThreads, kResident<T>) rotary_kernel(const __grid_constant__ Work w) {
   __shared__ unsigned long long phase[kRotaryPairs];     // turns per position, times 2^64
   __shared__ int axis_of[kRotaryPairs];                  // -1: no number
   pdl_wait();
@@ -97,22 +190,22 @@ __global__ void __launch_bounds__(kMaxThreads) rotary_kernel(const __grid_consta
   const int local = tid / per_token, rest = tid - local * per_token;
   const int block = rest / w.slots, slot = rest - block * w.slots;
   if (local >= w.tokens) return;
-  const bool turns = slot < w.turned;
-  int at[2];                                             // the chunks' first elements
-  if (turns) {
-    at[0] = w.r.adjacent ? 2 * E * slot : E * slot;
-    at[1] = w.r.adjacent ? at[0] + E : w.r.rot / 2 + E * slot;
-  } else {
-    at[0] = w.r.rot + 2 * E * (slot - w.turned);
-    at[1] = at[0] + E;
-  }
-  const bool second = at[1] < w.dim;                     // not the last element of an odd rest
-  const int heads = w.q.heads + w.k.heads + w.v.heads;
-  constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;         // heads on their way together
-
+  Turn<E> t;
+  t.turns = slot < w.turned;
+  t.at = t.turns ? (ADJ ? 2 * E * slot : E * slot) : w.r.rot + 2 * E * (slot - w.turned);
+  t.apart = t.turns && !ADJ ? w.r.rot / 2 : E;
+  t.second = t.at + t.apart < w.dim;                     // not the last element of an odd rest
   for (long long n = (long long)blockIdx.x * w.tokens + local; n < w.N; n += (long long)gridDim.x * w.tokens) {
-    float c[E], s[E];
-    if (turns) {
+    long long place = -1;                                // of the entry: (page kv_heads) page + offset in it
+    if constexpr (PAGED) {
+      const int b = w.sequence[n], e = w.entry[n];
+      if ((unsigned)b < (unsigned)w.c.B && e >= 0 && e < (long long)w.c.width * w.c.page) {
+        const int id = w.c.table[(long long)b * w.c.width + e / w.c.page];
+        if ((unsigned)id < (unsigned)w.c.n_pages) place = (long long)id * w.c.kv_heads * w.c.page + e % w.c.page;
+      }
+      if (place < 0 && w.q.heads == 0) continue;
+    }
+    if (t.turns) {
       int axis = -2, p = 0;
 #pragma unroll
       for (int i = 0; i < E; ++i) {
@@ -121,104 +214,51 @@ __global__ void __launch_bounds__(kMaxThreads) rotary_kernel(const __grid_consta
           axis = next;
           p = axis < 0 ? 0 : w.r.positions[axis * w.r.pos_ld + n];
         }
-        const unsigned long long turn = (unsigned long long)(long long)p * phase[j];
-        const int hi = (int)(turn >> 32);                // in 2^-32 turns, signed
-        sincospif((float)hi * 4.656612873077393e-10f, &s[i], &c[i]);   // 2^-31
-        if (w.r.inverse) s[i] = -s[i];
-        if (axis < 0) c[i] = s[i] = NAN;
+        cos_sin((uint32_t)(((unsigned long long)(long long)p * phase[j]) >> 32), t.c[i], t.s[i]);
+        if (w.r.inverse) t.s[i] = -t.s[i];
+        if (axis < 0) t.c[i] = t.s[i] = NAN;
       }
     }
-    long long place = -1;                                // of the entry: (page kv_heads) page + offset in it
+    const long long out_step = (long long)w.blocks * w.dim;
+    if (w.q.heads > 0)
+      run_heads<T, T, E, ADJ, true>(t, static_cast<const T*>(w.q.x) + n * w.q.ld + block * w.q.hs + t.at, w.blocks * w.q.hs,
+                               static_cast<T*>(w.q_out) + (n * w.q.heads + block) * w.dim + t.at, out_step, block,
+                               w.blocks, w.q.heads, nullptr);
+    const T* k = static_cast<const T*>(w.k.x) + n * w.k.ld + block * w.k.hs + t.at;
     if constexpr (PAGED) {
-      const int b = w.sequence[n], e = w.entry[n];
-      if ((unsigned)b < (unsigned)w.c.B && e >= 0 && e < (long long)w.c.width * w.c.page) {
-        const int id = w.c.table[(long long)b * w.c.width + e / w.c.page];
-        if ((unsigned)id < (unsigned)w.c.n_pages) place = (long long)id * w.c.kv_heads * w.c.page + e % w.c.page;
-      }
-    }
-    for (int h0 = block; h0 < heads; h0 += kAhead * w.blocks) {
-      Chunk<T, E> x[kAhead][2];
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int h = h0 + i * w.blocks;
-        if (h < heads) {
-          const bool is_q = h < w.q.heads, is_k = h < w.q.heads + w.k.heads;
-          const HeadRows& r = is_q ? w.q : is_k ? w.k : w.v;
-          const int head = is_q ? h : is_k ? h - w.q.heads : h - w.q.heads - w.k.heads;
-          const T* p = static_cast<const T*>(r.x) + n * r.ld + head * r.hs;
-          x[i][0].load(p + at[0]);
-          if (second) x[i][1].load(p + at[1]);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int h = h0 + i * w.blocks;
-        if (h >= heads) break;
-        const bool is_q = h < w.q.heads, is_k = h < w.q.heads + w.k.heads;
-        float y[2][E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          y[0][e] = x[i][0].get(e);
-          y[1][e] = second ? x[i][1].get(e) : 0.0f;
-        }
-        if (turns && is_k) {
-          if (w.r.adjacent && E > 1) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) {                // pair e: elements 2e, 2e + 1 of both chunks
-              float& a = y[2 * e / E][2 * e % E];
-              float& b = y[2 * e / E][(2 * e + 1) % E];
-              const float a0 = a, b0 = b;
-              a = a0 * c[e] - b0 * s[e];
-              b = a0 * s[e] + b0 * c[e];
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const float a0 = y[0][e], b0 = y[1][e];
-              y[0][e] = a0 * c[e] - b0 * s[e];
-              y[1][e] = a0 * s[e] + b0 * c[e];
-            }
-          }
-        }
-        if (is_q) {
-          T* p = static_cast<T*>(w.q_out) + (n * w.q.heads + h) * w.dim;
-          store<T, E>(p + at[0], y[0], 1.0f);
-          if (second) store<T, E>(p + at[1], y[1], 1.0f);
-        } else if constexpr (PAGED) {
-          if (place >= 0) {
-            const int head = is_k ? h - w.q.heads : h - w.q.heads - w.k.heads;
-            C* p = static_cast<C*>(is_k ? w.c.k : w.c.v) + (place + (long long)head * w.c.page) * w.dim;
-            const float* scales = is_k ? w.c.k_scale : w.c.v_scale;
-            const float scale = sizeof(C) == 1 && scales != nullptr ? scales[head] : 1.0f;
-            store<C, E>(p + at[0], y[0], scale);
-            if (second) store<C, E>(p + at[1], y[1], scale);
-          }
-        } else {
-          T* p = static_cast<T*>(w.k_out) + (n * w.k.heads + h - w.q.heads) * w.dim;
-          store<T, E>(p + at[0], y[0], 1.0f);
-          if (second) store<T, E>(p + at[1], y[1], 1.0f);
-        }
-      }
+      if (place < 0) continue;
+      const long long to = (place + (long long)block * w.c.page) * w.dim + t.at, page_step = out_step * w.c.page;
+      run_heads<T, C, E, ADJ, true>(t, k, w.blocks * w.k.hs, static_cast<C*>(w.c.k) + to, page_step, block, w.blocks,
+                               w.k.heads, w.c.k_scale);
+      run_heads<T, C, E, ADJ, false>(t, static_cast<const T*>(w.v.x) + n * w.v.ld + block * w.v.hs + t.at,
+                                w.blocks * w.v.hs, static_cast<C*>(w.c.v) + to, page_step, block, w.blocks, w.v.heads,
+                                w.c.v_scale);
+    } else if (w.k.heads > 0) {
+      run_heads<T, T, E, ADJ, true>(t, k, w.blocks * w.k.hs, static_cast<T*>(w.k_out) + (n * w.k.heads + block) * w.dim + t.at,
+                               out_step, block, w.blocks, w.k.heads, nullptr);
     }
   }
 }
 
-template <class T, class C, int E, bool PAGED>
+template <class T, class C, int E, bool ADJ, bool PAGED>
 cudaError_t launch_as(Work w, cudaStream_t s) {
   const int rot = w.r.rot, heads = w.q.heads + w.k.heads + w.v.heads;
   w.turned = rot / 2 / E;
   w.slots = w.turned + (w.dim - rot + 2 * E - 1) / (2 * E);
-  // heads a thread: up to eight share its sines, fewer where that leaves SMs without work
-  int per = 8;
-  while (per > 1 && (long long)w.N * ((heads + per - 1) / per) * w.slots < 152 * 1024) per /= 2;
-  while ((heads + per - 1) / per * w.slots > kMaxThreads) per *= 2;
-  w.blocks = (heads + per - 1) / per;
+  // Threads that share a token's heads, a power of two (so that q, k and v, often of 4, 8 or
+  // 32 heads, go even): the fewest that leave a thread's sines to fewer than 16 heads, more
+  // where that leaves SMs without work.
+  w.blocks = 1;
+  while (w.blocks * 16 <= heads || (w.blocks < heads && (long long)w.N * w.blocks * w.slots < 152 * 1024)) w.blocks *= 2;
+  while (w.blocks > 1 && w.blocks * w.slots > kMaxThreads) w.blocks /= 2;
   const int per_token = w.blocks * w.slots;
   w.tokens = per_token >= 256 ? 1 : 256 / per_token;
   const int threads = (w.tokens * per_token + 31) / 32 * 32;
   const long long ctas = ((long long)w.N + w.tokens - 1) / w.tokens;
-  const int grid = (int)(ctas < 152 * 8 ? ctas : 152 * 8);
-  return launch_pdl(rotary_kernel<T, C, E, PAGED>, dim3(grid), dim3(threads), 0, s, w);
+  // CTAs go on to further tokens: each makes the table of turns, which a CTA for every few
+  // tokens would pay for (image prompts 66 us instead of 62)
+  const int grid = (int)(ctas < 152 * 4 ? ctas : 152 * 4);
+  return launch_pdl(rotary_kernel<T, C, E, ADJ, PAGED>, dim3(grid), dim3(threads), 0, s, w);
 }
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -228,9 +268,11 @@ bool vectors(const HeadRows& r, size_t size) {
 
 template <class T, class C, bool PAGED>
 cudaError_t launch_type(const Work& w, cudaStream_t s) {
-  const bool whole = w.dim % 16 == 0 && w.r.rot % 16 == 0 && vectors(w.q, sizeof(T)) && vectors(w.k, sizeof(T)) &&
+  constexpr int E = kChunk;
+  const bool whole = w.dim % (2 * E) == 0 && w.r.rot % (2 * E) == 0 && vectors(w.q, sizeof(T)) && vectors(w.k, sizeof(T)) &&
                      vectors(w.v, sizeof(T)) && aligned(w.q_out, 16) && aligned(w.k_out, 16);
-  return whole ? launch_as<T, C, 8, PAGED>(w, s) : launch_as<T, C, 1, PAGED>(w, s);
+  return whole ? (w.r.adjacent ? launch_as<T, C, E, true, PAGED>(w, s) : launch_as<T, C, E, false, PAGED>(w, s))
+               : (w.r.adjacent ? launch_as<T, C, 1, true, PAGED>(w, s) : launch_as<T, C, 1, false, PAGED>(w, s));
 }
 
 }  // namespace
