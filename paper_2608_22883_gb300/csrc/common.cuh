@@ -522,6 +522,9 @@ struct PagedArgs {
 };
 size_t paged_attention_workspace(const PagedArgs& a);
 cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s);
+// The same for many rows a key head, bf16 and e4m3 caches (paged_rows.cu); workspace not
+// null: its bytes instead.
+cudaError_t launch_paged_rows(const PagedArgs& a, cudaStream_t s, size_t* workspace);
 
 // The memory build's GEMMs out[i] = R . F[i]^T on CTA pairs (gemm_build.cu):
 // token rows R [rows, K] (R0 for part 0, R1 for the others) against up to

@@ -13,33 +13,15 @@
 // fragments as they come (a lane of the quad takes every fourth chunk of a row), and
 // those of values become fragments of V^T by pairing two entries' halves (one prmt a
 // register).  P goes from S^T's layout to the other operand's by movmatrix.
-//
-// The entries of all sequences and key heads are one list of blocks of 16, cut into equal
-// runs, one a CTA; a run covers parts of one or several (sequence, head, rows) segments.
-// A segment within one run is finished there; the others leave partial sums, which a
-// second kernel joins in the order of the runs (results do not vary from run to run).
-#include <cuda_fp16.h>
-#include <cuda_fp8.h>
-
 #include <atomic>
 #include <cstddef>
 
-#include "common.cuh"
+#include "paged_core.cuh"
 
 namespace fovea {
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kBlock = 16;           // entries of a block
-constexpr int kLeast = kWarps;       // blocks of a run, at least
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-__device__ __forceinline__ float exp2_(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
@@ -48,17 +30,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x5410); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x7632); }
 
-template <bool HALF>                 // HALF: fp16 operands, else bf16
-__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  if constexpr (HALF)
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  else
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -71,11 +42,6 @@ __device__ __forceinline__ void split_tf32(uint32_t x, uint32_t& hi, uint32_t& l
   hi = finite ? x & 0xFFFFE000u : x;
   lo = finite ? __float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) : 0u;
 }
-__device__ __forceinline__ uint32_t halves_of_e4m3(uint32_t two) {   // the low 16 bits: two values
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
-  return (uint32_t)h.x | ((uint32_t)h.y << 16);
-}
-
 // How entries of a type are cut among the lanes.  g = lane / 4, t = lane % 4.
 // Keys: lane (g, t) holds entries g and g + 8, of each the 16-byte chunks t, t + 4, ...
 // Values: lane (g, t) holds, of its entries, `kSpan` dims from kSpan g of each part of
@@ -92,78 +58,6 @@ template <class C, int D> struct Cut {
   static constexpr int kSteps = kSize == 4 ? D / 8 : D / 16;      // of the contraction over dims
 };
 
-// A segment's rows are staged and its sums put together, which takes a CTA as long as some
-// blocks: the runs are cut as if each segment had so many empty ones in front.  (The batch
-// of 64 sequences of 0 to 8192 entries, us, with 0 / 4 / 8 / 16 / 24: 85 / 49 / 38 / 36 / 37;
-// eight trees of 32 nodes 204 / 85 / 63 / 46 / 44.)
-template <int RT> constexpr uint32_t kFront = RT == 1 ? 16 : 24;
-
-// The blocks of all segments as one list: sequence by sequence, key head by key head, rows
-// by rows.
-struct Plan {
-  uint64_t total;      // blocks
-  uint32_t runs;       // that have any
-  __device__ __forceinline__ uint64_t start(uint32_t run) const { return total * run / runs; }
-  __device__ __forceinline__ uint32_t run_of(uint64_t block) const {     // start(run) <= block < start(run + 1)
-    return (uint32_t)(((block + 1) * runs + total - 1) / total - 1);
-  }
-};
-
-__device__ __forceinline__ int length_of(const PagedArgs& a, int b) {
-  const int n = a.lens[b];
-  const long long most = (long long)a.width * a.page;
-  return n < 0 ? 0 : n > most ? (int)most : n;
-}
-__device__ __forceinline__ bool too_long(const PagedArgs& a, int b) { return a.lens[b] > (long long)a.width * a.page; }
-__device__ __forceinline__ uint32_t blocks_of(int len, uint32_t front) {
-  return len > 0 ? (uint32_t)(len + kBlock - 1) / kBlock + front : 0;
-}
-
-// Sums of the sequences' blocks before each (before[0 .. B], in shared memory) and the
-// cut into runs.  All threads of the CTA.
-__device__ Plan make_plan(const PagedArgs& a, uint32_t* before, uint32_t* scratch, int max_runs, uint32_t front) {
-  const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (a.B + nt - 1) / nt, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
-  uint32_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += blocks_of(length_of(a, b), front);
-  uint32_t sum = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += up;
-  }
-  if (lane == 31) scratch[warp] = sum;
-  __syncthreads();
-  uint32_t base = sum - mine;
-  for (int w = 0; w < warp; ++w) base += scratch[w];
-  for (int b = b0; b < b1; ++b) {
-    before[b] = base;
-    base += blocks_of(length_of(a, b), front);
-  }
-  if (b1 == a.B && b0 < b1) before[a.B] = base;
-  __syncthreads();
-  Plan p;
-  p.total = (uint64_t)before[a.B] * (uint32_t)(a.kv_heads * a.row_blocks);
-  const uint64_t most = (p.total + kLeast - 1) / kLeast;
-  p.runs = most < (uint64_t)max_runs ? (uint32_t)most : (uint32_t)max_runs;
-  return p;
-}
-
-__device__ __forceinline__ const uint32_t* tree_of(const PagedArgs& a, int b) {
-  return a.tree != nullptr ? a.tree + (size_t)(a.tree_rows == 1 ? 0 : b) * a.nodes * a.words : nullptr;
-}
-__device__ __forceinline__ float to_f32_any(float x) { return x; }
-__device__ __forceinline__ float to_f32_any(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_f32_any(__nv_fp8_e4m3 x) { return float(x); }
-// Whether row `node` sees entry `at` of a sequence of n entries.
-__device__ __forceinline__ bool sees(const PagedArgs& a, const uint32_t* tree, int n, int node, int at) {
-  if (at >= n) return false;
-  const int j = at - (n - a.nodes);
-  if (j < 0) return true;
-  if (tree == nullptr) return j <= node;
-  return (tree[(size_t)node * a.words + (j >> 5)] >> (j & 31)) & 1u;
-}
-
 // Blocks that a warp takes together.
 template <class C, int D, int RT> constexpr int kTogether = sizeof(C) * D * RT <= 128 ? 2 : 1;
 
@@ -171,7 +65,9 @@ template <class C, class Q, int D, int RT>
 struct Attention {
   using G = Cut<C, D>;
   static constexpr bool kF32 = sizeof(C) == 4, kE4 = sizeof(C) == 1;
-  static constexpr int kRows = 8 * RT;
+  static constexpr int kRows = 8 * RT, kBlock = 16, kLeast = kWarps;
+  static constexpr uint32_t kFront = RT == 1 ? 16 : 24;
+  static constexpr int kSlot = kRows * (D + 2);                  // floats of a partial segment
   static constexpr uint32_t kBytes = kBlock * D * sizeof(C);     // of a block
   // p of 8-bit values is held in fp16, times 2^15: its smallest step is then 2^-39
   static constexpr float kLift = kE4 ? 15.0f : 0.0f;
@@ -406,9 +302,7 @@ struct Attention {
           for (int w = 0; w < G::kSpanWords; ++w) v[u][e][p][w] = 0;
   }
 
-  // Values that are infinite or NaN, where only some rows see an entry: a product with a
-  // p of 0 would give NaN to the others.  They are cleared here, and the rows that see one
-  // take it when the segment is finished.  True where there was one.
+  // Odd values cleared (odd_values): true where there was one.
   __device__ __forceinline__ bool clear_odd_values(int u) {
     uint32_t any = 0;
 #pragma unroll
@@ -417,45 +311,20 @@ struct Attention {
       for (int p = 0; p < G::kParts; ++p)
 #pragma unroll
         for (int w = 0; w < G::kSpanWords; ++w) {
-          uint32_t& x = v[u][e][p][w];
-          uint32_t odd;
-          if constexpr (kF32) odd = (x & 0x7F800000u) == 0x7F800000u ? 0xFFFFFFFFu : 0u;
-          else if constexpr (kE4) odd = __vcmpeq4(x & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
-          else odd = __vcmpeq2(x & 0x7F807F80u, 0x7F807F80u);
-          x &= ~odd;
+          const uint32_t odd = odd_in<C>(v[u][e][p][w]);
+          v[u][e][p][w] &= ~odd;
           any |= odd;
         }
     return any != 0;
-  }
-  // Dims d .. d + 3 of such values of the entries from `from` to `to` that the row sees, added to x.
-  __device__ __noinline__ static float4 odd_values(const PagedArgs& a, int b, int h, int node, int n, int from, int to,
-                                                   int d, float4 x) {
-    const uint32_t* tree = tree_of(a, b);
-    for (int at = max(from, n - a.nodes); at < min(to, n); ++at) {
-      const int page = a.table[(size_t)b * a.width + at / a.page];
-      if (!sees(a, tree, n, node, at) || (unsigned)page >= (unsigned)a.n_pages) continue;
-      const C* p = static_cast<const C*>(a.v_pages) + (((size_t)page * a.kv_heads + h) * a.page + at % a.page) * D + d;
-      float* y = &x.x;
-      for (int e = 0; e < 4; ++e) {
-        const float value = to_f32_any(p[e]);
-        if (!isfinite(value)) y[e] += value;
-      }
-    }
-    return x;
   }
 
   // Q^T's fragments of the rows from row0 on.  All threads; between barriers of the caller.
   __device__ __forceinline__ static void stage_rows(const PagedArgs& a, Shared& sh, int b, int h, int row0) {
     const int tid = threadIdx.x, lane = tid & 31;
-    const Q* q = static_cast<const Q*>(a.q);
     const int rows = a.nodes * a.group;
-    auto row_at = [&](int r) -> const Q* {
-      const int node = r / a.group;
-      return q + ((long long)b * a.nodes + node) * a.q_ld + (long long)(h * a.group + (r - node * a.group)) * a.q_hs;
-    };
+    auto row_at = [&](int r) { return row_of<Q>(a, b, h, r); };
     if (tid == 0) sh.odd = 0;
     if constexpr (kE4) {
-      // rows to a largest magnitude in [1, 2), by a power of two, for fp16
       for (int r = tid >> 5; r < kRows; r += kWarps) {
         float top = 0.0f;
         if (row0 + r < rows) {
@@ -464,9 +333,7 @@ struct Attention {
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const uint32_t e = __float_as_uint(top) >> 23;
-        // 2^(e - 127); 1 for rows of zeros, subnormals and infinities
-        if (lane == 0) sh.row_scale[r] = e > 0 && e < 254 ? __uint_as_float(e << 23) : 1.0f;
+        if (lane == 0) sh.row_scale[r] = row_power(top);
       }
       __syncthreads();
     }
@@ -513,15 +380,12 @@ struct Attention {
     clear();
     uint32_t at = lo + warp * kSub;
     if (at >= hi) return;
-    // Where a block's page stands in the table and where the block in its page: a page has
-    // 1 to 64 blocks and a sequence fewer than 2^26, for which the product is exact.
-    auto page_of = [&](uint32_t block) { return a.page_magic == 0 ? block : __umulhi(block, a.page_magic); };
     int id[kSub];
     uint32_t in_page[kSub];
     auto look_up = [&](uint32_t first) {
 #pragma unroll
       for (int u = 0; u < kSub; ++u) {
-        const uint32_t block = u == 0 ? first : min(first + u, hi - 1), p = page_of(block);
+        const uint32_t block = u == 0 ? first : min(first + u, hi - 1), p = page_of(a, block);
         id[u] = table[p];
         in_page[u] = block - p * per_page;
       }
@@ -542,7 +406,7 @@ struct Attention {
 #pragma unroll
     for (int u = 0; u < kSub; ++u) load_keys(u, keys + off[u]);
     const int end = min(n, (int)(hi * kBlock));            // the run's last entry
-    const int plain = min(end, n - a.nodes + (a.nodes == 1 && tree == nullptr));   // up to here all rows see all
+    const int plain = min(end, plain_end(a, n));
     while (true) {
 #pragma unroll
       for (int u = 0; u < kSub; ++u) load_values(u, values + off[u]);
@@ -570,7 +434,7 @@ struct Attention {
         for (int u = 0; u < kSub; ++u) {
           const int start = first + u * kBlock;
           // which of the block's pages: looked up again, this is rare
-          const bool out = was_bad && start < end && (unsigned)table[page_of(at + u)] >= (unsigned)a.n_pages;
+          const bool out = was_bad && start < end && (unsigned)table[page_of(a, at + u)] >= (unsigned)a.n_pages;
 #pragma unroll
           for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -679,7 +543,7 @@ struct Attention {
         x.x += c * y.x; x.y += c * y.y; x.z += c * y.z; x.w += c * y.w;
       }
       if (poison) sum = NAN;
-      if (sh.odd) x = odd_values(a, b, h, (row0 + r) / a.group, n, (int)lo * kBlock, (int)hi * kBlock, d, x);
+      if (sh.odd) x = odd_values<C, D>(a, b, h, (row0 + r) / a.group, n, (int)lo * kBlock, (int)hi * kBlock, d, x);
       if (!whole) {
         *reinterpret_cast<float4*>(slot + r * D + d) = x;
         if (d == 0) {
@@ -693,22 +557,6 @@ struct Attention {
       }
     }
   }
-
-  template <class T>
-  __device__ __forceinline__ static void write_row(const PagedArgs& a, long long n, int head, int d, int dim, float4 x,
-                                                   float top, float sum, float v_scale, float lift) {
-    const float k = sum == 0.0f ? 0.0f : v_scale / sum;    // nothing seen: 0 (an infinite value stays NaN)
-    T* out = static_cast<T*>(a.out) + (n * a.heads + head) * dim + d;
-    if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<float4*>(out) = make_float4(x.x * k, x.y * k, x.z * k, x.w * k);
-    } else {
-      const __nv_bfloat162 lo = __floats2bfloat162_rn(x.x * k, x.y * k), hi = __floats2bfloat162_rn(x.z * k, x.w * k);
-      *reinterpret_cast<uint2*>(out) =
-          make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-    }
-    if (d == 0 && a.lse != nullptr)
-      a.lse[n * a.heads + head] = sum == 0.0f ? -INFINITY : (top - lift + log2f(sum)) * kLn2;
-  }
 };
 
 // CTAs an SM, by registers.
@@ -721,142 +569,42 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_attention_
   using A = Attention<C, Q, D, RT>;
   extern __shared__ __align__(16) uint8_t raw[];
   typename A::Shared& sh = *reinterpret_cast<typename A::Shared*>(raw);
-  uint32_t* before = reinterpret_cast<uint32_t*>(raw + sizeof(typename A::Shared));
   static_assert(offsetof(typename A::Shared, o) % 16 == 0 && sizeof(typename A::Shared) % 16 == 0, "16-byte loads");
+  uint32_t* before = reinterpret_cast<uint32_t*>(raw + sizeof(typename A::Shared));
   __shared__ uint32_t scratch[kWarps];
-  constexpr uint32_t front = kFront<RT>;
   pdl_wait();
   pdl_trigger();                     // the joining kernel makes the same plan meanwhile
-  const Plan plan = make_plan(a, before, scratch, (int)gridDim.x, front);
-  if (blockIdx.x >= plan.runs) return;
-  const uint64_t from = plan.start(blockIdx.x), to = plan.start(blockIdx.x + 1);
-  const uint32_t segments = a.kv_heads * a.row_blocks;    // of a sequence
-  float* slots = static_cast<float*>(a.workspace) + (size_t)blockIdx.x * 2 * A::kRows * (D + 2);
-  int b = 0;
-  {
-    int hi = a.B - 1;                // the last b with before[b] * segments <= from
-    while (b < hi) {
-      const int mid = (b + hi + 1) >> 1;
-      if ((uint64_t)before[mid] * segments <= from) b = mid; else hi = mid - 1;
-    }
-  }
+  const Plan plan = make_plan<A>(a, before, scratch, (int)gridDim.x);
   A at;
-  for (uint64_t u = from; u < to;) {
-    while ((uint64_t)before[b + 1] * segments <= u) ++b;
-    const uint32_t count = before[b + 1] - before[b];
-    const uint64_t within = u - (uint64_t)before[b] * segments;
-    const uint32_t seg = (uint32_t)(within / count), first = (uint32_t)(within % count);
-    const uint32_t end = (uint32_t)min((uint64_t)count, first + (to - u));
-    // a segment that begins before or with this run goes to its first slot, a later one to its second
-    const bool begun = u - first <= from;
-    u += end - first;
-    if (end <= front) continue;
-    const uint32_t lo = max(first, front) - front, hi = end - front;
-    const int h = seg / a.row_blocks, row0 = (seg % a.row_blocks) * A::kRows;
+  each_segment<A>(a, plan, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool whole, float* slot) {
     A::stage_rows(a, sh, b, h, row0);
     __syncthreads();
     const int n = length_of(a, b);
     at.blocks(a, sh, b, h, row0, n, lo, hi);
-    at.finish(a, sh, b, h, row0, n, lo, hi, lo == 0 && hi == count - front, slots + (begun ? 0 : A::kRows * (D + 2)));
+    at.finish(a, sh, b, h, row0, n, lo, hi, whole, slot);
     __syncthreads();
-  }
+  });
 }
 
-// A row whose segment is cut between runs, joined in their order; rows of sequences
-// without entries get 0.  A warp a row.
-template <class C, class Q, int D, int RT>
-__global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_constant__ PagedArgs a, int runs) {
-  using A = Attention<C, Q, D, RT>;
-  extern __shared__ __align__(16) uint8_t raw[];
-  uint32_t* before = reinterpret_cast<uint32_t*>(raw);
-  __shared__ uint32_t scratch[kWarps];
-  constexpr uint32_t front = kFront<RT>;
-  const int lane = threadIdx.x & 31;
-  const Plan plan = make_plan(a, before, scratch, runs, front);
-  pdl_wait();
-  const long long rows = (long long)a.B * a.nodes * a.heads;
-  for (long long i = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * kWarps) {
-    const long long n = i / a.heads;
-    const int head = (int)(i - n * a.heads), b = (int)(n / a.nodes), node = (int)(n - (long long)b * a.nodes);
-    const int h = head / a.group, row = node * a.group + head - h * a.group;
-    const uint32_t segments = a.kv_heads * a.row_blocks, count = before[b + 1] - before[b];
-    const float v_scale = A::kE4 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
-    if (count == 0) {
-      for (int d = 4 * lane; d < D; d += 128)
-        A::template write_row<Q>(a, n, head, d, D, make_float4(0.0f, 0.0f, 0.0f, 0.0f), -INFINITY, 0.0f, 1.0f, 0.0f);
-      continue;
-    }
-    const uint64_t s0 = (uint64_t)before[b] * segments + (uint64_t)(h * a.row_blocks + row / A::kRows) * count;
-    const uint32_t first = plan.run_of(s0 + front), last = plan.run_of(s0 + count - 1);
-    if (first == last) continue;     // written already
-    const float* base = static_cast<const float*>(a.workspace);
-    const int r = row % A::kRows;
-    auto slot = [&](uint32_t run) {
-      return base + ((size_t)run * 2 + (run == first && plan.start(run) < s0)) * A::kRows * (D + 2);
-    };
-    float top = -INFINITY;
-    for (uint32_t run = first + lane; run <= last; run += 32) top = fmaxf(top, __ldcg(slot(run) + A::kRows * D + 2 * r));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    float sum = 0.0f;
-    constexpr int kVecs = (D + 127) / 128;
-    float4 x[kVecs];
-#pragma unroll
-    for (int c = 0; c < kVecs; ++c) x[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-    for (uint32_t run = first; run <= last; ++run) {
-      const float* p = slot(run);
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + A::kRows * D + 2 * r));
-      const float c = ml.x == top ? 1.0f : exp2_(ml.x - top);
-      sum += c * ml.y;
-#pragma unroll
-      for (int v = 0; v < kVecs; ++v) {
-        const int d = 128 * v + 4 * lane;
-        if (d < D) {
-          const float4 y = __ldcg(reinterpret_cast<const float4*>(p + r * D + d));
-          x[v].x += c * y.x; x[v].y += c * y.y; x[v].z += c * y.z; x[v].w += c * y.w;
-        }
-      }
-    }
-#pragma unroll
-    for (int v = 0; v < kVecs; ++v) {
-      const int d = 128 * v + 4 * lane;
-      if (d < D) A::template write_row<Q>(a, n, head, d, D, x[v], top, sum, v_scale, A::kLift);
-    }
-  }
-}
-
+// More rows than these go to the kernel of many rows.
+constexpr int kManyRows = 16;
 // Rows that a warp takes together, by 8: as many as there are, up to what its registers hold.
 template <class C, int D> constexpr int most_tiles() {
   return sizeof(C) == 4 || D == 256 ? 1 : D == 128 ? 2 : 4;
 }
 
 template <class C, class Q, int D, int RT>
-cudaError_t launch_as(PagedArgs a, cudaStream_t s, size_t* workspace) {
+cudaError_t launch_as(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
   using A = Attention<C, Q, D, RT>;
-  const uint32_t per_page = a.page / kBlock;
-  a.page_magic = per_page <= 1 ? 0 : (uint32_t)((1ull << 32) / per_page + 1);
-  a.row_blocks = (a.nodes * a.group + A::kRows - 1) / A::kRows;
-  const size_t plan_bytes = ((size_t)a.B + 1) * 4;
-  const size_t smem = sizeof(typename A::Shared) + plan_bytes;
   static std::atomic<unsigned long long> raised{0};
-  const int grid = 152 * per_sm<C, D, RT>();
-  if (workspace != nullptr) {
-    *workspace = (size_t)grid * 2 * A::kRows * (D + 2) * 4;
-    return cudaSuccess;
-  }
-  cudaError_t e = raise_smem_limit(paged_attention_kernel<C, Q, D, RT>, 227 * 1024 - 1024, raised);
-  if (e != cudaSuccess) return e;
-  e = launch_pdl(paged_attention_kernel<C, Q, D, RT>, dim3(grid), dim3(kThreads), smem, s, a);
-  if (e != cudaSuccess) return e;
-  const long long rows = (long long)a.B * a.nodes * a.heads;
-  const int join = (int)((rows + kWarps - 1) / kWarps < 152 * 8 ? (rows + kWarps - 1) / kWarps : 152 * 8);
-  return launch_pdl(paged_join_kernel<C, Q, D, RT>, dim3(join), dim3(kThreads), plan_bytes, s, a, grid);
+  return launch_runs<A, C, Q, D>(a, paged_attention_kernel<C, Q, D, RT>, sizeof(typename A::Shared),
+                                 152 * per_sm<C, D, RT>(), s, workspace, raised);
 }
 
 template <class C, class Q, int D>
 cudaError_t launch_dim(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
   const int rows = a.nodes * a.group;
+  if (sizeof(C) < 4 && rows > kManyRows) return launch_paged_rows(a, s, workspace);
   if constexpr (most_tiles<C, D>() >= 4)
     if (rows > 16) return launch_as<C, Q, D, 4>(a, s, workspace);
   if constexpr (most_tiles<C, D>() >= 2)

@@ -1,0 +1,299 @@
+// What the kernels of fovea_paged_attention share: the cut of the work into runs, which
+// entries a row sees, the rows' results, and the joining of runs.
+//
+// The entries of all sequences and key heads are one list of blocks, cut into equal runs,
+// one a CTA; a run covers parts of one or several (sequence, head, rows) segments.  A
+// segment within one run is finished there; the others leave partial sums, which a second
+// kernel joins in the order of the runs (results do not vary from run to run).
+#pragma once
+
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include <atomic>
+
+#include "common.cuh"
+
+namespace fovea {
+
+namespace {
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+template <bool HALF>                 // HALF: fp16 operands, else bf16
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (HALF)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t halves_of_e4m3(uint32_t two) {   // the low 16 bits: two values
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
+  return (uint32_t)h.x | ((uint32_t)h.y << 16);
+}
+__device__ __forceinline__ uint32_t bits_of(__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); }
+__device__ __forceinline__ uint32_t bits_of(__nv_bfloat162 x) { return *reinterpret_cast<const uint32_t*>(&x); }
+
+struct Plan {
+  uint64_t total;      // blocks
+  uint32_t runs;       // that have any
+  __device__ __forceinline__ uint64_t start(uint32_t run) const { return total * run / runs; }
+  __device__ __forceinline__ uint32_t run_of(uint64_t block) const {     // start(run) <= block < start(run + 1)
+    return (uint32_t)(((block + 1) * runs + total - 1) / total - 1);
+  }
+};
+
+__device__ __forceinline__ int length_of(const PagedArgs& a, int b) {
+  const int n = a.lens[b];
+  const long long most = (long long)a.width * a.page;
+  return n < 0 ? 0 : n > most ? (int)most : n;
+}
+__device__ __forceinline__ bool too_long(const PagedArgs& a, int b) { return a.lens[b] > (long long)a.width * a.page; }
+
+// K, of a kernel: kBlock entries a block; kLeast blocks of a run, at least; kFront: the
+// staging of a segment's rows and the end of its sums take a CTA as long as some blocks,
+// and the runs are cut as if each segment had so many empty ones in front.
+template <class K> __device__ __forceinline__ uint32_t blocks_of(int len) {
+  return len > 0 ? (uint32_t)(len + K::kBlock - 1) / K::kBlock + K::kFront : 0;
+}
+// Sums of the sequences' blocks before each (before[0 .. B], in shared memory) and the
+// cut into runs.  All threads of the CTA.
+template <class K> __device__ Plan make_plan(const PagedArgs& a, uint32_t* before, uint32_t* scratch, int max_runs) {
+  const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (a.B + nt - 1) / nt, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
+  uint32_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += blocks_of<K>(length_of(a, b));
+  uint32_t sum = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += up;
+  }
+  if (lane == 31) scratch[warp] = sum;
+  __syncthreads();
+  uint32_t base = sum - mine;
+  for (int w = 0; w < warp; ++w) base += scratch[w];
+  for (int b = b0; b < b1; ++b) {
+    before[b] = base;
+    base += blocks_of<K>(length_of(a, b));
+  }
+  if (b1 == a.B && b0 < b1) before[a.B] = base;
+  __syncthreads();
+  Plan p;
+  p.total = (uint64_t)before[a.B] * (uint32_t)(a.kv_heads * a.row_blocks);
+  const uint64_t most = (p.total + K::kLeast - 1) / K::kLeast;
+  p.runs = most < (uint64_t)max_runs ? (uint32_t)most : (uint32_t)max_runs;
+  return p;
+}
+
+// The segments of a CTA's run: body(sequence, key head, first row, first block, end, whether
+// the segment is whole, its partial slot).
+template <class K, class F>
+__device__ __forceinline__ void each_segment(const PagedArgs& a, const Plan& plan, const uint32_t* before, F body) {
+  if (blockIdx.x >= plan.runs) return;
+  const uint64_t from = plan.start(blockIdx.x), to = plan.start(blockIdx.x + 1);
+  const uint32_t segments = a.kv_heads * a.row_blocks;    // of a sequence
+  float* slots = static_cast<float*>(a.workspace) + (size_t)blockIdx.x * 2 * K::kSlot;
+  int b = 0;
+  {
+    int hi = a.B - 1;                // the last b with before[b] * segments <= from
+    while (b < hi) {
+      const int mid = (b + hi + 1) >> 1;
+      if ((uint64_t)before[mid] * segments <= from) b = mid; else hi = mid - 1;
+    }
+  }
+  for (uint64_t u = from; u < to;) {
+    while ((uint64_t)before[b + 1] * segments <= u) ++b;
+    const uint32_t count = before[b + 1] - before[b];
+    const uint64_t within = u - (uint64_t)before[b] * segments;
+    const uint32_t seg = (uint32_t)(within / count), first = (uint32_t)(within % count);
+    const uint32_t end = (uint32_t)min((uint64_t)count, first + (to - u));
+    // a segment that begins before or with this run goes to its first slot, a later one to its second
+    const bool begun = u - first <= from;
+    u += end - first;
+    if (end <= K::kFront) continue;
+    const uint32_t lo = max(first, K::kFront) - K::kFront, hi = end - K::kFront;
+    body(b, (int)(seg / a.row_blocks), (int)(seg % a.row_blocks) * K::kRows, lo, hi,
+         lo == 0 && hi == count - K::kFront, slots + (begun ? 0 : K::kSlot));
+  }
+}
+
+__device__ __forceinline__ const uint32_t* tree_of(const PagedArgs& a, int b) {
+  return a.tree != nullptr ? a.tree + (size_t)(a.tree_rows == 1 ? 0 : b) * a.nodes * a.words : nullptr;
+}
+// Whether row `node` sees entry `at` of a sequence of n entries.
+__device__ __forceinline__ bool sees(const PagedArgs& a, const uint32_t* tree, int n, int node, int at) {
+  if (at >= n) return false;
+  const int j = at - (n - a.nodes);
+  if (j < 0) return true;
+  if (tree == nullptr) return j <= node;
+  return (tree[(size_t)node * a.words + (j >> 5)] >> (j & 31)) & 1u;
+}
+// Entries up to here are seen by all rows.
+__device__ __forceinline__ int plain_end(const PagedArgs& a, int n) {
+  return n - a.nodes + (a.nodes == 1 && a.tree == nullptr);
+}
+
+__device__ __forceinline__ float to_f32_any(float x) { return x; }
+__device__ __forceinline__ float to_f32_any(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f32_any(__nv_fp8_e4m3 x) { return float(x); }
+
+// Values that are infinite or NaN, where only some rows see an entry: a product with a p of
+// 0 would give NaN to the others.  They are cleared before the products, and the rows that
+// see one take it when a segment is finished: dims d .. d + 3 of those of the entries from
+// `from` to `to`, added to x.
+template <class C, int D>
+__device__ __noinline__ float4 odd_values(const PagedArgs& a, int b, int h, int node, int n, int from, int to, int d,
+                                          float4 x) {
+  const uint32_t* tree = tree_of(a, b);
+  for (int at = max(max(from, n - a.nodes), 0); at < min(to, n); ++at) {
+    const int page = a.table[(size_t)b * a.width + at / a.page];
+    if (!sees(a, tree, n, node, at) || (unsigned)page >= (unsigned)a.n_pages) continue;
+    const C* p = static_cast<const C*>(a.v_pages) + (((size_t)page * a.kv_heads + h) * a.page + at % a.page) * D + d;
+    float* y = &x.x;
+    for (int e = 0; e < 4; ++e) {
+      const float value = to_f32_any(p[e]);
+      if (!isfinite(value)) y[e] += value;
+    }
+  }
+  return x;
+}
+// The odd halves, bytes or words of x as all ones.
+template <class C> __device__ __forceinline__ uint32_t odd_in(uint32_t x) {
+  if constexpr (sizeof(C) == 4) return (x & 0x7F800000u) == 0x7F800000u ? 0xFFFFFFFFu : 0u;
+  else if constexpr (sizeof(C) == 1) return __vcmpeq4(x & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+  else return __vcmpeq2(x & 0x7F807F80u, 0x7F807F80u);
+}
+
+// Dims d .. d + 3 of a row's result, from the sums of p v and of p (p times 2^lift).
+template <class T>
+__device__ __forceinline__ void write_row(const PagedArgs& a, long long n, int head, int d, int dim, float4 x, float top,
+                                          float sum, float v_scale, float lift) {
+  const float k = sum == 0.0f ? 0.0f : v_scale / sum;      // nothing seen: 0 (an infinite value stays NaN)
+  T* out = static_cast<T*>(a.out) + (n * a.heads + head) * dim + d;
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(out) = make_float4(x.x * k, x.y * k, x.z * k, x.w * k);
+  } else {
+    *reinterpret_cast<uint2*>(out) = make_uint2(bits_of(__floats2bfloat162_rn(x.x * k, x.y * k)),
+                                                bits_of(__floats2bfloat162_rn(x.z * k, x.w * k)));
+  }
+  if (d == 0 && a.lse != nullptr)
+    a.lse[n * a.heads + head] = sum == 0.0f ? -INFINITY : (top - lift + log2f(sum)) * kLn2;
+}
+
+// A power of two that takes a row's largest magnitude, `top`, to [1, 2), for fp16; 1 for
+// rows of zeros, subnormals and infinities.
+__device__ __forceinline__ float row_power(float top) {
+  const uint32_t e = __float_as_uint(top) >> 23;
+  return e > 0 && e < 254 ? __uint_as_float(e << 23) : 1.0f;
+}
+
+// Where row r of a key head's rows stands in q.
+template <class Q> __device__ __forceinline__ const Q* row_of(const PagedArgs& a, int b, int h, int r) {
+  const int node = r / a.group;
+  return static_cast<const Q*>(a.q) + ((long long)b * a.nodes + node) * a.q_ld +
+         (long long)(h * a.group + (r - node * a.group)) * a.q_hs;
+}
+
+// A row whose segment is cut between runs, joined in their order; rows of sequences
+// without entries get 0.  A warp a row.
+template <class K, class C, class Q, int D>
+__global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_constant__ PagedArgs a, int runs) {
+  extern __shared__ __align__(16) uint8_t raw[];
+  uint32_t* before = reinterpret_cast<uint32_t*>(raw);
+  __shared__ uint32_t scratch[kWarps];
+  const int lane = threadIdx.x & 31;
+  const Plan plan = make_plan<K>(a, before, scratch, runs);
+  pdl_wait();
+  pdl_trigger();
+  const long long rows = (long long)a.B * a.nodes * a.heads;
+  for (long long i = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * kWarps) {
+    const long long n = i / a.heads;
+    const int head = (int)(i - n * a.heads), b = (int)(n / a.nodes), node = (int)(n - (long long)b * a.nodes);
+    const int h = head / a.group, row = node * a.group + head - h * a.group;
+    const uint32_t segments = a.kv_heads * a.row_blocks, count = before[b + 1] - before[b];
+    const float v_scale = sizeof(C) == 1 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
+    if (count == 0) {
+      for (int d = 4 * lane; d < D; d += 128)
+        write_row<Q>(a, n, head, d, D, make_float4(0.0f, 0.0f, 0.0f, 0.0f), -INFINITY, 0.0f, 1.0f, 0.0f);
+      continue;
+    }
+    const uint64_t s0 = (uint64_t)before[b] * segments + (uint64_t)(h * a.row_blocks + row / K::kRows) * count;
+    const uint32_t first = plan.run_of(s0 + K::kFront), last = plan.run_of(s0 + count - 1);
+    if (first == last) continue;     // written already
+    const float* base = static_cast<const float*>(a.workspace);
+    const int r = row % K::kRows;
+    const bool second = plan.start(first) < s0;            // the first run's second slot
+    auto slot = [&](uint32_t run) { return base + ((size_t)run * 2 + (run == first && second)) * K::kSlot; };
+    float top = -INFINITY;
+    for (uint32_t run = first + lane; run <= last; run += 32) top = fmaxf(top, __ldcg(slot(run) + K::kRows * D + 2 * r));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float sum = 0.0f;
+    constexpr int kVecs = (D + 127) / 128;
+    float4 x[kVecs];
+#pragma unroll
+    for (int c = 0; c < kVecs; ++c) x[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (uint32_t run = first; run <= last; ++run) {
+      const float* p = slot(run);
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + K::kRows * D + 2 * r));
+      const float c = ml.x == top ? 1.0f : exp2_(ml.x - top);
+      sum += c * ml.y;
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) {
+        const int d = 128 * v + 4 * lane;
+        if (d < D) {
+          const float4 y = __ldcg(reinterpret_cast<const float4*>(p + r * D + d));
+          x[v].x += c * y.x; x[v].y += c * y.y; x[v].z += c * y.z; x[v].w += c * y.w;
+        }
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+      const int d = 128 * v + 4 * lane;
+      if (d < D) write_row<Q>(a, n, head, d, D, x[v], top, sum, v_scale, K::kLift);
+    }
+  }
+}
+
+// Launches a kernel of `grid` CTAs and the joining one, or tells the workspace's bytes.
+template <class K, class C, class Q, int D, class Kernel>
+cudaError_t launch_runs(PagedArgs a, Kernel kernel, size_t shared, int grid, cudaStream_t s, size_t* workspace,
+                        std::atomic<unsigned long long>& raised) {
+  if (workspace != nullptr) {
+    *workspace = (size_t)grid * 2 * K::kSlot * 4;
+    return cudaSuccess;
+  }
+  const uint32_t per_page = a.page / 16;
+  a.page_magic = per_page <= 1 ? 0 : (uint32_t)((1ull << 32) / per_page + 1);
+  a.row_blocks = (a.nodes * a.group + K::kRows - 1) / K::kRows;
+  const size_t plan_bytes = ((size_t)a.B + 1) * 4;
+  cudaError_t e = raise_smem_limit(kernel, 227 * 1024 - 1024, raised);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(kernel, dim3(grid), dim3(kThreads), shared + plan_bytes, s, a);
+  if (e != cudaSuccess) return e;
+  const long long ctas = ((long long)a.B * a.nodes * a.heads + kWarps - 1) / kWarps;
+  return launch_pdl(paged_join_kernel<K, C, Q, D>, dim3((unsigned)(ctas < 152 * 8 ? ctas : 152 * 8)), dim3(kThreads),
+                    plan_bytes, s, a, grid);
+}
+
+// The number of a block of 16 entries' page in the table: a page has 1 to 64 blocks and a
+// sequence fewer than 2^26, for which the product is exact.
+__device__ __forceinline__ uint32_t page_of(const PagedArgs& a, uint32_t block) {
+  return a.page_magic == 0 ? block : __umulhi(block, a.page_magic);
+}
+
+}  // namespace
+
+}  // namespace fovea

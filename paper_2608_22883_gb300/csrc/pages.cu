@@ -9,56 +9,53 @@ namespace fovea {
 
 namespace {
 
-constexpr int kKeepThreads = 256, kKeepBytes = 48 * 1024;
+constexpr int kKeepThreads = 128, kKeepBytes = 48 * 1024;
 
 // Entry base + i <- entry base + nodes[i], base = lens - size: all sources are read, into
 // shared memory, before an entry is written, so that any list of nodes is right.  A CTA
 // takes `cols` 16-byte columns of a head of a sequence's keys or values.  Bound by latency:
-// a path's entries are a few KB a head.
+// a path's entries are a few KB a head, behind the loads of a length and of a page.
 __global__ void __launch_bounds__(kKeepThreads) cache_keep_kernel(const __grid_constant__ CachePages c,
                                                                   const int32_t* lens, const int32_t* nodes, int path,
                                                                   int size, int cols, int row_vecs, int32_t* new_lens) {
   extern __shared__ uint4 staged[];
-  __shared__ int node_of[FOVEA_MAX_TREE];
+  // each entry's first vector where it is and where it goes; no move: -1
+  __shared__ long long from[FOVEA_MAX_TREE], to[FOVEA_MAX_TREE];
   __shared__ int count;
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x, b = blockIdx.y;
   const int parts = (row_vecs + cols - 1) / cols, h = blockIdx.x / parts, col0 = blockIdx.x % parts * cols;
   if (tid == 0) count = path;
+  const int n = lens[b], base = n - size;
   __syncthreads();
-  const int n = lens[b];
-  for (int i = tid; i < path; i += kKeepThreads) {
-    const int x = nodes[(long long)b * path + i];
-    node_of[i] = x;
-    if ((unsigned)x >= (unsigned)size) atomicMin(&count, i);       // the path ends before it
-  }
-  __syncthreads();
-  const bool there = n >= size;      // else (an idle sequence) nothing moves
-  if (blockIdx.x == 0 && blockIdx.z == 0 && tid == 0) new_lens[b] = there ? n - size + count : n;
-  if (!there) return;
-  uint4* pool = static_cast<uint4*>(blockIdx.z == 0 ? c.k : c.v);
-  const int base = n - size, most = min(cols, row_vecs - col0);
   const long long room = (long long)c.width * c.page;
-  auto place = [&](int e) -> long long {                           // of an entry's first vector, -1: none
+  auto place = [&](int e) -> long long {                 // of an entry's first vector, -1: none
     if (e >= room) return -1;
     const int id = c.table[(long long)b * c.width + e / c.page];
     if ((unsigned)id >= (unsigned)c.n_pages) return -1;
     return (((long long)id * c.kv_heads + h) * c.page + e % c.page) * row_vecs + col0;
   };
-  for (int i = tid; i < count * most; i += kKeepThreads) {
-    const int p = i / most;
-    if (node_of[p] == p) continue;
-    const long long from = place(base + node_of[p]);
-    if (from >= 0) staged[i] = pool[from + i % most];
+  for (int i = tid; i < path; i += kKeepThreads) {
+    const int x = nodes[(long long)b * path + i];
+    const bool valid = (unsigned)x < (unsigned)size;
+    if (!valid) atomicMin(&count, i);                    // the path ends before it
+    const bool moves = valid && x != i && base >= 0;     // a shorter (idle) sequence stays as it is
+    const long long p = moves ? place(base + x) : -1, q = moves ? place(base + i) : -1;
+    from[i] = q < 0 ? -1 : p;
+    to[i] = q;
   }
   __syncthreads();
-  for (int i = tid; i < count * most; i += kKeepThreads) {
-    const int p = i / most;
-    if (node_of[p] == p || place(base + node_of[p]) < 0) continue;
-    const long long to = place(base + p);
-    if (to >= 0) pool[to + i % most] = staged[i];
+  if (blockIdx.x == 0 && blockIdx.z == 0 && tid == 0) new_lens[b] = base >= 0 ? base + count : n;
+  uint4* pool = static_cast<uint4*>(blockIdx.z == 0 ? c.k : c.v);
+  const int most = min(cols, row_vecs - col0), total = count * most;
+  for (int i = tid; i < total; i += kKeepThreads) {
+    const long long p = from[i / most];
+    if (p >= 0) staged[i] = pool[p + i % most];
   }
+  __syncthreads();
+  for (int i = tid; i < total; i += kKeepThreads)
+    if (from[i / most] >= 0) pool[to[i / most] + i % most] = staged[i];
 }
 
 // ---------------------------------------------------------------------------
@@ -112,34 +109,74 @@ __device__ __forceinline__ int block_scan(int x, int* scratch, int& total) {
   return before;
 }
 
+// Shared memory of the plan, in words: the marks, a bit a page; of each continuation; the
+// table of last pages.
+struct PlanLayout {
+  int words, C, slots;               // slots: of the table, a power of two
+  __host__ __device__ PlanLayout(int n_pages, int C_) : words((n_pages + 31) / 32), C(C_), slots(32) {
+    while (slots < 2 * C) slots *= 2;
+  }
+  __host__ __device__ size_t total() const { return (size_t)words + 6 * (size_t)C + 1 + 2 * (size_t)slots; }
+};
+__device__ __forceinline__ uint32_t slot_of(int page, int slots) { return ((uint32_t)page * 2654435761u >> 8) & (slots - 1); }
+
 // Which pages are held, which last pages stay, and the fresh pages of every continuation,
-// the lowest free pages first.  One CTA: the marks are a bit a page in shared memory, and
-// the steps depend on one another.  Writes the fresh entries of the new table, the entry
-// of each partly filled page and the number of pages left; the rest is the copies' kernel's.
+// the lowest free pages first.  One CTA, bound by latency: the marks are a bit a page in
+// shared memory, and the steps depend on one another.  Writes the fresh entries of the new
+// table, the entry of each partly filled page and the number of pages left; the rest is the
+// copies' kernel's.
 __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const __grid_constant__ CachePages c,
                                                                  const __grid_constant__ ForkArgs f) {
-  extern __shared__ uint32_t marks[];                    // a bit a page, then the children's arrays
-  const int words = (c.n_pages + 31) / 32;
-  int* last = reinterpret_cast<int*>(marks + words);     // partly filled page of a child, -1: none
-  int* begin = last + f.C;                               // fresh pages of the children before it
-  int* have = begin + f.C + 1;                           // pages that it has without fresh ones
+  extern __shared__ uint32_t marks[];
+  const PlanLayout y(c.n_pages, f.C);
+  int* last = reinterpret_cast<int*>(marks + y.words);   // partly filled page of a child, -1: none
+  int* parent = last + f.C;
+  int* whole = parent + f.C;                             // full pages
+  int* need = whole + f.C;                               // pages that it shall have
+  int* have = need + f.C;                                // pages that it has without fresh ones
+  int* begin = have + f.C;                               // fresh pages of the children before it
+  int* keys = begin + f.C + 1;                           // last pages, -1: an empty slot
+  int* first = keys + y.slots;                           // the first child that holds each
   __shared__ int scratch[kPlanThreads / 32];
   __shared__ int chunk_free[kPlanThreads];               // free pages before each thread's words
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  for (int i = tid; i < words; i += kPlanThreads) marks[i] = 0;
+  for (int child = tid; child < f.C; child += kPlanThreads) {
+    const Kept k = kept_of(c, f, child);
+    parent[child] = k.parent;
+    whole[child] = k.whole;
+    need[child] = k.need;
+    last[child] = k.rest > 0 ? 0 : -1;
+  }
+  for (int i = tid; i < y.words; i += kPlanThreads) marks[i] = 0;
+  for (int i = tid; i < y.slots; i += kPlanThreads) {
+    keys[i] = -1;
+    first[i] = f.C;
+  }
   __syncthreads();
   for (int child = warp; child < f.C; child += kPlanThreads / 32) {
-    const Kept k = kept_of(c, f, child);
-    const int32_t* row = c.table + (long long)max(k.parent, 0) * c.width;
-    for (int i = lane; i < k.whole; i += 32) {
+    const int n = whole[child];
+    const bool part = last[child] >= 0;
+    const int32_t* row = c.table + (long long)max(parent[child], 0) * c.width;
+    for (int i = lane; i < n + part; i += 32) {
       const int id = row[i];
-      if ((unsigned)id < (unsigned)c.n_pages) atomicOr(&marks[id >> 5], 1u << (id & 31));
-    }
-    if (lane == 0) {
-      const int id = k.rest > 0 ? row[k.whole] : -1;
-      last[child] = (unsigned)id < (unsigned)c.n_pages ? id : -1;
+      const bool there = (unsigned)id < (unsigned)c.n_pages;
+      if (i < n) {
+        if (there) atomicOr(&marks[id >> 5], 1u << (id & 31));
+      } else {
+        // its place in the table of last pages (at most half full: the search ends)
+        last[child] = there ? id : -2;                   // -2: a partly filled page outside the pool
+        if (there) {
+          uint32_t at = slot_of(id, y.slots);
+          while (true) {
+            const int key = atomicCAS(&keys[at], -1, id);
+            if (key == -1 || key == id) break;
+            at = (at + 1) & (y.slots - 1);
+          }
+          atomicMin(&first[at], child);
+        }
+      }
     }
   }
   __syncthreads();
@@ -148,36 +185,35 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const __grid_co
   const int per = (f.C + kPlanThreads - 1) / kPlanThreads;
   const int c0 = min(tid * per, f.C), c1 = min(c0 + per, f.C);
   for (int child = c0; child < c1; ++child) {
-    const Kept k = kept_of(c, f, child);
-    const int id = last[child];
-    bool stays = k.rest > 0;
+    const int id = last[child], w = whole[child];
+    bool stays = id == -2;
     if (id >= 0) {
-      stays = (marks[id >> 5] >> (id & 31) & 1u) == 0;
-      for (int other = 0; stays && other < child; ++other) stays = last[other] != id;
+      uint32_t at = slot_of(id, y.slots);
+      while (keys[at] != id) at = (at + 1) & (y.slots - 1);
+      stays = first[at] == child && (marks[id >> 5] >> (id & 31) & 1u) == 0;
     }
-    if (stays) f.new_table[(long long)child * f.new_width + k.whole] =
-        id >= 0 ? id : c.table[(long long)k.parent * c.width + k.whole];
-    have[child] = k.whole + stays;
-    sum += k.need - have[child];
+    if (stays)
+      f.new_table[(long long)child * f.new_width + w] = id >= 0 ? id : c.table[(long long)parent[child] * c.width + w];
+    have[child] = w + stays;
+    sum += need[child] - have[child];
   }
   int fresh;
-  int at = block_scan(sum, scratch, fresh);
+  int at = block_scan(sum, scratch, fresh);              // a barrier: the marks have been read
   for (int child = c0; child < c1; ++child) {
     begin[child] = at;
-    at += kept_of(c, f, child).need - have[child];
+    at += need[child] - have[child];
+    const int id = last[child];
+    if (id >= 0) atomicOr(&marks[id >> 5], 1u << (id & 31));
   }
   if (tid == 0) begin[f.C] = fresh;
-  __syncthreads();
-  for (int child = tid; child < f.C; child += kPlanThreads)
-    if (last[child] >= 0) atomicOr(&marks[last[child] >> 5], 1u << (last[child] & 31));
   __syncthreads();
   // free pages: those without a mark
   auto free_in = [&](int word) -> uint32_t {
     const int left = c.n_pages - 32 * word;
     return ~marks[word] & (left >= 32 ? 0xffffffffu : (1u << left) - 1u);
   };
-  const int span = (words + kPlanThreads - 1) / kPlanThreads;
-  const int w0 = min(tid * span, words), w1 = min(w0 + span, words);
+  const int span = (y.words + kPlanThreads - 1) / kPlanThreads;
+  const int w0 = min(tid * span, y.words), w1 = min(w0 + span, y.words);
   sum = 0;
   for (int i = w0; i < w1; ++i) sum += __popc(free_in(i));
   int available;
@@ -204,18 +240,20 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const __grid_co
         skip -= here;
         ++word;
       }
-      id = 32 * word + __fns(free_in(word), 0, skip + 1);
+      uint32_t bits = free_in(word);
+      for (; skip > 0; --skip) bits &= bits - 1;
+      id = 32 * word + __ffs(bits) - 1;
     }
     f.new_table[(long long)lo * f.new_width + have[lo] + (r - begin[lo])] = id;
   }
 }
 
 // The new tables' other entries and lengths, and the copies of last pages: a CTA a child,
-// head and kind.
+// head and kind.  What does not depend on the plan, the entries to copy among it (no page is
+// both copied from and to), is read while that is made.
 __global__ void __launch_bounds__(256) fork_copy_kernel(const __grid_constant__ CachePages c,
                                                         const __grid_constant__ ForkArgs f, int row_vecs) {
-  pdl_wait();
-  pdl_trigger();
+  constexpr int kAhead = 4;
   const int tid = threadIdx.x, child = blockIdx.x, h = blockIdx.y >> 1;
   const Kept k = kept_of(c, f, child);
   const int32_t* row = c.table + (long long)max(k.parent, 0) * c.width;
@@ -227,20 +265,28 @@ __global__ void __launch_bounds__(256) fork_copy_kernel(const __grid_constant__ 
     }
     if (tid == 0) f.new_lens[child] = k.n;
   }
-  if (k.rest == 0 || *f.free < 0) return;
-  const int src = row[k.whole], dst = to[k.whole];
-  if (src == dst || (unsigned)src >= (unsigned)c.n_pages || (unsigned)dst >= (unsigned)c.n_pages) return;
+  const int src = k.rest > 0 ? row[k.whole] : -1, n = k.rest * row_vecs;
+  const bool there = (unsigned)src < (unsigned)c.n_pages;
   uint4* pool = static_cast<uint4*>(blockIdx.y & 1 ? c.v : c.k);
-  const uint4* p = pool + ((long long)src * c.kv_heads + h) * c.page * row_vecs;
+  const uint4* p = pool + ((long long)(there ? src : 0) * c.kv_heads + h) * c.page * row_vecs;
+  uint4 x[kAhead];
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j)
+    if (there && tid + 256 * j < n) x[j] = p[tid + 256 * j];
+  pdl_wait();
+  pdl_trigger();
+  if (!there || *f.free < 0) return;
+  const int dst = to[k.whole];
+  if (src == dst || (unsigned)dst >= (unsigned)c.n_pages) return;
   uint4* q = pool + ((long long)dst * c.kv_heads + h) * c.page * row_vecs;
-  const int n = k.rest * row_vecs;
-  for (int i = tid; i < n; i += 4 * 256) {               // four on their way together
-    uint4 x[4];
+  for (int i = tid; i < n; i += kAhead * 256) {
+    if (i != tid) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (i + 256 * j < n) x[j] = p[i + 256 * j];
+      for (int j = 0; j < kAhead; ++j)
+        if (i + 256 * j < n) x[j] = p[i + 256 * j];
+    }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < kAhead; ++j)
       if (i + 256 * j < n) q[i + 256 * j] = x[j];
   }
 }
@@ -263,8 +309,8 @@ cudaError_t launch_cache_keep(const CachePages& c, const int32_t* lens, const in
 
 cudaError_t launch_cache_fork(const CachePages& c, const ForkArgs& f, cudaStream_t s) {
   static std::atomic<unsigned long long> raised{0};
-  const size_t smem = ((size_t)(c.n_pages + 31) / 32 + 3 * (size_t)f.C + 1) * 4;
-  cudaError_t e = raise_smem_limit(fork_plan_kernel, 200 * 1024, raised);
+  const size_t smem = PlanLayout(c.n_pages, f.C).total() * 4;
+  cudaError_t e = raise_smem_limit(fork_plan_kernel, 220 * 1024, raised);
   if (e != cudaSuccess) return e;
   e = launch_pdl(fork_plan_kernel, dim3(1), dim3(kPlanThreads), smem, s, c, f);
   if (e != cudaSuccess || f.C == 0) return e;

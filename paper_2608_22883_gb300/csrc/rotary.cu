@@ -123,10 +123,9 @@ template <int E> struct Turn {
 
 // The heads block, block + blocks, ... of a token: from `in`, `step` elements from one to the
 // next, to `out`.  TURN: they are rotated where the thread's dims are; ADJ: in adjacent pairs.
-template <class T, class C, int E, bool ADJ, bool TURN>
+template <class T, class C, int E, bool ADJ, bool TURN, int kHeads>
 __device__ __forceinline__ void run_heads(const Turn<E>& w, const T* in, long long step, C* out, long long out_step,
                                           int block, int blocks, int heads, const float* scales) {
-  constexpr int kHeads = kAhead<T>;
   for (int h = block; h < heads; h += kHeads * blocks) {
     Chunk<T, E> x[kHeads][2];
 #pragma unroll
@@ -171,21 +170,30 @@ __device__ __forceinline__ void run_heads(const Turn<E>& w, const T* in, long lo
   }
 }
 
-template <class T, class C, int E, bool ADJ, bool PAGED>
-__global__ void __launch_bounds__(kMaxThreads, kResident<T>) rotary_kernel(const __grid_constant__ Work w) {
-  __shared__ unsigned long long phase[kRotaryPairs];     // turns per position, times 2^64
-  __shared__ int axis_of[kRotaryPairs];                  // -1: no number
+// MODE: rotated rows to dense outputs, to pages, or rows as they are to pages (with two heads
+// on their way: 16 trees of 64 entries of 40 heads stored and kept, 13.1 us; one 14.6, four
+// and two CTAs an SM 16.2).
+enum Mode { kDense, kTurned, kPlain };
+
+template <class T, class C, int E, bool ADJ, int MODE>
+__global__ void __launch_bounds__(kMaxThreads, MODE == kPlain ? 4 : kResident<T>) rotary_kernel(const __grid_constant__ Work w) {
+  constexpr bool PAGED = MODE != kDense, ROTARY = MODE != kPlain;
+  constexpr int kHeads = MODE == kPlain && sizeof(T) == 2 ? 2 : kAhead<T>;
+  __shared__ unsigned long long phase[ROTARY ? kRotaryPairs : 1];     // turns per position, times 2^64
+  __shared__ int axis_of[ROTARY ? kRotaryPairs : 1];                  // -1: no number
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x;
-  for (int j = tid; j < w.r.rot / 2; j += blockDim.x) {
-    double f = w.r.frequencies[j] * 0.15915494309189533577;       // 1 / (2 pi)
-    const int axis = w.r.axis != nullptr ? w.r.axis[j] : 0;
-    axis_of[j] = (unsigned)axis < (unsigned)w.r.axes && isfinite(f) ? axis : -1;
-    f -= rint(f);                                                 // within half a turn
-    phase[j] = (unsigned long long)__double2ll_rn(f * 18446744073709551616.0);
+  if constexpr (ROTARY) {
+    for (int j = tid; j < w.r.rot / 2; j += blockDim.x) {
+      double f = w.r.frequencies[j] * 0.15915494309189533577;     // 1 / (2 pi)
+      const int axis = w.r.axis != nullptr ? w.r.axis[j] : 0;
+      axis_of[j] = (unsigned)axis < (unsigned)w.r.axes && isfinite(f) ? axis : -1;
+      f -= rint(f);                                               // within half a turn
+      phase[j] = (unsigned long long)__double2ll_rn(f * 18446744073709551616.0);
+    }
+    __syncthreads();
   }
-  __syncthreads();
   const int per_token = w.blocks * w.slots;
   const int local = tid / per_token, rest = tid - local * per_token;
   const int block = rest / w.slots, slot = rest - block * w.slots;
@@ -205,7 +213,7 @@ __global__ void __launch_bounds__(kMaxThreads, kResident<T>) rotary_kernel(const
       }
       if (place < 0 && w.q.heads == 0) continue;
     }
-    if (t.turns) {
+    if (ROTARY && t.turns) {
       int axis = -2, p = 0;
 #pragma unroll
       for (int i = 0; i < E; ++i) {
@@ -220,27 +228,27 @@ __global__ void __launch_bounds__(kMaxThreads, kResident<T>) rotary_kernel(const
       }
     }
     const long long out_step = (long long)w.blocks * w.dim;
-    if (w.q.heads > 0)
-      run_heads<T, T, E, ADJ, true>(t, static_cast<const T*>(w.q.x) + n * w.q.ld + block * w.q.hs + t.at, w.blocks * w.q.hs,
+    if (ROTARY && w.q.heads > 0)
+      run_heads<T, T, E, ADJ, true, kHeads>(t, static_cast<const T*>(w.q.x) + n * w.q.ld + block * w.q.hs + t.at, w.blocks * w.q.hs,
                                static_cast<T*>(w.q_out) + (n * w.q.heads + block) * w.dim + t.at, out_step, block,
                                w.blocks, w.q.heads, nullptr);
     const T* k = static_cast<const T*>(w.k.x) + n * w.k.ld + block * w.k.hs + t.at;
     if constexpr (PAGED) {
       if (place < 0) continue;
       const long long to = (place + (long long)block * w.c.page) * w.dim + t.at, page_step = out_step * w.c.page;
-      run_heads<T, C, E, ADJ, true>(t, k, w.blocks * w.k.hs, static_cast<C*>(w.c.k) + to, page_step, block, w.blocks,
+      run_heads<T, C, E, ADJ, MODE == kTurned, kHeads>(t, k, w.blocks * w.k.hs, static_cast<C*>(w.c.k) + to, page_step, block, w.blocks,
                                w.k.heads, w.c.k_scale);
-      run_heads<T, C, E, ADJ, false>(t, static_cast<const T*>(w.v.x) + n * w.v.ld + block * w.v.hs + t.at,
+      run_heads<T, C, E, ADJ, false, kHeads>(t, static_cast<const T*>(w.v.x) + n * w.v.ld + block * w.v.hs + t.at,
                                 w.blocks * w.v.hs, static_cast<C*>(w.c.v) + to, page_step, block, w.blocks, w.v.heads,
                                 w.c.v_scale);
     } else if (w.k.heads > 0) {
-      run_heads<T, T, E, ADJ, true>(t, k, w.blocks * w.k.hs, static_cast<T*>(w.k_out) + (n * w.k.heads + block) * w.dim + t.at,
+      run_heads<T, T, E, ADJ, true, kHeads>(t, k, w.blocks * w.k.hs, static_cast<T*>(w.k_out) + (n * w.k.heads + block) * w.dim + t.at,
                                out_step, block, w.blocks, w.k.heads, nullptr);
     }
   }
 }
 
-template <class T, class C, int E, bool ADJ, bool PAGED>
+template <class T, class C, int E, bool ADJ, int MODE>
 cudaError_t launch_as(Work w, cudaStream_t s) {
   const int rot = w.r.rot, heads = w.q.heads + w.k.heads + w.v.heads;
   w.turned = rot / 2 / E;
@@ -258,7 +266,7 @@ cudaError_t launch_as(Work w, cudaStream_t s) {
   // CTAs go on to further tokens: each makes the table of turns, which a CTA for every few
   // tokens would pay for (image prompts 66 us instead of 62)
   const int grid = (int)(ctas < 152 * 4 ? ctas : 152 * 4);
-  return launch_pdl(rotary_kernel<T, C, E, ADJ, PAGED>, dim3(grid), dim3(threads), 0, s, w);
+  return launch_pdl(rotary_kernel<T, C, E, ADJ, MODE>, dim3(grid), dim3(threads), 0, s, w);
 }
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -266,13 +274,16 @@ bool vectors(const HeadRows& r, size_t size) {
   return r.heads == 0 || (aligned(r.x, 16) && r.ld * size % 16 == 0 && r.hs * size % 16 == 0);
 }
 
-template <class T, class C, bool PAGED>
+template <class T, class C, int MODE>
 cudaError_t launch_type(const Work& w, cudaStream_t s) {
   constexpr int E = kChunk;
   const bool whole = w.dim % (2 * E) == 0 && w.r.rot % (2 * E) == 0 && vectors(w.q, sizeof(T)) && vectors(w.k, sizeof(T)) &&
                      vectors(w.v, sizeof(T)) && aligned(w.q_out, 16) && aligned(w.k_out, 16);
-  return whole ? (w.r.adjacent ? launch_as<T, C, E, true, PAGED>(w, s) : launch_as<T, C, E, false, PAGED>(w, s))
-               : (w.r.adjacent ? launch_as<T, C, 1, true, PAGED>(w, s) : launch_as<T, C, 1, false, PAGED>(w, s));
+  if constexpr (MODE != kPlain) {
+    if (w.r.adjacent)
+      return whole ? launch_as<T, C, E, true, MODE>(w, s) : launch_as<T, C, 1, true, MODE>(w, s);
+  }
+  return whole ? launch_as<T, C, E, false, MODE>(w, s) : launch_as<T, C, 1, false, MODE>(w, s);
 }
 
 }  // namespace
@@ -282,8 +293,8 @@ cudaError_t launch_rotary(int dtype, const HeadRows& q, const HeadRows& k, int N
   Work w{};
   w.q = q; w.k = k; w.N = N; w.dim = dim; w.r = r;
   w.q_out = q_out; w.k_out = k_out;
-  return dtype == FOVEA_BF16 ? launch_type<__nv_bfloat16, __nv_bfloat16, false>(w, s)
-                             : launch_type<float, float, false>(w, s);
+  return dtype == FOVEA_BF16 ? launch_type<__nv_bfloat16, __nv_bfloat16, kDense>(w, s)
+                             : launch_type<float, float, kDense>(w, s);
 }
 
 cudaError_t launch_cache_append(int dtype, const HeadRows& q, const HeadRows& k, const HeadRows& v, int N,
@@ -293,9 +304,13 @@ cudaError_t launch_cache_append(int dtype, const HeadRows& q, const HeadRows& k,
   w.q = q; w.k = k; w.v = v; w.N = N; w.dim = c.dim; w.r = r;
   w.q_out = q_out;
   w.c = c; w.sequence = sequence; w.entry = entry;
-  return dtype == FOVEA_FP32         ? launch_type<float, float, true>(w, s)
-         : c.dtype == FOVEA_E4M3 ? launch_type<__nv_bfloat16, __nv_fp8_e4m3, true>(w, s)
-                                 : launch_type<__nv_bfloat16, __nv_bfloat16, true>(w, s);
+  if (r.rot == 0)
+    return dtype == FOVEA_FP32     ? launch_type<float, float, kPlain>(w, s)
+           : c.dtype == FOVEA_E4M3 ? launch_type<__nv_bfloat16, __nv_fp8_e4m3, kPlain>(w, s)
+                                   : launch_type<__nv_bfloat16, __nv_bfloat16, kPlain>(w, s);
+  return dtype == FOVEA_FP32     ? launch_type<float, float, kTurned>(w, s)
+         : c.dtype == FOVEA_E4M3 ? launch_type<__nv_bfloat16, __nv_fp8_e4m3, kTurned>(w, s)
+                                 : launch_type<__nv_bfloat16, __nv_bfloat16, kTurned>(w, s);
 }
 
 }  // namespace fovea
