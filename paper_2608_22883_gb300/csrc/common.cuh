@@ -518,6 +518,7 @@ struct PagedArgs {
   void* workspace;
   // set by the launch
   int row_blocks;                                  // of a key head
+  bool q_words;                                    // pairs of 16-bit elements of q are aligned
   uint32_t page_magic;                             // block / (page / 16) = the high word of block * this; 0: block
 };
 size_t paged_attention_workspace(const PagedArgs& a);

@@ -277,6 +277,7 @@ cudaError_t launch_runs(PagedArgs a, Kernel kernel, size_t shared, int grid, cud
   }
   const uint32_t per_page = a.page / 16;
   a.page_magic = per_page <= 1 ? 0 : (uint32_t)((1ull << 32) / per_page + 1);
+  a.q_words = (reinterpret_cast<uintptr_t>(a.q) & 3) == 0 && a.q_ld % 2 == 0 && a.q_hs % 2 == 0;
   a.row_blocks = (a.nodes * a.group + K::kRows - 1) / K::kRows;
   const size_t plan_bytes = ((size_t)a.B + 1) * 4;
   cudaError_t e = raise_smem_limit(kernel, 227 * 1024 - 1024, raised);

@@ -32,7 +32,7 @@ template <class C, int D> struct Rows {
   static constexpr bool kE4 = sizeof(C) == 1;
   static constexpr float kLift = kE4 ? 15.0f : 0.0f;             // as in paged.cu
   static constexpr int kRows = 16 * kWarps, kTile = D == 256 ? 32 : 64, kBlock = kTile, kLeast = 1;
-  static constexpr uint32_t kFront = 4;
+  static constexpr uint32_t kFront = 2;
   static constexpr int kSlot = kRows * (D + 2);
   static constexpr int kRowBytes = D * sizeof(C), kChunks = kRowBytes / 16;
   static constexpr int kTileBytes = kTile * kRowBytes;
@@ -87,12 +87,36 @@ template <class C, int D> struct Rows {
             if constexpr (kE4) {
               v = bits_of(__floats2half2_rn(to_f32(d[0]) * k, to_f32(d[1]) * k));
             } else {
-              const uint16_t* w = reinterpret_cast<const uint16_t*>(d);
-              v = (uint32_t)w[0] | ((uint32_t)w[1] << 16);
+              if (a.q_words) {
+                v = *reinterpret_cast<const uint32_t*>(d);
+              } else {
+                const uint16_t* w = reinterpret_cast<const uint16_t*>(d);
+                v = (uint32_t)w[0] | ((uint32_t)w[1] << 16);
+              }
             }
           }
           q[i][2 * x + e] = v;
         }
+    }
+  }
+
+  // Which of the entries first .. first + 63 row `node` sees, those from `end` on not.
+  __device__ __forceinline__ static void seen_bits(const PagedArgs& a, const uint32_t* tree, int n, int node, int first,
+                                                   int end, uint32_t (&bits)[2]) {
+    const int j0 = first - (n - a.nodes), w0 = j0 >> 5;          // the first one's number among the newest
+    uint32_t w[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const int word = w0 + k;
+      if (word < 0) w[k] = 0xFFFFFFFFu;                          // before the newest: seen
+      else if (tree != nullptr) w[k] = word < a.words ? tree[(size_t)node * a.words + word] : 0u;
+      else w[k] = node >= 32 * word + 31 ? 0xFFFFFFFFu : node < 32 * word ? 0u : (2u << (node - 32 * word)) - 1u;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      bits[k] = __funnelshift_r(w[k], w[k + 1], j0 & 31);
+      const int left = end - first - 32 * k;
+      if (left < 32) bits[k] &= left <= 0 ? 0u : (1u << left) - 1u;
     }
   }
 
@@ -192,12 +216,14 @@ template <class C, int D> struct Rows {
         float s[kTile / 8][4];
 #pragma unroll
         for (int j = 0; j < kTile / 8; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.0f;
+        // a step of the dims for all entries, then the next: products in a row have
+        // accumulators of their own
+        if constexpr (kE4) {
+          // matrices (entries 0-7, 8-15) of chunk i, of chunk i + 1
 #pragma unroll
-        for (int j = 0; j < kTile / 16; ++j) {
-          if constexpr (kE4) {
-            // entries 16j .. + 15 by two steps a time: matrices (entries 0-7, 8-15) of chunk i, of chunk i + 1
+          for (int i = 0; i < kSteps; i += 2)
 #pragma unroll
-            for (int i = 0; i < kSteps; i += 2) {
+            for (int j = 0; j < kTile / 16; ++j) {
               uint32_t r[4];
               ldmatrix4(r, ks + place(16 * j + (lane & 15), i + (lane >> 4)));
 #pragma unroll
@@ -207,16 +233,17 @@ template <class C, int D> struct Rows {
                   mma16<kE4>(s[2 * j + x], q[i + c], halves_of_e4m3(r[2 * c + x] & 0xFFFFu),
                              halves_of_e4m3(r[2 * c + x] >> 16));
             }
-          } else {
-            // matrices (entries 0-7) of chunks 2i and 2i + 1, (entries 8-15) of the same
+        } else {
+          // matrices (entries 0-7) of chunks 2i and 2i + 1, (entries 8-15) of the same
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
+          for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int j = 0; j < kTile / 16; ++j) {
               uint32_t r[4];
               ldmatrix4(r, ks + place(16 * j + (lane & 7) + (lane >> 4) * 8, 2 * i + (lane >> 3 & 1)));
               mma16<kE4>(s[2 * j], q[i], r[0], r[1]);
               mma16<kE4>(s[2 * j + 1], q[i], r[2], r[3]);
             }
-          }
         }
 #pragma unroll
         for (int j = 0; j < kTile / 8; ++j)
@@ -226,14 +253,17 @@ template <class C, int D> struct Rows {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int node = min((warp_row + g + 8 * e) / a.group, a.nodes - 1);
+            uint32_t bits[2];                                    // entries 0-31, 32-63 of the tile
+            seen_bits(a, tree, n, node, first, end, bits);
+            bits[0] >>= 2 * t;
+            bits[1] >>= 2 * t;
 #pragma unroll
             for (int j = 0; j < kTile / 8; ++j)
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
-                const int entry = first + 8 * j + 2 * t + x;
-                const bool yes = entry < end && sees(a, tree, n, node, entry);
-                const bool out = outside >> (j / 2) & 1u;
-                s[j][2 * e + x] = yes ? (out ? NAN : s[j][2 * e + x]) : -INFINITY;
+                float& y = s[j][2 * e + x];
+                y = bits[j / 4] >> (8 * (j & 3) + x) & 1u ? y : -INFINITY;
+                if (outside >> (j / 2) & 1u && y > -INFINITY) y = NAN;
               }
           }
         }
@@ -297,13 +327,14 @@ template <class C, int D> struct Rows {
             }
           } else {
 #pragma unroll
-            for (int i = 0; i < kChunks; i += 2) {
-              uint32_t r[4];
-              ldmatrix4_trans(r, vs + place(16 * j + (lane & 15), i + (lane >> 4)));
-              mma16<kE4>(o[i], hi_, r[0], r[1]);
-              mma16<kE4>(o[i + 1], hi_, r[2], r[3]);
-              mma16<kE4>(o[i], lo_, r[0], r[1]);
-              mma16<kE4>(o[i + 1], lo_, r[2], r[3]);
+            for (int i = 0; i < kChunks; i += 4) {
+              uint32_t r[2][4];
+              ldmatrix4_trans(r[0], vs + place(16 * j + (lane & 15), i + (lane >> 4)));
+              ldmatrix4_trans(r[1], vs + place(16 * j + (lane & 15), i + 2 + (lane >> 4)));
+#pragma unroll
+              for (int x = 0; x < 4; ++x) mma16<kE4>(o[i + x], hi_, r[x >> 1][2 * (x & 1)], r[x >> 1][2 * (x & 1) + 1]);
+#pragma unroll
+              for (int x = 0; x < 4; ++x) mma16<kE4>(o[i + x], lo_, r[x >> 1][2 * (x & 1)], r[x >> 1][2 * (x & 1) + 1]);
             }
           }
         }
