@@ -518,14 +518,17 @@ struct PagedArgs {
   void* workspace;
   // set by the launch
   int row_blocks;                                  // of a key head
-  bool q_words;                                    // pairs of 16-bit elements of q are aligned
+  int* header; float* slots; int* gave_up;         // the workspace: partial sums, and a word a run
+  unsigned long long wait_ns;
+  bool q_words, q_chunks;                          // pairs of 16-bit elements of q, 16 bytes of them, are aligned
   uint32_t page_magic;                             // block / (page / 16) = the high word of block * this; 0: block
 };
 size_t paged_attention_workspace(const PagedArgs& a);
 cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s);
-// The same for many rows a key head, bf16 and e4m3 caches (paged_rows.cu); workspace not
-// null: its bytes instead.
+// The same for many rows a key head, bf16 and e4m3 caches (paged_rows.cu; paged_tree.cu on
+// tcgen05); workspace not null: its bytes instead.
 cudaError_t launch_paged_rows(const PagedArgs& a, cudaStream_t s, size_t* workspace);
+cudaError_t launch_paged_tree(const PagedArgs& a, cudaStream_t s, size_t* workspace);
 
 // The memory build's GEMMs out[i] = R . F[i]^T on CTA pairs (gemm_build.cu):
 // token rows R [rows, K] (R0 for part 0, R1 for the others) against up to

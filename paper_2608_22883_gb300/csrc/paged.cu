@@ -65,6 +65,7 @@ template <class C, class Q, int D, int RT>
 struct Attention {
   using G = Cut<C, D>;
   static constexpr bool kF32 = sizeof(C) == 4, kE4 = sizeof(C) == 1;
+  static constexpr bool kWaits = false;
   static constexpr int kRows = 8 * RT, kBlock = 16, kLeast = kWarps;
   static constexpr uint32_t kFront = RT == 1 ? 16 : 24;
   static constexpr int kSlot = kRows * (D + 2);                  // floats of a partial segment
@@ -587,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_attention_
 }
 
 // More rows than these go to the kernel of many rows.
-constexpr int kManyRows = 16;
+constexpr int kManyRows = 16, kTreeRows = 32;
 // Rows that a warp takes together, by 8: as many as there are, up to what its registers hold.
 template <class C, int D> constexpr int most_tiles() {
   return sizeof(C) == 4 || D == 256 ? 1 : D == 128 ? 2 : 4;
@@ -597,13 +598,14 @@ template <class C, class Q, int D, int RT>
 cudaError_t launch_as(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
   using A = Attention<C, Q, D, RT>;
   static std::atomic<unsigned long long> raised{0};
-  return launch_runs<A, C, Q, D>(a, paged_attention_kernel<C, Q, D, RT>, sizeof(typename A::Shared),
+  return launch_runs<A, C, Q, D>(a, paged_attention_kernel<C, Q, D, RT>, kThreads, sizeof(typename A::Shared),
                                  152 * per_sm<C, D, RT>(), s, workspace, raised);
 }
 
 template <class C, class Q, int D>
 cudaError_t launch_dim(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
   const int rows = a.nodes * a.group;
+  if (sizeof(C) < 4 && D < 256 && rows > kTreeRows) return launch_paged_tree(a, s, workspace);
   if (sizeof(C) < 4 && rows > kManyRows) return launch_paged_rows(a, s, workspace);
   if constexpr (most_tiles<C, D>() >= 4)
     if (rows > 16) return launch_as<C, Q, D, 4>(a, s, workspace);

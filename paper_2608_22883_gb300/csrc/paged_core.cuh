@@ -60,7 +60,7 @@ __device__ __forceinline__ int length_of(const PagedArgs& a, int b) {
 }
 __device__ __forceinline__ bool too_long(const PagedArgs& a, int b) { return a.lens[b] > (long long)a.width * a.page; }
 
-// K, of a kernel: kBlock entries a block; kLeast blocks of a run, at least; kFront: the
+// K, of a kernel: kWaits: its waits may give up; kBlock entries a block; kLeast blocks of a run, at least; kFront: the
 // staging of a segment's rows and the end of its sums take a CTA as long as some blocks,
 // and the runs are cut as if each segment had so many empty ones in front.
 template <class K> __device__ __forceinline__ uint32_t blocks_of(int len) {
@@ -103,7 +103,7 @@ __device__ __forceinline__ void each_segment(const PagedArgs& a, const Plan& pla
   if (blockIdx.x >= plan.runs) return;
   const uint64_t from = plan.start(blockIdx.x), to = plan.start(blockIdx.x + 1);
   const uint32_t segments = a.kv_heads * a.row_blocks;    // of a sequence
-  float* slots = static_cast<float*>(a.workspace) + (size_t)blockIdx.x * 2 * K::kSlot;
+  float* slots = a.slots + (size_t)blockIdx.x * 2 * K::kSlot;
   int b = 0;
   {
     int hi = a.B - 1;                // the last b with before[b] * segments <= from
@@ -139,6 +139,31 @@ __device__ __forceinline__ bool sees(const PagedArgs& a, const uint32_t* tree, i
   if (tree == nullptr) return j <= node;
   return (tree[(size_t)node * a.words + (j >> 5)] >> (j & 31)) & 1u;
 }
+  // Which of the entries first .. first + 63 row `node` sees, those from `end` on not.
+  __device__ __forceinline__ void seen_bits(const PagedArgs& a, const uint32_t* tree, int n, int node, int first,
+                                                   int end, uint32_t (&bits)[2]) {
+    const int j0 = first - (n - a.nodes), w0 = j0 >> 5;          // the first one's number among the newest
+    uint32_t w[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const int word = w0 + k;
+      if (word < 0) w[k] = 0xFFFFFFFFu;                          // before the newest: seen
+      else if (tree != nullptr) w[k] = word < a.words ? tree[(size_t)node * a.words + word] : 0u;
+      else w[k] = node >= 32 * word + 31 ? 0xFFFFFFFFu : node < 32 * word ? 0u : (2u << (node - 32 * word)) - 1u;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      bits[k] = __funnelshift_r(w[k], w[k + 1], j0 & 31);
+      const int left = end - first - 32 * k;
+      if (left < 32) bits[k] &= left <= 0 ? 0u : (1u << left) - 1u;
+    }
+  }
+
+// 16 bytes to shared memory, zeros when not `there` (nothing is read then).
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+
 // Entries up to here are seen by all rows.
 __device__ __forceinline__ int plain_end(const PagedArgs& a, int n) {
   return n - a.nodes + (a.nodes == 1 && a.tree == nullptr);
@@ -216,6 +241,14 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
   const Plan plan = make_plan<K>(a, before, scratch, runs);
   pdl_wait();
   pdl_trigger();
+  if (blockIdx.x == 0 && threadIdx.x < 32) {               // the header, and the waits that gave up
+    if (lane == 0) ensure_header(a.header);
+    if constexpr (K::kWaits) {
+      bool any = false;
+      for (uint32_t run = lane; run < plan.runs; run += 32) any |= __ldcg(a.gave_up + run) != 0;
+      if (__any_sync(0xffffffffu, any) && lane == 0) atomicOr(a.header, kErrTimeout);
+    }
+  }
   const long long rows = (long long)a.B * a.nodes * a.heads;
   for (long long i = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * kWarps) {
     const long long n = i / a.heads;
@@ -231,7 +264,7 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
     const uint64_t s0 = (uint64_t)before[b] * segments + (uint64_t)(h * a.row_blocks + row / K::kRows) * count;
     const uint32_t first = plan.run_of(s0 + K::kFront), last = plan.run_of(s0 + count - 1);
     if (first == last) continue;     // written already
-    const float* base = static_cast<const float*>(a.workspace);
+    const float* base = a.slots;
     const int r = row % K::kRows;
     const bool second = plan.start(first) < s0;            // the first run's second slot
     auto slot = [&](uint32_t run) { return base + ((size_t)run * 2 + (run == first && second)) * K::kSlot; };
@@ -269,20 +302,27 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
 
 // Launches a kernel of `grid` CTAs and the joining one, or tells the workspace's bytes.
 template <class K, class C, class Q, int D, class Kernel>
-cudaError_t launch_runs(PagedArgs a, Kernel kernel, size_t shared, int grid, cudaStream_t s, size_t* workspace,
-                        std::atomic<unsigned long long>& raised) {
+cudaError_t launch_runs(PagedArgs a, Kernel kernel, int threads, size_t shared, int grid, cudaStream_t s,
+                        size_t* workspace, std::atomic<unsigned long long>& raised) {
+  const size_t slots = (size_t)grid * 2 * K::kSlot * 4;
   if (workspace != nullptr) {
-    *workspace = (size_t)grid * 2 * K::kSlot * 4;
+    *workspace = kWsHeaderBytes + slots + (size_t)grid * 4;
     return cudaSuccess;
   }
+  uint8_t* ws = static_cast<uint8_t*>(a.workspace);
+  a.header = reinterpret_cast<int*>(ws);
+  a.slots = reinterpret_cast<float*>(ws + kWsHeaderBytes);
+  a.gave_up = reinterpret_cast<int*>(ws + kWsHeaderBytes + slots);
+  a.wait_ns = wait_limit_ns();
   const uint32_t per_page = a.page / 16;
   a.page_magic = per_page <= 1 ? 0 : (uint32_t)((1ull << 32) / per_page + 1);
   a.q_words = (reinterpret_cast<uintptr_t>(a.q) & 3) == 0 && a.q_ld % 2 == 0 && a.q_hs % 2 == 0;
+  a.q_chunks = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && a.q_ld % 8 == 0 && a.q_hs % 8 == 0;
   a.row_blocks = (a.nodes * a.group + K::kRows - 1) / K::kRows;
   const size_t plan_bytes = ((size_t)a.B + 1) * 4;
   cudaError_t e = raise_smem_limit(kernel, 227 * 1024 - 1024, raised);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(kernel, dim3(grid), dim3(kThreads), shared + plan_bytes, s, a);
+  e = launch_pdl(kernel, dim3(grid), dim3(threads), shared + plan_bytes, s, a);
   if (e != cudaSuccess) return e;
   const long long ctas = ((long long)a.B * a.nodes * a.heads + kWarps - 1) / kWarps;
   return launch_pdl(paged_join_kernel<K, C, Q, D>, dim3((unsigned)(ctas < 152 * 8 ? ctas : 152 * 8)), dim3(kThreads),

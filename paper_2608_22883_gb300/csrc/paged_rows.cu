@@ -23,13 +23,8 @@ __device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
-// 16 bytes to shared memory, zeros when not `there` (nothing is read then).
-__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
-}
-
 template <class C, int D> struct Rows {
-  static constexpr bool kE4 = sizeof(C) == 1;
+  static constexpr bool kE4 = sizeof(C) == 1, kWaits = false;
   static constexpr float kLift = kE4 ? 15.0f : 0.0f;             // as in paged.cu
   static constexpr int kRows = 16 * kWarps, kTile = D == 256 ? 32 : 64, kBlock = kTile, kLeast = 1;
   static constexpr uint32_t kFront = 2;
@@ -97,26 +92,6 @@ template <class C, int D> struct Rows {
           }
           q[i][2 * x + e] = v;
         }
-    }
-  }
-
-  // Which of the entries first .. first + 63 row `node` sees, those from `end` on not.
-  __device__ __forceinline__ static void seen_bits(const PagedArgs& a, const uint32_t* tree, int n, int node, int first,
-                                                   int end, uint32_t (&bits)[2]) {
-    const int j0 = first - (n - a.nodes), w0 = j0 >> 5;          // the first one's number among the newest
-    uint32_t w[3];
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      const int word = w0 + k;
-      if (word < 0) w[k] = 0xFFFFFFFFu;                          // before the newest: seen
-      else if (tree != nullptr) w[k] = word < a.words ? tree[(size_t)node * a.words + word] : 0u;
-      else w[k] = node >= 32 * word + 31 ? 0xFFFFFFFFu : node < 32 * word ? 0u : (2u << (node - 32 * word)) - 1u;
-    }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      bits[k] = __funnelshift_r(w[k], w[k + 1], j0 & 31);
-      const int left = end - first - 32 * k;
-      if (left < 32) bits[k] &= left <= 0 ? 0u : (1u << left) - 1u;
     }
   }
 
@@ -418,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, rows_per_sm<C, D>) paged_rows_kernel
 template <class C, int D> cudaError_t launch_as(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
   using A = Rows<C, D>;
   static std::atomic<unsigned long long> raised{0};
-  return launch_runs<A, C, __nv_bfloat16, D>(a, paged_rows_kernel<C, D>, sizeof(typename A::Shared),
+  return launch_runs<A, C, __nv_bfloat16, D>(a, paged_rows_kernel<C, D>, kThreads, sizeof(typename A::Shared),
                                              152 * rows_per_sm<C, D>, s, workspace, raised);
 }
 template <class C> cudaError_t launch_type(const PagedArgs& a, cudaStream_t s, size_t* workspace) {

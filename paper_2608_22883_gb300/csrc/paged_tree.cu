@@ -1,0 +1,587 @@
+// fovea_paged_attention with many rows a key head (draft trees) on tcgen05: paged.cu has
+// the formulas, paged_rows.cu the form for other sizes.
+//
+// A CTA takes 128 rows and tiles of 64 entries.  S = Q K^T goes to tensor memory, a row a
+// lane, so that a thread has a row's scores of a tile and no maximum or sum crosses lanes.
+// It writes p back over the scores, as the first operand of O += P V (two bf16 values that
+// add up to 16 bits of p, or 11 bits of fp16 beside 8-bit values, lifted so that the largest
+// fit).  V lies as it is cached, entries by dims, and is read along its rows (MN-major).
+// Three roles, joined by mbarriers with bounded waits: four warps turn S into P; four copy
+// keys and values of the pages (asynchronous copies, or through registers where 8 bits
+// become fp16) into the 128-byte-swizzled layout; one issues the products.  S of a tile is
+// formed while P of the one before is made (two places in tensor memory), and two CTAs an
+// SM fill one another's waits.
+//
+// O stays in tensor memory.  A row's reference moves only when its maximum has grown by
+// 2^8, so that O is seldom read back and rescaled; until then p is up to 2^8.
+#include <atomic>
+
+#include "paged_core.cuh"
+#include "tc_ptx.cuh"
+
+namespace fovea {
+
+namespace {
+
+using namespace tc;
+
+constexpr int kTreeThreads = 9 * 32;
+constexpr uint32_t kTmemCols = 256;
+constexpr float kSlack = 8.0f;       // growth of a maximum that a row's reference bears
+
+__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc,
+                                        uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void arrive(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+template <class C, int D> struct Tree {
+  static constexpr bool kE4 = sizeof(C) == 1, kWaits = true;
+  static constexpr float kLift = kE4 ? 7.0f : 0.0f;              // p 2^7 2^8 fits fp16
+  static constexpr int kRows = 128, kBlock = 64, kLeast = 1;
+  static constexpr uint32_t kFront = 2;
+  static constexpr int kSlot = kRows * (D + 2);
+  static constexpr int kStages = 2, kParts = kBlock / 16;
+  static constexpr int kHalves = D / 64;                         // blocks of 64 dims, 128 bytes a row
+  static constexpr int kTileBytes = kHalves * kBlock * 128;      // keys or values of a tile, 16 bits each
+  static constexpr int kRowBytes = D * sizeof(C), kChunks = kRowBytes / 16;
+  static constexpr int kPass = 128 / kChunks, kCopies = kBlock / kPass;    // rows a pass of the copying threads
+  static constexpr uint32_t kFormat = kE4 ? 0u : 1u;
+  // D fp32, A and B of the format, M = 128; S: N = 64 entries, K-major; O: N = D dims, MN-major
+  static constexpr uint32_t kIdesc = (1u << 4) | (kFormat << 7) | (kFormat << 10) | ((uint32_t)(kRows >> 4) << 24);
+  static constexpr uint32_t kIdescS = kIdesc | ((uint32_t)(kBlock >> 3) << 17);
+  static constexpr uint32_t kIdescO = kIdesc | ((uint32_t)(D >> 3) << 17) | (1u << 16);
+  static constexpr uint32_t kColS = 128;                         // two places of 64 columns behind O
+
+  struct Shared {
+    uint8_t q[kHalves * kRows * 128];
+    uint8_t kv[kStages][2][kTileBytes];
+    // of the last segments begun, four at most before one is done: rows' powers (8 bits),
+    // and whether a masked tile had odd values
+    float power[4][kRows];
+    int odd[4];
+    uint32_t outside[kStages];       // parts of a tile whose page is not in the pool, as bits
+    uint64_t kv_full[kStages], kv_empty[kStages], q_empty, s_full[2], p_full[2], o_done, drain;
+    uint32_t tmem;
+    int abort;
+    uint32_t scratch[kTreeThreads / 32];
+  };
+  // A chunk of 16 bytes in a tile of rows of 128 bytes with the 128-byte swizzle.
+  __device__ __forceinline__ static uint32_t place(int row, int chunk, int rows) {
+    return (uint32_t)((chunk >> 3) * rows * 128 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4));
+  }
+};
+
+// Sixteen 8-bit values as two chunks of fp16.
+__device__ __forceinline__ void widen(const uint4& x, uint4& lo, uint4& hi) {
+  lo = make_uint4(halves_of_e4m3(x.x & 0xFFFFu), halves_of_e4m3(x.x >> 16), halves_of_e4m3(x.y & 0xFFFFu),
+                  halves_of_e4m3(x.y >> 16));
+  hi = make_uint4(halves_of_e4m3(x.z & 0xFFFFu), halves_of_e4m3(x.z >> 16), halves_of_e4m3(x.w & 0xFFFFu),
+                  halves_of_e4m3(x.w >> 16));
+}
+template <class C> __device__ __forceinline__ uint32_t clear_odd(uint4& x) {
+  const uint4 odd = make_uint4(odd_in<C>(x.x), odd_in<C>(x.y), odd_in<C>(x.z), odd_in<C>(x.w));
+  x = make_uint4(x.x & ~odd.x, x.y & ~odd.y, x.z & ~odd.z, x.w & ~odd.w);
+  return odd.x | odd.y | odd.z | odd.w;
+}
+
+// Copies of the pages: the queries of each segment and its tiles, by warps 4 to 7.
+template <class C, int D> struct Copier {
+  using T = Tree<C, D>;
+  using S = typename T::Shared;
+  const PagedArgs& a;
+  S& sh;
+  int tid;                           // 0 .. 127
+  uint32_t tiles = 0, segments = 0;  // begun
+  bool go = true;
+
+  __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
+    if (!__all_sync(0xffffffffu, mbar_wait(bar, parity, &sh.abort, a.wait_ns))) {
+      *static_cast<volatile int*>(&sh.abort) = 1;
+      go = false;
+    }
+    return go;
+  }
+  __device__ __forceinline__ void queries(int b, int h, int row0) {
+    const int rows = a.nodes * a.group, r = tid, row = row0 + r;
+    const bool there = row < rows;
+    const __nv_bfloat16* p = row_of<__nv_bfloat16>(a, b, h, there ? row : 0);
+    float power = 1.0f;
+    if constexpr (T::kE4) {
+      float top = 0.0f;
+      for (int d = 0; d < D; ++d) top = fmaxf(top, there ? fabsf(to_f32(p[d])) : 0.0f);
+      power = row_power(top);
+      sh.power[segments & 3][r] = power;
+    }
+    const float k = 1.0f / power;
+#pragma unroll 4
+    for (int c = 0; c < D / 8; ++c) {
+      uint4 x = make_uint4(0u, 0u, 0u, 0u);
+      if (there) {
+        if (a.q_chunks) {
+          x = *reinterpret_cast<const uint4*>(p + 8 * c);
+        } else {
+          const uint16_t* w = reinterpret_cast<const uint16_t*>(p + 8 * c);
+          x = make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16,
+                         w[6] | (uint32_t)w[7] << 16);
+        }
+        if constexpr (T::kE4) {
+          uint32_t* w = &x.x;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            w[i] = bits_of(__floats2half2_rn(__uint_as_float(w[i] << 16) * k, __uint_as_float(w[i] & 0xFFFF0000u) * k));
+        }
+      }
+      *reinterpret_cast<uint4*>(sh.q + T::place(r, c, T::kRows)) = x;
+    }
+  }
+
+  __device__ __forceinline__ void segment(int b, int h, int row0, uint32_t lo, uint32_t hi) {
+    if (!go) return;
+    const int n = length_of(a, b);
+    const int end = min(n, (int)(hi * T::kBlock)), plain = min(end, plain_end(a, n));
+    const uint32_t last_block = (uint32_t)(end - 1) / 16;
+    const int32_t* table = a.table + (size_t)b * a.width;
+    const uint32_t per_page = a.page / 16, stride = a.kv_heads * per_page;
+    const uint8_t* keys = static_cast<const uint8_t*>(a.k_pages) + (size_t)h * per_page * 16 * T::kRowBytes;
+    const uint8_t* values = static_cast<const uint8_t*>(a.v_pages) + (size_t)h * per_page * 16 * T::kRowBytes;
+    const bool mixed = a.nodes > 1 || a.tree != nullptr;         // rows may differ in what they see
+    const int chunk = tid % T::kChunks, row = tid / T::kChunks;
+    int id[T::kParts];
+    auto look_up = [&](uint32_t tile) {
+#pragma unroll
+      for (int u = 0; u < T::kParts; ++u) id[u] = table[page_of(a, min(tile * T::kParts + u, last_block))];
+    };
+    unsigned long long off[T::kParts];
+    uint32_t outside = 0;
+    auto find = [&](uint32_t tile) {
+      outside = 0;
+#pragma unroll
+      for (int u = 0; u < T::kParts; ++u) {
+        const uint32_t block = min(tile * T::kParts + u, last_block);
+        const bool out = (unsigned)id[u] >= (unsigned)a.n_pages;
+        outside |= (uint32_t)out << u;
+        off[u] = ((unsigned long long)(out ? 0u : (uint32_t)id[u]) * stride + (block - page_of(a, block) * per_page)) *
+                 (16 * T::kRowBytes);
+      }
+    };
+    // this thread's chunk of pass i: where it comes from, and whether it is there
+    auto source = [&](uint32_t tile, int i, bool& there) {
+      const int u0 = i * T::kPass / 16;
+      unsigned long long from = off[u0];
+      uint32_t out = outside >> u0 & 1u;
+      if constexpr (T::kPass > 16) {
+        if (row >= 16) {
+          from = off[u0 + 1];
+          out = outside >> (u0 + 1) & 1u;
+        }
+      }
+      const int r = row + i * T::kPass;
+      there = !out && (int)(tile * T::kBlock) + r < end;
+      return from + (uint32_t)(r & 15) * T::kRowBytes + (uint32_t)chunk * 16;
+    };
+    look_up(lo);
+    if (segments > 0 && !wait(&sh.q_empty, (segments - 1) & 1)) return;
+    queries(b, h, row0);
+    if constexpr (T::kE4) {
+      uint4 kx[T::kCopies], vx[T::kCopies];
+      auto load = [&](uint32_t tile) {
+        find(tile);
+#pragma unroll
+        for (int i = 0; i < T::kCopies; ++i) {
+          bool there;
+          const unsigned long long from = source(tile, i, there);
+          kx[i] = vx[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (there) {
+            kx[i] = __ldg(reinterpret_cast<const uint4*>(keys + from));
+            vx[i] = __ldg(reinterpret_cast<const uint4*>(values + from));
+          }
+        }
+      };
+      load(lo);
+      if (lo + 1 < hi) look_up(lo + 1);
+      for (uint32_t tile = lo; tile < hi; ++tile, ++tiles) {
+        const int st = tiles % T::kStages;
+        if (tiles >= T::kStages && !wait(&sh.kv_empty[st], (tiles / T::kStages - 1) & 1)) return;
+        const bool masked = outside != 0 || (int)(tile + 1) * T::kBlock > plain;
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < T::kCopies; ++i) {
+          const int r = row + i * T::kPass;
+          if (masked && mixed) any |= clear_odd<C>(vx[i]);
+          uint4 x, y;
+          widen(kx[i], x, y);
+          *reinterpret_cast<uint4*>(sh.kv[st][0] + T::place(r, 2 * chunk, T::kBlock)) = x;
+          *reinterpret_cast<uint4*>(sh.kv[st][0] + T::place(r, 2 * chunk + 1, T::kBlock)) = y;
+          widen(vx[i], x, y);
+          *reinterpret_cast<uint4*>(sh.kv[st][1] + T::place(r, 2 * chunk, T::kBlock)) = x;
+          *reinterpret_cast<uint4*>(sh.kv[st][1] + T::place(r, 2 * chunk + 1, T::kBlock)) = y;
+        }
+        landed(st, outside, any);
+        if (tile + 1 < hi) {
+          load(tile + 1);
+          if (tile + 2 < hi) look_up(tile + 2);
+        }
+      }
+    } else {
+      // up to kStages tiles on their way: the oldest is waited for when no place is free
+      uint32_t tile = lo, oldest = lo;
+      uint32_t outsides[T::kStages];
+      while (oldest < hi) {
+        const int st = tiles % T::kStages;
+        const bool want = tile < hi;
+        bool place_free = want && (tiles < T::kStages ||
+                                   __all_sync(0xffffffffu, mbar_test_wait(&sh.kv_empty[st], (tiles / T::kStages - 1) & 1)));
+        if (want && !place_free && tile == oldest) {             // nothing on its way
+          if (!wait(&sh.kv_empty[st], (tiles / T::kStages - 1) & 1)) return;
+          place_free = true;
+        }
+        if (place_free) {
+          find(tile);
+          const uint32_t ks = smem_u32(sh.kv[st][0]), vs = smem_u32(sh.kv[st][1]);
+#pragma unroll
+          for (int i = 0; i < T::kCopies; ++i) {
+            bool there;
+            const unsigned long long from = source(tile, i, there);
+            const uint32_t to = T::place(row + i * T::kPass, chunk, T::kBlock);
+            copy16(ks + to, keys + from, there);
+            copy16(vs + to, values + from, there);
+          }
+          asm volatile("cp.async.commit_group;" ::: "memory");
+          outsides[st] = outside;
+          if (tile + 1 < hi) look_up(tile + 1);
+          ++tile;
+          ++tiles;
+          if (tile < hi && tile - oldest < T::kStages) continue;
+        }
+        if (tile - oldest > 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+        const int at = (tiles - (tile - oldest)) % T::kStages;
+        uint32_t any = 0;
+        if (mixed && (outsides[at] != 0 || (int)(oldest + 1) * T::kBlock > plain)) {
+#pragma unroll 1
+          for (int i = 0; i < T::kCopies; ++i) {
+            uint4* p = reinterpret_cast<uint4*>(sh.kv[at][1] + T::place(row + i * T::kPass, chunk, T::kBlock));
+            uint4 x = *p;
+            const uint32_t here = clear_odd<C>(x);
+            if (here != 0) *p = x;
+            any |= here;
+          }
+        }
+        landed(at, outsides[at], any);
+        ++oldest;
+      }
+    }
+    ++segments;
+  }
+  // A tile is in its place: seen by the tensor cores after the fence, by all with the arrival.
+  __device__ __forceinline__ void landed(int st, uint32_t outside, uint32_t any) {
+    if (any != 0) sh.odd[segments & 3] = 1;
+    if (tid == 0) sh.outside[st] = outside;
+    fence_async();
+    __syncwarp();
+    if ((tid & 31) == 0) arrive(&sh.kv_full[st]);
+  }
+};
+
+// The products, by warp 8: S of a tile before O of the one in front of it.
+template <class C, int D> struct Issuer {
+  using T = Tree<C, D>;
+  using S = typename T::Shared;
+  const PagedArgs& a;
+  S& sh;
+  uint32_t tmem;
+  uint32_t formed = 0, added = 0;    // tiles of S, of O
+  bool go = true;
+
+  __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
+    if (!__all_sync(0xffffffffu, mbar_wait(bar, parity, &sh.abort, a.wait_ns))) {
+      *static_cast<volatile int*>(&sh.abort) = 1;
+      go = false;
+    }
+    return go;
+  }
+  __device__ __forceinline__ void form(bool first, bool last) {
+    const int st = formed % T::kStages, buf = formed & 1;
+    if (!wait(&sh.kv_full[st], formed / T::kStages & 1)) return;
+    // the place of S held P of two tiles before; at a segment's start the products of the
+    // last tile too have been issued, and the barrier's parity tells only of the last
+    if (first ? formed >= 1 && !wait(&sh.o_done, (formed - 1) & 1) : formed >= 2 && !wait(&sh.o_done, formed & 1)) return;
+    tc_fence_after();
+    if (elect_one()) {
+      const uint64_t q = sw128_desc(smem_u32(sh.q)), k = sw128_desc(smem_u32(sh.kv[st][0]));
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+        umma_bf16(tmem + T::kColS + buf * 64, q + (uint64_t)(((i >> 2) * T::kRows * 128 >> 4) + 2 * (i & 3)),
+                  k + (uint64_t)(((i >> 2) * T::kBlock * 128 >> 4) + 2 * (i & 3)), T::kIdescS, i > 0);
+      umma_commit(&sh.s_full[buf]);
+      if (last) umma_commit(&sh.q_empty);
+    }
+    __syncwarp();
+    ++formed;
+  }
+  __device__ __forceinline__ void add(bool first) {
+    const int st = added % T::kStages, buf = added & 1;
+    if (!wait(&sh.p_full[buf], added / 2 & 1)) return;
+    tc_fence_after();
+    if (elect_one()) {
+      // 64 dims of V, 16 entries a step: 1 KB from 8 entries to the next, a block of dims
+      // behind the other
+      const uint64_t v = sw128_desc(smem_u32(sh.kv[st][1])) + ((uint64_t)((T::kBlock * 128 >> 4) - 1) << 16);
+      const uint32_t p = tmem + T::kColS + buf * 64;
+#pragma unroll
+      for (int part = 0; part < (T::kE4 ? 1 : 2); ++part)        // p's upper and lower bits
+#pragma unroll
+        for (int i = 0; i < T::kBlock / 16; ++i)
+          umma_ts(tmem, p + part * 32 + i * 8, v + (uint64_t)(i * (16 * 128 >> 4)), T::kIdescO,
+                  !first || part > 0 || i > 0);
+      umma_commit(&sh.kv_empty[st]);
+      umma_commit(&sh.o_done);
+    }
+    __syncwarp();
+    ++added;
+  }
+  __device__ __forceinline__ void segment(uint32_t lo, uint32_t hi) {
+    if (go) form(true, lo + 1 == hi);
+    for (uint32_t tile = lo; go && tile < hi; ++tile) {
+      if (tile + 1 < hi) form(false, tile + 2 == hi);
+      if (go) add(tile == lo);
+    }
+  }
+};
+
+// Scores to p, and the rows' results: warps 0 to 3, a row a thread.
+template <class C, int D> struct Softmax {
+  using T = Tree<C, D>;
+  using S = typename T::Shared;
+  const PagedArgs& a;
+  S& sh;
+  uint32_t tmem;                     // with the warp's first lane
+  uint32_t tiles = 0, segments = 0;
+  bool go = true;
+
+  __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
+    if (!__all_sync(0xffffffffu, mbar_wait(bar, parity, &sh.abort, a.wait_ns))) {
+      *static_cast<volatile int*>(&sh.abort) = 1;
+      go = false;
+    }
+    return go;
+  }
+  __device__ __forceinline__ void segment(int b, int h, int row0, uint32_t lo, uint32_t hi, bool whole, float* slot) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = threadIdx.x;
+    const int rows = a.nodes * a.group, row = row0 + r;
+    const int n = length_of(a, b);
+    const int end = min(n, (int)(hi * T::kBlock)), plain = min(end, plain_end(a, n));
+    const uint32_t* tree = tree_of(a, b);
+    const bool works = row0 + 32 * warp < rows;                  // else its rows are none
+    const int node = min(row, rows - 1) / a.group;
+    float f = a.scale * kLog2e * (T::kE4 && a.k_scale != nullptr ? a.k_scale[h] : 1.0f);
+    float m = -INFINITY, l = 0.0f;
+    for (uint32_t tile = lo; go && tile < hi; ++tile, ++tiles) {
+      const int buf = tiles & 1;
+      if (!wait(&sh.s_full[buf], tiles / 2 & 1)) break;
+      tc_fence_after();
+      if (works) {
+        if (T::kE4 && tile == lo) f *= sh.power[segments & 3][r];
+        const uint32_t at = tmem + T::kColS + buf * 64;
+        float s[64];
+        {
+          float (&x)[32] = *reinterpret_cast<float (*)[32]>(&s[0]);
+          float (&y)[32] = *reinterpret_cast<float (*)[32]>(&s[32]);
+          tmem_ld32(at, x);
+          tmem_ld32(at + 32, y);
+        }
+#pragma unroll
+        for (int i = 0; i < 64; ++i) s[i] *= f;
+        const uint32_t outside = *static_cast<volatile uint32_t*>(&sh.outside[tiles % T::kStages]);
+        const int first = (int)tile * T::kBlock;
+        if (outside != 0 || first + T::kBlock > plain) {
+          uint32_t bits[2];
+          seen_bits(a, tree, n, node, first, end, bits);
+#pragma unroll
+          for (int i = 0; i < 64; ++i) {
+            s[i] = bits[i / 32] >> (i & 31) & 1u ? s[i] : -INFINITY;
+            if (outside >> (i / 16) & 1u && s[i] > -INFINITY) s[i] = NAN;
+          }
+        }
+        __syncwarp();
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 64; ++i) top = fmaxf(top, s[i]);
+        const bool grows = top > m + kSlack || (m == -INFINITY && top > -INFINITY);
+        const float c = grows ? exp2_(m - top) : 1.0f;
+        if (grows) m = top;
+        l *= c;
+        if (tile > lo && __any_sync(0xffffffffu, grows)) {       // O of the tiles before, rescaled
+          if (!wait(&sh.o_done, (tiles - 1) & 1)) break;
+          tc_fence_after();
+#pragma unroll 1
+          for (int d = 0; d < D; d += 8) {
+            float x[8];
+            tmem_ld8(tmem + d, x);
+            uint32_t y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = __float_as_uint(x[i] * c);
+            tmem_st8(tmem + d, y);
+          }
+        }
+        const float below = m == -INFINITY ? 0.0f : m - T::kLift;
+#pragma unroll
+        for (int i = 0; i < 64; i += 16) {
+          uint32_t hi_[8], lo_[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float p0 = exp2_(s[i + 2 * j] - below), p1 = exp2_(s[i + 2 * j + 1] - below);
+            l += p0 + p1;
+            if constexpr (T::kE4) {
+              hi_[j] = bits_of(__floats2half2_rn(p0, p1));
+            } else {
+              const __nv_bfloat162 two = __floats2bfloat162_rn(p0, p1);
+              const float2 back = __bfloat1622float2(two);
+              hi_[j] = bits_of(two);
+              lo_[j] = bits_of(__floats2bfloat162_rn(p0 - back.x, p1 - back.y));
+            }
+          }
+          tmem_st8(at + i / 2, hi_);
+          if constexpr (!T::kE4) tmem_st8(at + 32 + i / 2, lo_);
+        }
+        tmem_st_wait();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive(&sh.p_full[buf]);
+    }
+    if (go) wait(&sh.o_done, (tiles - 1) & 1);
+    tc_fence_after();
+    const bool there = row < rows, poison = !go || too_long(a, b);
+    const bool odd = *static_cast<volatile int*>(&sh.odd[segments & 3]) != 0;
+    const float v_scale = T::kE4 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
+    const int head = h * a.group + row - node * a.group;
+    const float sum = poison ? NAN : l;
+    if (works) {
+#pragma unroll 1
+      for (int d = 0; d < D; d += 32) {
+        float x[32];
+        if (go) tmem_ld32(tmem + d, x);
+        if (there) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            float4 y = go ? make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]) : make_float4(NAN, NAN, NAN, NAN);
+            if (odd) y = odd_values<C, D>(a, b, h, node, n, (int)(lo * T::kBlock), (int)(hi * T::kBlock), d + i, y);
+            if (whole) {
+              write_row<__nv_bfloat16>(a, (long long)b * a.nodes + node, head, d + i, D, y, m, sum, v_scale, T::kLift);
+            } else {
+              *reinterpret_cast<float4*>(slot + r * D + d + i) = y;
+              if (d + i == 0) {
+                slot[T::kRows * D + 2 * r] = m;
+                slot[T::kRows * D + 2 * r + 1] = sum;
+              }
+            }
+          }
+        }
+        __syncwarp();
+      }
+    }
+    tc_fence_before();
+    asm volatile("bar.sync 1, 128;" ::: "memory");               // all four warps have read the segment's word
+    if (threadIdx.x == 0) *static_cast<volatile int*>(&sh.odd[segments & 3]) = 0;
+    ++segments;
+  }
+};
+
+template <class C, int D>
+__global__ void __launch_bounds__(kTreeThreads, 2) paged_tree_kernel(const __grid_constant__ PagedArgs a) {
+  using T = Tree<C, D>;
+  using S = typename T::Shared;
+  extern __shared__ uint8_t tree_raw[];
+  uint8_t* base = tree_raw + ((1024u - (smem_u32(tree_raw) & 1023u)) & 1023u);
+  S& sh = *reinterpret_cast<S*>(base);
+  uint32_t* before = reinterpret_cast<uint32_t*>(base + sizeof(S));
+  const int warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < T::kStages; ++i) {
+      mbar_init(&sh.kv_full[i], 4);
+      mbar_init(&sh.kv_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.s_full[i], 1);
+      mbar_init(&sh.p_full[i], 4);
+    }
+    mbar_init(&sh.q_empty, 1);
+    mbar_init(&sh.o_done, 1);
+    mbar_init(&sh.drain, 1);
+    for (int i = 0; i < 4; ++i) sh.odd[i] = 0;
+    sh.abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 8) {
+    tmem_alloc(&sh.tmem, kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem;
+  pdl_wait();
+  pdl_trigger();                     // the joining kernel makes the same plan meanwhile
+  const Plan plan = make_plan<T>(a, before, sh.scratch, (int)gridDim.x);
+  if (warp < 4) {
+    Softmax<C, D> w{a, sh, tmem + ((uint32_t)(32 * warp) << 16)};
+    each_segment<T>(a, plan, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool whole, float* slot) {
+      w.segment(b, h, row0, lo, hi, whole, slot);
+    });
+  } else if (warp < 8) {
+    Copier<C, D> w{a, sh, (int)threadIdx.x - 128};
+    each_segment<T>(a, plan, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool, float*) {
+      w.segment(b, h, row0, lo, hi);
+    });
+    if constexpr (!T::kE4) asm volatile("cp.async.wait_all;" ::: "memory");
+  } else {
+    Issuer<C, D> w{a, sh, tmem};
+    each_segment<T>(a, plan, before, [&](int, int, int, uint32_t lo, uint32_t hi, bool, float*) { w.segment(lo, hi); });
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const bool gave_up = *static_cast<volatile int*>(&sh.abort) != 0;
+  if (gave_up && warp == 8) {        // the products issued end before tensor memory goes
+    if (elect_one()) umma_commit(&sh.drain);
+    __syncwarp();
+    mbar_wait(&sh.drain, 0, nullptr, kDefaultWaitLimitNs);
+  }
+  if (threadIdx.x == 0 && blockIdx.x < plan.runs) a.gave_up[blockIdx.x] = gave_up;
+  __syncwarp();
+  if (warp == 8) tmem_dealloc(tmem, kTmemCols);
+}
+
+template <class C, int D> cudaError_t launch_as(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
+  using T = Tree<C, D>;
+  static std::atomic<unsigned long long> raised{0};
+  return launch_runs<T, C, __nv_bfloat16, D>(a, paged_tree_kernel<C, D>, kTreeThreads, 1024 + sizeof(typename T::Shared),
+                                             152 * 2, s, workspace, raised);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_tree(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
+  if (a.cache_dtype == FOVEA_BF16)
+    return a.dim == 64 ? launch_as<__nv_bfloat16, 64>(a, s, workspace) : launch_as<__nv_bfloat16, 128>(a, s, workspace);
+  return a.dim == 64 ? launch_as<__nv_fp8_e4m3, 64>(a, s, workspace) : launch_as<__nv_fp8_e4m3, 128>(a, s, workspace);
+}
+
+}  // namespace fovea

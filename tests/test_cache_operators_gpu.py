@@ -846,3 +846,31 @@ def test_refusals_of_the_binding(fovea):
         fovea.cache_fork(k, v, table, lens, ints([0]), width=0)
     with pytest.raises(ValueError):
         fovea.rotary_frequencies(16, [3, 4])
+
+
+def test_a_wait_that_gives_up(fovea):
+    """Trees through the tensor cores with waits that give up: NaN, an error for the
+    workspace, and the next call on it as ever."""
+    g = gen(16)
+    for cache in (BF16, E4M3):
+        lens = [900, 400]
+        k, v, table, scales = make_cache(g, cache, lens, 4, 128, 64)
+        q = normal(g, 2 * 64, 8, 128).to(BF16)
+        ws = torch.full((fovea.paged_attention_workspace_size(2, 64, 8, 4, 128, cache),), 255, dtype=torch.uint8,
+                        device="cuda")
+        args = (q, k, v, table, ints(lens))
+        want = fovea.paged_attention(*args, workspace=ws, want_lse=True, **scales)
+        fovea.sync_errors(ws)
+        fovea.debug_wait_limit(1)
+        try:
+            got = fovea.paged_attention(*args, workspace=ws, want_lse=True, **scales)
+            torch.cuda.synchronize()
+        finally:
+            fovea.debug_wait_limit(0)
+        assert torch.isnan(got["out"]).any() and torch.isnan(got["lse"]).any()
+        again = fovea.paged_attention(*args, workspace=ws, want_lse=True, **scales)
+        with pytest.raises(fovea.FoveaError) as e:
+            fovea.sync_errors(ws)
+        assert e.value.status == fovea.ERR_TIMEOUT
+        fovea.sync_errors(ws)
+        assert same(again["out"], want["out"]) and same(again["lse"], want["lse"])
