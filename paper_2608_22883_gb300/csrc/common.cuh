@@ -518,6 +518,7 @@ struct PagedArgs {
   void* workspace;
   // set by the launch
   int row_blocks;                                  // of a key head
+  int room;                                        // entries of a table
   int* header; float* slots; int* gave_up;         // the workspace: partial sums, and a word a run
   unsigned long long wait_ns;
   bool q_words, q_chunks;                          // pairs of 16-bit elements of q, 16 bytes of them, are aligned

@@ -576,8 +576,9 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_attention_
   pdl_wait();
   pdl_trigger();                     // the joining kernel makes the same plan meanwhile
   const Plan plan = make_plan<A>(a, before, scratch, (int)gridDim.x);
+  const Run run = make_run(a, plan, before);
   A at;
-  each_segment<A>(a, plan, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool whole, float* slot) {
+  each_segment<A>(a, run, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool whole, float* slot) {
     A::stage_rows(a, sh, b, h, row0);
     __syncthreads();
     const int n = length_of(a, b);

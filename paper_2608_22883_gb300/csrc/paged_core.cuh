@@ -44,21 +44,31 @@ __device__ __forceinline__ uint32_t halves_of_e4m3(uint32_t two) {   // the low 
 __device__ __forceinline__ uint32_t bits_of(__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); }
 __device__ __forceinline__ uint32_t bits_of(__nv_bfloat162 x) { return *reinterpret_cast<const uint32_t*>(&x); }
 
+// The kernels' code is fetched by every SM when it is first run, which small calls wait
+// for; divisions of 64 bits, a kilobyte each, stay out of line or are replaced here.
+__device__ __noinline__ uint64_t divide_long(uint64_t x, uint32_t d) { return x / d; }
+
 struct Plan {
   uint64_t total;      // blocks
   uint32_t runs;       // that have any
-  __device__ __forceinline__ uint64_t start(uint32_t run) const { return total * run / runs; }
-  __device__ __forceinline__ uint32_t run_of(uint64_t block) const {     // start(run) <= block < start(run + 1)
-    return (uint32_t)(((block + 1) * runs + total - 1) / total - 1);
+  uint64_t each;       // total / runs
+  uint32_t rest;       // total % runs
+  float runs_a_block;
+  __device__ __forceinline__ uint64_t start(uint32_t run) const { return each * run + rest * run / runs; }   // total run / runs
+  // The run of a block: start(run) <= block < start(run + 1).  The estimate is off by one at
+  // most (runs < 2^16).
+  __device__ __forceinline__ uint32_t run_of(uint64_t block) const {
+    uint32_t run = min((uint32_t)((float)block * runs_a_block), runs - 1);
+#pragma unroll 1
+    while (start(run) > block) --run;
+#pragma unroll 1
+    while (start(run + 1) <= block) ++run;
+    return run;
   }
 };
 
-__device__ __forceinline__ int length_of(const PagedArgs& a, int b) {
-  const int n = a.lens[b];
-  const long long most = (long long)a.width * a.page;
-  return n < 0 ? 0 : n > most ? (int)most : n;
-}
-__device__ __forceinline__ bool too_long(const PagedArgs& a, int b) { return a.lens[b] > (long long)a.width * a.page; }
+__device__ __forceinline__ int length_of(const PagedArgs& a, int b) { return max(0, min(a.lens[b], a.room)); }
+__device__ __forceinline__ bool too_long(const PagedArgs& a, int b) { return a.lens[b] > a.room; }
 
 // K, of a kernel: kWaits: its waits may give up; kBlock entries a block; kLeast blocks of a run, at least; kFront: the
 // staging of a segment's rows and the end of its sums take a CTA as long as some blocks,
@@ -68,10 +78,12 @@ template <class K> __device__ __forceinline__ uint32_t blocks_of(int len) {
 }
 // Sums of the sequences' blocks before each (before[0 .. B], in shared memory) and the
 // cut into runs.  All threads of the CTA.
-template <class K> __device__ Plan make_plan(const PagedArgs& a, uint32_t* before, uint32_t* scratch, int max_runs) {
+template <class K> __device__ __forceinline__ Plan make_plan(const PagedArgs& a, uint32_t* before, uint32_t* scratch,
+                                                             int max_runs) {
   const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5;
   const int per = (a.B + nt - 1) / nt, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
   uint32_t mine = 0;
+#pragma unroll 1
   for (int b = b0; b < b1; ++b) mine += blocks_of<K>(length_of(a, b));
   uint32_t sum = mine;
 #pragma unroll
@@ -82,7 +94,9 @@ template <class K> __device__ Plan make_plan(const PagedArgs& a, uint32_t* befor
   if (lane == 31) scratch[warp] = sum;
   __syncthreads();
   uint32_t base = sum - mine;
+#pragma unroll 1
   for (int w = 0; w < warp; ++w) base += scratch[w];
+#pragma unroll 1
   for (int b = b0; b < b1; ++b) {
     before[b] = base;
     base += blocks_of<K>(length_of(a, b));
@@ -91,40 +105,71 @@ template <class K> __device__ Plan make_plan(const PagedArgs& a, uint32_t* befor
   __syncthreads();
   Plan p;
   p.total = (uint64_t)before[a.B] * (uint32_t)(a.kv_heads * a.row_blocks);
-  const uint64_t most = (p.total + K::kLeast - 1) / K::kLeast;
-  p.runs = most < (uint64_t)max_runs ? (uint32_t)most : (uint32_t)max_runs;
+  const uint64_t most = p.total < (uint64_t)max_runs * K::kLeast ? ((uint32_t)p.total + K::kLeast - 1) / K::kLeast : max_runs;
+  p.runs = (uint32_t)most;
+  const uint32_t d = max(p.runs, 1u);
+  p.each = p.total >> 32 == 0 ? (uint32_t)p.total / d : divide_long(p.total, d);
+  p.rest = (uint32_t)(p.total - p.each * d);
+  p.runs_a_block = (float)p.runs / (float)max(p.total, (uint64_t)1);
   return p;
 }
 
+// Where a CTA's run begins, found once; each_segment goes on from there.
+struct Run {
+  uint64_t from, to;
+  int b;               // sequence
+  uint32_t seg, first; // its segment, the block within it
+};
+__device__ __forceinline__ Run make_run(const PagedArgs& a, const Plan& plan, const uint32_t* before) {
+  Run r{};
+  if (blockIdx.x >= plan.runs) return r;
+  r.from = plan.start(blockIdx.x);
+  r.to = plan.start(blockIdx.x + 1);
+  const uint32_t segments = a.kv_heads * a.row_blocks;    // of a sequence, < 2^16
+  int hi = a.B - 1;                  // the last b with before[b] * segments <= from
+#pragma unroll 1
+  while (r.b < hi) {
+    const int mid = (r.b + hi + 1) >> 1;
+    if ((uint64_t)before[mid] * segments <= r.from) r.b = mid; else hi = mid - 1;
+  }
+  const uint32_t count = before[r.b + 1] - before[r.b];   // not 0: `from` lies in it
+  const uint64_t within = r.from - (uint64_t)before[r.b] * segments;
+  r.seg = min((uint32_t)((float)within / (float)count), segments - 1);   // off by one at most
+#pragma unroll 1
+  while ((uint64_t)r.seg * count > within) --r.seg;
+#pragma unroll 1
+  while ((uint64_t)(r.seg + 1) * count <= within) ++r.seg;
+  r.first = (uint32_t)(within - (uint64_t)r.seg * count);
+  return r;
+}
 // The segments of a CTA's run: body(sequence, key head, first row, first block, end, whether
 // the segment is whole, its partial slot).
 template <class K, class F>
-__device__ __forceinline__ void each_segment(const PagedArgs& a, const Plan& plan, const uint32_t* before, F body) {
-  if (blockIdx.x >= plan.runs) return;
-  const uint64_t from = plan.start(blockIdx.x), to = plan.start(blockIdx.x + 1);
-  const uint32_t segments = a.kv_heads * a.row_blocks;    // of a sequence
+__device__ __forceinline__ void each_segment(const PagedArgs& a, const Run& run, const uint32_t* before, F body) {
   float* slots = a.slots + (size_t)blockIdx.x * 2 * K::kSlot;
-  int b = 0;
-  {
-    int hi = a.B - 1;                // the last b with before[b] * segments <= from
-    while (b < hi) {
-      const int mid = (b + hi + 1) >> 1;
-      if ((uint64_t)before[mid] * segments <= from) b = mid; else hi = mid - 1;
-    }
-  }
-  for (uint64_t u = from; u < to;) {
-    while ((uint64_t)before[b + 1] * segments <= u) ++b;
+  const uint32_t segments = a.kv_heads * a.row_blocks;
+  int b = run.b;
+  uint32_t seg = run.seg, first = run.first;
+#pragma unroll 1
+  for (uint64_t u = run.from; u < run.to;) {
     const uint32_t count = before[b + 1] - before[b];
-    const uint64_t within = u - (uint64_t)before[b] * segments;
-    const uint32_t seg = (uint32_t)(within / count), first = (uint32_t)(within % count);
-    const uint32_t end = (uint32_t)min((uint64_t)count, first + (to - u));
+    if (seg == segments || count == 0) {                  // the next sequence
+      ++b;
+      seg = 0;
+      continue;
+    }
+    const uint32_t end = (uint32_t)min((uint64_t)count, first + (run.to - u));
     // a segment that begins before or with this run goes to its first slot, a later one to its second
-    const bool begun = u - first <= from;
+    const bool begun = u - first <= run.from;
     u += end - first;
-    if (end <= K::kFront) continue;
-    const uint32_t lo = max(first, K::kFront) - K::kFront, hi = end - K::kFront;
-    body(b, (int)(seg / a.row_blocks), (int)(seg % a.row_blocks) * K::kRows, lo, hi,
-         lo == 0 && hi == count - K::kFront, slots + (begun ? 0 : K::kSlot));
+    if (end > K::kFront) {
+      const uint32_t lo = max(first, K::kFront) - K::kFront, hi = end - K::kFront;
+      const int h = (int)(seg / (uint32_t)a.row_blocks);
+      body(b, h, (int)(seg - h * a.row_blocks) * K::kRows, lo, hi, lo == 0 && hi == count - K::kFront,
+           slots + (begun ? 0 : K::kSlot));
+    }
+    first = 0;
+    ++seg;
   }
 }
 
@@ -204,7 +249,7 @@ template <class C> __device__ __forceinline__ uint32_t odd_in(uint32_t x) {
 template <class T>
 __device__ __forceinline__ void write_row(const PagedArgs& a, long long n, int head, int d, int dim, float4 x, float top,
                                           float sum, float v_scale, float lift) {
-  const float k = sum == 0.0f ? 0.0f : v_scale / sum;      // nothing seen: 0 (an infinite value stays NaN)
+  const float k = sum == 0.0f ? 0.0f : v_scale * __frcp_rn(sum);   // nothing seen: 0 (an infinite value stays NaN)
   T* out = static_cast<T*>(a.out) + (n * a.heads + head) * dim + d;
   if constexpr (sizeof(T) == 4) {
     *reinterpret_cast<float4*>(out) = make_float4(x.x * k, x.y * k, x.z * k, x.w * k);
@@ -245,50 +290,81 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
     if (lane == 0) ensure_header(a.header);
     if constexpr (K::kWaits) {
       bool any = false;
+#pragma unroll 1
       for (uint32_t run = lane; run < plan.runs; run += 32) any |= __ldcg(a.gave_up + run) != 0;
       if (__any_sync(0xffffffffu, any) && lane == 0) atomicOr(a.header, kErrTimeout);
     }
   }
-  const long long rows = (long long)a.B * a.nodes * a.heads;
-  for (long long i = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * kWarps) {
-    const long long n = i / a.heads;
-    const int head = (int)(i - n * a.heads), b = (int)(n / a.nodes), node = (int)(n - (long long)b * a.nodes);
+  const uint32_t rows = (uint32_t)a.B * a.nodes * a.heads;       // < 2^30
+#pragma unroll 1
+  for (uint32_t i = blockIdx.x * kWarps + (threadIdx.x >> 5); i < rows; i += gridDim.x * kWarps) {
+    const uint32_t n = i / a.heads;
+    const int head = (int)(i - n * a.heads), b = (int)(n / a.nodes), node = (int)(n - b * a.nodes);
     const int h = head / a.group, row = node * a.group + head - h * a.group;
     const uint32_t segments = a.kv_heads * a.row_blocks, count = before[b + 1] - before[b];
     const float v_scale = sizeof(C) == 1 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
-    if (count == 0) {
-      for (int d = 4 * lane; d < D; d += 128)
-        write_row<Q>(a, n, head, d, D, make_float4(0.0f, 0.0f, 0.0f, 0.0f), -INFINITY, 0.0f, 1.0f, 0.0f);
-      continue;
-    }
-    const uint64_t s0 = (uint64_t)before[b] * segments + (uint64_t)(h * a.row_blocks + row / K::kRows) * count;
-    const uint32_t first = plan.run_of(s0 + K::kFront), last = plan.run_of(s0 + count - 1);
-    if (first == last) continue;     // written already
-    const float* base = a.slots;
-    const int r = row % K::kRows;
-    const bool second = plan.start(first) < s0;            // the first run's second slot
-    auto slot = [&](uint32_t run) { return base + ((size_t)run * 2 + (run == first && second)) * K::kSlot; };
-    float top = -INFINITY;
-    for (uint32_t run = first + lane; run <= last; run += 32) top = fmaxf(top, __ldcg(slot(run) + K::kRows * D + 2 * r));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    float sum = 0.0f;
-    constexpr int kVecs = (D + 127) / 128;
+    constexpr int kVecs = (D + 127) / 128, kAhead = 4;
+    float top = -INFINITY, sum = 0.0f;
     float4 x[kVecs];
 #pragma unroll
     for (int c = 0; c < kVecs; ++c) x[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-    for (uint32_t run = first; run <= last; ++run) {
-      const float* p = slot(run);
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + K::kRows * D + 2 * r));
-      const float c = ml.x == top ? 1.0f : exp2_(ml.x - top);
-      sum += c * ml.y;
+    if (count != 0) {
+      const uint64_t s0 = (uint64_t)before[b] * segments + (uint64_t)(h * a.row_blocks + row / K::kRows) * count;
+      const uint32_t first = plan.run_of(s0 + K::kFront), last = plan.run_of(s0 + count - 1);
+      if (first == last) continue;   // written already
+      const bool second = plan.start(first) < s0;          // the first run's second slot
+      const float* slot = a.slots + (size_t)(2 * first + second) * K::kSlot;   // of `run`
+      const int r = row % K::kRows;
+      // maxima and sums a lane a run, 32 runs at a time, with the first runs' sums of p v on
+      // their way beside them
+#pragma unroll 1
+      for (uint32_t run0 = first; run0 <= last; run0 += 32) {
+        const int left = (int)min(32u, last - run0 + 1);
+        float2 ml = make_float2(-INFINITY, 0.0f);
+        float c = 0.0f;              // of this lane's run
+        if (lane < left)
+          ml = __ldcg(reinterpret_cast<const float2*>(a.slots + (size_t)(2 * (run0 + lane) + (run0 + lane == first && second)) * K::kSlot +
+                                                      K::kRows * D + 2 * r));
+#pragma unroll 1
+        for (int j0 = 0; j0 < left; j0 += kAhead) {
+          float4 y[kAhead][kVecs];
 #pragma unroll
-      for (int v = 0; v < kVecs; ++v) {
-        const int d = 128 * v + 4 * lane;
-        if (d < D) {
-          const float4 y = __ldcg(reinterpret_cast<const float4*>(p + r * D + d));
-          x[v].x += c * y.x; x[v].y += c * y.y; x[v].z += c * y.z; x[v].w += c * y.w;
+          for (int j = 0; j < kAhead; ++j) {
+#pragma unroll
+            for (int v = 0; v < kVecs; ++v) {
+              const int d = 128 * v + 4 * lane;
+              y[j][v] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+              if (j0 + j < left && d < D) y[j][v] = __ldcg(reinterpret_cast<const float4*>(slot + r * D + d));
+            }
+            slot += run0 + j0 + j == first && second ? K::kSlot : 2 * K::kSlot;
+          }
+          if (j0 == 0) {
+            float high = ml.x;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+            high = fmaxf(high, top);
+            const float keep = top == high ? 1.0f : exp2_(top - high);
+            top = high;
+            c = ml.x == top ? 1.0f : exp2_(ml.x - top);
+            float mine = lane < left ? c * ml.y : 0.0f;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+            sum = sum * keep + mine;
+#pragma unroll
+            for (int v = 0; v < kVecs; ++v) {
+              x[v].x *= keep; x[v].y *= keep; x[v].z *= keep; x[v].w *= keep;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) {
+            const float cj = __shfl_sync(0xffffffffu, c, (j0 + j) & 31);
+            if (j0 + j < left) {
+#pragma unroll
+              for (int v = 0; v < kVecs; ++v) {
+                x[v].x += cj * y[j][v].x; x[v].y += cj * y[j][v].y; x[v].z += cj * y[j][v].z; x[v].w += cj * y[j][v].w;
+              }
+            }
+          }
         }
       }
     }
@@ -318,6 +394,7 @@ cudaError_t launch_runs(PagedArgs a, Kernel kernel, int threads, size_t shared, 
   a.page_magic = per_page <= 1 ? 0 : (uint32_t)((1ull << 32) / per_page + 1);
   a.q_words = (reinterpret_cast<uintptr_t>(a.q) & 3) == 0 && a.q_ld % 2 == 0 && a.q_hs % 2 == 0;
   a.q_chunks = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && a.q_ld % 8 == 0 && a.q_hs % 8 == 0;
+  a.room = a.width * a.page;
   a.row_blocks = (a.nodes * a.group + K::kRows - 1) / K::kRows;
   const size_t plan_bytes = ((size_t)a.B + 1) * 4;
   cudaError_t e = raise_smem_limit(kernel, 227 * 1024 - 1024, raised);

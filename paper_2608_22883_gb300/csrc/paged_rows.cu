@@ -238,8 +238,11 @@ template <class C, int D> struct Rows {
               for (int x = 0; x < 2; ++x) {
                 float& y = s[j][2 * e + x];
                 y = bits[j / 4] >> (8 * (j & 3) + x) & 1u ? y : -INFINITY;
-                if (outside >> (j / 2) & 1u && y > -INFINITY) y = NAN;
               }
+            // a row that sees an entry of a page outside the pool is NaN
+            const uint32_t out0 = (outside & 1u ? 0xFFFFu : 0u) | (outside & 2u ? 0xFFFF0000u : 0u);
+            const uint32_t out1 = (outside & 4u ? 0xFFFFu : 0u) | (outside & 8u ? 0xFFFF0000u : 0u);
+            if (((bits[0] << 2 * t & out0) | (bits[1] << 2 * t & out1)) != 0) l[e] = NAN;
           }
         }
         float c[2];
@@ -379,8 +382,9 @@ __global__ void __launch_bounds__(kThreads, rows_per_sm<C, D>) paged_rows_kernel
   pdl_wait();
   pdl_trigger();                     // the joining kernel makes the same plan meanwhile
   const Plan plan = make_plan<A>(a, before, scratch, (int)gridDim.x);
+  const Run run = make_run(a, plan, before);
   A at;
-  each_segment<A>(a, plan, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool whole, float* slot) {
+  each_segment<A>(a, run, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool whole, float* slot) {
     if (threadIdx.x == 0) sh.odd = 0;
     __syncthreads();
     const int n = length_of(a, b);

@@ -47,6 +47,14 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 __device__ __forceinline__ void arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+// mbar_wait of a converged warp (the same answer in every lane), its first try in line; a
+// wait that gives up tells the other roles.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* abort, uint64_t limit_ns) {
+  if (__all_sync(0xffffffffu, mbar_test_wait(bar, parity))) return true;
+  if (__all_sync(0xffffffffu, mbar_wait(bar, parity, abort, limit_ns))) return true;
+  *static_cast<volatile int*>(abort) = 1;
+  return false;
+}
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 template <class C, int D> struct Tree {
@@ -69,13 +77,14 @@ template <class C, int D> struct Tree {
 
   struct Shared {
     uint8_t q[kHalves * kRows * 128];
-    uint8_t kv[kStages][2][kTileBytes];
+    uint8_t k[kStages][kTileBytes], v[kStages][kTileBytes];
     // of the last segments begun, four at most before one is done: rows' powers (8 bits),
     // and whether a masked tile had odd values
     float power[4][kRows];
     int odd[4];
-    uint32_t outside[kStages];       // parts of a tile whose page is not in the pool, as bits
-    uint64_t kv_full[kStages], kv_empty[kStages], q_empty, s_full[2], p_full[2], o_done, drain;
+    uint32_t outside[4];             // of the last tiles: parts whose page is not in the pool, as bits
+    uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+    uint64_t q_empty, s_full[2], p_full[2], o_done, drain;
     uint32_t tmem;
     int abort;
     uint32_t scratch[kTreeThreads / 32];
@@ -106,15 +115,11 @@ template <class C, int D> struct Copier {
   const PagedArgs& a;
   S& sh;
   int tid;                           // 0 .. 127
-  uint32_t tiles = 0, segments = 0;  // begun
+  uint32_t keys_begun = 0, values_begun = 0, segments = 0;   // tiles, segments
   bool go = true;
 
   __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
-    if (!__all_sync(0xffffffffu, mbar_wait(bar, parity, &sh.abort, a.wait_ns))) {
-      *static_cast<volatile int*>(&sh.abort) = 1;
-      go = false;
-    }
-    return go;
+    return go = warp_wait(bar, parity, &sh.abort, a.wait_ns);
   }
   __device__ __forceinline__ void queries(int b, int h, int row0) {
     const int rows = a.nodes * a.group, r = tid, row = row0 + r;
@@ -127,8 +132,14 @@ template <class C, int D> struct Copier {
       power = row_power(top);
       sh.power[segments & 3][r] = power;
     }
+    if (!T::kE4 && a.q_chunks) {     // with the copies of the first keys
+      const uint32_t q = smem_u32(sh.q);
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) copy16(q + T::place(r, c, T::kRows), p + 8 * c, there);
+      return;
+    }
     const float k = 1.0f / power;
-#pragma unroll 4
+#pragma unroll 2
     for (int c = 0; c < D / 8; ++c) {
       uint4 x = make_uint4(0u, 0u, 0u, 0u);
       if (there) {
@@ -161,140 +172,180 @@ template <class C, int D> struct Copier {
     const uint8_t* values = static_cast<const uint8_t*>(a.v_pages) + (size_t)h * per_page * 16 * T::kRowBytes;
     const bool mixed = a.nodes > 1 || a.tree != nullptr;         // rows may differ in what they see
     const int chunk = tid % T::kChunks, row = tid / T::kChunks;
-    int id[T::kParts];
-    auto look_up = [&](uint32_t tile) {
+    // The pages' places of a tile, looked up a tile ahead for keys and for values.
+    struct Where {
+      int id[T::kParts];
+      unsigned long long off[T::kParts];
+      uint32_t outside;
+    } kw, vw;
+    auto look_up = [&](Where& w, uint32_t tile) {
 #pragma unroll
-      for (int u = 0; u < T::kParts; ++u) id[u] = table[page_of(a, min(tile * T::kParts + u, last_block))];
+      for (int u = 0; u < T::kParts; ++u) w.id[u] = table[page_of(a, min(tile * T::kParts + u, last_block))];
     };
-    unsigned long long off[T::kParts];
-    uint32_t outside = 0;
-    auto find = [&](uint32_t tile) {
-      outside = 0;
+    auto find = [&](Where& w, uint32_t tile) {
+      w.outside = 0;
 #pragma unroll
       for (int u = 0; u < T::kParts; ++u) {
         const uint32_t block = min(tile * T::kParts + u, last_block);
-        const bool out = (unsigned)id[u] >= (unsigned)a.n_pages;
-        outside |= (uint32_t)out << u;
-        off[u] = ((unsigned long long)(out ? 0u : (uint32_t)id[u]) * stride + (block - page_of(a, block) * per_page)) *
-                 (16 * T::kRowBytes);
+        const bool out = (unsigned)w.id[u] >= (unsigned)a.n_pages;
+        w.outside |= (uint32_t)out << u;
+        w.off[u] = ((unsigned long long)(out ? 0u : (uint32_t)w.id[u]) * stride + (block - page_of(a, block) * per_page)) *
+                   (16 * T::kRowBytes);
       }
     };
     // this thread's chunk of pass i: where it comes from, and whether it is there
-    auto source = [&](uint32_t tile, int i, bool& there) {
+    auto source = [&](const Where& w, uint32_t tile, int i, bool& there) {
       const int u0 = i * T::kPass / 16;
-      unsigned long long from = off[u0];
-      uint32_t out = outside >> u0 & 1u;
+      unsigned long long from = w.off[u0];
+      uint32_t out = w.outside >> u0 & 1u;
       if constexpr (T::kPass > 16) {
         if (row >= 16) {
-          from = off[u0 + 1];
-          out = outside >> (u0 + 1) & 1u;
+          from = w.off[u0 + 1];
+          out = w.outside >> (u0 + 1) & 1u;
         }
       }
       const int r = row + i * T::kPass;
       there = !out && (int)(tile * T::kBlock) + r < end;
       return from + (uint32_t)(r & 15) * T::kRowBytes + (uint32_t)chunk * 16;
     };
-    look_up(lo);
+    auto masked = [&](uint32_t outside, uint32_t tile) {
+      return mixed && (outside != 0 || (int)(tile + 1) * T::kBlock > plain);
+    };
+    look_up(kw, lo);
+    look_up(vw, lo);
     if (segments > 0 && !wait(&sh.q_empty, (segments - 1) & 1)) return;
     queries(b, h, row0);
+    // keys run a tile ahead of values: k0 k1 v0 k2 v1 ...
+    uint32_t kt = lo, vt = lo;       // next to come
+    auto keys_next = [&] { return kt < hi && kt < vt + 2; };
     if constexpr (T::kE4) {
-      uint4 kx[T::kCopies], vx[T::kCopies];
-      auto load = [&](uint32_t tile) {
-        find(tile);
+      uint4 kx[T::kCopies], vx[T::kCopies];                      // the next tile's, on their way
+      auto load = [&](Where& w, const uint8_t* from, uint32_t tile, uint4 (&x)[T::kCopies]) {
+        find(w, tile);
 #pragma unroll
         for (int i = 0; i < T::kCopies; ++i) {
           bool there;
-          const unsigned long long from = source(tile, i, there);
-          kx[i] = vx[i] = make_uint4(0u, 0u, 0u, 0u);
-          if (there) {
-            kx[i] = __ldg(reinterpret_cast<const uint4*>(keys + from));
-            vx[i] = __ldg(reinterpret_cast<const uint4*>(values + from));
-          }
+          const unsigned long long at = source(w, tile, i, there);
+          x[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (there) x[i] = __ldg(reinterpret_cast<const uint4*>(from + at));
         }
+        if (tile + 1 < hi) look_up(w, tile + 1);
       };
-      load(lo);
-      if (lo + 1 < hi) look_up(lo + 1);
-      for (uint32_t tile = lo; tile < hi; ++tile, ++tiles) {
-        const int st = tiles % T::kStages;
-        if (tiles >= T::kStages && !wait(&sh.kv_empty[st], (tiles / T::kStages - 1) & 1)) return;
-        const bool masked = outside != 0 || (int)(tile + 1) * T::kBlock > plain;
-        uint32_t any = 0;
+      auto put = [&](uint8_t* to, const uint4 (&x)[T::kCopies]) {
 #pragma unroll
         for (int i = 0; i < T::kCopies; ++i) {
           const int r = row + i * T::kPass;
-          if (masked && mixed) any |= clear_odd<C>(vx[i]);
-          uint4 x, y;
-          widen(kx[i], x, y);
-          *reinterpret_cast<uint4*>(sh.kv[st][0] + T::place(r, 2 * chunk, T::kBlock)) = x;
-          *reinterpret_cast<uint4*>(sh.kv[st][0] + T::place(r, 2 * chunk + 1, T::kBlock)) = y;
-          widen(vx[i], x, y);
-          *reinterpret_cast<uint4*>(sh.kv[st][1] + T::place(r, 2 * chunk, T::kBlock)) = x;
-          *reinterpret_cast<uint4*>(sh.kv[st][1] + T::place(r, 2 * chunk + 1, T::kBlock)) = y;
+          uint4 y, z;
+          widen(x[i], y, z);
+          *reinterpret_cast<uint4*>(to + T::place(r, 2 * chunk, T::kBlock)) = y;
+          *reinterpret_cast<uint4*>(to + T::place(r, 2 * chunk + 1, T::kBlock)) = z;
         }
-        landed(st, outside, any);
-        if (tile + 1 < hi) {
-          load(tile + 1);
-          if (tile + 2 < hi) look_up(tile + 2);
+      };
+      load(kw, keys, lo, kx);
+      load(vw, values, lo, vx);
+      while (vt < hi) {
+        if (keys_next()) {
+          const int st = keys_begun % T::kStages;
+          if (keys_begun >= T::kStages && !wait(&sh.k_empty[st], (keys_begun / T::kStages - 1) & 1)) return;
+          put(sh.k[st], kx);
+          keys_landed(keys_begun++, kw.outside);
+          if (++kt < hi) load(kw, keys, kt, kx);
+        } else {
+          const int st = values_begun % T::kStages;
+          if (values_begun >= T::kStages && !wait(&sh.v_empty[st], (values_begun / T::kStages - 1) & 1)) return;
+          uint32_t any = 0;
+          if (masked(vw.outside, vt)) {
+#pragma unroll
+            for (int i = 0; i < T::kCopies; ++i) any |= clear_odd<C>(vx[i]);
+          }
+          put(sh.v[st], vx);
+          values_landed(values_begun++, any);
+          if (++vt < hi) load(vw, values, vt, vx);
         }
       }
     } else {
-      // up to kStages tiles on their way: the oldest is waited for when no place is free
-      uint32_t tile = lo, oldest = lo;
-      uint32_t outsides[T::kStages];
-      while (oldest < hi) {
-        const int st = tiles % T::kStages;
-        const bool want = tile < hi;
-        bool place_free = want && (tiles < T::kStages ||
-                                   __all_sync(0xffffffffu, mbar_test_wait(&sh.kv_empty[st], (tiles / T::kStages - 1) & 1)));
-        if (want && !place_free && tile == oldest) {             // nothing on its way
-          if (!wait(&sh.kv_empty[st], (tiles / T::kStages - 1) & 1)) return;
-          place_free = true;
-        }
-        if (place_free) {
-          find(tile);
-          const uint32_t ks = smem_u32(sh.kv[st][0]), vs = smem_u32(sh.kv[st][1]);
+      // As many copies on their way as there are places; the oldest is waited for when the
+      // next has none.
+      uint32_t kd = lo, vd = lo;     // the oldest that have not landed
+      uint32_t k_outside = 0, v_outside = 0;                     // of the tiles on their way, 4 bits a place
+      auto begin = [&](Where& w, uint8_t* place, const uint8_t* from, uint32_t& tile, uint32_t& outside, uint32_t& begun) {
+        find(w, tile);
+        const uint32_t to = smem_u32(place);
 #pragma unroll
-          for (int i = 0; i < T::kCopies; ++i) {
-            bool there;
-            const unsigned long long from = source(tile, i, there);
-            const uint32_t to = T::place(row + i * T::kPass, chunk, T::kBlock);
-            copy16(ks + to, keys + from, there);
-            copy16(vs + to, values + from, there);
-          }
-          asm volatile("cp.async.commit_group;" ::: "memory");
-          outsides[st] = outside;
-          if (tile + 1 < hi) look_up(tile + 1);
-          ++tile;
-          ++tiles;
-          if (tile < hi && tile - oldest < T::kStages) continue;
+        for (int i = 0; i < T::kCopies; ++i) {
+          bool there;
+          const unsigned long long at = source(w, tile, i, there);
+          copy16(to + T::place(row + i * T::kPass, chunk, T::kBlock), from + at, there);
         }
-        if (tile - oldest > 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        const int bits = 4 * (begun % T::kStages);
+        outside = (outside & ~(15u << bits)) | w.outside << bits;
+        ++tile;
+        ++begun;
+        if (tile < hi) look_up(w, tile);
+      };
+      while (vd < hi) {
+        const bool any_left = vt < hi, is_key = keys_next();
+        bool is_free = false;
+        if (any_left) {
+          const uint32_t begun = is_key ? keys_begun : values_begun;
+          uint64_t* empty = &(is_key ? sh.k_empty : sh.v_empty)[begun % T::kStages];
+          const uint32_t parity = (begun / T::kStages - 1) & 1;
+          is_free = begun < T::kStages || __all_sync(0xffffffffu, mbar_test_wait(empty, parity));
+          if (!is_free && kd == kt && vd == vt) {                // nothing on its way
+            if (!wait(empty, parity)) return;
+            is_free = true;
+          }
+        }
+        if (is_free) {
+          if (is_key) begin(kw, sh.k[keys_begun % T::kStages], keys, kt, k_outside, keys_begun);
+          else begin(vw, sh.v[values_begun % T::kStages], values, vt, v_outside, values_begun);
+          continue;
+        }
+        // copies land in the order in which they were begun: keys first while as many values
+        // as two tiles before are in
+        const uint32_t on_way = (kt - kd) + (vt - vd);
+        if (on_way == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        else if (on_way == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else if (on_way == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
-        const int at = (tiles - (tile - oldest)) % T::kStages;
-        uint32_t any = 0;
-        if (mixed && (outsides[at] != 0 || (int)(oldest + 1) * T::kBlock > plain)) {
+        if (kd < kt && kd < vd + 2) {
+          const uint32_t tile = keys_begun - (kt - kd);
+          keys_landed(tile, k_outside >> 4 * (tile % T::kStages) & 15u);
+          ++kd;
+        } else {
+          const uint32_t tile = values_begun - (vt - vd);
+          const int st = tile % T::kStages;
+          uint32_t any = 0;
+          if (masked(v_outside >> 4 * st & 15u, vd)) {
 #pragma unroll 1
-          for (int i = 0; i < T::kCopies; ++i) {
-            uint4* p = reinterpret_cast<uint4*>(sh.kv[at][1] + T::place(row + i * T::kPass, chunk, T::kBlock));
-            uint4 x = *p;
-            const uint32_t here = clear_odd<C>(x);
-            if (here != 0) *p = x;
-            any |= here;
+            for (int i = 0; i < T::kCopies; ++i) {
+              uint4* p = reinterpret_cast<uint4*>(sh.v[st] + T::place(row + i * T::kPass, chunk, T::kBlock));
+              uint4 x = *p;
+              const uint32_t here = clear_odd<C>(x);
+              if (here != 0) *p = x;
+              any |= here;
+            }
           }
+          values_landed(tile, any);
+          ++vd;
         }
-        landed(at, outsides[at], any);
-        ++oldest;
       }
     }
     ++segments;
   }
   // A tile is in its place: seen by the tensor cores after the fence, by all with the arrival.
-  __device__ __forceinline__ void landed(int st, uint32_t outside, uint32_t any) {
-    if (any != 0) sh.odd[segments & 3] = 1;
-    if (tid == 0) sh.outside[st] = outside;
+  __device__ __forceinline__ void keys_landed(uint32_t tile, uint32_t outside) {
+    if (tid == 0) sh.outside[tile & 3] = outside;
     fence_async();
     __syncwarp();
-    if ((tid & 31) == 0) arrive(&sh.kv_full[st]);
+    if ((tid & 31) == 0) arrive(&sh.k_full[tile % T::kStages]);
+  }
+  __device__ __forceinline__ void values_landed(uint32_t tile, uint32_t any) {
+    if (any != 0) sh.odd[segments & 3] = 1;
+    fence_async();
+    __syncwarp();
+    if ((tid & 31) == 0) arrive(&sh.v_full[tile % T::kStages]);
   }
 };
 
@@ -309,26 +360,23 @@ template <class C, int D> struct Issuer {
   bool go = true;
 
   __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
-    if (!__all_sync(0xffffffffu, mbar_wait(bar, parity, &sh.abort, a.wait_ns))) {
-      *static_cast<volatile int*>(&sh.abort) = 1;
-      go = false;
-    }
-    return go;
+    return go = warp_wait(bar, parity, &sh.abort, a.wait_ns);
   }
   __device__ __forceinline__ void form(bool first, bool last) {
     const int st = formed % T::kStages, buf = formed & 1;
-    if (!wait(&sh.kv_full[st], formed / T::kStages & 1)) return;
+    if (!wait(&sh.k_full[st], formed / T::kStages & 1)) return;
     // the place of S held P of two tiles before; at a segment's start the products of the
     // last tile too have been issued, and the barrier's parity tells only of the last
     if (first ? formed >= 1 && !wait(&sh.o_done, (formed - 1) & 1) : formed >= 2 && !wait(&sh.o_done, formed & 1)) return;
     tc_fence_after();
     if (elect_one()) {
-      const uint64_t q = sw128_desc(smem_u32(sh.q)), k = sw128_desc(smem_u32(sh.kv[st][0]));
+      const uint64_t q = sw128_desc(smem_u32(sh.q)), k = sw128_desc(smem_u32(sh.k[st]));
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
         umma_bf16(tmem + T::kColS + buf * 64, q + (uint64_t)(((i >> 2) * T::kRows * 128 >> 4) + 2 * (i & 3)),
                   k + (uint64_t)(((i >> 2) * T::kBlock * 128 >> 4) + 2 * (i & 3)), T::kIdescS, i > 0);
       umma_commit(&sh.s_full[buf]);
+      umma_commit(&sh.k_empty[st]);
       if (last) umma_commit(&sh.q_empty);
     }
     __syncwarp();
@@ -336,12 +384,12 @@ template <class C, int D> struct Issuer {
   }
   __device__ __forceinline__ void add(bool first) {
     const int st = added % T::kStages, buf = added & 1;
-    if (!wait(&sh.p_full[buf], added / 2 & 1)) return;
+    if (!wait(&sh.v_full[st], added / T::kStages & 1) || !wait(&sh.p_full[buf], added / 2 & 1)) return;
     tc_fence_after();
     if (elect_one()) {
       // 64 dims of V, 16 entries a step: 1 KB from 8 entries to the next, a block of dims
       // behind the other
-      const uint64_t v = sw128_desc(smem_u32(sh.kv[st][1])) + ((uint64_t)((T::kBlock * 128 >> 4) - 1) << 16);
+      const uint64_t v = sw128_desc(smem_u32(sh.v[st])) + ((uint64_t)((T::kBlock * 128 >> 4) - 1) << 16);
       const uint32_t p = tmem + T::kColS + buf * 64;
 #pragma unroll
       for (int part = 0; part < (T::kE4 ? 1 : 2); ++part)        // p's upper and lower bits
@@ -349,7 +397,7 @@ template <class C, int D> struct Issuer {
         for (int i = 0; i < T::kBlock / 16; ++i)
           umma_ts(tmem, p + part * 32 + i * 8, v + (uint64_t)(i * (16 * 128 >> 4)), T::kIdescO,
                   !first || part > 0 || i > 0);
-      umma_commit(&sh.kv_empty[st]);
+      umma_commit(&sh.v_empty[st]);
       umma_commit(&sh.o_done);
     }
     __syncwarp();
@@ -375,11 +423,7 @@ template <class C, int D> struct Softmax {
   bool go = true;
 
   __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
-    if (!__all_sync(0xffffffffu, mbar_wait(bar, parity, &sh.abort, a.wait_ns))) {
-      *static_cast<volatile int*>(&sh.abort) = 1;
-      go = false;
-    }
-    return go;
+    return go = warp_wait(bar, parity, &sh.abort, a.wait_ns);
   }
   __device__ __forceinline__ void segment(int b, int h, int row0, uint32_t lo, uint32_t hi, bool whole, float* slot) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = threadIdx.x;
@@ -390,9 +434,14 @@ template <class C, int D> struct Softmax {
     const bool works = row0 + 32 * warp < rows;                  // else its rows are none
     const int node = min(row, rows - 1) / a.group;
     float f = a.scale * kLog2e * (T::kE4 && a.k_scale != nullptr ? a.k_scale[h] : 1.0f);
+    const bool long_one = too_long(a, b);
     float m = -INFINITY, l = 0.0f;
     for (uint32_t tile = lo; go && tile < hi; ++tile, ++tiles) {
       const int buf = tiles & 1;
+      const int first = (int)tile * T::kBlock;
+      // the words of the tree, while the scores are on their way
+      uint32_t bits[2] = {0xFFFFFFFFu, 0xFFFFFFFFu};
+      if (works && first + T::kBlock > plain) seen_bits(a, tree, n, node, first, end, bits);
       if (!wait(&sh.s_full[buf], tiles / 2 & 1)) break;
       tc_fence_after();
       if (works) {
@@ -407,21 +456,22 @@ template <class C, int D> struct Softmax {
         }
 #pragma unroll
         for (int i = 0; i < 64; ++i) s[i] *= f;
-        const uint32_t outside = *static_cast<volatile uint32_t*>(&sh.outside[tiles % T::kStages]);
-        const int first = (int)tile * T::kBlock;
+        const uint32_t outside = *static_cast<volatile uint32_t*>(&sh.outside[tiles & 3]);
         if (outside != 0 || first + T::kBlock > plain) {
-          uint32_t bits[2];
-          seen_bits(a, tree, n, node, first, end, bits);
 #pragma unroll
           for (int i = 0; i < 64; ++i) {
             s[i] = bits[i / 32] >> (i & 31) & 1u ? s[i] : -INFINITY;
-            if (outside >> (i / 16) & 1u && s[i] > -INFINITY) s[i] = NAN;
           }
+          // a row that sees an entry of a page outside the pool is NaN
+          const uint32_t out0 = (outside & 1u ? 0xFFFFu : 0u) | (outside & 2u ? 0xFFFF0000u : 0u);
+          const uint32_t out1 = (outside & 4u ? 0xFFFFu : 0u) | (outside & 8u ? 0xFFFF0000u : 0u);
+          if (((bits[0] & out0) | (bits[1] & out1)) != 0) l = NAN;
         }
         __syncwarp();
-        float top = s[0];
+        float tops[4] = {s[0], s[1], s[2], s[3]};                // four chains
 #pragma unroll
-        for (int i = 1; i < 64; ++i) top = fmaxf(top, s[i]);
+        for (int i = 4; i < 64; ++i) tops[i & 3] = fmaxf(tops[i & 3], s[i]);
+        const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         const bool grows = top > m + kSlack || (m == -INFINITY && top > -INFINITY);
         const float c = grows ? exp2_(m - top) : 1.0f;
         if (grows) m = top;
@@ -440,13 +490,15 @@ template <class C, int D> struct Softmax {
           }
         }
         const float below = m == -INFINITY ? 0.0f : m - T::kLift;
+        float sums[4] = {l, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < 64; i += 16) {
           uint32_t hi_[8], lo_[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const float p0 = exp2_(s[i + 2 * j] - below), p1 = exp2_(s[i + 2 * j + 1] - below);
-            l += p0 + p1;
+            sums[2 * (j & 1)] += p0;
+            sums[2 * (j & 1) + 1] += p1;
             if constexpr (T::kE4) {
               hi_[j] = bits_of(__floats2half2_rn(p0, p1));
             } else {
@@ -459,6 +511,7 @@ template <class C, int D> struct Softmax {
           tmem_st8(at + i / 2, hi_);
           if constexpr (!T::kE4) tmem_st8(at + 32 + i / 2, lo_);
         }
+        l = (sums[0] + sums[1]) + (sums[2] + sums[3]);
         tmem_st_wait();
       }
       tc_fence_before();
@@ -467,34 +520,53 @@ template <class C, int D> struct Softmax {
     }
     if (go) wait(&sh.o_done, (tiles - 1) & 1);
     tc_fence_after();
-    const bool there = row < rows, poison = !go || too_long(a, b);
+    const bool there = row < rows, poison = !go || long_one;
     const bool odd = *static_cast<volatile int*>(&sh.odd[segments & 3]) != 0;
     const float v_scale = T::kE4 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
     const int head = h * a.group + row - node * a.group;
     const float sum = poison ? NAN : l;
+    const float k = sum == 0.0f ? 0.0f : v_scale * __frcp_rn(sum);   // as in write_row; NaN when given up
     if (works) {
+      const long long at = ((long long)b * a.nodes + node) * a.heads + head;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + at * D;
 #pragma unroll 1
       for (int d = 0; d < D; d += 32) {
         float x[32];
-        if (go) tmem_ld32(tmem + d, x);
+        tmem_ld32(tmem + d, x);
         if (there) {
+          if (whole) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            float4 y = go ? make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]) : make_float4(NAN, NAN, NAN, NAN);
-            if (odd) y = odd_values<C, D>(a, b, h, node, n, (int)(lo * T::kBlock), (int)(hi * T::kBlock), d + i, y);
-            if (whole) {
-              write_row<__nv_bfloat16>(a, (long long)b * a.nodes + node, head, d + i, D, y, m, sum, v_scale, T::kLift);
-            } else {
-              *reinterpret_cast<float4*>(slot + r * D + d + i) = y;
-              if (d + i == 0) {
-                slot[T::kRows * D + 2 * r] = m;
-                slot[T::kRows * D + 2 * r + 1] = sum;
-              }
-            }
+            for (int i = 0; i < 32; i += 8)
+              *reinterpret_cast<uint4*>(out + d + i) =
+                  make_uint4(bits_of(__floats2bfloat162_rn(x[i] * k, x[i + 1] * k)),
+                             bits_of(__floats2bfloat162_rn(x[i + 2] * k, x[i + 3] * k)),
+                             bits_of(__floats2bfloat162_rn(x[i + 4] * k, x[i + 5] * k)),
+                             bits_of(__floats2bfloat162_rn(x[i + 6] * k, x[i + 7] * k)));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+              *reinterpret_cast<float4*>(slot + r * D + d + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
           }
         }
         __syncwarp();
       }
+      if (there && odd) {            // infinite values and NaN that the row sees, added to what is written
+#pragma unroll 1
+        for (int d = 0; d < D; d += 4) {
+          const float4 y = odd_values<C, D>(a, b, h, node, n, (int)(lo * T::kBlock), (int)(hi * T::kBlock), d,
+                                            make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+#pragma unroll 1
+          for (int e = 0; e < 4; ++e) {
+            const float v = e == 0 ? y.x : e == 1 ? y.y : e == 2 ? y.z : y.w;
+            if (v == 0.0f) continue;
+            if (whole) out[d + e] = __float2bfloat16_rn(to_f32(out[d + e]) + v * k);
+            else slot[r * D + d + e] += v;
+          }
+        }
+      }
+      if (there && !whole) *reinterpret_cast<float2*>(slot + T::kRows * D + 2 * r) = make_float2(m, sum);
+      if (there && whole && a.lse != nullptr)
+        a.lse[at] = sum == 0.0f ? -INFINITY : (m - T::kLift + log2f(sum)) * kLn2;
     }
     tc_fence_before();
     asm volatile("bar.sync 1, 128;" ::: "memory");               // all four warps have read the segment's word
@@ -514,8 +586,10 @@ __global__ void __launch_bounds__(kTreeThreads, 2) paged_tree_kernel(const __gri
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     for (int i = 0; i < T::kStages; ++i) {
-      mbar_init(&sh.kv_full[i], 4);
-      mbar_init(&sh.kv_empty[i], 1);
+      mbar_init(&sh.k_full[i], 4);
+      mbar_init(&sh.k_empty[i], 1);
+      mbar_init(&sh.v_full[i], 4);
+      mbar_init(&sh.v_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.s_full[i], 1);
@@ -539,20 +613,21 @@ __global__ void __launch_bounds__(kTreeThreads, 2) paged_tree_kernel(const __gri
   pdl_wait();
   pdl_trigger();                     // the joining kernel makes the same plan meanwhile
   const Plan plan = make_plan<T>(a, before, sh.scratch, (int)gridDim.x);
+  const Run run = make_run(a, plan, before);
   if (warp < 4) {
     Softmax<C, D> w{a, sh, tmem + ((uint32_t)(32 * warp) << 16)};
-    each_segment<T>(a, plan, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool whole, float* slot) {
+    each_segment<T>(a, run, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool whole, float* slot) {
       w.segment(b, h, row0, lo, hi, whole, slot);
     });
   } else if (warp < 8) {
     Copier<C, D> w{a, sh, (int)threadIdx.x - 128};
-    each_segment<T>(a, plan, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool, float*) {
+    each_segment<T>(a, run, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool, float*) {
       w.segment(b, h, row0, lo, hi);
     });
     if constexpr (!T::kE4) asm volatile("cp.async.wait_all;" ::: "memory");
   } else {
     Issuer<C, D> w{a, sh, tmem};
-    each_segment<T>(a, plan, before, [&](int, int, int, uint32_t lo, uint32_t hi, bool, float*) { w.segment(lo, hi); });
+    each_segment<T>(a, run, before, [&](int, int, int, uint32_t lo, uint32_t hi, bool, float*) { w.segment(lo, hi); });
   }
   __syncwarp();
   tc_fence_before();
