@@ -439,11 +439,12 @@ struct Attention {
 #pragma unroll
           for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int node = min((row0 + 8 * r + 2 * t + (e & 1)) / a.group, a.nodes - 1);
-              const int entry = start + g + 8 * (e >> 1);
-              const bool yes = entry < end && sees(a, tree, n, node, entry);
-              s[u][r][e] = yes ? (out ? NAN : s[u][r][e]) : -INFINITY;
+            for (int e = 0; e < 2; ++e) {
+              const int node = min((row0 + 8 * r + 2 * t + e) / a.group, a.nodes - 1);
+              const uint32_t bits = seen_bits(a, tree, n, node, start, end);
+#pragma unroll
+              for (int x = e; x < 4; x += 2) s[u][r][x] = bits >> (g + 4 * (x - e)) & 1u ? s[u][r][x] : -INFINITY;
+              if (out && (bits & 0xFFFFu) != 0) l[r][e] = NAN;   // a page that is not there
             }
           clear_values(u, out ? 0 : end - start);
           if ((a.nodes > 1 || tree != nullptr) && clear_odd_values(u)) sh.odd = 1;
@@ -529,6 +530,7 @@ struct Attention {
     const int rows = min(a.nodes * a.group - row0, kRows);
     const float v_scale = kE4 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
     const bool poison = too_long(a, b);
+#pragma unroll 1
     for (int i = tid; i < rows * (D / 4); i += kThreads) {
       const int r = i / (D / 4), d = (i % (D / 4)) * 4;
       float top = -INFINITY;
@@ -544,7 +546,6 @@ struct Attention {
         x.x += c * y.x; x.y += c * y.y; x.z += c * y.z; x.w += c * y.w;
       }
       if (poison) sum = NAN;
-      if (sh.odd) x = odd_values<C, D>(a, b, h, (row0 + r) / a.group, n, (int)lo * kBlock, (int)hi * kBlock, d, x);
       if (!whole) {
         *reinterpret_cast<float4*>(slot + r * D + d) = x;
         if (d == 0) {
@@ -556,6 +557,11 @@ struct Attention {
         const int head = h * a.group + row - node * a.group;
         write_row<Q>(a, (long long)b * a.nodes + node, head, d, D, x, top, sum, v_scale, kLift);
       }
+    }
+    if (sh.odd) {
+      __syncthreads();
+      add_odd_values<C, Q, D>(a, b, h, row0, rows, n, (int)lo * kBlock, (int)hi * kBlock, whole ? nullptr : slot, tid,
+                              kThreads);
     }
   }
 };

@@ -52,13 +52,12 @@ struct Plan {
   uint64_t total;      // blocks
   uint32_t runs;       // that have any
   uint64_t each;       // total / runs
-  uint32_t rest;       // total % runs
+  uint32_t rest;       // the first runs, which have one block more
   float runs_a_block;
-  __device__ __forceinline__ uint64_t start(uint32_t run) const { return each * run + rest * run / runs; }   // total run / runs
-  // The run of a block: start(run) <= block < start(run + 1).  The estimate is off by one at
-  // most (runs < 2^16).
+  __device__ __forceinline__ uint64_t start(uint32_t run) const { return each * run + min(run, rest); }
+  // The run of a block: start(run) <= block < start(run + 1), from an estimate near it.
   __device__ __forceinline__ uint32_t run_of(uint64_t block) const {
-    uint32_t run = min((uint32_t)((float)block * runs_a_block), runs - 1);
+    uint32_t run = min((uint32_t)(__ull2float_rn(block) * runs_a_block), runs - 1);
 #pragma unroll 1
     while (start(run) > block) --run;
 #pragma unroll 1
@@ -110,7 +109,7 @@ template <class K> __device__ __forceinline__ Plan make_plan(const PagedArgs& a,
   const uint32_t d = max(p.runs, 1u);
   p.each = p.total >> 32 == 0 ? (uint32_t)p.total / d : divide_long(p.total, d);
   p.rest = (uint32_t)(p.total - p.each * d);
-  p.runs_a_block = (float)p.runs / (float)max(p.total, (uint64_t)1);
+  p.runs_a_block = __fdividef((float)p.runs, __ull2float_rn(max(p.total, (uint64_t)1)));
   return p;
 }
 
@@ -134,7 +133,7 @@ __device__ __forceinline__ Run make_run(const PagedArgs& a, const Plan& plan, co
   }
   const uint32_t count = before[r.b + 1] - before[r.b];   // not 0: `from` lies in it
   const uint64_t within = r.from - (uint64_t)before[r.b] * segments;
-  r.seg = min((uint32_t)((float)within / (float)count), segments - 1);   // off by one at most
+  r.seg = min((uint32_t)__fdividef(__ull2float_rn(within), (float)count), segments - 1);   // near it
 #pragma unroll 1
   while ((uint64_t)r.seg * count > within) --r.seg;
 #pragma unroll 1
@@ -184,26 +183,29 @@ __device__ __forceinline__ bool sees(const PagedArgs& a, const uint32_t* tree, i
   if (tree == nullptr) return j <= node;
   return (tree[(size_t)node * a.words + (j >> 5)] >> (j & 31)) & 1u;
 }
-  // Which of the entries first .. first + 63 row `node` sees, those from `end` on not.
-  __device__ __forceinline__ void seen_bits(const PagedArgs& a, const uint32_t* tree, int n, int node, int first,
-                                                   int end, uint32_t (&bits)[2]) {
-    const int j0 = first - (n - a.nodes), w0 = j0 >> 5;          // the first one's number among the newest
-    uint32_t w[3];
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      const int word = w0 + k;
-      if (word < 0) w[k] = 0xFFFFFFFFu;                          // before the newest: seen
-      else if (tree != nullptr) w[k] = word < a.words ? tree[(size_t)node * a.words + word] : 0u;
-      else w[k] = node >= 32 * word + 31 ? 0xFFFFFFFFu : node < 32 * word ? 0u : (2u << (node - 32 * word)) - 1u;
-    }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      bits[k] = __funnelshift_r(w[k], w[k + 1], j0 & 31);
-      const int left = end - first - 32 * k;
-      if (left < 32) bits[k] &= left <= 0 ? 0u : (1u << left) - 1u;
-    }
-  }
-
+  // The word of bits that tells which of the newest entries 32 w, 32 w + 1, ... row `node` sees
+// (all before the newest, w < 0).
+__device__ __forceinline__ uint32_t seen_word(const PagedArgs& a, const uint32_t* tree, int node, int w) {
+  if (w < 0) return 0xFFFFFFFFu;
+  if (tree != nullptr) return w < a.words ? tree[(size_t)node * a.words + w] : 0u;
+  return node >= 32 * w + 31 ? 0xFFFFFFFFu : node < 32 * w ? 0u : (2u << (node - 32 * w)) - 1u;
+}
+__device__ __forceinline__ uint32_t below(int left) {      // the lowest `left` bits
+  return left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u;
+}
+// Which of the entries first .. first + 31 (those from `end` on not) row `node` sees.
+__device__ __forceinline__ uint32_t seen_bits(const PagedArgs& a, const uint32_t* tree, int n, int node, int first, int end) {
+  const int j0 = first - (n - a.nodes), w0 = j0 >> 5;      // the first one's number among the newest
+  return __funnelshift_r(seen_word(a, tree, node, w0), seen_word(a, tree, node, w0 + 1), j0 & 31) & below(end - first);
+}
+// The same of 64 entries.
+__device__ __forceinline__ void seen_bits(const PagedArgs& a, const uint32_t* tree, int n, int node, int first, int end,
+                                          uint32_t (&bits)[2]) {
+  const int j0 = first - (n - a.nodes), w0 = j0 >> 5;
+  const uint32_t middle = seen_word(a, tree, node, w0 + 1);
+  bits[0] = __funnelshift_r(seen_word(a, tree, node, w0), middle, j0 & 31) & below(end - first);
+  bits[1] = __funnelshift_r(middle, seen_word(a, tree, node, w0 + 2), j0 & 31) & below(end - first - 32);
+}
 // 16 bytes to shared memory, zeros when not `there` (nothing is read then).
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
@@ -219,30 +221,41 @@ __device__ __forceinline__ float to_f32_any(__nv_bfloat16 x) { return __bfloat16
 __device__ __forceinline__ float to_f32_any(__nv_fp8_e4m3 x) { return float(x); }
 
 // Values that are infinite or NaN, where only some rows see an entry: a product with a p of
-// 0 would give NaN to the others.  They are cleared before the products, and the rows that
-// see one take it when a segment is finished: dims d .. d + 3 of those of the entries from
-// `from` to `to`, added to x.
-template <class C, int D>
-__device__ __noinline__ float4 odd_values(const PagedArgs& a, int b, int h, int node, int n, int from, int to, int d,
-                                          float4 x) {
+// 0 would give NaN to the others.  They are cleared before the products; when a segment's
+// rows have been written (to out, or to a partial slot) those of the entries from `from` to
+// `to` are added to the rows that see them, by `threads` threads.
+template <class C, class Q, int D>
+__device__ __noinline__ void add_odd_values(const PagedArgs& a, int b, int h, int row0, int rows, int n, int from, int to,
+                                            float* slot, int tid, int threads) {
   const uint32_t* tree = tree_of(a, b);
-  for (int at = max(max(from, n - a.nodes), 0); at < min(to, n); ++at) {
-    const int page = a.table[(size_t)b * a.width + at / a.page];
-    if (!sees(a, tree, n, node, at) || (unsigned)page >= (unsigned)a.n_pages) continue;
-    const C* p = static_cast<const C*>(a.v_pages) + (((size_t)page * a.kv_heads + h) * a.page + at % a.page) * D + d;
-    float* y = &x.x;
-    for (int e = 0; e < 4; ++e) {
-      const float value = to_f32_any(p[e]);
-      if (!isfinite(value)) y[e] += value;
+  const float sign = sizeof(C) == 1 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
+#pragma unroll 1
+  for (int i = tid; i < rows * D; i += threads) {
+    const int r = i / D, d = i % D, row = row0 + r, node = row / a.group;
+    float odd = 0.0f;
+#pragma unroll 1
+    for (int at = max(max(from, n - a.nodes), 0); at < min(to, n); ++at) {
+      const int page = a.table[(size_t)b * a.width + at / a.page];
+      if (!sees(a, tree, n, node, at) || (unsigned)page >= (unsigned)a.n_pages) continue;
+      const float v = to_f32_any(
+          static_cast<const C*>(a.v_pages)[(((size_t)page * a.kv_heads + h) * a.page + at % a.page) * D + d]);
+      if (!isfinite(v)) odd += v;
+    }
+    if (odd == 0.0f) continue;
+    if (slot != nullptr) {
+      slot[i] += odd;
+    } else {
+      Q* out = static_cast<Q*>(a.out) + (((long long)b * a.nodes + node) * a.heads + h * a.group + row - node * a.group) * D + d;
+      *out = from_f32<Q>(to_f32(*out) + odd * sign);
     }
   }
-  return x;
 }
-// The odd halves, bytes or words of x as all ones.
+// The odd halves, bytes or words of x as all ones: the exponent (of 8 bits: all seven) is
+// ones where one more carries out of it.
 template <class C> __device__ __forceinline__ uint32_t odd_in(uint32_t x) {
   if constexpr (sizeof(C) == 4) return (x & 0x7F800000u) == 0x7F800000u ? 0xFFFFFFFFu : 0u;
-  else if constexpr (sizeof(C) == 1) return __vcmpeq4(x & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
-  else return __vcmpeq2(x & 0x7F807F80u, 0x7F807F80u);
+  else if constexpr (sizeof(C) == 1) return (((x & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu;
+  else return (((x & 0x7F807F80u) + 0x00800080u) >> 15 & 0x00010001u) * 0xFFFFu;
 }
 
 // Dims d .. d + 3 of a row's result, from the sums of p v and of p (p times 2^lift).

@@ -355,7 +355,6 @@ template <class C, int D> struct Rows {
           d = 16 * i + (odd ? 8 : 0) + 4 * (t >> 1);
         }
         if (row >= rows) continue;
-        if (sh.odd) x = odd_values<C, D>(a, b, h, node, n, (int)(lo * kTile), (int)(hi * kTile), d, x);
         if (whole) {
           write_row<__nv_bfloat16>(a, (long long)b * a.nodes + node, head, d, D, x, m[e], sum, v_scale, kLift);
         } else {
@@ -366,6 +365,11 @@ template <class C, int D> struct Rows {
           }
         }
       }
+    }
+    if (sh.odd) {
+      __syncthreads();
+      add_odd_values<C, __nv_bfloat16, D>(a, b, h, row0, min(rows - row0, kRows), n, (int)(lo * kTile), (int)(hi * kTile),
+                                          whole ? nullptr : slot, threadIdx.x, kThreads);
     }
   }
 };

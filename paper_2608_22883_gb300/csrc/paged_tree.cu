@@ -550,26 +550,15 @@ template <class C, int D> struct Softmax {
         }
         __syncwarp();
       }
-      if (there && odd) {            // infinite values and NaN that the row sees, added to what is written
-#pragma unroll 1
-        for (int d = 0; d < D; d += 4) {
-          const float4 y = odd_values<C, D>(a, b, h, node, n, (int)(lo * T::kBlock), (int)(hi * T::kBlock), d,
-                                            make_float4(0.0f, 0.0f, 0.0f, 0.0f));
-#pragma unroll 1
-          for (int e = 0; e < 4; ++e) {
-            const float v = e == 0 ? y.x : e == 1 ? y.y : e == 2 ? y.z : y.w;
-            if (v == 0.0f) continue;
-            if (whole) out[d + e] = __float2bfloat16_rn(to_f32(out[d + e]) + v * k);
-            else slot[r * D + d + e] += v;
-          }
-        }
-      }
       if (there && !whole) *reinterpret_cast<float2*>(slot + T::kRows * D + 2 * r) = make_float2(m, sum);
       if (there && whole && a.lse != nullptr)
         a.lse[at] = sum == 0.0f ? -INFINITY : (m - T::kLift + log2f(sum)) * kLn2;
     }
     tc_fence_before();
-    asm volatile("bar.sync 1, 128;" ::: "memory");               // all four warps have read the segment's word
+    asm volatile("bar.sync 1, 128;" ::: "memory");               // all four warps have written, and read the segment's word
+    if (odd)
+      add_odd_values<C, __nv_bfloat16, D>(a, b, h, row0, min(rows - row0, T::kRows), n, (int)(lo * T::kBlock),
+                                          (int)(hi * T::kBlock), whole ? nullptr : slot, r, 128);
     if (threadIdx.x == 0) *static_cast<volatile int*>(&sh.odd[segments & 3]) = 0;
     ++segments;
   }

@@ -246,11 +246,13 @@ def check_attention(fovea, q, k_pages, v_pages, table, lens, tree=None, scale=No
     nodes, group = q.shape[0] // B, heads // kv
     scale = dim ** -0.5 if scale is None else scale
     assert out.shape == q.shape and out.dtype == q.dtype and lse.shape == q.shape[:2]
+    got["bounds"] = []
     p_error = {BF16: 2.0 ** -16, E4M3: 2.0 ** -11, FP32: 2.0 ** -21}[k_pages.dtype]
     for b, n in enumerate(lens.tolist()):
         rows = slice(b * nodes, (b + 1) * nodes)
         if n <= 0:
             assert not out[rows].any() and bool((lse[rows] == -math.inf).all())
+            got["bounds"].append(None)
             continue
         k, v = (entries(x, table, b, n).double() for x in (k_pages, v_pages))
         if scales:
@@ -279,6 +281,7 @@ def check_attention(fovea, q, k_pages, v_pages, table, lens, tree=None, scale=No
         # Sums: a truncated addition a block of 16 and part of p, the joins of warps and runs.
         sums = (n / 8 + 64) * 2.0 ** -23
         bound = want.abs() * HALF_ULP[q.dtype] + size * (2 * delta[..., None] + sums + p_error) + 1e-38
+        got["bounds"].append(bound)
         within(out[rows].view_as(want), want, bound, f"out of sequence {b}")
         within(lse[rows].view_as(want_lse), want_lse, delta + sums + want_lse.abs().nan_to_num(0, 0, 0) * 2 * U, f"lse {b}")
     return got
@@ -404,9 +407,13 @@ def test_attention_bad_pages(fovea):
         table[0, 3] = -1
         table[1, 6] = k.shape[0]
         table[4, 2:] = 2 ** 31 - 1                 # behind the last one: not used
-        got = fovea.paged_attention(q, k, v, table, ints([100, 100, 129, 100, -5]), want_lse=True, **scales)
+        got = fovea.paged_attention(q, k, v, table, ints(lens), want_lse=True, **scales)
         for x, y in ((got["out"], want["out"]), (got["lse"], want["lse"])):
-            assert bool(torch.isnan(x[:3]).all()) and same(x[3], y[3])
+            assert bool(torch.isnan(x[:2]).all()) and same(x[2:], y[2:])
+        # other lengths cut the sums elsewhere: two results, each within the bound
+        got = fovea.paged_attention(q, k, v, table, ints([100, 100, 129, 100, -5]), want_lse=True, **scales)
+        assert bool(torch.isnan(got["out"][:3]).all()) and bool(torch.isnan(got["lse"][:3]).all())
+        within(got["out"][3], want["out"][3].double(), 2 * want["bounds"][3].view_as(got["out"][3]))
         assert not got["out"][4].any() and bool((got["lse"][4] == -math.inf).all())
         # a node's own row alone needs the page of the newest entries
         got = fovea.paged_attention(q[:4], k, v, table[1:3], ints([97, 97]), **scales,
