@@ -17,11 +17,17 @@
 #include <cstddef>
 
 #include "paged_core.cuh"
+#include "tc_ptx.cuh"
 
 namespace fovea {
 
 namespace {
 
+__device__ __forceinline__ float dsmem_f32(uint32_t at, uint32_t rank) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(tc::map_dsmem(at, rank)) : "memory");
+  return v;
+}
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
@@ -499,11 +505,9 @@ struct Attention {
     }
   }
 
-  // The warps' sums of a segment together; written to the output when the segment is
-  // whole, else to a partial slot.
-  __device__ __forceinline__ void finish(const PagedArgs& a, Shared& sh, int b, int h, int row0, int n, uint32_t lo,
-                                         uint32_t hi, bool whole, float* slot) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  // The warps' sums to shared memory, and of all warps together (dims d .. d + 3 of row r).
+  __device__ __forceinline__ void stage_sums(Shared& sh) const {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -526,6 +530,28 @@ struct Attention {
         for (int e = 0; e < 2; ++e)
           *reinterpret_cast<float2*>(&sh.o[warp][8 * r + 2 * t + e][d]) = make_float2(o[r][i][e], o[r][i][2 + e]);
       }
+  }
+  __device__ __forceinline__ static float4 warps_sum(const Shared& sh, int r, int d, float& top, float& sum) {
+    top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh.m[w][r]);
+    sum = 0.0f;
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float mw = sh.m[w][r], c = mw == top ? 1.0f : exp2_(mw - top);
+      const float4 y = *reinterpret_cast<const float4*>(&sh.o[w][r][d]);
+      sum += c * sh.l[w][r];
+      x.x += c * y.x; x.y += c * y.y; x.z += c * y.z; x.w += c * y.w;
+    }
+    return x;
+  }
+
+  // A segment's sums to the output when it is whole, else to a partial slot.
+  __device__ __forceinline__ void finish(const PagedArgs& a, Shared& sh, int b, int h, int row0, int n, uint32_t lo,
+                                         uint32_t hi, bool whole, float* slot) {
+    const int tid = threadIdx.x;
+    stage_sums(sh);
     __syncthreads();
     const int rows = min(a.nodes * a.group - row0, kRows);
     const float v_scale = kE4 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
@@ -533,18 +559,8 @@ struct Attention {
 #pragma unroll 1
     for (int i = tid; i < rows * (D / 4); i += kThreads) {
       const int r = i / (D / 4), d = (i % (D / 4)) * 4;
-      float top = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh.m[w][r]);
-      float sum = 0.0f;
-      float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float mw = sh.m[w][r], c = mw == top ? 1.0f : exp2_(mw - top);
-        const float4 y = *reinterpret_cast<const float4*>(&sh.o[w][r][d]);
-        sum += c * sh.l[w][r];
-        x.x += c * y.x; x.y += c * y.y; x.z += c * y.z; x.w += c * y.w;
-      }
+      float top, sum;
+      const float4 x = warps_sum(sh, r, d, top, sum);
       if (poison) sum = NAN;
       if (!whole) {
         *reinterpret_cast<float4*>(slot + r * D + d) = x;
@@ -568,7 +584,7 @@ struct Attention {
 
 // CTAs an SM, by registers.
 template <class C, int D, int RT> constexpr int per_sm() {
-  return sizeof(C) == 4 || RT * D >= 256 ? 2 : 3;
+  return sizeof(C) == 4 || RT * D >= 256 ? 2 : sizeof(C) == 2 && RT * D == 64 ? 4 : 3;
 }
 
 template <class C, class Q, int D, int RT>
@@ -594,6 +610,70 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_attention_
   });
 }
 
+// Small tables: a cluster of CTAs a segment, each an equal share of its blocks, which join
+// their sums through distributed shared memory: one launch, no partial sums in memory.
+template <class C, class Q, int D, int RT>
+__global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_cluster_kernel(const __grid_constant__ PagedArgs a,
+                                                                                     int ctas) {
+  using A = Attention<C, Q, D, RT>;
+  extern __shared__ __align__(16) uint8_t raw[];
+  typename A::Shared& sh = *reinterpret_cast<typename A::Shared*>(raw);
+  __shared__ float top[A::kRows], sum[A::kRows];
+  pdl_wait();
+  pdl_trigger();
+  const int tid = threadIdx.x, rank = (int)blockIdx.x % ctas, seg = (int)blockIdx.x / ctas;
+  const int segments = a.kv_heads * a.row_blocks, b = seg / segments, h = (seg - b * segments) / a.row_blocks;
+  const int row0 = (seg - b * segments - h * a.row_blocks) * A::kRows, rows = min(a.nodes * a.group - row0, A::kRows);
+  const int n = length_of(a, b);
+  if (blockIdx.x == 0 && tid == 0) ensure_header(a.header);
+  A::stage_rows(a, sh, b, h, row0);
+  __syncthreads();
+  const uint32_t blocks = (uint32_t)(n + A::kBlock - 1) / A::kBlock;
+  const uint32_t each = (blocks + ctas - 1) / ctas, lo = min(rank * each, blocks), hi = min(lo + each, blocks);
+  A at;
+  at.blocks(a, sh, b, h, row0, n, lo, hi);
+  at.stage_sums(sh);
+  __syncthreads();
+#pragma unroll 1
+  for (int i = tid; i < rows * (D / 4); i += kThreads) {         // the CTA's sums, in the first warp's place
+    const int r = i / (D / 4), d = (i % (D / 4)) * 4;
+    float m, l;
+    const float4 x = A::warps_sum(sh, r, d, m, l);
+    *reinterpret_cast<float4*>(&sh.o[0][r][d]) = x;
+    if (d == 0) {
+      top[r] = m;
+      sum[r] = l;
+    }
+  }
+  tc::cluster_sync();
+  const float v_scale = A::kE4 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
+  const uint32_t tops = tc::smem_u32(top), sums = tc::smem_u32(sum), mine = tc::smem_u32(&sh.o[0][0][0]);
+#pragma unroll 1
+  for (int i = tid * ctas + rank; i < rows * (D / 4); i += kThreads * ctas) {
+    const int r = i / (D / 4), d = (i % (D / 4)) * 4;
+    float m = -INFINITY, l = 0.0f;
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
+    for (int q = 0; q < ctas; ++q) m = fmaxf(m, dsmem_f32(tops + 4 * r, q));
+#pragma unroll 2
+    for (int q = 0; q < ctas; ++q) {
+      const float mq = dsmem_f32(tops + 4 * r, q), c = mq == m ? 1.0f : exp2_(mq - m);
+      const float4 y = tc::ld_dsmem_f4(tc::map_dsmem(mine + (r * (D + 4) + d) * 4, q));
+      l += c * dsmem_f32(sums + 4 * r, q);
+      x.x += c * y.x; x.y += c * y.y; x.z += c * y.z; x.w += c * y.w;
+    }
+    if (too_long(a, b)) l = NAN;
+    const int row = row0 + r, node = row / a.group;
+    write_row<Q>(a, (long long)b * a.nodes + node, h * a.group + row - node * a.group, d, D, x, m, l, v_scale, A::kLift);
+  }
+  bool odd = false;                  // of any of the cluster's CTAs: the first adds them
+  if (rank == 0)
+#pragma unroll 1
+    for (int q = 0; q < ctas; ++q) odd |= __float_as_uint(dsmem_f32(tc::smem_u32(&sh.odd), q)) != 0;
+  tc::cluster_sync();
+  if (odd) add_odd_values<C, Q, D>(a, b, h, row0, rows, n, 0, n, nullptr, tid, kThreads);
+}
+
 // More rows than these go to the kernel of many rows.
 constexpr int kManyRows = 16, kTreeRows = 32;
 // Rows that a warp takes together, by 8: as many as there are, up to what its registers hold.
@@ -601,10 +681,50 @@ template <class C, int D> constexpr int most_tiles() {
   return sizeof(C) == 4 || D == 256 ? 1 : D == 128 ? 2 : 4;
 }
 
+// CTAs a segment for a cluster of them each, or 0: few segments, of a table that leaves a
+// warp few steps, since a cluster whose sequence is shorter than its table idles.  One
+// sequence of 640 entries, 32 heads: 9.0 us and one launch (7.4 us on the host), 8.8 and
+// two (9.7) in runs; 4096 entries, 8 key heads: 12.2 and 15.3.  16 sequences of 1 to 4096
+// entries: 25 and 17; 8 of 2048, 32 key heads: 55 and 44.
+template <class A> int cluster_ctas(const PagedArgs& a) {
+  const long long segments = (long long)a.B * a.kv_heads * ((a.nodes * a.group + A::kRows - 1) / A::kRows);
+  int ctas = 1;
+  while (ctas < 8 && segments * ctas < 2 * 152) ctas *= 2;
+  const long long steps = ((long long)a.width * a.page + A::kBlock * kWarps * ctas - 1) / (A::kBlock * kWarps * ctas);
+  return segments <= 2 * 152 && steps <= (a.B == 1 ? 16 : 4) ? ctas : 0;
+}
+
+template <class C, class Q, int D, int RT>
+cudaError_t launch_cluster(PagedArgs a, int ctas, cudaStream_t s) {
+  using A = Attention<C, Q, D, RT>;
+  static std::atomic<unsigned long long> raised{0};
+  set_up<A>(a);
+  cudaError_t e = raise_smem_limit(paged_cluster_kernel<C, Q, D, RT>, 64 * 1024, raised);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((long long)a.B * a.kv_heads * a.row_blocks * ctas));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = sizeof(typename A::Shared);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, paged_cluster_kernel<C, Q, D, RT>, a, ctas);
+}
+
 template <class C, class Q, int D, int RT>
 cudaError_t launch_as(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
   using A = Attention<C, Q, D, RT>;
   static std::atomic<unsigned long long> raised{0};
+  if (workspace == nullptr) {
+    const int ctas = cluster_ctas<A>(a);
+    if (ctas > 0) return launch_cluster<C, Q, D, RT>(a, ctas, s);
+  }
   return launch_runs<A, C, Q, D>(a, paged_attention_kernel<C, Q, D, RT>, kThreads, sizeof(typename A::Shared),
                                  152 * per_sm<C, D, RT>(), s, workspace, raised);
 }

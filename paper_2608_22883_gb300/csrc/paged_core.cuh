@@ -389,6 +389,20 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
   }
 }
 
+// What the kernels are told beside the call's arguments.
+template <class K> void set_up(PagedArgs& a) {
+  uint8_t* ws = static_cast<uint8_t*>(a.workspace);
+  a.header = reinterpret_cast<int*>(ws);
+  a.slots = reinterpret_cast<float*>(ws + kWsHeaderBytes);
+  a.wait_ns = wait_limit_ns();
+  const uint32_t per_page = a.page / 16;
+  a.page_magic = per_page <= 1 ? 0 : (uint32_t)((1ull << 32) / per_page + 1);
+  a.q_words = (reinterpret_cast<uintptr_t>(a.q) & 3) == 0 && a.q_ld % 2 == 0 && a.q_hs % 2 == 0;
+  a.q_chunks = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && a.q_ld % 8 == 0 && a.q_hs % 8 == 0;
+  a.room = a.width * a.page;
+  a.row_blocks = (a.nodes * a.group + K::kRows - 1) / K::kRows;
+}
+
 // Launches a kernel of `grid` CTAs and the joining one, or tells the workspace's bytes.
 template <class K, class C, class Q, int D, class Kernel>
 cudaError_t launch_runs(PagedArgs a, Kernel kernel, int threads, size_t shared, int grid, cudaStream_t s,
@@ -398,17 +412,8 @@ cudaError_t launch_runs(PagedArgs a, Kernel kernel, int threads, size_t shared, 
     *workspace = kWsHeaderBytes + slots + (size_t)grid * 4;
     return cudaSuccess;
   }
-  uint8_t* ws = static_cast<uint8_t*>(a.workspace);
-  a.header = reinterpret_cast<int*>(ws);
-  a.slots = reinterpret_cast<float*>(ws + kWsHeaderBytes);
-  a.gave_up = reinterpret_cast<int*>(ws + kWsHeaderBytes + slots);
-  a.wait_ns = wait_limit_ns();
-  const uint32_t per_page = a.page / 16;
-  a.page_magic = per_page <= 1 ? 0 : (uint32_t)((1ull << 32) / per_page + 1);
-  a.q_words = (reinterpret_cast<uintptr_t>(a.q) & 3) == 0 && a.q_ld % 2 == 0 && a.q_hs % 2 == 0;
-  a.q_chunks = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && a.q_ld % 8 == 0 && a.q_hs % 8 == 0;
-  a.room = a.width * a.page;
-  a.row_blocks = (a.nodes * a.group + K::kRows - 1) / K::kRows;
+  set_up<K>(a);
+  a.gave_up = reinterpret_cast<int*>(static_cast<uint8_t*>(a.workspace) + kWsHeaderBytes + slots);
   const size_t plan_bytes = ((size_t)a.B + 1) * 4;
   cudaError_t e = raise_smem_limit(kernel, 227 * 1024 - 1024, raised);
   if (e != cudaSuccess) return e;
