@@ -1555,6 +1555,8 @@ static fovea_status check_cache(const CachePages& c, int rows) {
     return fail(FOVEA_ERR_INVALID_ARG, "the table's sizes %d and %d must be at least 0 and 1", c.B, c.width);
   if (c.B > FOVEA_MAX_CACHE_SEQ)
     return fail(FOVEA_ERR_UNSUPPORTED, "%d sequences > %d", c.B, FOVEA_MAX_CACHE_SEQ);
+  if ((long long)c.n_pages * c.kv_heads * (c.page / 16) >= (1ll << 32))
+    return fail(FOVEA_ERR_UNSUPPORTED, "%d pages of %d heads of %d entries", c.n_pages, c.kv_heads, c.page);
   if ((long long)c.width * c.page > (1ll << 30) || (long long)c.B * c.width * c.page > (1ll << 34))
     return fail(FOVEA_ERR_UNSUPPORTED, "tables of %d by %d pages of %d entries", c.B, c.width, c.page);
   WANT_ALIGNED(c.k_scale, 4, "k_scale");

@@ -288,10 +288,11 @@ template <class Q> __device__ __forceinline__ const Q* row_of(const PagedArgs& a
          (long long)(h * a.group + (r - node * a.group)) * a.q_hs;
 }
 
-// A row whose segment is cut between runs, joined in their order; rows of sequences
-// without entries get 0.  A warp a row.
+// Rows whose segment is cut between runs, joined in their order; rows of sequences without
+// entries get 0.  A warp takes `chunk` rows of a key head together (a divisor of kRows), as
+// a segment that one run has written is passed over whole.
 template <class K, class C, class Q, int D>
-__global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_constant__ PagedArgs a, int runs) {
+__global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_constant__ PagedArgs a, int runs, int chunk) {
   extern __shared__ __align__(16) uint8_t raw[];
   uint32_t* before = reinterpret_cast<uint32_t*>(raw);
   __shared__ uint32_t scratch[kWarps];
@@ -308,24 +309,31 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
       if (__any_sync(0xffffffffu, any) && lane == 0) atomicOr(a.header, kErrTimeout);
     }
   }
-  const uint32_t rows = (uint32_t)a.B * a.nodes * a.heads;       // < 2^30
+  const uint32_t rows = a.nodes * a.group, chunks = (rows + chunk - 1) / chunk;
+  const uint32_t items = (uint32_t)a.B * a.kv_heads * chunks;    // < 2^30
 #pragma unroll 1
-  for (uint32_t i = blockIdx.x * kWarps + (threadIdx.x >> 5); i < rows; i += gridDim.x * kWarps) {
-    const uint32_t n = i / a.heads;
-    const int head = (int)(i - n * a.heads), b = (int)(n / a.nodes), node = (int)(n - b * a.nodes);
-    const int h = head / a.group, row = node * a.group + head - h * a.group;
+  for (uint32_t i = blockIdx.x * kWarps + (threadIdx.x >> 5); i < items; i += gridDim.x * kWarps) {
+    const uint32_t head_of = i / chunks, row_from = (i - head_of * chunks) * chunk;
+    const int b = (int)(head_of / a.kv_heads), h = (int)(head_of - b * a.kv_heads);
     const uint32_t segments = a.kv_heads * a.row_blocks, count = before[b + 1] - before[b];
     const float v_scale = sizeof(C) == 1 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
     constexpr int kVecs = (D + 127) / 128, kAhead = 4;
-    float top = -INFINITY, sum = 0.0f;
-    float4 x[kVecs];
-#pragma unroll
-    for (int c = 0; c < kVecs; ++c) x[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    uint32_t first = 1, last = 0;    // runs; none
+    bool second = false;             // the first run's second slot
     if (count != 0) {
-      const uint64_t s0 = (uint64_t)before[b] * segments + (uint64_t)(h * a.row_blocks + row / K::kRows) * count;
-      const uint32_t first = plan.run_of(s0 + K::kFront), last = plan.run_of(s0 + count - 1);
+      const uint64_t s0 = (uint64_t)before[b] * segments + (uint64_t)(h * a.row_blocks + row_from / K::kRows) * count;
+      first = plan.run_of(s0 + K::kFront);
+      last = plan.run_of(s0 + count - 1);
       if (first == last) continue;   // written already
-      const bool second = plan.start(first) < s0;          // the first run's second slot
+      second = plan.start(first) < s0;
+    }
+    const uint32_t row_to = min(row_from + chunk, rows);
+#pragma unroll 1
+    for (uint32_t row = row_from; row < row_to; ++row) {
+      float top = -INFINITY, sum = 0.0f;
+      float4 x[kVecs];
+#pragma unroll
+      for (int c = 0; c < kVecs; ++c) x[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       const float* slot = a.slots + (size_t)(2 * first + second) * K::kSlot;   // of `run`
       const int r = row % K::kRows;
       // maxima and sums a lane a run, 32 runs at a time, with the first runs' sums of p v on
@@ -380,11 +388,12 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
           }
         }
       }
-    }
+      const int node = (int)(row / a.group), head = h * a.group + (int)row - node * a.group;
 #pragma unroll
-    for (int v = 0; v < kVecs; ++v) {
-      const int d = 128 * v + 4 * lane;
-      if (d < D) write_row<Q>(a, n, head, d, D, x[v], top, sum, v_scale, K::kLift);
+      for (int v = 0; v < kVecs; ++v) {
+        const int d = 128 * v + 4 * lane;
+        if (d < D) write_row<Q>(a, (long long)b * a.nodes + node, head, d, D, x[v], top, sum, v_scale, K::kLift);
+      }
     }
   }
 }
@@ -419,9 +428,13 @@ cudaError_t launch_runs(PagedArgs a, Kernel kernel, int threads, size_t shared, 
   if (e != cudaSuccess) return e;
   e = launch_pdl(kernel, dim3(grid), dim3(threads), shared + plan_bytes, s, a);
   if (e != cudaSuccess) return e;
-  const long long ctas = ((long long)a.B * a.nodes * a.heads + kWarps - 1) / kWarps;
+  // rows a warp: few enough to leave every SM its warps
+  int chunk = 4;
+  const long long rows = (long long)a.nodes * a.group, heads = (long long)a.B * a.kv_heads;
+  while (chunk > 1 && heads * ((rows + chunk - 1) / chunk) < 152 * 32) chunk /= 2;
+  const long long ctas = (heads * ((rows + chunk - 1) / chunk) + kWarps - 1) / kWarps;
   return launch_pdl(paged_join_kernel<K, C, Q, D>, dim3((unsigned)(ctas < 152 * 8 ? ctas : 152 * 8)), dim3(kThreads),
-                    plan_bytes, s, a, grid);
+                    plan_bytes, s, a, grid, chunk);
 }
 
 // The number of a block of 16 entries' page in the table: a page has 1 to 64 blocks and a

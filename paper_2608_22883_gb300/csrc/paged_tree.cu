@@ -6,8 +6,8 @@
 // It writes p back over the scores, as the first operand of O += P V (two bf16 values that
 // add up to 16 bits of p, or 11 bits of fp16 beside 8-bit values, lifted so that the largest
 // fit).  V lies as it is cached, entries by dims, and is read along its rows (MN-major).
-// Three roles, joined by mbarriers with bounded waits: four warps turn S into P; four copy
-// keys and values of the pages (asynchronous copies, or through registers where 8 bits
+// The roles, joined by mbarriers with bounded waits: four warps turn S into P; two copy
+// keys and two values of the pages (asynchronous copies, or through registers where 8 bits
 // become fp16) into the 128-byte-swizzled layout; one issues the products.  S of a tile is
 // formed while P of the one before is made (two places in tensor memory), and two CTAs an
 // SM fill one another's waits.
@@ -55,19 +55,25 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* a
   *static_cast<volatile int*>(abort) = 1;
   return false;
 }
+// 32 bytes, a whole sector (two stores of 16 each would write half of one).
+__device__ __forceinline__ void store32(void* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f,
+                                        uint32_t g, uint32_t h) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d),
+               "r"(e), "r"(f), "r"(g), "r"(h)
+               : "memory");
+}
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 template <class C, int D> struct Tree {
   static constexpr bool kE4 = sizeof(C) == 1, kWaits = true;
   static constexpr float kLift = kE4 ? 7.0f : 0.0f;              // p 2^7 2^8 fits fp16
-  static constexpr int kRows = 128, kBlock = 64, kLeast = 1;
+  static constexpr int kRows = 128, kBlock = 64, kLeast = 3;
   static constexpr uint32_t kFront = 2;
-  static constexpr int kSlot = kRows * (D + 2);
+  static constexpr int kSlot = kRows * (D + 2);                  // a multiple of 8 floats
   static constexpr int kStages = 2, kParts = kBlock / 16;
   static constexpr int kHalves = D / 64;                         // blocks of 64 dims, 128 bytes a row
   static constexpr int kTileBytes = kHalves * kBlock * 128;      // keys or values of a tile, 16 bits each
   static constexpr int kRowBytes = D * sizeof(C), kChunks = kRowBytes / 16;
-  static constexpr int kPass = 128 / kChunks, kCopies = kBlock / kPass;    // rows a pass of the copying threads
   static constexpr uint32_t kFormat = kE4 ? 0u : 1u;
   // D fp32, A and B of the format, M = 128; S: N = 64 entries, K-major; O: N = D dims, MN-major
   static constexpr uint32_t kIdesc = (1u << 4) | (kFormat << 7) | (kFormat << 10) | ((uint32_t)(kRows >> 4) << 24);
@@ -108,56 +114,63 @@ template <class C> __device__ __forceinline__ uint32_t clear_odd(uint4& x) {
   return odd.x | odd.y | odd.z | odd.w;
 }
 
-// Copies of the pages: the queries of each segment and its tiles, by warps 4 to 7.
-template <class C, int D> struct Copier {
+// Copies of the pages: keys (behind the queries of each segment) by warps 4 and 5, values by
+// warps 6 and 7.
+template <class C, int D, bool KEYS> struct Copier {
   using T = Tree<C, D>;
   using S = typename T::Shared;
+  static constexpr int kThreads2 = 64, kPass = kThreads2 / T::kChunks, kCopies = T::kBlock / kPass;
   const PagedArgs& a;
   S& sh;
-  int tid;                           // 0 .. 127
-  uint32_t keys_begun = 0, values_begun = 0, segments = 0;   // tiles, segments
+  int tid;                           // 0 .. 63
+  uint32_t begun = 0, segments = 0;  // tiles, segments
   bool go = true;
 
   __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
     return go = warp_wait(bar, parity, &sh.abort, a.wait_ns);
   }
   __device__ __forceinline__ void queries(int b, int h, int row0) {
-    const int rows = a.nodes * a.group, r = tid, row = row0 + r;
-    const bool there = row < rows;
-    const __nv_bfloat16* p = row_of<__nv_bfloat16>(a, b, h, there ? row : 0);
-    float power = 1.0f;
-    if constexpr (T::kE4) {
-      float top = 0.0f;
-      for (int d = 0; d < D; ++d) top = fmaxf(top, there ? fabsf(to_f32(p[d])) : 0.0f);
-      power = row_power(top);
-      sh.power[segments & 3][r] = power;
-    }
-    if (!T::kE4 && a.q_chunks) {     // with the copies of the first keys
-      const uint32_t q = smem_u32(sh.q);
+    const int rows = a.nodes * a.group;
+#pragma unroll 1
+    for (int r = tid; r < T::kRows; r += kThreads2) {
+      const int row = row0 + r;
+      const bool there = row < rows;
+      const __nv_bfloat16* p = row_of<__nv_bfloat16>(a, b, h, there ? row : 0);
+      if (!T::kE4 && a.q_chunks) {   // with the copies of the first keys
+        const uint32_t q = smem_u32(sh.q);
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c) copy16(q + T::place(r, c, T::kRows), p + 8 * c, there);
-      return;
-    }
-    const float k = 1.0f / power;
-#pragma unroll 2
-    for (int c = 0; c < D / 8; ++c) {
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (there) {
-        if (a.q_chunks) {
-          x = *reinterpret_cast<const uint4*>(p + 8 * c);
-        } else {
-          const uint16_t* w = reinterpret_cast<const uint16_t*>(p + 8 * c);
-          x = make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16,
-                         w[6] | (uint32_t)w[7] << 16);
-        }
-        if constexpr (T::kE4) {
-          uint32_t* w = &x.x;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            w[i] = bits_of(__floats2half2_rn(__uint_as_float(w[i] << 16) * k, __uint_as_float(w[i] & 0xFFFF0000u) * k));
-        }
+        for (int c = 0; c < D / 8; ++c) copy16(q + T::place(r, c, T::kRows), p + 8 * c, there);
+        continue;
       }
-      *reinterpret_cast<uint4*>(sh.q + T::place(r, c, T::kRows)) = x;
+      float power = 1.0f;
+      if constexpr (T::kE4) {
+        float top = 0.0f;
+#pragma unroll 16
+        for (int d = 0; d < D; ++d) top = fmaxf(top, there ? fabsf(to_f32(p[d])) : 0.0f);
+        power = row_power(top);
+        sh.power[segments & 3][r] = power;
+      }
+      const float k = 1.0f / power;
+#pragma unroll 4
+      for (int c = 0; c < D / 8; ++c) {
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (there) {
+          if (a.q_chunks) {
+            x = *reinterpret_cast<const uint4*>(p + 8 * c);
+          } else {
+            const uint16_t* w = reinterpret_cast<const uint16_t*>(p + 8 * c);
+            x = make_uint4(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16, w[4] | (uint32_t)w[5] << 16,
+                           w[6] | (uint32_t)w[7] << 16);
+          }
+          if constexpr (T::kE4) {
+            uint32_t* w = &x.x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              w[i] = bits_of(__floats2half2_rn(__uint_as_float(w[i] << 16) * k, __uint_as_float(w[i] & 0xFFFF0000u) * k));
+          }
+        }
+        *reinterpret_cast<uint4*>(sh.q + T::place(r, c, T::kRows)) = x;
+      }
     }
   }
 
@@ -168,184 +181,134 @@ template <class C, int D> struct Copier {
     const uint32_t last_block = (uint32_t)(end - 1) / 16;
     const int32_t* table = a.table + (size_t)b * a.width;
     const uint32_t per_page = a.page / 16, stride = a.kv_heads * per_page;
-    const uint8_t* keys = static_cast<const uint8_t*>(a.k_pages) + (size_t)h * per_page * 16 * T::kRowBytes;
-    const uint8_t* values = static_cast<const uint8_t*>(a.v_pages) + (size_t)h * per_page * 16 * T::kRowBytes;
     const bool mixed = a.nodes > 1 || a.tree != nullptr;         // rows may differ in what they see
-    const int chunk = tid % T::kChunks, row = tid / T::kChunks;
-    // The pages' places of a tile, looked up a tile ahead for keys and for values.
-    struct Where {
-      int id[T::kParts];
-      unsigned long long off[T::kParts];
-      uint32_t outside;
-    } kw, vw;
-    auto look_up = [&](Where& w, uint32_t tile) {
+    const int chunk = tid % T::kChunks, row = tid / T::kChunks;  // this thread's of the first pass
+    const uint8_t* mine = static_cast<const uint8_t*>(KEYS ? a.k_pages : a.v_pages) +
+                          (size_t)h * per_page * 16 * T::kRowBytes + row * T::kRowBytes + chunk * 16;
+    // The blocks of a tile in the pool (below 2^32 of them) and the parts that are not in it.
+    int id[T::kParts];
+    uint32_t block[T::kParts], outside = 0;
+    auto look_up = [&](uint32_t tile) {
 #pragma unroll
-      for (int u = 0; u < T::kParts; ++u) w.id[u] = table[page_of(a, min(tile * T::kParts + u, last_block))];
+      for (int u = 0; u < T::kParts; ++u) id[u] = table[page_of(a, min(tile * T::kParts + u, last_block))];
     };
-    auto find = [&](Where& w, uint32_t tile) {
-      w.outside = 0;
+    auto find = [&](uint32_t tile) {
+      outside = 0;
 #pragma unroll
       for (int u = 0; u < T::kParts; ++u) {
-        const uint32_t block = min(tile * T::kParts + u, last_block);
-        const bool out = (unsigned)w.id[u] >= (unsigned)a.n_pages;
-        w.outside |= (uint32_t)out << u;
-        w.off[u] = ((unsigned long long)(out ? 0u : (uint32_t)w.id[u]) * stride + (block - page_of(a, block) * per_page)) *
-                   (16 * T::kRowBytes);
+        const uint32_t at = min(tile * T::kParts + u, last_block);
+        const bool out = (unsigned)id[u] >= (unsigned)a.n_pages;
+        outside |= (uint32_t)out << u;
+        block[u] = (out ? 0u : (uint32_t)id[u]) * stride + (at - page_of(a, at) * per_page);
       }
     };
-    // this thread's chunk of pass i: where it comes from, and whether it is there
-    auto source = [&](const Where& w, uint32_t tile, int i, bool& there) {
-      const int u0 = i * T::kPass / 16;
-      unsigned long long from = w.off[u0];
-      uint32_t out = w.outside >> u0 & 1u;
-      if constexpr (T::kPass > 16) {
-        if (row >= 16) {
-          from = w.off[u0 + 1];
-          out = w.outside >> (u0 + 1) & 1u;
-        }
-      }
-      const int r = row + i * T::kPass;
-      there = !out && (int)(tile * T::kBlock) + r < end;
-      return from + (uint32_t)(r & 15) * T::kRowBytes + (uint32_t)chunk * 16;
+    // pass i: rows row + i kPass of the tile, of part i kPass / 16 (rows of 64 bytes: 16 rows
+    // a pass, one part)
+    auto source = [&](int i) {
+      constexpr int kRow = T::kRowBytes;
+      return mine + (unsigned long long)block[i * kPass / 16] * (16 * kRow) + (i * kPass % 16) * kRow;
     };
-    auto masked = [&](uint32_t outside, uint32_t tile) {
-      return mixed && (outside != 0 || (int)(tile + 1) * T::kBlock > plain);
+    auto there = [&](uint32_t tile, int i) {
+      return !(outside >> (i * kPass / 16) & 1u) && (int)(tile * T::kBlock) + row + i * kPass < end;
     };
-    look_up(kw, lo);
-    look_up(vw, lo);
-    if (segments > 0 && !wait(&sh.q_empty, (segments - 1) & 1)) return;
-    queries(b, h, row0);
-    // keys run a tile ahead of values: k0 k1 v0 k2 v1 ...
-    uint32_t kt = lo, vt = lo;       // next to come
-    auto keys_next = [&] { return kt < hi && kt < vt + 2; };
+    auto masked = [&](uint32_t out, uint32_t tile) {
+      return mixed && (out != 0 || (int)(tile + 1) * T::kBlock > plain);
+    };
+    uint64_t* empty = KEYS ? sh.k_empty : sh.v_empty;
+    uint8_t (*places)[T::kTileBytes] = KEYS ? sh.k : sh.v;
+    look_up(lo);
+    if constexpr (KEYS) {
+      if (segments > 0 && !wait(&sh.q_empty, (segments - 1) & 1)) return;
+      queries(b, h, row0);
+    }
     if constexpr (T::kE4) {
-      uint4 kx[T::kCopies], vx[T::kCopies];                      // the next tile's, on their way
-      auto load = [&](Where& w, const uint8_t* from, uint32_t tile, uint4 (&x)[T::kCopies]) {
-        find(w, tile);
+      uint4 x[kCopies];                                          // the next tile's, on their way
+      auto load = [&](uint32_t tile) {
+        find(tile);
 #pragma unroll
-        for (int i = 0; i < T::kCopies; ++i) {
-          bool there;
-          const unsigned long long at = source(w, tile, i, there);
+        for (int i = 0; i < kCopies; ++i) {
           x[i] = make_uint4(0u, 0u, 0u, 0u);
-          if (there) x[i] = __ldg(reinterpret_cast<const uint4*>(from + at));
+          if (there(tile, i)) x[i] = __ldg(reinterpret_cast<const uint4*>(source(i)));
         }
-        if (tile + 1 < hi) look_up(w, tile + 1);
+        if (tile + 1 < hi) look_up(tile + 1);
       };
-      auto put = [&](uint8_t* to, const uint4 (&x)[T::kCopies]) {
+      load(lo);
+#pragma unroll 1
+      for (uint32_t tile = lo; tile < hi; ++tile, ++begun) {
+        const int st = begun % T::kStages;
+        if (begun >= T::kStages && !wait(&empty[st], (begun / T::kStages - 1) & 1)) return;
+        uint32_t any = 0;
+        if (!KEYS && masked(outside, tile)) {
 #pragma unroll
-        for (int i = 0; i < T::kCopies; ++i) {
-          const int r = row + i * T::kPass;
+          for (int i = 0; i < kCopies; ++i) any |= clear_odd<C>(x[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
           uint4 y, z;
           widen(x[i], y, z);
-          *reinterpret_cast<uint4*>(to + T::place(r, 2 * chunk, T::kBlock)) = y;
-          *reinterpret_cast<uint4*>(to + T::place(r, 2 * chunk + 1, T::kBlock)) = z;
+          *reinterpret_cast<uint4*>(places[st] + T::place(row + i * kPass, 2 * chunk, T::kBlock)) = y;
+          *reinterpret_cast<uint4*>(places[st] + T::place(row + i * kPass, 2 * chunk + 1, T::kBlock)) = z;
         }
-      };
-      load(kw, keys, lo, kx);
-      load(vw, values, lo, vx);
-      while (vt < hi) {
-        if (keys_next()) {
-          const int st = keys_begun % T::kStages;
-          if (keys_begun >= T::kStages && !wait(&sh.k_empty[st], (keys_begun / T::kStages - 1) & 1)) return;
-          put(sh.k[st], kx);
-          keys_landed(keys_begun++, kw.outside);
-          if (++kt < hi) load(kw, keys, kt, kx);
-        } else {
-          const int st = values_begun % T::kStages;
-          if (values_begun >= T::kStages && !wait(&sh.v_empty[st], (values_begun / T::kStages - 1) & 1)) return;
-          uint32_t any = 0;
-          if (masked(vw.outside, vt)) {
-#pragma unroll
-            for (int i = 0; i < T::kCopies; ++i) any |= clear_odd<C>(vx[i]);
-          }
-          put(sh.v[st], vx);
-          values_landed(values_begun++, any);
-          if (++vt < hi) load(vw, values, vt, vx);
-        }
+        landed(begun, outside, any);
+        if (tile + 1 < hi) load(tile + 1);
       }
     } else {
-      // As many copies on their way as there are places; the oldest is waited for when the
+      // As many tiles on their way as there are places; the oldest is waited for when the
       // next has none.
-      uint32_t kd = lo, vd = lo;     // the oldest that have not landed
-      uint32_t k_outside = 0, v_outside = 0;                     // of the tiles on their way, 4 bits a place
-      auto begin = [&](Where& w, uint8_t* place, const uint8_t* from, uint32_t& tile, uint32_t& outside, uint32_t& begun) {
-        find(w, tile);
-        const uint32_t to = smem_u32(place);
-#pragma unroll
-        for (int i = 0; i < T::kCopies; ++i) {
-          bool there;
-          const unsigned long long at = source(w, tile, i, there);
-          copy16(to + T::place(row + i * T::kPass, chunk, T::kBlock), from + at, there);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        const int bits = 4 * (begun % T::kStages);
-        outside = (outside & ~(15u << bits)) | w.outside << bits;
-        ++tile;
-        ++begun;
-        if (tile < hi) look_up(w, tile);
-      };
-      while (vd < hi) {
-        const bool any_left = vt < hi, is_key = keys_next();
-        bool is_free = false;
-        if (any_left) {
-          const uint32_t begun = is_key ? keys_begun : values_begun;
-          uint64_t* empty = &(is_key ? sh.k_empty : sh.v_empty)[begun % T::kStages];
+      uint32_t tile = lo, oldest = lo, outsides = 0;             // of the tiles on their way, 4 bits a place
+#pragma unroll 1
+      while (oldest < hi) {
+        const int st = begun % T::kStages;
+        bool is_free = tile < hi && tile - oldest < T::kStages;
+        if (is_free && begun >= T::kStages) {
           const uint32_t parity = (begun / T::kStages - 1) & 1;
-          is_free = begun < T::kStages || __all_sync(0xffffffffu, mbar_test_wait(empty, parity));
-          if (!is_free && kd == kt && vd == vt) {                // nothing on its way
-            if (!wait(empty, parity)) return;
+          is_free = __all_sync(0xffffffffu, mbar_test_wait(&empty[st], parity));
+          if (!is_free && tile == oldest) {                      // nothing on its way
+            if (!wait(&empty[st], parity)) return;
             is_free = true;
           }
         }
         if (is_free) {
-          if (is_key) begin(kw, sh.k[keys_begun % T::kStages], keys, kt, k_outside, keys_begun);
-          else begin(vw, sh.v[values_begun % T::kStages], values, vt, v_outside, values_begun);
+          find(tile);
+          const uint32_t to = smem_u32(places[st]);
+          const bool all = outside == 0 && (int)(tile + 1) * T::kBlock <= end;
+#pragma unroll
+          for (int i = 0; i < kCopies; ++i)
+            copy16(to + T::place(row + i * kPass, chunk, T::kBlock), source(i), all || there(tile, i));
+          asm volatile("cp.async.commit_group;" ::: "memory");
+          outsides = (outsides & ~(15u << 4 * st)) | outside << 4 * st;
+          ++tile;
+          ++begun;
+          if (tile < hi) look_up(tile);
           continue;
         }
-        // copies land in the order in which they were begun: keys first while as many values
-        // as two tiles before are in
-        const uint32_t on_way = (kt - kd) + (vt - vd);
-        if (on_way == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
-        else if (on_way == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
-        else if (on_way == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        if (tile - oldest == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
-        if (kd < kt && kd < vd + 2) {
-          const uint32_t tile = keys_begun - (kt - kd);
-          keys_landed(tile, k_outside >> 4 * (tile % T::kStages) & 15u);
-          ++kd;
-        } else {
-          const uint32_t tile = values_begun - (vt - vd);
-          const int st = tile % T::kStages;
-          uint32_t any = 0;
-          if (masked(v_outside >> 4 * st & 15u, vd)) {
+        const uint32_t done = begun - (tile - oldest), out = outsides >> 4 * (done % T::kStages) & 15u;
+        uint32_t any = 0;
+        if (!KEYS && masked(out, oldest)) {
 #pragma unroll 1
-            for (int i = 0; i < T::kCopies; ++i) {
-              uint4* p = reinterpret_cast<uint4*>(sh.v[st] + T::place(row + i * T::kPass, chunk, T::kBlock));
-              uint4 x = *p;
-              const uint32_t here = clear_odd<C>(x);
-              if (here != 0) *p = x;
-              any |= here;
-            }
+          for (int i = 0; i < kCopies; ++i) {
+            uint4* p = reinterpret_cast<uint4*>(places[done % T::kStages] + T::place(row + i * kPass, chunk, T::kBlock));
+            uint4 x = *p;
+            const uint32_t here = clear_odd<C>(x);
+            if (here != 0) *p = x;
+            any |= here;
           }
-          values_landed(tile, any);
-          ++vd;
         }
+        landed(done, out, any);
+        ++oldest;
       }
     }
     ++segments;
   }
   // A tile is in its place: seen by the tensor cores after the fence, by all with the arrival.
-  __device__ __forceinline__ void keys_landed(uint32_t tile, uint32_t outside) {
-    if (tid == 0) sh.outside[tile & 3] = outside;
-    fence_async();
-    __syncwarp();
-    if ((tid & 31) == 0) arrive(&sh.k_full[tile % T::kStages]);
-  }
-  __device__ __forceinline__ void values_landed(uint32_t tile, uint32_t any) {
+  __device__ __forceinline__ void landed(uint32_t tile, uint32_t outside, uint32_t any) {
+    if (KEYS && tid == 0) sh.outside[tile & 3] = outside;
     if (any != 0) sh.odd[segments & 3] = 1;
     fence_async();
     __syncwarp();
-    if ((tid & 31) == 0) arrive(&sh.v_full[tile % T::kStages]);
+    if ((tid & 31) == 0) arrive(&(KEYS ? sh.k_full : sh.v_full)[tile % T::kStages]);
   }
 };
 
@@ -529,23 +492,30 @@ template <class C, int D> struct Softmax {
     if (works) {
       const long long at = ((long long)b * a.nodes + node) * a.heads + head;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + at * D;
+      const bool sectors = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
 #pragma unroll 1
       for (int d = 0; d < D; d += 32) {
         float x[32];
         tmem_ld32(tmem + d, x);
         if (there) {
           if (whole) {
+            uint32_t y[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) y[i] = bits_of(__floats2bfloat162_rn(x[2 * i] * k, x[2 * i + 1] * k));
+            if (sectors) {
+#pragma unroll
+              for (int i = 0; i < 16; i += 8)
+                store32(out + d + 2 * i, y[i], y[i + 1], y[i + 2], y[i + 3], y[i + 4], y[i + 5], y[i + 6], y[i + 7]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<uint4*>(out + d + 2 * i) = make_uint4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+            }
+          } else {
+            const uint32_t* y = reinterpret_cast<const uint32_t*>(x);
 #pragma unroll
             for (int i = 0; i < 32; i += 8)
-              *reinterpret_cast<uint4*>(out + d + i) =
-                  make_uint4(bits_of(__floats2bfloat162_rn(x[i] * k, x[i + 1] * k)),
-                             bits_of(__floats2bfloat162_rn(x[i + 2] * k, x[i + 3] * k)),
-                             bits_of(__floats2bfloat162_rn(x[i + 4] * k, x[i + 5] * k)),
-                             bits_of(__floats2bfloat162_rn(x[i + 6] * k, x[i + 7] * k)));
-          } else {
-#pragma unroll
-            for (int i = 0; i < 32; i += 4)
-              *reinterpret_cast<float4*>(slot + r * D + d + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+              store32(slot + r * D + d + i, y[i], y[i + 1], y[i + 2], y[i + 3], y[i + 4], y[i + 5], y[i + 6], y[i + 7]);
           }
         }
         __syncwarp();
@@ -575,9 +545,9 @@ __global__ void __launch_bounds__(kTreeThreads, 2) paged_tree_kernel(const __gri
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     for (int i = 0; i < T::kStages; ++i) {
-      mbar_init(&sh.k_full[i], 4);
+      mbar_init(&sh.k_full[i], 2);
       mbar_init(&sh.k_empty[i], 1);
-      mbar_init(&sh.v_full[i], 4);
+      mbar_init(&sh.v_full[i], 2);
       mbar_init(&sh.v_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -609,10 +579,13 @@ __global__ void __launch_bounds__(kTreeThreads, 2) paged_tree_kernel(const __gri
       w.segment(b, h, row0, lo, hi, whole, slot);
     });
   } else if (warp < 8) {
-    Copier<C, D> w{a, sh, (int)threadIdx.x - 128};
-    each_segment<T>(a, run, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool, float*) {
-      w.segment(b, h, row0, lo, hi);
-    });
+    auto copy = [&](auto w) {
+      each_segment<T>(a, run, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool, float*) {
+        w.segment(b, h, row0, lo, hi);
+      });
+    };
+    if (warp < 6) copy(Copier<C, D, true>{a, sh, (int)threadIdx.x - 128});
+    else copy(Copier<C, D, false>{a, sh, (int)threadIdx.x - 192});
     if constexpr (!T::kE4) asm volatile("cp.async.wait_all;" ::: "memory");
   } else {
     Issuer<C, D> w{a, sh, tmem};
