@@ -81,6 +81,11 @@ template <class C, int D> struct Tree {
   static constexpr uint32_t kIdescO = kIdesc | ((uint32_t)(D >> 3) << 17) | (1u << 16);
   static constexpr uint32_t kColS = 128;                         // two places of 64 columns behind O
 
+  // A wait by parity tells of a phase only while its barrier is neither a phase behind it nor
+  // ahead.  Every barrier serves every second tile (q_empty: every segment), and the wait for
+  // a tile comes when the one two tiles before is known to have ended and the one two tiles
+  // behind cannot have: tile c's S is formed when O has tile c - 2, O gets tile c when the
+  // softmax has given its P, and the products end in the order in which they are issued.
   struct Shared {
     uint8_t q[kHalves * kRows * 128];
     uint8_t k[kStages][kTileBytes], v[kStages][kTileBytes];
@@ -90,7 +95,7 @@ template <class C, int D> struct Tree {
     int odd[4];
     uint32_t outside[4];             // of the last tiles: parts whose page is not in the pool, as bits
     uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
-    uint64_t q_empty, s_full[2], p_full[2], o_done, drain;
+    uint64_t q_empty, s_full[2], p_full[2], o_done[2], drain;
     uint32_t tmem;
     int abort;
     uint32_t scratch[kTreeThreads / 32];
@@ -325,12 +330,11 @@ template <class C, int D> struct Issuer {
   __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
     return go = warp_wait(bar, parity, &sh.abort, a.wait_ns);
   }
-  __device__ __forceinline__ void form(bool first, bool last) {
+  __device__ __forceinline__ void form(bool last) {
     const int st = formed % T::kStages, buf = formed & 1;
     if (!wait(&sh.k_full[st], formed / T::kStages & 1)) return;
-    // the place of S held P of two tiles before; at a segment's start the products of the
-    // last tile too have been issued, and the barrier's parity tells only of the last
-    if (first ? formed >= 1 && !wait(&sh.o_done, (formed - 1) & 1) : formed >= 2 && !wait(&sh.o_done, formed & 1)) return;
+    // the place of S held P of two tiles before
+    if (formed >= 2 && !wait(&sh.o_done[buf], (formed - 2) / 2 & 1)) return;
     tc_fence_after();
     if (elect_one()) {
       const uint64_t q = sw128_desc(smem_u32(sh.q)), k = sw128_desc(smem_u32(sh.k[st]));
@@ -361,15 +365,15 @@ template <class C, int D> struct Issuer {
           umma_ts(tmem, p + part * 32 + i * 8, v + (uint64_t)(i * (16 * 128 >> 4)), T::kIdescO,
                   !first || part > 0 || i > 0);
       umma_commit(&sh.v_empty[st]);
-      umma_commit(&sh.o_done);
+      umma_commit(&sh.o_done[buf]);
     }
     __syncwarp();
     ++added;
   }
   __device__ __forceinline__ void segment(uint32_t lo, uint32_t hi) {
-    if (go) form(true, lo + 1 == hi);
+    if (go) form(lo + 1 == hi);
     for (uint32_t tile = lo; go && tile < hi; ++tile) {
-      if (tile + 1 < hi) form(false, tile + 2 == hi);
+      if (tile + 1 < hi) form(tile + 2 == hi);
       if (go) add(tile == lo);
     }
   }
@@ -440,7 +444,7 @@ template <class C, int D> struct Softmax {
         if (grows) m = top;
         l *= c;
         if (tile > lo && __any_sync(0xffffffffu, grows)) {       // O of the tiles before, rescaled
-          if (!wait(&sh.o_done, (tiles - 1) & 1)) break;
+          if (!wait(&sh.o_done[(tiles - 1) & 1], (tiles - 1) / 2 & 1)) break;
           tc_fence_after();
 #pragma unroll 1
           for (int d = 0; d < D; d += 8) {
@@ -481,7 +485,7 @@ template <class C, int D> struct Softmax {
       __syncwarp();
       if (lane == 0) arrive(&sh.p_full[buf]);
     }
-    if (go) wait(&sh.o_done, (tiles - 1) & 1);
+    if (go) wait(&sh.o_done[(tiles - 1) & 1], (tiles - 1) / 2 & 1);
     tc_fence_after();
     const bool there = row < rows, poison = !go || long_one;
     const bool odd = *static_cast<volatile int*>(&sh.odd[segments & 3]) != 0;
@@ -553,9 +557,9 @@ __global__ void __launch_bounds__(kTreeThreads, 2) paged_tree_kernel(const __gri
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.s_full[i], 1);
       mbar_init(&sh.p_full[i], 4);
+      mbar_init(&sh.o_done[i], 1);
     }
     mbar_init(&sh.q_empty, 1);
-    mbar_init(&sh.o_done, 1);
     mbar_init(&sh.drain, 1);
     for (int i = 0; i < 4; ++i) sh.odd[i] = 0;
     sh.abort = 0;

@@ -333,6 +333,24 @@ def test_attention(fovea, cache, case):
             check_attention(fovea, q, k, v, table, ints(lens), tree_bits(g, batch, nodes, True), scales=scales)
 
 
+@pytest.mark.parametrize("cache", [BF16, E4M3])
+@pytest.mark.parametrize("lens,nodes,heads,kv,dim", [
+    ([2912, 1531, 805, 423, 222, 117, 61, 32], 32, 28, 4, 128), ([64, 65, 333], 64, 28, 4, 128), ([700], 64, 32, 32, 128),
+    ([600] * 16, 64, 40, 40, 128), ([900, 30, 64, 1500], 12, 16, 2, 64), ([1000, 900], 7, 8, 2, 256)])
+def test_attention_repeats(fovea, cache, lens, nodes, heads, kv, dim):
+    """Trees through every kernel of many rows give the same bits in every run, with the
+    machine to themselves and behind other work."""
+    g = gen(17)
+    k, v, table, scales = make_cache(g, cache, lens, kv, dim, 16)
+    q = (2 * normal(g, len(lens) * nodes, heads, dim)).to(BF16)
+    tree = tree_bits(g, len(lens), nodes)
+    want = check_attention(fovea, q, k, v, table, ints(lens), tree, scales=scales)
+    for _ in range(5):
+        got = [fovea.paged_attention(q, k, v, table, ints(lens), tree=tree, want_lse=True, **scales) for _ in range(20)]
+        torch.cuda.synchronize()
+        assert all(same(r["out"], want["out"]) and same(r["lse"], want["lse"]) for r in got)
+
+
 @pytest.mark.parametrize("cache", [BF16, E4M3, FP32])
 def test_attention_long(fovea, cache):
     g = gen(9)
