@@ -518,7 +518,7 @@ FOVEA_API fovea_status fovea_token_logprobs_grad(const void* logits, int64_t ld,
  * from that of the outputs.
  *   q [N, heads, dim], k [N, kv_heads, dim] dtype (FOVEA_BF16 or FOVEA_FP32; k NULL
  *               and kv_heads 0: q alone)
- *   positions   [axes, N] int32 (row stride pos_ld), any value
+ *   positions   [axes, N] int32 (row stride pos_ld; 0: one row for all axes), any value
  *   frequencies [rot / 2] fp64, radians per position; axis [rot / 2] int32, or NULL
  *               (axis 0).  A frequency that is not finite, or an axis outside
  *               [0, axes), gives NaN.

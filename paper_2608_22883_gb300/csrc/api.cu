@@ -1525,8 +1525,8 @@ static fovea_status check_rotary(int N, int dim, const int32_t* positions, long 
     return fail(FOVEA_ERR_INVALID_ARG, "rot %d must be even and in [2, dim = %d]", rot, dim);
   if (axes < 1) return fail(FOVEA_ERR_INVALID_ARG, "axes = %d < 1", axes);
   if (axes > FOVEA_MAX_AXES) return fail(FOVEA_ERR_UNSUPPORTED, "axes %d > %d", axes, FOVEA_MAX_AXES);
-  if (axes > 1 && pos_ld < N)
-    return fail(FOVEA_ERR_INVALID_ARG, "row stride %lld of positions is below N = %d", pos_ld, N);
+  if (axes > 1 && pos_ld < 0)
+    return fail(FOVEA_ERR_INVALID_ARG, "row stride %lld of positions must not be negative", pos_ld);
   if (N > 0) {
     NEED_ALIGNED(positions, 4, "positions");
     NEED_ALIGNED(frequencies, 8, "frequencies");

@@ -65,7 +65,7 @@ CACHE = [(dict(cache=3), BAD), (dict(dim=96), NO), (dict(dim=0), NO), (dict(page
     (rotary, dict(dtype=E4M3), BAD), (rotary, dict(N=-1), BAD), (rotary, dict(dim=1), BAD), (rotary, dict(dim=513), NO),
     (rotary, dict(heads=0), BAD), (rotary, dict(kv=-1), BAD), (rotary, dict(heads=1024), NO), (rotary, dict(rot=0), BAD),
     (rotary, dict(rot=7), BAD), (rotary, dict(rot=130), BAD), (rotary, dict(axes=0), BAD), (rotary, dict(axes=9), NO),
-    (rotary, dict(pos_ld=3), BAD), (rotary, dict(pos=None), BAD), (rotary, dict(f=None), BAD), (rotary, dict(f=P + 4), BAD),
+    (rotary, dict(pos_ld=-1), BAD), (rotary, dict(pos=None), BAD), (rotary, dict(f=None), BAD), (rotary, dict(f=P + 4), BAD),
     (rotary, dict(axis=P + 1), BAD), (rotary, dict(q=None), BAD), (rotary, dict(k=None), BAD), (rotary, dict(q=P + 1), BAD),
     (rotary, dict(q_out=None), BAD), (rotary, dict(k_out=None), BAD), (rotary, dict(q_ld=-1), BAD),
     (rotary, dict(q_out=P, q_ld=640), BAD), (rotary, dict(k_out=P, k_ld=129), BAD),

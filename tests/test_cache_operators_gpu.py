@@ -131,6 +131,7 @@ def test_rotary_strides(fovea, dtype):
     wide = torch.zeros(3, 64, **I32)
     wide[:, :40] = positions
     check_rotary(fovea, heads[:, :28], None, wide[:, :40], f, axis)
+    check_rotary(fovea, heads[:, :28], None, positions[:1].expand(3, 40), f, axis)       # one position for all axes
 
 
 def test_rotary_far_positions(fovea):
@@ -699,6 +700,32 @@ def test_fork_many(fovea):
 # ---------------------------------------------------------------------------
 # Together, and as programs call them
 # ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("cache,n_pages", [(BF16, 36000), (E4M3, 70000), (FP32, 18000)])
+def test_offsets_beyond_32_bits(fovea, cache, n_pages):
+    """Pools of more than 2^32 bytes (of 8 bits: elements), entries in their last pages."""
+    g = gen(18)
+    kv, page, dim, dt = 8, 64, 128, FP32 if cache is FP32 else BF16
+    assert n_pages * kv * page * dim * torch.empty(0, dtype=cache).element_size() > 1 << 32
+    k_pages, v_pages = (torch.empty(n_pages, kv, page, dim, dtype=cache, device="cuda") for _ in range(2))
+    scales = dict(k_scale=torch.full((kv,), 0.02, device="cuda"), v_scale=torch.full((kv,), 0.01, device="cuda")) \
+        if cache is E4M3 else {}
+    table = ints([[n_pages - 1, n_pages - 3, n_pages - 5], [n_pages - 2, 1, n_pages - 4]])
+    lens, nodes = [170, 129], 20
+    sequence = torch.cat([torch.full((n,), b, **I32) for b, n in enumerate(lens)])
+    entry = torch.cat([torch.arange(n, **I32) for n in lens])
+    x = normal(g, sum(lens), 2 * kv, dim).to(dt)
+    fovea.cache_append(x[:, :kv], x[:, kv:], k_pages, v_pages, table, sequence, entry, **scales)
+    for heads in (16, 40):                          # few rows a key head, and many
+        q = normal(g, 2 * nodes, heads, dim).to(dt)
+        check_attention(fovea, q, k_pages, v_pages, table, ints(lens), scales=scales)
+    rows = entries(v_pages, table, 0, 170).clone()
+    held = fovea.cache_keep(k_pages, v_pages, table, ints(lens), ints([[3, 19], [0, -1]]), nodes)
+    assert held.tolist() == [152, 110]
+    assert same(entries(v_pages, table, 0, 152)[150:], rows[[153, 169]])
+    r = fovea.cache_fork(k_pages, v_pages, table, held, ints([0, 0]), None, ints([0, 0]))
+    assert r["table"].tolist() == [[n_pages - 1, n_pages - 3, n_pages - 5], [n_pages - 1, n_pages - 3, 0]]
+    assert same(entries(k_pages, r["table"], 1, 152), entries(k_pages, table, 0, 152))
 
 @pytest.mark.parametrize("cache", [BF16, E4M3, FP32])
 def test_a_draft_round(fovea, cache):
