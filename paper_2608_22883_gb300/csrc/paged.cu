@@ -610,6 +610,8 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_attention_
   });
 }
 
+constexpr int kMostCtas = 8;
+
 // Small tables: a cluster of CTAs a segment, each an equal share of its blocks, which join
 // their sums through distributed shared memory: one launch, no partial sums in memory.
 template <class C, class Q, int D, int RT>
@@ -618,7 +620,8 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_cluster_ke
   using A = Attention<C, Q, D, RT>;
   extern __shared__ __align__(16) uint8_t raw[];
   typename A::Shared& sh = *reinterpret_cast<typename A::Shared*>(raw);
-  __shared__ float top[A::kRows], sum[A::kRows];
+  // a CTA's maxima and sums of its rows, whether it has met odd values; of all CTAs
+  __shared__ float mine_of[2 * A::kRows + 1], all[kMostCtas][2 * A::kRows + 1];
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x, rank = (int)blockIdx.x % ctas, seg = (int)blockIdx.x / ctas;
@@ -641,35 +644,54 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_cluster_ke
     const float4 x = A::warps_sum(sh, r, d, m, l);
     *reinterpret_cast<float4*>(&sh.o[0][r][d]) = x;
     if (d == 0) {
-      top[r] = m;
-      sum[r] = l;
+      mine_of[r] = m;
+      mine_of[A::kRows + r] = l;
     }
   }
+  if (tid == 0) mine_of[2 * A::kRows] = sh.odd ? 1.0f : 0.0f;
   tc::cluster_sync();
+  // every value of the others is asked for at once: a load through the cluster takes as long
+  // as a pass over the rows
   const float v_scale = A::kE4 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
-  const uint32_t tops = tc::smem_u32(top), sums = tc::smem_u32(sum), mine = tc::smem_u32(&sh.o[0][0][0]);
-#pragma unroll 1
-  for (int i = tid * ctas + rank; i < rows * (D / 4); i += kThreads * ctas) {
+  const uint32_t theirs = tc::smem_u32(mine_of), sums_at = tc::smem_u32(&sh.o[0][0][0]);
+  const int i0 = tid * ctas + rank, most = rows * (D / 4);
+  float4 y[kMostCtas];
+  auto fetch = [&](int i) {
     const int r = i / (D / 4), d = (i % (D / 4)) * 4;
+#pragma unroll
+    for (int q = 0; q < kMostCtas; ++q)
+      if (q < ctas) y[q] = tc::ld_dsmem_f4(tc::map_dsmem(sums_at + (r * (D + 4) + d) * 4, q));
+  };
+  if (i0 < most) fetch(i0);
+#pragma unroll 1
+  for (int i = tid; i < ctas * (2 * A::kRows + 1); i += kThreads) {
+    const int q = i / (2 * A::kRows + 1), e = i - q * (2 * A::kRows + 1);
+    all[q][e] = dsmem_f32(theirs + 4 * e, q);
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int i = i0; i < most; i += kThreads * ctas) {
+    const int r = i / (D / 4), d = (i % (D / 4)) * 4;
+    if (i != i0) fetch(i);
     float m = -INFINITY, l = 0.0f;
     float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 1
-    for (int q = 0; q < ctas; ++q) m = fmaxf(m, dsmem_f32(tops + 4 * r, q));
-#pragma unroll 2
-    for (int q = 0; q < ctas; ++q) {
-      const float mq = dsmem_f32(tops + 4 * r, q), c = mq == m ? 1.0f : exp2_(mq - m);
-      const float4 y = tc::ld_dsmem_f4(tc::map_dsmem(mine + (r * (D + 4) + d) * 4, q));
-      l += c * dsmem_f32(sums + 4 * r, q);
-      x.x += c * y.x; x.y += c * y.y; x.z += c * y.z; x.w += c * y.w;
-    }
+#pragma unroll
+    for (int q = 0; q < kMostCtas; ++q)
+      if (q < ctas) m = fmaxf(m, all[q][r]);
+#pragma unroll
+    for (int q = 0; q < kMostCtas; ++q)
+      if (q < ctas) {
+        const float mq = all[q][r], c = mq == m ? 1.0f : exp2_(mq - m);
+        l += c * all[q][A::kRows + r];
+        x.x += c * y[q].x; x.y += c * y[q].y; x.z += c * y[q].z; x.w += c * y[q].w;
+      }
     if (too_long(a, b)) l = NAN;
     const int row = row0 + r, node = row / a.group;
     write_row<Q>(a, (long long)b * a.nodes + node, h * a.group + row - node * a.group, d, D, x, m, l, v_scale, A::kLift);
   }
   bool odd = false;                  // of any of the cluster's CTAs: the first adds them
-  if (rank == 0)
 #pragma unroll 1
-    for (int q = 0; q < ctas; ++q) odd |= __float_as_uint(dsmem_f32(tc::smem_u32(&sh.odd), q)) != 0;
+  for (int q = 0; rank == 0 && q < ctas; ++q) odd |= all[q][2 * A::kRows] != 0.0f;
   tc::cluster_sync();
   if (odd) add_odd_values<C, Q, D>(a, b, h, row0, rows, n, 0, n, nullptr, tid, kThreads);
 }
@@ -689,7 +711,7 @@ template <class C, int D> constexpr int most_tiles() {
 template <class A> int cluster_ctas(const PagedArgs& a) {
   const long long segments = (long long)a.B * a.kv_heads * ((a.nodes * a.group + A::kRows - 1) / A::kRows);
   int ctas = 1;
-  while (ctas < 8 && segments * ctas < 2 * 152) ctas *= 2;
+  while (ctas < kMostCtas && segments * ctas < 2 * 152) ctas *= 2;
   const long long steps = ((long long)a.width * a.page + A::kBlock * kWarps * ctas - 1) / (A::kBlock * kWarps * ctas);
   return segments <= 2 * 152 && steps <= (a.B == 1 ? 16 : 4) ? ctas : 0;
 }
