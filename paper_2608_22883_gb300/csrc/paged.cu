@@ -67,6 +67,11 @@ template <class C, int D> struct Cut {
 // Blocks that a warp takes together.
 template <class C, int D, int RT> constexpr int kTogether = sizeof(C) * D * RT <= 128 ? 2 : 1;
 
+// Whether a step's pages are asked for a step ahead: with 8-bit entries (four sequences of
+// 131072: 168 us without, 162 with) and dims of 256 (49.7 and 46.2); it costs the others (one
+// sequence of 4096 10.3 and 11.5, fp32 33 and 39).
+template <class C, int D> constexpr bool kAsks = sizeof(C) == 1 || (sizeof(C) == 2 && D == 256);
+
 template <class C, class Q, int D, int RT>
 struct Attention {
   using G = Cut<C, D>;
@@ -88,6 +93,7 @@ struct Attention {
   };
 
   static constexpr int kSub = kTogether<C, D, RT>;
+  static constexpr bool kAsk = kAsks<C, D>;
   // The keys and values of kSub blocks as a lane holds them.
   uint4 k[kSub][2][G::kKeyChunks];
   uint32_t v[kSub][4][G::kParts][G::kSpanWords];
@@ -387,47 +393,78 @@ struct Attention {
     clear();
     uint32_t at = lo + warp * kSub;
     if (at >= hi) return;
+    // Pages are looked up a step ahead; with kAsk two, and the next step's keys and values are
+    // asked for from memory, into L2, a step before their loads: registers hold one step's alone.
     int id[kSub];
     uint32_t in_page[kSub];
     auto look_up = [&](uint32_t first) {
 #pragma unroll
       for (int u = 0; u < kSub; ++u) {
-        const uint32_t block = u == 0 ? first : min(first + u, hi - 1), p = page_of(a, block);
+        const uint32_t block = min(first + u, hi - 1), p = page_of(a, block);
         id[u] = table[p];
         in_page[u] = block - p * per_page;
       }
     };
-    unsigned long long off[kSub];                          // bytes from the pools' lane pointers
-    bool bad = false;                                      // a page is not in the pool
+    unsigned long long off[kSub], next_off[kSub];          // bytes from the pools' lane pointers
+    bool bad = false, next_bad = false;                    // a page is not in the pool
     auto place = [&]() {
-      bad = false;
+      next_bad = false;
 #pragma unroll
       for (int u = 0; u < kSub; ++u) {
         const bool out = (unsigned)id[u] >= (unsigned)a.n_pages;
-        bad |= out;
-        off[u] = ((unsigned long long)(out ? 0u : (uint32_t)id[u]) * stride + in_page[u]) * kBytes;
+        next_bad |= out;
+        next_off[u] = ((unsigned long long)(out ? 0u : (uint32_t)id[u]) * stride + in_page[u]) * kBytes;
       }
+    };
+    auto ask = [&]() {
+      constexpr uint32_t kLines = kBytes / 128;
+#pragma unroll
+      for (int u = 0; u < kSub; ++u)
+#pragma unroll
+        for (uint32_t i = 0; i < kLines; i += 32)
+          if (kLines >= 32 || lane < (int)kLines) {
+            const size_t line = next_off[u] + (i + lane) * 128;
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(keys - keys_from() + line));
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(values - values_from() + line));
+          }
     };
     look_up(at);
     place();
 #pragma unroll
-    for (int u = 0; u < kSub; ++u) load_keys(u, keys + off[u]);
+    for (int u = 0; u < kSub; ++u) {
+      off[u] = next_off[u];
+      load_keys(u, keys + off[u]);
+    }
+    bad = next_bad;
+    if (kAsk && at + kWarps * kSub < hi) look_up(at + kWarps * kSub);
     const int end = min(n, (int)(hi * kBlock));            // the run's last entry
     const int plain = min(end, plain_end(a, n));
     while (true) {
 #pragma unroll
       for (int u = 0; u < kSub; ++u) load_values(u, values + off[u]);
-      const uint32_t next = at + kWarps * kSub;
+      const uint32_t next = at + kWarps * kSub, after = next + kWarps * kSub;
       const bool more = next < hi;
-      if (more) look_up(next);
+      if (more) {
+        if constexpr (kAsk) {
+          place();
+          ask();
+          if (after < hi) look_up(after);
+        } else {
+          look_up(next);
+        }
+      }
       float s[kSub][RT][4];
 #pragma unroll
       for (int u = 0; u < kSub; ++u) scores(u, sh, s[u]);
       const bool was_bad = bad;
       if (more) {
-        place();
+        if constexpr (!kAsk) place();
+        bad = next_bad;
 #pragma unroll
-        for (int u = 0; u < kSub; ++u) load_keys(u, keys + off[u]);
+        for (int u = 0; u < kSub; ++u) {
+          off[u] = next_off[u];
+          load_keys(u, keys + off[u]);
+        }
       }
       const int first = (int)at * kBlock;
 #pragma unroll
@@ -708,12 +745,12 @@ template <class C, int D> constexpr int most_tiles() {
 // sequence of 640 entries, 32 heads: 9.0 us and one launch (7.4 us on the host), 8.8 and
 // two (9.7) in runs; 4096 entries, 8 key heads: 12.2 and 15.3.  16 sequences of 1 to 4096
 // entries: 25 and 17; 8 of 2048, 32 key heads: 55 and 44.
-template <class A> int cluster_ctas(const PagedArgs& a) {
+template <class A> int cluster_ctas(const PagedArgs& a, int resident) {
   const long long segments = (long long)a.B * a.kv_heads * ((a.nodes * a.group + A::kRows - 1) / A::kRows);
   int ctas = 1;
-  while (ctas < kMostCtas && segments * ctas < 2 * 152) ctas *= 2;
+  while (ctas < kMostCtas && segments * ctas * 2 <= 152 * resident) ctas *= 2;
   const long long steps = ((long long)a.width * a.page + A::kBlock * kWarps * ctas - 1) / (A::kBlock * kWarps * ctas);
-  return segments <= 2 * 152 && steps <= (a.B == 1 ? 16 : 4) ? ctas : 0;
+  return segments <= 152 * resident && steps <= (a.B == 1 ? 16 : 4) ? ctas : 0;
 }
 
 template <class C, class Q, int D, int RT>
@@ -744,7 +781,7 @@ cudaError_t launch_as(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
   using A = Attention<C, Q, D, RT>;
   static std::atomic<unsigned long long> raised{0};
   if (workspace == nullptr) {
-    const int ctas = cluster_ctas<A>(a);
+    const int ctas = cluster_ctas<A>(a, per_sm<C, D, RT>());
     if (ctas > 0) return launch_cluster<C, Q, D, RT>(a, ctas, s);
   }
   return launch_runs<A, C, Q, D>(a, paged_attention_kernel<C, Q, D, RT>, kThreads, sizeof(typename A::Shared),
