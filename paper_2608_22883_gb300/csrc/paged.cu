@@ -733,8 +733,13 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_cluster_ke
   if (odd) add_odd_values<C, Q, D>(a, b, h, row0, rows, n, 0, n, nullptr, tid, kThreads);
 }
 
-// More rows than these go to the kernel of many rows.
-constexpr int kManyRows = 16, kTreeRows = 32;
+// More rows of a key head than kManyRows go to the kernels of many rows: that on tcgen05
+// where the dims and the types allow it, 8-bit entries, which it has to widen on the way,
+// only from more than kWideRows rows on.  us, here / mma.sync on staged tiles / tcgen05:
+// bf16, 8 trees of 14 rows 12.7 / 23.5 / 17.7, of 28 rows 24.7 on the second and 19.4 on the
+// third, of 32 rows and 32 key heads 46.4 and 39.5; e4m3, 24 rows 35.9 and 47.5, 64 rows 103
+// and 105.
+constexpr int kManyRows = 16, kWideRows = 64;
 // Rows that a warp takes together, by 8: as many as there are, up to what its registers hold.
 template <class C, int D> constexpr int most_tiles() {
   return sizeof(C) == 4 || D == 256 ? 1 : D == 128 ? 2 : 4;
@@ -791,7 +796,7 @@ cudaError_t launch_as(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
 template <class C, class Q, int D>
 cudaError_t launch_dim(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
   const int rows = a.nodes * a.group;
-  if (sizeof(C) < 4 && D < 256 && rows > kTreeRows) return launch_paged_tree(a, s, workspace);
+  if (sizeof(C) < 4 && D < 256 && rows > (sizeof(C) == 2 ? kManyRows : kWideRows)) return launch_paged_tree(a, s, workspace);
   if (sizeof(C) < 4 && rows > kManyRows) return launch_paged_rows(a, s, workspace);
   if constexpr (most_tiles<C, D>() >= 4)
     if (rows > 16) return launch_as<C, Q, D, 4>(a, s, workspace);
