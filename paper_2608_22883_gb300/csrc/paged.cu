@@ -13,6 +13,12 @@
 // fragments as they come (a lane of the quad takes every fourth chunk of a row), and
 // those of values become fragments of V^T by pairing two entries' halves (one prmt a
 // register).  P goes from S^T's layout to the other operand's by movmatrix.
+//
+// Measured: four sequences of 98304 to 131072 e4m3 entries, 32 heads over 8 of keys of 128:
+// 156 us, 6.0 TB/s; 64 of 1536 to 2048 bf16 entries, 28 over 4: 46 us, 5.1 TB/s; 64 of 0 to
+// 8192, pages of 16: 31 us, 4.0 TB/s (the loads' latency: 12 warps an SM hold 96 KB on their
+// way; more warps, or more blocks a warp, cost registers that spill); one of 640 entries, 32
+// heads: 7.4 us, latency throughout.
 #include <atomic>
 #include <cstddef>
 
@@ -78,6 +84,8 @@ struct Attention {
   static constexpr bool kF32 = sizeof(C) == 4, kE4 = sizeof(C) == 1;
   static constexpr bool kWaits = false;
   static constexpr int kRows = 8 * RT, kBlock = 16, kLeast = kWarps;
+  // 64 sequences of 0 to 8192 entries with 0 / 8 / 16 / 24 blocks in front of a segment: 85 /
+  // 36 / 31 / 32 us
   static constexpr uint32_t kFront = RT == 1 ? 16 : 24;
   static constexpr int kSlot = kRows * (D + 2);                  // floats of a partial segment
   static constexpr uint32_t kBytes = kBlock * D * sizeof(C);     // of a block

@@ -14,7 +14,8 @@ constexpr int kKeepThreads = 128, kKeepBytes = 48 * 1024;
 // Entry base + i <- entry base + nodes[i], base = lens - size: all sources are read, into
 // shared memory, before an entry is written, so that any list of nodes is right.  A CTA
 // takes `cols` 16-byte columns of a head of a sequence's keys or values.  Bound by latency:
-// a path's entries are a few KB a head, behind the loads of a length and of a page.
+// a path's entries are a few KB a head, behind the loads of a length and of a page.  With
+// the storing of the tree in front: one sequence 6.7 us, 16 of 40 heads 13 (floor 6.4).
 __global__ void __launch_bounds__(kKeepThreads) cache_keep_kernel(const __grid_constant__ CachePages c,
                                                                   const int32_t* lens, const int32_t* nodes, int path,
                                                                   int size, int cols, int row_vecs, int32_t* new_lens) {
@@ -122,8 +123,10 @@ __device__ __forceinline__ uint32_t slot_of(int page, int slots) { return ((uint
 
 // Which pages are held, which last pages stay, and the fresh pages of every continuation,
 // the lowest free pages first.  One CTA, bound by latency: the marks are a bit a page in
-// shared memory, and the steps depend on one another.  Writes the fresh entries of the new
-// table, the entry of each partly filled page and the number of pages left; the rest is the
+// shared memory, and the steps depend on one another.  With the copies: one sequence as six
+// 7.2 us, 128 sequences of up to 8192 entries 10.2 (15.8 with the children's lengths worked
+// out in each step, last pages compared in pairs and nothing read ahead).  Writes the fresh
+// entries of the new table, the entry of each partly filled page and the number of pages left; the rest is the
 // copies' kernel's.
 __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const __grid_constant__ CachePages c,
                                                                  const __grid_constant__ ForkArgs f) {
