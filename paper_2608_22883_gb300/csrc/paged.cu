@@ -84,7 +84,7 @@ struct Attention {
   static constexpr bool kF32 = sizeof(C) == 4, kE4 = sizeof(C) == 1;
   static constexpr bool kWaits = false;
   static constexpr int kRows = 8 * RT, kBlock = 16, kLeast = kWarps;
-  // 64 sequences of 0 to 8192 entries with 0 / 8 / 16 / 24 blocks in front of a segment: 85 /
+  // 64 sequences of 0 to 8192 entries with 0 / 8 / 16 / 24 blocks in front of a segment: 83 /
   // 36 / 31 / 32 us
   static constexpr uint32_t kFront = RT == 1 ? 16 : 24;
   static constexpr int kSlot = kRows * (D + 2);                  // floats of a partial segment

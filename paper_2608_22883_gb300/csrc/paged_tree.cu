@@ -12,11 +12,10 @@
 // formed while P of the one before is made (two places in tensor memory), and two CTAs an
 // SM fill one another's waits.
 //
-// Measured: eight trees of 32 nodes over 32 to 2912 entries, 28 heads over 4: 26 us, of which
-// the joining of runs takes 5; 16 of 64 nodes, 40 key heads, 480 to 640 entries: 84 us (floor
+// Measured: eight trees of 32 nodes over 32 to 2912 entries, 28 heads over 4: 26 us; 16 of 64 nodes, 40 key heads, 480 to 640 entries: 84 us (floor
 // 30).  What bounds it is a tile's chain, most of it the 64 exponentials and twice as many
-// conversions of a row in one thread (1.0 to 1.5 us, 29 % of the issue slots used), and per
-// run the first tile's and the last products' latencies (3 and 2.5 us).
+// conversions of a row in one thread (1 to 2 us by time stamps, 27 % of the issue slots used),
+// and per run the first tile's and the last products' latencies (about 3 us each).
 //
 // O stays in tensor memory.  A row's reference moves only when its maximum has grown by
 // 2^8, so that O is seldom read back and rescaled; until then p is up to 2^8.

@@ -126,8 +126,8 @@ __device__ __forceinline__ uint32_t slot_of(int page, int slots) { return ((uint
 // shared memory, and the steps depend on one another.  With the copies: one sequence as six
 // 7.2 us, 128 sequences of up to 8192 entries 10.2 (15.8 with the children's lengths worked
 // out in each step, last pages compared in pairs and nothing read ahead).  Writes the fresh
-// entries of the new table, the entry of each partly filled page and the number of pages left; the rest is the
-// copies' kernel's.
+// entries of the new table, the entry of each partly filled page and the number of pages
+// left; the rest is the copies' kernel's.
 __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const __grid_constant__ CachePages c,
                                                                  const __grid_constant__ ForkArgs f) {
   extern __shared__ uint32_t marks[];
