@@ -1773,8 +1773,8 @@ FOVEA_API fovea_status fovea_cache_fork(void* k_pages, void* v_pages, int cache_
     return fail(FOVEA_ERR_INVALID_ARG, "the new table's sizes %d and %d must be at least 0 and 1", C, new_width);
   if (C > FOVEA_MAX_CACHE_SEQ) return fail(FOVEA_ERR_UNSUPPORTED, "%d continuations > %d", C, FOVEA_MAX_CACHE_SEQ);
   if (n_pages > FOVEA_MAX_PAGES) return fail(FOVEA_ERR_UNSUPPORTED, "n_pages %d > %d", n_pages, FOVEA_MAX_PAGES);
-  if ((long long)new_width * page > (1ll << 30))
-    return fail(FOVEA_ERR_UNSUPPORTED, "tables of %d pages of %d entries", new_width, page);
+  if ((long long)new_width * page > (1ll << 30) || (long long)C * new_width * page > (1ll << 34))
+    return fail(FOVEA_ERR_UNSUPPORTED, "tables of %d by %d pages of %d entries", C, new_width, page);
   NEED_ALIGNED(free_pages, 4, "free_pages");
   if (C > 0) {
     if (B > 0) NEED_ALIGNED(lens, 4, "lens");

@@ -86,6 +86,7 @@ CACHE = [(dict(cache=3), BAD), (dict(dim=96), NO), (dict(dim=0), NO), (dict(page
     (fork, dict(C=-1), BAD), (fork, dict(C=2049), NO), (fork, dict(new_width=0), BAD), (fork, dict(new_width=1 << 27), NO),
     (fork, dict(n_pages=(1 << 20) + 1), NO), (fork, dict(lens=None), BAD), (fork, dict(parents=None), BAD),
     (fork, dict(new=None), BAD), (fork, dict(new=P), BAD), (fork, dict(new_lens=P), BAD), (fork, dict(free=None), BAD),
+    (fork, dict(C=2048, new_width=1 << 26), NO), (fork, dict(C=17, new_width=1 << 26), NO),
     (fork, dict(kept=P + 1), BAD), (fork, dict(room=P + 2), BAD),
 ] + [(call, kw, status) for call in (append, attention, keep, fork) for kw, status in CACHE])
 def test_refusals(L, call, kw, status):
