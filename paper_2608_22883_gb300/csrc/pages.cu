@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(kKeepThreads) cache_keep_kernel(const __grid_c
   const int tid = threadIdx.x, b = blockIdx.y;
   const int parts = (row_vecs + cols - 1) / cols, h = blockIdx.x / parts, col0 = blockIdx.x % parts * cols;
   if (tid == 0) count = path;
-  const int n = lens[b], base = n - size;
+  const int n = lens[b], base = n >= size ? n - size : -1;     // the lowest lengths would wrap
   __syncthreads();
   const long long room = (long long)c.width * c.page;
   auto place = [&](int e) -> long long {                 // of an entry's first vector, -1: none

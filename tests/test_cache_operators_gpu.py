@@ -603,6 +603,10 @@ def test_keep_bad_pages(fovea):
     before = k.clone()
     assert fovea.cache_keep(k, v, table, ints([60]), ints([[19]]), 20).tolist() == [41]
     assert same(k, before)
+    # lengths below zero, down to the lowest
+    for n in (-1, -2 ** 31, -2 ** 31 + 19):
+        assert fovea.cache_keep(k, v, table, ints([n]), ints([[19]]), 20).tolist() == [n]
+    assert same(k, before)
 
 
 # ---------------------------------------------------------------------------
