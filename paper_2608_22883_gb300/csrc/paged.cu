@@ -74,9 +74,16 @@ template <class C, int D> struct Cut {
 template <class C, int D, int RT> constexpr int kTogether = sizeof(C) * D * RT <= 128 ? 2 : 1;
 
 // Whether a step's pages are asked for a step ahead: with 8-bit entries (four sequences of
-// 131072: 168 us without, 162 with) and dims of 256 (49.7 and 46.2); it costs the others (one
-// sequence of 4096 10.3 and 11.5, fp32 33 and 39).
+// 131072: 168 us without, 162 with) and bf16 of 256 dims (49.7 and 46.2); it costs the
+// others (one sequence of 4096 10.3 and 11.5, fp32 of 128 dims 33 and 39, of 256 68.7 and 71.6).
 template <class C, int D> constexpr bool kAsks = sizeof(C) == 1 || (sizeof(C) == 2 && D == 256);
+
+// Whether a block's values are loaded when its scores are formed, and the next keys when its
+// values are used, in the same registers: keys and values of fp32 entries of 256 dims take 128
+// registers a lane each.  16 sequences of 2048: 68.7 us, with both on their way, which spills
+// 1.5 KB, 98.9; one of 1000 15.6 and 22.3.  It costs those that fit: fp32 of 128 dims 33.6 to
+// 34.8, bf16 of 256 45.8 to 47.7.
+template <class C, int D> constexpr bool kTakesTurns = sizeof(C) * D > 512;
 
 template <class C, class Q, int D, int RT>
 struct Attention {
@@ -102,6 +109,7 @@ struct Attention {
 
   static constexpr int kSub = kTogether<C, D, RT>;
   static constexpr bool kAsk = kAsks<C, D>;
+  static constexpr bool kInTurn = kTakesTurns<C, D>;
   // The keys and values of kSub blocks as a lane holds them.
   uint4 k[kSub][2][G::kKeyChunks];
   uint32_t v[kSub][4][G::kParts][G::kSpanWords];
@@ -441,7 +449,7 @@ struct Attention {
 #pragma unroll
     for (int u = 0; u < kSub; ++u) {
       off[u] = next_off[u];
-      load_keys(u, keys + off[u]);
+      if constexpr (!kInTurn) load_keys(u, keys + off[u]);
     }
     bad = next_bad;
     if (kAsk && at + kWarps * kSub < hi) look_up(at + kWarps * kSub);
@@ -449,7 +457,10 @@ struct Attention {
     const int plain = min(end, plain_end(a, n));
     while (true) {
 #pragma unroll
-      for (int u = 0; u < kSub; ++u) load_values(u, values + off[u]);
+      for (int u = 0; u < kSub; ++u) {
+        if constexpr (kInTurn) load_keys(u, keys + off[u]);
+        else load_values(u, values + off[u]);
+      }
       const uint32_t next = at + kWarps * kSub, after = next + kWarps * kSub;
       const bool more = next < hi;
       if (more) {
@@ -464,6 +475,10 @@ struct Attention {
       float s[kSub][RT][4];
 #pragma unroll
       for (int u = 0; u < kSub; ++u) scores(u, sh, s[u]);
+      if constexpr (kInTurn) {
+#pragma unroll
+        for (int u = 0; u < kSub; ++u) load_values(u, values + off[u]);
+      }
       const bool was_bad = bad;
       if (more) {
         if constexpr (!kAsk) place();
@@ -471,7 +486,7 @@ struct Attention {
 #pragma unroll
         for (int u = 0; u < kSub; ++u) {
           off[u] = next_off[u];
-          load_keys(u, keys + off[u]);
+          if constexpr (!kInTurn) load_keys(u, keys + off[u]);
         }
       }
       const int first = (int)at * kBlock;
