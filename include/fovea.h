@@ -574,7 +574,7 @@ FOVEA_API fovea_status fovea_cache_append(const void* q, int64_t q_ld, int64_t q
  *         that it did not reach and FOVEA_ERR_TIMEOUT for fovea_sync_errors(workspace).
  * A row that sees nothing (or only scores of -inf) has out 0 and lse -inf.  Where a page
  * that a row needs is outside the pool, or lens[b] beyond the table, the row is NaN.
- * Softmax and sums are fp32: p is held to 16 bits beside bf16 values, to 11 beside e4m3,
+ * Softmax and sums are fp32: p is held to 16 bits beside bf16 values, to 22 beside e4m3,
  * fp32 in full; out is rounded once.  The order of the sums depends on the sizes alone.
  * 1 <= nodes <= FOVEA_MAX_TREE; kv_heads divides heads; scale finite.
  */

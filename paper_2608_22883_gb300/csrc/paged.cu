@@ -85,9 +85,13 @@ template <class C, int D> constexpr bool kAsks = sizeof(C) == 1 || (sizeof(C) ==
 // 34.8, bf16 of 256 45.8 to 47.7.
 template <class C, int D> constexpr bool kTakesTurns = sizeof(C) * D > 512;
 
-template <class C, class Q, int D, int RT>
+// FOLD: at most four rows, over 8-bit entries.  They stand twice among the eight of a
+// product, the second time for p's lower halves: one product does for both (four sequences
+// of 131072: 158 us; with two products 169, with p to 11 bits 157).
+template <class C, class Q, int D, int RT, bool FOLD = false>
 struct Attention {
   using G = Cut<C, D>;
+  static_assert(!FOLD || (sizeof(C) == 1 && RT == 1), "one tile of rows");
   static constexpr bool kF32 = sizeof(C) == 4, kE4 = sizeof(C) == 1;
   static constexpr bool kWaits = false;
   static constexpr int kRows = 8 * RT, kBlock = 16, kLeast = kWarps;
@@ -96,7 +100,7 @@ struct Attention {
   static constexpr uint32_t kFront = RT == 1 ? 16 : 24;
   static constexpr int kSlot = kRows * (D + 2);                  // floats of a partial segment
   static constexpr uint32_t kBytes = kBlock * D * sizeof(C);     // of a block
-  // p of 8-bit values is held in fp16, times 2^15: its smallest step is then 2^-39
+  // p beside 8-bit values is held in fp16, times 2^15: its smallest step is then 2^-39
   static constexpr float kLift = kE4 ? 15.0f : 0.0f;
 
   struct Shared {
@@ -116,6 +120,7 @@ struct Attention {
   float o[RT][G::kTiles][4];
   float m[RT][2], l[RT][2];
 
+  __device__ __forceinline__ static int row_in(int r) { return FOLD ? r & 3 : r; }   // of place r
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -288,7 +293,8 @@ struct Attention {
       }
     } else {
       // p as two bf16 values that add up to 16 bits of it (one alone would add an error of
-      // the output's own rounding); 11 bits of fp16 beside values of four
+      // the output's own rounding), beside 8-bit values as two of fp16: 22 bits (p times
+      // 2^kLift is 2^15 at most, the smallest step 2^-24)
       uint32_t bh[RT][2], bl[RT][2];
 #pragma unroll
       for (int r = 0; r < RT; ++r)
@@ -296,8 +302,10 @@ struct Attention {
         for (int e = 0; e < 2; ++e) {
           const float x = p[r][2 * e], y = p[r][2 * e + 1];
           if constexpr (kE4) {
-            const __half2 h = __floats2half2_rn(x, y);
-            bh[r][e] = transpose8(*reinterpret_cast<const uint32_t*>(&h));
+            uint32_t hi, lo;
+            split_halves(x, y, hi, lo);
+            bh[r][e] = transpose8(FOLD && t >= 2 ? lo : hi);      // rows 2t, 2t + 1
+            if constexpr (!FOLD) bl[r][e] = transpose8(lo);
           } else {
             const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
             const float2 f = __bfloat1622float2(h);
@@ -313,7 +321,7 @@ struct Attention {
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
           mma16<kE4>(o[r][i], f, bh[r][0], bh[r][1]);
-          if constexpr (!kE4) mma16<kE4>(o[r][i], f, bl[r][0], bl[r][1]);
+          if constexpr (!FOLD) mma16<kE4>(o[r][i], f, bl[r][0], bl[r][1]);
         }
       }
     }
@@ -356,8 +364,8 @@ struct Attention {
     if constexpr (kE4) {
       for (int r = tid >> 5; r < kRows; r += kWarps) {
         float top = 0.0f;
-        if (row0 + r < rows) {
-          const Q* p = row_at(row0 + r);
+        if (row0 + row_in(r) < rows) {
+          const Q* p = row_at(row0 + row_in(r));
           for (int d = lane; d < D; d += 32) top = fmaxf(top, fabsf(to_f32(p[d])));
         }
 #pragma unroll
@@ -368,7 +376,7 @@ struct Attention {
     }
     for (int i = tid; i < RT * G::kSteps * 32; i += kThreads) {
       const int lane_of = i & 31, step = (i >> 5) % G::kSteps, r = (i >> 5) / G::kSteps;
-      const int row = row0 + 8 * r + (lane_of >> 2), t = lane_of & 3;
+      const int row = row0 + row_in(8 * r + (lane_of >> 2)), t = lane_of & 3;
       uint2 f = make_uint2(0u, 0u);
       if (row < rows) {
         const Q* p = row_at(row);
@@ -506,7 +514,7 @@ struct Attention {
           for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const int node = min((row0 + 8 * r + 2 * t + e) / a.group, a.nodes - 1);
+              const int node = min((row0 + row_in(8 * r + 2 * t + e)) / a.group, a.nodes - 1);
               const uint32_t bits = seen_bits(a, tree, n, node, start, end);
 #pragma unroll
               for (int x = e; x < 4; x += 2) s[u][r][x] = bits >> (g + 4 * (x - e)) & 1u ? s[u][r][x] : -INFINITY;
@@ -600,7 +608,11 @@ struct Attention {
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
       const float mw = sh.m[w][r], c = mw == top ? 1.0f : exp2_(mw - top);
-      const float4 y = *reinterpret_cast<const float4*>(&sh.o[w][r][d]);
+      float4 y = *reinterpret_cast<const float4*>(&sh.o[w][r][d]);
+      if constexpr (FOLD) {
+        const float4 z = *reinterpret_cast<const float4*>(&sh.o[w][r + 4][d]);
+        y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+      }
       sum += c * sh.l[w][r];
       x.x += c * y.x; x.y += c * y.y; x.z += c * y.z; x.w += c * y.w;
     }
@@ -647,9 +659,9 @@ template <class C, int D, int RT> constexpr int per_sm() {
   return sizeof(C) == 4 || RT * D >= 256 ? 2 : sizeof(C) == 2 && RT * D == 64 ? 4 : 3;
 }
 
-template <class C, class Q, int D, int RT>
+template <class C, class Q, int D, int RT, bool FOLD>
 __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_attention_kernel(const __grid_constant__ PagedArgs a) {
-  using A = Attention<C, Q, D, RT>;
+  using A = Attention<C, Q, D, RT, FOLD>;
   extern __shared__ __align__(16) uint8_t raw[];
   typename A::Shared& sh = *reinterpret_cast<typename A::Shared*>(raw);
   static_assert(offsetof(typename A::Shared, o) % 16 == 0 && sizeof(typename A::Shared) % 16 == 0, "16-byte loads");
@@ -674,10 +686,10 @@ constexpr int kMostCtas = 8;
 
 // Small tables: a cluster of CTAs a segment, each an equal share of its blocks, which join
 // their sums through distributed shared memory: one launch, no partial sums in memory.
-template <class C, class Q, int D, int RT>
+template <class C, class Q, int D, int RT, bool FOLD>
 __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_cluster_kernel(const __grid_constant__ PagedArgs a,
                                                                                      int ctas) {
-  using A = Attention<C, Q, D, RT>;
+  using A = Attention<C, Q, D, RT, FOLD>;
   extern __shared__ __align__(16) uint8_t raw[];
   typename A::Shared& sh = *reinterpret_cast<typename A::Shared*>(raw);
   // a CTA's maxima and sums of its rows, whether it has met odd values; of all CTAs
@@ -781,12 +793,12 @@ template <class A> int cluster_ctas(const PagedArgs& a, int resident) {
   return segments <= 152 * resident && steps <= (a.B == 1 ? 16 : 4) ? ctas : 0;
 }
 
-template <class C, class Q, int D, int RT>
+template <class C, class Q, int D, int RT, bool FOLD>
 cudaError_t launch_cluster(PagedArgs a, int ctas, cudaStream_t s) {
-  using A = Attention<C, Q, D, RT>;
+  using A = Attention<C, Q, D, RT, FOLD>;
   static std::atomic<unsigned long long> raised{0};
   set_up<A>(a);
-  cudaError_t e = raise_smem_limit(paged_cluster_kernel<C, Q, D, RT>, 64 * 1024, raised);
+  cudaError_t e = raise_smem_limit(paged_cluster_kernel<C, Q, D, RT, FOLD>, 64 * 1024, raised);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((long long)a.B * a.kv_heads * a.row_blocks * ctas));
@@ -801,18 +813,18 @@ cudaError_t launch_cluster(PagedArgs a, int ctas, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, paged_cluster_kernel<C, Q, D, RT>, a, ctas);
+  return cudaLaunchKernelEx(&cfg, paged_cluster_kernel<C, Q, D, RT, FOLD>, a, ctas);
 }
 
-template <class C, class Q, int D, int RT>
+template <class C, class Q, int D, int RT, bool FOLD = false>
 cudaError_t launch_as(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
-  using A = Attention<C, Q, D, RT>;
+  using A = Attention<C, Q, D, RT, FOLD>;
   static std::atomic<unsigned long long> raised{0};
   if (workspace == nullptr) {
     const int ctas = cluster_ctas<A>(a, per_sm<C, D, RT>());
-    if (ctas > 0) return launch_cluster<C, Q, D, RT>(a, ctas, s);
+    if (ctas > 0) return launch_cluster<C, Q, D, RT, FOLD>(a, ctas, s);
   }
-  return launch_runs<A, C, Q, D>(a, paged_attention_kernel<C, Q, D, RT>, kThreads, sizeof(typename A::Shared),
+  return launch_runs<A, C, Q, D>(a, paged_attention_kernel<C, Q, D, RT, FOLD>, kThreads, sizeof(typename A::Shared),
                                  152 * per_sm<C, D, RT>(), s, workspace, raised);
 }
 
@@ -825,6 +837,8 @@ cudaError_t launch_dim(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
     if (rows > 16) return launch_as<C, Q, D, 4>(a, s, workspace);
   if constexpr (most_tiles<C, D>() >= 2)
     if (rows > 8) return launch_as<C, Q, D, 2>(a, s, workspace);
+  if constexpr (sizeof(C) == 1)
+    if (rows <= 4) return launch_as<C, Q, D, 1, true>(a, s, workspace);
   return launch_as<C, Q, D, 1>(a, s, workspace);
 }
 template <class C, class Q>

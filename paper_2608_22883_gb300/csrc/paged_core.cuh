@@ -44,6 +44,14 @@ __device__ __forceinline__ uint32_t halves_of_e4m3(uint32_t two) {   // the low 
 __device__ __forceinline__ uint32_t bits_of(__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); }
 __device__ __forceinline__ uint32_t bits_of(__nv_bfloat162 x) { return *reinterpret_cast<const uint32_t*>(&x); }
 
+// x and y (below 2^16) as sums of two fp16 values each: 22 bits, or down to 2^-25.
+__device__ __forceinline__ void split_halves(float x, float y, uint32_t& hi, uint32_t& lo) {
+  const __half2 h = __floats2half2_rn(x, y);
+  const float2 back = __half22float2(h);
+  hi = bits_of(h);
+  lo = bits_of(__floats2half2_rn(x - back.x, y - back.y));
+}
+
 // The kernels' code is fetched by every SM when it is first run, which small calls wait
 // for; divisions of 64 bits, a kilobyte each, stay out of line or are replaced here.
 __device__ __noinline__ uint64_t divide_long(uint64_t x, uint32_t d) { return x / d; }

@@ -276,7 +276,7 @@ template <class C, int D> struct Rows {
 #pragma unroll
         for (int j = 0; j < kTile / 16; ++j) {
           // p of 16 entries as the fragment of a step: two bf16 values that add up to 16 bits
-          // of it, or 11 bits of fp16 beside 8-bit values (paged.cu)
+          // of it, or two of fp16 beside 8-bit values (22 bits, paged.cu)
           uint32_t hi_[4], lo_[4];
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
@@ -285,7 +285,7 @@ template <class C, int D> struct Rows {
             const float p0 = exp2_(y[0] - below[e]), p1 = exp2_(y[1] - below[e]);
             l[e] += p0 + p1;
             if constexpr (kE4) {
-              hi_[x] = bits_of(__floats2half2_rn(p0, p1));
+              split_halves(p0, p1, hi_[x], lo_[x]);
             } else {
               const __nv_bfloat162 two = __floats2bfloat162_rn(p0, p1);
               const float2 back = __bfloat1622float2(two);
@@ -303,8 +303,12 @@ template <class C, int D> struct Rows {
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
                 const uint32_t u = __byte_perm(r[2 * x], 0, 0x3120), w = __byte_perm(r[2 * x + 1], 0, 0x3120);
-                mma16<kE4>(o[2 * (i + x)], hi_, halves_of_e4m3(u & 0xFFFFu), halves_of_e4m3(w & 0xFFFFu));
-                mma16<kE4>(o[2 * (i + x) + 1], hi_, halves_of_e4m3(u >> 16), halves_of_e4m3(w >> 16));
+                const uint32_t u0 = halves_of_e4m3(u & 0xFFFFu), w0 = halves_of_e4m3(w & 0xFFFFu);
+                const uint32_t u1 = halves_of_e4m3(u >> 16), w1 = halves_of_e4m3(w >> 16);
+                mma16<kE4>(o[2 * (i + x)], hi_, u0, w0);
+                mma16<kE4>(o[2 * (i + x) + 1], hi_, u1, w1);
+                mma16<kE4>(o[2 * (i + x)], lo_, u0, w0);
+                mma16<kE4>(o[2 * (i + x) + 1], lo_, u1, w1);
               }
             }
           } else {

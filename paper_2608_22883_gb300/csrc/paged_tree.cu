@@ -4,8 +4,8 @@
 // A CTA takes 128 rows and tiles of 64 entries.  S = Q K^T goes to tensor memory, a row a
 // lane, so that a thread has a row's scores of a tile and no maximum or sum crosses lanes.
 // It writes p back over the scores, as the first operand of O += P V (two bf16 values that
-// add up to 16 bits of p, or 11 bits of fp16 beside 8-bit values, lifted so that the largest
-// fit).  V lies as it is cached, entries by dims, and is read along its rows (MN-major).
+// add up to 16 bits of p, or two of fp16 beside 8-bit values: 22 bits, lifted so that the
+// largest fit).  V lies as it is cached, entries by dims, and is read along its rows (MN-major).
 // The roles, joined by mbarriers with bounded waits: four warps turn S into P; two copy
 // keys and two values of the pages (asynchronous copies, or through registers where 8 bits
 // become fp16) into the 128-byte-swizzled layout; one issues the products.  S of a tile is
@@ -365,7 +365,7 @@ template <class C, int D> struct Issuer {
       const uint64_t v = sw128_desc(smem_u32(sh.v[st])) + ((uint64_t)((T::kBlock * 128 >> 4) - 1) << 16);
       const uint32_t p = tmem + T::kColS + buf * 64;
 #pragma unroll
-      for (int part = 0; part < (T::kE4 ? 1 : 2); ++part)        // p's upper and lower bits
+      for (int part = 0; part < 2; ++part)                       // p's upper and lower bits
 #pragma unroll
         for (int i = 0; i < T::kBlock / 16; ++i)
           umma_ts(tmem, p + part * 32 + i * 8, v + (uint64_t)(i * (16 * 128 >> 4)), T::kIdescO,
@@ -473,7 +473,7 @@ template <class C, int D> struct Softmax {
             sums[2 * (j & 1)] += p0;
             sums[2 * (j & 1) + 1] += p1;
             if constexpr (T::kE4) {
-              hi_[j] = bits_of(__floats2half2_rn(p0, p1));
+              split_halves(p0, p1, hi_[j], lo_[j]);
             } else {
               const __nv_bfloat162 two = __floats2bfloat162_rn(p0, p1);
               const float2 back = __bfloat1622float2(two);
@@ -482,7 +482,7 @@ template <class C, int D> struct Softmax {
             }
           }
           tmem_st8(at + i / 2, hi_);
-          if constexpr (!T::kE4) tmem_st8(at + 32 + i / 2, lo_);
+          tmem_st8(at + 32 + i / 2, lo_);
         }
         l = (sums[0] + sums[1]) + (sums[2] + sums[3]);
         tmem_st_wait();

@@ -1,0 +1,79 @@
+"""Edges of the drafter's cache that random rows do not reach: the bits of
+probabilities, values that are no numbers in front of a tree, long paths, far and
+small angles, outputs in the inputs' place, scales and rows at the ends of their range."""
+
+import math
+
+import pytest
+import torch
+
+from test_cache_operators_gpu import (BF16, E4M3, FP32, I32, U, check_attention, entries, fovea,  # noqa: F401
+                                      gen, ints, make_cache, normal, same, tree_bits, within)
+
+pytestmark = pytest.mark.gpu
+
+# (cache, nodes, heads, key heads, dim): each form of the attention, by rows of a key head
+FORMS = [
+    (BF16, 1, 6, 2, 64), (BF16, 6, 4, 2, 128), (BF16, 3, 8, 2, 256),                      # few rows
+    (BF16, 7, 8, 2, 256),                                                                 # staged tiles
+    (BF16, 32, 8, 2, 128), (BF16, 20, 2, 1, 64), (BF16, 160, 2, 2, 128),                  # tensor memory
+    (FP32, 1, 4, 2, 128), (FP32, 6, 4, 2, 64), (FP32, 9, 4, 2, 256),
+    (E4M3, 1, 4, 2, 256), (E4M3, 1, 8, 2, 128), (E4M3, 2, 4, 2, 64),                      # four rows and fewer
+    (E4M3, 6, 4, 2, 64), (E4M3, 6, 4, 2, 128),
+    (E4M3, 6, 8, 2, 128), (E4M3, 9, 4, 2, 64), (E4M3, 7, 8, 2, 256),
+    (E4M3, 32, 8, 2, 128), (E4M3, 70, 2, 2, 64), (E4M3, 160, 2, 2, 128),
+]
+
+
+def rows_type(cache):
+    return FP32 if cache is FP32 else BF16
+
+
+def put(pool, table, b, e, dims, value):
+    """value at entry e of sequence b, in these dims of all heads."""
+    page = pool.shape[2]
+    pool[int(table[b, e // page]), :, e % page, dims] = torch.tensor(value).to(pool.dtype).cuda()
+
+
+# ---------------------------------------------------------------------------
+# The bits of p
+# ---------------------------------------------------------------------------
+
+def cancelling():
+    """(a, b) in 4 significant bits with a as near to b e^(i / 8) as there are, for i = 1 .. 15."""
+    found = []
+    for i in range(1, 16):
+        r = math.exp(i / 8)
+        pairs = [(x * 2.0 ** s, float(y)) for x in range(8, 16) for y in range(8, 16) for s in range(4)]
+        found.append(min(pairs, key=lambda p: abs(p[0] / p[1] - r)))
+    return found
+
+
+@pytest.mark.parametrize("cache,nodes,heads,kv,dim", [f for f in FORMS if f[0] is E4M3])
+def test_values_that_cancel(fovea, cache, nodes, heads, kv, dim):
+    """Sixteen entries in front of a tree that is not seen, with exact scores 0, 1/8, ..., 15/8, and in
+    each dim two values whose products with p nearly cancel: what is left shows p's roundings."""
+    n = 16 + nodes
+    k, v, table, _ = make_cache(gen(1), cache, [n, n], kv, dim, 16)
+    for b in range(2):
+        for e in range(16):
+            put(k, table, b, e, slice(None), 0.0)
+            put(k, table, b, e, 0, e / 8)
+            put(v, table, b, e, slice(None), 0.0)
+        for d, (x, y) in zip(range(dim), cancelling() * dim):
+            put(v, table, b, 0, d, -x)
+            put(v, table, b, 1 + d % 15, d, y)
+    q = torch.zeros(2 * nodes, heads, dim, dtype=BF16, device="cuda")
+    q[..., 0] = 1.0
+    got = fovea.paged_attention(q, k, v, table, ints([n, n]), tree=torch.zeros(1, nodes, -(-nodes // 32), **I32), scale=1.0)
+    z = torch.arange(16, dtype=torch.float64, device="cuda") / 8
+    p = torch.softmax(z, 0)
+    x = entries(v, table, 0, 16)[:, 0].double()
+    want, size = p @ x, p @ x.abs()
+    assert bool((want.abs() < size / 100).all())
+    # Of an element of p: 22 bits in its product (2^-22), its score times log2 e in two roundings
+    # (2 * 15/8 u) and the exponential's 2^-22; of the sums: a block's truncated addition to 2^-23
+    # of its magnitudes and the joins of eight parts (8 * 2^-23); the last rounding.
+    bound = want.abs() * 2.0 ** -9 * 2 + size * (2 * 2.0 ** -22 + 4 * U + 9 * 2.0 ** -23)
+    out = got["out"].double()
+    within(out, want.expand_as(out), bound, "cancelling values")
