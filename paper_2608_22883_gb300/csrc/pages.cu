@@ -9,7 +9,10 @@ namespace fovea {
 
 namespace {
 
-constexpr int kKeepThreads = 128, kKeepBytes = 48 * 1024;
+constexpr int kKeepThreads = 128;
+// Staged entries: what is left of the 48 KB of a launch without a raised limit, beside the
+// kernel's places of the entries and their number.
+constexpr int kKeepBytes = 48 * 1024 - 2 * FOVEA_MAX_TREE * 8 - 64;
 
 // Entry base + i <- entry base + nodes[i], base = lens - size: all sources are read, into
 // shared memory, before an entry is written, so that any list of nodes is right.  A CTA

@@ -77,3 +77,27 @@ def test_values_that_cancel(fovea, cache, nodes, heads, kv, dim):
     bound = want.abs() * 2.0 ** -9 * 2 + size * (2 * 2.0 ** -22 + 4 * U + 9 * 2.0 ** -23)
     out = got["out"].double()
     within(out, want.expand_as(out), bound, "cancelling values")
+
+
+# ---------------------------------------------------------------------------
+# Paths of every length
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("cache,dim", [(BF16, 64), (BF16, 128), (BF16, 256), (FP32, 64), (FP32, 128), (FP32, 256),
+                                       (E4M3, 64), (E4M3, 256)])
+def test_paths_of_every_length(fovea, cache, dim):
+    """The staging of a path takes what shared memory is left beside the places of its entries."""
+    g = gen(dim)
+    size, page, n = 256, 64, 300
+    k, v, table, _ = make_cache(g, cache, [n], 1, dim, page)
+    before = [entries(x, table, 0, n).clone() for x in (k, v)]
+    stored = [x.clone() for x in (k, v)]
+    for path in list(range(1, 257, 5)) + [43, 44, 45, 48, 49, 88, 89, 96, 97, 176, 177, 192, 193, 255, 256]:
+        for pool, old in zip((k, v), stored):
+            pool.copy_(old)
+        nodes = torch.randint(0, size, (1, path), generator=g, **I32)
+        got = fovea.cache_keep(k, v, table, ints([n]), nodes, size)
+        assert got.tolist() == [n - size + path]
+        for pool, old in zip((k, v), before):
+            kept = entries(pool, table, 0, n - size + path)
+            assert same(kept[:n - size], old[:n - size]) and same(kept[n - size:], old[n - size + nodes[0].long()]), path
