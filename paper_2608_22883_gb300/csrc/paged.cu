@@ -339,19 +339,21 @@ struct Attention {
           for (int w = 0; w < G::kSpanWords; ++w) v[u][e][p][w] = 0;
   }
 
-  // Odd values cleared (odd_values): true where there was one.
-  __device__ __forceinline__ bool clear_odd_values(int u) {
+  // Odd values of the block's entries from `from` on cleared (add_odd_values): true where there was one.
+  __device__ __forceinline__ bool clear_odd_values(int u, int from) {
+    const int t = threadIdx.x & 3;
     uint32_t any = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
+      if (value_entry(t, e) >= from)
 #pragma unroll
-      for (int p = 0; p < G::kParts; ++p)
+        for (int p = 0; p < G::kParts; ++p)
 #pragma unroll
-        for (int w = 0; w < G::kSpanWords; ++w) {
-          const uint32_t odd = odd_in<C>(v[u][e][p][w]);
-          v[u][e][p][w] &= ~odd;
-          any |= odd;
-        }
+          for (int w = 0; w < G::kSpanWords; ++w) {
+            const uint32_t odd = odd_in<C>(v[u][e][p][w]);
+            v[u][e][p][w] &= ~odd;
+            any |= odd;
+          }
     return any != 0;
   }
 
@@ -521,7 +523,7 @@ struct Attention {
               if (out && (bits & 0xFFFFu) != 0) l[r][e] = NAN;   // a page that is not there
             }
           clear_values(u, out ? 0 : end - start);
-          if ((a.nodes > 1 || tree != nullptr) && clear_odd_values(u)) sh.odd = 1;
+          if ((a.nodes > 1 || tree != nullptr) && clear_odd_values(u, n - a.nodes - start)) sh.odd = 1;
         }
       }
       // running maxima and sums

@@ -228,8 +228,9 @@ __device__ __forceinline__ float to_f32_any(float x) { return x; }
 __device__ __forceinline__ float to_f32_any(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f32_any(__nv_fp8_e4m3 x) { return float(x); }
 
-// Values that are infinite or NaN, where only some rows see an entry: a product with a p of
-// 0 would give NaN to the others.  They are cleared before the products; when a segment's
+// Values that are infinite or NaN, where only some rows see an entry, that is among the newest:
+// a product with a p of 0 would give NaN to the others.  They are cleared before the products
+// (those of entries in front of the newest, which all rows see, are not); when a segment's
 // rows have been written (to out, or to a partial slot) those of the entries from `from` to
 // `to` are added to the rows that see them, by `threads` threads.
 template <class C, class Q, int D>

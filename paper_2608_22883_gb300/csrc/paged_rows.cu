@@ -175,11 +175,12 @@ template <class C, int D> struct Rows {
       const bool masked = outside != 0 || first + kTile > plain;
       const uint32_t ks = base + stage * 2 * kTileBytes, vs = ks + kTileBytes;
       if (masked && (a.nodes > 1 || tree != nullptr)) {
-        // odd values of this thread's own copies, which have arrived
+        // odd values of the newest entries, of this thread's own copies, which have arrived
         uint32_t any = 0;
 #pragma unroll 1
         for (int i = 0; i < kCopies; ++i) {
           constexpr int kPass = kThreads / kChunks;
+          if (first + tid / kChunks + i * kPass < n - a.nodes) continue;
           uint4* p = reinterpret_cast<uint4*>(&sh.kv[stage][1][place(tid / kChunks + i * kPass, tid % kChunks)]);
           uint4 x = *p;
           const uint4 odd = make_uint4(odd_in<C>(x.x), odd_in<C>(x.y), odd_in<C>(x.z), odd_in<C>(x.w));

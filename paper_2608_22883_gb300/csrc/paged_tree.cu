@@ -188,7 +188,7 @@ template <class C, int D, bool KEYS> struct Copier {
   __device__ __forceinline__ void segment(int b, int h, int row0, uint32_t lo, uint32_t hi) {
     if (!go) return;
     const int n = length_of(a, b);
-    const int end = min(n, (int)(hi * T::kBlock)), plain = min(end, plain_end(a, n));
+    const int end = min(n, (int)(hi * T::kBlock));
     const uint32_t last_block = (uint32_t)(end - 1) / 16;
     const int32_t* table = a.table + (size_t)b * a.width;
     const uint32_t per_page = a.page / 16, stride = a.kv_heads * per_page;
@@ -222,9 +222,9 @@ template <class C, int D, bool KEYS> struct Copier {
     auto there = [&](uint32_t tile, int i) {
       return !(outside >> (i * kPass / 16) & 1u) && (int)(tile * T::kBlock) + row + i * kPass < end;
     };
-    auto masked = [&](uint32_t out, uint32_t tile) {
-      return mixed && (out != 0 || (int)(tile + 1) * T::kBlock > plain);
-    };
+    // pass i's row is one of the newest entries, whose odd values are cleared
+    auto newest = [&](uint32_t tile, int i) { return (int)(tile * T::kBlock) + row + i * kPass >= n - a.nodes; };
+    auto masked = [&](uint32_t tile) { return mixed && (int)(tile + 1) * T::kBlock > n - a.nodes; };
     uint64_t* empty = KEYS ? sh.k_empty : sh.v_empty;
     uint8_t (*places)[T::kTileBytes] = KEYS ? sh.k : sh.v;
     look_up(lo);
@@ -249,9 +249,10 @@ template <class C, int D, bool KEYS> struct Copier {
         const int st = begun % T::kStages;
         if (begun >= T::kStages && !wait(&empty[st], (begun / T::kStages - 1) & 1)) return;
         uint32_t any = 0;
-        if (!KEYS && masked(outside, tile)) {
+        if (!KEYS && masked(tile)) {
 #pragma unroll
-          for (int i = 0; i < kCopies; ++i) any |= clear_odd<C>(x[i]);
+          for (int i = 0; i < kCopies; ++i)
+            if (newest(tile, i)) any |= clear_odd<C>(x[i]);
         }
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
@@ -297,9 +298,10 @@ template <class C, int D, bool KEYS> struct Copier {
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
         const uint32_t done = begun - (tile - oldest), out = outsides >> 4 * (done % T::kStages) & 15u;
         uint32_t any = 0;
-        if (!KEYS && masked(out, oldest)) {
+        if (!KEYS && masked(oldest)) {
 #pragma unroll 1
           for (int i = 0; i < kCopies; ++i) {
+            if (!newest(oldest, i)) continue;
             uint4* p = reinterpret_cast<uint4*>(places[done % T::kStages] + T::place(row + i * kPass, chunk, T::kBlock));
             uint4 x = *p;
             const uint32_t here = clear_odd<C>(x);

@@ -101,3 +101,46 @@ def test_paths_of_every_length(fovea, cache, dim):
         for pool, old in zip((k, v), before):
             kept = entries(pool, table, 0, n - size + path)
             assert same(kept[:n - size], old[:n - size]) and same(kept[n - size:], old[n - size + nodes[0].long()]), path
+
+
+# ---------------------------------------------------------------------------
+# Values that are no numbers
+# ---------------------------------------------------------------------------
+
+def spoiled(fovea, form, lens, marks, seed=3):
+    """The attention with values marked in front of (entry negative: from the tree's first on
+    backwards) or within the trees: marks (sequence, entry from the tree's first, first dim, value)."""
+    cache, nodes, heads, kv, dim = form
+    g = gen(seed)
+    k, v, table, scales = make_cache(g, cache, lens, kv, dim, 16)
+    for b, at, d, value in marks:
+        if 0 <= lens[b] - nodes + at < lens[b]:
+            put(v, table, b, lens[b] - nodes + at, slice(d, None, 8), value)
+    q = normal(g, len(lens) * nodes, heads, dim).to(rows_type(cache))
+    for tree in (None, tree_bits(g, len(lens), nodes), tree_bits(g, 1, nodes)):
+        check_attention(fovea, q, k, v, table, ints(lens), tree, scales=scales)
+
+
+def spots(nodes, n):
+    """In front of a tree of a sequence of n entries: its last, and the first of the blocks of 16, 32
+    and 64 in which the tree begins."""
+    at = n - nodes
+    return sorted({-1} | {at // size * size - at for size in (16, 32, 64) if at % size})
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("more", [39, 700, 61])
+def test_nan_in_front_of_a_tree(fovea, form, more):
+    """Every row sees the entries in front of a tree, those that share a tile with it too."""
+    nodes = form[1]
+    lens = [nodes + more, nodes + 2 * more + 1, nodes + 5]
+    marks = [(b, at, i % 8, float("nan")) for b in (0, 1) for i, at in enumerate(spots(nodes, lens[b]))]
+    spoiled(fovea, form, lens, marks)
+
+
+@pytest.mark.parametrize("form", [f for f in FORMS if f[1] > 1])
+def test_nan_at_a_node(fovea, form):
+    """A node's value reaches the rows that see it, in every form."""
+    nodes = form[1]
+    lens = [nodes + 39, nodes, nodes + 900]
+    spoiled(fovea, form, lens, [(b, (3 * b + 2) % nodes, b, float("nan")) for b in range(3)] + [(2, nodes - 1, 5, float("nan"))])
