@@ -572,6 +572,8 @@ FOVEA_API fovea_status fovea_cache_append(const void* q, int64_t q_ld, int64_t q
  *         the stream may use it next; it needs no fovea_workspace_init (a call writes a header
  *         where there is none).  A bounded device wait that gives up leaves NaN in the rows
  *         that it did not reach and FOVEA_ERR_TIMEOUT for fovea_sync_errors(workspace).
+ * A value that is infinite or NaN makes its dim so in every row that sees it (infinities of
+ * both signs: NaN).
  * A row that sees nothing (or only scores of -inf) has out 0 and lse -inf.  Where a page
  * that a row needs is outside the pool, or lens[b] beyond the table, the row is NaN.
  * Softmax and sums are fp32: p is held to 16 bits beside bf16 values, to 22 beside e4m3,

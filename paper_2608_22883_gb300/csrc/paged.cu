@@ -106,7 +106,8 @@ struct Attention {
   struct Shared {
     uint2 q[RT][G::kSteps][32];      // Q^T's fragments
     float row_scale[kRows];          // of s, to powers of two
-    int odd;                         // a masked block had infinite values or NaN
+    int odd;                         // what the segment has met (Odd)
+    uint32_t lost;                   // rows whose sum is no number, as bits
     float m[kWarps][kRows], l[kWarps][kRows];
     alignas(16) float o[kWarps][kRows][D + 4];
   };
@@ -523,7 +524,7 @@ struct Attention {
               if (out && (bits & 0xFFFFu) != 0) l[r][e] = NAN;   // a page that is not there
             }
           clear_values(u, out ? 0 : end - start);
-          if ((a.nodes > 1 || tree != nullptr) && clear_odd_values(u, n - a.nodes - start)) sh.odd = 1;
+          if ((a.nodes > 1 || tree != nullptr) && clear_odd_values(u, n - a.nodes - start)) sh.odd = kOddCleared;
         }
       }
       // running maxima and sums
@@ -636,6 +637,7 @@ struct Attention {
       float top, sum;
       const float4 x = warps_sum(sh, r, d, top, sum);
       if (poison) sum = NAN;
+      if (odd_sums(x)) atomicOr(&sh.odd, kOddSums);
       if (!whole) {
         *reinterpret_cast<float4*>(slot + r * D + d) = x;
         if (d == 0) {
@@ -648,10 +650,16 @@ struct Attention {
         write_row<Q>(a, (long long)b * a.nodes + node, head, d, D, x, top, sum, v_scale, kLift);
       }
     }
-    if (sh.odd) {
-      __syncthreads();
-      add_odd_values<C, Q, D>(a, b, h, row0, rows, n, (int)lo * kBlock, (int)hi * kBlock, whole ? nullptr : slot, tid,
-                              kThreads);
+    __syncthreads();
+    if (sh.odd != 0) {
+      if (tid < 32) {
+        float top, sum = 0.0f;
+        if (tid < rows) warps_sum(sh, tid, 0, top, sum);
+        const uint32_t lost = __ballot_sync(0xffffffffu, poison || !(sum > 0.0f));
+        if (tid == 0) sh.lost = lost;
+      }
+      add_odd_values<C, Q, D>(a, b, h, row0, rows, n, (int)lo * kBlock, (int)hi * kBlock, whole ? nullptr : slot, sh.odd,
+                              &sh.o[0][0][0], &sh.lost);
     }
   }
 };
@@ -694,7 +702,7 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_cluster_ke
   using A = Attention<C, Q, D, RT, FOLD>;
   extern __shared__ __align__(16) uint8_t raw[];
   typename A::Shared& sh = *reinterpret_cast<typename A::Shared*>(raw);
-  // a CTA's maxima and sums of its rows, whether it has met odd values; of all CTAs
+  // a CTA's maxima and sums of its rows, what it has met of odd values; of all CTAs
   __shared__ float mine_of[2 * A::kRows + 1], all[kMostCtas][2 * A::kRows + 1];
   pdl_wait();
   pdl_trigger();
@@ -703,6 +711,8 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_cluster_ke
   const int row0 = (seg - b * segments - h * a.row_blocks) * A::kRows, rows = min(a.nodes * a.group - row0, A::kRows);
   const int n = length_of(a, b);
   if (blockIdx.x == 0 && tid == 0) ensure_header(a.header);
+  int* met = reinterpret_cast<int*>(&mine_of[2 * A::kRows]);
+  if (tid == 0) *met = 0;
   A::stage_rows(a, sh, b, h, row0);
   __syncthreads();
   const uint32_t blocks = (uint32_t)(n + A::kBlock - 1) / A::kBlock;
@@ -717,12 +727,13 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_cluster_ke
     float m, l;
     const float4 x = A::warps_sum(sh, r, d, m, l);
     *reinterpret_cast<float4*>(&sh.o[0][r][d]) = x;
+    if (odd_sums(x)) atomicOr(met, kOddSums);
     if (d == 0) {
       mine_of[r] = m;
       mine_of[A::kRows + r] = l;
     }
   }
-  if (tid == 0) mine_of[2 * A::kRows] = sh.odd ? 1.0f : 0.0f;
+  if (tid == 0) atomicOr(met, sh.odd);
   tc::cluster_sync();
   // every value of the others is asked for at once: a load through the cluster takes as long
   // as a pass over the rows
@@ -763,11 +774,24 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_cluster_ke
     const int row = row0 + r, node = row / a.group;
     write_row<Q>(a, (long long)b * a.nodes + node, h * a.group + row - node * a.group, d, D, x, m, l, v_scale, A::kLift);
   }
-  bool odd = false;                  // of any of the cluster's CTAs: the first adds them
+  int odd = 0;                       // of any of the cluster's CTAs: the first adds them
 #pragma unroll 1
-  for (int q = 0; rank == 0 && q < ctas; ++q) odd |= all[q][2 * A::kRows] != 0.0f;
+  for (int q = 0; rank == 0 && q < ctas; ++q) odd |= __float_as_int(all[q][2 * A::kRows]);
   tc::cluster_sync();
-  if (odd) add_odd_values<C, Q, D>(a, b, h, row0, rows, n, 0, n, nullptr, tid, kThreads);
+  if (odd == 0) return;
+  if (tid < 32) {                    // the rows' sums again
+    float m = -INFINITY, l = 0.0f;
+#pragma unroll 1
+    for (int q = 0; tid < rows && q < ctas; ++q) m = fmaxf(m, all[q][tid]);
+#pragma unroll 1
+    for (int q = 0; tid < rows && q < ctas; ++q) {
+      const float mq = all[q][tid];
+      l += (mq == m ? 1.0f : exp2_(mq - m)) * all[q][A::kRows + tid];
+    }
+    const uint32_t lost = __ballot_sync(0xffffffffu, too_long(a, b) || !(l > 0.0f));
+    if (tid == 0) sh.lost = lost;
+  }
+  add_odd_values<C, Q, D>(a, b, h, row0, rows, n, 0, n, nullptr, odd, &sh.o[0][0][0], &sh.lost);
 }
 
 // More rows of a key head than kManyRows go to the kernels of many rows: that on tcgen05

@@ -228,37 +228,6 @@ __device__ __forceinline__ float to_f32_any(float x) { return x; }
 __device__ __forceinline__ float to_f32_any(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f32_any(__nv_fp8_e4m3 x) { return float(x); }
 
-// Values that are infinite or NaN, where only some rows see an entry, that is among the newest:
-// a product with a p of 0 would give NaN to the others.  They are cleared before the products
-// (those of entries in front of the newest, which all rows see, are not); when a segment's
-// rows have been written (to out, or to a partial slot) those of the entries from `from` to
-// `to` are added to the rows that see them, by `threads` threads.
-template <class C, class Q, int D>
-__device__ __noinline__ void add_odd_values(const PagedArgs& a, int b, int h, int row0, int rows, int n, int from, int to,
-                                            float* slot, int tid, int threads) {
-  const uint32_t* tree = tree_of(a, b);
-  const float sign = sizeof(C) == 1 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
-#pragma unroll 1
-  for (int i = tid; i < rows * D; i += threads) {
-    const int r = i / D, d = i % D, row = row0 + r, node = row / a.group;
-    float odd = 0.0f;
-#pragma unroll 1
-    for (int at = max(max(from, n - a.nodes), 0); at < min(to, n); ++at) {
-      const int page = a.table[(size_t)b * a.width + at / a.page];
-      if (!sees(a, tree, n, node, at) || (unsigned)page >= (unsigned)a.n_pages) continue;
-      const float v = to_f32_any(
-          static_cast<const C*>(a.v_pages)[(((size_t)page * a.kv_heads + h) * a.page + at % a.page) * D + d]);
-      if (!isfinite(v)) odd += v;
-    }
-    if (odd == 0.0f) continue;
-    if (slot != nullptr) {
-      slot[i] += odd;
-    } else {
-      Q* out = static_cast<Q*>(a.out) + (((long long)b * a.nodes + node) * a.heads + h * a.group + row - node * a.group) * D + d;
-      *out = from_f32<Q>(to_f32(*out) + odd * sign);
-    }
-  }
-}
 // The odd halves, bytes or words of x as all ones: the exponent (of 8 bits: all seven) is
 // ones where one more carries out of it.
 template <class C> __device__ __forceinline__ uint32_t odd_in(uint32_t x) {
@@ -267,6 +236,71 @@ template <class C> __device__ __forceinline__ uint32_t odd_in(uint32_t x) {
   else return (((x & 0x7F807F80u) + 0x00800080u) >> 15 & 0x00010001u) * 0xFFFFu;
 }
 
+// Values that are infinite or NaN ("odd"), which no product with p gets right: with a p of 0,
+// of a row that does not see them, it is NaN, and p's upper and lower parts may differ in
+// sign.  Among the newest entries, of which rows see different ones, they are cleared before
+// the products; in front of them the sums lose their numbers (odd_sums).  When a segment's
+// rows have been written (to out, or to a partial slot), every element with odd values among
+// the entries from `from` to `to` that its row sees becomes their sum: infinite, or NaN.
+enum Odd { kOddCleared = 1, kOddSums = 2 };                // what a segment has met
+__device__ __forceinline__ bool odd_sums(const float4& x) {
+  return fmaf(x.x, 0.0f, fmaf(x.y, 0.0f, fmaf(x.z, 0.0f, x.w * 0.0f))) != 0.0f;
+}
+__device__ __forceinline__ void bar_rows() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// By the CTA's first kThreads threads; front: D floats of theirs; lost: rows whose sum of p
+// is 0 or no number, as bits, which stay as they are.
+template <class C, class Q, int D>
+__device__ __noinline__ void add_odd_values(const PagedArgs& a, int b, int h, int row0, int rows, int n, int from, int to,
+                                            float* slot, int met, float* front, const uint32_t* lost) {
+  const int tid = threadIdx.x;
+  constexpr int kUnit = 16 / sizeof(C), kChunks = D / kUnit;
+  const uint32_t* tree = tree_of(a, b);
+  const int32_t* table = a.table + (size_t)b * a.width;
+  const C* pool = static_cast<const C*>(a.v_pages);
+  const int newest = max(n - a.nodes, 0);
+  auto place = [&](int at) -> const C* {                   // null: not in the pool
+    const int page = table[at / a.page];
+    return (unsigned)page < (unsigned)a.n_pages ? pool + (((size_t)page * a.kv_heads + h) * a.page + at % a.page) * D : nullptr;
+  };
+  bar_rows();
+#pragma unroll 1
+  for (int d = tid; d < D; d += kThreads) front[d] = 0.0f;
+  bar_rows();
+  if (met & kOddSums) {              // of the entries that all rows see, one sum a dim
+    float mine[kUnit] = {};
+#pragma unroll 1
+    for (int at = from + tid / kChunks; at < min(to, newest); at += kThreads / kChunks) {
+      const C* p = place(at);
+      if (p == nullptr) continue;
+      const uint4 x = *reinterpret_cast<const uint4*>(p + tid % kChunks * kUnit);
+      if ((odd_in<C>(x.x) | odd_in<C>(x.y) | odd_in<C>(x.z) | odd_in<C>(x.w)) == 0) continue;
+#pragma unroll
+      for (int i = 0; i < kUnit; ++i) {
+        const float v = to_f32_any(reinterpret_cast<const C*>(&x)[i]);
+        if (!isfinite(v)) mine[i] += v;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i)
+      if (mine[i] != 0.0f) atomicAdd(&front[tid % kChunks * kUnit + i], mine[i]);   // the same in any order
+  }
+  bar_rows();
+#pragma unroll 1
+  for (int i = tid; i < rows * D; i += kThreads) {
+    const int r = i / D, d = i % D, row = row0 + r, node = row / a.group;
+    if (lost[r >> 5] >> (r & 31) & 1u) continue;
+    float odd = front[d];
+#pragma unroll 1
+    for (int at = max(from, newest); at < min(to, n); ++at) {
+      const C* p = sees(a, tree, n, node, at) ? place(at) : nullptr;
+      const float v = p != nullptr ? to_f32_any(p[d]) : 0.0f;
+      if (!isfinite(v)) odd += v;
+    }
+    if (odd == 0.0f) continue;
+    if (slot != nullptr) slot[i] = odd;
+    else static_cast<Q*>(a.out)[(((long long)b * a.nodes + node) * a.heads + h * a.group + row - node * a.group) * D + d] = from_f32<Q>(odd);
+  }
+}
 // Dims d .. d + 3 of a row's result, from the sums of p v and of p (p times 2^lift).
 template <class T>
 __device__ __forceinline__ void write_row(const PagedArgs& a, long long n, int head, int d, int dim, float4 x, float top,
@@ -373,13 +407,16 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const __grid_const
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
             high = fmaxf(high, top);
-            const float keep = top == high ? 1.0f : exp2_(top - high);
+            float keep = top == high ? 1.0f : exp2_(top - high);
             top = high;
             c = ml.x == top ? 1.0f : exp2_(ml.x - top);
             float mine = lane < left ? c * ml.y : 0.0f;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
             sum = sum * keep + mine;
+            // the weights of p v are not 0, so that an infinite sum stays one
+            keep = fmaxf(keep, 0x1p-149f);
+            c = fmaxf(c, 0x1p-149f);
 #pragma unroll
             for (int v = 0; v < kVecs; ++v) {
               x[v].x *= keep; x[v].y *= keep; x[v].z *= keep; x[v].w *= keep;

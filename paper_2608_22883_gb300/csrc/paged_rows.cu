@@ -41,6 +41,8 @@ template <class C, int D> struct Rows {
 
   struct Shared {
     alignas(128) uint8_t kv[2][2][kTileBytes];                   // stage; keys, values
+    float front[D];                                              // of add_odd_values
+    uint32_t lost[kRows / 32];
     int odd;
   };
   // A chunk's place in a tile: rows of 128 bytes and more put it at chunk ^ (row % 8), two
@@ -332,12 +334,13 @@ template <class C, int D> struct Rows {
   }
 
   // Each warp's rows to the output, or to a partial slot.
-  __device__ __forceinline__ void finish(const PagedArgs& a, const Shared& sh, int b, int h, int row0, int n, uint32_t lo,
+  __device__ __forceinline__ void finish(const PagedArgs& a, Shared& sh, int b, int h, int row0, int n, uint32_t lo,
                                          uint32_t hi, bool whole, float* slot) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int rows = a.nodes * a.group;
     const float v_scale = kE4 && a.v_scale != nullptr ? a.v_scale[h] : 1.0f;
     const bool poison = too_long(a, b);
+    bool any_odd = false;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       float sum = l[e];
@@ -346,6 +349,7 @@ template <class C, int D> struct Rows {
       if (poison) sum = NAN;
       const int r = 16 * warp + g + 8 * e, row = row0 + r;
       const int node = min(row, rows - 1) / a.group, head = h * a.group + row - node * a.group;
+      if (t == 0 && !(sum > 0.0f)) atomicOr(&sh.lost[r >> 5], 1u << (r & 31));
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
         // four dims side by side: 8-bit values have them (even and odd tiles); else the lanes
@@ -364,6 +368,7 @@ template <class C, int D> struct Rows {
           d = 16 * i + (odd ? 8 : 0) + 4 * (t >> 1);
         }
         if (row >= rows) continue;
+        any_odd |= odd_sums(x);
         if (whole) {
           write_row<__nv_bfloat16>(a, (long long)b * a.nodes + node, head, d, D, x, m[e], sum, v_scale, kLift);
         } else {
@@ -375,11 +380,11 @@ template <class C, int D> struct Rows {
         }
       }
     }
-    if (sh.odd) {
-      __syncthreads();
+    any_odd = __syncthreads_or(any_odd);
+    if (any_odd || sh.odd)
       add_odd_values<C, __nv_bfloat16, D>(a, b, h, row0, min(rows - row0, kRows), n, (int)(lo * kTile), (int)(hi * kTile),
-                                          whole ? nullptr : slot, threadIdx.x, kThreads);
-    }
+                                          whole ? nullptr : slot, any_odd ? kOddCleared | kOddSums : kOddCleared, sh.front,
+                                          sh.lost);
   }
 };
 
@@ -399,6 +404,7 @@ __global__ void __launch_bounds__(kThreads, rows_per_sm<C, D>) paged_rows_kernel
   A at;
   each_segment<A>(a, run, before, [&](int b, int h, int row0, uint32_t lo, uint32_t hi, bool whole, float* slot) {
     if (threadIdx.x == 0) sh.odd = 0;
+    if (threadIdx.x < A::kRows / 32) sh.lost[threadIdx.x] = 0;
     __syncthreads();
     const int n = length_of(a, b);
     at.tiles(a, sh, b, h, row0, n, lo, hi);

@@ -21,6 +21,7 @@
 // 2^8, so that O is seldom read back and rescaled; until then p is up to 2^8.
 #include <atomic>
 
+#include "packed.cuh"
 #include "paged_core.cuh"
 #include "tc_ptx.cuh"
 
@@ -67,6 +68,16 @@ __device__ __forceinline__ void store32(void* p, uint32_t a, uint32_t b, uint32_
                "r"(e), "r"(f), "r"(g), "r"(h)
                : "memory");
 }
+// A barrier of the four warps that hold the rows, and whether any thread of theirs has x.
+__device__ __forceinline__ bool any_row(bool x) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.or.pred q, 1, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n}\n" : "=r"(any) : "r"((uint32_t)x) : "memory");
+  return any != 0;
+}
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 template <class C, int D> struct Tree {
@@ -99,6 +110,8 @@ template <class C, int D> struct Tree {
     // and whether a masked tile had odd values
     float power[4][kRows];
     int odd[4];
+    uint32_t lost[kRows / 32];       // rows whose sum is no number, as bits
+    float front[D];                  // of add_odd_values
     uint32_t outside[4];             // of the last tiles: parts whose page is not in the pool, as bits
     uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
     uint64_t q_empty, s_full[2], p_full[2], o_done[2], drain;
@@ -501,6 +514,7 @@ template <class C, int D> struct Softmax {
     const int head = h * a.group + row - node * a.group;
     const float sum = poison ? NAN : l;
     const float k = sum == 0.0f ? 0.0f : v_scale * __frcp_rn(sum);   // as in write_row; NaN when given up
+    uint64_t check[2] = {0, 0};      // stay 0 beside finite sums
     if (works) {
       const long long at = ((long long)b * a.nodes + node) * a.heads + head;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + at * D;
@@ -510,6 +524,8 @@ template <class C, int D> struct Softmax {
         float x[32];
         tmem_ld32(tmem + d, x);
         if (there) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) check[i / 2 & 1] = fma2(pack2(x[i], x[i + 1]), 0, check[i / 2 & 1]);
           if (whole) {
             uint32_t y[16];
 #pragma unroll
@@ -537,10 +553,14 @@ template <class C, int D> struct Softmax {
         a.lse[at] = sum == 0.0f ? -INFINITY : (m - T::kLift + log2f(sum)) * kLn2;
     }
     tc_fence_before();
-    asm volatile("bar.sync 1, 128;" ::: "memory");               // all four warps have written, and read the segment's word
-    if (odd)
+    const uint32_t none = __ballot_sync(0xffffffffu, !(sum > 0.0f));
+    if (lane == 0) sh.lost[warp] = none;
+    const uint64_t checked = add2(check[0], check[1]);
+    const bool odd_sum = any_row(lo2(checked) != 0.0f || hi2(checked) != 0.0f);   // all four warps have written, and read the segment's word
+    if (odd || odd_sum)
       add_odd_values<C, __nv_bfloat16, D>(a, b, h, row0, min(rows - row0, T::kRows), n, (int)(lo * T::kBlock),
-                                          (int)(hi * T::kBlock), whole ? nullptr : slot, r, 128);
+                                          (int)(hi * T::kBlock), whole ? nullptr : slot,
+                                          odd_sum ? kOddCleared | kOddSums : kOddCleared, sh.front, sh.lost);
     if (threadIdx.x == 0) *static_cast<volatile int*>(&sh.odd[segments & 3]) = 0;
     ++segments;
   }

@@ -144,3 +144,46 @@ def test_nan_at_a_node(fovea, form):
     nodes = form[1]
     lens = [nodes + 39, nodes, nodes + 900]
     spoiled(fovea, form, lens, [(b, (3 * b + 2) % nodes, b, float("nan")) for b in range(3)] + [(2, nodes - 1, 5, float("nan"))])
+
+
+@pytest.mark.parametrize("form", [f for f in FORMS if f[0] is not E4M3])
+@pytest.mark.parametrize("more", [39, 700, 3000])
+def test_infinite_values(fovea, form, more):
+    """An infinite value makes its dim infinite in the rows that see it, wherever it stands; with
+    one of the other sign, or with a NaN, there is no number."""
+    nodes, inf = form[1], math.inf
+    lens = [nodes + more, nodes + more // 2, nodes + 5]
+    marks = []
+    for b in (0, 1):
+        at = spots(nodes, lens[b])
+        marks += [(b, at[0], 0, inf), (b, at[-1], 1, -inf),
+                  (b, nodes - lens[b], 2, inf), (b, -more // 3, 3, -inf),             # first, and far in front
+                  (b, -1, 4, inf), (b, 0, 4, inf),                                    # in both places
+                  (b, -more // 4, 5, inf), (b, -2, 5, -inf),                          # of both signs
+                  (b, -more // 4, 6, inf), (b, nodes - 1, 6, -inf),                   # the other at a node
+                  (b, 0, 7, -inf), (b, nodes - lens[b], 7, float("nan"))]
+    spoiled(fovea, form, lens, marks)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_rows_without_numbers_stay_so(fovea, form):
+    """A row whose scores are no numbers has none in any dim, with infinite values or without."""
+    cache, nodes, heads, kv, dim = form
+    g = gen(6)
+    lens = [nodes + 70, nodes + 700]
+    k, v, table, scales = make_cache(g, cache, lens, kv, dim, 16)
+    for b in range(2):
+        put(k, table, b, 20, 3, float("nan"))
+        put(v, table, b, 30, slice(0, None, 2), float("nan") if cache is E4M3 else math.inf)
+    q = normal(g, 2 * nodes, heads, dim).to(rows_type(cache))
+    q[0] = 0
+    got = fovea.paged_attention(q, k, v, table, ints(lens), want_lse=True, **scales)
+    assert bool(torch.isnan(got["out"]).all()) and bool(torch.isnan(got["lse"]).all())
+    # a page that is not there, and a length beyond the table
+    k, v, table, scales = make_cache(g, cache, lens, kv, dim, 16)
+    for b in range(2):
+        put(v, table, b, 30, slice(0, None, 2), float("nan") if cache is E4M3 else math.inf)
+    table[0, 0] = -1
+    lens[1] = table.shape[1] * 16 + 1
+    got = fovea.paged_attention(q, k, v, table, ints(lens), want_lse=True, **scales)
+    assert bool(torch.isnan(got["out"]).all()) and bool(torch.isnan(got["lse"]).all())
