@@ -523,8 +523,8 @@ FOVEA_API fovea_status fovea_token_logprobs_grad(const void* logits, int64_t ld,
  *               (axis 0).  A frequency that is not finite, or an axis outside
  *               [0, axes), gives NaN.
  *   q_out, k_out dense, dtype; may be q and k where these are dense
- * The angle is right to 1e-7 at every position (whole turns are taken off in 64-bit
- * fixed point); sums are fp32, rounded once.  rot even, 2 <= rot <= dim <= FOVEA_MAX_HEAD.
+ * The angle is right to 2^-23 at every position and for frequencies up to 2^40 (whole turns
+ * are taken off in 64-bit fixed point); sums are fp32, rounded once.  rot even, 2 <= rot <= dim <= FOVEA_MAX_HEAD.
  */
 FOVEA_API fovea_status fovea_rotary_axes(const void* q, int64_t q_ld, int64_t q_hs, int heads,
                                          const void* k, int64_t k_ld, int64_t k_hs, int kv_heads,

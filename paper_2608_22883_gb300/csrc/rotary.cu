@@ -4,9 +4,10 @@
 // Pair j of a token's head is turned by phi_j = positions[axis_j] f_j:
 //   a' = a cos phi - b sin phi,  b' = a sin phi + b cos phi   (inverse: -phi, the gradient).
 // Angles of far positions lose their bits in fp32 (position 10^6 by 1 radian: 0.06), and in
-// fp64 they cost the few fp64 units.  A turn is therefore held in fixed point: f / 2 pi is
-// rounded once to 64 fractional bits, and its product with an integer position modulo
-// 2^64 is exact in integers; the upper 32 bits are the angle to 1.5e-9.
+// fp64 they cost the few fp64 units.  A turn is therefore held in fixed point: f / 2 pi, as
+// the sum of two fp64 values, is taken to 64 fractional bits, and its product with an integer
+// position modulo 2^64 is exact in integers; the upper 32 bits are the angle to 2.2e-9 (of
+// frequencies up to 2^40, whose lower value is below a turn).
 //
 // Bound by memory: each element is read and written once.  A thread keeps the sines of
 // eight pairs of a token and applies them to up to sixteen heads, so that their cost is
@@ -34,6 +35,18 @@ constexpr int kMaxThreads = 256;
 template <class T> constexpr int kResident = sizeof(T) == 2 ? 4 : 2;
 template <class T> constexpr int kAhead = sizeof(T) == 2 ? 1 : 2;
 constexpr int kChunk = 8;            // elements of a thread's chunk
+
+// Turns per position of a frequency in radians, modulo 1, times 2^64.  1 / (2 pi) is the sum of
+// its fp64 value and what that leaves out; the product's rounding is got back exactly.
+__device__ __forceinline__ unsigned long long turns_of(double f) {
+  constexpr double kUpper = 0.15915494309189535, kLower = -9.839338337591243e-18;
+  const double upper = f * kUpper;
+  double lower = fma(f, kLower, fma(f, kUpper, -upper));
+  lower -= rint(lower);
+  const double frac = upper - rint(upper);                        // within half a turn, exactly
+  return (unsigned long long)__double2ll_rn(frac * 18446744073709551616.0) +
+         (unsigned long long)__double2ll_rn(lower * 18446744073709551616.0);
+}
 
 struct Work {
   HeadRows q, k, v;                  // v: entries alone
@@ -186,11 +199,10 @@ __global__ void __launch_bounds__(kMaxThreads, MODE == kPlain ? 4 : kResident<T>
   const int tid = threadIdx.x;
   if constexpr (ROTARY) {
     for (int j = tid; j < w.r.rot / 2; j += blockDim.x) {
-      double f = w.r.frequencies[j] * 0.15915494309189533577;     // 1 / (2 pi)
+      const double f = w.r.frequencies[j];
       const int axis = w.r.axis != nullptr ? w.r.axis[j] : 0;
       axis_of[j] = (unsigned)axis < (unsigned)w.r.axes && isfinite(f) ? axis : -1;
-      f -= rint(f);                                               // within half a turn
-      phase[j] = (unsigned long long)__double2ll_rn(f * 18446744073709551616.0);
+      phase[j] = turns_of(f);
     }
     __syncthreads();
   }

@@ -187,3 +187,35 @@ def test_rows_without_numbers_stay_so(fovea, form):
     lens[1] = table.shape[1] * 16 + 1
     got = fovea.paged_attention(q, k, v, table, ints(lens), want_lse=True, **scales)
     assert bool(torch.isnan(got["out"]).all()) and bool(torch.isnan(got["lse"]).all())
+
+
+# ---------------------------------------------------------------------------
+# Angles
+# ---------------------------------------------------------------------------
+
+def turned(fovea, frequencies, at):
+    """(cos, sin) [positions, frequencies] as the operator has them, and the angles' own in 64 bits."""
+    from fractions import Fraction
+    half = len(frequencies)
+    q = torch.zeros(len(at), 1, 2 * half, device="cuda")
+    q[..., :half] = 1.0
+    got, _ = fovea.rotary_axes(q, None, ints([at]), torch.tensor(frequencies, dtype=torch.float64, device="cuda"))
+    turn = Fraction(int("6283185307179586476925286766559005768394338798750211641949889184615632812572417997256069650684234135"),
+                    10 ** 99)
+    want = torch.empty(2, len(at), half, dtype=torch.float64)
+    for n, p in enumerate(at):
+        for j, w in enumerate(frequencies):
+            x = Fraction(w) * p / turn
+            x -= round(x)                          # within half a turn, exactly
+            want[0, n, j], want[1, n, j] = math.cos(float(x * turn)), math.sin(float(x * turn))
+    got = got[:, 0].double().cpu()
+    return torch.stack((got[:, :half], got[:, half:])), want
+
+
+def test_far_angles_of_fast_pairs(fovea):
+    """The angle's error does not grow with the position or the frequency."""
+    w = [0.92, 2.5, 100.0, 1e4, 12345.678, 2.0 ** 20 + 1 / 3, 1e9, 2.0 ** 40 - 1 / 7]
+    got, want = turned(fovea, w, [2139596203, 2 ** 31 - 1, -2 ** 31, 1999999973, 1, 77])
+    # the rest of an angle, up to pi / 4, in three roundings (2.4 u); the series' last two
+    # steps (1.5 u); the fixed point's 2^-33 and the product's lower part (below u / 16)
+    assert float((got - want).abs().max()) <= 4 * U
