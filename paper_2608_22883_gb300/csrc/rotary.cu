@@ -6,8 +6,9 @@
 // Angles of far positions lose their bits in fp32 (position 10^6 by 1 radian: 0.06), and in
 // fp64 they cost the few fp64 units.  A turn is therefore held in fixed point: f / 2 pi, as
 // the sum of two fp64 values, is taken to 64 fractional bits, and its product with an integer
-// position modulo 2^64 is exact in integers; the upper 32 bits are the angle to 2.2e-9 (of
-// frequencies up to 2^40, whose lower value is below a turn).
+// position modulo 2^64 is exact in integers: the angle is right to 7e-10 (of frequencies up to
+// 2^40, whose lower value is below a turn) before it is rounded to 24 bits of what it has over
+// the nearest quarter turn.
 //
 // Bound by memory: each element is read and written once.  A thread keeps the sines of
 // eight pairs of a token and applies them to up to sixteen heads, so that their cost is
@@ -112,12 +113,14 @@ __device__ __forceinline__ void store(C* p, const float (&x)[E], float inverse) 
   }
 }
 
-// cos and sin of an angle in 2^-32 turns.  It is taken to the nearest quarter turn, the
+// cos and sin of an angle in 2^-64 turns.  It is taken to the nearest quarter turn, the
 // rest (at most pi / 4) goes through the Taylor series: up to x^9 and x^8, whose next terms
-// are below 2e-9 and 2.5e-8.
-__device__ __forceinline__ void cos_sin(uint32_t turn, float& c, float& s) {
-  const uint32_t quarter = (turn + 0x20000000u) >> 30;
-  const float x = (float)(int)(turn - (quarter << 30)) * 1.4629180792671596e-9f;   // 2 pi / 2^32
+// are below 2e-9 and 2.5e-8.  The lower 32 bits count in small angles, whose sine would
+// otherwise keep few bits (1e-6 radians are 683 steps of the upper ones).
+__device__ __forceinline__ void cos_sin(unsigned long long angle, float& c, float& s) {
+  const uint32_t turn = (uint32_t)(angle >> 32), quarter = (turn + 0x20000000u) >> 30;
+  const float rest = fmaf((float)(uint32_t)angle, 0x1p-32f, (float)(int)(turn - (quarter << 30)));
+  const float x = rest * 1.4629180792671596e-9f;         // 2 pi / 2^32
   const float y = x * x;
   const float sine = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f), x);
   const float cosine = fmaf(y, fmaf(y, fmaf(y, fmaf(y, 2.4801587e-5f, -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.0f);
@@ -234,7 +237,7 @@ __global__ void __launch_bounds__(kMaxThreads, MODE == kPlain ? 4 : kResident<T>
           axis = next;
           p = axis < 0 ? 0 : w.r.positions[axis * w.r.pos_ld + n];
         }
-        cos_sin((uint32_t)(((unsigned long long)(long long)p * phase[j]) >> 32), t.c[i], t.s[i]);
+        cos_sin((unsigned long long)(long long)p * phase[j], t.c[i], t.s[i]);
         if (w.r.inverse) t.s[i] = -t.s[i];
         if (axis < 0) t.c[i] = t.s[i] = NAN;
       }

@@ -219,3 +219,13 @@ def test_far_angles_of_fast_pairs(fovea):
     # the rest of an angle, up to pi / 4, in three roundings (2.4 u); the series' last two
     # steps (1.5 u); the fixed point's 2^-33 and the product's lower part (below u / 16)
     assert float((got - want).abs().max()) <= 4 * U
+
+
+def test_small_angles(fovea):
+    """The sine of a small angle keeps its bits, which a pair with one half zero shows."""
+    w = [1e-6, 3e-5, 1e-8, 1e-10, 7.7e-4, 0.01]
+    got, want = turned(fovea, w, [1, 7, -3, 1000, -12345])
+    # the angle in three roundings, the series in three, the product in one; 2^-64 of a turn
+    # beside the frequency's 1e-10 / 2 pi (2^-30)
+    assert float(((got - want).abs() / want.abs())[1].max()) <= 8 * U
+    assert float((got - want).abs()[0].max()) <= 4 * U
