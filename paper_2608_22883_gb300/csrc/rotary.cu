@@ -61,7 +61,8 @@ struct Work {
   int tokens;                        // of a CTA at a time
 };
 
-// E elements of a row of T.
+// E elements of a row of T.  Plain loads: the outputs may be the inputs' own memory, which the
+// read-only path is not for.
 template <class T, int E>
 struct Chunk {
   uint4 raw[E == 1 ? 1 : E * sizeof(T) / 16];
@@ -70,7 +71,7 @@ struct Chunk {
       *reinterpret_cast<T*>(raw) = *p;
     } else {
 #pragma unroll
-      for (int i = 0; i < (int)(E * sizeof(T) / 16); ++i) raw[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+      for (int i = 0; i < (int)(E * sizeof(T) / 16); ++i) raw[i] = reinterpret_cast<const uint4*>(p)[i];
     }
   }
   template <class C> __device__ __forceinline__ void copy(C* p) const {

@@ -229,3 +229,31 @@ def test_small_angles(fovea):
     # beside the frequency's 1e-10 / 2 pi (2^-30)
     assert float(((got - want).abs() / want.abs())[1].max()) <= 8 * U
     assert float((got - want).abs()[0].max()) <= 4 * U
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("adjacent", [0, 1])
+@pytest.mark.parametrize("n,heads,kv,dim,rot", [(1, 4, 1, 128, 128), (300, 28, 4, 128, 96), (1000, 40, 40, 64, 64), (33, 3, 2, 81, 34)])
+def test_rotated_in_place(fovea, dtype, adjacent, n, heads, kv, dim, rot):
+    """The outputs may be the inputs' own memory (at the C entry)."""
+    g = gen(n)
+    q, k, v = (normal(g, n, h, dim).to(dtype) for h in (heads, kv, kv))
+    f, axis = fovea.rotary_frequencies(rot, [rot // 4, rot // 2 - rot // 4])
+    positions = torch.randint(0, 5000, (2, n), generator=g, **I32)
+    want = fovea.rotary_axes(q, k, positions, f, axis, adjacent=bool(adjacent))
+    kind = fovea.BF16 if dtype is BF16 else fovea.FP32
+    stream = torch.cuda.current_stream().cuda_stream
+    turns = (positions.data_ptr(), n, 2, f.data_ptr(), axis.data_ptr(), rot, adjacent)
+    x, y = q.clone(), k.clone()
+    assert fovea.lib().fovea_rotary_axes(x.data_ptr(), heads * dim, dim, heads, y.data_ptr(), kv * dim, dim, kv, n, dim, kind,
+                                         *turns, 0, x.data_ptr(), y.data_ptr(), stream) == 0
+    assert same(x, want[0]) and same(y, want[1])
+    if dim not in (64, 128):
+        return
+    pages, table = torch.empty(2, n // 16 + 1, kv, 16, dim, dtype=dtype, device="cuda"), torch.arange(n // 16 + 1, **I32)[None]
+    x, sequence, entry = q.clone(), torch.zeros(n, **I32), torch.arange(n, **I32)
+    assert fovea.lib().fovea_cache_append(x.data_ptr(), heads * dim, dim, heads, k.data_ptr(), kv * dim, dim, v.data_ptr(),
+                                          kv * dim, dim, n, kind, *turns, x.data_ptr(), pages[0].data_ptr(),
+                                          pages[1].data_ptr(), kind, None, None, n // 16 + 1, 16, kv, dim, table.data_ptr(),
+                                          1, n // 16 + 1, sequence.data_ptr(), entry.data_ptr(), stream) == 0
+    assert same(x, want[0]) and same(entries(pages[0], table, 0, n), want[1]) and same(entries(pages[1], table, 0, n), v)
