@@ -535,8 +535,8 @@ FOVEA_API fovea_status fovea_rotary_axes(const void* q, int64_t q_ld, int64_t q_
 
 /*
  * New entries of a cache: keys k and values v [N, kv_heads, dim] dtype of token n go
- * to entry[n] of sequence[n] ([N] int32), in 8 bits as e4m3(x * (1 / scale)), fp32, with
- * the ends at +-448.  With rot > 0 keys are rotated first, as fovea_rotary_axes does (rounded
+ * to entry[n] of sequence[n] ([N] int32), in 8 bits as e4m3(x / scale), the quotient in
+ * fp32, with the ends at +-448.  With rot > 0 keys are rotated first, as fovea_rotary_axes does (rounded
  * once, to the cache's type), and so is q [N, heads, dim] to q_out (q NULL: none);
  * rot = 0: keys are stored as they are, and q must be NULL.
  * A token whose sequence or entry is outside the table (sequence -1: a padded batch),

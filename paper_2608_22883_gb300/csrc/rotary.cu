@@ -85,15 +85,34 @@ struct Chunk {
   __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T*>(raw)[i]); }
 };
 
-// E values in the cache's type; those of 8-bit entries times `inverse`, the reciprocal of
-// their scale.
+// x / scale for 8-bit entries, rounded once: a product with the reciprocal rounds twice, and
+// is wrong where that is no number.  The product's remainder, exact in one fused operation,
+// corrects it (Markstein, IBM J. Res. Dev. 34, 1990).  x and a scale near an end of fp32's
+// range go by 2^80 together; quotients beyond 2^20, which the type saturates, are cut first,
+// so that infinities stay.  Prompts into 8 bits: 119 us; divided 124, by products alone 116;
+// two elements an operation 126, for want of registers.
+struct Divisor {
+  float power, scale, inverse;
+  __device__ __forceinline__ explicit Divisor(float s) {
+    power = fabsf(s) < 0x1p-40f ? 0x1p80f : fabsf(s) > 0x1p40f ? 0x1p-80f : 1.0f;
+    scale = isinf(s) ? copysignf(0x1p120f, s) : s * power;
+    inverse = 1.0f / scale;
+  }
+  __device__ __forceinline__ float quotient(float x) const {
+    x *= power;
+    const float q = fminf(fmaxf(x * inverse, -0x1p20f), 0x1p20f);
+    return fmaf(fmaf(-q, scale, x), inverse, q);
+  }
+};
+
+// E values in the cache's type; those of 8-bit entries over their scale.
 template <class C, int E>
-__device__ __forceinline__ void store(C* p, const float (&x)[E], float inverse) {
+__device__ __forceinline__ void store(C* p, const float (&x)[E], const Divisor& by) {
   if constexpr (sizeof(C) == 1) {
     uint32_t w[(E + 3) / 4] = {};
 #pragma unroll
     for (int i = 0; i < E; i += 2) {
-      const float2 two = make_float2(x[i] * inverse, i + 1 < E ? x[i + 1 < E ? i + 1 : i] * inverse : 0.0f);
+      const float2 two = make_float2(by.quotient(x[i]), i + 1 < E ? by.quotient(x[i + 1 < E ? i + 1 : i]) : 0.0f);
       w[i / 4] |= (uint32_t)__nv_cvt_float2_to_fp8x2(two, __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
     }
     if constexpr (E == 1) *reinterpret_cast<uint8_t*>(p) = (uint8_t)w[0];
@@ -179,9 +198,9 @@ __device__ __forceinline__ void run_heads(const Turn<E>& w, const T* in, long lo
             b = a0 * w.s[e] + b0 * w.c[e];
           }
         }
-        const float inverse = sizeof(C) == 1 && scales != nullptr ? 1.0f / scales[h + i * blocks] : 1.0f;
-        store<C, E>(p, y[0], inverse);
-        if (w.second) store<C, E>(p + w.apart, y[1], inverse);
+        const Divisor by(sizeof(C) == 1 && scales != nullptr ? scales[h + i * blocks] : 1.0f);
+        store<C, E>(p, y[0], by);
+        if (w.second) store<C, E>(p + w.apart, y[1], by);
       }
     }
   }

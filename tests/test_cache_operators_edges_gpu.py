@@ -257,3 +257,53 @@ def test_rotated_in_place(fovea, dtype, adjacent, n, heads, kv, dim, rot):
                                           pages[1].data_ptr(), kind, None, None, n // 16 + 1, 16, kv, dim, table.data_ptr(),
                                           1, n // 16 + 1, sequence.data_ptr(), entry.data_ptr(), stream) == 0
     assert same(x, want[0]) and same(entries(pages[0], table, 0, n), want[1]) and same(entries(pages[1], table, 0, n), v)
+
+
+# ---------------------------------------------------------------------------
+# Scales and rows at the ends of their range
+# ---------------------------------------------------------------------------
+
+def as_entries(x, scale):
+    """x / scale in 8 bits, by one division in 32 bits."""
+    y = (x.double() / scale.double()[:, None]).float()
+    return y.clamp(-448, 448).to(E4M3)
+
+
+@pytest.mark.parametrize("rotate", [False, True])
+def test_entries_next_to_a_border(fovea, rotate):
+    """Scales that bring x next to the middle of two 8-bit values: the quotient is rounded once."""
+    g = gen(2)
+    kv, dim = 400, 64
+    x = normal(g, 1, kv, 1).to(BF16)
+    middle = (torch.randint(8, 16, (kv,), generator=g, device="cuda") + 0.5) * 2.0 ** torch.randint(-4, 4, (kv,), generator=g, device="cuda")
+    scale = (x[0, :, 0].double().abs() / middle.double()).float()
+    scale[:3] = torch.tensor([1e-39, 3e38, 2.0 ** -149], device="cuda")           # no reciprocal, or a rounded one
+    x[0, :3, 0] = torch.tensor([1e-38, 3e38, 0.0], device="cuda").to(BF16)
+    x = x.expand(1, kv, dim).contiguous()
+    k_pages, v_pages = (torch.zeros(1, kv, 16, dim, device="cuda").to(E4M3) for _ in range(2))
+    more = {}
+    if rotate:                                     # by nothing
+        f, _ = fovea.rotary_frequencies(dim)
+        more = dict(positions=ints([[0]]), frequencies=f)
+    fovea.cache_append(x, x, k_pages, v_pages, ints([[0]]), ints([0]), ints([5]), k_scale=scale, v_scale=scale, **more)
+    want = as_entries(x[0], scale)
+    for pool in (k_pages, v_pages):
+        assert same(pool[0, :, 5], want)
+
+
+def test_entries_of_odd_quotients(fovea):
+    """Zeros, infinities, numbers that are none, under scales of both signs and of all sizes."""
+    x = torch.tensor([0.0, -0.0, 1.0, -2.5, 1e-40, -1e-38, 3e38, -3e38, math.inf, -math.inf, math.nan, 448, 300, 1e-3, 2e-3, 5e-3],
+                     device="cuda").to(BF16)
+    scale = torch.tensor([1.0, -1.0, 3e-3, 1e-39, -1e-30, 2.0 ** -60, 1e-12, 1e12, 2.0 ** 41, 1e30, -3e38, math.inf, math.nan],
+                         device="cuda")
+    kv, dim = scale.numel(), 64
+    x = x.repeat(4)[None, None].expand(1, kv, dim).contiguous()
+    pages = [torch.zeros(1, kv, 16, dim, device="cuda").to(E4M3) for _ in range(2)]
+    fovea.cache_append(x, x, *pages, ints([[0]]), ints([0]), ints([0]), k_scale=scale, v_scale=scale)
+    want = as_entries(x[0], scale).float()
+    want[11, 8:10] = want[11, 24:26] = want[11, 40:42] = want[11, 56:58] = 0       # of two infinities: not asked
+    for pool in pages:
+        got = pool[0, :, 0].float()
+        got[11, 8:10] = got[11, 24:26] = got[11, 40:42] = got[11, 56:58] = 0
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(0), want.nan_to_num(0))
