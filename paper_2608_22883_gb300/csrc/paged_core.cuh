@@ -317,11 +317,12 @@ __device__ __forceinline__ void write_row(const PagedArgs& a, long long n, int h
     a.lse[n * a.heads + head] = sum == 0.0f ? -INFINITY : (top - lift + log2f(sum)) * kLn2;
 }
 
-// A power of two that takes a row's largest magnitude, `top`, to [1, 2), for fp16; 1 for
-// rows of zeros, subnormals and infinities.
+// A power of two, with a reciprocal, that takes a row's largest magnitude, `top`, to [1, 2), for
+// fp16; that of the very largest to [2, 4), subnormal ones (at least 2^-133) below 1.  1 for
+// infinities.
 __device__ __forceinline__ float row_power(float top) {
   const uint32_t e = __float_as_uint(top) >> 23;
-  return e > 0 && e < 254 ? __uint_as_float(e << 23) : 1.0f;
+  return e == 255 ? 1.0f : __uint_as_float(min(max(e, 1u), 253u) << 23);
 }
 
 // Where row r of a key head's rows stands in q.

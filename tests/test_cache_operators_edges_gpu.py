@@ -307,3 +307,20 @@ def test_entries_of_odd_quotients(fovea):
         got = pool[0, :, 0].float()
         got[11, 8:10] = got[11, 24:26] = got[11, 40:42] = got[11, 56:58] = 0
         assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(0), want.nan_to_num(0))
+
+
+@pytest.mark.parametrize("form", [f for f in FORMS if f[0] is E4M3])
+@pytest.mark.parametrize("power,scale,k_scale", [(127, 2.0 ** -120, 2.0 ** -9), (126, 2.0 ** -120, 2.0 ** -8),
+                                                 (-126, 2.0 ** 26, 2.0 ** 98), (-131, 2.0 ** 26, 2.0 ** 101)])
+def test_rows_at_the_ends_of_their_range(fovea, form, power, scale, k_scale):
+    """Rows of q beside 8-bit keys are brought to fp16's range, from bf16's largest and smallest."""
+    cache, nodes, heads, kv, dim = form
+    g = gen(power + 200)
+    lens = [nodes + 40, nodes + 300]
+    k, v, table, scales = make_cache(g, cache, lens, kv, dim, 16)
+    k.copy_((k.float() / 64).to(E4M3))
+    scales["k_scale"] = torch.full((kv,), k_scale, device="cuda")
+    q = normal(g, 2 * nodes, heads, dim).sign() * (1 + torch.randint(0, 4, (2 * nodes, heads, dim), generator=g, device="cuda") / 4)
+    q = (q.double() * 2.0 ** power).to(BF16)
+    assert bool(torch.isfinite(q).all()) and float((q == 0).float().mean()) < 1e-3
+    check_attention(fovea, q, k, v, table, ints(lens), scale=scale, scales=scales)
