@@ -4,13 +4,14 @@ it fovea_binding.so, the Python module of the drafter's cache.
 Each translation unit under csrc/ is compiled in parallel, then linked into
 ``paper_2608_22883_gb300/_lib/libfovea.so`` (the CUDA ones) and
 ``_lib/fovea_binding.so`` (binding.cpp, with torch's headers and the host
-compiler).  Objects go to ``_build/`` at the repository root.  All of it is
-git-ignored.
+compiler; without a torch with CUDA it is left out).  Objects go to ``_build/`` at the
+repository root.  All of it is git-ignored.
 """
 
 from __future__ import annotations
 
 import concurrent.futures
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -42,13 +43,17 @@ def sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
 
 
-def binding_flags():
-    """(flags to compile binding.cpp, flags to link it) against the torch that is installed."""
-    import torch
-    home = os.path.dirname(torch.__file__)
+def torch_home():
+    """The folder of the torch with CUDA that is installed, None without one (it is not imported)."""
+    spec = importlib.util.find_spec("torch")
+    home = "" if spec is None else os.path.dirname(spec.origin)
+    return home if os.path.exists(os.path.join(home, "lib", "libc10_cuda.so")) else None
+
+
+def binding_flags(home):
+    """(flags to compile binding.cpp, flags to link it) against the torch in this folder."""
     cuda = os.path.dirname(os.path.dirname(nvcc()))
-    compile_flags = ["-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-                     "-I", INCLUDE, "-isystem", os.path.join(home, "include"),
+    compile_flags = ["-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", INCLUDE, "-isystem", os.path.join(home, "include"),
                      "-isystem", os.path.join(home, "include", "torch", "csrc", "api", "include"),
                      "-isystem", os.path.join(cuda, "include"), "-isystem", sysconfig.get_paths()["include"]]
     link_flags = ["-L", LIBDIR, "-lfovea", "-Wl,-rpath,$ORIGIN", "-L", os.path.join(home, "lib"), "-ltorch_python",
@@ -64,8 +69,9 @@ def _newer(out: str, deps) -> bool:
 
 
 def build(verbose: bool = False, force: bool = False, extra_flags=()) -> str:
-    """Compile and link libfovea.so; returns its path.  Rebuilds only what
-    changed (any header change rebuilds every object)."""
+    """Compile and link libfovea.so, and fovea_binding.so where there is a torch;
+    returns the library's path.  Rebuilds only what changed (any header change
+    rebuilds every object)."""
     os.makedirs(BUILD, exist_ok=True)
     os.makedirs(LIBDIR, exist_ok=True)
     cc = nvcc()
@@ -80,12 +86,16 @@ def build(verbose: bool = False, force: bool = False, extra_flags=()) -> str:
         if force or not _newer(obj, [src] + headers):
             jobs.append([cc, *ARCH, *CFLAGS, *extra_flags, "-c", src, "-o", obj])
 
-    compile_flags, link_flags = binding_flags()
-    cxx = os.environ.get("CXX") or shutil.which("g++")
-    source, binding = os.path.join(CSRC, "binding.cpp"), os.path.join(BUILD, "binding.o")
-    if force or not _newer(binding, [source] + headers):
-        # first: it takes as long as the longest of the others
-        jobs.insert(0, [cxx, *compile_flags, "-c", source, "-o", binding])
+    links = [(LIB, objs, [cc, *ARCH, "-shared", "-o", LIB, *objs, "-lpthread", "-ldl", "-lrt"])]
+    home = torch_home()
+    if home is not None:
+        compile_flags, link_flags = binding_flags(home)
+        cxx = os.environ.get("CXX") or shutil.which("g++")
+        source, binding = os.path.join(CSRC, "binding.cpp"), os.path.join(BUILD, "binding.o")
+        if force or not _newer(binding, [source] + headers):
+            # first: it takes as long as the longest of the others
+            jobs.insert(0, [cxx, *compile_flags, "-c", source, "-o", binding])
+        links.append((BINDING, [binding, LIB], [cxx, "-shared", "-o", BINDING, binding, *link_flags]))
 
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
@@ -98,8 +108,7 @@ def build(verbose: bool = False, force: bool = False, extra_flags=()) -> str:
                     sys.stderr.write(" ".join(cmd) + "\n" + r.stdout + r.stderr)
                 if r.returncode != 0:
                     raise RuntimeError(f"{os.path.basename(cmd[0])} failed on {cmd[-3]}")
-    for out, parts, cmd in ((LIB, objs, [cc, *ARCH, "-shared", "-o", LIB, *objs, "-lpthread", "-ldl", "-lrt"]),
-                            (BINDING, [binding, LIB], [cxx, "-shared", "-o", BINDING, binding, *link_flags])):
+    for out, parts, cmd in links:
         if not force and not jobs and _newer(out, parts):
             continue
         _, r = run(cmd)

@@ -1,0 +1,50 @@
+"""What the build asks of the machine, with the compilers' commands recorded and not run."""
+
+import os
+import subprocess
+import sys
+
+import pytest
+
+from paper_2608_22883_gb300 import _build
+
+
+@pytest.fixture
+def made(tmp_path, monkeypatch):
+    """build() into an empty folder: the commands that it runs, each of which makes its output."""
+    for name, path in (("BUILD", "b"), ("LIBDIR", "l"), ("LIB", "l/libfovea.so"), ("BINDING", "l/fovea_binding.so")):
+        monkeypatch.setattr(_build, name, str(tmp_path / path))
+    commands = []
+
+    def run(cmd, **kw):
+        assert all(isinstance(word, str) for word in cmd), cmd
+        commands.append(cmd)
+        with open(cmd[cmd.index("-o") + 1], "w") as f:
+            f.write("x")
+        return subprocess.CompletedProcess(cmd, 0, "", "")
+
+    monkeypatch.setattr(_build.subprocess, "run", run)
+    return commands
+
+
+def outputs(commands):
+    names = [os.path.basename(cmd[cmd.index("-o") + 1]) for cmd in commands]
+    commands.clear()
+    return names
+
+
+def test_everything_is_made_once(made):
+    _build.build()
+    first = outputs(made)
+    assert {"binding.o", "libfovea.so", "fovea_binding.so"} < set(first) and len(first) == len(_build.sources()) + 3
+    _build.build()
+    assert outputs(made) == []
+
+
+def test_the_library_needs_no_torch(made, monkeypatch):
+    """libfovea is for C programs too: without torch it is made, and the Python module is not."""
+    monkeypatch.setitem(sys.modules, "torch", None)
+    assert _build.build() == _build.LIB and os.path.exists(_build.LIB)
+    names = outputs(made)
+    assert "libfovea.so" in names and len(names) == len(_build.sources()) + 1
+    assert not os.path.exists(_build.BINDING)
