@@ -39,6 +39,13 @@ def nvcc() -> str:
     raise RuntimeError("nvcc not found: the CUDA toolkit is required to build libfovea")
 
 
+def cxx() -> str:
+    found = os.environ.get("CXX") or shutil.which("g++")
+    if not found:
+        raise RuntimeError("no host compiler: set CXX, or put g++ on the path")
+    return found
+
+
 def sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
 
@@ -90,12 +97,12 @@ def build(verbose: bool = False, force: bool = False, extra_flags=()) -> str:
     home = torch_home()
     if home is not None:
         compile_flags, link_flags = binding_flags(home)
-        cxx = os.environ.get("CXX") or shutil.which("g++")
+        host = cxx()
         source, binding = os.path.join(CSRC, "binding.cpp"), os.path.join(BUILD, "binding.o")
         if force or not _newer(binding, [source] + headers):
             # first: it takes as long as the longest of the others
-            jobs.insert(0, [cxx, *compile_flags, "-c", source, "-o", binding])
-        links.append((BINDING, [binding, LIB], [cxx, "-shared", "-o", BINDING, binding, *link_flags]))
+            jobs.insert(0, [host, *compile_flags, "-c", source, "-o", binding])
+        links.append((BINDING, [binding, LIB], [host, "-shared", "-o", BINDING, binding, *link_flags]))
 
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)

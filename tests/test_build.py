@@ -48,3 +48,15 @@ def test_the_library_needs_no_torch(made, monkeypatch):
     names = outputs(made)
     assert "libfovea.so" in names and len(names) == len(_build.sources()) + 1
     assert not os.path.exists(_build.BINDING)
+
+
+def test_a_missing_compiler_is_named(made, monkeypatch):
+    monkeypatch.delenv("CXX", raising=False)
+    which = _build.shutil.which
+    monkeypatch.setattr(_build.shutil, "which", lambda name: None if name == "g++" else which(name))
+    with pytest.raises(RuntimeError, match="g\\+\\+"):
+        _build.build()
+    assert outputs(made) == []
+    monkeypatch.setenv("CXX", "some-c++")
+    _build.build()
+    assert sum(cmd[0] == "some-c++" for cmd in made) == 2
