@@ -75,6 +75,13 @@ def _newer(out: str, deps) -> bool:
     return all(os.path.getmtime(d) <= t for d in deps)
 
 
+def _read(path: str):
+    if not os.path.exists(path):
+        return None
+    with open(path) as f:
+        return f.read()
+
+
 def build(verbose: bool = False, force: bool = False, extra_flags=()) -> str:
     """Compile and link libfovea.so, and fovea_binding.so where there is a torch;
     returns the library's path.  Rebuilds only what changed (any header change
@@ -93,15 +100,21 @@ def build(verbose: bool = False, force: bool = False, extra_flags=()) -> str:
         if force or not _newer(obj, [src] + headers):
             jobs.append([cc, *ARCH, *CFLAGS, *extra_flags, "-c", src, "-o", obj])
 
+    note, made_with = os.path.join(BUILD, "binding.txt"), None
     links = [(LIB, objs, [cc, *ARCH, "-shared", "-o", LIB, *objs, "-lpthread", "-ldl", "-lrt"])]
     home = torch_home()
     if home is not None:
         compile_flags, link_flags = binding_flags(home)
         host = cxx()
         source, binding = os.path.join(CSRC, "binding.cpp"), os.path.join(BUILD, "binding.o")
-        if force or not _newer(binding, [source] + headers):
-            # first: it takes as long as the longest of the others
-            jobs.insert(0, [host, *compile_flags, "-c", source, "-o", binding])
+        cmd = [host, *compile_flags, "-c", source, "-o", binding]
+        # made with this command against this torch: another one's objects do not go with its libraries
+        with open(os.path.join(home, "version.py")) as f:
+            made_with = " ".join(cmd) + "\n" + f.read()
+        if force or _read(note) != made_with or not _newer(binding, [source] + headers):
+            if os.path.exists(note):
+                os.remove(note)
+            jobs.insert(0, cmd)      # first: it takes as long as the longest of the others
         links.append((BINDING, [binding, LIB], [host, "-shared", "-o", BINDING, binding, *link_flags]))
 
     def run(cmd):
@@ -115,6 +128,9 @@ def build(verbose: bool = False, force: bool = False, extra_flags=()) -> str:
                     sys.stderr.write(" ".join(cmd) + "\n" + r.stdout + r.stderr)
                 if r.returncode != 0:
                     raise RuntimeError(f"{os.path.basename(cmd[0])} failed on {cmd[-3]}")
+    if made_with is not None and _read(note) != made_with:
+        with open(note, "w") as f:
+            f.write(made_with)
     for out, parts, cmd in links:
         if not force and not jobs and _newer(out, parts):
             continue

@@ -60,3 +60,29 @@ def test_a_missing_compiler_is_named(made, monkeypatch):
     monkeypatch.setenv("CXX", "some-c++")
     _build.build()
     assert sum(cmd[0] == "some-c++" for cmd in made) == 2
+
+
+def test_another_torch_makes_the_module_again(made, monkeypatch, tmp_path):
+    """The module goes with the torch that it was compiled against, whatever the files' times."""
+    homes = []
+    for version in ("1", "2"):
+        home = tmp_path / version
+        home.mkdir()
+        (home / "version.py").write_text(f"__version__ = '{version}'")
+        os.utime(home / "version.py", (1, 1))
+        homes.append(str(home))
+    monkeypatch.setattr(_build, "torch_home", lambda: homes[0])
+    _build.build()
+    outputs(made)
+    _build.build()
+    assert outputs(made) == []
+    monkeypatch.setattr(_build, "torch_home", lambda: homes[1])
+    _build.build()
+    assert {"binding.o", "fovea_binding.so"} <= set(outputs(made))
+    with open(os.path.join(homes[1], "version.py"), "w") as f:      # replaced in its place
+        f.write("__version__ = '3'")
+    os.utime(os.path.join(homes[1], "version.py"), (1, 1))
+    _build.build()
+    assert {"binding.o", "fovea_binding.so"} <= set(outputs(made))
+    _build.build()
+    assert outputs(made) == []
