@@ -526,8 +526,9 @@ struct PagedArgs {
 };
 size_t paged_attention_workspace(const PagedArgs& a);
 cudaError_t launch_paged_attention(const PagedArgs& a, cudaStream_t s);
-// The same for many rows a key head, bf16 and e4m3 caches (paged_rows.cu; paged_tree.cu on
-// tcgen05); workspace not null: its bytes instead.
+// The same for many rows a key head: heads of 256 dims, bf16 and e4m3, and narrower ones of
+// e4m3 (paged_rows.cu); bf16 and e4m3 heads of 64 and 128 on tcgen05 (paged_tree.cu).
+// workspace not null: its bytes instead.
 cudaError_t launch_paged_rows(const PagedArgs& a, cudaStream_t s, size_t* workspace);
 cudaError_t launch_paged_tree(const PagedArgs& a, cudaStream_t s, size_t* workspace);
 

@@ -801,10 +801,8 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_cluster_ke
 // third, of 32 rows and 32 key heads 46.4 and 39.5; e4m3, 24 rows 35.9 and 47.5, 64 rows 103
 // and 105.
 constexpr int kManyRows = 16, kWideRows = 64;
-// Rows that a warp takes together, by 8: as many as there are, up to what its registers hold.
-template <class C, int D> constexpr int most_tiles() {
-  return sizeof(C) == 4 || D == 256 ? 1 : D == 128 ? 2 : 4;
-}
+// Whether a warp takes 9 to 16 rows together: where its registers hold them.
+template <class C, int D> constexpr bool kTwoTiles = sizeof(C) < 4 && D < 256;
 
 // CTAs a segment for a cluster of them each, or 0: few segments, of a table that leaves a
 // warp few steps, since a cluster whose sequence is shorter than its table idles.  One
@@ -859,9 +857,7 @@ cudaError_t launch_dim(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
   const int rows = a.nodes * a.group;
   if (sizeof(C) < 4 && D < 256 && rows > (sizeof(C) == 2 ? kManyRows : kWideRows)) return launch_paged_tree(a, s, workspace);
   if (sizeof(C) < 4 && rows > kManyRows) return launch_paged_rows(a, s, workspace);
-  if constexpr (most_tiles<C, D>() >= 4)
-    if (rows > 16) return launch_as<C, Q, D, 4>(a, s, workspace);
-  if constexpr (most_tiles<C, D>() >= 2)
+  if constexpr (kTwoTiles<C, D>)
     if (rows > 8) return launch_as<C, Q, D, 2>(a, s, workspace);
   if constexpr (sizeof(C) == 1)
     if (rows <= 4) return launch_as<C, Q, D, 1, true>(a, s, workspace);

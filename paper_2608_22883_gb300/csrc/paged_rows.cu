@@ -419,16 +419,14 @@ template <class C, int D> cudaError_t launch_as(const PagedArgs& a, cudaStream_t
   return launch_runs<A, C, __nv_bfloat16, D>(a, paged_rows_kernel<C, D>, kThreads, sizeof(typename A::Shared),
                                              152 * rows_per_sm<C, D>, s, workspace, raised);
 }
-template <class C> cudaError_t launch_type(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
-  return a.dim == 64 ? launch_as<C, 64>(a, s, workspace)
-       : a.dim == 128 ? launch_as<C, 128>(a, s, workspace) : launch_as<C, 256>(a, s, workspace);
-}
 
 }  // namespace
 
 cudaError_t launch_paged_rows(const PagedArgs& a, cudaStream_t s, size_t* workspace) {
-  return a.cache_dtype == FOVEA_BF16 ? launch_type<__nv_bfloat16>(a, s, workspace)
-                                     : launch_type<__nv_fp8_e4m3>(a, s, workspace);
+  if (a.cache_dtype == FOVEA_BF16) return launch_as<__nv_bfloat16, 256>(a, s, workspace);
+  return a.dim == 64    ? launch_as<__nv_fp8_e4m3, 64>(a, s, workspace)
+         : a.dim == 128 ? launch_as<__nv_fp8_e4m3, 128>(a, s, workspace)
+                        : launch_as<__nv_fp8_e4m3, 256>(a, s, workspace);
 }
 
 }  // namespace fovea
