@@ -576,8 +576,8 @@ FOVEA_API fovea_status fovea_cache_append(const void* q, int64_t q_ld, int64_t q
  * both signs: NaN).
  * A row that sees nothing (or only scores of -inf) has out 0 and lse -inf.  Where a page
  * that a row needs is outside the pool, or lens[b] beyond the table, the row is NaN.
- * Softmax and sums are fp32: p is held to 16 bits beside bf16 values, to 22 beside e4m3,
- * fp32 in full; out is rounded once.  The order of the sums depends on the sizes alone.
+ * Softmax and sums are fp32: p is held to 16 bits beside bf16 values, to 22 beside e4m3; the
+ * products of an fp32 cache are right to 2^-19; out is rounded once.  The order of the sums depends on the sizes alone.
  * 1 <= nodes <= FOVEA_MAX_TREE; kv_heads divides heads; scale finite.
  */
 FOVEA_API fovea_status fovea_paged_attention(const void* q, int64_t q_ld, int64_t q_hs, int heads,

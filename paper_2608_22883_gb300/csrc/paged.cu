@@ -48,7 +48,10 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], 
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 // x as the sum of two tf32 values: hi its upper 11 bits, lo the other 13, of which the
-// product reads 11 (an error of 2^-21 of x at most).
+// product reads 11 (an error of 2^-21 of x at most).  The product of two lower parts, 2^-20 at
+// most, is left out: a product is right to 2^-19.  Upper parts that are rounded to nearest
+// bring it to 2^-21, for two more instructions an element: 8 sequences of 2048 37 us instead
+// of 34, heads of 256 79 instead of 69, 64 rows over 4 heads 132 instead of 115.
 __device__ __forceinline__ void split_tf32(uint32_t x, uint32_t& hi, uint32_t& lo) {
   const bool finite = (x << 1) < 0xFF000000u;
   hi = finite ? x & 0xFFFFE000u : x;
@@ -797,9 +800,9 @@ __global__ void __launch_bounds__(kThreads, per_sm<C, D, RT>()) paged_cluster_ke
 // More rows of a key head than kManyRows go to the kernels of many rows: that on tcgen05
 // where the dims and the types allow it, 8-bit entries, which it has to widen on the way,
 // only from more than kWideRows rows on.  us, here / mma.sync on staged tiles / tcgen05:
-// bf16, 8 trees of 14 rows 12.7 / 23.5 / 17.7, of 28 rows 24.7 on the second and 19.4 on the
-// third, of 32 rows and 32 key heads 46.4 and 39.5; e4m3, 24 rows 35.9 and 47.5, 64 rows 103
-// and 105.
+// bf16, 8 trees of 14 rows 12.7 / 23.5 / 17.7, of 28 rows 24.7 on the second and 19.2 on the
+// third, of 32 rows and 32 key heads 46.4 and 39.5; e4m3, 24 rows 40.4 and 50.3, 64 rows 52.1
+// and 58.6, 100 rows 85.8 and 77.0.
 constexpr int kManyRows = 16, kWideRows = 64;
 // Whether a warp takes 9 to 16 rows together: where its registers hold them.
 template <class C, int D> constexpr bool kTwoTiles = sizeof(C) < 4 && D < 256;

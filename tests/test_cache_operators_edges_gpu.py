@@ -324,3 +324,28 @@ def test_rows_at_the_ends_of_their_range(fovea, form, power, scale, k_scale):
     q = (q.double() * 2.0 ** power).to(BF16)
     assert bool(torch.isfinite(q).all()) and float((q == 0).float().mean()) < 1e-3
     check_attention(fovea, q, k, v, table, ints(lens), scale=scale, scales=scales)
+
+
+# ---------------------------------------------------------------------------
+# Products of an fp32 cache
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_bits_of_fp32_products(fovea, dim):
+    """One entry a sequence: the score is one product, the output its value."""
+    g = gen(dim)
+    B, kv = 500, 8
+    k_pages, v_pages = (torch.zeros(B, kv, 16, dim, device="cuda") for _ in range(2))
+    k, v, q = (normal(g, B, kv, n).exp() for n in (1, dim, 1))
+    v[0, 0, :2] = torch.tensor([3.4028e38, -3.4028e38], device="cuda")             # rounded up, they would be infinite
+    k_pages[:, :, 0, :1], v_pages[:, :, 0] = k, v
+    rows = torch.zeros(B, kv, dim, device="cuda")
+    rows[..., :1] = q
+    got = fovea.paged_attention(rows, k_pages, v_pages, torch.arange(B, **I32)[:, None].contiguous(), torch.ones(B, **I32),
+                                scale=1.0, want_lse=True)
+    # a factor is its upper 11 bits and 11 of the others, off by 2^-21; the product of both
+    # lower parts (2^-10 each) is left out: 2 * 2^-21 + 2^-20; sums that truncate to 2^-23 (two),
+    # roundings of the score by log2 e, of the factor and of the way back (four).  p is 1, exactly.
+    want = q.double()[..., 0] * k.double()[..., 0]
+    within(got["lse"], want, want * (2.0 ** -19 + 2 * 2.0 ** -23 + 4 * U), "score")
+    within(got["out"], v.double(), v.double().abs() * (2.0 ** -21 + 2 * 2.0 ** -23 + U), "value")
