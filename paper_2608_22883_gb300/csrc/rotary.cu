@@ -101,7 +101,7 @@ struct Divisor {
   __device__ __forceinline__ float quotient(float x) const {
     x *= power;
     const float q = fminf(fmaxf(x * inverse, -0x1p20f), 0x1p20f);
-    return fmaf(fmaf(-q, scale, x), inverse, q);
+    return fmaf(fmaf(q, scale, -x), -inverse, q);        // so that zeros keep their sign
   }
 };
 

@@ -349,3 +349,14 @@ def test_bits_of_fp32_products(fovea, dim):
     want = q.double()[..., 0] * k.double()[..., 0]
     within(got["lse"], want, want * (2.0 ** -19 + 2 * 2.0 ** -23 + 4 * U), "score")
     within(got["out"], v.double(), v.double().abs() * (2.0 ** -21 + 2 * 2.0 ** -23 + U), "value")
+
+
+def test_stored_zeros_keep_their_sign(fovea):
+    x = torch.tensor([0.0, -0.0, -1e-30, 1e-30], device="cuda").to(BF16).repeat(16)[None, None]
+    pages = [torch.ones(1, 1, 16, 64, device="cuda").to(E4M3) for _ in range(2)]
+    for s in (0.3, 1e-45, 1e20):
+        scale = torch.tensor([s], device="cuda")
+        fovea.cache_append(x, x, *pages, ints([[0]]), ints([0]), ints([0]), k_scale=scale, v_scale=scale)
+        for pool in pages:
+            assert pool[0, 0, 0].view(torch.uint8)[:2].tolist() == [0, 128]
+            assert same(pool[0, :, 0], as_entries(x[0], scale))
