@@ -497,7 +497,7 @@ FOVEA_API fovea_status fovea_token_logprobs_grad(const void* logits, int64_t ld,
  * Rows of q, k and v are [N, heads, dim] with a stride of tokens `ld` and of heads
  * `hs` in elements (a row itself is contiguous), aligned to their element.
  * None of these calls allocates or synchronises; all enqueue on `stream` and can
- * be captured.  N = 0 or B = 0 is valid and does nothing (fovea_cache_fork counts its
+ * be captured.  Outputs do not overlap inputs, but where a call says so.  N = 0 or B = 0 is valid and does nothing (fovea_cache_fork counts its
  * free pages all the same).
  * Errors: INVALID_ARG, UNSUPPORTED (nothing enqueued), CUDA.
  */
@@ -573,7 +573,8 @@ FOVEA_API fovea_status fovea_cache_append(const void* q, int64_t q_ld, int64_t q
  *         where there is none).  A bounded device wait that gives up leaves NaN in the rows
  *         that it did not reach and FOVEA_ERR_TIMEOUT for fovea_sync_errors(workspace).
  * A value that is infinite or NaN makes its dim so in every row that sees it (infinities of
- * both signs: NaN).
+ * both signs: NaN).  Finite ones are added up before they are divided by the sum of e^s, in
+ * fp32: those of 2^96 and more may pass its range.
  * A row that sees nothing (or only scores of -inf) has out 0 and lse -inf.  Where a page
  * that a row needs is outside the pool, or lens[b] beyond the table, the row is NaN.
  * Softmax and sums are fp32: p is held to 16 bits beside bf16 values, to 22 beside e4m3; the
@@ -601,7 +602,9 @@ FOVEA_API fovea_status fovea_paged_attention_workspace_size(int B, int nodes, in
  *   new_lens[b] = lens[b] - size + their number.
  * All are read before any is written.  A sequence of fewer than `size` entries is left as
  * it is, its length too; entries whose page is outside the pool are not moved.  Places
- * that no entry moves to are left as they were.  1 <= path <= size <= FOVEA_MAX_TREE.
+ * that no entry moves to are left as they were.  A page whose entries move belongs to one
+ * sequence of the call alone (of two, either may be stored, or a mixture).
+ * 1 <= path <= size <= FOVEA_MAX_TREE.
  * new_lens is not lens' own memory.
  */
 FOVEA_API fovea_status fovea_cache_keep(void* k_pages, void* v_pages, int cache_dtype, int n_pages,

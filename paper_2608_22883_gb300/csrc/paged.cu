@@ -77,7 +77,7 @@ template <class C, int D> struct Cut {
 template <class C, int D, int RT> constexpr int kTogether = sizeof(C) * D * RT <= 128 ? 2 : 1;
 
 // Whether a step's pages are asked for a step ahead: with 8-bit entries (four sequences of
-// 131072: 168 us without, 162 with) and bf16 of 256 dims (49.7 and 46.2); it costs the
+// 131072: 179 us without, 155 with) and bf16 of 256 dims (49.7 and 46.2); it costs the
 // others (one sequence of 4096 10.3 and 11.5, fp32 of 128 dims 33 and 39, of 256 68.7 and 71.6).
 template <class C, int D> constexpr bool kAsks = sizeof(C) == 1 || (sizeof(C) == 2 && D == 256);
 
@@ -90,7 +90,7 @@ template <class C, int D> constexpr bool kTakesTurns = sizeof(C) * D > 512;
 
 // FOLD: at most four rows, over 8-bit entries.  They stand twice among the eight of a
 // product, the second time for p's lower halves: one product does for both (four sequences
-// of 131072: 158 us; with two products 169, with p to 11 bits 157).
+// of 131072: 155 us; with two products 169, with p to 11 bits 157).
 template <class C, class Q, int D, int RT, bool FOLD = false>
 struct Attention {
   using G = Cut<C, D>;
@@ -98,8 +98,8 @@ struct Attention {
   static constexpr bool kF32 = sizeof(C) == 4, kE4 = sizeof(C) == 1;
   static constexpr bool kWaits = false;
   static constexpr int kRows = 8 * RT, kBlock = 16, kLeast = kWarps;
-  // 64 sequences of 0 to 8192 entries with 0 / 8 / 16 / 24 blocks in front of a segment: 83 /
-  // 36 / 31 / 32 us
+  // 64 sequences of 0 to 8192 entries with 0 / 8 / 16 / 24 blocks in front of a segment: 85 /
+  // 37 / 31 / 31 us
   static constexpr uint32_t kFront = RT == 1 ? 16 : 24;
   static constexpr int kSlot = kRows * (D + 2);                  // floats of a partial segment
   static constexpr uint32_t kBytes = kBlock * D * sizeof(C);     // of a block
@@ -809,7 +809,7 @@ template <class C, int D> constexpr bool kTwoTiles = sizeof(C) < 4 && D < 256;
 
 // CTAs a segment for a cluster of them each, or 0: few segments, of a table that leaves a
 // warp few steps, since a cluster whose sequence is shorter than its table idles.  One
-// sequence of 640 entries, 32 heads: 9.0 us and one launch (7.4 us on the host), 8.8 and
+// sequence of 640 entries, 32 heads: 7.4 us and one launch (7.4 us on the host), 9.5 and
 // two (9.7) in runs; 4096 entries, 8 key heads: 12.2 and 15.3.  16 sequences of 1 to 4096
 // entries: 25 and 17; 8 of 2048, 32 key heads: 55 and 44.
 template <class A> int cluster_ctas(const PagedArgs& a, int resident) {

@@ -191,7 +191,7 @@ __device__ __forceinline__ bool sees(const PagedArgs& a, const uint32_t* tree, i
   if (tree == nullptr) return j <= node;
   return (tree[(size_t)node * a.words + (j >> 5)] >> (j & 31)) & 1u;
 }
-  // The word of bits that tells which of the newest entries 32 w, 32 w + 1, ... row `node` sees
+// The word of bits that tells which of the newest entries 32 w, 32 w + 1, ... row `node` sees
 // (all before the newest, w < 0).
 __device__ __forceinline__ uint32_t seen_word(const PagedArgs& a, const uint32_t* tree, int node, int w) {
   if (w < 0) return 0xFFFFFFFFu;

@@ -7,7 +7,7 @@
 // chunks, swizzled by row, so that ldmatrix reads without conflicts).  A warp keeps its rows
 // of Q and of O in registers; S = Q K^T of a tile stays there too and becomes the operand of
 // P V in place.  A warp has all entries of its rows: nothing is joined within the CTA.
-// Eight trees of 6 nodes over 3000 e4m3 entries, 24 rows a key head: 36 us (floor 6.4), bound
+// Eight trees of 6 nodes over 3000 e4m3 entries, 24 rows a key head: 40 us (floor 6.4), bound
 // by the latencies of a run's few tiles; 16 sequences of 4096 bf16 entries of 256 dims, 16
 // heads over 4: 46 us (floor 34).
 #include <atomic>
@@ -31,7 +31,7 @@ template <class C, int D> struct Rows {
   static constexpr bool kE4 = sizeof(C) == 1, kWaits = false;
   static constexpr float kLift = kE4 ? 15.0f : 0.0f;             // as in paged.cu
   static constexpr int kRows = 16 * kWarps, kTile = D == 256 ? 32 : 64, kBlock = kTile, kLeast = 1;
-  static constexpr uint32_t kFront = 2;                          // tiles: 1 / 2 / 4 / 8: 36 / 36 / 38 / 38 us (24 rows)
+  static constexpr uint32_t kFront = 2;                          // tiles: 1 / 2 / 4 / 8: 40 / 40 / 44 / 43 us (24 rows)
   static constexpr int kSlot = kRows * (D + 2);
   static constexpr int kRowBytes = D * sizeof(C), kChunks = kRowBytes / 16;
   static constexpr int kTileBytes = kTile * kRowBytes;

@@ -12,7 +12,7 @@
 // formed while P of the one before is made (two places in tensor memory), and two CTAs an
 // SM fill one another's waits.
 //
-// Measured: eight trees of 32 nodes over 32 to 2912 entries, 28 heads over 4: 26 us; 16 of 64 nodes, 40 key heads, 480 to 640 entries: 84 us (floor
+// Measured: eight trees of 32 nodes over 32 to 2912 entries, 28 heads over 4: 26 us; 16 of 64 nodes, 40 key heads, 480 to 640 entries: 86 us (floor
 // 30).  What bounds it is a tile's chain, most of it the 64 exponentials and twice as many
 // conversions of a row in one thread (1 to 2 us by time stamps, 27 % of the issue slots used),
 // and per run the first tile's and the last products' latencies (about 3 us each).
@@ -83,7 +83,7 @@ __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.
 template <class C, int D> struct Tree {
   static constexpr bool kE4 = sizeof(C) == 1, kWaits = true;
   static constexpr float kLift = kE4 ? 7.0f : 0.0f;              // p 2^7 2^8 fits fp16
-  // runs of three tiles at least: one tree of 64 nodes over 704 entries 16.5 us, with one 22
+  // runs of three tiles at least: one tree of 64 nodes over 704 entries 17 us, with one 23
   static constexpr int kRows = 128, kBlock = 64, kLeast = 3;
   static constexpr uint32_t kFront = 2;
   static constexpr int kSlot = kRows * (D + 2);                  // a multiple of 8 floats

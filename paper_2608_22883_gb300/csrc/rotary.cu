@@ -14,8 +14,10 @@
 // eight pairs of a token and applies them to up to sixteen heads, so that their cost is
 // shared; its two chunks of eight elements of a head are the pairs' two halves.  Measured:
 // image prompts (23040 bf16 tokens, 28 + 4 heads of 128, three axes) 62 us, 6.1 TB/s; the
-// gradient of 9216 fp32 tokens of 80 heads 120 us, 6.3 TB/s; prompts into an 8-bit cache
-// (32768 rows, 20480 of them stored, 32 + 8 heads) 115 us, 5.8 TB/s.
+// gradient of 9216 fp32 tokens of 80 heads 121 us, 6.2 TB/s; prompts into an 8-bit cache
+// (32768 rows, 20480 of them stored, 32 + 8 heads) 119 us, 5.6 TB/s.  Rows off 16 bytes, and
+// heads or rotated dims that are no multiples of 16, go one element a thread: heads of 72 take
+// 176 us (floor 31), 24 rotated dims of 128 198 (56).
 #include <cuda_fp8.h>
 
 #include <atomic>
